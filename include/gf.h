@@ -20,13 +20,15 @@
  *     are caller-allocated and caller-owned, and must outlive the handle.
  *   - `stream` is a cudaStream_t passed as void* (NULL = default stream).
  *     gf_node_kv_write, gf_node_kv_read, gf_node_kv_reconstruct,
+ *     gf_node_kv4_write, gf_path_attention_weights, gf_node_kv_evict,
  *     gf_residual_encode, gf_transition_counts, gf_select_transitions,
  *     gf_path_attention_decode and gf_path_attention_extend only enqueue work.  gf_build_path_tables enqueues its kernels and then
  *     waits on the stream once, to read back four table sizes and the
  *     validation result.
  *   - Argument errors are detected on the host before anything is launched.
  *   - One handle is used from one host thread at a time.
- *   - bf16 everywhere for K, V, Q and the output; accumulation is fp32.
+ *   - bf16 everywhere for K, V, Q and the output (a node's state may be held in 4 bits instead, see
+ *     gf_node_kv4_write); accumulation is fp32.
  */
 #ifndef GF_H_
 #define GF_H_
@@ -171,12 +173,81 @@ gf_status_t gf_node_kv_release(gf_wgraph_t* g, int32_t node, void* stream);
  * Either pointer may be NULL.  GF_ERR_NOT_WRITTEN for a node without an extent. */
 gf_status_t gf_node_extent(const gf_wgraph_t* g, int32_t node, int32_t* n_tokens_host, int32_t* token_offset_host);
 
+/* ---- states held in 4 bits ------------------------------------------------------------------------
+ * A node's state may be held in 4 bits instead of bf16: 64 neighbouring entries of one token and KV head
+ * form a group with two bf16 numbers, lo (its least entry) and s (hi / 16 - lo / 16 in fp32, rounded to bf16); an
+ * entry x has the code floor((x - lo) / s) within 0..15 (0 where s is 0) and stands for
+ * lo + s (code + 1/2), the middle of its cell, or lo where s is 0.  4.5 bits per entry; a normal group is
+ * off by about 0.09 of its standard deviation (root mean square).  Inputs are finite.
+ * Such states live in a pool of their own, and paths name them like any other: one batch may mix both
+ * kinds, shared as usual.  gf_path_attention_decode (and _static) computes with the values that the codes
+ * stand for, without rounding them to bf16 first.  Extend mode takes no path through such a node
+ * (GF_ERR_INVALID_PATH: read it back and write it to a bf16 node for that), and it cannot be the base of a
+ * residual or of a reconstruction (GF_ERR_INVALID_ARG). */
+
+/* Bytes of the 4-bit pool one 64-token tile of one KV head occupies (9216 for head_dim 128). */
+uint64_t gf_kv4_bytes_per_tile(int32_t head_dim);
+
+/* Gives the handle the memory for its 4-bit states: caller-allocated, caller-owned, 1024-byte aligned, must
+ * outlive the handle; holds floor(bytes / gf_kv4_bytes_per_tile / num_kv_heads / num_layers) tiles, handed
+ * out first fit like the bf16 pool's.  May be called again as long as no node is held in 4 bits
+ * (GF_ERR_INVALID_ARG otherwise).  GF_ERR_CAPACITY when not one tile fits, or when the token slots of
+ * both pools (64 per tile) would pass 2^31. */
+gf_status_t gf_kv4_pool_attach(gf_wgraph_t* g, void* kv4_pool_dev, uint64_t kv4_pool_bytes);
+
+/* gf_node_kv_write into 4 bits: same arguments, same rules (the first write of a node, any layer, fixes its
+ * length and reserves its extent; later ones pass the same n_tokens; a node held in bf16 is refused with
+ * GF_ERR_INVALID_ARG, and so is gf_node_kv_write of a node held in 4 bits: release it first).
+ * gf_node_kv_read gives the values back, rounded to bf16; gf_node_kv_release frees the tiles.
+ * GF_ERR_CAPACITY when no pool is attached or it is full.  Enqueued on `stream`. */
+gf_status_t gf_node_kv4_write(gf_wgraph_t* g, int32_t node, int32_t layer, const void* k_dev, const void* v_dev,
+                              int32_t n_tokens, void* stream);
+
+/* ---- eviction by accumulated attention weight --------------------------------------------------------
+ * Every token of a pool has a slot: its offset in the bf16 pool, or the bf16 pool's capacity in tokens
+ * plus its offset in the 4-bit pool; a node's tokens have consecutive slots from the offset that
+ * gf_node_extent reports.  gf_weight_slots: how many there are, 64 * (tiles of both pools); it grows
+ * with gf_kv4_pool_attach.  The weights are the caller's array, fp32 [num_layers, num_kv_heads, slots]. */
+int64_t gf_weight_slots(const gf_wgraph_t* g);
+
+/* What share of the attention of one decode step every resident token received, one layer:
+ *   weight[kvh][slot of t] = sum over the requests whose path holds t's node and the query heads h of KV
+ *                            head kvh of exp(scale * q_rh . k_t - lse_rh)
+ * q_dev and lse_dev are those of the step's gf_path_attention_decode with the same tables.  accumulate 1
+ * adds the sum to what weights_dev holds, 0 replaces it (a node's first step); slots of tokens that are
+ * on no path of the batch are left as they are, and so are those of nodes kept as base + residual, which
+ * have no tiles of their own.  Sums run in a fixed order: equal inputs give equal bits.  weights_dev is the
+ * whole array, 4-byte aligned; only `layer`'s part is touched.  Asynchronous. */
+gf_status_t gf_path_attention_weights(gf_wgraph_t* g, const gf_tables_t* t, int32_t layer, const void* q_dev,
+                                      const float* lse_dev, int32_t accumulate, float* weights_dev, void* stream);
+
+typedef struct {
+  int32_t node;        /* receives the kept tokens: unwritten, or of this length and kind already   */
+  int32_t src_node;    /* the state that is cut down; itself unchanged (gf_node_kv_release frees it) */
+  int32_t keep;        /* tokens to keep; all of them when the node has no more                     */
+  int32_t keep_first;  /* this many first and last tokens are kept whatever their weight;           */
+  int32_t keep_last;   /*   keep_first + keep_last <= keep                                          */
+} gf_evict_t;
+
+/* Cuts nodes down to their heaviest tokens.  For every entry of list_host, in every layer and KV head by
+ * itself: the first keep_first and last keep_last tokens and, of the others, those with the largest weight
+ * (ties to the lower index; NaN counts as the least) are kept, m = min(keep, length) in all, and become, in
+ * their order, layer by layer the state of `node`, which gets m tokens and an extent in the source's pool;
+ * their weights go to its slots.  K rows keep the positions that they were encoded with.
+ * kept_dev: int32, for every entry in turn [num_layers, num_kv_heads, m], the kept indices, ascending.
+ * The destinations are distinct and none is a source of the same call (GF_ERR_INVALID_ARG), nor may either be
+ * kept as base + residual.  GF_ERR_CAPACITY when a pool is full: then nothing has changed.  New nodes make
+ * built tables stale.  Enqueued on `stream`; no device memory is needed beside the arguments. */
+gf_status_t gf_node_kv_evict(gf_wgraph_t* g, const gf_evict_t* list_host, int32_t count, float* weights_dev,
+                             int32_t* kept_dev, void* stream);
+
 typedef struct {
   uint32_t capacity_tiles;   /* tiles per (layer, KV head) the pool holds                       */
   uint32_t tiles_in_use;     /* tiles of live extents                                           */
   uint32_t high_water_tiles; /* one past the highest tile in use                                */
 } gf_pool_info_t;
 gf_status_t gf_pool_info(const gf_wgraph_t* g, gf_pool_info_t* out_host);
+gf_status_t gf_kv4_pool_info(const gf_wgraph_t* g, gf_pool_info_t* out_host); /* the 4-bit pool; zeros when there is none */
 
 /* Copies one layer of a node's KV state from the pool back to the caller layout
  * ([n_tokens, num_kv_heads, head_dim] bf16 each, caller-owned device buffers of the node's

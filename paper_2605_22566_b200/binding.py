@@ -33,6 +33,8 @@ EXPORTS = [
     "gf_debug_counters", "gf_debug_wait_probe", "gf_node_kv_reserve", "gf_node_kv_release", "gf_pool_info",
     "gf_path_attention_extend_append", "gf_node_extent", "gf_debug_bounds_enabled", "gf_debug_bounds_site",
     "gf_node_kv_attach_residual", "gf_edge_scores", "gf_edge_scores_scratch_bytes",
+    "gf_kv4_bytes_per_tile", "gf_kv4_pool_attach", "gf_kv4_pool_info", "gf_node_kv4_write", "gf_weight_slots",
+    "gf_path_attention_weights", "gf_node_kv_evict",
 ]
 
 
@@ -92,6 +94,11 @@ class Scorer(C.Structure):
                 ("w_gcn1_dev", C.c_void_p), ("w_gcn2_dev", C.c_void_p), ("w_mlp1_dev", C.c_void_p),
                 ("b_mlp1_dev", C.c_void_p), ("w_mlp2_dev", C.c_void_p), ("b_mlp2_dev", C.c_void_p),
                 ("w_mlp3_dev", C.c_void_p), ("b_mlp3", C.c_float)]
+
+
+class Evict(C.Structure):
+    _fields_ = [("node", C.c_int32), ("src_node", C.c_int32), ("keep", C.c_int32), ("keep_first", C.c_int32),
+                ("keep_last", C.c_int32)]
 
 
 class PoolInfo(C.Structure):
@@ -154,6 +161,16 @@ def lib():
         L.gf_edge_scores_scratch_bytes.argtypes = [C.c_void_p, C.POINTER(Scorer), C.c_int32, C.c_int32]
         L.gf_edge_scores.argtypes = [C.c_void_p, C.POINTER(Scorer), C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p,
                                      C.c_void_p, C.c_uint64, C.c_void_p]
+        L.gf_kv4_bytes_per_tile.restype = C.c_uint64
+        L.gf_kv4_bytes_per_tile.argtypes = [C.c_int32]
+        L.gf_kv4_pool_attach.argtypes = [C.c_void_p, C.c_void_p, C.c_uint64]
+        L.gf_kv4_pool_info.argtypes = [C.c_void_p, C.POINTER(PoolInfo)]
+        L.gf_node_kv4_write.argtypes = L.gf_node_kv_write.argtypes
+        L.gf_weight_slots.restype = C.c_int64
+        L.gf_weight_slots.argtypes = [C.c_void_p]
+        L.gf_path_attention_weights.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32,
+                                                C.c_void_p, C.c_void_p]
+        L.gf_node_kv_evict.argtypes = [C.c_void_p, C.POINTER(Evict), C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]
         L.gf_debug_bounds_enabled.restype = C.c_int32
         L.gf_debug_bounds_site.restype = C.c_int32
         L.gf_debug_bounds_site.argtypes = [C.c_void_p]
@@ -335,6 +352,40 @@ def gf_pool_info(g) -> PoolInfo:
     if st != GF_OK:
         raise GfError(st, "gf_pool_info")
     return info
+
+
+def gf_kv4_bytes_per_tile(head_dim: int) -> int:
+    return int(lib().gf_kv4_bytes_per_tile(head_dim))
+
+
+def gf_kv4_pool_attach(g, kv4_pool_ptr, kv4_pool_bytes) -> int:
+    return lib().gf_kv4_pool_attach(g, kv4_pool_ptr, kv4_pool_bytes)
+
+
+def gf_kv4_pool_info(g) -> PoolInfo:
+    info = PoolInfo()
+    st = lib().gf_kv4_pool_info(g, C.byref(info))
+    if st != GF_OK:
+        raise GfError(st, "gf_kv4_pool_info")
+    return info
+
+
+def gf_node_kv4_write(g, node, layer, k_ptr, v_ptr, n_tokens, stream=0) -> int:
+    return lib().gf_node_kv4_write(g, node, layer, k_ptr, v_ptr, n_tokens, stream)
+
+
+def gf_weight_slots(g) -> int:
+    return int(lib().gf_weight_slots(g))
+
+
+def gf_path_attention_weights(g, t, layer, q_ptr, lse_ptr, accumulate, weights_ptr, stream=0) -> int:
+    return lib().gf_path_attention_weights(g, t, layer, q_ptr, lse_ptr, int(accumulate), weights_ptr, stream)
+
+
+def gf_node_kv_evict(g, entries, weights_ptr, kept_ptr, stream=0) -> int:
+    """entries: (node, src_node, keep, keep_first, keep_last) tuples."""
+    arr = (Evict * max(len(entries), 1))(*[Evict(*e) for e in entries])
+    return lib().gf_node_kv_evict(g, arr, len(entries), weights_ptr, kept_ptr, stream)
 
 
 def gf_edge_scores_scratch_bytes(g, scorer: Scorer, num_tasks: int, tasks_per_pass: int) -> int:

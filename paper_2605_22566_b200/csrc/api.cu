@@ -20,6 +20,8 @@ struct gf_tables {
   int32_t bad_req = -1;
   int32_t max_q_rows = 0;
   int32_t num_wide = -1;       // items flagged wide; -1: not known on the host (deferred, or phase B still to run)
+  int32_t kv4_items = -1;      // items held in 4 bits, and their row groups; -1: not known on the host
+  int32_t kv4_units = -1;
   int32_t split_sms = 0;       // multiprocessors the tensor-memory decode kernel gets beside the warp kernel (0: one after the other)
   bool pending = false;        // deferred build: sizes and validity not read back yet
   cudaStream_t build_stream = nullptr;
@@ -84,6 +86,12 @@ struct gf_wgraph {
   ScoreGraphDev score_graph{};             // the task-conditioned graph for gf_edge_scores
   int32_t res_rows_in_use = 0;
   TilePool tiles;
+  // the 4-bit pool (gf_kv4_pool_attach): tiles of its own, whose token slots follow the bf16 pool's
+  PoolGeom pool4{};
+  TilePool tiles4;
+  std::vector<uint8_t> node_kv4;  // 1: the node's extent lies in the 4-bit pool
+  int32_t kv4_nodes = 0;          // how many such nodes exist
+  int device = 0;                 // the device the handle was created on
   char* ws = nullptr;
   size_t ws_bytes = 0;
   size_t ws_graph_end = 0;  // tables are carved after this offset
@@ -158,6 +166,18 @@ size_t phase_a_bytes(int num_nodes, int R, int P) {
   return b + 256;
 }
 
+// Makes the handle's device current while a call enqueues its work, and puts the caller's back.
+struct DeviceGuard {
+  int before = -1;
+  bool ok = false;
+  explicit DeviceGuard(int device) {
+    if (cudaGetDevice(&before) != cudaSuccess) return;
+    ok = before == device || cudaSetDevice(device) == cudaSuccess;
+    if (before == device) before = -1;
+  }
+  ~DeviceGuard() { if (before >= 0) cudaSetDevice(before); }
+};
+
 enum { kSpanTables = 0, kSpanDecode, kSpanMerge, kSpanExtend };
 
 cudaEvent_t take_event(gf_wgraph* g) {
@@ -227,6 +247,8 @@ const char* gf_status_string(gf_status_t s) {
 }
 
 uint64_t gf_pool_bytes_per_tile(int32_t head_dim) { return (uint64_t)2 * kTile * head_dim * 2; }
+
+uint64_t gf_kv4_bytes_per_tile(int32_t head_dim) { return (uint64_t)kTile * head_dim + (uint64_t)2 * kTile * (head_dim / 64) * 4; }
 
 uint64_t gf_workspace_bytes(int32_t num_nodes, int32_t num_edges, int32_t max_requests,
                             int32_t max_pairs, int32_t max_items, int32_t max_slots,
@@ -376,9 +398,11 @@ gf_status_t gf_wgraph_create(const gf_wgraph_desc_t* d, gf_wgraph_t** out) {
   g->node_base.assign(d->num_nodes, -1);
   g->node_res.assign(d->num_nodes, -1);
   g->variants_of.assign(d->num_nodes, 0);
+  g->node_kv4.assign(d->num_nodes, 0);
   for (int r = d->max_residual_nodes - 1; r >= 0; --r) g->free_res_rows.push_back(r);
   {
     int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) == cudaSuccess) g->device = dev;
     if (cudaGetDevice(&dev) == cudaSuccess &&
         cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && sms > 0)
       g->num_sms = sms;
@@ -402,11 +426,17 @@ gf_status_t gf_wgraph_destroy(gf_wgraph_t* g) {
   return GF_OK;
 }
 
+// First tile of a node's extent inside its own pool.
+static int tile_in_pool(const gf_wgraph* g, int32_t node) {
+  return g->node_off[node] / kTile - (g->node_kv4[node] ? (int)g->tiles.cap : 0);
+}
+
 // Gives an unwritten node its extent (first fit), or checks that a written one has this length.
 // *fresh tells the caller that the device copy of the node's length and offset still has to be set.
 static gf_status_t reserve_extent(gf_wgraph* g, int32_t node, int32_t n_tokens, bool* fresh) {
   *fresh = false;
   if (g->node_base[node] >= 0) return GF_ERR_INVALID_ARG;  // kept as base + residual: it has no extent to write
+  if (g->node_kv4[node]) return GF_ERR_INVALID_ARG;         // held in 4 bits
   if (g->node_len[node] >= 0) return g->node_len[node] == n_tokens ? GF_OK : GF_ERR_INVALID_ARG;
   uint32_t first = 0;
   if (!g->tiles.take((uint32_t)((n_tokens + kTile - 1) / kTile), &first)) return GF_ERR_CAPACITY;
@@ -470,6 +500,10 @@ gf_status_t gf_node_kv_release(gf_wgraph_t* g, int32_t node, void* stream) {
     const int m = launch_set_residual(nullptr, ResidualEntry{}, g->gd.node_res, node, -1, st);
     if (m < 0) return GF_ERR_CUDA;
     g->launches += m;
+  } else if (g->node_kv4[node]) {
+    g->tiles4.give((uint32_t)tile_in_pool(g, node), (uint32_t)((g->node_len[node] + kTile - 1) / kTile));
+    g->node_kv4[node] = 0;
+    g->kv4_nodes--;
   } else {
     g->tiles.give((uint32_t)(g->node_off[node] / kTile), (uint32_t)((g->node_len[node] + kTile - 1) / kTile));
   }
@@ -506,6 +540,15 @@ gf_status_t gf_node_kv_read(gf_wgraph_t* g, int32_t node, int32_t layer, void* k
   const int n_tokens = g->node_len[node];
   if (n_tokens > 0 && (!k_out_dev || !v_out_dev || ((uintptr_t)k_out_dev & 15) || ((uintptr_t)v_out_dev & 15)))
     return GF_ERR_INVALID_ARG;
+  if (g->node_kv4[node]) {
+    DeviceGuard dev(g->device);
+    if (!dev.ok) return GF_ERR_CUDA;
+    const int m = launch_kv4_read(g->pool4, layer, g->desc.num_kv_heads, g->desc.head_dim, tile_in_pool(g, node), k_out_dev,
+                                  v_out_dev, n_tokens, g->num_sms, (cudaStream_t)stream);
+    if (m < 0) return GF_ERR_CUDA;
+    g->launches += m;
+    return GF_OK;
+  }
   int n = launch_kv_read(g->pool, layer, g->desc.num_kv_heads, g->desc.head_dim, g->node_off[node] / kTile,
                          k_out_dev, v_out_dev, n_tokens, (cudaStream_t)stream);
   if (n < 0) return GF_ERR_CUDA;
@@ -526,6 +569,7 @@ gf_status_t gf_node_kv_reconstruct(gf_wgraph_t* g, int32_t node, int32_t layer, 
       node == base_node || layer < 0 || layer >= g->desc.num_layers || !residual_ok(k_res) || !residual_ok(v_res))
     return GF_ERR_INVALID_ARG;
   if (g->node_len[base_node] < 0) return GF_ERR_NOT_WRITTEN;
+  if (g->node_kv4[base_node]) return GF_ERR_INVALID_ARG;  // the base must be held in bf16
   const int n_tokens = g->node_len[base_node];
   if (((int64_t)n_tokens + kTile) * g->desc.num_kv_heads > 0x7fffffff) return GF_ERR_INVALID_ARG;  // rows are indexed with int32
   cudaStream_t st = (cudaStream_t)stream;
@@ -552,6 +596,7 @@ gf_status_t gf_node_kv_attach_residual(gf_wgraph_t* g, int32_t node, int32_t lay
     return GF_ERR_INVALID_ARG;
   if (g->node_len[base_node] < 0) return GF_ERR_NOT_WRITTEN;
   if (g->node_base[base_node] >= 0) return GF_ERR_INVALID_ARG;  // the base must own its tiles
+  if (g->node_kv4[base_node]) return GF_ERR_INVALID_ARG;        // and hold them in bf16
   const int n_tokens = g->node_len[base_node];
   if ((int64_t)n_tokens * g->desc.num_kv_heads > 0x7fffffff) return GF_ERR_INVALID_ARG;  // rows are indexed with int32
   cudaStream_t st = (cudaStream_t)stream;
@@ -600,6 +645,7 @@ gf_status_t gf_residual_encode(gf_wgraph_t* g, int32_t base_node, int32_t layer,
       !(threshold >= 0.f) || !residual_buf_ok(k_out, k_full_dev) || !residual_buf_ok(v_out, v_full_dev))
     return GF_ERR_INVALID_ARG;
   if (g->node_len[base_node] < 0) return GF_ERR_NOT_WRITTEN;
+  if (g->node_kv4[base_node]) return GF_ERR_INVALID_ARG;  // the base must be held in bf16
   const int n_tokens = g->node_len[base_node];
   if ((int64_t)n_tokens * g->desc.num_kv_heads > 0x7fffffff) return GF_ERR_INVALID_ARG;  // rows are indexed with int32
   int n = launch_residual_encode(g->pool, layer, g->desc.num_kv_heads, g->desc.head_dim,
@@ -647,7 +693,7 @@ static int decode_split(const gf_wgraph* g, const Header& h) {
   const int sms = g->num_sms;
   const double heads = g->desc.num_kv_heads;
   const double wide_sm_us = (0.80 * h.wide_work + 13.0 * h.wide_tile_units) * heads;  // us x multiprocessors
-  const double stream_tokens = (double)h.resident_tokens - (double)h.wide_tokens;
+  const double stream_tokens = (double)h.resident_tokens - (double)h.wide_tokens - (double)h.kv4_tokens;
   if (!(wide_sm_us > 0.0) || !(stream_tokens > 0.0)) return 0;
   const double steps_per_tile = (double)h.stream_steps / (stream_tokens / kTile);
   double rate = 6.2 - 2.46 * (steps_per_tile - 1.17);   // TB/s
@@ -687,6 +733,8 @@ static gf_status_t read_back_tables(gf_tables* T) {
   T->info.num_q_rows = (int64_t)h.num_q_rows;
   T->max_q_rows = h.max_q_rows;
   T->num_wide = h.num_wide;
+  T->kv4_items = h.kv4_items;
+  T->kv4_units = h.kv4_units;
   T->owner->wide_hint = h.wide_units >= T->dev.wide_min_units;
   T->split_sms = h.num_wide > 0 ? decode_split(T->owner, h) : 0;
   T->owner->split_hint = T->split_sms;
@@ -758,6 +806,7 @@ gf_status_t gf_build_path_tables(gf_wgraph_t* g, int32_t num_requests, int32_t n
   t.wide_min_units = (g->num_sms + g->desc.num_kv_heads - 1) / g->desc.num_kv_heads;
   t.num_sms = g->num_sms;
   t.wide_unit_req = 256 / gqa;
+  t.kv4_tile0 = (int32_t)g->tiles.cap;
 
   // Items, merge slots and partials take the rest of the workspace; how many exist is only known on
   // the device until the header is read back, so the room is expressed as a slot capacity.
@@ -777,6 +826,7 @@ gf_status_t gf_build_path_tables(gf_wgraph_t* g, int32_t num_requests, int32_t n
   }
   T.pending = false;
   T.num_wide = -1;
+  T.kv4_items = T.kv4_units = -1;
   T.error = GF_OK;
   T.build_stream = st;
   T.info = gf_tables_info_t{};
@@ -918,6 +968,10 @@ static int launch_decode_kernels(gf_wgraph* g, const gf_tables* t, const TablesD
   const int num_items = t->pending ? -1 : t->info.num_items;
   const ResidualEntry* residuals =
       g->res_rows_in_use > 0 ? g->res_table_dev + (size_t)layer * g->desc.max_residual_nodes : nullptr;
+  // segments held in 4 bits: a kernel of its own, last in the stream; the others have nothing to do when all are
+  const int kv4_units = g->kv4_nodes > 0 ? t->kv4_units : 0;
+  const bool only_kv4 = !t->pending && kv4_units > 0 && t->kv4_items == t->info.num_items;
+  if (only_kv4) return launch_decode4(g->pool4, g->shape, td, kv4_units, layer, q, g->status_dev, true, st);
   const bool wide = td.wide_min_group > 0 && t->num_wide != 0;
   const int split = wide ? (t->pending ? g->split_hint : t->split_sms) : 0;
   if (wide && split > 0 && ensure_side_stream(g)) {
@@ -930,13 +984,15 @@ static int launch_decode_kernels(gf_wgraph* g, const gf_tables* t, const TablesD
     if (a < 0 || cudaEventRecord(g->ev_join, g->side_stream) != cudaSuccess) return -1;
     if (cudaStreamWaitEvent(st, g->ev_join, 0) != cudaSuccess || b < 0) return -1;
     *joined = true;
-    return a + b;
+    const int c = launch_decode4(g->pool4, g->shape, td, kv4_units, layer, q, g->status_dev, false, st);
+    return c < 0 ? -1 : a + b + c;
   }
   const int b = launch_decode(g->pool, g->shape, td, num_items, layer, q, g->status_dev, 0, residuals, st);
   if (b < 0) return -1;
   int a = 0;
   if (wide) a = launch_decode_wide(g->pool, g->shape, td, num_items, layer, q, g->status_dev, 0, 0, true, st);
-  return a < 0 ? -1 : a + b;
+  const int c = launch_decode4(g->pool4, g->shape, td, kv4_units, layer, q, g->status_dev, true, st);
+  return a < 0 || c < 0 ? -1 : a + b + c;
 }
 
 gf_status_t gf_path_attention_decode(gf_wgraph_t* g, const gf_tables_t* t, int32_t layer,
@@ -981,6 +1037,168 @@ gf_status_t gf_path_attention_extend_append(gf_wgraph_t* g, const gf_tables_t* t
   });
   if (n < 0) return GF_ERR_CUDA;
   g->launches += n;
+  return GF_OK;
+}
+
+gf_status_t gf_kv4_pool_attach(gf_wgraph_t* g, void* kv4_pool_dev, uint64_t kv4_pool_bytes) {
+  if (!g || !kv4_pool_dev || ((uintptr_t)kv4_pool_dev & 1023) || g->kv4_nodes > 0) return GF_ERR_INVALID_ARG;
+  const uint64_t per_tile_all = gf_kv4_bytes_per_tile(g->desc.head_dim) * g->desc.num_kv_heads * g->desc.num_layers;
+  const uint64_t cap = kv4_pool_bytes / per_tile_all;
+  // token slots of both pools are numbered in one int32 range
+  if (cap < 1 || cap + g->tiles.cap > 0x7fffffffull / kTile) return GF_ERR_CAPACITY;
+  g->pool4.base = (char*)kv4_pool_dev;
+  g->pool4.tile_bytes = (uint32_t)gf_kv4_bytes_per_tile(g->desc.head_dim);
+  g->pool4.cap_tiles = (uint32_t)cap;
+  g->pool4.head_stride = (uint64_t)cap * g->pool4.tile_bytes;
+  g->pool4.layer_stride = g->pool4.head_stride * g->desc.num_kv_heads;
+  g->tiles4 = TilePool{};
+  g->tiles4.cap = (uint32_t)cap;
+  return GF_OK;
+}
+
+gf_status_t gf_kv4_pool_info(const gf_wgraph_t* g, gf_pool_info_t* out) {
+  if (!g || !out) return GF_ERR_INVALID_ARG;
+  out->capacity_tiles = g->tiles4.cap;
+  out->tiles_in_use = g->tiles4.in_use;
+  out->high_water_tiles = g->tiles4.top;
+  return GF_OK;
+}
+
+// Gives an unwritten node an extent in the 4-bit pool, or checks that it has one of this length.
+static gf_status_t reserve_extent4(gf_wgraph* g, int32_t node, int32_t n_tokens, bool* fresh) {
+  *fresh = false;
+  if (g->node_len[node] >= 0) return g->node_kv4[node] && g->node_len[node] == n_tokens ? GF_OK : GF_ERR_INVALID_ARG;
+  uint32_t first = 0;
+  if (!g->pool4.base || !g->tiles4.take((uint32_t)(((int64_t)n_tokens + kTile - 1) / kTile), &first)) return GF_ERR_CAPACITY;
+  g->node_len[node] = n_tokens;
+  // (an empty node has no tiles: its offset is not used, and must not pass the slots' range)
+  g->node_off[node] = n_tokens > 0 ? (int32_t)((g->tiles.cap + first) * kTile) : 0;
+  g->node_kv4[node] = 1;
+  g->kv4_nodes++;
+  g->generation++;
+  *fresh = true;
+  return GF_OK;
+}
+
+gf_status_t gf_node_kv4_write(gf_wgraph_t* g, int32_t node, int32_t layer, const void* k_dev, const void* v_dev,
+                              int32_t n_tokens, void* stream) {
+  if (!g || node < 0 || node >= g->desc.num_nodes || layer < 0 || layer >= g->desc.num_layers || n_tokens < 0)
+    return GF_ERR_INVALID_ARG;
+  if (n_tokens > 0 && (!k_dev || !v_dev || ((uintptr_t)k_dev & 15) || ((uintptr_t)v_dev & 15))) return GF_ERR_INVALID_ARG;
+  cudaStream_t st = (cudaStream_t)stream;
+  DeviceGuard dev(g->device);
+  if (!dev.ok) return GF_ERR_CUDA;
+  bool fresh = false;
+  const gf_status_t rs = reserve_extent4(g, node, n_tokens, &fresh);
+  if (rs != GF_OK) return rs;
+  if (fresh && n_tokens == 0) {
+    const int n = launch_graph_set_node(g->gd, node, n_tokens, g->node_off[node], st);
+    if (n < 0) return GF_ERR_CUDA;
+    g->launches += n;
+  }
+  const int n = launch_kv4_write(g->pool4, layer, g->desc.num_kv_heads, g->desc.head_dim, n_tokens > 0 ? tile_in_pool(g, node) : 0,
+                                 k_dev, v_dev, n_tokens, fresh ? &g->gd : nullptr, node, g->node_off[node], g->num_sms, st);
+  if (n < 0) return GF_ERR_CUDA;
+  g->launches += n;
+  return GF_OK;
+}
+
+int64_t gf_weight_slots(const gf_wgraph_t* g) {
+  return g ? ((int64_t)g->tiles.cap + g->tiles4.cap) * kTile : 0;
+}
+
+gf_status_t gf_path_attention_weights(gf_wgraph_t* g, const gf_tables_t* t, int32_t layer, const void* q_dev,
+                                      const float* lse_dev, int32_t accumulate, float* weights_dev, void* stream) {
+  // (weights_dev is checked in the place of an output of 16-byte rows below, which it need not be)
+  const gf_status_t s = check_attention_args(g, t, layer, q_dev, (void*)q_dev, GF_MODE_DECODE);
+  if (s != GF_OK) return s;
+  if (!lse_dev || !weights_dev || ((uintptr_t)lse_dev & 3) || ((uintptr_t)weights_dev & 3) || accumulate < 0 || accumulate > 1)
+    return GF_ERR_INVALID_ARG;
+  DeviceGuard dev(g->device);
+  if (!dev.ok) return GF_ERR_CUDA;
+  const int64_t slots = gf_weight_slots(g);
+  const int n = launch_weights(g->pool, g->pool4, g->shape, t->dev, layer, q_dev, lse_dev, accumulate,
+                               weights_dev + (int64_t)layer * g->desc.num_kv_heads * slots, slots, g->status_dev, (cudaStream_t)stream);
+  if (n < 0) return GF_ERR_CUDA;
+  g->launches += n;
+  return GF_OK;
+}
+
+gf_status_t gf_node_kv_evict(gf_wgraph_t* g, const gf_evict_t* list, int32_t count, float* weights_dev, int32_t* kept_dev,
+                             void* stream) {
+  if (!g || count < 0 || (count > 0 && (!list || !weights_dev || !kept_dev || ((uintptr_t)weights_dev & 3) || ((uintptr_t)kept_dev & 3))))
+    return GF_ERR_INVALID_ARG;
+  if (count == 0) return GF_OK;
+  if ((int64_t)g->desc.num_layers * g->desc.num_kv_heads > 65535) return GF_ERR_INVALID_ARG;  // a grid dimension
+  // everything is checked before anything changes
+  std::vector<int32_t> dst, src;
+  std::vector<EvictEntry> entry;
+  try {
+    dst.reserve(count); src.reserve(count); entry.reserve(count);
+  } catch (...) { return GF_ERR_CAPACITY; }
+  for (int i = 0; i < count; ++i) {
+    const gf_evict_t& e = list[i];
+    if (e.node < 0 || e.node >= g->desc.num_nodes || e.src_node < 0 || e.src_node >= g->desc.num_nodes || e.keep < 0 ||
+        e.keep_first < 0 || e.keep_last < 0 || (int64_t)e.keep_first + e.keep_last > e.keep)
+      return GF_ERR_INVALID_ARG;
+    if (g->node_len[e.src_node] < 0) return GF_ERR_NOT_WRITTEN;
+    if (g->node_base[e.src_node] >= 0 || g->node_base[e.node] >= 0) return GF_ERR_INVALID_ARG;  // no tiles of their own
+    const int32_t m = std::min(e.keep, g->node_len[e.src_node]);
+    if (g->node_len[e.node] >= 0 && (g->node_len[e.node] != m || g->node_kv4[e.node] != g->node_kv4[e.src_node])) return GF_ERR_INVALID_ARG;
+    dst.push_back(e.node);
+    src.push_back(e.src_node);
+  }
+  std::sort(dst.begin(), dst.end());
+  std::sort(src.begin(), src.end());
+  if (std::adjacent_find(dst.begin(), dst.end()) != dst.end()) return GF_ERR_INVALID_ARG;  // two states for one node
+  for (size_t i = 0, j = 0; i < dst.size(); ++i) {
+    while (j < src.size() && src[j] < dst[i]) ++j;
+    if (j < src.size() && src[j] == dst[i]) return GF_ERR_INVALID_ARG;  // read and written by the same call
+  }
+  DeviceGuard dev(g->device);
+  if (!dev.ok) return GF_ERR_CUDA;
+  int64_t kept_off = 0;
+  const uint64_t generation = g->generation;
+  for (int i = 0; i < count; ++i) {
+    const gf_evict_t& e = list[i];
+    EvictEntry x{};
+    x.node = e.node;
+    x.len = g->node_len[e.src_node];
+    x.keep = std::min(e.keep, x.len);
+    x.first = e.keep_first;
+    x.last = e.keep_last;
+    x.four = g->node_kv4[e.src_node];
+    bool fresh = false;
+    const gf_status_t rs = x.four ? reserve_extent4(g, e.node, x.keep, &fresh) : reserve_extent(g, e.node, x.keep, &fresh);
+    if (rs != GF_OK) {  // the pool is full: the extents given out above go back
+      for (const EvictEntry& y : entry)
+        if (y.fresh) {
+          const uint32_t tiles = (uint32_t)((y.keep + kTile - 1) / kTile);
+          if (y.four) { g->tiles4.give((uint32_t)y.dst_tile0, tiles); g->node_kv4[y.node] = 0; g->kv4_nodes--; }
+          else g->tiles.give((uint32_t)y.dst_tile0, tiles);
+          g->node_len[y.node] = g->node_off[y.node] = -1;
+        }
+      g->generation = generation;
+      return rs;
+    }
+    x.fresh = fresh;
+    x.src_slot = g->node_off[e.src_node];
+    x.dst_slot = g->node_off[e.node];
+    x.src_tile0 = x.len > 0 ? tile_in_pool(g, e.src_node) : 0;
+    x.dst_tile0 = x.keep > 0 ? tile_in_pool(g, e.node) : 0;
+    x.kept_off = kept_off;
+    kept_off += (int64_t)x.keep * g->desc.num_layers * g->desc.num_kv_heads;
+    entry.push_back(x);
+  }
+  for (int i0 = 0; i0 < count; i0 += kEvictBatch) {
+    EvictBatch b{};
+    b.count = std::min(count - i0, kEvictBatch);
+    for (int i = 0; i < b.count; ++i) b.entry[i] = entry[i0 + i];
+    const int n = launch_evict(g->pool, g->pool4, b, g->desc.num_layers, g->desc.num_kv_heads, g->desc.head_dim, weights_dev,
+                               gf_weight_slots(g), kept_dev, g->gd, (cudaStream_t)stream);
+    if (n < 0) return GF_ERR_CUDA;
+    g->launches += n;
+  }
   return GF_OK;
 }
 

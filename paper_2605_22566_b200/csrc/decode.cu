@@ -227,7 +227,8 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) k_decode(const DecodeParams
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kProducerRegs));
     // ------------------------------- producer -------------------------------
     if (warp == kConsumerWarps && lane == 0) {
-      const int num_units = tables_usable(*p.hdr, p.slot_cap) ? p.hdr->num_items * p.num_kv_heads : 0;
+      // (when every item is held in 4 bits there is nothing here to walk past)
+      const int num_units = tables_usable(*p.hdr, p.slot_cap) && p.hdr->kv4_items < p.hdr->num_items ? p.hdr->num_items * p.num_kv_heads : 0;
       int n = 0;                                            // stages issued so far
       uint32_t free_mask = (1u << kConsumerWarps) - 1, live_mask = 0;  // live: indexed by a unit's lowest warp
       // A unit is claimed (one atomic on the global counter) only when a warp is free or about to be:

@@ -1,0 +1,211 @@
+// Eviction by accumulated attention weight: the kept tokens of one node's state become the state of another.
+//
+// Per (node, layer, KV head) the kept tokens are the first and last few (as many as the caller protects) and
+// then those with the largest weight, ties to the lower index, m in all; they keep their order.  Two kernels:
+//
+//   k_select  one CTA per (entry, layer, head): a radix select over 32-bit keys whose order is the weights'
+//             (four passes of eight bits, counts in shared memory), then one ordered pass that writes the
+//             kept indices and carries the weights to the destination's slots.  The choice is a function of
+//             the weights alone: integer counts, and ranks from scans.
+//   k_gather  copies the kept rows, in the 4-bit layout by moving the codes of whole tokens (the values are
+//             not touched).  Rows of the last tile past the end become zeros, as every writer of the pools
+//             leaves them.
+//
+// The destination is another node, so nothing is read after it was overwritten and both kernels spread over
+// everything at once.
+#include "kv4_device.cuh"
+
+namespace gf {
+namespace {
+
+constexpr int kSelectThreads = 512;
+constexpr int kGatherThreads = 256;
+
+// Keys in the order of the weights; NaN counts as the least, -0 as +0.  Protected tokens get the largest
+// key, which no weight has.
+__device__ __forceinline__ uint32_t key_of(float w, int t, int n, int first, int last) {
+  if (t < first || t >= n - last) return 0xffffffffu;
+  if (w != w) return 0u;
+  const uint32_t b = __float_as_uint(w + 0.f);
+  return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
+}
+
+__global__ void __launch_bounds__(kSelectThreads) k_select(const EvictBatch batch, float* __restrict__ weights,
+                                                           int64_t layer_slots, int64_t slots, int num_kv_heads,
+                                                           int32_t* __restrict__ kept, int32_t* node_len, int32_t* node_off) {
+  const EvictEntry e = batch.entry[blockIdx.y];
+  if (e.fresh && blockIdx.x == 0 && threadIdx.x == 0) {
+    node_len[e.node] = e.keep;
+    node_off[e.node] = (int32_t)e.dst_slot;
+  }
+  if (e.keep == 0) return;
+  const int layer = blockIdx.x / num_kv_heads, head = blockIdx.x % num_kv_heads;
+  const float* src = weights + layer * layer_slots + head * slots + e.src_slot;
+  float* dst = weights + layer * layer_slots + head * slots + e.dst_slot;
+  int32_t* out = kept + e.kept_off + (int64_t)blockIdx.x * e.keep;
+  const int n = e.len, tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  __shared__ uint32_t hist[256];
+  __shared__ uint32_t pick_s, need_s;
+  __shared__ int32_t wsum[2][kSelectThreads / 32];
+  // the key of rank `keep`, digit by digit from the top
+  uint32_t prefix = 0, need = (uint32_t)e.keep;
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    for (int i = tid; i < 256; i += kSelectThreads) hist[i] = 0u;
+    __syncthreads();
+    const uint32_t mask = shift == 24 ? 0u : 0xffffffffu << (shift + 8);
+    for (int t = tid; t < n; t += kSelectThreads) {
+      const uint32_t key = key_of(src[t], t, n, e.first, e.last);
+      if ((key & mask) == prefix) atomicAdd(&hist[(key >> shift) & 255u], 1u);
+    }
+    __syncthreads();
+    if (wid == 0) {  // counts from the top: lane l owns bins 255 - 8 l .. 248 - 8 l
+      uint32_t c[8], local = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) { c[i] = hist[255 - 8 * lane - i]; local += c[i]; }
+      uint32_t incl = local;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const uint32_t y = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += y;
+      }
+      uint32_t above = incl - local;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (above < need && need <= above + c[i]) { pick_s = 255u - 8u * lane - i; need_s = need - above; }
+        above += c[i];
+      }
+    }
+    __syncthreads();
+    prefix |= pick_s << shift;
+    need = need_s;
+  }
+  // `prefix` is that key; of the tokens that have it, the first `need` are kept
+  int greater = 0, equal = 0;  // before this chunk
+  for (int base = 0; base < n; base += kSelectThreads) {
+    const int t = base + tid;
+    float w = 0.f;
+    uint32_t key = 0;
+    if (t < n) { w = src[t]; key = key_of(w, t, n, e.first, e.last); }
+    const bool gt = t < n && key > prefix, eq = t < n && key == prefix;
+    const uint32_t bg = __ballot_sync(0xffffffffu, gt), be = __ballot_sync(0xffffffffu, eq), below = (1u << lane) - 1u;
+    if (lane == 0) { wsum[0][wid] = __popc(bg); wsum[1][wid] = __popc(be); }
+    __syncthreads();
+    int g = greater + __popc(bg & below), q = equal + __popc(be & below);
+    for (int i = 0; i < kSelectThreads / 32; ++i) {
+      if (i < wid) { g += wsum[0][i]; q += wsum[1][i]; }
+      greater += wsum[0][i];
+      equal += wsum[1][i];
+    }
+    if (gt || (eq && q < (int)need)) {
+      const int at = g + min(q, (int)need);
+      out[at] = t;
+      dst[at] = w;
+    }
+    __syncthreads();
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void gather_tile16(const char* src_head, char* dst_tile, int src_tile0, int count,
+                                              const int32_t* __restrict__ idx) {
+  constexpr int kChunks = D / 8;  // 16-byte pieces of a row
+  constexpr uint32_t kTileBytes = 2 * kTile * D * 2;
+  for (int i = threadIdx.x; i < 2 * kTile * kChunks; i += kGatherThreads) {
+    // eight neighbouring threads share a 128-byte line of one row
+    const uint32_t chunk = i & 7, row = (i >> 3) & (kTile - 1), cb = (i >> 9) % (D / 64), which = (i >> 9) / (D / 64);
+    const uint32_t block = which * (kTileBytes / 2) + cb * (kTile * 128u);
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if ((int)row < count) {
+      const int t = idx[row];
+      v = *reinterpret_cast<const uint4*>(src_head + (uint64_t)(src_tile0 + t / kTile) * kTileBytes + block + swz128(t & (kTile - 1), chunk));
+    }
+    *reinterpret_cast<uint4*>(dst_tile + block + swz128(row, chunk)) = v;
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void gather_tile4(const char* src_head, char* dst_tile, int src_tile0, int count,
+                                             const int32_t* __restrict__ idx) {
+  constexpr int NG = D / kGroup4;
+  constexpr uint32_t kTileBytes = kv4_tile_bytes(D), kPart = kv4_part_bytes(D), kCodes = kv4_code_bytes(D);
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, l4 = lane & 3, l8 = lane >> 2;
+  // a warp per (part, block of 16 tokens, group): every lane builds its 16 bytes from its tokens' pieces
+  for (int job = wid; job < 2 * 4 * NG; job += kGatherThreads / 32) {
+    const int g = job % NG, b = job / NG % 4, which = job / NG / 4;
+    const char* part = src_head + which * kPart;
+    uint4 acc = make_uint4(0u, 0u, 0u, 0u);
+    if (which == 0) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {  // K: tokens l8 + 8 j; a token's codes are nibbles j' and j' + 2, j' = bit 3 of its place
+        const int row = b * 16 + l8 + 8 * j;
+        if (row >= count) continue;
+        const int t = idx[row], in = t & (kTile - 1);
+        const uint4 w = reinterpret_cast<const uint4*>(part + (uint64_t)(src_tile0 + t / kTile) * kTileBytes)[((in >> 4) * NG + g) * 32 + (in & 7) * 4 + l4];
+        const int from = 4 * ((in >> 3) & 1), to = 4 * j;
+        acc.x |= ((w.x >> from) & 0x0f0f0f0fu) << to;
+        acc.y |= ((w.y >> from) & 0x0f0f0f0fu) << to;
+        acc.z |= ((w.z >> from) & 0x0f0f0f0fu) << to;
+        acc.w |= ((w.w >> from) & 0x0f0f0f0fu) << to;
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {  // V: tokens 2 l4 + (k & 1) + 8 (k / 2); a token's codes are one byte of every word
+        const int row = b * 16 + 2 * l4 + (k & 1) + 8 * (k >> 1);
+        if (row >= count) continue;
+        const int t = idx[row], in = t & (kTile - 1);
+        const uint4 w = reinterpret_cast<const uint4*>(part + (uint64_t)(src_tile0 + t / kTile) * kTileBytes)[((in >> 4) * NG + g) * 32 + l8 * 4 + ((in & 7) >> 1)];
+        const int from = 16 * (in & 1) + 8 * ((in >> 3) & 1), to = 16 * (k & 1) + 8 * (k >> 1);
+        acc.x |= ((w.x >> from) & 0xffu) << to;
+        acc.y |= ((w.y >> from) & 0xffu) << to;
+        acc.z |= ((w.z >> from) & 0xffu) << to;
+        acc.w |= ((w.w >> from) & 0xffu) << to;
+      }
+    }
+    reinterpret_cast<uint4*>(dst_tile + which * kPart)[(b * NG + g) * 32 + lane] = acc;
+  }
+  for (int i = threadIdx.x; i < 2 * kTile * NG; i += kGatherThreads) {
+    const int g = i % NG, row = i / NG % kTile, which = i / NG / kTile;
+    uint32_t sl = 0u;
+    if (row < count) {
+      const int t = idx[row];
+      sl = reinterpret_cast<const uint32_t*>(src_head + (uint64_t)(src_tile0 + t / kTile) * kTileBytes + which * kPart + kCodes)[(t & (kTile - 1)) * NG + g];
+    }
+    reinterpret_cast<uint32_t*>(dst_tile + which * kPart + kCodes)[row * NG + g] = sl;
+  }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kGatherThreads) k_gather(const EvictBatch batch, const PoolGeom pool16, const PoolGeom pool4,
+                                                           int num_kv_heads, const int32_t* __restrict__ kept) {
+  const EvictEntry e = batch.entry[blockIdx.z];
+  const int tile = blockIdx.x;
+  if (tile * kTile >= e.keep) return;
+  const int layer = blockIdx.y / num_kv_heads, head = blockIdx.y % num_kv_heads;
+  const int32_t* idx = kept + e.kept_off + (int64_t)blockIdx.y * e.keep + tile * kTile;
+  const int count = min(kTile, e.keep - tile * kTile);
+  const PoolGeom& pool = e.four ? pool4 : pool16;
+  char* head_base = pool.base + (uint64_t)layer * pool.layer_stride + (uint64_t)head * pool.head_stride;
+  char* dst = head_base + (uint64_t)(e.dst_tile0 + tile) * pool.tile_bytes;
+  if (e.four) gather_tile4<D>(head_base, dst, e.src_tile0, count, idx);
+  else gather_tile16<D>(head_base, dst, e.src_tile0, count, idx);
+}
+
+}  // namespace
+
+int launch_evict(const PoolGeom& pool16, const PoolGeom& pool4, const EvictBatch& batch, int num_layers, int num_kv_heads,
+                 int head_dim, float* weights, int64_t slots, int32_t* kept, const GraphDev& g, cudaStream_t st) {
+  int most = 0;
+  for (int i = 0; i < batch.count; ++i) most = batch.entry[i].keep > most ? batch.entry[i].keep : most;
+  const unsigned lh = (unsigned)(num_layers * num_kv_heads);
+  k_select<<<dim3(lh, batch.count), kSelectThreads, 0, st>>>(batch, weights, slots * num_kv_heads, slots, num_kv_heads, kept, g.node_len, g.node_off);
+  int launched = 1;
+  if (most > 0) {
+    const dim3 grid((unsigned)((most + kTile - 1) / kTile), lh, batch.count);
+    if (head_dim == 128) k_gather<128><<<grid, kGatherThreads, 0, st>>>(batch, pool16, pool4, num_kv_heads, kept);
+    else k_gather<64><<<grid, kGatherThreads, 0, st>>>(batch, pool16, pool4, num_kv_heads, kept);
+    ++launched;
+  }
+  return cudaGetLastError() == cudaSuccess ? launched : -1;
+}
+
+}  // namespace gf

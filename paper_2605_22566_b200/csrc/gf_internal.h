@@ -16,6 +16,7 @@ enum StatusWord {
   kStatusGiveUp = 1,       // non-zero: a bounded device wait gave up (GF_ERR_TIMEOUT)
   kStatusBounds = 2,       // debug build only: the largest site code of a range check that failed (GF_ERR_BOUNDS)
   kStatusDecodeQueue = 4,  // [0] next unit of the warp decode kernel, [1] its CTAs that finished
+  kStatusKv4Queue = 6,     // the same pair for the decode kernel over 4-bit states
   kStatusWideQueue = 8,    // the same pair for the tensor-memory decode kernel
   kStatusProbe = 3,        // what the wait probe's waiter saw (gf_debug_wait_probe)
   kStatusRescales = 12,    // diagnostic: times a tensor-memory tile moved its softmax reference after its first stage
@@ -29,7 +30,8 @@ enum StatusWord {
 struct __align__(32) Item {
   int32_t seg, tok_begin, tok_count, grp_begin, grp_count, part_base;
   int32_t tile0;  // pool tile index of the chunk's first token
-  int32_t pad;    // bit 0: chunk of a widely shared segment, handled by the tensor-memory decode kernel;
+  int32_t pad;    // bit 0: not the warp decode kernel's (a chunk of a widely shared segment, handled by the
+                  // tensor-memory kernel, or one held in 4 bits, handled by the decode kernel for those);
                   // bits 8..: 1 + row of the residual table if the segment's state is base + residual
 };
 
@@ -49,6 +51,10 @@ struct Header {
   int32_t wide_tokens; // tokens of the segments the wide kernel handles (the warp kernel streams the rest)
   int32_t wide_tile_units;  // (chunk x 128-row tile) pairs of the wide kernel per KV head: each loads queries and writes partials
   int32_t stream_steps;     // work of the warp kernel per KV head, in (64-token tile x 16-row group) steps
+  int32_t kv4_items;   // items of segments held in 4 bits
+  int32_t kv4_units;   // their (item, 16-row group) pairs: the length the list below will have
+  int32_t kv4_list_n;  // pairs listed for the 4-bit decode kernel (from the end of wide_list)
+  int32_t kv4_tokens;  // tokens of the segments held in 4 bits
   unsigned long long resident_tokens;
   unsigned long long materialised_tokens;
   unsigned long long num_q_rows;
@@ -103,7 +109,10 @@ struct TablesDev {
   int32_t* ext_written; // [R] extend with append: tiles of every request's new node written so far
   Item* items;         // [num_items]   (carved after the read-back)
   int32_t* mrg_slot;   // [num_slots]   (carved after the read-back)
-  int32_t* wide_list;  // [wide_list_n] item index of the first item of every wide unit, any order
+  int32_t* wide_list;  // [wide_list_n] item index of the first item of every wide unit, any order;
+                       // from the last of its slot_cap entries backwards, [kv4_list_n]: 4 * item + row
+                       // group of every 16-row group of the items held in 4 bits, any order.  A wide unit
+                       // and a row group each stand for one partial slot at least, so the two never meet
   float* part_o;       // [num_slots, Hq, D] fp32 un-normalised partial outputs
   float* part_ml;      // [num_slots, Hq, 2] running max (log2 units) and sum
   const int32_t* node_res;  // [num_nodes] the graph's residual rows (see GraphDev)
@@ -115,6 +124,7 @@ struct TablesDev {
   int32_t wide_min_units;  // ... provided the batch has at least this many wide units per KV head
   int32_t num_sms;         // multiprocessors of the device the handle lives on (grid sizing)
   int32_t wide_unit_req;   // requests per unit of the wide kernel: 256 stacked query rows / GQA group size
+  int32_t kv4_tile0;       // pool tiles from this index on lie in the 4-bit pool (at tile - kv4_tile0 there)
 };
 
 // True when the tables on the device are usable: every path valid and the items / partial slots fit
@@ -129,6 +139,20 @@ struct PoolGeom {
   uint64_t head_stride;   // bytes between KV heads of one layer
   uint32_t tile_bytes;    // K block + V block of one 64-token tile of one head
   uint32_t cap_tiles;     // tiles per (layer, head)
+};
+
+// One node's eviction (see gf_node_kv_evict), sizes and places worked out by the host.
+struct EvictEntry {
+  int64_t src_slot, dst_slot;  // first token slots
+  int64_t kept_off;            // where the entry's kept indices start
+  int32_t node, len, keep, first, last;
+  int32_t src_tile0, dst_tile0;  // in the node's own pool
+  int32_t four, fresh;           // held in 4 bits; the device has to learn the destination's length and offset
+};
+constexpr int kEvictBatch = 32;  // entries per launch, passed by value
+struct EvictBatch {
+  EvictEntry entry[kEvictBatch];
+  int32_t count;
 };
 
 struct AttnShape {
@@ -255,6 +279,18 @@ int launch_decode_wide(const PoolGeom& pool, const AttnShape& sh, const TablesDe
 size_t edge_scores_scratch_floats(int num_ops, const gf_scorer_t& m, int num_queries, int per_pass);
 int launch_edge_scores(const ScoreGraphDev& g, const gf_scorer_t& m, const float* x_op, int num_queries,
                        const float* x_task, float* scores, float* scratch, int per_pass, cudaStream_t st);
+// token_off: the node's first token slot.
+int launch_kv4_write(const PoolGeom& pool, int layer, int num_kv_heads, int head_dim, int tile0, const void* k,
+                     const void* v, int n_tokens, const GraphDev* set, int node, int token_off, int num_sms, cudaStream_t st);
+int launch_kv4_read(const PoolGeom& pool, int layer, int num_kv_heads, int head_dim, int tile0, void* k, void* v,
+                    int n_tokens, int num_sms, cudaStream_t st);
+// num_units: (item, row group) pairs, < 0: not known on the host.  chained: see launch_decode_wide.
+int launch_decode4(const PoolGeom& pool, const AttnShape& sh, const TablesDev& t, int num_units, int layer, const void* q,
+                   int32_t* status, bool chained, cudaStream_t st);
+int launch_weights(const PoolGeom& pool16, const PoolGeom& pool4, const AttnShape& sh, const TablesDev& t, int layer, const void* q,
+                   const float* lse, int accumulate, float* weights, int64_t slots, int32_t* status, cudaStream_t st);
+int launch_evict(const PoolGeom& pool16, const PoolGeom& pool4, const EvictBatch& batch, int num_layers, int num_kv_heads,
+                 int head_dim, float* weights, int64_t slots, int32_t* kept, const GraphDev& g, cudaStream_t st);
 int launch_wait_probe(int32_t* status, long long limit, int32_t* returned, cudaStream_t st);
 // k_new / v_new non-null: the new segments' K/V (caller layout, request-major rows) are written to their
 // pool extents by the same launch (extend with append).

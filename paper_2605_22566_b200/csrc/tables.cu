@@ -83,6 +83,7 @@ __global__ void k_init(TablesDev t, int num_nodes) {
     h.wide_tokens = 0;
     h.wide_tile_units = 0;
     h.stream_steps = 0;
+    h.kv4_items = h.kv4_units = h.kv4_list_n = h.kv4_tokens = 0;
     h.max_q_rows = 0;
     h.resident_tokens = h.materialised_tokens = h.num_q_rows = 0ull;
     *t.hdr = h;
@@ -130,9 +131,11 @@ __global__ void k_validate(GraphDev g, TablesDev t, const int32_t* __restrict__ 
       }
     }
     if (lane == 0 && t.mode == GF_MODE_EXTEND && g.node_len[path_node[e - 1]] <= 0) bad = true;
-    if (t.mode == GF_MODE_EXTEND)  // extend streams whole extents: a state kept as base + residual has none of its own
-      for (int i = b + lane; i < e; i += 32)
-        if (g.node_res[path_node[i]] >= 0) bad = true;
+    if (t.mode == GF_MODE_EXTEND)  // extend streams whole bf16 extents: a state kept as base + residual or in 4 bits has none
+      for (int i = b + lane; i < e; i += 32) {
+        const int v = path_node[i];
+        if (g.node_res[v] >= 0 || (g.node_len[v] > 0 && g.node_off[v] / kTile >= t.kv4_tile0)) bad = true;
+      }
     bad = __any_sync(0xffffffffu, bad);
   }
   if (bad) {
@@ -233,6 +236,15 @@ __global__ void k_scan_nodes_segments(GraphDev g, TablesDev t, gf_policy_t pol) 
     t.seg_nchunk[s] = nchunk;
     t.seg_item_base[s] = nchunk * ceil_div(G, pol.group_tile);
     t.seg_part_base[s] = nchunk * G;
+    if (t.seg_off[s] / kTile >= t.kv4_tile0) {
+      // held in 4 bits: a kernel of its own, a unit of which is one 16-row group of an item
+      const int gqa = 256 / t.wide_unit_req;
+      const int groups = (G / pol.group_tile) * ceil_div(pol.group_tile * gqa, 16) + ceil_div((G % pol.group_tile) * gqa, 16);
+      atomicAdd(&t.hdr->kv4_items, nchunk * ceil_div(G, pol.group_tile));
+      atomicAdd(&t.hdr->kv4_units, nchunk * groups);
+      atomicAdd(&t.hdr->kv4_tokens, l);
+      continue;
+    }
     // (a segment whose state is base + residual is patched in shared memory by the warp kernel only)
     if (G >= t.wide_probe_group && (t.wide_unit_req % pol.group_tile) == 0 && t.node_res[t.seg_node[s]] < 0) {
       atomicAdd(&wide_units, nchunk * ceil_div(G, t.wide_unit_req));  // CTAs' worth of work for the wide kernel, per KV head
@@ -438,13 +450,20 @@ __device__ void emit_item(const TablesDev& t, const gf_policy_t& pol, int i, con
   it.tile0 = (t.seg_off[s] + it.tok_begin) / kTile;
   // the group tiles of wide_unit_req / group_tile consecutive items form one unit of the wide kernel
   const int res = t.node_res[t.seg_node[s]];
-  const bool wide = t.hdr->num_wide > 0 && G >= t.wide_min_group && (t.wide_unit_req % pol.group_tile) == 0 && res < 0;
-  it.pad = (wide ? 1 : 0) | ((res + 1) << 8);
+  const bool four = it.tile0 >= t.kv4_tile0;
+  const bool wide = t.hdr->num_wide > 0 && G >= t.wide_min_group && (t.wide_unit_req % pol.group_tile) == 0 && res < 0 && !four;
+  it.pad = (wide || four ? 1 : 0) | ((res + 1) << 8);
   t.items[i] = it;
   // the first item of every wide_unit_req requests of a wide chunk stands for a unit of the wide kernel
   if (wide && ((it.grp_begin - t.grp_ptr[s]) % t.wide_unit_req) == 0) {
     const int at = atomicAdd(&t.hdr->wide_list_n, 1);
     if (GF_CHECK(at < t.slot_cap, t.status, 305)) t.wide_list[at] = i;
+  }
+  if (four) {
+    const int groups = ceil_div(it.grp_count * (256 / t.wide_unit_req), 16);
+    const int at = atomicAdd(&t.hdr->kv4_list_n, groups);
+    for (int k = 0; k < groups; ++k)
+      if (GF_CHECK(at + k < t.slot_cap, t.status, 308)) t.wide_list[t.slot_cap - 1 - at - k] = 4 * i + k;
   }
 }
 

@@ -36,7 +36,10 @@ class PathAttention:
     """One wGraph handle with its pool and workspace, fed from a `workloads.Workload`."""
 
     def __init__(self, w: W.Workload, device: str = "cuda:0", layers: Optional[int] = None,
-                 policy: Optional[tuple] = None, extra_tiles: int = 0, max_residual_nodes: int = 0):
+                 policy: Optional[tuple] = None, extra_tiles: int = 0, max_residual_nodes: int = 0,
+                 kv4_nodes=(), extra_kv4_tiles: int = 0):
+        """kv4_nodes: the nodes whose state is held in 4 bits (write_nodes and write_node go by it).  Either pool
+        is sized for the used nodes that it holds, plus the extra tiles."""
         if not torch.cuda.is_available():
             raise RuntimeError("a CUDA device is required (the path has no CPU fallback)")
         self.w = w
@@ -46,8 +49,11 @@ class PathAttention:
         self.policy = policy
         chunk = policy[0] if policy is not None else 256
         used = w.used_nodes()
-        tiles = int(((w.node_len[used].astype(np.int64) + B.GF_TILE_TOKENS - 1) // B.GF_TILE_TOKENS).sum())
-        tiles = max(tiles + extra_tiles, 1)
+        self.kv4_nodes = frozenset(int(v) for v in kv4_nodes)
+        node_tiles = (w.node_len[used].astype(np.int64) + B.GF_TILE_TOKENS - 1) // B.GF_TILE_TOKENS
+        in4 = np.isin(used, np.fromiter(self.kv4_nodes, np.int64, len(self.kv4_nodes)))
+        tiles = max(int(node_tiles[~in4].sum()) + extra_tiles, 1)
+        kv4_tiles = int(node_tiles[in4].sum()) + extra_kv4_tiles
         self.pool_bytes = tiles * B.gf_pool_bytes_per_tile(w.head_dim) * w.num_kv_heads * self.layers
         self._guards = []
         # the pool must start on a 1024-byte boundary; the caching allocator only promises 512
@@ -66,6 +72,10 @@ class PathAttention:
             kv_pool_bytes=self.pool_bytes, workspace_ptr=self.ws.data_ptr(), workspace_bytes=self.ws_bytes,
             max_residual_nodes=max_residual_nodes)
         B.check(st, "gf_wgraph_create")
+        if self.kv4_nodes or kv4_tiles:
+            nbytes = max(kv4_tiles, 1) * B.gf_kv4_bytes_per_tile(w.head_dim) * w.num_kv_heads * self.layers
+            self.pool4 = self.guarded(nbytes, "4-bit kv pool", align=1024)
+            B.check(B.gf_kv4_pool_attach(self.g, self.pool4.data_ptr(), nbytes), "gf_kv4_pool_attach")
         self.path_ptr = torch.from_numpy(w.path_ptr.astype(np.int32)).to(self.dev)
         self.path_node = torch.from_numpy(w.path_node.astype(np.int32)).to(self.dev)
         self.tables = None
@@ -148,10 +158,32 @@ class PathAttention:
                     kb, vb = w.node_kv_bits(layer, v)
                     kt, vt = _bits_to_tensor(kb, self.dev), _bits_to_tensor(vb, self.dev)
                     kp, vp = kt.data_ptr(), vt.data_ptr()
-                B.check(B.gf_node_kv_write(self.g, v, layer, kp, vp, n, self.stream), "gf_node_kv_write")
+                write = B.gf_node_kv4_write if v in self.kv4_nodes else B.gf_node_kv_write
+                B.check(write(self.g, v, layer, kp, vp, n, self.stream), "gf_node_kv_write")
                 if source != "device":
                     torch.cuda.current_stream(self.dev).synchronize()  # kt/vt are freed next turn
         torch.cuda.current_stream(self.dev).synchronize()
+
+    def write_node(self, node: int, layer: int, k: torch.Tensor, v: torch.Tensor) -> None:
+        """gf_node_kv_write, or gf_node_kv4_write for a node of `kv4_nodes`, of bf16 tensors [tokens, Hkv, D]."""
+        self._check_kv(k, v)
+        write = B.gf_node_kv4_write if node in self.kv4_nodes else B.gf_node_kv_write
+        B.check(write(self.g, node, layer, k.data_ptr(), v.data_ptr(), k.shape[0], self.stream), "gf_node_kv_write")
+
+    def load_node(self, node: int, layer: int):
+        """gf_node_kv_read into two new bf16 tensors [tokens, Hkv, D]; nothing is waited for."""
+        st, n, _ = B.gf_node_extent(self.g, node)
+        B.check(st, "gf_node_extent")
+        k = torch.empty((n, self.w.num_kv_heads, self.w.head_dim), dtype=torch.bfloat16, device=self.dev)
+        v = torch.empty_like(k)
+        B.check(B.gf_node_kv_read(self.g, node, layer, k.data_ptr(), v.data_ptr(), self.stream), "gf_node_kv_read")
+        return k, v
+
+    def _check_kv(self, k: torch.Tensor, v: torch.Tensor) -> None:
+        for name, t in (("k", k), ("v", v)):
+            if t.dtype != torch.bfloat16 or t.device != self.pool.device or not t.is_contiguous() or t.dim() != 3 or \
+                    t.shape[1:] != (self.w.num_kv_heads, self.w.head_dim) or t.shape[0] != k.shape[0]:
+                raise ValueError(f"{name}: a contiguous bf16 tensor [tokens, {self.w.num_kv_heads}, {self.w.head_dim}] on {self.pool.device}")
 
     def new_nodes(self):
         """The last node of every path: in an extend batch, the request's new segment."""
@@ -233,6 +265,63 @@ class PathAttention:
                                                   v_new.data_ptr(), out.data_ptr(),
                                                   None if lse is None else lse.data_ptr(), self.stream),
                 "gf_path_attention_extend_append")
+        return out
+
+    # ---- eviction by accumulated attention weight --------------------------------------------
+    def new_weights(self) -> torch.Tensor:
+        """Zeroed weights for every token slot of both pools: fp32 [layers, Hkv, slots]."""
+        shape = (self.layers, self.w.num_kv_heads, B.gf_weight_slots(self.g))
+        buf = self.guarded(4 * shape[0] * shape[1] * shape[2], "attention weights").view(torch.float32).view(shape)
+        return buf.zero_()
+
+    def node_slot(self, node: int) -> int:
+        """The first token slot of a node."""
+        st, _, slot = B.gf_node_extent(self.g, node)
+        B.check(st, "gf_node_extent")
+        return slot
+
+    def node_weights(self, weights: torch.Tensor, node: int) -> torch.Tensor:
+        """A view of one node's weights: [layers, Hkv, tokens]."""
+        st, n, slot = B.gf_node_extent(self.g, node)
+        B.check(st, "gf_node_extent")
+        return weights[:, :, slot:slot + n]
+
+    def _check_weights(self, weights: torch.Tensor) -> None:
+        shape = (self.layers, self.w.num_kv_heads, B.gf_weight_slots(self.g))
+        if weights.dtype != torch.float32 or weights.device != self.pool.device or not weights.is_contiguous() or \
+                tuple(weights.shape) != shape:
+            raise ValueError(f"weights: a contiguous fp32 tensor {list(shape)} on {self.pool.device}")
+
+    def attention_weights(self, layer: int, q: torch.Tensor, lse: torch.Tensor, weights: torch.Tensor,
+                          accumulate: bool = True) -> torch.Tensor:
+        """gf_path_attention_weights: adds to `weights` (or sets) what every token of the batch's paths received in
+        the decode step of q and lse."""
+        self._check_weights(weights)
+        rows = (self.w.num_requests, self.w.num_q_heads)
+        if q.dtype != torch.bfloat16 or not q.is_contiguous() or tuple(q.shape) != rows + (self.w.head_dim,) or q.device != self.pool.device:
+            raise ValueError(f"q: a contiguous bf16 tensor {[*rows, self.w.head_dim]} on {self.pool.device}")
+        if lse.dtype != torch.float32 or not lse.is_contiguous() or tuple(lse.shape) != rows or lse.device != self.pool.device:
+            raise ValueError(f"lse: a contiguous fp32 tensor {list(rows)} on {self.pool.device}")
+        B.check(B.gf_path_attention_weights(self.g, self.tables, layer, q.data_ptr(), lse.data_ptr(), accumulate,
+                                            weights.data_ptr(), self.stream), "gf_path_attention_weights")
+        return weights
+
+    def evict(self, entries, weights: torch.Tensor):
+        """gf_node_kv_evict of (node, src_node, keep, keep_first, keep_last) entries; every entry's kept indices,
+        int32 [layers, Hkv, kept]."""
+        self._check_weights(weights)
+        sizes = []
+        for e in entries:
+            st, n, _ = B.gf_node_extent(self.g, e[1])
+            B.check(st, "gf_node_extent")
+            sizes.append(max(min(n, e[2]), 0))
+        lh = self.layers * self.w.num_kv_heads
+        kept = torch.empty(max(lh * sum(sizes), 1), dtype=torch.int32, device=self.dev)
+        B.check(B.gf_node_kv_evict(self.g, entries, weights.data_ptr(), kept.data_ptr(), self.stream), "gf_node_kv_evict")
+        out, at = [], 0
+        for m in sizes:
+            out.append(kept[at:at + lh * m].view(self.layers, self.w.num_kv_heads, m))
+            at += lh * m
         return out
 
     def read_node(self, node: int, layer: int):

@@ -1,0 +1,296 @@
+"""Node states held in 4 bits: what is stored against the definition, and decode over them against fp64 attention over the
+values that the codes stand for."""
+import numpy as np
+import pytest
+import torch
+
+from helpers import assert_close
+from kv4_cases import ODD_LENS, View, private_workload, random_case
+from oracle import attention as OA
+from oracle import kv4
+from oracle.residual import bf16_to_f64, f64_to_bf16_rne
+from paper_2605_22566_b200 import workloads as W
+
+pytestmark = pytest.mark.gpu
+
+
+def _handle(w, four, **kw):
+    from paper_2605_22566_b200.runtime import PathAttention
+    return PathAttention(w, kv4_nodes=four, **kw)
+
+
+def _bits(t):
+    return t.view(torch.int16).cpu().numpy().view(np.uint16)
+
+
+_bf16 = kv4.round_to_bf16
+
+
+def _tensor(x):
+    """bf16 numbers in fp64 as a tensor."""
+    return torch.from_numpy((x.astype(np.float32).view(np.uint32) >> 16).astype(np.uint16).view(np.int16)).cuda().view(torch.bfloat16)
+
+
+# ---- storage --------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("hkv,d", [(1, 64), (3, 64), (8, 128), (2, 128)])
+def test_stored_values_bit_for_bit(hkv, d):
+    lens = [1, 15, 16, 17, 64, 65, 200]
+    w = private_workload(lens, [[i] for i in range(len(lens))], hkv, hkv, d, layers=2)
+    pa = _handle(w, range(len(lens)))
+    pa.write_nodes("host")
+    for layer in (0, 1):
+        for v, n in enumerate(lens):
+            for got, bits in zip(pa.load_node(v, layer), w.node_kv_bits(layer, v)):
+                want = f64_to_bf16_rne(kv4.values(W.bf16_bits_to_f64(bits)))
+                assert np.array_equal(_bits(got), want), (layer, v)
+    assert pa.status() == 0
+    pa.close()
+
+
+@pytest.mark.parametrize("scale", [1e-35, 1.0, 2e36])
+def test_stored_values_of_unusual_groups(scale):
+    """Constant groups, one outlier, a spread far below the values, tiny and huge entries.  A value is computed in fp32 and
+    rounded to bf16: within half a bf16 step (2^-8) and half an fp32 step (2^-24) of the definition's."""
+    rng = np.random.default_rng(7)
+    x = rng.standard_normal((70, 2, 128))
+    x[0] = 0.75
+    x[1, 0, :64] = 0.0
+    x[2, 1, 5] = 90.0
+    x[3] = 64.0 + 0.5 * rng.integers(0, 3, (2, 128))
+    x[4] = -np.abs(x[4])
+    x = _bf16(x * scale)
+    w = private_workload([70], [[0]], 2, 2, 128)
+    pa = _handle(w, [0])
+    t = _tensor(x)
+    pa.write_node(0, 0, t, t)
+    want = kv4.values(x)
+    for got in pa.load_node(0, 0):
+        got = bf16_to_f64(_bits(got))
+        assert np.all(np.abs(got - want) <= np.abs(want) * (2.0 ** -8 + 2.0 ** -23))
+    pa.close()
+
+
+def test_largest_finite_range_does_not_overflow():
+    big = float(torch.finfo(torch.bfloat16).max)
+    x = np.zeros((3, 1, 64))
+    x[:, :, ::2], x[:, :, 1::2] = big, -big
+    w = private_workload([3], [[0]], 1, 1, 64)
+    pa = _handle(w, [0])
+    t = _tensor(x)
+    pa.write_node(0, 0, t, t)
+    k, v = pa.load_node(0, 0)
+    want = kv4.values(x)
+    assert np.all(np.isfinite(want))
+    for got in (k, v):
+        assert np.all(np.abs(bf16_to_f64(_bits(got)) - want) <= np.abs(want) * (2.0 ** -8 + 2.0 ** -23))
+    pa.close()
+
+
+def test_extents_release_rewrite_and_refusals():
+    from paper_2605_22566_b200 import binding as B
+    w = private_workload([100, 64, 30, 0, 100, 10], [[0], [1], [2]], 2, 2, 64)
+    pa = _handle(w, [0, 1], extra_tiles=1)      # 4-bit pool: 3 tiles; bf16 pool: 2
+    buf = torch.randn(128, 2, 64, device="cuda").to(torch.bfloat16)
+    p, s = buf.data_ptr(), pa.stream
+    cap16 = B.gf_pool_info(pa.g).capacity_tiles
+    assert B.gf_kv4_pool_info(pa.g).capacity_tiles == 3
+    assert B.gf_node_kv4_write(pa.g, 0, 0, p, p, 100, s) == B.GF_OK
+    assert B.gf_node_extent(pa.g, 0) == (B.GF_OK, 100, cap16 * 64)
+    assert B.gf_node_kv4_write(pa.g, 1, 0, p, p, 64, s) == B.GF_OK
+    assert B.gf_node_extent(pa.g, 1) == (B.GF_OK, 64, cap16 * 64 + 128)
+    assert B.gf_weight_slots(pa.g) == (cap16 + 3) * 64
+    assert B.gf_node_kv4_write(pa.g, 4, 0, p, p, 1, s) == B.GF_ERR_CAPACITY
+    assert B.gf_node_kv4_write(pa.g, 0, 0, p, p, 99, s) == B.GF_ERR_INVALID_ARG      # another length
+    assert B.gf_node_kv4_write(pa.g, 0, 0, p + 2, p, 100, s) == B.GF_ERR_INVALID_ARG  # alignment
+    assert B.gf_node_kv4_write(pa.g, 0, 1, p, p, 100, s) == B.GF_ERR_INVALID_ARG     # no such layer
+    assert B.gf_node_kv_write(pa.g, 0, 0, p, p, 100, s) == B.GF_ERR_INVALID_ARG      # held in 4 bits
+    assert B.gf_node_kv_reserve(pa.g, 0, 100, s) == B.GF_ERR_INVALID_ARG
+    assert B.gf_node_kv_write(pa.g, 2, 0, p, p, 30, s) == B.GF_OK
+    assert B.gf_node_kv4_write(pa.g, 2, 0, p, p, 30, s) == B.GF_ERR_INVALID_ARG      # held in bf16
+    assert B.gf_node_kv_reconstruct(pa.g, 4, 0, 0, None, None, s) == B.GF_ERR_INVALID_ARG
+    assert B.gf_node_kv_attach_residual(pa.g, 4, 0, 0, None, None, s) == B.GF_ERR_INVALID_ARG
+    assert B.gf_residual_encode(pa.g, 0, 0, p, p, 0.0, None, None, s) == B.GF_ERR_INVALID_ARG
+    assert B.gf_kv4_pool_attach(pa.g, pa.pool4.data_ptr(), pa.pool4.numel()) == B.GF_ERR_INVALID_ARG  # nodes in it
+    assert B.gf_node_kv4_write(pa.g, 3, 0, None, None, 0, s) == B.GF_OK              # an empty node has no tiles
+    assert B.gf_node_kv_read(pa.g, 3, 0, None, None, s) == B.GF_OK
+    assert B.gf_node_kv_release(pa.g, 0, s) == B.GF_OK
+    assert B.gf_kv4_pool_info(pa.g).tiles_in_use == 1
+    assert B.gf_node_kv4_write(pa.g, 5, 0, p, p, 10, s) == B.GF_OK                   # takes the hole's first tile
+    assert B.gf_node_extent(pa.g, 5) == (B.GF_OK, 10, cap16 * 64)
+    assert B.gf_node_kv_write(pa.g, 0, 0, p, p, 30, s) == B.GF_OK                    # and node 0 may be held in bf16 now
+    for v in (1, 3, 5):
+        assert B.gf_node_kv_release(pa.g, v, s) == B.GF_OK
+    info = B.gf_kv4_pool_info(pa.g)
+    assert (info.tiles_in_use, info.high_water_tiles) == (0, 0)
+    assert B.gf_kv4_pool_attach(pa.g, pa.pool4.data_ptr() + 16, pa.pool4.numel()) == B.GF_ERR_INVALID_ARG
+    assert B.gf_kv4_pool_attach(pa.g, pa.pool4.data_ptr(), 64) == B.GF_ERR_CAPACITY
+    assert B.gf_kv4_pool_attach(pa.g, pa.pool4.data_ptr(), pa.pool4.numel()) == B.GF_OK
+    assert pa.status() == 0
+    with pytest.raises(ValueError):
+        pa.write_node(1, 0, buf.float(), buf.float())
+    with pytest.raises(ValueError):
+        pa.write_node(1, 0, buf[:, :, :32], buf[:, :, :32])
+    pa.close()
+
+
+def test_a_handle_without_a_4_bit_pool_refuses():
+    from paper_2605_22566_b200 import binding as B
+    w = private_workload([10], [[0]], 2, 2, 64)
+    pa = _handle(w, [])
+    buf = torch.zeros(10, 2, 64, dtype=torch.bfloat16, device="cuda")
+    assert B.gf_node_kv4_write(pa.g, 0, 0, buf.data_ptr(), buf.data_ptr(), 10, pa.stream) == B.GF_ERR_CAPACITY
+    assert B.gf_kv4_pool_info(pa.g).capacity_tiles == 0
+    pa.close()
+
+
+# ---- decode ---------------------------------------------------------------------------------------------
+
+
+def _decode(w, four, policy=None, deferred=False, check=True, source="host"):
+    from paper_2605_22566_b200.runtime import tensor_to_f64
+    pa = _handle(w, four, policy=policy)
+    pa.write_nodes(source)
+    pa.build(deferred=deferred)
+    q = pa.make_q(0, source)
+    lse = pa.guarded(w.num_requests * w.num_q_heads * 4, "lse").view(torch.float32).view(w.num_requests, w.num_q_heads)
+    out = pa.decode(0, q, lse=lse)
+    assert pa.status() == 0
+    got, got_lse = tensor_to_f64(out), tensor_to_f64(lse)
+    if check:
+        view = View(w, four)
+        ref, ref_lse = OA.decode(view.paths(), view.node_kv, view.q(), w.num_kv_heads)
+        assert_close(got, ref, "out")
+        seen = np.isfinite(ref_lse)
+        assert np.array_equal(np.isneginf(got_lse), ~seen)
+        assert np.abs(got_lse[seen] - ref_lse[seen]).max() < 2e-3
+    pa.close()
+    return got, got_lse
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(4, 4, 64), (2, 1, 64), (8, 2, 64), (16, 2, 64), (3, 3, 128), (4, 2, 128), (32, 8, 128), (8, 1, 128)])
+@pytest.mark.parametrize("four", ["all", "some"])
+def test_decode_every_head_layout_and_odd_lengths(hq, hkv, d, four):
+    w = random_case(hq, hkv, d, requests=9)
+    _decode(w, range(len(ODD_LENS)) if four == "all" else [v for v in range(len(ODD_LENS)) if v % 3 != 1])
+
+
+@pytest.mark.parametrize("requests", [1, 3, 16, 17, 70])
+def test_decode_shared_by_few_and_many(requests):
+    """One to many 16-row groups per item, more requests than one item takes, every node shared."""
+    w = random_case(8, 2, 128, requests, lens=[300, 40, 129, 64], shared=0)
+    _decode(w, range(4))
+
+
+@pytest.mark.parametrize("policy", [(64, 1, 1, 1), (64, 3, 1, 2), (128, 16, 16, 4), (1024, 7, 2, 16)])
+@pytest.mark.parametrize("deferred", [False, True])
+def test_decode_policies(policy, deferred):
+    w = random_case(8, 2, 128, 20, lens=[700, 40, 129, 64, 333], shared=0)
+    _decode(w, [0, 2, 3], policy=policy, deferred=deferred)
+
+
+@pytest.mark.parametrize("cfg,frac", [(1, 0.5), (3, 0.5), (3, 1.0)])
+def test_decode_beside_the_tensor_memory_kernel(cfg, frac):
+    """Batches whose widely shared bf16 segments run on the side stream, while others are held in 4 bits: two reduced configurations."""
+    over = dict(n_requests=150, n_nodes=40, root_len=2500, len_lo=20, len_hi=300, suffix_max=60)
+    w = W.make_config(cfg, **over)
+    used = w.used_nodes()
+    rng = np.random.default_rng(4)
+    four = [int(v) for v in used if v != 0 and rng.random() < frac] + ([0] if frac == 1.0 else [])
+    _decode(w, four, source="device")
+
+
+@pytest.mark.parametrize("q_log2", [3, 5])
+def test_decode_peaked_scores(q_log2):
+    """Queries scaled up and planted keys: the running maximum moves late in the walk; scores reach hundreds."""
+    w = random_case(8, 2, 128, 5, lens=[400, 200, 100, 64], shared=0, q_scale_log2=q_log2, v_scale_log2=-2,
+                    planted=((0, 1, 0, 390, -1), (2, 6, 0, 170, -1), (4, 3, 0, 70, -1)))
+    _decode(w, range(4))
+
+
+def test_decode_large_and_tiny_value_scales():
+    """Values whose groups differ by 2^40 in size between tokens: a small token that carries the weight is not drowned by
+    a large one that carries none."""
+    d, n = 128, 100
+    rng = np.random.default_rng(11)
+    k = rng.standard_normal((n, 1, d)) * 0.1
+    q = rng.standard_normal((1, 1, d)) * 4
+    k[50] = q[0] * 8          # nearly all of the weight
+    v = rng.standard_normal((n, 1, d))
+    v[7] *= 2.0 ** 20
+    v[50] *= 2.0 ** -20
+    k, q, v = _bf16(k), _bf16(q), _bf16(v)
+    w = private_workload([n], [[0]], 1, 1, d)
+    pa = _handle(w, [0])
+    pa.write_node(0, 0, _tensor(k), _tensor(v))
+    pa.build()
+    out = pa.decode(0, _tensor(q)).double().cpu().numpy()
+    ref, _ = OA.decode([[0]], lambda _: (kv4.values(k), kv4.values(v)), q, 1)
+    assert pa.status() == 0
+    # one rounding of p to bf16 (2^-8) per term and the output's (2^-8), against the largest output of the head
+    assert np.abs(out - ref).max() <= 2.0 ** -7 * np.abs(ref).max()
+    pa.close()
+
+
+def test_constant_values_and_equal_keys():
+    """Equal keys give the mean of V; constant V comes back exactly (its groups are held exactly)."""
+    d, n = 64, 77
+    rng = np.random.default_rng(12)
+    k = np.broadcast_to(_bf16(rng.standard_normal((1, 2, d))), (n, 2, d)).copy()
+    v = np.full((n, 2, d), 0.7109375)
+    w = private_workload([n], [[0]], 4, 2, d)
+    pa = _handle(w, [0])
+    pa.write_node(0, 0, _tensor(k), _tensor(v))
+    pa.build()
+    q = torch.randn(1, 4, d, device="cuda").to(torch.bfloat16)
+    assert torch.equal(pa.decode(0, q), torch.full_like(q, 0.7109375))
+    pa.close()
+
+
+def test_mixed_with_residual_nodes_layers_streams_static_and_capture():
+    """4-bit nodes beside a node kept as base + residual, two layers; the static entry point, another stream and a replayed
+    graph give the same bits as the plain call."""
+    from paper_2605_22566_b200 import binding as B
+    lens = [200, 90, 64, 90]
+    w = private_workload(lens, [[0, 3], [1, 2], [3], [0, 2]], 8, 2, 128, layers=2)
+    pa = _handle(w, [0, 2], max_residual_nodes=1)
+    pa.write_nodes("host", skip=[3])
+    for layer in (0, 1):
+        assert B.gf_node_kv_attach_residual(pa.g, 3, layer, 1, None, None, pa.stream) == B.GF_OK   # node 3 = node 1 as it is
+    pa.build()
+    for layer in (0, 1):
+        q = pa.make_q(layer, "host")
+        out = pa.decode(layer, q)
+        view = View(w, [0, 2], layer)
+        ref, _ = OA.decode(view.paths(), lambda v: view.node_kv(1 if v == 3 else v), view.q(), 2)
+        assert_close(out.double().cpu().numpy(), ref, f"layer {layer}")
+        other = torch.zeros_like(out)
+        assert B.gf_path_attention_decode_static(pa.g, pa.tables, layer, q.data_ptr(), other.data_ptr(), None, pa.stream) == B.GF_OK
+        assert torch.equal(other, out)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            third = pa.decode(layer, q, out=torch.zeros_like(out))
+        side.synchronize()
+        assert torch.equal(third, out)
+        graph = torch.cuda.CUDAGraph()
+        fourth = torch.zeros_like(out)
+        with torch.cuda.graph(graph):
+            pa.decode(layer, q, out=fourth)
+        for _ in range(2):
+            fourth.zero_()
+            graph.replay()
+            assert torch.equal(fourth, out)
+    assert pa.status() == 0
+    pa.close()
+
+
+def test_extend_refuses_paths_through_4_bit_nodes():
+    from paper_2605_22566_b200 import binding as B
+    w = private_workload([70, 64, 10], [[0, 2], [1, 2]], 4, 2, 64)
+    pa = _handle(w, [1])
+    pa.write_nodes("host")
+    st, t = B.gf_build_path_tables(pa.g, 2, 4, pa.path_ptr.data_ptr(), pa.path_node.data_ptr(), B.GF_MODE_EXTEND, None, pa.stream)
+    assert st == B.GF_ERR_INVALID_PATH and B.gf_tables_bad_request(t) == 1
+    pa.close()
