@@ -88,6 +88,7 @@ typedef struct {
 /* Work-list policy (pure integer formula, applied per segment of length l shared by G requests):
  *   mult = min(max_chunk_mult, max(1, ceil(G / group_unit)));  n0 = ceil(l / (chunk_tokens*mult));
  *   chunk = 64*ceil(ceil(l / n0) / 64);  chunks = ceil(l / chunk);  tiles = ceil(G / group_tile).
+ * For a segment held in 4 bits mult is also at most 4.
  * chunk_tokens is a positive multiple of 64, group_tile is 1..16, the others are >= 1. */
 typedef struct {
   int32_t chunk_tokens;

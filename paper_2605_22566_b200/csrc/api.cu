@@ -20,8 +20,9 @@ struct gf_tables {
   int32_t bad_req = -1;
   int32_t max_q_rows = 0;
   int32_t num_wide = -1;       // items flagged wide; -1: not known on the host (deferred, or phase B still to run)
-  int32_t kv4_items = -1;      // items held in 4 bits, and their row groups; -1: not known on the host
-  int32_t kv4_units = -1;
+  int32_t kv4_items = -1;      // items held in 4 bits; their 16-row groups with up to 8 query rows, and the others;
+  int32_t kv4_rows8 = -1;      // -1: not known on the host
+  int32_t kv4_rows16 = -1;
   int32_t split_sms = 0;       // multiprocessors the tensor-memory decode kernel gets beside the warp kernel (0: one after the other)
   bool pending = false;        // deferred build: sizes and validity not read back yet
   cudaStream_t build_stream = nullptr;
@@ -734,7 +735,8 @@ static gf_status_t read_back_tables(gf_tables* T) {
   T->max_q_rows = h.max_q_rows;
   T->num_wide = h.num_wide;
   T->kv4_items = h.kv4_items;
-  T->kv4_units = h.kv4_units;
+  T->kv4_rows8 = h.kv4_rows8;
+  T->kv4_rows16 = h.kv4_rows16;
   T->owner->wide_hint = h.wide_units >= T->dev.wide_min_units;
   T->split_sms = h.num_wide > 0 ? decode_split(T->owner, h) : 0;
   T->owner->split_hint = T->split_sms;
@@ -826,7 +828,7 @@ gf_status_t gf_build_path_tables(gf_wgraph_t* g, int32_t num_requests, int32_t n
   }
   T.pending = false;
   T.num_wide = -1;
-  T.kv4_items = T.kv4_units = -1;
+  T.kv4_items = T.kv4_rows8 = T.kv4_rows16 = -1;
   T.error = GF_OK;
   T.build_stream = st;
   T.info = gf_tables_info_t{};
@@ -968,10 +970,10 @@ static int launch_decode_kernels(gf_wgraph* g, const gf_tables* t, const TablesD
   const int num_items = t->pending ? -1 : t->info.num_items;
   const ResidualEntry* residuals =
       g->res_rows_in_use > 0 ? g->res_table_dev + (size_t)layer * g->desc.max_residual_nodes : nullptr;
-  // segments held in 4 bits: a kernel of its own, last in the stream; the others have nothing to do when all are
-  const int kv4_units = g->kv4_nodes > 0 ? t->kv4_units : 0;
-  const bool only_kv4 = !t->pending && kv4_units > 0 && t->kv4_items == t->info.num_items;
-  if (only_kv4) return launch_decode4(g->pool4, g->shape, td, kv4_units, layer, q, g->status_dev, true, st);
+  // segments held in 4 bits: kernels of their own, last in the stream; the others have nothing to do when all are
+  const int rows8 = g->kv4_nodes > 0 ? t->kv4_rows8 : 0, rows16 = g->kv4_nodes > 0 ? t->kv4_rows16 : 0;
+  auto decode4 = [&](bool chained) { return launch_decode4(g->pool4, g->shape, td, rows8, rows16, layer, q, g->status_dev, chained, st); };
+  if (!t->pending && t->kv4_items > 0 && t->kv4_items == t->info.num_items) return decode4(true);
   const bool wide = td.wide_min_group > 0 && t->num_wide != 0;
   const int split = wide ? (t->pending ? g->split_hint : t->split_sms) : 0;
   if (wide && split > 0 && ensure_side_stream(g)) {
@@ -984,14 +986,14 @@ static int launch_decode_kernels(gf_wgraph* g, const gf_tables* t, const TablesD
     if (a < 0 || cudaEventRecord(g->ev_join, g->side_stream) != cudaSuccess) return -1;
     if (cudaStreamWaitEvent(st, g->ev_join, 0) != cudaSuccess || b < 0) return -1;
     *joined = true;
-    const int c = launch_decode4(g->pool4, g->shape, td, kv4_units, layer, q, g->status_dev, false, st);
+    const int c = decode4(false);
     return c < 0 ? -1 : a + b + c;
   }
   const int b = launch_decode(g->pool, g->shape, td, num_items, layer, q, g->status_dev, 0, residuals, st);
   if (b < 0) return -1;
   int a = 0;
   if (wide) a = launch_decode_wide(g->pool, g->shape, td, num_items, layer, q, g->status_dev, 0, 0, true, st);
-  const int c = launch_decode4(g->pool4, g->shape, td, kv4_units, layer, q, g->status_dev, true, st);
+  const int c = decode4(true);
   return a < 0 || c < 0 ? -1 : a + b + c;
 }
 

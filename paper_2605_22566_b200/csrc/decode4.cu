@@ -2,30 +2,36 @@
 //
 // Same units, partials and merge as decode.cu: for a chunk of one node's segment and up to 16 of the query
 // rows that share it, S^T = K Q^T (tokens are the MMA's rows), an online softmax with shuffles across the
-// token lanes, O^T += V^T P^T.  What differs is the operand: the MMAs multiply the codes themselves (c - 8,
-// exact in bf16), and a token's (s, lo) enter outside of them, in fp32:
-//   S_t = sum over groups G of  s_tG (q_G . (c - 8))  +  (lo_tG + 8.5 s_tG) (sum of q_G)
-//   O   = sum over tokens of  (p_t s_tG) (c - 8)  +  sum of  p_t (lo_tG + 8.5 s_tG)
-// so the scores carry no rounding but fp32's; p s is rounded to bf16 for the second product, as P is in the
-// bf16 kernel (the sum of p and the second term are not).
+// token lanes, O^T += V^T P^T.  What differs is the operand: the MMAs multiply the codes themselves, and a
+// token's (s, lo) enter outside of them, in fp32:
+//   S_t = sum over groups G of  s_tG (q_G . c)  +  (lo_tG + s_tG / 2) (sum of q_G)
+//   O   = sum over tokens of  (p_t s_tG) c  +  sum of  p_t (lo_tG + s_tG / 2)
+// What bounds it is the number of instructions that turn codes into operands.  A code in the low bits of an
+// fp16 pattern is the subnormal number c 2^-24, and one nibble up 16 c 2^-24: both exact MMA operands, so
+// eight codes take one shift and four ANDs, and the powers of two go into the scales.  Queries are fp16 times
+// a power of two per row (all eight bits of every entry down to 2^-31 of the row's largest), p s is fp16 times
+// one power of two per group, chosen with the softmax's reference; scores, sums, O and the terms without
+// codes are fp32.
 //
-// No shared memory and no barriers: the layout (kv4_device.cuh) gives every lane its MMA operands as 16-byte
-// pieces of the tile, so a warp reads them straight from global memory into registers, and every warp is
-// on its own: it takes a unit (from a counter, longest segments first), walks its tiles and writes the
-// partial.
+// Every warp is on its own: it takes units (an item's 16 query rows, or what is left of them) from a counter,
+// longest segments first, streams their tiles through a ring of its own in shared memory (bulk copies,
+// completion counted in bytes on mbarriers; the layout of kv4_device.cuh makes every operand load a
+// conflict-free 16 bytes per lane) and writes the partial.  The next unit is claimed while the current one
+// streams, a step of the claim (counter, list, item) per tile, so that none of its round trips is waited for.
+// Units of up to 8 rows use one column block of the MMA and run twelve warps to an SM, the others eight.
 #include "kv4_device.cuh"
 
 namespace gf {
 namespace {
 
 constexpr int kThreads = 128;
-
+constexpr int kWarps = kThreads / 32;
 struct Params {
   const char* pool_layer;
   uint64_t head_stride;
   int32_t tile_base;  // index of the 4-bit pool's first tile among all tiles
   const Item* items;
-  const int32_t* list;  // last entry; entry i is list[-i] = 4 * item + row group
+  const int32_t* list;  // the handle's unit lists (see TablesDev::wide_list)
   const int32_t* grp_req;
   const __nv_bfloat16* q;
   float* part_o;
@@ -38,65 +44,137 @@ struct Params {
   int32_t cap_tiles, num_pairs, num_requests;
 };
 
-template <int D>
+// D(16x8, fp32) += A(16x16, fp16, row) * B(16x8, fp16, col)
+__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// Four A registers from one word of codes: fp16 pairs c 2^-24 (registers 0 and 2) and 16 c 2^-24 (1 and 3).
+__device__ __forceinline__ void expand_f16(uint32_t (&a)[4], uint32_t w) {
+  const uint32_t v = w >> 8;
+  a[0] = w & 0x000f000fu;
+  a[1] = w & 0x00f000f0u;
+  a[2] = v & 0x000f000fu;
+  a[3] = v & 0x00f000f0u;
+}
+constexpr float kUnit0 = 16777216.f, kUnit1 = 1048576.f;  // what undoes them: 2^24, 2^20
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// 2^(t - e) for the exponent e of x (2^e <= x < 2^(e + 1)), held within 2^-100 .. 2^100; 1 for x = 0.
+__device__ __forceinline__ float pow2_to(float x, int t) {
+  if (!(x > 0.f)) return 1.f;
+  const int e = (int)(__float_as_uint(x) >> 23) - 127;
+  return __uint_as_float((uint32_t)(min(100, max(-100, t - e)) + 127) << 23);
+}
+
+// The state of one unit: 8 NT query rows over its tokens, a tile at a time.  Token rows 8..15 of a block come out of
+// the first product 16 times too large (registers 1 and 3 hold them), odd entries of O out of the second.
+template <int D, int NT>
 struct Warp4 {
   static constexpr int NG = D / kGroup4, KS = D / 16;
-  uint32_t qf[2][KS][2];
-  float qsum[2][NG][2];  // sum of a query row's entries per group, for this thread's two columns
-  float o[KS][2][4];
-  float oz[2][NG][2];    // sum over tokens of p (lo + 8.5 s), this thread's tokens
-  float m_run[2][2], l_run[2][2];
+  uint32_t qf[NT][KS][2];
+  float qsum[NT][NG][2];  // sum of a query row's entries per group, for this thread's two columns
+  float scale[NT][2];     // softmax scale in log2 units over the power of two that the row was multiplied by
+  float bias[NT][2];      // 0, or -inf for a row that does not exist (its p are 0)
+  float o[KS][NT][4];     // O^T in units of 2^-24 / f and 2^-20 / f
+  float oz[NT][NG][2];    // sum over tokens of p (lo + s / 2), this thread's tokens
+  float ref[NT][2], l_run[NT][2];
+  float f[NG];            // power of two that the second product's p s is multiplied by
+  float most[NG];         // upper bound of p s when the reference moved last
+
+  // Queries in fp16: a row is multiplied by the power of two that brings its largest entry to 2^14..2^15,
+  // which keeps all eight bits of every entry down to 2^-31 of the largest.
+  __device__ __forceinline__ void load_queries(const Params& p, int grp_begin, int row0, int kvh, int rows, int lane) {
+    const int l4 = lane & 3, l8 = lane >> 2, g = p.gqa;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const int row = j * 8 + l8;
+      const bool ok = row < rows;
+      int req = ok ? p.grp_req[GF_CLAMP(grp_begin + (row0 + row) / g, p.num_pairs, p.status, 122)] : 0;
+      req = GF_CLAMP(req, p.num_requests, p.status, 123);
+      const uint4* qrow = reinterpret_cast<const uint4*>(p.q + ((size_t)req * p.num_q_heads + kvh * g + (row0 + row) % g) * D);
+      uint4 v[D / 32];
+#pragma unroll
+      for (int x = 0; x < D / 32; ++x) v[x] = ok ? qrow[4 * x + l4] : make_uint4(0u, 0u, 0u, 0u);
+      float big = 0.f;
+#pragma unroll
+      for (int x = 0; x < D / 32; ++x) {
+        const uint32_t w[4] = {v[x].x, v[x].y, v[x].z, v[x].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          big = fmaxf(big, fmaxf(fabsf(__uint_as_float(w[i] << 16)), fabsf(__uint_as_float(w[i] & 0xffff0000u))));
+      }
+      big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
+      big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+      const float mul = pow2_to(big, 14);
+#pragma unroll
+      for (int x = 0; x < D / 32; ++x) {  // entries 32 x + 8 l4 .. + 7: MMAs 2 x and 2 x + 1
+        const uint32_t w[4] = {v[x].x, v[x].y, v[x].z, v[x].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          qf[j][2 * x + (i >> 1)][i & 1] = pack_f16(__uint_as_float(w[i] << 16) * mul, __uint_as_float(w[i] & 0xffff0000u) * mul);
+      }
+      // this thread's columns are the rows of the lanes 8 l4 and 8 l4 + 4
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        scale[j][c] = p.scale_log2 / __shfl_sync(0xffffffffu, mul, 8 * l4 + 4 * c);
+        bias[j][c] = j * 8 + 2 * l4 + c < rows ? 0.f : -INFINITY;
+      }
+    }
+  }
 
   __device__ __forceinline__ void init() {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+    for (int g = 0; g < NG; ++g) { f[g] = 1.f; most[g] = 0.f; }
 #pragma unroll
-      for (int c = 0; c < 2; ++c) { m_run[j][c] = -INFINITY; l_run[j][c] = 0.f; }
+    for (int j = 0; j < NT; ++j) {
 #pragma unroll
-      for (int g = 0; g < NG; ++g) oz[j][g][0] = oz[j][g][1] = 0.f;
+      for (int c = 0; c < 2; ++c) { ref[j][c] = bias[j][c] == 0.f ? -INFINITY : 0.f; l_run[j][c] = 0.f; }
 #pragma unroll
       for (int i = 0; i < KS; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[i][j][e] = 0.f;
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
-        const uint32_t ones[4] = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+        oz[j][g][0] = oz[j][g][1] = 0.f;
+        const uint32_t ones[4] = {0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u};
         float acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) mma_bf16(acc, ones, qf[j][g * 4 + kk][0], qf[j][g * 4 + kk][1]);
+        for (int kk = 0; kk < 4; ++kk) mma_f16(acc, ones, qf[j][g * 4 + kk][0], qf[j][g * 4 + kk][1]);
         qsum[j][g][0] = acc[0];
         qsum[j][g][1] = acc[1];
       }
     }
   }
 
-  // One tile: tokens 0..nv-1 of the 64 at `tile`.  NT: 8-row halves of the row group in use.
-  template <int NT, bool kMask>
-  __device__ __forceinline__ void step(const char* tile, int nv, float scale_log2, int lane) {
-    constexpr uint32_t kPart = kv4_part_bytes(D), kCodes = kv4_code_bytes(D);
-    const int l8 = lane >> 2;
-    const int nb = kMask ? (nv + 15) >> 4 : 4;  // blocks of 16 tokens that hold any
-    const uint4* kc = reinterpret_cast<const uint4*>(tile) + lane;
-    const uint4* vc = reinterpret_cast<const uint4*>(tile + kPart) + lane;
-    const uint32_t* ks = reinterpret_cast<const uint32_t*>(tile + kCodes);
-    const uint32_t* vs = reinterpret_cast<const uint32_t*>(tile + kPart + kCodes);
-    float s[4][NT][4];
+  // The (s, lo) words of this thread's tokens of block b: l8 and l8 + 8.
+  static __device__ __forceinline__ void load_words(uint32_t (&sl)[2][NG], const char* part, int b, int lane) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t* w = reinterpret_cast<const uint32_t*>(part + kv4_code_bytes(D)) + (b * 16 + (lane >> 2) + 8 * h) * NG;
+      if (NG == 2) {
+        const uint2 v = *reinterpret_cast<const uint2*>(w);
+        sl[h][0] = v.x;
+        sl[h][NG - 1] = v.y;
+      } else {
+        sl[h][0] = *w;
+      }
+    }
+  }
+
+  // The tile's scores in log2 units: x[b][j][2 h + c] of token 16 b + l8 + 8 h and this thread's column c.
+  __device__ __forceinline__ void scores(float (&x)[4][NT][4], const char* part, int nv, int lane) const {
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
-      if (kMask && b >= nb) {
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[b][j][e] = -INFINITY;
-        continue;
-      }
-#pragma unroll
-      for (int j = 0; j < NT; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[b][j][e] = 0.f;
+      uint32_t sl[2][NG];
+      load_words(sl, part, b, lane);
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
-        const uint4 c4 = kc[(b * NG + g) * 32];
+        const uint4 c4 = reinterpret_cast<const uint4*>(part)[(b * NG + g) * 32 + lane];
         const uint32_t w[4] = {c4.x, c4.y, c4.z, c4.w};
         float acc[NT][4];
 #pragma unroll
@@ -106,109 +184,143 @@ struct Warp4 {
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) {
           uint32_t a[4];
-          kv4_expand(a, w[kk]);
+          expand_f16(a, w[kk]);
 #pragma unroll
-          for (int j = 0; j < NT; ++j) mma_bf16(acc[j], a, qf[j][g * 4 + kk][0], qf[j][g * 4 + kk][1]);
+          for (int j = 0; j < NT; ++j) mma_f16(acc[j], a, qf[j][g * 4 + kk][0], qf[j][g * 4 + kk][1]);
         }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {  // tokens l8 and l8 + 8
-          const uint32_t sl = ks[(b * 16 + l8 + 8 * h) * NG + g];
-          const float sc = kv4_s(sl), z = fmaf(8.5f, sc, kv4_lo(sl));
+        for (int h = 0; h < 2; ++h) {
+          const float sc = kv4_s(sl[h][g]), z = fmaf(0.5f, sc, kv4_lo(sl[h][g])), su = sc * (h ? kUnit1 : kUnit0);
 #pragma unroll
           for (int j = 0; j < NT; ++j)
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
-              s[b][j][2 * h + c] = fmaf(acc[j][2 * h + c], sc, fmaf(qsum[j][g][c], z, s[b][j][2 * h + c]));
+            for (int c = 0; c < 2; ++c) {
+              const float zq = g ? fmaf(qsum[j][g][c], z, x[b][j][2 * h + c]) : qsum[j][g][c] * z;
+              x[b][j][2 * h + c] = fmaf(acc[j][2 * h + c], su, zq);
+            }
         }
       }
-    }
-    float mx[NT][2];
-#pragma unroll
-    for (int j = 0; j < NT; ++j) { mx[j][0] = -INFINITY; mx[j][1] = -INFINITY; }
-#pragma unroll
-    for (int b = 0; b < 4; ++b)
 #pragma unroll
       for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const bool on = !kMask || b * 16 + l8 + 8 * (e >> 1) < nv;
-          s[b][j][e] = on ? s[b][j][e] * scale_log2 : -INFINITY;
-          mx[j][e & 1] = fmaxf(mx[j][e & 1], s[b][j][e]);
-        }
-    bool grew = false;
+        for (int e = 0; e < 4; ++e) x[b][j][e] = fmaf(x[b][j][e], scale[j][e & 1], bias[j][e & 1]);
+    }
+    if (nv < kTile) {  // the last tile: tokens past the end
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (b * 16 + (lane >> 2) + 8 * (e >> 1) >= nv) x[b][j][e] = -INFINITY;
+    }
+  }
+
+  // Adds the tile to (O, l).  Any reference of the softmax is exact as long as p, l and O share it: it moves only
+  // when a score outgrew it by more than 2^8.  The second product's p s are fp16 times a power of two f, chosen
+  // whenever the reference moves so that the largest p s so far stands at 2^2..2^3; an s with which p s could
+  // pass fp16's range makes it move too.  Rounding them costs a token 2^-12 of its part at most, or 2^-27
+  // of the largest p s among the unit's rows.
+  __device__ __forceinline__ void accumulate(const float (&x)[4][NT][4], const char* part, int lane) {
+    uint32_t sl[4][2][NG];
+#pragma unroll
+    for (int b = 0; b < 4; ++b) load_words(sl[b], part, b, lane);
+    bool move = false;
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        float v = mx[j][c];
-        v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
-        v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
-        v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
-        mx[j][c] = fmaxf(v, m_run[j][c]);
-        grew |= mx[j][c] > m_run[j][c];
+        float m = fmaxf(x[0][j][c], x[0][j][2 + c]);
+#pragma unroll
+        for (int b = 1; b < 4; ++b) m = fmaxf(m, fmaxf(x[b][j][c], x[b][j][2 + c]));
+        move |= m > ref[j][c] + 8.f;
       }
-    if (__any_sync(0xffffffffu, grew)) {
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        float r[2];
+    for (int g = 0; g < NG; ++g) {
+      float m = 0.f;
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          r[c] = (mx[j][c] == -INFINITY) ? 0.f : fast_exp2(m_run[j][c] - mx[j][c]);
-          l_run[j][c] *= r[c];
-          m_run[j][c] = mx[j][c];
-#pragma unroll
-          for (int g = 0; g < NG; ++g) oz[j][g][c] *= r[c];
-        }
-#pragma unroll
-        for (int i = 0; i < KS; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[i][j][e] *= r[e & 1];
-      }
+      for (int b = 0; b < 4; ++b) m = fmaxf(m, fmaxf(kv4_s(sl[b][0][g]), kv4_s(sl[b][1][g])));
+      move |= m * f[g] > 128.f;
     }
-    float ref[NT][2];
-#pragma unroll
-    for (int j = 0; j < NT; ++j)
-#pragma unroll
-      for (int c = 0; c < 2; ++c) ref[j][c] = (m_run[j][c] == -INFINITY) ? 0.f : m_run[j][c];
+    if (__any_sync(0xffffffffu, move)) move_reference(x, sl);
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
-      if (kMask && b >= nb) continue;
-      float p[NT][4];
+      float pr[NT][4];
 #pragma unroll
       for (int j = 0; j < NT; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          p[j][e] = fast_exp2(s[b][j][e] - ref[j][e & 1]);
-          l_run[j][e & 1] += p[j][e];
+          pr[j][e] = fast_exp2(x[b][j][e] - ref[j][e & 1]);
+          l_run[j][e & 1] += pr[j][e];
         }
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
-        float sc[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t sl = vs[(b * 16 + l8 + 8 * h) * NG + g];
-          sc[h] = kv4_s(sl);
-          const float z = fmaf(8.5f, sc[h], kv4_lo(sl));
-#pragma unroll
-          for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int c = 0; c < 2; ++c) oz[j][g][c] = fmaf(p[j][2 * h + c], z, oz[j][g][c]);
-        }
         uint32_t pb[NT][2];
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
+        for (int h = 0; h < 2; ++h) {
+          const float sc = kv4_s(sl[b][h][g]), z = fmaf(0.5f, sc, kv4_lo(sl[b][h][g])), sf = sc * f[g];
 #pragma unroll
-          for (int h = 0; h < 2; ++h)  // P^T as the B operand: k = token, n = row
-            pb[j][h] = movmatrix_trans(pack_bf16(p[j][2 * h] * sc[h], p[j][2 * h + 1] * sc[h]));
-        const uint4 c4 = vc[(b * NG + g) * 32];
+          for (int j = 0; j < NT; ++j) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) oz[j][g][c] = fmaf(pr[j][2 * h + c], z, oz[j][g][c]);
+            // P^T as the B operand: k = token, n = row
+            pb[j][h] = movmatrix_trans(pack_f16(pr[j][2 * h] * sf, pr[j][2 * h + 1] * sf));
+          }
+        }
+        const uint4 c4 = reinterpret_cast<const uint4*>(part)[(b * NG + g) * 32 + lane];
         const uint32_t w[4] = {c4.x, c4.y, c4.z, c4.w};
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) {
           uint32_t a[4];
-          kv4_expand(a, w[kk]);
+          expand_f16(a, w[kk]);
 #pragma unroll
-          for (int j = 0; j < NT; ++j) mma_bf16(o[g * 4 + kk][j], a, pb[j][0], pb[j][1]);
+          for (int j = 0; j < NT; ++j) mma_f16(o[g * 4 + kk][j], a, pb[j][0], pb[j][1]);
         }
+      }
+    }
+  }
+
+  __device__ __forceinline__ void move_reference(const float (&x)[4][NT][4], const uint32_t (&sl)[4][2][NG]) {
+    float r[NT][2];
+    float down = 0.f;  // by how much the largest p so far shrinks at least: the largest r
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        float m = ref[j][c];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) m = fmaxf(m, fmaxf(x[b][j][c], x[b][j][2 + c]));
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+        r[j][c] = fast_exp2(ref[j][c] - m);  // 0 for the unit's first tile
+        ref[j][c] = m;
+        l_run[j][c] *= r[j][c];
+        if (bias[j][c] == 0.f) down = fmaxf(down, r[j][c]);
+      }
+#pragma unroll
+    for (int d = 1; d < 4; d <<= 1) down = fmaxf(down, __shfl_xor_sync(0xffffffffu, down, d));
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      float ps = 0.f;  // the tile's largest p s
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) ps = fmaxf(ps, fast_exp2(x[b][j][e] - ref[j][e & 1]) * kv4_s(sl[b][e >> 1][g]));
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) ps = fmaxf(ps, __shfl_xor_sync(0xffffffffu, ps, d));
+      most[g] = fmaxf(most[g] * down, ps);
+      const float fn = pow2_to(most[g], 2), ratio = fn / f[g];
+      f[g] = fn;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) oz[j][g][c] *= r[j][c];
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[g * 4 + kk][j][e] *= r[j][e & 1] * ratio;
       }
     }
   }
@@ -216,86 +328,193 @@ struct Warp4 {
   // Adds up what the token lanes hold apart: the row sums and the second term of O.
   __device__ __forceinline__ void finish_sums() {
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < NT; ++j)
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
+      for (int c = 0; c < 2; ++c)
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) {
           l_run[j][c] += __shfl_xor_sync(0xffffffffu, l_run[j][c], d);
 #pragma unroll
           for (int g = 0; g < NG; ++g) oz[j][g][c] += __shfl_xor_sync(0xffffffffu, oz[j][g][c], d);
         }
+  }
+};
+
+// Registers -> fp32 partial of the unit's rows row0 .. row0 + rows - 1.
+template <int D, int NT>
+__device__ __forceinline__ void write_partial(const Params& p, Warp4<D, NT>& wa, int part_base, int row0, int kvh, int rows, int lane) {
+  constexpr int NG = D / kGroup4;
+  wa.finish_sums();
+  const int l4 = lane & 3, l8 = lane >> 2, g = p.gqa;
+  float inv[NG];
+#pragma unroll
+  for (int gr = 0; gr < NG; ++gr) inv[gr] = kUnit1 / wa.f[gr];
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int row = j * 8 + l4 * 2 + c;
+      if (row < rows && GF_CHECK(part_base + (row0 + row) / g < p.slot_cap, p.status, 125)) {
+        const int srow = row0 + row;
+        const size_t ph = (size_t)(part_base + srow / g) * p.num_q_heads + kvh * g + srow % g;
+        float4* po = reinterpret_cast<float4*>(p.part_o + ph * D);
+#pragma unroll
+        for (int gr = 0; gr < NG; ++gr) {  // entries 8 l8 .. + 7 of the group
+          const float z = wa.oz[j][gr][c];
+          float v[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] = fmaf(wa.o[gr * 4 + (i >> 1)][j][2 * (i & 1) + c], (i & 1) ? inv[gr] : 16.f * inv[gr], z);
+          po[gr * 16 + l8 * 2] = make_float4(v[0], v[1], v[2], v[3]);
+          po[gr * 16 + l8 * 2 + 1] = make_float4(v[4], v[5], v[6], v[7]);
+        }
+        if (l8 == 0) *reinterpret_cast<float2*>(p.part_ml + ph * 2) = make_float2(wa.ref[j][c], wa.l_run[j][c]);
       }
+    }
+}
+
+// A unit in progress: what is needed when its first tile is consumed.
+struct __align__(16) Unit {
+  int32_t grp_begin, rows, part_base, tok_count;
+  int32_t kvh, row0, pad0, pad1;
+};
+
+// The claims of one warp (every lane calls; what they read is the same for all).
+struct Claims {
+  const int32_t* list;  // 4 * item + 16-row group of unit u: list[dir * (u / num_kv_heads)]
+  int dir, num_units, claimants;
+  int state = 0;  // 0 ask the counter, 1 read the list, 2 read the item, 3 ready, 4 no more
+  int u = 0, index = 0;
+  Item item;
+  // the first claim needs no counter: claimant i starts with unit i, and the counter counts from the last of those
+  __device__ __forceinline__ void first(int i) { u = i; state = 1; }
+  __device__ __forceinline__ void step(const Params& p, int lane) {
+    if (state == 0) {
+      if (lane == 0) u = atomicAdd(&p.counters[0], 1) + claimants;
+      state = 1;
+    } else if (state == 1) {
+      u = __shfl_sync(0xffffffffu, u, 0);
+      if (u >= num_units) {
+        state = 4;
+      } else {
+        index = list[(long long)dir * (u / p.num_kv_heads)];
+        state = 2;
+      }
+    } else if (state == 2) {
+      item = p.items[GF_CLAMP(index >> 2, p.slot_cap, p.status, 121)];
+      state = 3;
+    }
+  }
+  __device__ __forceinline__ Unit unit(const Params& p) const {
+    Unit x{};
+    x.grp_begin = item.grp_begin;
+    x.row0 = (index & 3) * 16;
+    x.rows = min(16, item.grp_count * p.gqa - x.row0);
+    x.part_base = item.part_base;
+    x.tok_count = item.tok_count;
+    x.kvh = u % p.num_kv_heads;
+    return x;
+  }
+  __device__ __forceinline__ const char* tiles(const Params& p, uint32_t tile_bytes) const {
+    return p.pool_layer + (uint64_t)(u % p.num_kv_heads) * p.head_stride +
+           (uint64_t)GF_CLAMP(item.tile0 - p.tile_base, p.cap_tiles, p.status, 124) * tile_bytes;
   }
 };
 
 template <int D>
-__global__ void __launch_bounds__(kThreads, 2) k_decode4(const Params p) {
-  constexpr int NG = D / kGroup4;
+struct __align__(16) WarpSmem {
+  unsigned char part[4][kv4_part_bytes(D)];  // K and V of two tiles
+  Unit unit[4];
+  uint64_t full[4];
+};
+
+// One warp's stream of tiles, K and V copied one after the other, two tiles ahead of their use.
+template <int D>
+struct TileStream {
+  const Params& p;
+  WarpSmem<D>& ws;
+  const int lane;
+  Claims& claims;
+  int issued = 0;             // tiles whose K was issued
+  int issue_units = 0;        // units whose issue has begun
+  int left = 0;               // tiles of the current one not issued yet
+  const char* src = nullptr;  // the tile whose K was issued last
+  const char *v_even = nullptr, *v_odd = nullptr;  // where V of the last even and odd tile lies
+  int v_issued = 0;
+
+  __device__ __forceinline__ void copy(int slot, const char* from) {
+    if (lane == 0) {
+      mbar_arrive_expect_tx(&ws.full[slot], kv4_part_bytes(D));
+      bulk_g2s(ws.part[slot], from, kv4_part_bytes(D), &ws.full[slot]);
+    }
+  }
+  // K of the next tile, V of the next tile: their slots must be free.
+  __device__ __forceinline__ void issue_k() {
+    if (left == 0) {
+      while (claims.state < 3) claims.step(p, lane);
+      if (claims.state == 4) return;
+      const Unit u = claims.unit(p);
+      if (lane == 0) ws.unit[issue_units & 3] = u;
+      ++issue_units;
+      left = (u.tok_count + kTile - 1) / kTile;
+      src = claims.tiles(p, kv4_tile_bytes(D));
+      claims.state = 0;
+    } else {
+      src += kv4_tile_bytes(D);
+      if (claims.state < 3) claims.step(p, lane);
+    }
+    copy(2 * (issued & 1), src);
+    if (issued & 1) v_odd = src + kv4_part_bytes(D);
+    else v_even = src + kv4_part_bytes(D);
+    --left;
+    ++issued;
+  }
+  __device__ __forceinline__ void issue_v() {
+    if (v_issued == issued) return;
+    copy(2 * (v_issued & 1) + 1, (v_issued & 1) ? v_odd : v_even);
+    ++v_issued;
+  }
+  __device__ __forceinline__ bool wait(int tile, int v) { return mbar_wait(&ws.full[2 * (tile & 1) + v], (tile >> 1) & 1, p.status); }
+  __device__ __forceinline__ const char* part(int tile, int v) const { return reinterpret_cast<const char*>(ws.part[2 * (tile & 1) + v]); }
+};
+
+template <int D, int NT>
+__global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) k_decode4(const Params p) {
+  extern __shared__ __align__(128) unsigned char smem[];
+  const int lane = threadIdx.x & 31;
+  WarpSmem<D>& ws = reinterpret_cast<WarpSmem<D>*>(smem)[threadIdx.x >> 5];
+  if (lane == 0) {
+    for (int i = 0; i < 4; ++i) mbar_init(&ws.full[i], 1);
+    mbar_fence_init();
+  }
+  __syncwarp();
   chain_enter();
-  const int lane = threadIdx.x & 31, l4 = lane & 3, l8 = lane >> 2, g = p.gqa;
-  const int num_units = tables_usable(*p.hdr, p.slot_cap) ? p.hdr->kv4_list_n * p.num_kv_heads : 0;
-  Warp4<D> wa;
-  while (true) {
-    int u = 0;
-    if (lane == 0) u = atomicAdd(&p.counters[0], 1);
-    u = __shfl_sync(0xffffffffu, u, 0);
-    if (u >= num_units) break;
-    const int entry = p.list[-(long long)(u / p.num_kv_heads)], kvh = u % p.num_kv_heads;
-    const Item it = p.items[GF_CLAMP(entry >> 2, p.slot_cap, p.status, 121)];
-    const int row0 = (entry & 3) * 16;
-    const int rows_here = min(16, it.grp_count * g - row0);
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int row = j * 8 + l8;
-      const bool ok = row < rows_here;
-      int req = ok ? p.grp_req[GF_CLAMP(it.grp_begin + (row0 + row) / g, p.num_pairs, p.status, 122)] : 0;
-      req = GF_CLAMP(req, p.num_requests, p.status, 123);
-      const uint4* qrow = reinterpret_cast<const uint4*>(p.q + ((size_t)req * p.num_q_heads + kvh * g + (row0 + row) % g) * D);
-#pragma unroll
-      for (int x = 0; x < D / 32; ++x) {  // entries 32 x + 8 l4 .. + 7: MMAs 2 x and 2 x + 1
-        const uint4 v = ok ? qrow[4 * x + l4] : make_uint4(0u, 0u, 0u, 0u);
-        wa.qf[j][2 * x][0] = v.x;
-        wa.qf[j][2 * x][1] = v.y;
-        wa.qf[j][2 * x + 1][0] = v.z;
-        wa.qf[j][2 * x + 1][1] = v.w;
-      }
-    }
+  const bool usable = tables_usable(*p.hdr, p.slot_cap);
+  Claims claims{NT == 1 ? p.list + p.slot_cap - 1 : p.list + p.hdr->kv4_rows16_first, NT == 1 ? -1 : 1,
+                usable ? (NT == 1 ? p.hdr->kv4_rows8_n : p.hdr->kv4_rows16_n) * p.num_kv_heads : 0, (int)gridDim.x * kWarps};
+  claims.first((int)blockIdx.x * kWarps + (threadIdx.x >> 5));
+  TileStream<D> ts{p, ws, lane, claims};
+  for (int i = 0; i < 2; ++i) { ts.issue_k(); ts.issue_v(); }
+  int tile = 0;
+  bool ok = true;
+  for (int n = 0; ok && tile < ts.issued; ++n) {
+    __syncwarp();
+    const Unit it = ws.unit[n & 3];
+    Warp4<D, NT> wa;
+    wa.load_queries(p, it.grp_begin, it.row0, it.kvh, it.rows, lane);
     wa.init();
-    const char* base = p.pool_layer + (uint64_t)kvh * p.head_stride;
-    const int ntile = (it.tok_count + kTile - 1) / kTile;
-    for (int t = 0; t < ntile; ++t) {
-      const int nv = it.tok_count - t * kTile;
-      const char* tile = base + (uint64_t)GF_CLAMP(it.tile0 - p.tile_base + t, p.cap_tiles, p.status, 124) * kv4_tile_bytes(D);
-      if (rows_here <= 8) {
-        if (nv >= kTile) wa.template step<1, false>(tile, kTile, p.scale_log2, lane);
-        else wa.template step<1, true>(tile, nv, p.scale_log2, lane);
-      } else {
-        if (nv >= kTile) wa.template step<2, false>(tile, kTile, p.scale_log2, lane);
-        else wa.template step<2, true>(tile, nv, p.scale_log2, lane);
-      }
+    for (int left = it.tok_count; left > 0; left -= kTile, ++tile) {
+      float x[4][NT][4];
+      if (!(ok = ts.wait(tile, 0))) break;
+      wa.scores(x, ts.part(tile, 0), left, lane);
+      __syncwarp();
+      ts.issue_k();
+      if (!(ok = ts.wait(tile, 1))) break;
+      wa.accumulate(x, ts.part(tile, 1), lane);
+      __syncwarp();
+      ts.issue_v();
     }
-    wa.finish_sums();
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const int row = j * 8 + l4 * 2 + c;
-        if (row < rows_here && GF_CHECK(it.part_base + (row0 + row) / g < p.slot_cap, p.status, 125)) {
-          const int srow = row0 + row;
-          const size_t ph = (size_t)(it.part_base + srow / g) * p.num_q_heads + kvh * g + srow % g;
-          float4* po = reinterpret_cast<float4*>(p.part_o + ph * D);
-#pragma unroll
-          for (int gr = 0; gr < NG; ++gr) {  // entries 8 l8 .. + 7 of the group
-            const float z = wa.oz[j][gr][c];
-            po[gr * 16 + l8 * 2] = make_float4(wa.o[gr * 4][j][c] + z, wa.o[gr * 4][j][2 + c] + z,
-                                               wa.o[gr * 4 + 1][j][c] + z, wa.o[gr * 4 + 1][j][2 + c] + z);
-            po[gr * 16 + l8 * 2 + 1] = make_float4(wa.o[gr * 4 + 2][j][c] + z, wa.o[gr * 4 + 2][j][2 + c] + z,
-                                                   wa.o[gr * 4 + 3][j][c] + z, wa.o[gr * 4 + 3][j][2 + c] + z);
-          }
-          if (l8 == 0) *reinterpret_cast<float2*>(p.part_ml + ph * 2) = make_float2(wa.m_run[j][c], wa.l_run[j][c]);
-        }
-      }
+    if (!ok) break;
+    write_partial(p, wa, it.part_base, it.row0, it.kvh, it.rows, lane);
   }
   // the last CTA to run out of work re-arms the counters for the next launch
   __syncthreads();
@@ -310,15 +529,15 @@ __global__ void __launch_bounds__(kThreads, 2) k_decode4(const Params p) {
 
 }  // namespace
 
-int launch_decode4(const PoolGeom& pool, const AttnShape& sh, const TablesDev& t, int num_units, int layer, const void* q,
-                   int32_t* status, bool chained, cudaStream_t st) {
-  if (num_units == 0) return 0;
+int launch_decode4(const PoolGeom& pool, const AttnShape& sh, const TablesDev& t, int rows8, int rows16, int layer,
+                   const void* q, int32_t* status, bool chained, cudaStream_t st) {
+  if (rows8 == 0 && rows16 == 0) return 0;
   Params p;
   p.pool_layer = pool.base + (uint64_t)layer * pool.layer_stride;
   p.head_stride = pool.head_stride;
   p.tile_base = t.kv4_tile0;
   p.items = t.items;
-  p.list = t.wide_list + t.slot_cap - 1;
+  p.list = t.wide_list;
   p.grp_req = t.grp_req;
   p.q = (const __nv_bfloat16*)q;
   p.part_o = t.part_o;
@@ -334,16 +553,24 @@ int launch_decode4(const PoolGeom& pool, const AttnShape& sh, const TablesDev& t
   p.cap_tiles = (int32_t)pool.cap_tiles;
   p.num_pairs = t.num_pairs_in;
   p.num_requests = t.num_requests;
-  const long long warps = num_units < 0 ? (1ll << 40) : (long long)num_units * sh.num_kv_heads;
-  const long long blocks = (warps + kThreads / 32 - 1) / (kThreads / 32), most = 2ll * t.num_sms;
-  const dim3 grid((unsigned)(blocks < most ? blocks : most));
-  auto go = [&](auto kernel) {
-    if (chained) launch_chained(kernel, grid, dim3(kThreads), 0, st, p);
-    else kernel<<<grid, dim3(kThreads), 0, st>>>(p);  // behind a join with another stream
+  auto go = [&](auto kernel, size_t smem, int units, int per_sm, bool (&optin)[kMaxDevices]) {
+    if (units == 0) return true;
+    if (!ensure_dynamic_smem(kernel, smem, optin)) return false;
+    const long long warps = units < 0 ? (1ll << 40) : (long long)units * sh.num_kv_heads;
+    const long long blocks = (warps + kWarps - 1) / kWarps, most = (long long)per_sm * t.num_sms;
+    const dim3 grid((unsigned)(blocks < most ? blocks : most));
+    if (chained) launch_chained(kernel, grid, dim3(kThreads), smem, st, p);
+    else kernel<<<grid, dim3(kThreads), smem, st>>>(p);  // behind a join with another stream
+    chained = true;
+    return true;
   };
-  if (sh.head_dim == 128) go(k_decode4<128>);
-  else go(k_decode4<64>);
-  return cudaGetLastError() == cudaSuccess ? 1 : -1;
+  static bool optin[4][kMaxDevices] = {};
+  const bool ok = sh.head_dim == 128 ? go(k_decode4<128, 2>, kWarps * sizeof(WarpSmem<128>), rows16, 2, optin[0]) &&
+                                           go(k_decode4<128, 1>, kWarps * sizeof(WarpSmem<128>), rows8, 3, optin[1])
+                                     : go(k_decode4<64, 2>, kWarps * sizeof(WarpSmem<64>), rows16, 2, optin[2]) &&
+                                           go(k_decode4<64, 1>, kWarps * sizeof(WarpSmem<64>), rows8, 3, optin[3]);
+  if (!ok) return -1;
+  return cudaGetLastError() == cudaSuccess ? (rows16 != 0) + (rows8 != 0) : -1;
 }
 
 }  // namespace gf

@@ -52,8 +52,11 @@ struct Header {
   int32_t wide_tile_units;  // (chunk x 128-row tile) pairs of the wide kernel per KV head: each loads queries and writes partials
   int32_t stream_steps;     // work of the warp kernel per KV head, in (64-token tile x 16-row group) steps
   int32_t kv4_items;   // items of segments held in 4 bits
-  int32_t kv4_units;   // their (item, 16-row group) pairs: the length the list below will have
-  int32_t kv4_list_n;  // pairs listed for the 4-bit decode kernel (from the end of wide_list)
+  int32_t kv4_rows8;   // their 16-row groups that hold up to 8 query rows, and the others
+  int32_t kv4_rows16;
+  int32_t kv4_rows8_n;   // how many of either are listed for the 4-bit decode kernels
+  int32_t kv4_rows16_n;
+  int32_t kv4_rows16_first;  // where the list of the latter starts
   int32_t kv4_tokens;  // tokens of the segments held in 4 bits
   unsigned long long resident_tokens;
   unsigned long long materialised_tokens;
@@ -110,9 +113,10 @@ struct TablesDev {
   Item* items;         // [num_items]   (carved after the read-back)
   int32_t* mrg_slot;   // [num_slots]   (carved after the read-back)
   int32_t* wide_list;  // [wide_list_n] item index of the first item of every wide unit, any order;
-                       // from the last of its slot_cap entries backwards, [kv4_list_n]: 4 * item + row
-                       // group of every 16-row group of the items held in 4 bits, any order.  A wide unit
-                       // and a row group each stand for one partial slot at least, so the two never meet
+                       // behind them [kv4_rows16_n] 4 * item + row group of the 16-row groups of the items
+                       // held in 4 bits, and from the last of its slot_cap entries backwards [kv4_rows8_n]
+                       // those that hold up to 8 rows.  A wide unit and a row group each stand for one
+                       // partial slot at least, so the lists never meet
   float* part_o;       // [num_slots, Hq, D] fp32 un-normalised partial outputs
   float* part_ml;      // [num_slots, Hq, 2] running max (log2 units) and sum
   const int32_t* node_res;  // [num_nodes] the graph's residual rows (see GraphDev)
@@ -126,6 +130,10 @@ struct TablesDev {
   int32_t wide_unit_req;   // requests per unit of the wide kernel: 256 stacked query rows / GQA group size
   int32_t kv4_tile0;       // pool tiles from this index on lie in the 4-bit pool (at tile - kv4_tile0 there)
 };
+
+// Longest chunk of a segment held in 4 bits, in multiples of the policy's chunk_tokens: its kernel gives a chunk's
+// 16 query rows to one warp, which has to come to an end.
+constexpr int kKv4ChunkMult = 4;
 
 // True when the tables on the device are usable: every path valid and the items / partial slots fit
 // the room the host carved for them.  Kernels that consume the tables do nothing otherwise.
@@ -284,9 +292,10 @@ int launch_kv4_write(const PoolGeom& pool, int layer, int num_kv_heads, int head
                      const void* v, int n_tokens, const GraphDev* set, int node, int token_off, int num_sms, cudaStream_t st);
 int launch_kv4_read(const PoolGeom& pool, int layer, int num_kv_heads, int head_dim, int tile0, void* k, void* v,
                     int n_tokens, int num_sms, cudaStream_t st);
-// num_units: (item, row group) pairs, < 0: not known on the host.  chained: see launch_decode_wide.
-int launch_decode4(const PoolGeom& pool, const AttnShape& sh, const TablesDev& t, int num_units, int layer, const void* q,
-                   int32_t* status, bool chained, cudaStream_t st);
+// rows8, rows16: 16-row groups with up to 8 query rows and the others, < 0: not known on the host.
+// chained: see launch_decode_wide.
+int launch_decode4(const PoolGeom& pool, const AttnShape& sh, const TablesDev& t, int rows8, int rows16, int layer,
+                   const void* q, int32_t* status, bool chained, cudaStream_t st);
 int launch_weights(const PoolGeom& pool16, const PoolGeom& pool4, const AttnShape& sh, const TablesDev& t, int layer, const void* q,
                    const float* lse, int accumulate, float* weights, int64_t slots, int32_t* status, cudaStream_t st);
 int launch_evict(const PoolGeom& pool16, const PoolGeom& pool4, const EvictBatch& batch, int num_layers, int num_kv_heads,

@@ -83,7 +83,7 @@ __global__ void k_init(TablesDev t, int num_nodes) {
     h.wide_tokens = 0;
     h.wide_tile_units = 0;
     h.stream_steps = 0;
-    h.kv4_items = h.kv4_units = h.kv4_list_n = h.kv4_tokens = 0;
+    h.kv4_items = h.kv4_rows8 = h.kv4_rows16 = h.kv4_rows8_n = h.kv4_rows16_n = h.kv4_rows16_first = h.kv4_tokens = 0;
     h.max_q_rows = 0;
     h.resident_tokens = h.materialised_tokens = h.num_q_rows = 0ull;
     *t.hdr = h;
@@ -228,7 +228,9 @@ __global__ void k_scan_nodes_segments(GraphDev g, TablesDev t, gf_policy_t pol) 
   for (int s = tid; s < S; s += blockDim.x) {
     const int G = t.grp_ptr[s];
     const int l = t.seg_len[s];
-    const int mult = min(pol.max_chunk_mult, max(1, ceil_div(G, pol.group_unit)));
+    const bool four = t.seg_off[s] / kTile >= t.kv4_tile0;
+    const int most = four ? min(pol.max_chunk_mult, kKv4ChunkMult) : pol.max_chunk_mult;
+    const int mult = min(most, max(1, ceil_div(G, pol.group_unit)));
     const int n0 = ceil_div(l, pol.chunk_tokens * mult);
     const int chunk = kTile * ceil_div(ceil_div(l, n0), kTile);
     const int nchunk = ceil_div(l, chunk);
@@ -236,12 +238,14 @@ __global__ void k_scan_nodes_segments(GraphDev g, TablesDev t, gf_policy_t pol) 
     t.seg_nchunk[s] = nchunk;
     t.seg_item_base[s] = nchunk * ceil_div(G, pol.group_tile);
     t.seg_part_base[s] = nchunk * G;
-    if (t.seg_off[s] / kTile >= t.kv4_tile0) {
-      // held in 4 bits: a kernel of its own, a unit of which is one 16-row group of an item
-      const int gqa = 256 / t.wide_unit_req;
-      const int groups = (G / pol.group_tile) * ceil_div(pol.group_tile * gqa, 16) + ceil_div((G % pol.group_tile) * gqa, 16);
+    if (four) {
+      // held in 4 bits: kernels of their own, a unit of which is one 16-row group of an item
+      const int gqa = 256 / t.wide_unit_req, full = G / pol.group_tile, rows = pol.group_tile * gqa, last = (G % pol.group_tile) * gqa;
+      const int r16 = full * (rows / 16 + (rows % 16 > 8)) + last / 16 + (last % 16 > 8);
+      const int groups = full * ceil_div(rows, 16) + ceil_div(last, 16);
       atomicAdd(&t.hdr->kv4_items, nchunk * ceil_div(G, pol.group_tile));
-      atomicAdd(&t.hdr->kv4_units, nchunk * groups);
+      atomicAdd(&t.hdr->kv4_rows16, nchunk * r16);
+      atomicAdd(&t.hdr->kv4_rows8, nchunk * (groups - r16));
       atomicAdd(&t.hdr->kv4_tokens, l);
       continue;
     }
@@ -272,6 +276,7 @@ __global__ void k_scan_nodes_segments(GraphDev g, TablesDev t, gf_policy_t pol) 
     t.hdr->wide_tile_units = wide_tile_units;
     t.hdr->stream_steps = stream_steps;
     if (wide_units < t.wide_min_units) t.hdr->num_wide = 0;
+    t.hdr->kv4_rows16_first = t.hdr->num_wide > 0 ? wide_units : 0;
   }
   __syncthreads();
   int tot[3];
@@ -460,10 +465,17 @@ __device__ void emit_item(const TablesDev& t, const gf_policy_t& pol, int i, con
     if (GF_CHECK(at < t.slot_cap, t.status, 305)) t.wide_list[at] = i;
   }
   if (four) {
-    const int groups = ceil_div(it.grp_count * (256 / t.wide_unit_req), 16);
-    const int at = atomicAdd(&t.hdr->kv4_list_n, groups);
-    for (int k = 0; k < groups; ++k)
-      if (GF_CHECK(at + k < t.slot_cap, t.status, 308)) t.wide_list[t.slot_cap - 1 - at - k] = 4 * i + k;
+    const int rows = it.grp_count * (256 / t.wide_unit_req);
+    const int r16 = rows / 16 + (rows % 16 > 8);
+    if (r16 > 0) {
+      const int at = t.hdr->kv4_rows16_first + atomicAdd(&t.hdr->kv4_rows16_n, r16);
+      for (int k = 0; k < r16; ++k)
+        if (GF_CHECK(at + k < t.slot_cap, t.status, 308)) t.wide_list[at + k] = 4 * i + k;
+    }
+    if (r16 * 16 < rows) {
+      const int at = t.slot_cap - 1 - atomicAdd(&t.hdr->kv4_rows8_n, 1);
+      if (GF_CHECK(at >= 0, t.status, 309)) t.wide_list[at] = 4 * i + r16;
+    }
   }
 }
 
