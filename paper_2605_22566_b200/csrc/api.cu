@@ -997,6 +997,15 @@ static int launch_decode_kernels(gf_wgraph* g, const gf_tables* t, const TablesD
   return a < 0 || c < 0 ? -1 : a + b + c;
 }
 
+// Few (request, head) rows with many partial slots each leave most of the GPU idle under a warp per row (one
+// request over 57 000 tokens: 224 slots a row, 30 us of merge).  Only for batches with 4-bit segments, whose
+// chunks are the shorter ones; the others' results stay what they were bit for bit.
+static bool merge_is_split(const gf_wgraph* g, const gf_tables* t) {
+  if (t->pending || t->kv4_items <= 0) return false;
+  const int64_t rows = (int64_t)t->info.num_requests * g->shape.num_q_heads;
+  return rows <= 8ll * g->num_sms && t->info.num_slots > 32ll * t->info.num_requests;
+}
+
 gf_status_t gf_path_attention_decode(gf_wgraph_t* g, const gf_tables_t* t, int32_t layer,
                                      const void* q_dev, void* out_dev, float* lse_dev, void* stream) {
   gf_status_t s = check_attention_args(g, t, layer, q_dev, out_dev, GF_MODE_DECODE);
@@ -1006,7 +1015,7 @@ gf_status_t gf_path_attention_decode(gf_wgraph_t* g, const gf_tables_t* t, int32
   int n = timed(g, kSpanDecode, st, [&] { return launch_decode_kernels(g, t, t->dev, layer, q_dev, st, &joined); });
   if (n < 0) return GF_ERR_CUDA;
   g->launches += n;
-  n = timed(g, kSpanMerge, st, [&] { return launch_merge(g->shape, t->dev, out_dev, lse_dev, !joined, st); });
+  n = timed(g, kSpanMerge, st, [&] { return launch_merge(g->shape, t->dev, out_dev, lse_dev, !joined, merge_is_split(g, t), st); });
   if (n < 0) return GF_ERR_CUDA;
   g->launches += n;
   return GF_OK;
@@ -1345,7 +1354,7 @@ extern "C" gf_status_t gf_path_attention_decode_static(gf_wgraph_t* g, const gf_
   int n = timed(g, kSpanDecode, st, [&] { return launch_decode_kernels(g, t, td, layer, q_dev, st, &joined); });
   if (n < 0) return GF_ERR_CUDA;
   g->launches += n;
-  n = timed(g, kSpanMerge, st, [&] { return launch_merge(g->shape, td, out_dev, lse_dev, !joined, st); });
+  n = timed(g, kSpanMerge, st, [&] { return launch_merge(g->shape, td, out_dev, lse_dev, !joined, merge_is_split(g, t), st); });
   if (n < 0) return GF_ERR_CUDA;
   g->launches += n;
   return GF_OK;

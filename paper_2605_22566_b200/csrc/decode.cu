@@ -433,6 +433,79 @@ __global__ void __launch_bounds__(kDecodeThreads, 2) k_decode(const DecodeParams
   }
 }
 
+// What a warp has gathered of one (request, query head)'s partials: M = max m, L = sum 2^(m - M) l and, in lanes
+// 0 .. D/4 - 1, four columns each of sum 2^(m - M) o.
+struct Merged {
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  float L = 0.f, M = -INFINITY;
+  __device__ __forceinline__ void rescale(float Mn) {
+    const float resc = (M == -INFINITY) ? 0.f : fast_exp2(M - Mn);
+    acc.x *= resc; acc.y *= resc; acc.z *= resc; acc.w *= resc;
+    L *= resc;
+    M = Mn;
+  }
+};
+
+// Slots first, first + 1, ..., 32 at a time, `stride` apart from batch to batch: lane i fetches slot index and (m, l)
+// of the i-th; the maximum of the batch is folded into the running one, then the partial rows are read four at a
+// time (independent loads).
+template <int D>
+__device__ __forceinline__ void merge_slots(Merged& a, const float* __restrict__ part_o, const float* __restrict__ part_ml,
+                                            const int32_t* __restrict__ mrg_slot, int first, int end, int stride, int h,
+                                            int num_q_heads, int slot_cap, int32_t* status, int lane) {
+  constexpr int kLanes = D / 4;  // lanes that carry output columns
+  for (int base = first; base < end; base += stride) {
+    const int cnt = min(32, end - base);
+    int slot = 0;
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (lane < cnt) {
+      slot = mrg_slot[base + lane];
+      slot = GF_CLAMP(slot, slot_cap, status, 111);
+      ml = *reinterpret_cast<const float2*>(part_ml + ((size_t)slot * num_q_heads + h) * 2);
+    }
+    float mb = ml.x;
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) mb = fmaxf(mb, __shfl_xor_sync(0xffffffffu, mb, d));
+    a.rescale(fmaxf(a.M, mb));
+    const float wl = (ml.x == -INFINITY) ? 0.f : fast_exp2(ml.x - a.M);
+    float lsum = wl * ml.y;
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) lsum += __shfl_xor_sync(0xffffffffu, lsum, d);
+    a.L += lsum;
+    for (int i0 = 0; i0 < cnt; i0 += 4) {
+      float4 v[4];
+      float w[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int i = min(i0 + k, cnt - 1);
+        const int sl = __shfl_sync(0xffffffffu, slot, i);
+        w[k] = (i0 + k < cnt) ? __shfl_sync(0xffffffffu, wl, i) : 0.f;
+        v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (lane < kLanes)
+          v[k] = *reinterpret_cast<const float4*>(part_o + ((size_t)sl * num_q_heads + h) * D + lane * 4);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        a.acc.x += w[k] * v[k].x; a.acc.y += w[k] * v[k].y; a.acc.z += w[k] * v[k].z; a.acc.w += w[k] * v[k].w;
+      }
+    }
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void write_merged(const Merged& a, int r, int h, int num_q_heads, __nv_bfloat16* __restrict__ out,
+                                             float* __restrict__ lse, int lane) {
+  const float inv = (a.L > 0.f) ? 1.f / a.L : 0.f;
+  if (lane < D / 4) {
+    uint2 packed;
+    packed.x = pack_bf16(a.acc.x * inv, a.acc.y * inv);
+    packed.y = pack_bf16(a.acc.z * inv, a.acc.w * inv);
+    *reinterpret_cast<uint2*>(out + ((size_t)r * num_q_heads + h) * D + lane * 4) = packed;
+  }
+  if (lse != nullptr && lane == 0)
+    lse[(size_t)r * num_q_heads + h] = (a.L > 0.f) ? (a.M + log2f(a.L)) * 0.6931471805599453f : -INFINITY;
+}
+
 // K4.  One warp per (request, query head): out = sum_i w_i o_i / sum_i w_i l_i with
 // w_i = 2^(m_i - max m) over the request's partial slots; lse in natural-log units.
 template <int D>
@@ -450,60 +523,43 @@ __global__ void __launch_bounds__(256) k_merge(const float* __restrict__ part_o,
   const int r = gw / num_q_heads, h = gw % num_q_heads;
   int b = mrg_ptr[r], e = mrg_ptr[r + 1];
   if (!GF_CHECK(b >= 0 && b <= e && e <= slot_cap, status, 110)) e = b = 0;
-  constexpr int kLanes = D / 4;  // lanes that carry output columns
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  float L = 0.f, M = -INFINITY;
-  // 32 slots at a time: lane i fetches slot index and (m, l) of the i-th; the maximum of the batch is
-  // folded into the running one, then the partial rows are read four at a time (independent loads).
-  for (int base = b; base < e; base += 32) {
-    const int cnt = min(32, e - base);
-    int slot = 0;
-    float2 ml = make_float2(-INFINITY, 0.f);
-    if (lane < cnt) {
-      slot = mrg_slot[base + lane];
-      slot = GF_CLAMP(slot, slot_cap, status, 111);
-      ml = *reinterpret_cast<const float2*>(part_ml + ((size_t)slot * num_q_heads + h) * 2);
-    }
-    float mb = ml.x;
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) mb = fmaxf(mb, __shfl_xor_sync(0xffffffffu, mb, d));
-    const float Mn = fmaxf(M, mb);
-    const float resc = (M == -INFINITY) ? 0.f : fast_exp2(M - Mn);
-    acc.x *= resc; acc.y *= resc; acc.z *= resc; acc.w *= resc;
-    L *= resc;
-    M = Mn;
-    const float wl = (ml.x == -INFINITY) ? 0.f : fast_exp2(ml.x - M);
-    float lsum = wl * ml.y;
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) lsum += __shfl_xor_sync(0xffffffffu, lsum, d);
-    L += lsum;
-    for (int i0 = 0; i0 < cnt; i0 += 4) {
-      float4 v[4];
-      float w[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int i = min(i0 + k, cnt - 1);
-        const int sl = __shfl_sync(0xffffffffu, slot, i);
-        w[k] = (i0 + k < cnt) ? __shfl_sync(0xffffffffu, wl, i) : 0.f;
-        v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (lane < kLanes)
-          v[k] = *reinterpret_cast<const float4*>(part_o + ((size_t)sl * num_q_heads + h) * D + lane * 4);
-      }
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        acc.x += w[k] * v[k].x; acc.y += w[k] * v[k].y; acc.z += w[k] * v[k].z; acc.w += w[k] * v[k].w;
-      }
-    }
+  Merged a;
+  merge_slots<D>(a, part_o, part_ml, mrg_slot, b, e, 32, h, num_q_heads, slot_cap, status, lane);
+  write_merged<D>(a, r, h, num_q_heads, out, lse, lane);
+}
+
+// The same for few rows with many slots each (one request over a long context): the eight warps of a CTA share the
+// slots of one row, 32 in turn, and join what they have in shared memory.
+template <int D>
+__global__ void __launch_bounds__(256) k_merge_split(const float* __restrict__ part_o, const float* __restrict__ part_ml,
+                                                     const int32_t* __restrict__ mrg_ptr, const int32_t* __restrict__ mrg_slot,
+                                                     int num_requests, int num_q_heads, __nv_bfloat16* __restrict__ out,
+                                                     float* __restrict__ lse, const Header* __restrict__ hdr, int slot_cap,
+                                                     int32_t* status) {
+  __shared__ float4 acc[8][32];
+  __shared__ float2 ml[8];
+  chain_enter();
+  if (!tables_usable(*hdr, slot_cap)) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int r = blockIdx.x / num_q_heads, h = blockIdx.x % num_q_heads;
+  int b = mrg_ptr[r], e = mrg_ptr[r + 1];
+  if (!GF_CHECK(b >= 0 && b <= e && e <= slot_cap, status, 112)) e = b = 0;
+  Merged a;
+  merge_slots<D>(a, part_o, part_ml, mrg_slot, b + warp * 32, e, 256, h, num_q_heads, slot_cap, status, lane);
+  acc[warp][lane] = a.acc;
+  if (lane == 0) ml[warp] = make_float2(a.M, a.L);
+  __syncthreads();
+  if (warp != 0) return;
+  for (int w = 1; w < 8; ++w) {
+    const float2 x = ml[w];
+    if (x.x == -INFINITY) continue;
+    const float4 v = acc[w][lane];
+    a.rescale(fmaxf(a.M, x.x));
+    const float f = fast_exp2(x.x - a.M);
+    a.L += f * x.y;
+    a.acc.x += f * v.x; a.acc.y += f * v.y; a.acc.z += f * v.z; a.acc.w += f * v.w;
   }
-  const float inv = (L > 0.f) ? 1.f / L : 0.f;
-  if (lane < kLanes) {
-    uint2 packed;
-    packed.x = pack_bf16(acc.x * inv, acc.y * inv);
-    packed.y = pack_bf16(acc.z * inv, acc.w * inv);
-    *reinterpret_cast<uint2*>(out + ((size_t)r * num_q_heads + h) * D + lane * 4) = packed;
-  }
-  if (lse != nullptr && lane == 0)
-    lse[(size_t)r * num_q_heads + h] = (L > 0.f) ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+  write_merged<D>(a, r, h, num_q_heads, out, lse, lane);
 }
 
 template <int D, bool kRes>
@@ -574,10 +630,10 @@ int launch_decode(const PoolGeom& pool, const AttnShape& sh, const TablesDev& t,
   return cudaGetLastError() == cudaSuccess ? 1 : -1;
 }
 
-int launch_merge(const AttnShape& sh, const TablesDev& t, void* out, float* lse, bool chained, cudaStream_t st) {
-  const long long warps = (long long)t.num_requests * sh.num_q_heads;
-  if (warps <= 0) return 0;
-  const unsigned blocks = (unsigned)((warps * 32 + 255) / 256);
+int launch_merge(const AttnShape& sh, const TablesDev& t, void* out, float* lse, bool chained, bool split, cudaStream_t st) {
+  const long long rows = (long long)t.num_requests * sh.num_q_heads;
+  if (rows <= 0) return 0;
+  const unsigned blocks = (unsigned)(split ? rows : (rows * 32 + 255) / 256);
   auto go = [&](auto kernel) {
     if (chained)
       launch_chained(kernel, dim3(blocks), dim3(256), 0, st, t.part_o, t.part_ml, t.mrg_ptr, t.mrg_slot, t.num_requests,
@@ -586,8 +642,8 @@ int launch_merge(const AttnShape& sh, const TablesDev& t, void* out, float* lse,
       kernel<<<dim3(blocks), dim3(256), 0, st>>>(t.part_o, t.part_ml, t.mrg_ptr, t.mrg_slot, t.num_requests, sh.num_q_heads,
                                                  (__nv_bfloat16*)out, lse, t.hdr, t.slot_cap, t.status);
   };
-  if (sh.head_dim == 128) go(k_merge<128>);
-  else go(k_merge<64>);
+  if (sh.head_dim == 128) split ? go(k_merge_split<128>) : go(k_merge<128>);
+  else split ? go(k_merge_split<64>) : go(k_merge<64>);
   return cudaGetLastError() == cudaSuccess ? 1 : -1;
 }
 

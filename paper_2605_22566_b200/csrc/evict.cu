@@ -6,7 +6,9 @@
 //   k_select  one CTA per (entry, layer, head): a radix select over 32-bit keys whose order is the weights'
 //             (four passes of eight bits, counts in shared memory), then one ordered pass that writes the
 //             kept indices and carries the weights to the destination's slots.  The choice is a function of
-//             the weights alone: integer counts, and ranks from scans.
+//             the weights alone: integer counts, and ranks from scans.  The weights are read once and their
+//             keys stay in shared memory as long as they fit (kKeyCache); longer nodes are read five times,
+//             from L2.
 //   k_gather  copies the kept rows, in the 4-bit layout by moving the codes of whole tokens (the values are
 //             not touched).  Rows of the last tile past the end become zeros, as every writer of the pools
 //             leaves them.
@@ -19,7 +21,8 @@ namespace gf {
 namespace {
 
 constexpr int kSelectThreads = 512;
-constexpr int kGatherThreads = 256;
+constexpr int kKeyCache = 10240;  // keys kept in shared memory (40 KB)
+constexpr int kGatherThreads = 256;  // 64 rows, 32 at a time, of eight 16-byte pieces
 
 // Keys in the order of the weights; NaN counts as the least, -0 as +0.  Protected tokens get the largest
 // key, which no weight has.
@@ -47,15 +50,27 @@ __global__ void __launch_bounds__(kSelectThreads) k_select(const EvictBatch batc
   __shared__ uint32_t hist[256];
   __shared__ uint32_t pick_s, need_s;
   __shared__ int32_t wsum[2][kSelectThreads / 32];
+  __shared__ uint32_t cache[kKeyCache];
+  const bool cached = n <= kKeyCache;
+  if (cached) {
+#pragma unroll 4
+    for (int t = tid; t < n; t += kSelectThreads) cache[t] = key_of(src[t], t, n, e.first, e.last);
+  }
+  auto key_at = [&](int t) { return cached ? cache[t] : key_of(src[t], t, n, e.first, e.last); };
   // the key of rank `keep`, digit by digit from the top
   uint32_t prefix = 0, need = (uint32_t)e.keep;
   for (int shift = 24; shift >= 0; shift -= 8) {
     for (int i = tid; i < 256; i += kSelectThreads) hist[i] = 0u;
     __syncthreads();
     const uint32_t mask = shift == 24 ? 0u : 0xffffffffu << (shift + 8);
-    for (int t = tid; t < n; t += kSelectThreads) {
-      const uint32_t key = key_of(src[t], t, n, e.first, e.last);
-      if ((key & mask) == prefix) atomicAdd(&hist[(key >> shift) & 255u], 1u);
+    // (lanes with the same digit count together: weights share their high digits, and many are equal)
+    for (int base = 0; base < n; base += kSelectThreads) {
+      const int t = base + tid;
+      const uint32_t key = t < n ? key_at(t) : 0u;
+      const bool on = t < n && (key & mask) == prefix;
+      if (!__any_sync(0xffffffffu, on)) continue;
+      const uint32_t digit = on ? (key >> shift) & 255u : 256u, same = __match_any_sync(0xffffffffu, digit);
+      if (on && (same & ((1u << lane) - 1u)) == 0u) atomicAdd(&hist[digit], (uint32_t)__popc(same));
     }
     __syncthreads();
     if (wid == 0) {  // counts from the top: lane l owns bins 255 - 8 l .. 248 - 8 l
@@ -83,9 +98,7 @@ __global__ void __launch_bounds__(kSelectThreads) k_select(const EvictBatch batc
   int greater = 0, equal = 0;  // before this chunk
   for (int base = 0; base < n; base += kSelectThreads) {
     const int t = base + tid;
-    float w = 0.f;
-    uint32_t key = 0;
-    if (t < n) { w = src[t]; key = key_of(w, t, n, e.first, e.last); }
+    const uint32_t key = t < n ? key_at(t) : 0u;
     const bool gt = t < n && key > prefix, eq = t < n && key == prefix;
     const uint32_t bg = __ballot_sync(0xffffffffu, gt), be = __ballot_sync(0xffffffffu, eq), below = (1u << lane) - 1u;
     if (lane == 0) { wsum[0][wid] = __popc(bg); wsum[1][wid] = __popc(be); }
@@ -99,7 +112,7 @@ __global__ void __launch_bounds__(kSelectThreads) k_select(const EvictBatch batc
     if (gt || (eq && q < (int)need)) {
       const int at = g + min(q, (int)need);
       out[at] = t;
-      dst[at] = w;
+      dst[at] = src[t];
     }
     __syncthreads();
   }
@@ -108,19 +121,25 @@ __global__ void __launch_bounds__(kSelectThreads) k_select(const EvictBatch batc
 template <int D>
 __device__ __forceinline__ void gather_tile16(const char* src_head, char* dst_tile, int src_tile0, int count,
                                               const int32_t* __restrict__ idx) {
-  constexpr int kChunks = D / 8;  // 16-byte pieces of a row
   constexpr uint32_t kTileBytes = 2 * kTile * D * 2;
-  for (int i = threadIdx.x; i < 2 * kTile * kChunks; i += kGatherThreads) {
-    // eight neighbouring threads share a 128-byte line of one row
-    const uint32_t chunk = i & 7, row = (i >> 3) & (kTile - 1), cb = (i >> 9) % (D / 64), which = (i >> 9) / (D / 64);
-    const uint32_t block = which * (kTileBytes / 2) + cb * (kTile * 128u);
-    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-    if ((int)row < count) {
-      const int t = idx[row];
-      v = *reinterpret_cast<const uint4*>(src_head + (uint64_t)(src_tile0 + t / kTile) * kTileBytes + block + swz128(t & (kTile - 1), chunk));
-    }
-    *reinterpret_cast<uint4*>(dst_tile + block + swz128(row, chunk)) = v;
+  constexpr int kBlocks = 2 * (D / 64);  // K's column blocks, then V's
+  // eight neighbouring threads share a 128-byte line; a thread has two rows, every block of them: all its loads are
+  // issued before its stores
+  const uint32_t chunk = threadIdx.x & 7;
+  uint4 v[2][kBlocks];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int row = (threadIdx.x >> 3) + 32 * h, t = row < count ? idx[row] : -1;
+    const char* from = src_head + (uint64_t)(src_tile0 + (t < 0 ? 0 : t) / kTile) * kTileBytes + swz128(t & (kTile - 1), chunk);
+#pragma unroll
+    for (int i = 0; i < kBlocks; ++i)
+      v[h][i] = t < 0 ? make_uint4(0u, 0u, 0u, 0u) : *reinterpret_cast<const uint4*>(from + i * (kTile * 128));
   }
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int i = 0; i < kBlocks; ++i)
+      *reinterpret_cast<uint4*>(dst_tile + i * (kTile * 128) + swz128((threadIdx.x >> 3) + 32 * h, chunk)) = v[h][i];
 }
 
 template <int D>
@@ -130,6 +149,7 @@ __device__ __forceinline__ void gather_tile4(const char* src_head, char* dst_til
   constexpr uint32_t kTileBytes = kv4_tile_bytes(D), kPart = kv4_part_bytes(D), kCodes = kv4_code_bytes(D);
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, l4 = lane & 3, l8 = lane >> 2;
   // a warp per (part, block of 16 tokens, group): every lane builds its 16 bytes from its tokens' pieces
+#pragma unroll
   for (int job = wid; job < 2 * 4 * NG; job += kGatherThreads / 32) {
     const int g = job % NG, b = job / NG % 4, which = job / NG / 4;
     const char* part = src_head + which * kPart;

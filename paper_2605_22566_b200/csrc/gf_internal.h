@@ -277,7 +277,8 @@ int launch_decode(const PoolGeom& pool, const AttnShape& sh, const TablesDev& t,
                   cudaStream_t st);
 int launch_set_residual(ResidualEntry* slot, const ResidualEntry& value, int32_t* node_res, int node, int row,
                         cudaStream_t st);
-int launch_merge(const AttnShape& sh, const TablesDev& t, void* out, float* lse, bool chained, cudaStream_t st);
+// split: eight warps per (request, head) instead of one.
+int launch_merge(const AttnShape& sh, const TablesDev& t, void* out, float* lse, bool chained, bool split, cudaStream_t st);
 // Two launches: the kernel and, behind it, its exact variant, which leaves at once unless the first
 // met scores beyond what its lagging softmax reference may keep.  num_ctas / exact_ctas <= 0: one per
 // multiprocessor.  chained: launched with programmatic stream serialization (only when its

@@ -7,34 +7,76 @@
 // 16-byte runs on both sides, so nothing goes through shared memory; a token's least and largest entry are
 // found with shuffles among the lanes that hold it.
 #include "kv4_device.cuh"
+#include "tc_device.cuh"
 
 namespace gf {
 namespace {
 
 constexpr int kThreads = 256;
 
-__device__ __forceinline__ void unpack8(float (&x)[8], const uint4& v) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(w[i] << 16);
-    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
+__device__ __forceinline__ uint32_t min_pair(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("min.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
 }
 
-// (s, lo) of a group from its extremes.  hi / 16 - lo / 16 cannot overflow; the scaling is exact.
-__device__ __forceinline__ uint32_t group_word(float lo, float hi) {
-  const __nv_bfloat16 s = __float2bfloat16_rn(__fsub_rn(hi * 0.0625f, lo * 0.0625f));
-  return (uint32_t)__bfloat16_as_ushort(s) | (__float_as_uint(lo) & 0xffff0000u);
-}
-// floor((x - lo) / s) within 0..15.  The division is rounded correctly, so no quotient below a whole number
-// reaches it (x, lo and s have 8 significant bits each).
-__device__ __forceinline__ uint32_t code_of(float x, uint32_t sl) {
-  const float s = kv4_s(sl);
-  if (!(s > 0.f)) return 0u;
-  const float c = floorf(__fdiv_rn(__fsub_rn(x * 0.0625f, kv4_lo(sl) * 0.0625f), s) * 16.f);
-  return (uint32_t)fminf(fmaxf(c, 0.f), 15.f);
-}
+// The lesser and the greater number of a pair.
+__device__ __forceinline__ float low_of(uint32_t p) { return fminf(__uint_as_float(p << 16), __uint_as_float(p & 0xffff0000u)); }
+__device__ __forceinline__ float high_of(uint32_t p) { return fmaxf(__uint_as_float(p << 16), __uint_as_float(p & 0xffff0000u)); }
+
+// A group's numbers as the coding of its entries takes them.  Everything is scaled by 1/16, which is exact and keeps
+// hi - lo from overflowing.
+struct GroupCoder {
+  uint32_t word;   // (s, lo) as stored
+  float lo16, cell;  // -lo / 16, s / 16
+  float inv;       // a little more than 16 / s; 0 where s is 0
+  __device__ __forceinline__ GroupCoder(float lo, float hi) {
+    const __nv_bfloat16 s = __float2bfloat16_rn(__fsub_rn(hi * 0.0625f, lo * 0.0625f));
+    word = (uint32_t)__bfloat16_as_ushort(s) | (__float_as_uint(lo) & 0xffff0000u);
+    lo16 = lo * -0.0625f;
+    cell = __bfloat162float(s) * 0.0625f;
+    inv = cell > 0.f ? __fmul_ru(__frcp_ru(cell), 1.0000003f) : 0.f;
+  }
+  // The codes of N bf16 pairs, floor((x - lo) / s) within 0..15, one in each half of out[i].  The quotient from the
+  // reciprocal is never below the true one and less than 2^-20 of it above, so its whole part is the code or,
+  // where a whole number lies between the two, one more: then the remainder (exact: an FMA on a small
+  // whole number and two short numbers) is negative.  That is rare, and put right behind a vote.
+  template <int N>
+  __device__ __forceinline__ void codes(const uint32_t (&pair)[N], uint32_t (&out)[N]) const {
+    const uint64_t magic = f2_pack(8388608.f, 8388608.f), minus = f2_pack(-8388608.f, -8388608.f), sixteenth = f2_pack(0.0625f, 0.0625f);
+    const uint64_t l2 = f2_pack(lo16, lo16), i2 = f2_pack(inv, inv), c2 = f2_pack(-cell, -cell);
+    uint32_t sign = 0u;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint64_t x = f2_pack(__uint_as_float(pair[i] << 16), __uint_as_float(pair[i] & 0xffff0000u));
+      const uint64_t r = f2_fma(x, sixteenth, l2);
+      uint64_t t, u;
+      asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(t) : "l"(r), "l"(i2));
+      asm("add.rm.f32x2 %0, %1, %2;" : "=l"(u) : "l"(t), "l"(magic));  // 2^23 + the whole part: it stands in the low bits
+      const uint64_t rem = f2_fma(f2_add(u, minus), c2, r);
+      uint32_t u0, u1, r0, r1;
+      asm("mov.b64 {%0, %1}, %2;" : "=r"(u0), "=r"(u1) : "l"(u));
+      asm("mov.b64 {%0, %1}, %2;" : "=r"(r0), "=r"(r1) : "l"(rem));
+      sign |= r0 | r1;
+      out[i] = __byte_perm(u0, u1, 0x5410);
+    }
+    if (__any_sync(0xffffffffu, (sign >> 31) != 0u)) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float r0 = fmaf(__uint_as_float(pair[i] << 16), 0.0625f, lo16), r1 = fmaf(__uint_as_float(pair[i] & 0xffff0000u), 0.0625f, lo16);
+        if (fmaf(-(float)(out[i] & 0xffffu), cell, r0) < 0.f) out[i] -= 1u;
+        if (fmaf(-(float)(out[i] >> 16), cell, r1) < 0.f) out[i] -= 0x10000u;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm("min.u16x2 %0, %0, %1;" : "+r"(out[i]) : "r"(0x000f000fu));
+  }
+};
 
 // Where block `b16` (16 tokens), group `grp` of a node's K or V part of one head lies.
 __device__ __forceinline__ char* block_codes(char* head_base, int tile0, uint32_t tile_bytes, int b16, int grp, int groups,
@@ -60,67 +102,72 @@ __global__ void __launch_bounds__(kThreads) k_kv4_write(char* __restrict__ layer
     node_off[node] = token_off;
   }
   const int lane = threadIdx.x & 31, l4 = lane & 3, l8 = lane >> 2;
-  const long long jobs = (long long)(n_pad / 16) * num_kv_heads * kGroups;
+  const uint32_t jobs = (uint32_t)(n_pad / 16) * num_kv_heads * kGroups;  // (a pool of 2^31 such blocks would be 10^12 bytes)
   const uint32_t part = blockIdx.y ? kv4_part_bytes(D) : 0u;
-  for (long long job = ((long long)blockIdx.x * kThreads + threadIdx.x) >> 5; job < jobs;
-       job += ((long long)gridDim.x * kThreads) >> 5) {
-    const int grp = (int)(job % kGroups);
-    const int head = (int)(job / kGroups % num_kv_heads);
-    const int b16 = (int)(job / kGroups / num_kv_heads);
+  for (uint32_t job = (blockIdx.x * kThreads + threadIdx.x) >> 5; job < jobs; job += (gridDim.x * kThreads) >> 5) {
+    const int grp = (int)(job % kGroups), b16 = (int)(job / kGroups / (uint32_t)num_kv_heads);
+    const int head = (int)(job / kGroups - (uint32_t)b16 * num_kv_heads);
     char* head_base = layer_base + (uint64_t)head * head_stride;
     uint32_t word[4] = {0u, 0u, 0u, 0u};
     if (blockIdx.y == 0) {
       // K: two tokens (l8, l8 + 8), 16 entries of each
+      uint4 raw[2][2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const int token = b16 * 16 + l8 + 8 * j;
-        uint4 raw[2] = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
+        raw[j][0] = raw[j][1] = make_uint4(0u, 0u, 0u, 0u);
         if (token < n_tokens) {
           const uint4* src = reinterpret_cast<const uint4*>(k + ((long long)token * num_kv_heads + head) * D + grp * kGroup4);
-          raw[0] = src[l4];
-          raw[1] = src[4 + l4];
+          raw[j][0] = src[l4];
+          raw[j][1] = src[4 + l4];
         }
-        float x[2][8];
-        unpack8(x[0], raw[0]);
-        unpack8(x[1], raw[1]);
-        float lo = x[0][0], hi = x[0][0];
+      }
 #pragma unroll
-        for (int e = 0; e < 16; ++e) { lo = fminf(lo, x[e >> 3][e & 7]); hi = fmaxf(hi, x[e >> 3][e & 7]); }
+      for (int j = 0; j < 2; ++j) {
+        const uint32_t x[8] = {raw[j][0].x, raw[j][0].y, raw[j][0].z, raw[j][0].w, raw[j][1].x, raw[j][1].y, raw[j][1].z, raw[j][1].w};
+        uint32_t lo2 = x[0], hi2 = x[0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) { lo2 = min_pair(lo2, x[i]); hi2 = max_pair(hi2, x[i]); }
 #pragma unroll
         for (int d = 1; d < 4; d <<= 1) {
-          lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, d));
-          hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, d));
+          lo2 = min_pair(lo2, __shfl_xor_sync(0xffffffffu, lo2, d));
+          hi2 = max_pair(hi2, __shfl_xor_sync(0xffffffffu, hi2, d));
         }
-        const uint32_t sl = group_word(lo, hi);
+        const GroupCoder coder(low_of(lo2), high_of(hi2));
+        uint32_t c[8];
+        coder.codes(x, c);
 #pragma unroll
-        for (int e = 0; e < 16; ++e)  // e = 4 kk + 2 (j / 2) + half
-          word[e >> 2] |= code_of(x[e >> 3][e & 7], sl) << (16 * (e & 1) + 4 * (j + 2 * ((e >> 1) & 1)));
-        if (l4 == 0) *token_word(head_base, tile0, kTileBytes, token, grp, kGroups, part, kCodes) = sl;
+        for (int i = 0; i < 8; ++i) word[i >> 1] += c[i] << (4 * (j + 2 * (i & 1)));  // entries e = 2 i, 2 i + 1
+        if (l4 == 0) *token_word(head_base, tile0, kTileBytes, b16 * 16 + l8 + 8 * j, grp, kGroups, part, kCodes) = coder.word;
       }
     } else {
       // V: four tokens (2 l4 + half + 8 t8), 8 entries of each
+      uint4 raw[4];
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        const int half = t & 1, t8 = t >> 1;
-        const int token = b16 * 16 + 2 * l4 + half + 8 * t8;
-        uint4 raw = make_uint4(0u, 0u, 0u, 0u);
+        const int token = b16 * 16 + 2 * l4 + (t & 1) + 8 * (t >> 1);
+        raw[t] = make_uint4(0u, 0u, 0u, 0u);
         if (token < n_tokens)
-          raw = reinterpret_cast<const uint4*>(v + ((long long)token * num_kv_heads + head) * D + grp * kGroup4)[l8];
-        float x[8];
-        unpack8(x, raw);
-        float lo = x[0], hi = x[0];
+          raw[t] = reinterpret_cast<const uint4*>(v + ((long long)token * num_kv_heads + head) * D + grp * kGroup4)[l8];
+      }
 #pragma unroll
-        for (int e = 1; e < 8; ++e) { lo = fminf(lo, x[e]); hi = fmaxf(hi, x[e]); }
+      for (int t = 0; t < 4; ++t) {
+        const uint32_t x[4] = {raw[t].x, raw[t].y, raw[t].z, raw[t].w};
+        uint32_t lo2 = x[0], hi2 = x[0];
+#pragma unroll
+        for (int i = 1; i < 4; ++i) { lo2 = min_pair(lo2, x[i]); hi2 = max_pair(hi2, x[i]); }
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) {
-          lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, d));
-          hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, d));
+          lo2 = min_pair(lo2, __shfl_xor_sync(0xffffffffu, lo2, d));
+          hi2 = max_pair(hi2, __shfl_xor_sync(0xffffffffu, hi2, d));
         }
-        const uint32_t sl = group_word(lo, hi);
+        const GroupCoder coder(low_of(lo2), high_of(hi2));
+        uint32_t c[4];
+        coder.codes(x, c);
 #pragma unroll
-        for (int e = 0; e < 8; ++e)  // e = 2 kk + (j & 1)
-          word[e >> 1] |= code_of(x[e], sl) << (16 * half + 4 * ((e & 1) + 2 * t8));
-        if (l8 == 0) *token_word(head_base, tile0, kTileBytes, token, grp, kGroups, part, kCodes) = sl;
+        for (int i = 0; i < 4; ++i) word[i] += ((c[i] | (c[i] >> 12)) & 0xffu) << (16 * (t & 1) + 8 * (t >> 1));  // entries 2 i, 2 i + 1
+        if (l8 == 0)
+          *token_word(head_base, tile0, kTileBytes, b16 * 16 + 2 * l4 + (t & 1) + 8 * (t >> 1), grp, kGroups, part, kCodes) = coder.word;
       }
     }
     reinterpret_cast<uint4*>(block_codes(head_base, tile0, kTileBytes, b16, grp, kGroups, part))[lane] =
@@ -139,13 +186,11 @@ __global__ void __launch_bounds__(kThreads) k_kv4_read(const char* __restrict__ 
   constexpr int kGroups = D / kGroup4;
   constexpr uint32_t kTileBytes = kv4_tile_bytes(D), kCodes = kv4_code_bytes(D);
   const int lane = threadIdx.x & 31, l4 = lane & 3, l8 = lane >> 2;
-  const long long jobs = (long long)((n_tokens + 15) / 16) * num_kv_heads * kGroups;
+  const uint32_t jobs = (uint32_t)((n_tokens + 15) / 16) * num_kv_heads * kGroups;
   const uint32_t part = blockIdx.y ? kv4_part_bytes(D) : 0u;
-  for (long long job = ((long long)blockIdx.x * kThreads + threadIdx.x) >> 5; job < jobs;
-       job += ((long long)gridDim.x * kThreads) >> 5) {
-    const int grp = (int)(job % kGroups);
-    const int head = (int)(job / kGroups % num_kv_heads);
-    const int b16 = (int)(job / kGroups / num_kv_heads);
+  for (uint32_t job = (blockIdx.x * kThreads + threadIdx.x) >> 5; job < jobs; job += (gridDim.x * kThreads) >> 5) {
+    const int grp = (int)(job % kGroups), b16 = (int)(job / kGroups / (uint32_t)num_kv_heads);
+    const int head = (int)(job / kGroups - (uint32_t)b16 * num_kv_heads);
     char* head_base = const_cast<char*>(layer_base) + (uint64_t)head * head_stride;
     const uint4 codes = reinterpret_cast<const uint4*>(block_codes(head_base, tile0, kTileBytes, b16, grp, kGroups, part))[lane];
     const uint32_t word[4] = {codes.x, codes.y, codes.z, codes.w};

@@ -119,7 +119,8 @@ class PathAttention:
 
     @property
     def stream(self) -> int:
-        return torch.cuda.current_stream(self.dev).cuda_stream
+        # (the raw handle: building a torch.cuda.Stream object costs as much as a kernel launch)
+        return torch._C._cuda_getCurrentRawStream(self.pool.device.index)
 
     # ---- inputs -------------------------------------------------------------------------
     def _fill(self, key: int, count: int, out: torch.Tensor, start: int = 0):
@@ -174,10 +175,10 @@ class PathAttention:
         """gf_node_kv_read into two new bf16 tensors [tokens, Hkv, D]; nothing is waited for."""
         st, n, _ = B.gf_node_extent(self.g, node)
         B.check(st, "gf_node_extent")
-        k = torch.empty((n, self.w.num_kv_heads, self.w.head_dim), dtype=torch.bfloat16, device=self.dev)
-        v = torch.empty_like(k)
-        B.check(B.gf_node_kv_read(self.g, node, layer, k.data_ptr(), v.data_ptr(), self.stream), "gf_node_kv_read")
-        return k, v
+        both = self.pool.new_empty((2, n, self.w.num_kv_heads, self.w.head_dim), dtype=torch.bfloat16)
+        k = both.data_ptr()
+        B.check(B.gf_node_kv_read(self.g, node, layer, k, k + both.numel(), self.stream), "gf_node_kv_read")
+        return both.unbind(0)
 
     def _check_kv(self, k: torch.Tensor, v: torch.Tensor) -> None:
         for name, t in (("k", k), ("v", v)):
@@ -284,7 +285,7 @@ class PathAttention:
         """A view of one node's weights: [layers, Hkv, tokens]."""
         st, n, slot = B.gf_node_extent(self.g, node)
         B.check(st, "gf_node_extent")
-        return weights[:, :, slot:slot + n]
+        return weights.narrow(2, slot, n)
 
     def _check_weights(self, weights: torch.Tensor) -> None:
         shape = (self.layers, self.w.num_kv_heads, B.gf_weight_slots(self.g))
@@ -315,13 +316,13 @@ class PathAttention:
             st, n, _ = B.gf_node_extent(self.g, e[1])
             B.check(st, "gf_node_extent")
             sizes.append(max(min(n, e[2]), 0))
-        lh = self.layers * self.w.num_kv_heads
-        kept = torch.empty(max(lh * sum(sizes), 1), dtype=torch.int32, device=self.dev)
+        hkv = self.w.num_kv_heads
+        kept = self.pool.new_empty((max(self.layers * hkv * sum(sizes), 1),), dtype=torch.int32)
         B.check(B.gf_node_kv_evict(self.g, entries, weights.data_ptr(), kept.data_ptr(), self.stream), "gf_node_kv_evict")
         out, at = [], 0
         for m in sizes:
-            out.append(kept[at:at + lh * m].view(self.layers, self.w.num_kv_heads, m))
-            at += lh * m
+            out.append(kept.as_strided((self.layers, hkv, m), (hkv * m, m, 1), at))
+            at += self.layers * hkv * m
         return out
 
     def read_node(self, node: int, layer: int):

@@ -190,6 +190,14 @@ def test_decode_policies(policy, deferred):
     _decode(w, [0, 2, 3], policy=policy, deferred=deferred)
 
 
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (4, 4, 64)])
+def test_decode_one_request_over_many_chunks(hq, hkv, d):
+    """Few rows with over 32 partial slots each: the merge shares them among eight warps."""
+    w = private_workload([6000, 3001, 70], [[0, 1, 2], [1]], hq, hkv, d)
+    _decode(w, [0, 1], policy=(64, 4, 1, 1))
+    _decode(w, [0], policy=(64, 4, 1, 1), deferred=True)
+
+
 @pytest.mark.parametrize("cfg,frac", [(1, 0.5), (3, 0.5), (3, 1.0)])
 def test_decode_beside_the_tensor_memory_kernel(cfg, frac):
     """Batches whose widely shared bf16 segments run on the side stream, while others are held in 4 bits: two reduced configurations."""
