@@ -18,8 +18,11 @@
 // completion counted in bytes on mbarriers; the layout of kv4_device.cuh makes every operand load a
 // conflict-free 16 bytes per lane) and writes the partial.  The next unit is claimed while the current one
 // streams, a step of the claim (counter, list, item) per tile, so that none of its round trips is waited for.
-// Units of up to 8 rows use one column block of the MMA and run twelve warps to an SM, the others eight.
+// Units of up to 8 rows use one column block of the MMA and run sixteen warps to an SM, the others eight.
+#include <stddef.h>
+
 #include "kv4_device.cuh"
+#include "tc_device.cuh"
 
 namespace gf {
 namespace {
@@ -59,6 +62,11 @@ __device__ __forceinline__ void expand_f16(uint32_t (&a)[4], uint32_t w) {
   a[3] = v & 0x00f000f0u;
 }
 constexpr float kUnit0 = 16777216.f, kUnit1 = 1048576.f;  // what undoes them: 2^24, 2^20
+__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -77,12 +85,13 @@ template <int D, int NT>
 struct Warp4 {
   static constexpr int NG = D / kGroup4, KS = D / 16;
   uint32_t qf[NT][KS][2];
-  float qsum[NT][NG][2];  // sum of a query row's entries per group, for this thread's two columns
-  float scale[NT][2];     // softmax scale in log2 units over the power of two that the row was multiplied by
-  float bias[NT][2];      // 0, or -inf for a row that does not exist (its p are 0)
+  // fp32 pairs are this thread's two columns (query rows); arithmetic on them is packed
+  uint64_t qsum[NT][NG];  // sum of a query row's entries per group
+  uint64_t scale[NT];     // softmax scale in log2 units over the power of two that the row was multiplied by
+  uint64_t bias[NT];      // 0, or -inf for a row that does not exist (its p are 0)
   float o[KS][NT][4];     // O^T in units of 2^-24 / f and 2^-20 / f
-  float oz[NT][NG][2];    // sum over tokens of p (lo + s / 2), this thread's tokens
-  float ref[NT][2], l_run[NT][2];
+  uint64_t oz[NT][NG];    // sum over tokens of p (lo + s / 2), this thread's tokens
+  uint64_t nref[NT], l_run[NT];  // the softmax's reference (negative), the sum of p
   float f[NG];            // power of two that the second product's p s is multiplied by
   float most[NG];         // upper bound of p s when the reference moved last
 
@@ -119,11 +128,14 @@ struct Warp4 {
           qf[j][2 * x + (i >> 1)][i & 1] = pack_f16(__uint_as_float(w[i] << 16) * mul, __uint_as_float(w[i] & 0xffff0000u) * mul);
       }
       // this thread's columns are the rows of the lanes 8 l4 and 8 l4 + 4
+      float sc[2], none[2];
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        scale[j][c] = p.scale_log2 / __shfl_sync(0xffffffffu, mul, 8 * l4 + 4 * c);
-        bias[j][c] = j * 8 + 2 * l4 + c < rows ? 0.f : -INFINITY;
+        sc[c] = p.scale_log2 / __shfl_sync(0xffffffffu, mul, 8 * l4 + 4 * c);
+        none[c] = j * 8 + 2 * l4 + c < rows ? 0.f : -INFINITY;
       }
+      scale[j] = f2_pack(sc[0], sc[1]);
+      bias[j] = f2_pack(none[0], none[1]);
     }
   }
 
@@ -132,21 +144,22 @@ struct Warp4 {
     for (int g = 0; g < NG; ++g) { f[g] = 1.f; most[g] = 0.f; }
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
-#pragma unroll
-      for (int c = 0; c < 2; ++c) { ref[j][c] = bias[j][c] == 0.f ? -INFINITY : 0.f; l_run[j][c] = 0.f; }
+      float b0, b1;
+      f2_unpack(bias[j], b0, b1);
+      nref[j] = f2_pack(b0 == 0.f ? INFINITY : 0.f, b1 == 0.f ? INFINITY : 0.f);
+      l_run[j] = 0;
 #pragma unroll
       for (int i = 0; i < KS; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[i][j][e] = 0.f;
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
-        oz[j][g][0] = oz[j][g][1] = 0.f;
+        oz[j][g] = 0;
         const uint32_t ones[4] = {0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u};
         float acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) mma_f16(acc, ones, qf[j][g * 4 + kk][0], qf[j][g * 4 + kk][1]);
-        qsum[j][g][0] = acc[0];
-        qsum[j][g][1] = acc[1];
+        qsum[j][g] = f2_pack(acc[0], acc[1]);
       }
     }
   }
@@ -166,8 +179,8 @@ struct Warp4 {
     }
   }
 
-  // The tile's scores in log2 units: x[b][j][2 h + c] of token 16 b + l8 + 8 h and this thread's column c.
-  __device__ __forceinline__ void scores(float (&x)[4][NT][4], const char* part, int nv, int lane) const {
+  // The tile's scores in log2 units: x[b][j][h] of token 16 b + l8 + 8 h.
+  __device__ __forceinline__ void scores(uint64_t (&x)[4][NT][2], const char* part, int nv, int lane) const {
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
       uint32_t sl[2][NG];
@@ -191,19 +204,18 @@ struct Warp4 {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const float sc = kv4_s(sl[h][g]), z = fmaf(0.5f, sc, kv4_lo(sl[h][g])), su = sc * (h ? kUnit1 : kUnit0);
+          const uint64_t z2 = f2_pack(z, z), su2 = f2_pack(su, su);
 #pragma unroll
-          for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              const float zq = g ? fmaf(qsum[j][g][c], z, x[b][j][2 * h + c]) : qsum[j][g][c] * z;
-              x[b][j][2 * h + c] = fmaf(acc[j][2 * h + c], su, zq);
-            }
+          for (int j = 0; j < NT; ++j) {
+            const uint64_t zq = f2_fma(qsum[j][g], z2, g ? x[b][j][h] : 0);
+            x[b][j][h] = f2_fma(f2_pack(acc[j][2 * h], acc[j][2 * h + 1]), su2, zq);
+          }
         }
       }
 #pragma unroll
       for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[b][j][e] = fmaf(x[b][j][e], scale[j][e & 1], bias[j][e & 1]);
+        for (int h = 0; h < 2; ++h) x[b][j][h] = f2_fma(x[b][j][h], scale[j], bias[j]);
     }
     if (nv < kTile) {  // the last tile: tokens past the end
 #pragma unroll
@@ -211,8 +223,20 @@ struct Warp4 {
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (b * 16 + (lane >> 2) + 8 * (e >> 1) >= nv) x[b][j][e] = -INFINITY;
+          for (int h = 0; h < 2; ++h)
+            if (b * 16 + (lane >> 2) + 8 * h >= nv) x[b][j][h] = f2_pack(-INFINITY, -INFINITY);
+    }
+  }
+
+  // Column maxima of a tile's scores (this thread's tokens).
+  static __device__ __forceinline__ void column_max(const uint64_t (&x)[4][NT][2], int j, float (&m)[2]) {
+    f2_unpack(x[0][j][0], m[0], m[1]);
+#pragma unroll
+    for (int i = 1; i < 8; ++i) {
+      float a, b;
+      f2_unpack(x[i >> 1][j][i & 1], a, b);
+      m[0] = fmaxf(m[0], a);
+      m[1] = fmaxf(m[1], b);
     }
   }
 
@@ -221,50 +245,57 @@ struct Warp4 {
   // whenever the reference moves so that the largest p s so far stands at 2^2..2^3; an s with which p s could
   // pass fp16's range makes it move too.  Rounding them costs a token 2^-12 of its part at most, or 2^-27
   // of the largest p s among the unit's rows.
-  __device__ __forceinline__ void accumulate(const float (&x)[4][NT][4], const char* part, int lane) {
-    uint32_t sl[4][2][NG];
-#pragma unroll
-    for (int b = 0; b < 4; ++b) load_words(sl[b], part, b, lane);
+  __device__ __forceinline__ void accumulate(const uint64_t (&x)[4][NT][2], const char* part, int lane) {
     bool move = false;
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
+    for (int j = 0; j < NT; ++j) {
+      float m[2], n[2];
+      column_max(x, j, m);
+      f2_unpack(nref[j], n[0], n[1]);
+      move |= m[0] + n[0] > 8.f || m[1] + n[1] > 8.f;
+    }
+    {
+      float m[NG];
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        float m = fmaxf(x[0][j][c], x[0][j][2 + c]);
+      for (int b = 0; b < 4; ++b) {
+        uint32_t sl[2][NG];
+        load_words(sl, part, b, lane);
 #pragma unroll
-        for (int b = 1; b < 4; ++b) m = fmaxf(m, fmaxf(x[b][j][c], x[b][j][2 + c]));
-        move |= m > ref[j][c] + 8.f;
+        for (int g = 0; g < NG; ++g) m[g] = fmaxf(b ? m[g] : 0.f, fmaxf(kv4_s(sl[0][g]), kv4_s(sl[1][g])));
       }
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      float m = 0.f;
-#pragma unroll
-      for (int b = 0; b < 4; ++b) m = fmaxf(m, fmaxf(kv4_s(sl[b][0][g]), kv4_s(sl[b][1][g])));
-      move |= m * f[g] > 128.f;
+      for (int g = 0; g < NG; ++g) move |= m[g] * f[g] > 128.f;
     }
-    if (__any_sync(0xffffffffu, move)) move_reference(x, sl);
+    if (__any_sync(0xffffffffu, move)) move_reference(x, part, lane);
+    asm volatile("" ::: "memory");  // (the words are read again below instead of being kept in registers)
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
-      float pr[NT][4];
+      uint32_t sl[2][NG];
+      load_words(sl, part, b, lane);
+      uint64_t pr[NT][2];
 #pragma unroll
       for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          pr[j][e] = fast_exp2(x[b][j][e] - ref[j][e & 1]);
-          l_run[j][e & 1] += pr[j][e];
+        for (int h = 0; h < 2; ++h) {
+          float lo, hi;
+          f2_unpack(f2_add(x[b][j][h], nref[j]), lo, hi);
+          pr[j][h] = f2_pack(fast_exp2(lo), fast_exp2(hi));
+          l_run[j] = f2_add(l_run[j], pr[j][h]);
         }
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
         uint32_t pb[NT][2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const float sc = kv4_s(sl[b][h][g]), z = fmaf(0.5f, sc, kv4_lo(sl[b][h][g])), sf = sc * f[g];
+          const float sc = kv4_s(sl[h][g]), z = fmaf(0.5f, sc, kv4_lo(sl[h][g])), sf = sc * f[g];
+          const uint64_t z2 = f2_pack(z, z), sf2 = f2_pack(sf, sf);
 #pragma unroll
           for (int j = 0; j < NT; ++j) {
-#pragma unroll
-            for (int c = 0; c < 2; ++c) oz[j][g][c] = fmaf(pr[j][2 * h + c], z, oz[j][g][c]);
+            oz[j][g] = f2_fma(pr[j][h], z2, oz[j][g]);
             // P^T as the B operand: k = token, n = row
-            pb[j][h] = movmatrix_trans(pack_f16(pr[j][2 * h] * sf, pr[j][2 * h + 1] * sf));
+            float lo, hi;
+            f2_unpack(f2_mul(pr[j][h], sf2), lo, hi);
+            pb[j][h] = movmatrix_trans(pack_f16(lo, hi));
           }
         }
         const uint4 c4 = reinterpret_cast<const uint4*>(part)[(b * NG + g) * 32 + lane];
@@ -280,43 +311,57 @@ struct Warp4 {
     }
   }
 
-  __device__ __forceinline__ void move_reference(const float (&x)[4][NT][4], const uint32_t (&sl)[4][2][NG]) {
+  __device__ __forceinline__ void move_reference(const uint64_t (&x)[4][NT][2], const char* part, int lane) {
     float r[NT][2];
     float down = 0.f;  // by how much the largest p so far shrinks at least: the largest r
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
+    for (int j = 0; j < NT; ++j) {
+      float m[2], n[2], l[2], b[2];
+      column_max(x, j, m);
+      f2_unpack(nref[j], n[0], n[1]);
+      f2_unpack(l_run[j], l[0], l[1]);
+      f2_unpack(bias[j], b[0], b[1]);
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        float m = ref[j][c];
+        m[c] = fmaxf(m[c], -n[c]);
 #pragma unroll
-        for (int b = 0; b < 4; ++b) m = fmaxf(m, fmaxf(x[b][j][c], x[b][j][2 + c]));
-#pragma unroll
-        for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-        r[j][c] = fast_exp2(ref[j][c] - m);  // 0 for the unit's first tile
-        ref[j][c] = m;
-        l_run[j][c] *= r[j][c];
-        if (bias[j][c] == 0.f) down = fmaxf(down, r[j][c]);
+        for (int d = 4; d < 32; d <<= 1) m[c] = fmaxf(m[c], __shfl_xor_sync(0xffffffffu, m[c], d));
+        r[j][c] = fast_exp2(-n[c] - m[c]);  // 0 for the unit's first tile
+        if (b[c] == 0.f) down = fmaxf(down, r[j][c]);
       }
+      nref[j] = f2_pack(-m[0], -m[1]);
+      l_run[j] = f2_pack(l[0] * r[j][0], l[1] * r[j][1]);
+    }
 #pragma unroll
     for (int d = 1; d < 4; d <<= 1) down = fmaxf(down, __shfl_xor_sync(0xffffffffu, down, d));
+    float big[NG];  // the tile's largest p s
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      float ps = 0.f;  // the tile's largest p s
+    for (int b = 0; b < 4; ++b) {
+      uint32_t sl[2][NG];
+      load_words(sl, part, b, lane);
 #pragma unroll
-      for (int b = 0; b < 4; ++b)
+      for (int g = 0; g < NG; ++g) {
+        if (b == 0) big[g] = 0.f;
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) ps = fmaxf(ps, fast_exp2(x[b][j][e] - ref[j][e & 1]) * kv4_s(sl[b][e >> 1][g]));
+          for (int h = 0; h < 2; ++h) {
+            float lo, hi;
+            f2_unpack(f2_add(x[b][j][h], nref[j]), lo, hi);
+            big[g] = fmaxf(big[g], fmaxf(fast_exp2(lo), fast_exp2(hi)) * kv4_s(sl[h][g]));
+          }
+      }
+    }
 #pragma unroll
-      for (int d = 1; d < 32; d <<= 1) ps = fmaxf(ps, __shfl_xor_sync(0xffffffffu, ps, d));
-      most[g] = fmaxf(most[g] * down, ps);
+    for (int g = 0; g < NG; ++g) {
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) big[g] = fmaxf(big[g], __shfl_xor_sync(0xffffffffu, big[g], d));
+      most[g] = fmaxf(most[g] * down, big[g]);
       const float fn = pow2_to(most[g], 2), ratio = fn / f[g];
       f[g] = fn;
 #pragma unroll
       for (int j = 0; j < NT; ++j) {
-#pragma unroll
-        for (int c = 0; c < 2; ++c) oz[j][g][c] *= r[j][c];
+        oz[j][g] = f2_mul(oz[j][g], f2_pack(r[j][0], r[j][1]));
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
@@ -327,16 +372,17 @@ struct Warp4 {
 
   // Adds up what the token lanes hold apart: the row sums and the second term of O.
   __device__ __forceinline__ void finish_sums() {
+    auto total = [](uint64_t v) {
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
+      for (int d = 4; d < 32; d <<= 1) v = f2_add(v, __shfl_xor_sync(0xffffffffu, v, d));
+      return v;
+    };
 #pragma unroll
-      for (int c = 0; c < 2; ++c)
+    for (int j = 0; j < NT; ++j) {
+      l_run[j] = total(l_run[j]);
 #pragma unroll
-        for (int d = 4; d < 32; d <<= 1) {
-          l_run[j][c] += __shfl_xor_sync(0xffffffffu, l_run[j][c], d);
-#pragma unroll
-          for (int g = 0; g < NG; ++g) oz[j][g][c] += __shfl_xor_sync(0xffffffffu, oz[j][g][c], d);
-        }
+      for (int g = 0; g < NG; ++g) oz[j][g] = total(oz[j][g]);
+    }
   }
 };
 
@@ -360,14 +406,19 @@ __device__ __forceinline__ void write_partial(const Params& p, Warp4<D, NT>& wa,
         float4* po = reinterpret_cast<float4*>(p.part_o + ph * D);
 #pragma unroll
         for (int gr = 0; gr < NG; ++gr) {  // entries 8 l8 .. + 7 of the group
-          const float z = wa.oz[j][gr][c];
+          float zz[2];
+          f2_unpack(wa.oz[j][gr], zz[0], zz[1]);
+          const float z = zz[c];
           float v[8];
 #pragma unroll
           for (int i = 0; i < 8; ++i) v[i] = fmaf(wa.o[gr * 4 + (i >> 1)][j][2 * (i & 1) + c], (i & 1) ? inv[gr] : 16.f * inv[gr], z);
           po[gr * 16 + l8 * 2] = make_float4(v[0], v[1], v[2], v[3]);
           po[gr * 16 + l8 * 2 + 1] = make_float4(v[4], v[5], v[6], v[7]);
         }
-        if (l8 == 0) *reinterpret_cast<float2*>(p.part_ml + ph * 2) = make_float2(wa.ref[j][c], wa.l_run[j][c]);
+        float n[2], l[2];
+        f2_unpack(wa.nref[j], n[0], n[1]);
+        f2_unpack(wa.l_run[j], l[0], l[1]);
+        if (l8 == 0) *reinterpret_cast<float2*>(p.part_ml + ph * 2) = make_float2(-n[c], l[c]);
       }
     }
 }
@@ -378,13 +429,12 @@ struct __align__(16) Unit {
   int32_t kvh, row0, pad0, pad1;
 };
 
-// The claims of one warp (every lane calls; what they read is the same for all).
+// The claims of one warp (every lane calls).  The claimed item lies in the lanes, a word each, until it is taken.
 struct Claims {
   const int32_t* list;  // 4 * item + 16-row group of unit u: list[dir * (u / num_kv_heads)]
   int dir, num_units, claimants;
   int state = 0;  // 0 ask the counter, 1 read the list, 2 read the item, 3 ready, 4 no more
-  int u = 0, index = 0;
-  Item item;
+  int u = 0, index = 0, word = 0;
   // the first claim needs no counter: claimant i starts with unit i, and the counter counts from the last of those
   __device__ __forceinline__ void first(int i) { u = i; state = 1; }
   __device__ __forceinline__ void step(const Params& p, int lane) {
@@ -400,90 +450,88 @@ struct Claims {
         state = 2;
       }
     } else if (state == 2) {
-      item = p.items[GF_CLAMP(index >> 2, p.slot_cap, p.status, 121)];
+      word = reinterpret_cast<const int32_t*>(p.items + GF_CLAMP(index >> 2, p.slot_cap, p.status, 121))[lane & 7];
       state = 3;
     }
   }
+  __device__ __forceinline__ int item_word(int i) const { return __shfl_sync(0xffffffffu, word, i); }  // in the order of Item
   __device__ __forceinline__ Unit unit(const Params& p) const {
+    static_assert(sizeof(Item) == 32 && offsetof(Item, tok_count) == 8 && offsetof(Item, grp_begin) == 12 && offsetof(Item, grp_count) == 16 &&
+                  offsetof(Item, part_base) == 20 && offsetof(Item, tile0) == 24, "the words that are taken below");
     Unit x{};
-    x.grp_begin = item.grp_begin;
+    x.tok_count = item_word(2);
+    x.grp_begin = item_word(3);
     x.row0 = (index & 3) * 16;
-    x.rows = min(16, item.grp_count * p.gqa - x.row0);
-    x.part_base = item.part_base;
-    x.tok_count = item.tok_count;
+    x.rows = min(16, item_word(4) * p.gqa - x.row0);
+    x.part_base = item_word(5);
     x.kvh = u % p.num_kv_heads;
     return x;
   }
   __device__ __forceinline__ const char* tiles(const Params& p, uint32_t tile_bytes) const {
     return p.pool_layer + (uint64_t)(u % p.num_kv_heads) * p.head_stride +
-           (uint64_t)GF_CLAMP(item.tile0 - p.tile_base, p.cap_tiles, p.status, 124) * tile_bytes;
+           (uint64_t)GF_CLAMP(item_word(6) - p.tile_base, p.cap_tiles, p.status, 124) * tile_bytes;
   }
 };
 
-template <int D>
+// Parts (K or V of a tile) in flight per warp, and CTAs of four warps per SM: what 128 or 255 registers per thread
+// and the shared memory allow.
+template <int NT> constexpr int kCtas4 = NT == 1 ? 3 : 2;
+template <int D, int NT> constexpr int kParts4 = NT == 1 ? 4 : 4;
+
+template <int D, int NT>
 struct __align__(16) WarpSmem {
-  unsigned char part[4][kv4_part_bytes(D)];  // K and V of two tiles
+  unsigned char part[kParts4<D, NT>][kv4_part_bytes(D)];
   Unit unit[4];
-  uint64_t full[4];
+  uint64_t full[kParts4<D, NT>];
 };
 
-// One warp's stream of tiles, K and V copied one after the other, two tiles ahead of their use.
-template <int D>
-struct TileStream {
+// One warp's stream: K and V of its units' tiles, one after the other (part 2 n is K of its n-th tile).
+template <int D, int NT>
+struct PartStream {
+  static constexpr int kParts = kParts4<D, NT>;
   const Params& p;
-  WarpSmem<D>& ws;
+  WarpSmem<D, NT>& ws;
   const int lane;
   Claims& claims;
-  int issued = 0;             // tiles whose K was issued
+  int issued = 0;             // parts issued
   int issue_units = 0;        // units whose issue has begun
-  int left = 0;               // tiles of the current one not issued yet
-  const char* src = nullptr;  // the tile whose K was issued last
-  const char *v_even = nullptr, *v_odd = nullptr;  // where V of the last even and odd tile lies
-  int v_issued = 0;
+  int left = 0;               // parts of the current one not issued yet
+  const char* src = nullptr;  // the next part
 
-  __device__ __forceinline__ void copy(int slot, const char* from) {
-    if (lane == 0) {
-      mbar_arrive_expect_tx(&ws.full[slot], kv4_part_bytes(D));
-      bulk_g2s(ws.part[slot], from, kv4_part_bytes(D), &ws.full[slot]);
-    }
-  }
-  // K of the next tile, V of the next tile: their slots must be free.
-  __device__ __forceinline__ void issue_k() {
+  // Issues the next part; its slot must be free.
+  __device__ __forceinline__ void issue() {
     if (left == 0) {
       while (claims.state < 3) claims.step(p, lane);
       if (claims.state == 4) return;
       const Unit u = claims.unit(p);
+      src = claims.tiles(p, kv4_tile_bytes(D));
       if (lane == 0) ws.unit[issue_units & 3] = u;
       ++issue_units;
-      left = (u.tok_count + kTile - 1) / kTile;
-      src = claims.tiles(p, kv4_tile_bytes(D));
+      left = 2 * ((u.tok_count + kTile - 1) / kTile);
       claims.state = 0;
-    } else {
-      src += kv4_tile_bytes(D);
-      if (claims.state < 3) claims.step(p, lane);
+    } else if (claims.state < 3) {
+      claims.step(p, lane);
     }
-    copy(2 * (issued & 1), src);
-    if (issued & 1) v_odd = src + kv4_part_bytes(D);
-    else v_even = src + kv4_part_bytes(D);
+    if (lane == 0) {
+      const int slot = issued % kParts;
+      mbar_arrive_expect_tx(&ws.full[slot], kv4_part_bytes(D));
+      bulk_g2s(ws.part[slot], src, kv4_part_bytes(D), &ws.full[slot]);
+    }
+    src += kv4_part_bytes(D);
     --left;
     ++issued;
   }
-  __device__ __forceinline__ void issue_v() {
-    if (v_issued == issued) return;
-    copy(2 * (v_issued & 1) + 1, (v_issued & 1) ? v_odd : v_even);
-    ++v_issued;
-  }
-  __device__ __forceinline__ bool wait(int tile, int v) { return mbar_wait(&ws.full[2 * (tile & 1) + v], (tile >> 1) & 1, p.status); }
-  __device__ __forceinline__ const char* part(int tile, int v) const { return reinterpret_cast<const char*>(ws.part[2 * (tile & 1) + v]); }
+  __device__ __forceinline__ bool wait(int n) { return mbar_wait(&ws.full[n % kParts], (n / kParts) & 1, p.status); }
+  __device__ __forceinline__ const char* part(int n) const { return reinterpret_cast<const char*>(ws.part[n % kParts]); }
 };
 
 template <int D, int NT>
-__global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) k_decode4(const Params p) {
+__global__ void __launch_bounds__(kThreads, kCtas4<NT>) k_decode4(const Params p) {
   extern __shared__ __align__(128) unsigned char smem[];
   const int lane = threadIdx.x & 31;
-  WarpSmem<D>& ws = reinterpret_cast<WarpSmem<D>*>(smem)[threadIdx.x >> 5];
+  WarpSmem<D, NT>& ws = reinterpret_cast<WarpSmem<D, NT>*>(smem)[threadIdx.x >> 5];
   if (lane == 0) {
-    for (int i = 0; i < 4; ++i) mbar_init(&ws.full[i], 1);
+    for (int i = 0; i < kParts4<D, NT>; ++i) mbar_init(&ws.full[i], 1);
     mbar_fence_init();
   }
   __syncwarp();
@@ -492,26 +540,26 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) k_decode4(const Par
   Claims claims{NT == 1 ? p.list + p.slot_cap - 1 : p.list + p.hdr->kv4_rows16_first, NT == 1 ? -1 : 1,
                 usable ? (NT == 1 ? p.hdr->kv4_rows8_n : p.hdr->kv4_rows16_n) * p.num_kv_heads : 0, (int)gridDim.x * kWarps};
   claims.first((int)blockIdx.x * kWarps + (threadIdx.x >> 5));
-  TileStream<D> ts{p, ws, lane, claims};
-  for (int i = 0; i < 2; ++i) { ts.issue_k(); ts.issue_v(); }
-  int tile = 0;
+  PartStream<D, NT> ps{p, ws, lane, claims};
+  for (int i = 0; i < kParts4<D, NT>; ++i) ps.issue();
+  int part = 0;
   bool ok = true;
-  for (int n = 0; ok && tile < ts.issued; ++n) {
+  for (int n = 0; ok && part < ps.issued; ++n) {
     __syncwarp();
     const Unit it = ws.unit[n & 3];
     Warp4<D, NT> wa;
     wa.load_queries(p, it.grp_begin, it.row0, it.kvh, it.rows, lane);
     wa.init();
-    for (int left = it.tok_count; left > 0; left -= kTile, ++tile) {
-      float x[4][NT][4];
-      if (!(ok = ts.wait(tile, 0))) break;
-      wa.scores(x, ts.part(tile, 0), left, lane);
+    for (int left = it.tok_count; left > 0; left -= kTile, part += 2) {
+      uint64_t x[4][NT][2];
+      if (!(ok = ps.wait(part))) break;
+      wa.scores(x, ps.part(part), left, lane);
       __syncwarp();
-      ts.issue_k();
-      if (!(ok = ts.wait(tile, 1))) break;
-      wa.accumulate(x, ts.part(tile, 1), lane);
+      ps.issue();
+      if (!(ok = ps.wait(part + 1))) break;
+      wa.accumulate(x, ps.part(part + 1), lane);
       __syncwarp();
-      ts.issue_v();
+      ps.issue();
     }
     if (!ok) break;
     write_partial(p, wa, it.part_base, it.row0, it.kvh, it.rows, lane);
@@ -565,10 +613,10 @@ int launch_decode4(const PoolGeom& pool, const AttnShape& sh, const TablesDev& t
     return true;
   };
   static bool optin[4][kMaxDevices] = {};
-  const bool ok = sh.head_dim == 128 ? go(k_decode4<128, 2>, kWarps * sizeof(WarpSmem<128>), rows16, 2, optin[0]) &&
-                                           go(k_decode4<128, 1>, kWarps * sizeof(WarpSmem<128>), rows8, 3, optin[1])
-                                     : go(k_decode4<64, 2>, kWarps * sizeof(WarpSmem<64>), rows16, 2, optin[2]) &&
-                                           go(k_decode4<64, 1>, kWarps * sizeof(WarpSmem<64>), rows8, 3, optin[3]);
+  const bool ok = sh.head_dim == 128 ? go(k_decode4<128, 2>, kWarps * sizeof(WarpSmem<128, 2>), rows16, kCtas4<2>, optin[0]) &&
+                                           go(k_decode4<128, 1>, kWarps * sizeof(WarpSmem<128, 1>), rows8, kCtas4<1>, optin[1])
+                                     : go(k_decode4<64, 2>, kWarps * sizeof(WarpSmem<64, 2>), rows16, kCtas4<2>, optin[2]) &&
+                                           go(k_decode4<64, 1>, kWarps * sizeof(WarpSmem<64, 1>), rows8, kCtas4<1>, optin[3]);
   if (!ok) return -1;
   return cudaGetLastError() == cudaSuccess ? (rows16 != 0) + (rows8 != 0) : -1;
 }
