@@ -20,8 +20,9 @@ struct gf_tables {
   int32_t bad_req = -1;
   int32_t max_q_rows = 0;
   int32_t num_wide = -1;       // items flagged wide; -1: not known on the host (deferred, or phase B still to run)
-  int32_t kv4_items = -1;      // items held in 4 bits; their 16-row groups with up to 8 query rows, and the others;
-  int32_t kv4_rows8 = -1;      // -1: not known on the host
+  int32_t kv4_items = -1;      // items held in 4 bits; the units of their three kernels (see Header);
+  int32_t kv4_wide = -1;       // -1: not known on the host
+  int32_t kv4_rows8 = -1;
   int32_t kv4_rows16 = -1;
   int32_t split_sms = 0;       // multiprocessors the tensor-memory decode kernel gets beside the warp kernel (0: one after the other)
   bool pending = false;        // deferred build: sizes and validity not read back yet
@@ -735,6 +736,7 @@ static gf_status_t read_back_tables(gf_tables* T) {
   T->max_q_rows = h.max_q_rows;
   T->num_wide = h.num_wide;
   T->kv4_items = h.kv4_items;
+  T->kv4_wide = h.kv4_wide;
   T->kv4_rows8 = h.kv4_rows8;
   T->kv4_rows16 = h.kv4_rows16;
   T->owner->wide_hint = h.wide_units >= T->dev.wide_min_units;
@@ -828,7 +830,7 @@ gf_status_t gf_build_path_tables(gf_wgraph_t* g, int32_t num_requests, int32_t n
   }
   T.pending = false;
   T.num_wide = -1;
-  T.kv4_items = T.kv4_rows8 = T.kv4_rows16 = -1;
+  T.kv4_items = T.kv4_wide = T.kv4_rows8 = T.kv4_rows16 = -1;
   T.error = GF_OK;
   T.build_stream = st;
   T.info = gf_tables_info_t{};
@@ -971,8 +973,14 @@ static int launch_decode_kernels(gf_wgraph* g, const gf_tables* t, const TablesD
   const ResidualEntry* residuals =
       g->res_rows_in_use > 0 ? g->res_table_dev + (size_t)layer * g->desc.max_residual_nodes : nullptr;
   // segments held in 4 bits: kernels of their own, last in the stream; the others have nothing to do when all are
-  const int rows8 = g->kv4_nodes > 0 ? t->kv4_rows8 : 0, rows16 = g->kv4_nodes > 0 ? t->kv4_rows16 : 0;
-  auto decode4 = [&](bool chained) { return launch_decode4(g->pool4, g->shape, td, rows8, rows16, layer, q, g->status_dev, chained, st); };
+  const bool any4 = g->kv4_nodes > 0;
+  const int units = any4 ? t->kv4_wide : 0, rows8 = any4 ? t->kv4_rows8 : 0, rows16 = any4 ? t->kv4_rows16 : 0;
+  auto decode4 = [&](bool chained) {
+    const int a = launch_decode4_wide(g->pool4, g->shape, td, units, layer, q, g->status_dev, chained, st);
+    if (a < 0) return -1;
+    const int b = launch_decode4(g->pool4, g->shape, td, rows8, rows16, layer, q, g->status_dev, chained || a > 0, st);
+    return b < 0 ? -1 : a + b;
+  };
   if (!t->pending && t->kv4_items > 0 && t->kv4_items == t->info.num_items) return decode4(true);
   const bool wide = td.wide_min_group > 0 && t->num_wide != 0;
   const int split = wide ? (t->pending ? g->split_hint : t->split_sms) : 0;

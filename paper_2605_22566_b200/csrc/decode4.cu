@@ -10,7 +10,7 @@
 // fp16 pattern is the subnormal number c 2^-24, and one nibble up 16 c 2^-24: both exact MMA operands, so
 // eight codes take one shift and four ANDs, and the powers of two go into the scales.  Queries are fp16 times
 // a power of two per row (all eight bits of every entry down to 2^-31 of the row's largest), p s is fp16 times
-// one power of two per group, chosen with the softmax's reference; scores, sums, O and the terms without
+// one power of two per row and group, chosen with the softmax's reference; scores, sums, O and the terms without
 // codes are fp32.
 //
 // Every warp is on its own: it takes units (an item's 16 query rows, or what is left of them) from a counter,
@@ -18,7 +18,8 @@
 // completion counted in bytes on mbarriers; the layout of kv4_device.cuh makes every operand load a
 // conflict-free 16 bytes per lane) and writes the partial.  The next unit is claimed while the current one
 // streams, a step of the claim (counter, list, item) per tile, so that none of its round trips is waited for.
-// Units of up to 8 rows use one column block of the MMA and run sixteen warps to an SM, the others eight.
+// Units of up to 8 rows use one column block of the MMA and run twelve warps to an SM, the others eight: what 168 and
+// 255 registers per thread allow.  Chunks shared by 64 rows and more go to decode4_wide.cu where those fill the GPU.
 #include <stddef.h>
 
 #include "kv4_device.cuh"
@@ -61,24 +62,6 @@ __device__ __forceinline__ void expand_f16(uint32_t (&a)[4], uint32_t w) {
   a[2] = v & 0x000f000fu;
   a[3] = v & 0x00f000f0u;
 }
-constexpr float kUnit0 = 16777216.f, kUnit1 = 1048576.f;  // what undoes them: 2^24, 2^20
-__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-// 2^(t - e) for the exponent e of x (2^e <= x < 2^(e + 1)), held within 2^-100 .. 2^100; 1 for x = 0.
-__device__ __forceinline__ float pow2_to(float x, int t) {
-  if (!(x > 0.f)) return 1.f;
-  const int e = (int)(__float_as_uint(x) >> 23) - 127;
-  return __uint_as_float((uint32_t)(min(100, max(-100, t - e)) + 127) << 23);
-}
-
 // The state of one unit: 8 NT query rows over its tokens, a tile at a time.  Token rows 8..15 of a block come out of
 // the first product 16 times too large (registers 1 and 3 hold them), odd entries of O out of the second.
 template <int D, int NT>
@@ -92,8 +75,7 @@ struct Warp4 {
   float o[KS][NT][4];     // O^T in units of 2^-24 / f and 2^-20 / f
   uint64_t oz[NT][NG];    // sum over tokens of p (lo + s / 2), this thread's tokens
   uint64_t nref[NT], l_run[NT];  // the softmax's reference (negative), the sum of p
-  float f[NG];            // power of two that the second product's p s is multiplied by
-  float most[NG];         // upper bound of p s when the reference moved last
+  uint64_t f[NT][NG];     // powers of two that the second product's p s are multiplied by (0: no such row)
 
   // Queries in fp16: a row is multiplied by the power of two that brings its largest entry to 2^14..2^15,
   // which keeps all eight bits of every entry down to 2^-31 of the largest.
@@ -131,7 +113,7 @@ struct Warp4 {
       float sc[2], none[2];
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        sc[c] = p.scale_log2 / __shfl_sync(0xffffffffu, mul, 8 * l4 + 4 * c);
+        sc[c] = p.scale_log2 * pow2_inverse(__shfl_sync(0xffffffffu, mul, 8 * l4 + 4 * c));
         none[c] = j * 8 + 2 * l4 + c < rows ? 0.f : -INFINITY;
       }
       scale[j] = f2_pack(sc[0], sc[1]);
@@ -140,8 +122,6 @@ struct Warp4 {
   }
 
   __device__ __forceinline__ void init() {
-#pragma unroll
-    for (int g = 0; g < NG; ++g) { f[g] = 1.f; most[g] = 0.f; }
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
       float b0, b1;
@@ -155,6 +135,7 @@ struct Warp4 {
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
         oz[j][g] = 0;
+        f[j][g] = f2_pack(b0 == 0.f ? 1.f : 0.f, b1 == 0.f ? 1.f : 0.f);
         const uint32_t ones[4] = {0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u};
         float acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -241,10 +222,11 @@ struct Warp4 {
   }
 
   // Adds the tile to (O, l).  Any reference of the softmax is exact as long as p, l and O share it: it moves only
-  // when a score outgrew it by more than 2^8.  The second product's p s are fp16 times a power of two f, chosen
-  // whenever the reference moves so that the largest p s so far stands at 2^2..2^3; an s with which p s could
-  // pass fp16's range makes it move too.  Rounding them costs a token 2^-12 of its part at most, or 2^-27
-  // of the largest p s among the unit's rows.
+  // when a score outgrew it by more than 2^8.  The second product's p s are fp16 times a power of two f per row and
+  // group, chosen whenever the reference moves so that the row's largest p s so far stands at 2^2 or above (a move may
+  // count what came before it half as large as it is); an s with which p s could pass fp16's range, or the first
+  // one that is not 0, makes it move too.  Rounding costs a token 2^-11 of its part at most, or 2^-27 of the row's
+  // largest p s.
   __device__ __forceinline__ void accumulate(const uint64_t (&x)[4][NT][2], const char* part, int lane) {
     bool move = false;
 #pragma unroll
@@ -264,7 +246,13 @@ struct Warp4 {
         for (int g = 0; g < NG; ++g) m[g] = fmaxf(b ? m[g] : 0.f, fmaxf(kv4_s(sl[0][g]), kv4_s(sl[1][g])));
       }
 #pragma unroll
-      for (int g = 0; g < NG; ++g) move |= m[g] * f[g] > 128.f;
+      for (int g = 0; g < NG; ++g)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          float a, b;
+          f2_unpack(f[j][g], a, b);
+          move |= m[g] * fmaxf(a, b) > 128.f;
+        }
     }
     if (__any_sync(0xffffffffu, move)) move_reference(x, part, lane);
     asm volatile("" ::: "memory");  // (the words are read again below instead of being kept in registers)
@@ -287,14 +275,14 @@ struct Warp4 {
         uint32_t pb[NT][2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const float sc = kv4_s(sl[h][g]), z = fmaf(0.5f, sc, kv4_lo(sl[h][g])), sf = sc * f[g];
-          const uint64_t z2 = f2_pack(z, z), sf2 = f2_pack(sf, sf);
+          const float sc = kv4_s(sl[h][g]), z = fmaf(0.5f, sc, kv4_lo(sl[h][g]));
+          const uint64_t z2 = f2_pack(z, z), s2 = f2_pack(sc, sc);
 #pragma unroll
           for (int j = 0; j < NT; ++j) {
             oz[j][g] = f2_fma(pr[j][h], z2, oz[j][g]);
             // P^T as the B operand: k = token, n = row
             float lo, hi;
-            f2_unpack(f2_mul(pr[j][h], sf2), lo, hi);
+            f2_unpack(f2_mul(f2_mul(pr[j][h], f[j][g]), s2), lo, hi);
             pb[j][h] = movmatrix_trans(pack_f16(lo, hi));
           }
         }
@@ -313,61 +301,64 @@ struct Warp4 {
 
   __device__ __forceinline__ void move_reference(const uint64_t (&x)[4][NT][2], const char* part, int lane) {
     float r[NT][2];
-    float down = 0.f;  // by how much the largest p so far shrinks at least: the largest r
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
-      float m[2], n[2], l[2], b[2];
+      float m[2], n[2], l[2];
       column_max(x, j, m);
       f2_unpack(nref[j], n[0], n[1]);
       f2_unpack(l_run[j], l[0], l[1]);
-      f2_unpack(bias[j], b[0], b[1]);
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         m[c] = fmaxf(m[c], -n[c]);
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) m[c] = fmaxf(m[c], __shfl_xor_sync(0xffffffffu, m[c], d));
         r[j][c] = fast_exp2(-n[c] - m[c]);  // 0 for the unit's first tile
-        if (b[c] == 0.f) down = fmaxf(down, r[j][c]);
       }
       nref[j] = f2_pack(-m[0], -m[1]);
       l_run[j] = f2_pack(l[0] * r[j][0], l[1] * r[j][1]);
     }
-#pragma unroll
-    for (int d = 1; d < 4; d <<= 1) down = fmaxf(down, __shfl_xor_sync(0xffffffffu, down, d));
-    float big[NG];  // the tile's largest p s
+    float big[NT][NG][2];  // the largest p s of the tile, by row and group
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
       uint32_t sl[2][NG];
       load_words(sl, part, b, lane);
 #pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        if (b == 0) big[g] = 0.f;
+      for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
+        for (int h = 0; h < 2; ++h) {
+          float pr[2];
+          f2_unpack(f2_add(x[b][j][h], nref[j]), pr[0], pr[1]);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            float lo, hi;
-            f2_unpack(f2_add(x[b][j][h], nref[j]), lo, hi);
-            big[g] = fmaxf(big[g], fmaxf(fast_exp2(lo), fast_exp2(hi)) * kv4_s(sl[h][g]));
+          for (int c = 0; c < 2; ++c) {
+            pr[c] = fast_exp2(pr[c]);
+#pragma unroll
+            for (int g = 0; g < NG; ++g) big[j][g][c] = fmaxf(b + h ? big[j][g][c] : 0.f, pr[c] * kv4_s(sl[h][g]));
           }
-      }
+        }
     }
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
+    for (int j = 0; j < NT; ++j)
 #pragma unroll
-      for (int d = 1; d < 32; d <<= 1) big[g] = fmaxf(big[g], __shfl_xor_sync(0xffffffffu, big[g], d));
-      most[g] = fmaxf(most[g] * down, big[g]);
-      const float fn = pow2_to(most[g], 2), ratio = fn / f[g];
-      f[g] = fn;
+      for (int g = 0; g < NG; ++g) {
+        float old[2], ratio[2];
+        f2_unpack(f[j][g], old[0], old[1]);
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
+        for (int c = 0; c < 2; ++c) {
+          float& m = big[j][g][c];
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+          const float inv = pow2_inverse(old[c]);  // 4 inv: half the largest p s before, or more
+          const float fn = old[c] > 0.f ? pow2_to(fmaxf(4.f * inv * r[j][c], m), 2) : 0.f;
+          ratio[c] = fn * r[j][c] * inv;  // (in this order: fn / f may leave fp32's range)
+          old[c] = fn;
+        }
+        f[j][g] = f2_pack(old[0], old[1]);
         oz[j][g] = f2_mul(oz[j][g], f2_pack(r[j][0], r[j][1]));
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[g * 4 + kk][j][e] *= r[j][e & 1] * ratio;
+          for (int e = 0; e < 4; ++e) o[g * 4 + kk][j][e] *= ratio[e & 1];
       }
-    }
   }
 
   // Adds up what the token lanes hold apart: the row sums and the second term of O.
@@ -392,9 +383,6 @@ __device__ __forceinline__ void write_partial(const Params& p, Warp4<D, NT>& wa,
   constexpr int NG = D / kGroup4;
   wa.finish_sums();
   const int l4 = lane & 3, l8 = lane >> 2, g = p.gqa;
-  float inv[NG];
-#pragma unroll
-  for (int gr = 0; gr < NG; ++gr) inv[gr] = kUnit1 / wa.f[gr];
 #pragma unroll
   for (int j = 0; j < NT; ++j)
 #pragma unroll
@@ -409,9 +397,12 @@ __device__ __forceinline__ void write_partial(const Params& p, Warp4<D, NT>& wa,
           float zz[2];
           f2_unpack(wa.oz[j][gr], zz[0], zz[1]);
           const float z = zz[c];
+          float ff[2];
+          f2_unpack(wa.f[j][gr], ff[0], ff[1]);
+          const float inv = pow2_inverse(ff[c]);
           float v[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = fmaf(wa.o[gr * 4 + (i >> 1)][j][2 * (i & 1) + c], (i & 1) ? inv[gr] : 16.f * inv[gr], z);
+          for (int i = 0; i < 8; ++i) v[i] = fmaf(wa.o[gr * 4 + (i >> 1)][j][2 * (i & 1) + c] * inv, (i & 1) ? kUnit1 : kUnit0, z);
           po[gr * 16 + l8 * 2] = make_float4(v[0], v[1], v[2], v[3]);
           po[gr * 16 + l8 * 2 + 1] = make_float4(v[4], v[5], v[6], v[7]);
         }
@@ -473,22 +464,22 @@ struct Claims {
   }
 };
 
-// Parts (K or V of a tile) in flight per warp, and CTAs of four warps per SM: what 128 or 255 registers per thread
-// and the shared memory allow.
+// CTAs of four warps per SM (four CTAs at 128 registers spill: 213 us instead of 194 for 256 requests), and parts (K or
+// V of a tile) in flight per warp.
 template <int NT> constexpr int kCtas4 = NT == 1 ? 3 : 2;
-template <int D, int NT> constexpr int kParts4 = NT == 1 ? 4 : 4;
+constexpr int kParts4 = 4;
 
 template <int D, int NT>
 struct __align__(16) WarpSmem {
-  unsigned char part[kParts4<D, NT>][kv4_part_bytes(D)];
+  unsigned char part[kParts4][kv4_part_bytes(D)];
   Unit unit[4];
-  uint64_t full[kParts4<D, NT>];
+  uint64_t full[kParts4];
 };
 
 // One warp's stream: K and V of its units' tiles, one after the other (part 2 n is K of its n-th tile).
 template <int D, int NT>
 struct PartStream {
-  static constexpr int kParts = kParts4<D, NT>;
+  static constexpr int kParts = kParts4;
   const Params& p;
   WarpSmem<D, NT>& ws;
   const int lane;
@@ -531,7 +522,7 @@ __global__ void __launch_bounds__(kThreads, kCtas4<NT>) k_decode4(const Params p
   const int lane = threadIdx.x & 31;
   WarpSmem<D, NT>& ws = reinterpret_cast<WarpSmem<D, NT>*>(smem)[threadIdx.x >> 5];
   if (lane == 0) {
-    for (int i = 0; i < kParts4<D, NT>; ++i) mbar_init(&ws.full[i], 1);
+    for (int i = 0; i < kParts4; ++i) mbar_init(&ws.full[i], 1);
     mbar_fence_init();
   }
   __syncwarp();
@@ -541,7 +532,7 @@ __global__ void __launch_bounds__(kThreads, kCtas4<NT>) k_decode4(const Params p
                 usable ? (NT == 1 ? p.hdr->kv4_rows8_n : p.hdr->kv4_rows16_n) * p.num_kv_heads : 0, (int)gridDim.x * kWarps};
   claims.first((int)blockIdx.x * kWarps + (threadIdx.x >> 5));
   PartStream<D, NT> ps{p, ws, lane, claims};
-  for (int i = 0; i < kParts4<D, NT>; ++i) ps.issue();
+  for (int i = 0; i < kParts4; ++i) ps.issue();
   int part = 0;
   bool ok = true;
   for (int n = 0; ok && part < ps.issued; ++n) {
@@ -564,6 +555,8 @@ __global__ void __launch_bounds__(kThreads, kCtas4<NT>) k_decode4(const Params p
     if (!ok) break;
     write_partial(p, wa, it.part_base, it.row0, it.kvh, it.rows, lane);
   }
+  for (; part < ps.issued; ++part)  // (after a wait that gave up)
+    if (lane == 0) mbar_drain(&ws.full[part % kParts4], (part / kParts4) & 1, p.status);
   // the last CTA to run out of work re-arms the counters for the next launch
   __syncthreads();
   if (threadIdx.x == 0) {

@@ -69,6 +69,18 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, int32_
   }
 }
 
+// The same for a kernel on its way out: waits for a copy or an MMA that it started itself, whether or not another
+// thread gave up, so that nothing writes to memory that is no longer its own.
+__device__ __forceinline__ void mbar_drain(uint64_t* bar, uint32_t parity, int32_t* status, long long limit = kWaitCycles) {
+  const long long t0 = clock64();
+  while (!mbar_try_wait(bar, parity)) {
+    if (clock64() - t0 > limit) {
+      atomicExch(status + kStatusGiveUp, (int32_t)8 /* GF_ERR_TIMEOUT */);
+      return;
+    }
+  }
+}
+
 // ---- bulk copy global -> shared, completion counted in bytes on an mbarrier ------------------
 // Source and destination 16-byte aligned, size a multiple of 16 bytes.
 __device__ __forceinline__ void bulk_g2s(void* dst_smem, const void* src_gmem, uint32_t bytes, uint64_t* bar) {

@@ -52,11 +52,14 @@ struct Header {
   int32_t wide_tile_units;  // (chunk x 128-row tile) pairs of the wide kernel per KV head: each loads queries and writes partials
   int32_t stream_steps;     // work of the warp kernel per KV head, in (64-token tile x 16-row group) steps
   int32_t kv4_items;   // items of segments held in 4 bits
-  int32_t kv4_rows8;   // their 16-row groups that hold up to 8 query rows, and the others
+  int32_t kv4_wide;    // units of the kernel for widely shared chunks of them
+  int32_t kv4_rows8;   // the other items' 16-row groups that hold up to 8 query rows, and those with more
   int32_t kv4_rows16;
-  int32_t kv4_rows8_n;   // how many of either are listed for the 4-bit decode kernels
+  int32_t kv4_wide_n;    // how many of each are listed for the 4-bit decode kernels
+  int32_t kv4_rows8_n;
   int32_t kv4_rows16_n;
-  int32_t kv4_rows16_first;  // where the list of the latter starts
+  int32_t kv4_wide_first;    // where the lists start (that of the 8-row groups: at the end)
+  int32_t kv4_rows16_first;
   int32_t kv4_tokens;  // tokens of the segments held in 4 bits
   unsigned long long resident_tokens;
   unsigned long long materialised_tokens;
@@ -113,8 +116,9 @@ struct TablesDev {
   Item* items;         // [num_items]   (carved after the read-back)
   int32_t* mrg_slot;   // [num_slots]   (carved after the read-back)
   int32_t* wide_list;  // [wide_list_n] item index of the first item of every wide unit, any order;
-                       // behind them [kv4_rows16_n] 4 * item + row group of the 16-row groups of the items
-                       // held in 4 bits, and from the last of its slot_cap entries backwards [kv4_rows8_n]
+                       // behind them [kv4_wide_n] those of the wide units held in 4 bits, behind these
+                       // [kv4_rows16_n] 4 * item + row group of the 16-row groups of the other items held
+                       // in 4 bits, and from the last of its slot_cap entries backwards [kv4_rows8_n]
                        // those that hold up to 8 rows.  A wide unit and a row group each stand for one
                        // partial slot at least, so the lists never meet
   float* part_o;       // [num_slots, Hq, D] fp32 un-normalised partial outputs
@@ -134,6 +138,15 @@ struct TablesDev {
 // Longest chunk of a segment held in 4 bits, in multiples of the policy's chunk_tokens: its kernel gives a chunk's
 // 16 query rows to one warp, which has to come to an end.
 constexpr int kKv4ChunkMult = 4;
+// A chunk of such a segment goes 128 stacked query rows at a time to the tcgen05 kernel; where fewer rows than this
+// are left, to the kernels that take 16.
+constexpr int kKv4WideUnit = 128, kKv4WideRows = 64;
+// Query rows (of `total`, gqa per request) that the tcgen05 kernel gets, when group tiles divide its units.
+__host__ __device__ inline int kv4_wide_rows(int total, int group_rows) {
+  if (kKv4WideUnit % group_rows != 0) return 0;
+  const int last = total % kKv4WideUnit;
+  return last >= kKv4WideRows ? total : total - last;
+}
 
 // True when the tables on the device are usable: every path valid and the items / partial slots fit
 // the room the host carved for them.  Kernels that consume the tables do nothing otherwise.
@@ -293,8 +306,10 @@ int launch_kv4_write(const PoolGeom& pool, int layer, int num_kv_heads, int head
                      const void* v, int n_tokens, const GraphDev* set, int node, int token_off, int num_sms, cudaStream_t st);
 int launch_kv4_read(const PoolGeom& pool, int layer, int num_kv_heads, int head_dim, int tile0, void* k, void* v,
                     int n_tokens, int num_sms, cudaStream_t st);
-// rows8, rows16: 16-row groups with up to 8 query rows and the others, < 0: not known on the host.
-// chained: see launch_decode_wide.
+// rows8, rows16: 16-row groups with up to 8 query rows and the others; units: chunks x 128 rows.  < 0: not known on
+// the host.  chained: see launch_decode_wide.
+int launch_decode4_wide(const PoolGeom& pool, const AttnShape& sh, const TablesDev& t, int units, int layer, const void* q,
+                        int32_t* status, bool chained, cudaStream_t st);
 int launch_decode4(const PoolGeom& pool, const AttnShape& sh, const TablesDev& t, int rows8, int rows16, int layer,
                    const void* q, int32_t* status, bool chained, cudaStream_t st);
 int launch_weights(const PoolGeom& pool16, const PoolGeom& pool4, const AttnShape& sh, const TablesDev& t, int layer, const void* q,

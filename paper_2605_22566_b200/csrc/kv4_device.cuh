@@ -47,4 +47,25 @@ __device__ __forceinline__ void kv4_expand(uint32_t (&a)[4], uint32_t w) {
 __device__ __forceinline__ float kv4_s(uint32_t sl) { return __uint_as_float(sl << 16); }
 __device__ __forceinline__ float kv4_lo(uint32_t sl) { return __uint_as_float(sl & 0xffff0000u); }
 
+// A code in the low bits of an fp16 pattern is the subnormal number c 2^-24, one nibble up 16 c 2^-24.  What undoes them:
+constexpr float kUnit0 = 16777216.f, kUnit1 = 1048576.f;
+__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// 2^(t - e) for the exponent e of x (2^e <= x < 2^(e + 1)), held within 2^-100 .. 2^100 (2^100 for x = 0).
+__device__ __forceinline__ float pow2_to(float x, int t) {
+  const int e = (int)(__float_as_uint(x) >> 23) - 127;
+  return __uint_as_float((uint32_t)(min(100, max(-100, t - e)) + 127) << 23);
+}
+// 1 / x for a power of two x within 2^-126 .. 2^126.
+__device__ __forceinline__ float pow2_inverse(float x) { return __uint_as_float(0x7f000000u - __float_as_uint(x)); }
+
 }  // namespace gf

@@ -83,7 +83,8 @@ __global__ void k_init(TablesDev t, int num_nodes) {
     h.wide_tokens = 0;
     h.wide_tile_units = 0;
     h.stream_steps = 0;
-    h.kv4_items = h.kv4_rows8 = h.kv4_rows16 = h.kv4_rows8_n = h.kv4_rows16_n = h.kv4_rows16_first = h.kv4_tokens = 0;
+    h.kv4_items = h.kv4_wide = h.kv4_rows8 = h.kv4_rows16 = h.kv4_wide_n = h.kv4_rows8_n = h.kv4_rows16_n = 0;
+    h.kv4_wide_first = h.kv4_rows16_first = h.kv4_tokens = 0;
     h.max_q_rows = 0;
     h.resident_tokens = h.materialised_tokens = h.num_q_rows = 0ull;
     *t.hdr = h;
@@ -171,9 +172,11 @@ __global__ void k_scan_nodes_segments(GraphDev g, TablesDev t, gf_policy_t pol) 
   __shared__ int warp_tot[32];
   __shared__ int carry_s;
   __shared__ int wide_units, wide_work, wide_tokens, wide_tile_units, stream_steps;
+  __shared__ int32_t kv4_units, kv4_all[2], kv4_rest[2];  // [0] 16-row groups with up to 8 rows, [1] the others
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, nw = blockDim.x >> 5;
   const int n = g.num_nodes;
   if (tid == 0) { carry_s = 0; wide_units = 0; wide_work = 0; wide_tokens = 0; wide_tile_units = 0; stream_steps = 0; }
+  if (tid == 32) kv4_units = kv4_all[0] = kv4_all[1] = kv4_rest[0] = kv4_rest[1] = 0;
   __syncthreads();
   unsigned long long sum = 0;
   for (int base = 0; base < n; base += blockDim.x) {
@@ -239,13 +242,18 @@ __global__ void k_scan_nodes_segments(GraphDev g, TablesDev t, gf_policy_t pol) 
     t.seg_item_base[s] = nchunk * ceil_div(G, pol.group_tile);
     t.seg_part_base[s] = nchunk * G;
     if (four) {
-      // held in 4 bits: kernels of their own, a unit of which is one 16-row group of an item
-      const int gqa = 256 / t.wide_unit_req, full = G / pol.group_tile, rows = pol.group_tile * gqa, last = (G % pol.group_tile) * gqa;
-      const int r16 = full * (rows / 16 + (rows % 16 > 8)) + last / 16 + (last % 16 > 8);
-      const int groups = full * ceil_div(rows, 16) + ceil_div(last, 16);
+      // held in 4 bits: kernels of their own, a unit of which is 128 rows of a chunk, or a 16-row group of an item
+      const int gqa = 256 / t.wide_unit_req, rows = pol.group_tile * gqa, wide = kv4_wide_rows(G * gqa, rows);
+      const auto narrow = [&](int total, int32_t (&n)[2]) {  // 16-row groups of `total` rows, a group tile at a time
+        const int full = total / rows, last = total % rows;
+        const int r16 = full * (rows / 16 + (rows % 16 > 8)) + last / 16 + (last % 16 > 8);
+        atomicAdd(&n[0], nchunk * (full * ceil_div(rows, 16) + ceil_div(last, 16) - r16));
+        atomicAdd(&n[1], nchunk * r16);
+      };
+      narrow(G * gqa, kv4_all);
+      narrow(G * gqa - wide, kv4_rest);
+      atomicAdd(&kv4_units, nchunk * ceil_div(wide, kKv4WideUnit));
       atomicAdd(&t.hdr->kv4_items, nchunk * ceil_div(G, pol.group_tile));
-      atomicAdd(&t.hdr->kv4_rows16, nchunk * r16);
-      atomicAdd(&t.hdr->kv4_rows8, nchunk * (groups - r16));
       atomicAdd(&t.hdr->kv4_tokens, l);
       continue;
     }
@@ -276,7 +284,15 @@ __global__ void k_scan_nodes_segments(GraphDev g, TablesDev t, gf_policy_t pol) 
     t.hdr->wide_tile_units = wide_tile_units;
     t.hdr->stream_steps = stream_steps;
     if (wide_units < t.wide_min_units) t.hdr->num_wide = 0;
-    t.hdr->kv4_rows16_first = t.hdr->num_wide > 0 ? wide_units : 0;
+    t.hdr->kv4_wide_first = t.hdr->num_wide > 0 ? wide_units : 0;
+    // The tcgen05 kernel's units take two per multiprocessor as long as one: with fewer than that many, the rows are
+    // spread wider over the kernels that take 16 (256 requests over 128 units: 202 us against 190; 1024
+    // requests over 608: 500 against 532).
+    const bool use = kv4_units >= 2 * t.wide_min_units;
+    t.hdr->kv4_wide = use ? kv4_units : 0;
+    t.hdr->kv4_rows8 = use ? kv4_rest[0] : kv4_all[0];
+    t.hdr->kv4_rows16 = use ? kv4_rest[1] : kv4_all[1];
+    t.hdr->kv4_rows16_first = t.hdr->kv4_wide_first + t.hdr->kv4_wide;
   }
   __syncthreads();
   int tot[3];
@@ -465,7 +481,15 @@ __device__ void emit_item(const TablesDev& t, const gf_policy_t& pol, int i, con
     if (GF_CHECK(at < t.slot_cap, t.status, 305)) t.wide_list[at] = i;
   }
   if (four) {
-    const int rows = it.grp_count * (256 / t.wide_unit_req);
+    const int gqa = 256 / t.wide_unit_req, row0 = (it.grp_begin - t.grp_ptr[s]) * gqa;
+    if (t.hdr->kv4_wide > 0 && row0 < kv4_wide_rows(G * gqa, pol.group_tile * gqa)) {
+      if (row0 % kKv4WideUnit == 0) {
+        const int at = t.hdr->kv4_wide_first + atomicAdd(&t.hdr->kv4_wide_n, 1);
+        if (GF_CHECK(at < t.slot_cap, t.status, 310)) t.wide_list[at] = i;
+      }
+      return;
+    }
+    const int rows = it.grp_count * gqa;
     const int r16 = rows / 16 + (rows % 16 > 8);
     if (r16 > 0) {
       const int at = t.hdr->kv4_rows16_first + atomicAdd(&t.hdr->kv4_rows16_n, r16);

@@ -241,6 +241,60 @@ def test_decode_large_and_tiny_value_scales():
     pa.close()
 
 
+@pytest.mark.parametrize("hq,hkv,d,requests", [(8, 1, 128, 7), (8, 1, 128, 17), (16, 2, 64, 24), (4, 4, 64, 64), (3, 3, 128, 127), (4, 2, 64, 200)])
+@pytest.mark.parametrize("deferred", [False, True])
+def test_decode_widely_shared(hq, hkv, d, requests, deferred):
+    """Many requests over few chunks: every 16-row group of an item, the last one whole or in part."""
+    w = random_case(hq, hkv, d, requests, lens=[700, 40, 129, 64, 1], shared=0)
+    _decode(w, range(5), deferred=deferred)
+    _decode(w, [0, 3, 4], policy=(64, 8, 1, 1), deferred=deferred)
+
+
+@pytest.mark.parametrize("hq,hkv,d,requests,chunk", [(32, 8, 128, 15, 192), (32, 8, 128, 16, 64), (32, 8, 128, 32, 192), (16, 8, 64, 65, 320), (8, 8, 128, 127, 128),
+                                                     (8, 8, 64, 200, 64), (64, 8, 128, 40, 128)])
+@pytest.mark.parametrize("four", ["all", "some"])
+def test_decode_many_widely_shared_chunks(hq, hkv, d, requests, chunk, four):
+    """Chunks enough for the tcgen05 kernel, 40 per KV head and more: one to several units of 128 query rows each, the last
+    one with all its rows, with half of them, or with fewer, which other kernels take; one tile to five, the last one
+    ending in its first or its second half."""
+    w = random_case(hq, hkv, d, requests, lens=[40 * chunk - 31, 40, 65, 3 * chunk - 1, 1], shared=0)
+    _decode(w, range(5) if four == "all" else [0, 3, 4], policy=(chunk, 8, 16, 1), deferred=four == "some")
+
+
+@pytest.mark.parametrize("requests,hkv,copies", [(1, 1, 1), (2, 1, 1), (24, 1, 1), (24, 8, 40)])
+def test_decode_scales_far_apart(requests, hkv, copies):
+    """Every query row has one token with nearly all of its weight, and values and groups lie up to 2^180 apart: the output
+    is that token's value, whatever the tokens before it weighed.  With 40 equal nodes and 8 equal heads there are
+    chunks enough for the tcgen05 kernel."""
+    d, n, gqa = 128, 200, 8
+    rng = np.random.default_rng(13)
+    k = rng.choice([-1.0, 1.0], (n, 1, d))
+    at = rng.permutation(n)[: requests * gqa].reshape(requests, gqa)
+    q = 24 * k[at, 0]
+    v = rng.standard_normal((n, 1, 2, d // 2)) * 2.0 ** rng.integers(-90, 91, (n, 1, 2, 1))
+    v[:64:2, 0] *= 0.0
+    k, q, v = _bf16(k), _bf16(q), _bf16(v.reshape(n, 1, d))
+    k, v, q = np.repeat(k, hkv, 1), np.repeat(v, hkv, 1), np.tile(q, (1, hkv, 1))
+    path = list(range(copies))
+    w = private_workload([n] * copies, [path] * requests, gqa * hkv, hkv, d)
+    pa = _handle(w, path)
+    for node in path:
+        pa.write_node(node, 0, _tensor(k), _tensor(v))
+    pa.build()
+    out = pa.decode(0, _tensor(q)).double().cpu().numpy()
+    kv = kv4.values(k), kv4.values(v)
+    ref, _ = OA.decode([path] * requests, lambda _: kv, q, hkv)
+    assert pa.status() == 0
+    # scores are 24 * 128 * 0.94 / sqrt(128) for a row's token and within 24 * 5 for the others (five standard deviations):
+    # the rest weighs less than 2^-190 of it, times 2^180.  Left are the output's rounding (2^-8) and that of p s f to fp16
+    # (2^-11 of a term of up to 15 steps s; the group's values spread over 15 steps, at most twice the largest).
+    # Where the row's token is 0 the reference is what the rest adds: scores 246 below in log2 give weights that fp32 does
+    # not hold, which come out as 0: 200 tokens of 2^-246 times values below 2^93 are below 2^-140
+    out, ref = (x.reshape(requests, hkv * gqa, 2, d // 2) for x in (out, ref))
+    assert np.all(np.abs(out - ref) <= (2.0 ** -8 + 2.0 ** -10 + 2.0 ** -16) * np.abs(ref).max(-1, keepdims=True) + 2.0 ** -140)
+    pa.close()
+
+
 def test_constant_values_and_equal_keys():
     """Equal keys give the mean of V; constant V comes back exactly (its groups are held exactly)."""
     d, n = 64, 77
