@@ -142,114 +142,137 @@ __device__ __forceinline__ Unit resolve(const Params& p, const int32_t* start, i
 
 // ---- up to kNarrowRows rows: a warp each --------------------------------------------------------------------------
 
-// B operands of eight query rows.  For bf16 keys in their natural order (entries 16 ks + 2 l4, + 8); for 4-bit keys in
-// their codes' order (kv4_device.cuh): entries 32 x + 8 l4 .. + 7 are MMAs 2 x and 2 x + 1.
-template <int D, bool k4>
+// B operands of eight query rows, for the order of the entries that 4-bit codes have (kv4_device.cuh) and bf16 keys are
+// read in: entries 32 x + 8 l4 .. + 7 are MMAs 2 x and 2 x + 1, so that a lane takes 16 bytes at a time.
+template <int D>
 struct QueryRows {
   uint32_t f[D / 16][2];
   __device__ __forceinline__ void load(const __nv_bfloat16* row, bool ok, int l4) {
-    if (k4) {
 #pragma unroll
-      for (int x = 0; x < D / 32; ++x) {
-        const uint4 v = ok ? reinterpret_cast<const uint4*>(row)[4 * x + l4] : make_uint4(0u, 0u, 0u, 0u);
-        f[2 * x][0] = v.x;
-        f[2 * x][1] = v.y;
-        f[2 * x + 1][0] = v.z;
-        f[2 * x + 1][1] = v.w;
-      }
-    } else {
-      const uint32_t* w = reinterpret_cast<const uint32_t*>(row) + l4;
-#pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) {
-        f[ks][0] = ok ? w[8 * ks] : 0u;
-        f[ks][1] = ok ? w[8 * ks + 4] : 0u;
-      }
+    for (int x = 0; x < D / 32; ++x) {
+      const uint4 v = ok ? reinterpret_cast<const uint4*>(row)[4 * x + l4] : make_uint4(0u, 0u, 0u, 0u);
+      f[2 * x][0] = v.x;
+      f[2 * x][1] = v.y;
+      f[2 * x + 1][0] = v.z;
+      f[2 * x + 1][1] = v.w;
     }
   }
 };
 
-// The scores of 16 tokens (block b of the unit's K in shared memory) and eight rows, in units of 1 / scale.
-template <int D, bool k4>
-__device__ __forceinline__ void block_scores(float (&s)[4], const unsigned char* k, int b, const QueryRows<D, k4>& q,
-                                             const float (&qsum)[D / kGroup4][2], int lane) {
+// The token of a block of 16 that the MMA's row r (and r + 8, with token + 8) stands for.  For bf16 neighbouring rows are
+// tokens whose swizzle differs in its highest bit, so that eight lanes read 16 bytes each from different banks.
+template <bool k4>
+__device__ __forceinline__ int token_of_row(int r) { return k4 ? r : (r >> 1) + 4 * (r & 1); }
+
+// The scores of 16 tokens (block b of the unit's K in shared memory) and 8 NT rows, in units of 1 / scale.
+template <int D, bool k4, int NT>
+__device__ __forceinline__ void block_scores(float (&s)[NT][4], const unsigned char* k, int b, const QueryRows<D> (&q)[NT],
+                                             const float (&qsum)[NT][D / kGroup4][2], int lane) {
   constexpr int NG = D / kGroup4;
-  s[0] = s[1] = s[2] = s[3] = 0.f;
+  const int l4 = lane & 3, l8 = lane >> 2;
+#pragma unroll
+  for (int j = 0; j < NT; ++j) s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
   if (k4) {
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
       const uint4 c = reinterpret_cast<const uint4*>(k)[(b * NG + g) * 32 + lane];
       const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-      float acc[4] = {0.f, 0.f, 0.f, 0.f};
+      float acc[NT][4];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) {
         uint32_t a[4];
         kv4_expand(a, w[kk]);
-        mma_bf16(acc, a, q.f[g * 4 + kk][0], q.f[g * 4 + kk][1]);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) mma_bf16(acc[j], a, q[j].f[g * 4 + kk][0], q[j].f[g * 4 + kk][1]);
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const uint32_t sl = reinterpret_cast<const uint32_t*>(k + kv4_code_bytes(D))[(b * 16 + (lane >> 2) + 8 * h) * NG + g];
+        const uint32_t sl = reinterpret_cast<const uint32_t*>(k + kv4_code_bytes(D))[(b * 16 + l8 + 8 * h) * NG + g];
         const float sc = kv4_s(sl), z = fmaf(8.5f, sc, kv4_lo(sl));
 #pragma unroll
-        for (int c2 = 0; c2 < 2; ++c2) s[2 * h + c2] = fmaf(acc[2 * h + c2], sc, fmaf(qsum[g][c2], z, s[2 * h + c2]));
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int c2 = 0; c2 < 2; ++c2) s[j][2 * h + c2] = fmaf(acc[j][2 * h + c2], sc, fmaf(qsum[j][g][c2], z, s[j][2 * h + c2]));
       }
     }
   } else {
-    const uint32_t base = smem_u32(k), row = b * 16 + (lane & 7) + (lane & 8);
+    const uint32_t row = b * 16 + token_of_row<k4>(l8);
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) {
-      const uint32_t chunk = 2 * ks + (lane >> 4);
-      uint32_t a[4];
-      ldmatrix_x4(a, base + (chunk >> 3) * (kTile * 128u) + swz128(row, chunk & 7u));
-      mma_bf16(s, a, q.f[ks][0], q.f[ks][1]);
+    for (int x = 0; x < D / 32; ++x) {
+      const uint32_t chunk = 4 * x + l4;
+      const unsigned char* at = k + (chunk >> 3) * (kTile * 128u);
+      const uint4 lo = *reinterpret_cast<const uint4*>(at + swz128(row, chunk & 7u)), hi = *reinterpret_cast<const uint4*>(at + swz128(row + 8, chunk & 7u));
+      const uint32_t a0[4] = {lo.x, hi.x, lo.y, hi.y}, a1[4] = {lo.z, hi.z, lo.w, hi.w};
+#pragma unroll
+      for (int j = 0; j < NT; ++j) mma_bf16(s[j], a0, q[j].f[2 * x][0], q[j].f[2 * x][1]);
+#pragma unroll
+      for (int j = 0; j < NT; ++j) mma_bf16(s[j], a1, q[j].f[2 * x + 1][0], q[j].f[2 * x + 1][1]);
     }
   }
 }
 
-// Adds the unit's rows to sum[b][h] (tokens 16 b + l8 + 8 h, this lane's two columns).  id and off: request and
-// -lse in log2 units of rows lane and lane + 32 (-inf: no such row).  The first rows are asked for before K has
-// come, the next eight before these are worked on.
+// Adds the unit's rows to sum[b][h] (MMA rows l8 and l8 + 8 of block b, this lane's columns).  id and off: request and
+// -lse in log2 units of rows lane and lane + 32 (-inf: no such row).  Sixteen rows share a walk over K (a walk's
+// reads of shared memory, 16 KB, are what it costs); the first are asked for before K has come, the next before
+// these are worked on.
 template <int D, bool k4, typename Arrived>
 __device__ __forceinline__ bool walk_rows(const Params& p, const unsigned char* k, const int (&id)[2], const float (&off)[2], int rows, int kvh,
                                           int lane, float (&sum)[4][2], Arrived&& arrived) {
   constexpr int NG = D / kGroup4;
   const int l4 = lane & 3, l8 = lane >> 2;
-  auto load = [&](QueryRows<D, k4>& q, int row0) {
-    const int row = row0 + l8;
-    const int req = __shfl_sync(0xffffffffu, row0 < 32 ? id[0] : id[1], row & 31);
-    q.load(p.q + ((size_t)req * p.num_q_heads + kvh * p.gqa + (row & (p.gqa - 1))) * D, row < rows, l4);
+  constexpr int NT = 1;
+  auto load = [&](QueryRows<D> (&q)[NT], int row0) {
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const int row = row0 + 8 * j + l8;
+      const int req = __shfl_sync(0xffffffffu, row0 < 32 ? id[0] : id[1], row & 31);
+      q[j].load(p.q + ((size_t)req * p.num_q_heads + kvh * p.gqa + (row & (p.gqa - 1))) * D, row < rows, l4);
+    }
   };
-  QueryRows<D, k4> next;
-  load(next, 0);
-  if (!arrived()) return false;
-#pragma unroll 1
-  for (int row0 = 0; row0 < rows; row0 += 8) {
-    const QueryRows<D, k4> q = next;
-    if (row0 + 8 < rows) load(next, row0 + 8);
-    float o[2];
+  QueryRows<D> q[NT];
+  auto walk = [&](int row0) {
+    float o[NT][2], qsum[NT][NG][2];
 #pragma unroll
-    for (int c = 0; c < 2; ++c) o[c] = __shfl_sync(0xffffffffu, row0 < 32 ? off[0] : off[1], (row0 + l4 * 2 + c) & 31);
-    float qsum[NG][2];
-    if (k4) {
+    for (int j = 0; j < NT; ++j) {
 #pragma unroll
-      for (int x = 0; x < NG; ++x) {
-        const uint32_t ones[4] = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
-        float acc[4] = {0.f, 0.f, 0.f, 0.f};
+      for (int c = 0; c < 2; ++c) o[j][c] = __shfl_sync(0xffffffffu, row0 < 32 ? off[0] : off[1], (row0 + 8 * j + l4 * 2 + c) & 31);
+      if (k4) {
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) mma_bf16(acc, ones, q.f[x * 4 + kk][0], q.f[x * 4 + kk][1]);
-        qsum[x][0] = acc[0];
-        qsum[x][1] = acc[1];
+        for (int x = 0; x < NG; ++x) {
+          const uint32_t ones[4] = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+          float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk) mma_bf16(acc, ones, q[j].f[x * 4 + kk][0], q[j].f[x * 4 + kk][1]);
+          qsum[j][x][0] = acc[0];
+          qsum[j][x][1] = acc[1];
+        }
       }
     }
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
-      float s[4];
-      block_scores<D, k4>(s, k, b, q, qsum, lane);
+      float s[NT][4];
+      block_scores<D, k4, NT>(s, k, b, q, qsum, lane);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sum[b][e >> 1] += fast_exp2(fmaf(s[e], p.scale_log2, o[e & 1]));
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[b][e >> 1] += fast_exp2(fmaf(s[j][e], p.scale_log2, o[j][e & 1]));
     }
+  };
+  load(q, 0);
+  if (!arrived()) return false;
+#pragma unroll 1
+  for (int row0 = 0;;) {
+    const int left = rows - row0;
+    QueryRows<D> next[NT];
+    if (left > 8 * NT) load(next, row0 + 8 * NT);
+    walk(row0);
+    if (left <= 8 * NT) return true;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) q[j] = next[j];
+    row0 += 8 * NT;
   }
-  return true;
 }
 
 template <int D>
@@ -336,7 +359,7 @@ __global__ void __launch_bounds__(kNarrowThreads, 3) k_weights_narrow(const Para
         float v = sum[b][h];
         v += __shfl_xor_sync(0xffffffffu, v, 1);
         v += __shfl_xor_sync(0xffffffffu, v, 2);
-        const int t = b * 16 + (lane >> 2) + 8 * h;
+        const int t = b * 16 + (u.four ? lane >> 2 : token_of_row<false>(lane >> 2)) + 8 * h;
         if ((lane & 3) == 0 && t < u.nv) w[t] = p.accumulate ? w[t] + v : v;
       }
   }
@@ -364,8 +387,9 @@ struct Smem {
 };
 constexpr int kUnitReaders = 8 + kSlots + 4 + 1;  // warps that read a unit's slot
 
-__device__ __forceinline__ void copy16(void* dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+// 16 bytes, of which the first `bytes` are read and the others become zeros.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 // Where an item's scores stand in tensor memory: 64 columns, and as many 128 further for the second group of a 4-bit
 // unit.  Two neighbouring items (an even one and the next) stand side by side.
@@ -494,19 +518,15 @@ __device__ __forceinline__ void load_queries(Smem& sm, const Params& p, int slot
       };
       const int id[2] = {request(lane), request(lane + 32)};  // of rows lane and lane + 32
       if (it >= kSlots && !wait(&sm.q_empty[slot], it / kSlots - 1, p)) return false;
-      const int padded = (rows + 15) & ~15;  // the MMA reads whole groups of 16 rows
+      const __nv_bfloat16* from = p.q + (size_t)head0 * D + chunk * 8;
+      const uint32_t to = smem_u32(tile) + swz128(lane >> 3, chunk), to1 = smem_u32(tile) + swz128(4 + (lane >> 3), chunk);
 #pragma unroll
-      for (int k = 0; k < 16; ++k) {
-        if (4 * k >= padded) break;
+      for (int k = 0; k < 16; ++k) {  // four rows; those that do not exist become zeros
         const int row = 4 * k + (lane >> 3);
         const int req = __shfl_sync(0xffffffffu, id[k >> 3], row & 31);
-        unsigned char* to = tile + swz128(row, chunk);
-        const __nv_bfloat16* src = p.q + ((size_t)req * p.num_q_heads + head0 + (row & (p.gqa - 1))) * D + chunk * 8;
+        const __nv_bfloat16* src = from + ((size_t)req * p.num_q_heads + (row & (p.gqa - 1))) * D;
 #pragma unroll
-        for (int cb = 0; cb < CB; ++cb) {
-          if (row < rows) copy16(to + cb * 16384, src + cb * 64);
-          else *reinterpret_cast<uint4*>(to + cb * 16384) = make_uint4(0u, 0u, 0u, 0u);
-        }
+        for (int cb = 0; cb < CB; ++cb) copy16((k & 1 ? to1 : to) + (k >> 1) * 1024 + cb * 16384, src + cb * 64, row < rows ? 16 : 0);
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
 #pragma unroll
