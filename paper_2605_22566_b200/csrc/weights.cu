@@ -327,16 +327,18 @@ __global__ void __launch_bounds__(kNarrowThreads, 3) k_weights_narrow(const Para
       nx.id[h] = row < nx.rows ? GF_CLAMP(p.grp_req[GF_CLAMP(gb + (row >> sh), p.num_pairs, p.status, 137)], p.num_requests, p.status, 138) : 0;
     }
   };
+  auto copy_keys = [&]() {  // of the next unit; its slot is free
+    if (lane != 0 || nx.rows == 0) return;
+    const uint32_t bytes = nx.four ? kv4_part_bytes(D) : kTile * D * 2u;
+    const char* src = nx.four ? p.layer4 + (uint64_t)nx.kvh * p.head_stride4 + (uint64_t)nx.tile * kv4_tile_bytes(D)
+                              : p.layer16 + (uint64_t)nx.kvh * p.head_stride16 + (uint64_t)nx.tile * p.tile_bytes16;
+    mbar_arrive_expect_tx(&sm.full[warp], bytes);
+    bulk_g2s(sm.k[warp], src, bytes, &sm.full[warp]);
+  };
   take();
+  copy_keys();
   for (int n = 0; nx.rows > 0; ++n) {
     const Next u = nx;
-    if (lane == 0) {
-      const uint32_t bytes = u.four ? kv4_part_bytes(D) : kTile * D * 2u;
-      const char* src = u.four ? p.layer4 + (uint64_t)u.kvh * p.head_stride4 + (uint64_t)u.tile * kv4_tile_bytes(D)
-                               : p.layer16 + (uint64_t)u.kvh * p.head_stride16 + (uint64_t)u.tile * p.tile_bytes16;
-      mbar_arrive_expect_tx(&sm.full[warp], bytes);
-      bulk_g2s(sm.k[warp], src, bytes, &sm.full[warp]);
-    }
     float sum[4][2], off[2];
 #pragma unroll
     for (int b = 0; b < 4; ++b) sum[b][0] = sum[b][1] = 0.f;
@@ -345,13 +347,23 @@ __global__ void __launch_bounds__(kNarrowThreads, 3) k_weights_narrow(const Para
       const int row = lane + 32 * h;
       off[h] = row < u.rows ? -1.4426950408889634f * p.lse[(size_t)u.id[h] * p.num_q_heads + u.kvh * p.gqa + (row & (p.gqa - 1))] : -INFINITY;
     }
+    float* w = p.weights + (int64_t)u.kvh * p.slots + u.slot0;
+    auto token = [&](int b, int h) { return b * 16 + (u.four ? lane >> 2 : token_of_row<false>(lane >> 2)) + 8 * h; };
+    float old[4][2];
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) old[b][h] = p.accumulate && (lane & 3) == 0 && token(b, h) < u.nv ? w[token(b, h)] : 0.f;
     take();
     auto arrived = [&] { return wait(&sm.full[warp], n, p); };
     const bool ok = u.four ? walk_rows<D, true>(p, sm.k[warp], u.id, off, u.rows, u.kvh, lane, sum, arrived)
                            : walk_rows<D, false>(p, sm.k[warp], u.id, off, u.rows, u.kvh, lane, sum, arrived);
-    if (!ok) break;
+    if (!ok) {
+      if (lane == 0) mbar_drain(&sm.full[warp], n & 1, p.status);  // (after a wait that gave up)
+      break;
+    }
     __syncwarp();  // K has been read by every lane: the slot is free
-    float* w = p.weights + (int64_t)u.kvh * p.slots + u.slot0;
+    copy_keys();
 #pragma unroll
     for (int b = 0; b < 4; ++b)
 #pragma unroll
@@ -359,8 +371,8 @@ __global__ void __launch_bounds__(kNarrowThreads, 3) k_weights_narrow(const Para
         float v = sum[b][h];
         v += __shfl_xor_sync(0xffffffffu, v, 1);
         v += __shfl_xor_sync(0xffffffffu, v, 2);
-        const int t = b * 16 + (u.four ? lane >> 2 : token_of_row<false>(lane >> 2)) + 8 * h;
-        if ((lane & 3) == 0 && t < u.nv) w[t] = p.accumulate ? w[t] + v : v;
+        const int t = token(b, h);
+        if ((lane & 3) == 0 && t < u.nv) w[t] = old[b][h] + v;
       }
   }
 }
