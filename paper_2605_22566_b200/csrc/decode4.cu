@@ -529,7 +529,7 @@ __global__ void __launch_bounds__(kThreads, kCtas4<NT>) k_decode4(const Params p
   chain_enter();
   const bool usable = tables_usable(*p.hdr, p.slot_cap);
   Claims claims{NT == 1 ? p.list + p.slot_cap - 1 : p.list + p.hdr->kv4_rows16_first, NT == 1 ? -1 : 1,
-                usable ? (NT == 1 ? p.hdr->kv4_rows8_n : p.hdr->kv4_rows16_n) * p.num_kv_heads : 0, (int)gridDim.x * kWarps};
+                usable ? (NT == 1 ? p.hdr->kv4_rows8 : p.hdr->kv4_rows16) * p.num_kv_heads : 0, (int)gridDim.x * kWarps};
   claims.first((int)blockIdx.x * kWarps + (threadIdx.x >> 5));
   PartStream<D, NT> ps{p, ws, lane, claims};
   for (int i = 0; i < kParts4; ++i) ps.issue();

@@ -543,7 +543,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_decode4_wide(const Params p) {
     mbar_fence_init();
   }
   chain_enter();
-  const int num_units = tables_usable(*p.hdr, p.slot_cap) ? p.hdr->kv4_wide_n * p.num_kv_heads : 0;
+  const int num_units = tables_usable(*p.hdr, p.slot_cap) ? p.hdr->kv4_wide * p.num_kv_heads : 0;
   if (num_units > 0) {  // uniform over the launch
     if (warp == 9) tmem_alloc(&sm.tmem_base, 256);
     tc_fence_before_sync();

@@ -35,6 +35,25 @@ struct __align__(32) Item {
                   // bits 8..: 1 + row of the residual table if the segment's state is base + residual
 };
 
+// Longest chunk of a segment held in 4 bits, in multiples of the policy's chunk_tokens: its kernel gives a chunk's
+// 16 query rows to one warp, which has to come to an end.
+constexpr int kKv4ChunkMult = 4;
+// A chunk of such a segment goes 128 stacked query rows at a time to the tcgen05 kernel; where fewer rows than this
+// are left, to the kernels that take 16.
+constexpr int kKv4WideUnit = 128, kKv4WideRows = 64;
+// Length class of a chunk: the kernels take the longest first, so that no long one is begun when the others end.
+constexpr int kKv4Classes = 8;
+__host__ __device__ inline int kv4_length_class(int chunk) {
+  const int t = chunk / kTile;
+  return t >= 32 ? 0 : t >= 16 ? 1 : t >= 12 ? 2 : t >= 8 ? 3 : t >= 6 ? 4 : t >= 4 ? 5 : t >= 2 ? 6 : 7;
+}
+// Query rows (of `total`, gqa per request) that the tcgen05 kernel gets, when group tiles divide its units.
+__host__ __device__ inline int kv4_wide_rows(int total, int group_rows) {
+  if (kKv4WideUnit % group_rows != 0) return 0;
+  const int last = total % kKv4WideUnit;
+  return last >= kKv4WideRows ? total : total - last;
+}
+
 // Small block the table builder leaves for the host to read back.
 struct Header {
   int32_t bad_req;    // INT_MAX while no bad request has been found
@@ -55,11 +74,9 @@ struct Header {
   int32_t kv4_wide;    // units of the kernel for widely shared chunks of them
   int32_t kv4_rows8;   // the other items' 16-row groups that hold up to 8 query rows, and those with more
   int32_t kv4_rows16;
-  int32_t kv4_wide_n;    // how many of each are listed for the 4-bit decode kernels
-  int32_t kv4_rows8_n;
-  int32_t kv4_rows16_n;
-  int32_t kv4_wide_first;    // where the lists start (that of the 8-row groups: at the end)
+  int32_t kv4_wide_first;  // where the lists start (that of the 8-row groups: at the end)
   int32_t kv4_rows16_first;
+  int32_t kv4_next[3][kKv4Classes];  // where the next entry goes: lists (8 rows, 16, wide) by length class, the longest first
   int32_t kv4_tokens;  // tokens of the segments held in 4 bits
   unsigned long long resident_tokens;
   unsigned long long materialised_tokens;
@@ -116,10 +133,10 @@ struct TablesDev {
   Item* items;         // [num_items]   (carved after the read-back)
   int32_t* mrg_slot;   // [num_slots]   (carved after the read-back)
   int32_t* wide_list;  // [wide_list_n] item index of the first item of every wide unit, any order;
-                       // behind them [kv4_wide_n] those of the wide units held in 4 bits, behind these
-                       // [kv4_rows16_n] 4 * item + row group of the 16-row groups of the other items held
-                       // in 4 bits, and from the last of its slot_cap entries backwards [kv4_rows8_n]
-                       // those that hold up to 8 rows.  A wide unit and a row group each stand for one
+                       // behind them [kv4_wide] those of the wide units held in 4 bits, behind these
+                       // [kv4_rows16] 4 * item + row group of the 16-row groups of the other items held
+                       // in 4 bits, and from the last of its slot_cap entries backwards [kv4_rows8]
+                       // those that hold up to 8 rows; longer chunks first.  A wide unit and a row group each stand for one
                        // partial slot at least, so the lists never meet
   float* part_o;       // [num_slots, Hq, D] fp32 un-normalised partial outputs
   float* part_ml;      // [num_slots, Hq, 2] running max (log2 units) and sum
@@ -134,19 +151,6 @@ struct TablesDev {
   int32_t wide_unit_req;   // requests per unit of the wide kernel: 256 stacked query rows / GQA group size
   int32_t kv4_tile0;       // pool tiles from this index on lie in the 4-bit pool (at tile - kv4_tile0 there)
 };
-
-// Longest chunk of a segment held in 4 bits, in multiples of the policy's chunk_tokens: its kernel gives a chunk's
-// 16 query rows to one warp, which has to come to an end.
-constexpr int kKv4ChunkMult = 4;
-// A chunk of such a segment goes 128 stacked query rows at a time to the tcgen05 kernel; where fewer rows than this
-// are left, to the kernels that take 16.
-constexpr int kKv4WideUnit = 128, kKv4WideRows = 64;
-// Query rows (of `total`, gqa per request) that the tcgen05 kernel gets, when group tiles divide its units.
-__host__ __device__ inline int kv4_wide_rows(int total, int group_rows) {
-  if (kKv4WideUnit % group_rows != 0) return 0;
-  const int last = total % kKv4WideUnit;
-  return last >= kKv4WideRows ? total : total - last;
-}
 
 // True when the tables on the device are usable: every path valid and the items / partial slots fit
 // the room the host carved for them.  Kernels that consume the tables do nothing otherwise.

@@ -83,8 +83,8 @@ __global__ void k_init(TablesDev t, int num_nodes) {
     h.wide_tokens = 0;
     h.wide_tile_units = 0;
     h.stream_steps = 0;
-    h.kv4_items = h.kv4_wide = h.kv4_rows8 = h.kv4_rows16 = h.kv4_wide_n = h.kv4_rows8_n = h.kv4_rows16_n = 0;
-    h.kv4_wide_first = h.kv4_rows16_first = h.kv4_tokens = 0;
+    h.kv4_items = h.kv4_wide = h.kv4_rows8 = h.kv4_rows16 = h.kv4_wide_first = h.kv4_rows16_first = h.kv4_tokens = 0;
+    for (int i = 0; i < 3 * kKv4Classes; ++i) h.kv4_next[i / kKv4Classes][i % kKv4Classes] = 0;
     h.max_q_rows = 0;
     h.resident_tokens = h.materialised_tokens = h.num_q_rows = 0ull;
     *t.hdr = h;
@@ -172,11 +172,13 @@ __global__ void k_scan_nodes_segments(GraphDev g, TablesDev t, gf_policy_t pol) 
   __shared__ int warp_tot[32];
   __shared__ int carry_s;
   __shared__ int wide_units, wide_work, wide_tokens, wide_tile_units, stream_steps;
-  __shared__ int32_t kv4_units, kv4_all[2], kv4_rest[2];  // [0] 16-row groups with up to 8 rows, [1] the others
+  // units by length class: 16-row groups with up to 8 rows, the others; with the wide kernel (rows it leaves, its own) and without
+  __shared__ int32_t kv4_all[2][kKv4Classes], kv4_split[3][kKv4Classes];
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, nw = blockDim.x >> 5;
   const int n = g.num_nodes;
   if (tid == 0) { carry_s = 0; wide_units = 0; wide_work = 0; wide_tokens = 0; wide_tile_units = 0; stream_steps = 0; }
-  if (tid == 32) kv4_units = kv4_all[0] = kv4_all[1] = kv4_rest[0] = kv4_rest[1] = 0;
+  if (tid < 3 * kKv4Classes) kv4_split[tid / kKv4Classes][tid % kKv4Classes] = 0;
+  if (tid < 2 * kKv4Classes) kv4_all[tid / kKv4Classes][tid % kKv4Classes] = 0;
   __syncthreads();
   unsigned long long sum = 0;
   for (int base = 0; base < n; base += blockDim.x) {
@@ -244,15 +246,16 @@ __global__ void k_scan_nodes_segments(GraphDev g, TablesDev t, gf_policy_t pol) 
     if (four) {
       // held in 4 bits: kernels of their own, a unit of which is 128 rows of a chunk, or a 16-row group of an item
       const int gqa = 256 / t.wide_unit_req, rows = pol.group_tile * gqa, wide = kv4_wide_rows(G * gqa, rows);
-      const auto narrow = [&](int total, int32_t (&n)[2]) {  // 16-row groups of `total` rows, a group tile at a time
+      const int cls = kv4_length_class(chunk);
+      const auto narrow = [&](int total, int32_t (*n)[kKv4Classes]) {  // 16-row groups of `total` rows, a group tile at a time
         const int full = total / rows, last = total % rows;
         const int r16 = full * (rows / 16 + (rows % 16 > 8)) + last / 16 + (last % 16 > 8);
-        atomicAdd(&n[0], nchunk * (full * ceil_div(rows, 16) + ceil_div(last, 16) - r16));
-        atomicAdd(&n[1], nchunk * r16);
+        atomicAdd(&n[0][cls], nchunk * (full * ceil_div(rows, 16) + ceil_div(last, 16) - r16));
+        atomicAdd(&n[1][cls], nchunk * r16);
       };
       narrow(G * gqa, kv4_all);
-      narrow(G * gqa - wide, kv4_rest);
-      atomicAdd(&kv4_units, nchunk * ceil_div(wide, kKv4WideUnit));
+      narrow(G * gqa - wide, kv4_split);
+      atomicAdd(&kv4_split[2][cls], nchunk * ceil_div(wide, kKv4WideUnit));
       atomicAdd(&t.hdr->kv4_items, nchunk * ceil_div(G, pol.group_tile));
       atomicAdd(&t.hdr->kv4_tokens, l);
       continue;
@@ -288,11 +291,20 @@ __global__ void k_scan_nodes_segments(GraphDev g, TablesDev t, gf_policy_t pol) 
     // The tcgen05 kernel's units take two per multiprocessor as long as one: with fewer than that many, the rows are
     // spread wider over the kernels that take 16 (256 requests over 128 units: 202 us against 190; 1024
     // requests over 608: 500 against 532).
-    const bool use = kv4_units >= 2 * t.wide_min_units;
-    t.hdr->kv4_wide = use ? kv4_units : 0;
-    t.hdr->kv4_rows8 = use ? kv4_rest[0] : kv4_all[0];
-    t.hdr->kv4_rows16 = use ? kv4_rest[1] : kv4_all[1];
-    t.hdr->kv4_rows16_first = t.hdr->kv4_wide_first + t.hdr->kv4_wide;
+    int units = 0;
+    for (int c = 0; c < kKv4Classes; ++c) units += kv4_split[2][c];
+    const bool use = units >= 2 * t.wide_min_units;
+    const auto place = [&](int list, const int32_t* n, int at) {  // returns where the list ends
+      for (int c = 0; c < kKv4Classes; ++c) {
+        t.hdr->kv4_next[list][c] = at;
+        if (n) at += n[c];
+      }
+      return at;
+    };
+    t.hdr->kv4_rows8 = place(0, use ? kv4_split[0] : kv4_all[0], 0);
+    t.hdr->kv4_rows16_first = place(2, use ? kv4_split[2] : nullptr, t.hdr->kv4_wide_first);
+    t.hdr->kv4_wide = t.hdr->kv4_rows16_first - t.hdr->kv4_wide_first;
+    t.hdr->kv4_rows16 = place(1, use ? kv4_split[1] : kv4_all[1], t.hdr->kv4_rows16_first) - t.hdr->kv4_rows16_first;
   }
   __syncthreads();
   int tot[3];
@@ -481,10 +493,10 @@ __device__ void emit_item(const TablesDev& t, const gf_policy_t& pol, int i, con
     if (GF_CHECK(at < t.slot_cap, t.status, 305)) t.wide_list[at] = i;
   }
   if (four) {
-    const int gqa = 256 / t.wide_unit_req, row0 = (it.grp_begin - t.grp_ptr[s]) * gqa;
+    const int gqa = 256 / t.wide_unit_req, row0 = (it.grp_begin - t.grp_ptr[s]) * gqa, cls = kv4_length_class(chunk);
     if (t.hdr->kv4_wide > 0 && row0 < kv4_wide_rows(G * gqa, pol.group_tile * gqa)) {
       if (row0 % kKv4WideUnit == 0) {
-        const int at = t.hdr->kv4_wide_first + atomicAdd(&t.hdr->kv4_wide_n, 1);
+        const int at = atomicAdd(&t.hdr->kv4_next[2][cls], 1);
         if (GF_CHECK(at < t.slot_cap, t.status, 310)) t.wide_list[at] = i;
       }
       return;
@@ -492,12 +504,12 @@ __device__ void emit_item(const TablesDev& t, const gf_policy_t& pol, int i, con
     const int rows = it.grp_count * gqa;
     const int r16 = rows / 16 + (rows % 16 > 8);
     if (r16 > 0) {
-      const int at = t.hdr->kv4_rows16_first + atomicAdd(&t.hdr->kv4_rows16_n, r16);
+      const int at = atomicAdd(&t.hdr->kv4_next[1][cls], r16);
       for (int k = 0; k < r16; ++k)
         if (GF_CHECK(at + k < t.slot_cap, t.status, 308)) t.wide_list[at + k] = 4 * i + k;
     }
     if (r16 * 16 < rows) {
-      const int at = t.slot_cap - 1 - atomicAdd(&t.hdr->kv4_rows8_n, 1);
+      const int at = t.slot_cap - 1 - atomicAdd(&t.hdr->kv4_next[0][cls], 1);
       if (GF_CHECK(at >= 0, t.status, 309)) t.wide_list[at] = 4 * i + r16;
     }
   }
