@@ -3,12 +3,12 @@
 // Per (node, layer, KV head) the kept tokens are the first and last few (as many as the caller protects) and
 // then those with the largest weight, ties to the lower index, m in all; they keep their order.  Two kernels:
 //
-//   k_select  one CTA per (entry, layer, head): a radix select over 32-bit keys whose order is the weights'
-//             (four passes of eight bits, counts in shared memory), then one ordered pass that writes the
-//             kept indices and carries the weights to the destination's slots.  The choice is a function of
-//             the weights alone: integer counts, and ranks from scans.  The weights are read once and their
-//             keys stay in shared memory as long as they fit (kKeyCache); longer nodes are read five times,
-//             from L2.
+//   k_select  one CTA per (entry, layer, head).  32-bit keys have the weights' order; the key of rank m is found from
+//             its top bits down, then one ordered pass writes the kept indices and carries the weights to the
+//             destination's slots.  The choice is a function of the weights alone: integer counts, and ranks from
+//             scans.  Up to kHeldTokens tokens the keys stay in registers and two bits cost a count over
+//             them (the search ends when nothing is left to decide); longer nodes are read five times, from L2, by
+//             a radix select of eight bits a pass.
 //   k_gather  copies the kept rows, in the 4-bit layout by moving the codes of whole tokens (the values are
 //             not touched).  Rows of the last tile past the end become zeros, as every writer of the pools
 //             leaves them.
@@ -21,7 +21,7 @@ namespace gf {
 namespace {
 
 constexpr int kSelectThreads = 512;
-constexpr int kKeyCache = 10240;  // keys kept in shared memory (40 KB)
+constexpr int kHeldKeys = 16, kHeldTokens = kHeldKeys * kSelectThreads;  // keys a thread keeps
 constexpr int kGatherThreads = 256;  // 64 rows, 32 at a time, of eight 16-byte pieces
 
 // Keys in the order of the weights; NaN counts as the least, -0 as +0.  Protected tokens get the largest
@@ -33,32 +33,57 @@ __device__ __forceinline__ uint32_t key_of(float w, int t, int n, int first, int
   return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
 }
 
-__global__ void __launch_bounds__(kSelectThreads) k_select(const EvictBatch batch, float* __restrict__ weights,
-                                                           int64_t layer_slots, int64_t slots, int num_kv_heads,
-                                                           int32_t* __restrict__ kept, int32_t* node_len, int32_t* node_off) {
-  const EvictEntry e = batch.entry[blockIdx.y];
-  if (e.fresh && blockIdx.x == 0 && threadIdx.x == 0) {
-    node_len[e.node] = e.keep;
-    node_off[e.node] = (int32_t)e.dst_slot;
+// The key of rank `need` (from the top) among the keys the CTA holds, and how many of its equals are kept.
+__device__ __forceinline__ void select_held(const uint32_t (&key)[kHeldKeys], int n, uint32_t& pick, uint32_t& need) {
+  constexpr int kWarps = kSelectThreads / 32;
+  static_assert(kHeldKeys * 32 < 1024 && kWarps <= 32, "a warp's three counts are packed, ten bits each");
+  __shared__ uint32_t count_s[2][kWarps];
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  uint32_t prefix = 0, above = 0, at_least = (uint32_t)n;  // keys above the candidates, and those with them
+  // two bits at a time (keys past the end are 0 and never counted: no trial is 0)
+  for (int shift = 30; shift >= 0 && at_least != need; shift -= 2) {
+    const uint32_t one = prefix | (1u << shift), two = prefix | (2u << shift), three = prefix | (3u << shift);
+    uint32_t c = 0;
+#pragma unroll
+    for (int i = 0; i < kHeldKeys; ++i) {
+      if (i * kSelectThreads >= n) break;
+      c += (key[i] >= one ? 1u : 0u) + (key[i] >= two ? 1u << 10 : 0u) + (key[i] >= three ? 1u << 20 : 0u);
+    }
+    c = __reduce_add_sync(0xffffffffu, c);
+    uint32_t* count = count_s[(shift >> 1) & 1];
+    if (lane == 0) count[wid] = c;
+    __syncthreads();
+    c = lane < kWarps ? count[lane] : 0u;
+    const uint32_t c1 = __reduce_add_sync(0xffffffffu, c & 1023u), c2 = __reduce_add_sync(0xffffffffu, (c >> 10) & 1023u),
+                   c3 = __reduce_add_sync(0xffffffffu, c >> 20);
+    // the digit of the key of rank `need`
+    if (c3 >= need) {
+      prefix = three;
+      at_least = c3;
+    } else if (c2 >= need) {
+      prefix = two;
+      at_least = c2;
+      above = c3;
+    } else if (c1 >= need) {
+      prefix = one;
+      at_least = c1;
+      above = c2;
+    } else {
+      above = c1;
+    }
   }
-  if (e.keep == 0) return;
-  const int layer = blockIdx.x / num_kv_heads, head = blockIdx.x % num_kv_heads;
-  const float* src = weights + layer * layer_slots + head * slots + e.src_slot;
-  float* dst = weights + layer * layer_slots + head * slots + e.dst_slot;
-  int32_t* out = kept + e.kept_off + (int64_t)blockIdx.x * e.keep;
-  const int n = e.len, tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  // either every bit is known, or exactly the keys >= prefix are kept: then all of prefix's equals are
+  pick = prefix;
+  need = at_least == need ? (uint32_t)n : need - above;
+}
+
+// The same where they are too many, digit by digit.
+template <typename KeyAt>
+__device__ __forceinline__ void select_radix(KeyAt&& key_at, int n, uint32_t& pick, uint32_t& need) {
   __shared__ uint32_t hist[256];
   __shared__ uint32_t pick_s, need_s;
-  __shared__ int32_t wsum[2][kSelectThreads / 32];
-  __shared__ uint32_t cache[kKeyCache];
-  const bool cached = n <= kKeyCache;
-  if (cached) {
-#pragma unroll 4
-    for (int t = tid; t < n; t += kSelectThreads) cache[t] = key_of(src[t], t, n, e.first, e.last);
-  }
-  auto key_at = [&](int t) { return cached ? cache[t] : key_of(src[t], t, n, e.first, e.last); };
-  // the key of rank `keep`, digit by digit from the top
-  uint32_t prefix = 0, need = (uint32_t)e.keep;
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  uint32_t prefix = 0;
   for (int shift = 24; shift >= 0; shift -= 8) {
     for (int i = tid; i < 256; i += kSelectThreads) hist[i] = 0u;
     __syncthreads();
@@ -94,26 +119,94 @@ __global__ void __launch_bounds__(kSelectThreads) k_select(const EvictBatch batc
     prefix |= pick_s << shift;
     need = need_s;
   }
-  // `prefix` is that key; of the tokens that have it, the first `need` are kept
+  pick = prefix;
+}
+
+__global__ void __launch_bounds__(kSelectThreads) k_select(const EvictBatch batch, float* __restrict__ weights,
+                                                           int64_t layer_slots, int64_t slots, int num_kv_heads,
+                                                           int32_t* __restrict__ kept, int32_t* node_len, int32_t* node_off) {
+  constexpr int kWarps = kSelectThreads / 32;
+  const EvictEntry e = batch.entry[blockIdx.y];
+  if (e.fresh && blockIdx.x == 0 && threadIdx.x == 0) {
+    node_len[e.node] = e.keep;
+    node_off[e.node] = (int32_t)e.dst_slot;
+  }
+  if (e.keep == 0) return;
+  const int layer = blockIdx.x / num_kv_heads, head = blockIdx.x % num_kv_heads;
+  const float* src = weights + layer * layer_slots + head * slots + e.src_slot;
+  float* dst = weights + layer * layer_slots + head * slots + e.dst_slot;
+  int32_t* out = kept + e.kept_off + (int64_t)blockIdx.x * e.keep;
+  const int n = e.len, tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  auto key_at = [&](int t) { return key_of(src[t], t, n, e.first, e.last); };
+  uint32_t pick, need = (uint32_t)e.keep;  // of the tokens whose key is `pick`, the first `need` are kept
+  const uint32_t below = (1u << lane) - 1u;
+  // Writes what is kept of 512 tokens (this thread's key of token t); g and q: how many greater and equal ones the
+  // warps before this one have.
+  auto write = [&](uint32_t key, float w, int t, int g, int q) {
+    const bool gt = t < n && key > pick, eq = t < n && key == pick;
+    g += __popc(__ballot_sync(0xffffffffu, gt) & below);
+    q += __popc(__ballot_sync(0xffffffffu, eq) & below);
+    if (gt || (eq && q < (int)need)) {
+      const int at = g + min(q, (int)need);
+      out[at] = t;
+      dst[at] = w;
+    }
+  };
+  if (n <= kHeldTokens) {
+    __shared__ uint32_t before_s[kHeldKeys * kWarps];  // by (512 tokens, warp): equal ones, and greater ones in the high half
+    __shared__ uint32_t total_s[kWarps];
+    uint32_t key[kHeldKeys];
+    float w[kHeldKeys];
+#pragma unroll
+    for (int i = 0; i < kHeldKeys; ++i) w[i] = i * kSelectThreads + tid < n ? src[i * kSelectThreads + tid] : 0.f;
+#pragma unroll
+    for (int i = 0; i < kHeldKeys; ++i) key[i] = i * kSelectThreads + tid < n ? key_of(w[i], i * kSelectThreads + tid, n, e.first, e.last) : 0u;
+    select_held(key, n, pick, need);
+#pragma unroll
+    for (int i = 0; i < kHeldKeys; ++i) {
+      const int t = i * kSelectThreads + tid;
+      const uint32_t gt = __ballot_sync(0xffffffffu, t < n && key[i] > pick), eq = __ballot_sync(0xffffffffu, t < n && key[i] == pick);
+      if (lane == 0) before_s[i * kWarps + wid] = (uint32_t)__popc(gt) << 16 | (uint32_t)__popc(eq);
+    }
+    __syncthreads();
+    // exclusive scan (both halves stay below 2^16)
+    static_assert(kHeldKeys * kWarps <= kSelectThreads && kHeldTokens < 65536, "a thread scans one count, of 16 bits each");
+    const uint32_t own = tid < kHeldKeys * kWarps ? before_s[tid] : 0u;
+    uint32_t incl = own;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const uint32_t y = __shfl_up_sync(0xffffffffu, incl, d);
+      if (lane >= d) incl += y;
+    }
+    if (lane == 31) total_s[wid] = incl;
+    __syncthreads();
+    const uint32_t warps = __reduce_add_sync(0xffffffffu, lane < wid ? total_s[lane & (kWarps - 1)] : 0u);
+    if (tid < kHeldKeys * kWarps) before_s[tid] = warps + incl - own;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kHeldKeys; ++i) {
+      if (i * kSelectThreads >= n) break;
+      const uint32_t b = before_s[i * kWarps + wid];
+      write(key[i], w[i], i * kSelectThreads + tid, (int)(b >> 16), (int)(b & 0xffffu));
+    }
+    return;
+  }
+  __shared__ int32_t wsum[2][kWarps];
+  select_radix(key_at, n, pick, need);
   int greater = 0, equal = 0;  // before this chunk
   for (int base = 0; base < n; base += kSelectThreads) {
     const int t = base + tid;
     const uint32_t key = t < n ? key_at(t) : 0u;
-    const bool gt = t < n && key > prefix, eq = t < n && key == prefix;
-    const uint32_t bg = __ballot_sync(0xffffffffu, gt), be = __ballot_sync(0xffffffffu, eq), below = (1u << lane) - 1u;
-    if (lane == 0) { wsum[0][wid] = __popc(bg); wsum[1][wid] = __popc(be); }
+    const uint32_t gt = __ballot_sync(0xffffffffu, t < n && key > pick), eq = __ballot_sync(0xffffffffu, t < n && key == pick);
+    if (lane == 0) { wsum[0][wid] = __popc(gt); wsum[1][wid] = __popc(eq); }
     __syncthreads();
-    int g = greater + __popc(bg & below), q = equal + __popc(be & below);
-    for (int i = 0; i < kSelectThreads / 32; ++i) {
+    int g = greater, q = equal;
+    for (int i = 0; i < kWarps; ++i) {
       if (i < wid) { g += wsum[0][i]; q += wsum[1][i]; }
       greater += wsum[0][i];
       equal += wsum[1][i];
     }
-    if (gt || (eq && q < (int)need)) {
-      const int at = g + min(q, (int)need);
-      out[at] = t;
-      dst[at] = src[t];
-    }
+    write(key, t < n ? src[t] : 0.f, t, g, q);
     __syncthreads();
   }
 }

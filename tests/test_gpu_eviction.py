@@ -220,6 +220,12 @@ def test_evict_a_long_node_and_many_entries():
     pa.close()
 
 
+@pytest.mark.parametrize("make", [None, _ties, _special, lambda r, s: np.full(s, np.nan)])
+def test_evict_around_the_longest_held_in_registers(make):
+    pa, _ = _evict_case([8191, 8192, 8193, 20000], [True, False, True, True], [8190, 4095, 1, 20000], layers=1, hkv=1, make=make, last=1)
+    pa.close()
+
+
 def test_evict_twice_into_the_same_node_and_one_source_into_two():
     pa, weights = _evict_case([150], [False], [70])
     again = pa.node_weights(weights, 0)
