@@ -464,32 +464,35 @@ struct Claims {
   }
 };
 
-// CTAs of four warps per SM (four CTAs at 128 registers spill: 213 us instead of 194 for 256 requests), and parts (K or
-// V of a tile) in flight per warp.
+// CTAs of four warps per SM (four CTAs at 128 registers spill: 213 us instead of 194 for 256 requests), and tiles in
+// flight or in use per warp.
 template <int NT> constexpr int kCtas4 = NT == 1 ? 3 : 2;
-constexpr int kParts4 = 4;
+constexpr int kTiles4 = 2;
 
 template <int D, int NT>
 struct __align__(16) WarpSmem {
-  unsigned char part[kParts4][kv4_part_bytes(D)];
+  unsigned char tile[kTiles4][kv4_tile_bytes(D)];
   Unit unit[4];
-  uint64_t full[kParts4];
+  uint64_t full[kTiles4];
 };
 
-// One warp's stream: K and V of its units' tiles, one after the other (part 2 n is K of its n-th tile).
+// One warp's stream of its units' tiles, one after the other.
 template <int D, int NT>
-struct PartStream {
-  static constexpr int kParts = kParts4;
+struct TileStream {
   const Params& p;
   WarpSmem<D, NT>& ws;
   const int lane;
   Claims& claims;
-  int issued = 0;             // parts issued
+  int issued = 0;             // tiles issued
   int issue_units = 0;        // units whose issue has begun
-  int left = 0;               // parts of the current one not issued yet
-  const char* src = nullptr;  // the next part
+  int left = 0;               // tiles of the current one not issued yet
+  const char* src = nullptr;  // the next tile
 
-  // Issues the next part; its slot must be free.
+  // A step of the next claim, if it is not complete.
+  __device__ __forceinline__ void claim() {
+    if (claims.state < 3) claims.step(p, lane);
+  }
+  // Issues the next tile; its slot must be free.
   __device__ __forceinline__ void issue() {
     if (left == 0) {
       while (claims.state < 3) claims.step(p, lane);
@@ -498,22 +501,20 @@ struct PartStream {
       src = claims.tiles(p, kv4_tile_bytes(D));
       if (lane == 0) ws.unit[issue_units & 3] = u;
       ++issue_units;
-      left = 2 * ((u.tok_count + kTile - 1) / kTile);
+      left = (u.tok_count + kTile - 1) / kTile;
       claims.state = 0;
-    } else if (claims.state < 3) {
-      claims.step(p, lane);
     }
     if (lane == 0) {
-      const int slot = issued % kParts;
-      mbar_arrive_expect_tx(&ws.full[slot], kv4_part_bytes(D));
-      bulk_g2s(ws.part[slot], src, kv4_part_bytes(D), &ws.full[slot]);
+      const int slot = issued % kTiles4;
+      mbar_arrive_expect_tx(&ws.full[slot], kv4_tile_bytes(D));
+      bulk_g2s(ws.tile[slot], src, kv4_tile_bytes(D), &ws.full[slot]);
     }
-    src += kv4_part_bytes(D);
+    src += kv4_tile_bytes(D);
     --left;
     ++issued;
   }
-  __device__ __forceinline__ bool wait(int n) { return mbar_wait(&ws.full[n % kParts], (n / kParts) & 1, p.status); }
-  __device__ __forceinline__ const char* part(int n) const { return reinterpret_cast<const char*>(ws.part[n % kParts]); }
+  __device__ __forceinline__ bool wait(int n) { return mbar_wait(&ws.full[n % kTiles4], (n / kTiles4) & 1, p.status); }
+  __device__ __forceinline__ const char* tile(int n) const { return reinterpret_cast<const char*>(ws.tile[n % kTiles4]); }
 };
 
 template <int D, int NT>
@@ -522,7 +523,7 @@ __global__ void __launch_bounds__(kThreads, kCtas4<NT>) k_decode4(const Params p
   const int lane = threadIdx.x & 31;
   WarpSmem<D, NT>& ws = reinterpret_cast<WarpSmem<D, NT>*>(smem)[threadIdx.x >> 5];
   if (lane == 0) {
-    for (int i = 0; i < kParts4; ++i) mbar_init(&ws.full[i], 1);
+    for (int i = 0; i < kTiles4; ++i) mbar_init(&ws.full[i], 1);
     mbar_fence_init();
   }
   __syncwarp();
@@ -531,32 +532,31 @@ __global__ void __launch_bounds__(kThreads, kCtas4<NT>) k_decode4(const Params p
   Claims claims{NT == 1 ? p.list + p.slot_cap - 1 : p.list + p.hdr->kv4_rows16_first, NT == 1 ? -1 : 1,
                 usable ? (NT == 1 ? p.hdr->kv4_rows8 : p.hdr->kv4_rows16) * p.num_kv_heads : 0, (int)gridDim.x * kWarps};
   claims.first((int)blockIdx.x * kWarps + (threadIdx.x >> 5));
-  PartStream<D, NT> ps{p, ws, lane, claims};
-  for (int i = 0; i < kParts4; ++i) ps.issue();
-  int part = 0;
+  TileStream<D, NT> ts{p, ws, lane, claims};
+  for (int i = 0; i < kTiles4; ++i) ts.issue();
+  int tile = 0;
   bool ok = true;
-  for (int n = 0; ok && part < ps.issued; ++n) {
+  for (int n = 0; ok && tile < ts.issued; ++n) {
     __syncwarp();
     const Unit it = ws.unit[n & 3];
     Warp4<D, NT> wa;
     wa.load_queries(p, it.grp_begin, it.row0, it.kvh, it.rows, lane);
     wa.init();
-    for (int left = it.tok_count; left > 0; left -= kTile, part += 2) {
+    for (int left = it.tok_count; left > 0; left -= kTile, ++tile) {
       uint64_t x[4][NT][2];
-      if (!(ok = ps.wait(part))) break;
-      wa.scores(x, ps.part(part), left, lane);
+      if (!(ok = ts.wait(tile))) break;
+      ts.claim();
+      wa.scores(x, ts.tile(tile), left, lane);
+      ts.claim();
+      wa.accumulate(x, ts.tile(tile) + kv4_part_bytes(D), lane);
       __syncwarp();
-      ps.issue();
-      if (!(ok = ps.wait(part + 1))) break;
-      wa.accumulate(x, ps.part(part + 1), lane);
-      __syncwarp();
-      ps.issue();
+      ts.issue();
     }
     if (!ok) break;
     write_partial(p, wa, it.part_base, it.row0, it.kvh, it.rows, lane);
   }
-  for (; part < ps.issued; ++part)  // (after a wait that gave up)
-    if (lane == 0) mbar_drain(&ws.full[part % kParts4], (part / kParts4) & 1, p.status);
+  for (; tile < ts.issued; ++tile)  // (after a wait that gave up)
+    if (lane == 0) mbar_drain(&ws.full[tile % kTiles4], (tile / kTiles4) & 1, p.status);
   // the last CTA to run out of work re-arms the counters for the next launch
   __syncthreads();
   if (threadIdx.x == 0) {
