@@ -237,13 +237,17 @@ struct Warp4 {
       move |= m[0] + n[0] > 8.f || m[1] + n[1] > 8.f;
     }
     {
-      float m[NG];
+      uint32_t m[NG];  // the largest s in the low half (not negative: its bits order as it does)
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
         uint32_t sl[2][NG];
         load_words(sl, part, b, lane);
 #pragma unroll
-        for (int g = 0; g < NG; ++g) m[g] = fmaxf(b ? m[g] : 0.f, fmaxf(kv4_s(sl[0][g]), kv4_s(sl[1][g])));
+        for (int g = 0; g < NG; ++g) {
+          if (b == 0) m[g] = sl[0][g];
+          else asm("max.u16x2 %0, %0, %1;" : "+r"(m[g]) : "r"(sl[0][g]));
+          asm("max.u16x2 %0, %0, %1;" : "+r"(m[g]) : "r"(sl[1][g]));
+        }
       }
 #pragma unroll
       for (int g = 0; g < NG; ++g)
@@ -251,7 +255,7 @@ struct Warp4 {
         for (int j = 0; j < NT; ++j) {
           float a, b;
           f2_unpack(f[j][g], a, b);
-          move |= m[g] * fmaxf(a, b) > 128.f;
+          move |= kv4_s(m[g]) * fmaxf(a, b) > 128.f;
         }
     }
     if (__any_sync(0xffffffffu, move)) move_reference(x, part, lane);
