@@ -153,7 +153,7 @@ def lib():
         L.gf_launch_count.argtypes = [C.c_void_p]
         L.gf_node_kv_reserve.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p]
         L.gf_node_kv_release.argtypes = [C.c_void_p, C.c_int32, C.c_void_p]
-        L.gf_node_extent.argtypes = [C.c_void_p, C.c_int32, C.POINTER(C.c_int32), C.POINTER(C.c_int32)]
+        L.gf_node_extent.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]
         L.gf_pool_info.argtypes = [C.c_void_p, C.POINTER(PoolInfo)]
         L.gf_path_attention_extend_append.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p,
                                                       C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
@@ -341,9 +341,10 @@ def gf_node_kv_release(g, node, stream=0) -> int:
 
 def gf_node_extent(g, node):
     """(status, n_tokens, token_offset) of a node's extent."""
-    n, off = C.c_int32(-1), C.c_int32(-1)
-    st = lib().gf_node_extent(g, node, C.byref(n), C.byref(off))
-    return st, int(n.value), int(off.value)
+    out = (C.c_int32 * 2)(-1, -1)
+    at = C.addressof(out)
+    st = lib().gf_node_extent(g, node, at, at + 4)
+    return st, out[0], out[1]
 
 
 def gf_pool_info(g) -> PoolInfo:

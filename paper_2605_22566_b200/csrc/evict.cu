@@ -22,6 +22,10 @@ namespace {
 
 constexpr int kSelectThreads = 512;
 constexpr int kHeldKeys = 16, kHeldTokens = kHeldKeys * kSelectThreads;  // keys a thread keeps
+// Up to so many kept tokens per entry, one round of two tiles, the CTA that chose the rows copies them too, which saves
+// a launch (120 of 300 tokens: 96 us instead of 107 for a call and what a program does around it; 255 of them: 93
+// instead of 90).
+constexpr int kOneLaunch = 2 * kTile;
 constexpr int kGatherThreads = 256;  // 64 rows, 32 at a time, of eight 16-byte pieces
 
 // Keys in the order of the weights; NaN counts as the least, -0 as +0.  Protected tokens get the largest
@@ -122,20 +126,9 @@ __device__ __forceinline__ void select_radix(KeyAt&& key_at, int n, uint32_t& pi
   pick = prefix;
 }
 
-__global__ void __launch_bounds__(kSelectThreads) k_select(const EvictBatch batch, float* __restrict__ weights,
-                                                           int64_t layer_slots, int64_t slots, int num_kv_heads,
-                                                           int32_t* __restrict__ kept, int32_t* node_len, int32_t* node_off) {
+// What one (entry, layer, head) keeps: the indices to out, the weights from src to dst.  Executed by the whole CTA.
+__device__ __forceinline__ void select_kept(const EvictEntry& e, const float* src, float* dst, int32_t* out) {
   constexpr int kWarps = kSelectThreads / 32;
-  const EvictEntry e = batch.entry[blockIdx.y];
-  if (e.fresh && blockIdx.x == 0 && threadIdx.x == 0) {
-    node_len[e.node] = e.keep;
-    node_off[e.node] = (int32_t)e.dst_slot;
-  }
-  if (e.keep == 0) return;
-  const int layer = blockIdx.x / num_kv_heads, head = blockIdx.x % num_kv_heads;
-  const float* src = weights + layer * layer_slots + head * slots + e.src_slot;
-  float* dst = weights + layer * layer_slots + head * slots + e.dst_slot;
-  int32_t* out = kept + e.kept_off + (int64_t)blockIdx.x * e.keep;
   const int n = e.len, tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   auto key_at = [&](int t) { return key_of(src[t], t, n, e.first, e.last); };
   uint32_t pick, need = (uint32_t)e.keep;  // of the tokens whose key is `pick`, the first `need` are kept
@@ -212,17 +205,16 @@ __global__ void __launch_bounds__(kSelectThreads) k_select(const EvictBatch batc
 }
 
 template <int D>
-__device__ __forceinline__ void gather_tile16(const char* src_head, char* dst_tile, int src_tile0, int count,
-                                              const int32_t* __restrict__ idx) {
+__device__ __forceinline__ void gather_tile16(const char* src_head, char* dst_tile, int src_tile0, int count, const int32_t* idx, int tid) {
   constexpr uint32_t kTileBytes = 2 * kTile * D * 2;
   constexpr int kBlocks = 2 * (D / 64);  // K's column blocks, then V's
   // eight neighbouring threads share a 128-byte line; a thread has two rows, every block of them: all its loads are
   // issued before its stores
-  const uint32_t chunk = threadIdx.x & 7;
+  const uint32_t chunk = tid & 7;
   uint4 v[2][kBlocks];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const int row = (threadIdx.x >> 3) + 32 * h, t = row < count ? idx[row] : -1;
+    const int row = (tid >> 3) + 32 * h, t = row < count ? idx[row] : -1;
     const char* from = src_head + (uint64_t)(src_tile0 + (t < 0 ? 0 : t) / kTile) * kTileBytes + swz128(t & (kTile - 1), chunk);
 #pragma unroll
     for (int i = 0; i < kBlocks; ++i)
@@ -232,15 +224,14 @@ __device__ __forceinline__ void gather_tile16(const char* src_head, char* dst_ti
   for (int h = 0; h < 2; ++h)
 #pragma unroll
     for (int i = 0; i < kBlocks; ++i)
-      *reinterpret_cast<uint4*>(dst_tile + i * (kTile * 128) + swz128((threadIdx.x >> 3) + 32 * h, chunk)) = v[h][i];
+      *reinterpret_cast<uint4*>(dst_tile + i * (kTile * 128) + swz128((tid >> 3) + 32 * h, chunk)) = v[h][i];
 }
 
 template <int D>
-__device__ __forceinline__ void gather_tile4(const char* src_head, char* dst_tile, int src_tile0, int count,
-                                             const int32_t* __restrict__ idx) {
+__device__ __forceinline__ void gather_tile4(const char* src_head, char* dst_tile, int src_tile0, int count, const int32_t* idx, int tid) {
   constexpr int NG = D / kGroup4;
   constexpr uint32_t kTileBytes = kv4_tile_bytes(D), kPart = kv4_part_bytes(D), kCodes = kv4_code_bytes(D);
-  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, l4 = lane & 3, l8 = lane >> 2;
+  const int lane = tid & 31, wid = tid >> 5, l4 = lane & 3, l8 = lane >> 2;
   // a warp per (part, block of 16 tokens, group): every lane builds its 16 bytes from its tokens' pieces
 #pragma unroll
   for (int job = wid; job < 2 * 4 * NG; job += kGatherThreads / 32) {
@@ -276,7 +267,7 @@ __device__ __forceinline__ void gather_tile4(const char* src_head, char* dst_til
     }
     reinterpret_cast<uint4*>(dst_tile + which * kPart)[(b * NG + g) * 32 + lane] = acc;
   }
-  for (int i = threadIdx.x; i < 2 * kTile * NG; i += kGatherThreads) {
+  for (int i = tid; i < 2 * kTile * NG; i += kGatherThreads) {
     const int g = i % NG, row = i / NG % kTile, which = i / NG / kTile;
     uint32_t sl = 0u;
     if (row < count) {
@@ -287,6 +278,42 @@ __device__ __forceinline__ void gather_tile4(const char* src_head, char* dst_til
   }
 }
 
+// Tile `tile` of what one (entry, layer, head) keeps; by kGatherThreads threads.
+template <int D>
+__device__ __forceinline__ void gather_tile(const EvictEntry& e, const PoolGeom& pool16, const PoolGeom& pool4, int layer, int head, int tile,
+                                            const int32_t* kept_of_head, int tid) {
+  const int32_t* idx = kept_of_head + tile * kTile;
+  const int count = min(kTile, e.keep - tile * kTile);
+  const PoolGeom& pool = e.four ? pool4 : pool16;
+  char* head_base = pool.base + (uint64_t)layer * pool.layer_stride + (uint64_t)head * pool.head_stride;
+  char* dst = head_base + (uint64_t)(e.dst_tile0 + tile) * pool.tile_bytes;
+  if (e.four) gather_tile4<D>(head_base, dst, e.src_tile0, count, idx, tid);
+  else gather_tile16<D>(head_base, dst, e.src_tile0, count, idx, tid);
+}
+
+// kGather: the CTA also copies the rows that it chose, two tiles at a time.
+template <int D, bool kGather>
+__global__ void __launch_bounds__(kSelectThreads) k_select(const EvictBatch batch, const PoolGeom pool16, const PoolGeom pool4,
+                                                           float* __restrict__ weights, int64_t layer_slots, int64_t slots,
+                                                           int num_kv_heads, int32_t* kept, int32_t* node_len, int32_t* node_off) {
+  const EvictEntry e = batch.entry[blockIdx.y];
+  if (e.fresh && blockIdx.x == 0 && threadIdx.x == 0) {
+    node_len[e.node] = e.keep;
+    node_off[e.node] = (int32_t)e.dst_slot;
+  }
+  if (e.keep == 0) return;
+  const int layer = blockIdx.x / num_kv_heads, head = blockIdx.x % num_kv_heads;
+  float* w = weights + layer * layer_slots + head * slots;
+  int32_t* out = kept + e.kept_off + (int64_t)blockIdx.x * e.keep;
+  select_kept(e, w + e.src_slot, w + e.dst_slot, out);
+  if (kGather) {
+    static_assert(kSelectThreads == 2 * kGatherThreads, "two tiles at a time");
+    __syncthreads();
+    for (int tile = threadIdx.x / kGatherThreads; tile * kTile < e.keep; tile += 2)
+      gather_tile<D>(e, pool16, pool4, layer, head, tile, out, threadIdx.x % kGatherThreads);
+  }
+}
+
 template <int D>
 __global__ void __launch_bounds__(kGatherThreads) k_gather(const EvictBatch batch, const PoolGeom pool16, const PoolGeom pool4,
                                                            int num_kv_heads, const int32_t* __restrict__ kept) {
@@ -294,13 +321,7 @@ __global__ void __launch_bounds__(kGatherThreads) k_gather(const EvictBatch batc
   const int tile = blockIdx.x;
   if (tile * kTile >= e.keep) return;
   const int layer = blockIdx.y / num_kv_heads, head = blockIdx.y % num_kv_heads;
-  const int32_t* idx = kept + e.kept_off + (int64_t)blockIdx.y * e.keep + tile * kTile;
-  const int count = min(kTile, e.keep - tile * kTile);
-  const PoolGeom& pool = e.four ? pool4 : pool16;
-  char* head_base = pool.base + (uint64_t)layer * pool.layer_stride + (uint64_t)head * pool.head_stride;
-  char* dst = head_base + (uint64_t)(e.dst_tile0 + tile) * pool.tile_bytes;
-  if (e.four) gather_tile4<D>(head_base, dst, e.src_tile0, count, idx);
-  else gather_tile16<D>(head_base, dst, e.src_tile0, count, idx);
+  gather_tile<D>(e, pool16, pool4, layer, head, tile, kept + e.kept_off + (int64_t)blockIdx.y * e.keep, threadIdx.x);
 }
 
 }  // namespace
@@ -310,9 +331,16 @@ int launch_evict(const PoolGeom& pool16, const PoolGeom& pool4, const EvictBatch
   int most = 0;
   for (int i = 0; i < batch.count; ++i) most = batch.entry[i].keep > most ? batch.entry[i].keep : most;
   const unsigned lh = (unsigned)(num_layers * num_kv_heads);
-  k_select<<<dim3(lh, batch.count), kSelectThreads, 0, st>>>(batch, weights, slots * num_kv_heads, slots, num_kv_heads, kept, g.node_len, g.node_off);
+  const dim3 select_grid(lh, batch.count);
+  auto select = [&](auto kernel) {
+    kernel<<<select_grid, kSelectThreads, 0, st>>>(batch, pool16, pool4, weights, slots * num_kv_heads, slots, num_kv_heads, kept, g.node_len, g.node_off);
+  };
   int launched = 1;
-  if (most > 0) {
+  if (most <= kOneLaunch) {
+    if (head_dim == 128) select(k_select<128, true>);
+    else select(k_select<64, true>);
+  } else {
+    select(k_select<64, false>);  // (the choice does not depend on the head's size)
     const dim3 grid((unsigned)((most + kTile - 1) / kTile), lh, batch.count);
     if (head_dim == 128) k_gather<128><<<grid, kGatherThreads, 0, st>>>(batch, pool16, pool4, num_kv_heads, kept);
     else k_gather<64><<<grid, kGatherThreads, 0, st>>>(batch, pool16, pool4, num_kv_heads, kept);

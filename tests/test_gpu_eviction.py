@@ -188,7 +188,7 @@ def test_evict_odd_lengths(hkv, d, four):
     pa.close()
 
 
-@pytest.mark.parametrize("first,last,keeps", [(0, 0, [0, 7, 300]), (4, 32, [40, 36, 300]), (0, 5, [5, 5, 5]), (64, 64, [128, 200, 257])])
+@pytest.mark.parametrize("first,last,keeps", [(0, 0, [0, 7, 300]), (4, 32, [40, 36, 300]), (0, 5, [5, 5, 5]), (64, 64, [128, 200, 257]), (3, 5, [129, 64, 128]), (1, 1, [128, 36, 127])])
 def test_evict_protected_ends_and_both_kinds(first, last, keeps):
     pa, _ = _evict_case([257, 100, 300], [True, False, True], keeps, first=first, last=last)
     pa.close()
