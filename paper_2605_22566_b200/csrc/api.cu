@@ -972,37 +972,55 @@ static int launch_decode_kernels(gf_wgraph* g, const gf_tables* t, const TablesD
   const int num_items = t->pending ? -1 : t->info.num_items;
   const ResidualEntry* residuals =
       g->res_rows_in_use > 0 ? g->res_table_dev + (size_t)layer * g->desc.max_residual_nodes : nullptr;
-  // segments held in 4 bits: kernels of their own, last in the stream; the others have nothing to do when all are
-  const bool any4 = g->kv4_nodes > 0;
-  const int units = any4 ? t->kv4_wide : 0, rows8 = any4 ? t->kv4_rows8 : 0, rows16 = any4 ? t->kv4_rows16 : 0;
-  auto decode4 = [&](bool chained) {
-    const int a = launch_decode4_wide(g->pool4, g->shape, td, units, layer, q, g->status_dev, chained, st);
-    if (a < 0) return -1;
-    const int b = launch_decode4(g->pool4, g->shape, td, rows8, rows16, layer, q, g->status_dev, chained || a > 0, st);
-    return b < 0 ? -1 : a + b;
+  // Segments held in 4 bits: up to three kernels of their own.  All kernels of a layer work on disjoint items.
+  const bool any4 = g->kv4_nodes > 0, only4 = !t->pending && t->kv4_items > 0 && t->kv4_items == num_items;
+  auto rows16 = [&](bool chained) {
+    return launch_decode4(g->pool4, g->shape, td, 16, any4 ? t->kv4_rows16 : 0, layer, q, g->status_dev, chained, st);
   };
-  if (!t->pending && t->kv4_items > 0 && t->kv4_items == t->info.num_items) return decode4(true);
-  const bool wide = td.wide_min_group > 0 && t->num_wide != 0;
+  auto rows8 = [&](bool chained, cudaStream_t s) {
+    return launch_decode4(g->pool4, g->shape, td, 8, any4 ? t->kv4_rows8 : 0, layer, q, g->status_dev, chained, s);
+  };
+  auto wide4 = [&](bool chained, cudaStream_t s) {
+    return launch_decode4_wide(g->pool4, g->shape, td, any4 ? t->kv4_wide : 0, layer, q, g->status_dev, chained, s);
+  };
+  const bool wide = !only4 && td.wide_min_group > 0 && t->num_wide != 0;
   const int split = wide ? (t->pending ? g->split_hint : t->split_sms) : 0;
-  if (wide && split > 0 && ensure_side_stream(g)) {
-    if (cudaEventRecord(g->ev_fork, st) != cudaSuccess || cudaStreamWaitEvent(g->side_stream, g->ev_fork, 0) != cudaSuccess)
-      return -1;
+  // Where two of them have work for every multiprocessor, one starts on what the other leaves free at its end.
+  auto large = [&](int units) { return (int64_t)units * g->desc.num_kv_heads >= g->num_sms; };
+  const int at_once = !any4 || t->pending ? 0 : large(num_items - t->kv4_items) + large(t->kv4_wide) + large(t->kv4_rows16) + large(t->kv4_rows8);
+  if ((split > 0 || at_once > 1) && ensure_side_stream(g)) {
+    cudaStream_t side = g->side_stream;
+    if (cudaEventRecord(g->ev_fork, st) != cudaSuccess || cudaStreamWaitEvent(side, g->ev_fork, 0) != cudaSuccess) return -1;
+    int n = 0, on_side = 0;
+    bool ok = true;
+    auto count = [&](int launched) {
+      ok = ok && launched >= 0;
+      n += launched;
+      return launched;
+    };
     // the warp kernel first: its CTAs are placed before the other kernel's, and those on the multiprocessors
     // it yields leave at once, so the tensor-memory kernel's first CTAs land there instead of ahead of it
-    const int b = launch_decode(g->pool, g->shape, td, num_items, layer, q, g->status_dev, split, residuals, st);
-    const int a = launch_decode_wide(g->pool, g->shape, td, num_items, layer, q, g->status_dev, 0, split, false, g->side_stream);
-    if (a < 0 || cudaEventRecord(g->ev_join, g->side_stream) != cudaSuccess) return -1;
-    if (cudaStreamWaitEvent(st, g->ev_join, 0) != cudaSuccess || b < 0) return -1;
+    if (!only4) count(launch_decode(g->pool, g->shape, td, num_items, layer, q, g->status_dev, split, residuals, st));
+    if (split > 0) on_side += count(launch_decode_wide(g->pool, g->shape, td, num_items, layer, q, g->status_dev, 0, split, false, side));
+    else if (wide) count(launch_decode_wide(g->pool, g->shape, td, num_items, layer, q, g->status_dev, 0, 0, true, st));
+    on_side += count(wide4(on_side > 0, side));
+    count(rows16(true));
+    count(rows8(on_side > 0, side));
+    // (joined whatever happened, so that nothing of this call is left behind on the side stream)
+    ok = cudaEventRecord(g->ev_join, side) == cudaSuccess && cudaStreamWaitEvent(st, g->ev_join, 0) == cudaSuccess && ok;
     *joined = true;
-    const int c = decode4(false);
-    return c < 0 ? -1 : a + b + c;
+    return ok ? n : -1;
   }
-  const int b = launch_decode(g->pool, g->shape, td, num_items, layer, q, g->status_dev, 0, residuals, st);
-  if (b < 0) return -1;
-  int a = 0;
-  if (wide) a = launch_decode_wide(g->pool, g->shape, td, num_items, layer, q, g->status_dev, 0, 0, true, st);
-  const int c = decode4(true);
-  return a < 0 || c < 0 ? -1 : a + b + c;
+  int n = 0;
+  if (!only4) {
+    const int b = launch_decode(g->pool, g->shape, td, num_items, layer, q, g->status_dev, 0, residuals, st);
+    if (b < 0) return -1;
+    const int a = wide ? launch_decode_wide(g->pool, g->shape, td, num_items, layer, q, g->status_dev, 0, 0, true, st) : 0;
+    if (a < 0) return -1;
+    n = a + b;
+  }
+  const int c = wide4(true, st), d = rows16(true), e = rows8(true, st);
+  return c < 0 || d < 0 || e < 0 ? -1 : n + c + d + e;
 }
 
 // Few (request, head) rows with many partial slots each leave most of the GPU idle under a warp per row (one

@@ -574,9 +574,9 @@ __global__ void __launch_bounds__(kThreads, kCtas4<NT>) k_decode4(const Params p
 
 }  // namespace
 
-int launch_decode4(const PoolGeom& pool, const AttnShape& sh, const TablesDev& t, int rows8, int rows16, int layer,
-                   const void* q, int32_t* status, bool chained, cudaStream_t st) {
-  if (rows8 == 0 && rows16 == 0) return 0;
+int launch_decode4(const PoolGeom& pool, const AttnShape& sh, const TablesDev& t, int rows, int units, int layer, const void* q,
+                   int32_t* status, bool chained, cudaStream_t st) {
+  if (units == 0) return 0;
   Params p;
   p.pool_layer = pool.base + (uint64_t)layer * pool.layer_stride;
   p.head_stride = pool.head_stride;
@@ -588,7 +588,7 @@ int launch_decode4(const PoolGeom& pool, const AttnShape& sh, const TablesDev& t
   p.part_o = t.part_o;
   p.part_ml = t.part_ml;
   p.status = status;
-  p.counters = status + kStatusKv4Queue;
+  p.counters = status + (rows == 8 ? kStatusKv4Queue8 : kStatusKv4Queue);
   p.hdr = t.hdr;
   p.slot_cap = t.slot_cap;
   p.num_q_heads = sh.num_q_heads;
@@ -598,24 +598,24 @@ int launch_decode4(const PoolGeom& pool, const AttnShape& sh, const TablesDev& t
   p.cap_tiles = (int32_t)pool.cap_tiles;
   p.num_pairs = t.num_pairs_in;
   p.num_requests = t.num_requests;
-  auto go = [&](auto kernel, size_t smem, int units, int per_sm, bool (&optin)[kMaxDevices]) {
-    if (units == 0) return true;
+  auto go = [&](auto kernel, size_t smem, int per_sm, bool (&optin)[kMaxDevices]) {
     if (!ensure_dynamic_smem(kernel, smem, optin)) return false;
     const long long warps = units < 0 ? (1ll << 40) : (long long)units * sh.num_kv_heads;
     const long long blocks = (warps + kWarps - 1) / kWarps, most = (long long)per_sm * t.num_sms;
     const dim3 grid((unsigned)(blocks < most ? blocks : most));
     if (chained) launch_chained(kernel, grid, dim3(kThreads), smem, st, p);
-    else kernel<<<grid, dim3(kThreads), smem, st>>>(p);  // behind a join with another stream
-    chained = true;
+    else kernel<<<grid, dim3(kThreads), smem, st>>>(p);  // behind an event of another stream
     return true;
   };
   static bool optin[4][kMaxDevices] = {};
-  const bool ok = sh.head_dim == 128 ? go(k_decode4<128, 2>, kWarps * sizeof(WarpSmem<128, 2>), rows16, kCtas4<2>, optin[0]) &&
-                                           go(k_decode4<128, 1>, kWarps * sizeof(WarpSmem<128, 1>), rows8, kCtas4<1>, optin[1])
-                                     : go(k_decode4<64, 2>, kWarps * sizeof(WarpSmem<64, 2>), rows16, kCtas4<2>, optin[2]) &&
-                                           go(k_decode4<64, 1>, kWarps * sizeof(WarpSmem<64, 1>), rows8, kCtas4<1>, optin[3]);
-  if (!ok) return -1;
-  return cudaGetLastError() == cudaSuccess ? (rows16 != 0) + (rows8 != 0) : -1;
+  bool ok;
+  if (sh.head_dim == 128)
+    ok = rows == 8 ? go(k_decode4<128, 1>, kWarps * sizeof(WarpSmem<128, 1>), kCtas4<1>, optin[1])
+                   : go(k_decode4<128, 2>, kWarps * sizeof(WarpSmem<128, 2>), kCtas4<2>, optin[0]);
+  else
+    ok = rows == 8 ? go(k_decode4<64, 1>, kWarps * sizeof(WarpSmem<64, 1>), kCtas4<1>, optin[3])
+                   : go(k_decode4<64, 2>, kWarps * sizeof(WarpSmem<64, 2>), kCtas4<2>, optin[2]);
+  return ok && cudaGetLastError() == cudaSuccess ? 1 : -1;
 }
 
 }  // namespace gf

@@ -591,7 +591,7 @@ int launch_decode4_wide(const PoolGeom& pool, const AttnShape& sh, const TablesD
   p.part_o = t.part_o;
   p.part_ml = t.part_ml;
   p.status = status;
-  p.counters = status + kStatusKv4Queue;
+  p.counters = status + kStatusKv4WideQueue;
   p.hdr = t.hdr;
   p.slot_cap = t.slot_cap;
   p.num_q_heads = sh.num_q_heads;
@@ -606,7 +606,7 @@ int launch_decode4_wide(const PoolGeom& pool, const AttnShape& sh, const TablesD
   auto go = [&](auto kernel, size_t smem, bool (&optin)[kMaxDevices]) {
     if (!ensure_dynamic_smem(kernel, smem, optin)) return false;
     if (chained) launch_chained(kernel, grid, dim3(kThreads), smem, st, p);
-    else kernel<<<grid, dim3(kThreads), smem, st>>>(p);  // behind a join with another stream
+    else kernel<<<grid, dim3(kThreads), smem, st>>>(p);  // behind an event of another stream
     return true;
   };
   static bool optin[2][kMaxDevices] = {};

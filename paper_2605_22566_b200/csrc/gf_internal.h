@@ -16,14 +16,16 @@ enum StatusWord {
   kStatusGiveUp = 1,       // non-zero: a bounded device wait gave up (GF_ERR_TIMEOUT)
   kStatusBounds = 2,       // debug build only: the largest site code of a range check that failed (GF_ERR_BOUNDS)
   kStatusDecodeQueue = 4,  // [0] next unit of the warp decode kernel, [1] its CTAs that finished
-  kStatusKv4Queue = 6,     // the same pair for the decode kernel over 4-bit states
+  kStatusKv4Queue = 6,     // the same pair for the decode kernel over 4-bit states that takes 16 rows
   kStatusWideQueue = 8,    // the same pair for the tensor-memory decode kernel
+  kStatusKv4Queue8 = 10,   // the one that takes 8
+  kStatusKv4WideQueue = 16, // and the one for widely shared chunks
   kStatusProbe = 3,        // what the wait probe's waiter saw (gf_debug_wait_probe)
   kStatusRescales = 12,    // diagnostic: times a tensor-memory tile moved its softmax reference after its first stage
   kStatusReruns = 13,      // diagnostic: times the exact tensor-memory kernel redid the work of the launch before it
   kStatusOverflow = 14,    // raised by a tensor-memory kernel that met a score too far above its lagging maximum
   kStatusExactDone = 15,   // CTAs of the exact kernel that finished (the last one lowers the flag)
-  kStatusWords = 16
+  kStatusWords = 18
 };
 
 // One work item: a chunk of one shared segment for one tile of the requests that share it.
@@ -310,12 +312,12 @@ int launch_kv4_write(const PoolGeom& pool, int layer, int num_kv_heads, int head
                      const void* v, int n_tokens, const GraphDev* set, int node, int token_off, int num_sms, cudaStream_t st);
 int launch_kv4_read(const PoolGeom& pool, int layer, int num_kv_heads, int head_dim, int tile0, void* k, void* v,
                     int n_tokens, int num_sms, cudaStream_t st);
-// rows8, rows16: 16-row groups with up to 8 query rows and the others; units: chunks x 128 rows.  < 0: not known on
-// the host.  chained: see launch_decode_wide.
+// units: chunks x 128 rows; 16-row groups with up to 8 query rows (rows = 8) or the others (rows = 16).  < 0: not
+// known on the host.  chained: see launch_decode_wide.
 int launch_decode4_wide(const PoolGeom& pool, const AttnShape& sh, const TablesDev& t, int units, int layer, const void* q,
                         int32_t* status, bool chained, cudaStream_t st);
-int launch_decode4(const PoolGeom& pool, const AttnShape& sh, const TablesDev& t, int rows8, int rows16, int layer,
-                   const void* q, int32_t* status, bool chained, cudaStream_t st);
+int launch_decode4(const PoolGeom& pool, const AttnShape& sh, const TablesDev& t, int rows, int units, int layer, const void* q,
+                   int32_t* status, bool chained, cudaStream_t st);
 int launch_weights(const PoolGeom& pool16, const PoolGeom& pool4, const AttnShape& sh, const TablesDev& t, int layer, const void* q,
                    const float* lse, int accumulate, float* weights, int64_t slots, int32_t* status, cudaStream_t st);
 int launch_evict(const PoolGeom& pool16, const PoolGeom& pool4, const EvictBatch& batch, int num_layers, int num_kv_heads,
