@@ -22,6 +22,7 @@ struct gf_tables {
   int32_t num_wide = -1;       // items flagged wide; -1: not known on the host (deferred, or phase B still to run)
   int32_t kv4_items = -1;      // items held in 4 bits; the units of their three kernels (see Header);
   int32_t kv4_wide = -1;       // -1: not known on the host
+  int32_t max_group = -1;      // likewise: most requests that share a segment
   int32_t kv4_rows8 = -1;
   int32_t kv4_rows16 = -1;
   int32_t split_sms = 0;       // multiprocessors the tensor-memory decode kernel gets beside the warp kernel (0: one after the other)
@@ -737,6 +738,7 @@ static gf_status_t read_back_tables(gf_tables* T) {
   T->num_wide = h.num_wide;
   T->kv4_items = h.kv4_items;
   T->kv4_wide = h.kv4_wide;
+  T->max_group = h.max_group;
   T->kv4_rows8 = h.kv4_rows8;
   T->kv4_rows16 = h.kv4_rows16;
   T->owner->wide_hint = h.wide_units >= T->dev.wide_min_units;
@@ -830,7 +832,7 @@ gf_status_t gf_build_path_tables(gf_wgraph_t* g, int32_t num_requests, int32_t n
   }
   T.pending = false;
   T.num_wide = -1;
-  T.kv4_items = T.kv4_wide = T.kv4_rows8 = T.kv4_rows16 = -1;
+  T.kv4_items = T.kv4_wide = T.kv4_rows8 = T.kv4_rows16 = T.max_group = -1;
   T.error = GF_OK;
   T.build_stream = st;
   T.info = gf_tables_info_t{};
@@ -1154,8 +1156,16 @@ gf_status_t gf_path_attention_weights(gf_wgraph_t* g, const gf_tables_t* t, int3
   DeviceGuard dev(g->device);
   if (!dev.ok) return GF_ERR_CUDA;
   const int64_t slots = gf_weight_slots(g);
+  cudaStream_t st = (cudaStream_t)stream, side = nullptr;
+  const int gqa = g->shape.num_q_heads / g->shape.num_kv_heads, most_rows = t->pending ? -1 : t->max_group * gqa;
+  // a batch for both kernels, with tiles for every multiprocessor: one starts on what the other leaves free at its end
+  if (most_rows > kNarrowRows && t->info.resident_tokens / kTile * g->desc.num_kv_heads >= 4ll * g->num_sms && ensure_side_stream(g)) {
+    side = g->side_stream;
+    if (cudaEventRecord(g->ev_fork, st) != cudaSuccess || cudaStreamWaitEvent(side, g->ev_fork, 0) != cudaSuccess) return GF_ERR_CUDA;
+  }
   const int n = launch_weights(g->pool, g->pool4, g->shape, t->dev, layer, q_dev, lse_dev, accumulate,
-                               weights_dev + (int64_t)layer * g->desc.num_kv_heads * slots, slots, g->status_dev, (cudaStream_t)stream);
+                               weights_dev + (int64_t)layer * g->desc.num_kv_heads * slots, slots, most_rows, g->status_dev, st, side);
+  if (side && (cudaEventRecord(g->ev_join, side) != cudaSuccess || cudaStreamWaitEvent(st, g->ev_join, 0) != cudaSuccess)) return GF_ERR_CUDA;
   if (n < 0) return GF_ERR_CUDA;
   g->launches += n;
   return GF_OK;

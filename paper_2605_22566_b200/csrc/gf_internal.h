@@ -49,6 +49,8 @@ __host__ __device__ inline int kv4_length_class(int chunk) {
   const int t = chunk / kTile;
   return t >= 32 ? 0 : t >= 16 ? 1 : t >= 12 ? 2 : t >= 8 ? 3 : t >= 6 ? 4 : t >= 4 ? 5 : t >= 2 ? 6 : 7;
 }
+// Query rows up to which a segment's attention weights go to the kernel without roles.
+constexpr int kNarrowRows = 64;
 // Query rows (of `total`, gqa per request) that the tcgen05 kernel gets, when group tiles divide its units.
 __host__ __device__ inline int kv4_wide_rows(int total, int group_rows) {
   if (kKv4WideUnit % group_rows != 0) return 0;
@@ -80,6 +82,7 @@ struct Header {
   int32_t kv4_rows16_first;
   int32_t kv4_next[3][kKv4Classes];  // where the next entry goes: lists (8 rows, 16, wide) by length class, the longest first
   int32_t kv4_tokens;  // tokens of the segments held in 4 bits
+  int32_t max_group;   // most requests that share a segment
   unsigned long long resident_tokens;
   unsigned long long materialised_tokens;
   unsigned long long num_q_rows;
@@ -318,8 +321,10 @@ int launch_decode4_wide(const PoolGeom& pool, const AttnShape& sh, const TablesD
                         int32_t* status, bool chained, cudaStream_t st);
 int launch_decode4(const PoolGeom& pool, const AttnShape& sh, const TablesDev& t, int rows, int units, int layer, const void* q,
                    int32_t* status, bool chained, cudaStream_t st);
+// most_rows: query rows of the segment that has most, < 0: not known on the host.  side: a stream behind `st` that the
+// second of the two kernels may use, or null.
 int launch_weights(const PoolGeom& pool16, const PoolGeom& pool4, const AttnShape& sh, const TablesDev& t, int layer, const void* q,
-                   const float* lse, int accumulate, float* weights, int64_t slots, int32_t* status, cudaStream_t st);
+                   const float* lse, int accumulate, float* weights, int64_t slots, int most_rows, int32_t* status, cudaStream_t st, cudaStream_t side);
 int launch_evict(const PoolGeom& pool16, const PoolGeom& pool4, const EvictBatch& batch, int num_layers, int num_kv_heads,
                  int head_dim, float* weights, int64_t slots, int32_t* kept, const GraphDev& g, cudaStream_t st);
 int launch_wait_probe(int32_t* status, long long limit, int32_t* returned, cudaStream_t st);

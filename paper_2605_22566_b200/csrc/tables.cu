@@ -83,7 +83,7 @@ __global__ void k_init(TablesDev t, int num_nodes) {
     h.wide_tokens = 0;
     h.wide_tile_units = 0;
     h.stream_steps = 0;
-    h.kv4_items = h.kv4_wide = h.kv4_rows8 = h.kv4_rows16 = h.kv4_wide_first = h.kv4_rows16_first = h.kv4_tokens = 0;
+    h.kv4_items = h.kv4_wide = h.kv4_rows8 = h.kv4_rows16 = h.kv4_wide_first = h.kv4_rows16_first = h.kv4_tokens = h.max_group = 0;
     for (int i = 0; i < 3 * kKv4Classes; ++i) h.kv4_next[i / kKv4Classes][i % kKv4Classes] = 0;
     h.max_q_rows = 0;
     h.resident_tokens = h.materialised_tokens = h.num_q_rows = 0ull;
@@ -171,12 +171,12 @@ __global__ void k_scan_nodes_segments(GraphDev g, TablesDev t, gf_policy_t pol) 
   __shared__ unsigned long long red[32];
   __shared__ int warp_tot[32];
   __shared__ int carry_s;
-  __shared__ int wide_units, wide_work, wide_tokens, wide_tile_units, stream_steps;
+  __shared__ int wide_units, wide_work, wide_tokens, wide_tile_units, stream_steps, max_group;
   // units by length class: 16-row groups with up to 8 rows, the others; with the wide kernel (rows it leaves, its own) and without
   __shared__ int32_t kv4_all[2][kKv4Classes], kv4_split[3][kKv4Classes];
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, nw = blockDim.x >> 5;
   const int n = g.num_nodes;
-  if (tid == 0) { carry_s = 0; wide_units = 0; wide_work = 0; wide_tokens = 0; wide_tile_units = 0; stream_steps = 0; }
+  if (tid == 0) { carry_s = 0; wide_units = 0; wide_work = 0; wide_tokens = 0; wide_tile_units = 0; stream_steps = 0; max_group = 0; }
   if (tid < 3 * kKv4Classes) kv4_split[tid / kKv4Classes][tid % kKv4Classes] = 0;
   if (tid < 2 * kKv4Classes) kv4_all[tid / kKv4Classes][tid % kKv4Classes] = 0;
   __syncthreads();
@@ -233,6 +233,7 @@ __global__ void k_scan_nodes_segments(GraphDev g, TablesDev t, gf_policy_t pol) 
   for (int s = tid; s < S; s += blockDim.x) {
     const int G = t.grp_ptr[s];
     const int l = t.seg_len[s];
+    atomicMax(&max_group, G);
     const bool four = t.seg_off[s] / kTile >= t.kv4_tile0;
     const int most = four ? min(pol.max_chunk_mult, kKv4ChunkMult) : pol.max_chunk_mult;
     const int mult = min(most, max(1, ceil_div(G, pol.group_unit)));
@@ -286,6 +287,7 @@ __global__ void k_scan_nodes_segments(GraphDev g, TablesDev t, gf_policy_t pol) 
     t.hdr->wide_tokens = wide_tokens;
     t.hdr->wide_tile_units = wide_tile_units;
     t.hdr->stream_steps = stream_steps;
+    t.hdr->max_group = max_group;
     if (wide_units < t.wide_min_units) t.hdr->num_wide = 0;
     t.hdr->kv4_wide_first = t.hdr->num_wide > 0 ? wide_units : 0;
     // The tcgen05 kernel's units take two per multiprocessor as long as one: with fewer than that many, the rows are

@@ -36,7 +36,6 @@
 namespace gf {
 namespace {
 
-constexpr int kNarrowRows = 64;
 constexpr int kNarrowThreads = 128;
 constexpr int kThreads = 640;
 constexpr int kBlock = 128;     // tokens of a unit
@@ -771,7 +770,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_weights_wide(const Params p) {
 }  // namespace
 
 int launch_weights(const PoolGeom& pool16, const PoolGeom& pool4, const AttnShape& sh, const TablesDev& t, int layer, const void* q,
-                   const float* lse, int accumulate, float* weights, int64_t slots, int32_t* status, cudaStream_t st) {
+                   const float* lse, int accumulate, float* weights, int64_t slots, int most_rows, int32_t* status, cudaStream_t st, cudaStream_t side) {
+  const bool any_wide = most_rows < 0 || most_rows > kNarrowRows;
   Params p;
   p.layer16 = pool16.base + (uint64_t)layer * pool16.layer_stride;
   p.layer4 = pool4.base ? pool4.base + (uint64_t)layer * pool4.layer_stride : nullptr;
@@ -803,15 +803,17 @@ int launch_weights(const PoolGeom& pool16, const PoolGeom& pool4, const AttnShap
   p.status = status;
   auto go = [&](auto wide, auto narrow, size_t narrow_smem, bool (&optin)[2][kMaxDevices]) {
     if (!ensure_dynamic_smem(wide, sizeof(Smem), optin[0]) || !ensure_dynamic_smem(narrow, narrow_smem, optin[1])) return false;
-    launch_chained(wide, dim3((unsigned)t.num_sms), dim3(kThreads), sizeof(Smem), st, p);
-    launch_chained(narrow, dim3((unsigned)(3 * t.num_sms)), dim3(kNarrowThreads), narrow_smem, st, p);
+    if (any_wide) launch_chained(wide, dim3((unsigned)t.num_sms), dim3(kThreads), sizeof(Smem), st, p);
+    const dim3 grid((unsigned)(3 * t.num_sms));
+    if (side) narrow<<<grid, kNarrowThreads, narrow_smem, side>>>(p);
+    else launch_chained(narrow, grid, dim3(kNarrowThreads), narrow_smem, st, p);
     return true;
   };
   static bool optin[2][2][kMaxDevices] = {};
   if (!(sh.head_dim == 128 ? go(k_weights_wide<128>, k_weights_narrow<128>, sizeof(NarrowSmem<128>), optin[0])
                            : go(k_weights_wide<64>, k_weights_narrow<64>, sizeof(NarrowSmem<64>), optin[1])))
     return -1;
-  return cudaGetLastError() == cudaSuccess ? 2 : -1;
+  return cudaGetLastError() == cudaSuccess ? 1 + any_wide : -1;
 }
 
 }  // namespace gf
