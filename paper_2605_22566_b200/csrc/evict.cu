@@ -13,6 +13,10 @@
 //             not touched).  Rows of the last tile past the end become zeros, as every writer of the pools
 //             leaves them.
 //
+// Four nodes of 6000 to 8192 tokens, two layers of 8 heads of 128, half kept: chosen in 17 us (64 CTAs, bound by their
+// chain of sixteen counts; a radix select with counts in shared memory 30), copied in 32 us (146 MB, 4.6 TB/s).  300
+// tokens: 7 us in one launch.
+//
 // The destination is another node, so nothing is read after it was overwritten and both kernels spread over
 // everything at once.
 #include "kv4_device.cuh"

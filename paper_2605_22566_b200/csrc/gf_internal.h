@@ -38,10 +38,11 @@ struct __align__(32) Item {
 };
 
 // Longest chunk of a segment held in 4 bits, in multiples of the policy's chunk_tokens: its kernel gives a chunk's
-// 16 query rows to one warp, which has to come to an end.
+// 16 query rows to one warp, which has to come to an end.  256 requests: 163 us with 2, 172 with 4, 182 with 8 (fewer
+// partials against later ends); 1024 requests: 504, 475 and 465.
 constexpr int kKv4ChunkMult = 4;
 // A chunk of such a segment goes 128 stacked query rows at a time to the tcgen05 kernel; where fewer rows than this
-// are left, to the kernels that take 16.
+// are left, to the kernels that take 16 (1024 requests: 464 us with 64, 467 with 128, 495 with 32).
 constexpr int kKv4WideUnit = 128, kKv4WideRows = 64;
 // Length class of a chunk: the kernels take the longest first, so that no long one is begun when the others end.
 constexpr int kKv4Classes = 8;
@@ -49,7 +50,8 @@ __host__ __device__ inline int kv4_length_class(int chunk) {
   const int t = chunk / kTile;
   return t >= 32 ? 0 : t >= 16 ? 1 : t >= 12 ? 2 : t >= 8 ? 3 : t >= 6 ? 4 : t >= 4 ? 5 : t >= 2 ? 6 : 7;
 }
-// Query rows up to which a segment's attention weights go to the kernel without roles.
+// Query rows up to which a segment's attention weights go to the kernel without roles (32: 94 and 134 us for 256 and 512
+// requests; 64: 93 and 138; all in the kernel with roles: 99 and 133, and 201 instead of 173 where all is held in 4 bits).
 constexpr int kNarrowRows = 64;
 // Query rows (of `total`, gqa per request) that the tcgen05 kernel gets, when group tiles divide its units.
 __host__ __device__ inline int kv4_wide_rows(int total, int group_rows) {

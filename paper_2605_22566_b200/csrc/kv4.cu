@@ -1,8 +1,9 @@
 // Node states held in 4 bits: put there from bf16 (k_kv4_write) and read back as the values that the
 // codes stand for (k_kv4_read).  Format and layout: kv4_device.cuh.
 //
-// Both are streams: 2 bytes of bf16 per entry on one side, 0.5625 on the other, nothing reused, so they are
-// bound by HBM (and by the launch, for a short node).  A warp works on one block of 16 tokens of one KV
+// Both are streams: 2 bytes of bf16 per entry on one side, 0.5625 on the other, nothing reused.  32 768 tokens of 8 heads
+// of 128, 172 MB either way: read in 28.6 us (6.0 TB/s, bound by HBM), written in 48 us (3.6 TB/s, bound by the
+// instructions of the exact quotients, 16 per entry; 113 us with divisions).  A short node costs its launch.  A warp works on one block of 16 tokens of one KV
 // head and one group of 64 entries, K or V: 2 KB of bf16, 512 bytes of codes.  The layout gives every lane
 // 16-byte runs on both sides, so nothing goes through shared memory; a token's least and largest entry are
 // found with shuffles among the lanes that hold it.

@@ -10,16 +10,22 @@
 // multiplied, exact in bf16, and the token's (s, lo) enter outside of the product, in fp32:
 //   s_t = sum over groups G of  s_tG (c . q_G)  +  (lo_tG + s_tG / 2) (sum of q_G)
 //
-// Two kernels, by how many query rows share a segment:
+// Two kernels, by how many query rows share a segment, beside each other on two streams:
 //
-// Up to kNarrowRows (k_weights_narrow): bound by the stream of K.  A warp copies 64 tokens of K into its piece of
-// shared memory and walks the rows eight at a time: S^T = K Q^T (mma.sync), exp2, sums per token in registers; at
-// the end a shuffle over the four lanes that share a token.  Nothing is shared between warps.
+// Up to kNarrowRows (k_weights_narrow): a stream of K, 64 tokens of it at a time copied into a warp's own piece of
+// shared memory; the warp walks the rows eight at a time: S^T = K Q^T (mma.sync), exp2, sums per token in
+// registers, and at the end a shuffle over the four lanes that share a token.  Nothing is shared between warps.
+// 256 requests, 256 nodes, a third in bf16: 73 us (K alone at the copy rate: 45), bound by the round trips of a unit (K, then
+// queries, sums before) that twelve warps per SM, as many as K finds room for, do not hide.  Walking K once for 16
+// rows spilled and took 120 us; queries through 4-byte loads in K's natural order 80.
 //
-// More (k_weights_wide): bound by the exponentials (16 per clock and SM).  tcgen05 MMAs with the tokens as
-// rows make the reduction run along the columns of tensor memory: a thread owns a token, reads its scores
-// 16 at a time and adds up 2^(scale s - lse), without a shuffle.  Keys come as they lie in the pool
-// (128-byte-swizzled, the operand layout) or are expanded from their codes, one accumulator per group.
+// More (k_weights_wide): tcgen05 MMAs with the tokens as rows make the reduction run along the columns of tensor
+// memory: a thread owns a token, reads its scores 16 at a time and adds up 2^(scale s - lse), without a shuffle.
+// Keys come as they lie in the pool (128-byte-swizzled, the operand layout) or are expanded from their codes, one
+// accumulator per group.  2048 rows over 8192 tokens and 8 heads: 77 us in bf16, 100 in 4 bits; the exponentials
+// alone, 16 per clock and SM, are 31.  Two warps per scheduler take 345 cycles for the 16 columns that need 256 of
+// the exponential unit, and wait a quarter of the time for queries or a unit's end; units of 256 tokens, which fetch
+// the queries half as often, or loads one step ahead changed nothing.
 // One persistent CTA per SM, roles by warp, work in items of up to 64 rows of a unit of 128 tokens:
 //   warp 19       resolves units (a fixed stride over all of them, 32 at a time) into a ring of eight
 //   warps 14-17   keys: bulk copies, or the expansion of 4-bit codes, into three stages of 128 tokens
