@@ -1,28 +1,29 @@
 // K2 over node states held in 4 bits, widely shared chunks: decode on tcgen05 tensor cores.
 //
 // A unit is a chunk of a 4-bit segment and up to 128 stacked query rows (request x GQA head) of the requests that
-// share it.  The codes are expanded once per unit instead of once per 16 rows (decode4.cu), into shared memory,
-// as fp16 subnormals c 2^-24 and 16 c 2^-24 (exact), and S = Q C^T and O += P C run as tcgen05 MMAs with
-// accumulators in tensor memory, one pair per group of 64 entries, because a token's (s, lo) differ by group:
-//   S_rt = sum over groups G of  s_tG (q_rG . c_tG)  +  (lo_tG + s_tG / 2) (sum of q_rG)
+// share it.  The codes are expanded once per unit instead of once per 16 rows (decode4.cu), into shared memory, and
+// S = Q K^T and O += P C run as tcgen05 MMAs with accumulators in tensor memory:
+//   K as the values that the codes stand for, in fp16 times a power of two per 16 tokens, so that a score takes one
+//   multiplication; V as codes, fp16 subnormals c 2^-24 and 16 c 2^-24 (exact), one accumulator per group of 64
+//   entries, because values of different tokens may lie any power of two apart and none may be lost:
 //   O_rG = sum over tokens of  (p_rt s_tG) c_tG  +  sum of  p_rt (lo_tG + s_tG / 2)
-// A thread owns a query row: it takes the 32 scores of a step from tensor memory, applies the tokens' scales
-// (tables in shared memory, read as broadcasts), exponentiates, keeps l and the second term of O in fp32, and
-// puts p s f over the scores as fp16, one P per group.  Reference, f and roundings are those of decode4.cu.
+// A thread owns a query row: it takes the 32 scores of a step from tensor memory, exponentiates, applies the
+// tokens' scales (tables in shared memory, read as broadcasts), keeps l and the second term of O in fp32, and puts
+// p s f over the scores as fp16, one P per group.  Reference, f and roundings are those of decode4.cu.
 //
 // Two CTAs per SM, whose phases fill each other's gaps.  Roles by warp:
 //   warps 0-3  softmax, a row per thread; at the end of a unit its fp32 partial
-//   warps 4-7  the unit's queries (fp16 times a power of two per row, their sums), then a block of 16 tokens
+//   warps 4-7  the unit's queries (fp16 times a power of two per row), then a block of 16 tokens
 //              each of every tile: codes and scale tables
 //   warp 8     claims units, streams their tiles as they lie in the pool (bulk copies, three in flight)
 //   warp 9     one thread issues the MMAs  (warps 10 and 11 only complete the group whose registers are handed over)
 // Every wait is bounded; a warp whose wait gave up leaves its role, and so do the others.
 //
-// 1024 requests, 608 units of mostly 128 rows, 8776 tiles of 64 tokens: 139 us; without this kernel the 16-row kernel
-// takes 170 us for the same.  A step alone on an SM takes 1700 cycles: 590 for the scores, 350 to settle the reference, 490
-// for p and its products, the rest waits; two CTAs interleave to 2600 for two.  Bound by the latency of one warp per
-// scheduler and CTA: tensor memory holds no third CTA.  Steps of a whole tile with one S: 169 us, because an MMA
-// or a commit costs its issuing thread 60 cycles, in the chain between two softmaxes.
+// 1024 requests, 608 units of mostly 128 rows, 8776 tiles of 64 tokens: 119 us (the 16-row kernel takes 170 for the
+// same).  Bound by the latency of one softmax warp per scheduler and CTA, two CTAs being what tensor memory holds, and by
+// shared memory: the scales' broadcasts cost 512 of a step's 1800 cycles, the MMAs' operands 400.  Measured before:
+// K as codes with its scales applied to the scores, twice the broadcasts, 139 us; steps of a whole tile with one S, 155:
+// an MMA or a commit costs its issuing thread 60 cycles, and there they stood between two softmaxes.
 #include "kv4_device.cuh"
 #include "tc_device.cuh"
 
@@ -62,8 +63,8 @@ struct __align__(16) Unit {
   int32_t grp_begin, part_base, kvh, tok_count, ntile, pad0, pad1;
 };
 
-// s and z = lo + s / 2 of a tile's tokens, [group][token]; of K's s times what undoes the operand's unit.
-struct Scales { float s[2][kTile], z[2][kTile]; };
+// s and z = lo + s / 2 of a tile's V, [group][token], and the powers of two that K's blocks of 16 tokens were divided by.
+struct Scales { float s[2][kTile], z[2][kTile], k[kTile / 16]; };
 
 template <int D>
 struct Smem {
@@ -72,8 +73,8 @@ struct Smem {
   unsigned char k[CB][kTile * 128];       // codes of a tile, K-major
   unsigned char v[CB][kTile * 128];       // and MN-major: both are rows of a token's 64 entries
   unsigned char stage[kStages][kv4_tile_bytes(D)];
-  Scales ks[kStages], vs[kStages];        // of tile n at n % kStages
-  float row_sum[2][kRows], row_scale[kRows];  // sums of q per group; softmax scale over the row's power of two
+  Scales scales[kStages];                 // of tile n at n % kStages
+  float row_scale[kRows];                 // softmax scale over the row's power of two
   Unit unit[kUnits];
   uint32_t tmem_base;
   uint64_t unit_full[kUnits], unit_empty[kUnits];
@@ -144,7 +145,7 @@ __device__ __forceinline__ void produce(Smem<D>& sm, const Params& p, int num_un
 }
 
 // ---- warps 4-7: queries and codes --------------------------------------------------------------------------
-// 32 query rows of the warp: fp16 times a power of two per row, their sums per group.
+// 32 query rows of the warp: fp16 times a power of two per row.
 template <int D>
 __device__ __forceinline__ void load_queries(Smem<D>& sm, const Params& p, const Unit& u, int row0, int lane) {
   constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;  // lanes per row, rows per load
@@ -174,40 +175,57 @@ __device__ __forceinline__ void load_queries(Smem<D>& sm, const Params& p, const
       for (int d = 1; d < kLanes; d <<= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, d));
       const float mul = pow2_to(big, 14);
       uint32_t h[4];
-      float sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        h[i] = pack_f16(__uint_as_float(w[i] << 16) * mul, __uint_as_float(w[i] & 0xffff0000u) * mul);
-        const float2 r = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
-        sum += r.x + r.y;
-      }
-#pragma unroll
-      for (int d = 1; d < 8; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+      for (int i = 0; i < 4; ++i) h[i] = pack_f16(__uint_as_float(w[i] << 16) * mul, __uint_as_float(w[i] & 0xffff0000u) * mul);
       *reinterpret_cast<uint4*>(sm.q[chunk / 8] + swz128(row, chunk % 8)) = make_uint4(h[0], h[1], h[2], h[3]);
-      if (chunk % 8 == 0) sm.row_sum[chunk / 8][row] = sum;
       if (chunk == 0) sm.row_scale[row] = p.scale_log2 * pow2_inverse(mul);
     }
   }
 }
 
-// Block b (16 tokens) of a tile's K: tokens l8 and l8 + 8, in units of 2^-24 and 2^-20.
+// Block b (16 tokens) of a tile's K: the values that the codes stand for, times a power of two that brings the block's
+// largest to 2^14..2^15, rounded to fp16 (2^-11 of a value; a score is wrong by 2^-11 of the sum of its terms at most,
+// where bf16 keys would be by 2^-8).  1024 + c and 1024 + 16 c are fp16 patterns with the code in their low bits.
 template <int D>
-__device__ __forceinline__ void expand_k(Smem<D>& sm, const char* part, int b, int lane) {
+__device__ __forceinline__ void expand_k(Smem<D>& sm, Scales& to, const char* part, int b, int lane) {
   constexpr int NG = D / kGroup4;
   const int l4 = lane & 3, l8 = lane >> 2;
+  // the block's numbers, a token per lane (twice)
+  uint32_t sl[NG], sz[NG];
+  float big = 0.f;
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    sl[g] = reinterpret_cast<const uint32_t*>(part + kv4_code_bytes(D))[(b * 16 + (lane & 15)) * NG + g];
+    const float s = kv4_s(sl[g]), lo = kv4_lo(sl[g]);
+    big = fmax3(big, fabsf(lo), fabsf(fmaf(16.f, s, lo)));
+  }
+  const float mul = pow2_to(__uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(big))), 14);
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    const float s = kv4_s(sl[g]);
+    sz[g] = pack_f16(s * mul, fmaf(0.5f, s, kv4_lo(sl[g])) * mul);
+  }
+  if (lane == 0) to.k[b] = pow2_inverse(mul);
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
     const uint4 c = reinterpret_cast<const uint4*>(part)[(b * NG + g) * 32 + lane];
     const uint32_t w[4] = {c.x, c.y, c.z, c.w};
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const uint32_t mask = h ? 0x00f000f0u : 0x000f000fu, row = b * 16 + l8 + 8 * h;
+      const uint32_t mask = h ? 0x00f000f0u : 0x000f000fu, row = b * 16 + l8 + 8 * h, token = __shfl_sync(0xffffffffu, sz[g], l8 + 8 * h);
+      const uint32_t s2 = __byte_perm(token, 0u, 0x1010u), z2 = __byte_perm(token, 0u, 0x3232u);
+      __half2 step = *reinterpret_cast<const __half2*>(&s2);
+      if (h) step = __hmul2(step, __float2half2_rn(0.0625f));
+      const __half2 least = *reinterpret_cast<const __half2*>(&z2), bias = __float2half2_rn(-1024.f);
       uint32_t x[8];
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk) {
-        x[2 * kk] = w[kk] & mask;
-        x[2 * kk + 1] = (w[kk] >> 8) & mask;
-      }
+      for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t code = ((e ? w[kk] >> 8 : w[kk]) & mask) | 0x64006400u;
+          const __half2 v = __hfma2(__hadd2(*reinterpret_cast<const __half2*>(&code), bias), step, least);
+          x[2 * kk + e] = *reinterpret_cast<const uint32_t*>(&v);
+        }
       *reinterpret_cast<uint4*>(sm.k[g] + swz128(row, l4)) = make_uint4(x[0], x[1], x[2], x[3]);
       *reinterpret_cast<uint4*>(sm.k[g] + swz128(row, 4 + l4)) = make_uint4(x[4], x[5], x[6], x[7]);
     }
@@ -234,28 +252,23 @@ __device__ __forceinline__ void expand_v(Smem<D>& sm, const char* part, int b, i
   }
 }
 
-// The scales of block b, of K by the lanes 0..15 and of V by the others.
+// The scales of block b of V: a token and a group per lane.
 template <int D>
-__device__ __forceinline__ void expand_scales(Scales& ks, Scales& vs, const char* tile, int b, int lane) {
+__device__ __forceinline__ void expand_scales(Scales& to, const char* part, int b, int lane) {
   constexpr int NG = D / kGroup4;
-  const bool v = lane >= 16;
-  const int t = b * 16 + (lane & 15);
-  Scales& to = v ? vs : ks;
-  const uint32_t* words = reinterpret_cast<const uint32_t*>(tile + (v ? kv4_part_bytes(D) : 0) + kv4_code_bytes(D)) + t * NG;
-  const float unit = v ? 1.f : (lane & 8) ? kUnit1 : kUnit0;
-#pragma unroll
-  for (int g = 0; g < NG; ++g) {
-    const float s = kv4_s(words[g]);
-    to.s[g][t] = s * unit;
-    to.z[g][t] = fmaf(0.5f, s, kv4_lo(words[g]));
-  }
+  const int t = b * 16 + (lane & 15), g = lane >> 4;
+  if (g >= NG) return;
+  const uint32_t sl = reinterpret_cast<const uint32_t*>(part + kv4_code_bytes(D))[t * NG + g];
+  const float s = kv4_s(sl);
+  to.s[g][t] = s;
+  to.z[g][t] = fmaf(0.5f, s, kv4_lo(sl));
 }
 
 template <int D>
 __device__ __forceinline__ void expand(Smem<D>& sm, const Params& p, int w, int lane) {
   int tile = 0, step = 0;  // the next one, and its first step
   for_units(sm, p, lane, [&](int n, const Unit& u) {
-    // the unit before has its last scores, and its rows' sums have been read
+    // the unit before has its last scores, and its rows' scales have been read
     if (n > 0 && (!wait_step(sm.s_full, step - 1, p) || !wait(&sm.q_empty, n - 1, p))) return false;
     load_queries(sm, p, u, w * 32, lane);
     fence_proxy_async_smem();
@@ -266,8 +279,9 @@ __device__ __forceinline__ void expand(Smem<D>& sm, const Params& p, int w, int 
       if (!wait(&sm.stage_full[st], tile / kStages, p)) return false;
       const char* at = reinterpret_cast<const char*>(sm.stage[st]);
       if (tile > 0 && !wait_step(sm.s_full, step - 1, p)) return false;  // K of the tile before has been read
-      expand_scales<D>(sm.ks[st], sm.vs[st], at, w, lane);  // (tile - 1 and tile - 2 may still be in the softmax, tile - 3 not)
-      expand_k<D>(sm, at, w, lane);
+      // (scales: tile - 1 and tile - 2 may still be in the softmax, tile - 3 not)
+      expand_scales<D>(sm.scales[st], at + kv4_part_bytes(D), w, lane);
+      expand_k<D>(sm, sm.scales[st], at, w, lane);
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(&sm.k_full);
@@ -286,17 +300,18 @@ __device__ __forceinline__ void expand(Smem<D>& sm, const Params& p, int w, int 
 }
 
 // ---- warp 9: MMAs ----------------------------------------------------------------------------------------
-// Tensor memory: S of step i and group g at columns 64 (i % 2) + 32 g, P over the first 16 of them; O of group g at
-// 128 + 64 g.  The scores of a step are formed while the softmax works on the step before.  (MMAs run in the order
+// Tensor memory: S of step i at columns 32 (i % 2), P of group g over 16 g of them; O of group g at 128 + 64 g.  The scores of a step are formed while the softmax works on the step before.  (MMAs run in the order
 // of their issue: P of step i has been read when S of step i + 2 is written.  Each commit takes the issuing
 // thread as long as an MMA, 60 cycles, so there are two per step and every role takes them for what it waits for.)
 template <int D>
 __device__ __forceinline__ void issue_scores(Smem<D>& sm, uint32_t tmem, uint32_t buf, uint32_t sub) {
   constexpr uint32_t idesc = idesc_f16(kRows, kSub, false);
 #pragma unroll
-  for (int g = 0; g < D / kGroup4; ++g)
-    umma_ss_kloop<1>(tmem + 64 * buf + 32 * g, tc_smem_desc(smem_u32(sm.q[g]), 0, 1024),
-                     tc_smem_desc(smem_u32(sm.k[g]), 0, 1024) + sub * (kSub * 128 >> 4), idesc);
+  for (int g = 0; g < D / kGroup4; ++g) {
+    const uint64_t qd = tc_smem_desc(smem_u32(sm.q[g]), 0, 1024), kd = tc_smem_desc(smem_u32(sm.k[g]), 0, 1024) + sub * (kSub * 128 >> 4);
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) umma_ss(tmem + 32 * buf, qd + 2 * ks, kd + 2 * ks, idesc, g + ks > 0 ? 1u : 0u);  // 16 entries each
+  }
   tc_commit(&sm.s_full[buf]);
 }
 template <int D>
@@ -329,7 +344,7 @@ __device__ __forceinline__ void issue_mmas(Smem<D>& sm, const Params& p, int lan
           const uint64_t vd = tc_smem_desc(smem_u32(sm.v[g]), 0, 1024) + (i & 1) * (kSub * 128 >> 4);
 #pragma unroll
           for (int ks = 0; ks < kSub / 16; ++ks)  // 16 token rows = 2048 bytes per MMA
-            umma_ts(tmem + 128 + 64 * g, tmem + 64 * buf + 32 * g + 8 * ks, vd + ks * (2048 >> 4), idesc_o, (i > 0 || ks > 0) ? 1u : 0u);
+            umma_ts(tmem + 128 + 64 * g, tmem + 32 * buf + 16 * g + 8 * ks, vd + ks * (2048 >> 4), idesc_o, (i > 0 || ks > 0) ? 1u : 0u);
         }
         tc_commit(&sm.o_full[buf]);
       }
@@ -355,21 +370,18 @@ __device__ __forceinline__ void softmax(Smem<D>& sm, const Params& p, int warp, 
   for_units(sm, p, lane, [&](int n, const Unit& u) {
     if (!wait(&sm.q_full, n, p)) return false;
     const float scale = sm.row_scale[row];
-    // the row's sums with its scale: x = sum of s (q . c) scale + z (sum of q) scale
-    const float qs0 = sm.row_sum[0][row] * scale, qs1 = NG == 2 ? sm.row_sum[1][row] * scale : 0.f;
     __syncwarp();
     if (lane == 0) mbar_arrive(&sm.q_empty);
-    const uint64_t scale2 = f2_pack(scale, scale), q0 = f2_pack(qs0, qs0), q1 = f2_pack(qs1, qs1);
     float top = -INFINITY;    // the reference's score
     float f[2] = {1.f, 1.f};  // as in decode4.cu
     uint64_t l2 = 0, oz[2] = {0, 0};
     for (int left = u.tok_count, i = 0; left > 0; left -= kSub, ++i, ++step) {
       // this step's tokens: scales as float4 of group g's tokens 4 k .. + 3
-      const Scales &ks = sm.ks[(tile0 + i / 2) % kStages], &vs = sm.vs[(tile0 + i / 2) % kStages];
+      const Scales& vs = sm.scales[(tile0 + i / 2) % kStages];
       const int at = (i & 1) * kSub;
       auto quad = [&](const float (&a)[2][kTile], int g, int k) { return *reinterpret_cast<const float4*>(&a[g][at + 4 * k]); };
       auto half = [](const float4& v, int h) { return h ? f2_pack(v.z, v.w) : f2_pack(v.x, v.y); };
-      const uint32_t cols = lanes + 64 * (step & 1);
+      const uint32_t cols = lanes + 32 * (step & 1);
       if (!wait_step(sm.s_full, step, p)) return false;
       tc_fence_after_sync();
       // the largest s per group (not negative: its bits order as it does)
@@ -379,24 +391,15 @@ __device__ __forceinline__ void softmax(Smem<D>& sm, const Params& p, int warp, 
       // scores of token pairs, in log2 units
       uint64_t x[kSub / 2];
       {
-        uint32_t a0[kSub], a1[kSub];
-        tmem_ld32(cols, a0);
-        if (NG == 2) tmem_ld32(cols + 32, a1);
+        uint32_t a[kSub];
+        tmem_ld32(cols, a);
         tmem_wait_ld();
 #pragma unroll
-        for (int k = 0; k < kSub / 4; ++k) {
-          const float4 s0 = quad(ks.s, 0, k), z0 = quad(ks.z, 0, k);
-          float4 s1, z1;
-          if (NG == 2) { s1 = quad(ks.s, 1, k); z1 = quad(ks.z, 1, k); }
+        for (int b = 0; b < 2; ++b) {
+          const float f = vs.k[at / 16 + b] * scale;
+          const uint64_t f2 = f2_pack(f, f);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int e = 4 * k + 2 * h;
-            uint64_t y = f2_mul(f2_pack(__uint_as_float(a0[e]), __uint_as_float(a0[e + 1])), half(s0, h));
-            if (NG == 2) y = f2_fma(f2_pack(__uint_as_float(a1[e]), __uint_as_float(a1[e + 1])), half(s1, h), y);
-            uint64_t zq = f2_mul(half(z0, h), q0);
-            if (NG == 2) zq = f2_fma(half(z1, h), q1, zq);
-            x[e >> 1] = f2_fma(y, scale2, zq);
-          }
+          for (int k = 8 * b; k < 8 * b + 8; ++k) x[k] = f2_mul(f2_pack(__uint_as_float(a[2 * k]), __uint_as_float(a[2 * k + 1])), f2);
         }
       }
       if (left < kSub) {
@@ -486,7 +489,7 @@ __device__ __forceinline__ void softmax(Smem<D>& sm, const Params& p, int warp, 
           }
         }
 #pragma unroll
-        for (int g = 0; g < NG; ++g) tmem_st8(cols + 32 * g + c0 / 2, pk[g]);
+        for (int g = 0; g < NG; ++g) tmem_st8(cols + 16 * g + c0 / 2, pk[g]);
       }
       tmem_wait_st();
       tc_fence_before_sync();
