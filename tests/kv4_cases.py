@@ -46,3 +46,9 @@ def random_case(hq, hkv, d, requests, lens=ODD_LENS, seed=3, shared=None, **over
             p = [shared] + [v for v in p if v != shared]
         paths.append(p)
     return private_workload(lens, paths, hq, hkv, d, seed=seed, **over)
+
+
+def two_stream_case(hq=32, hkv=8, d=128, layers=1):
+    """Enough of widely shared and of unshared chunks that a call runs its kernels on two streams: 40 requests over one long
+    node, 24 of them over a node of their own as well."""
+    return private_workload([5000] + [300] * 24, [[0] + ([1 + r] if r < 24 else []) for r in range(40)], hq, hkv, d, layers=layers)

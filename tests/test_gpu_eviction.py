@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from helpers import assert_close
-from kv4_cases import ODD_LENS, View, private_workload, random_case
+from kv4_cases import ODD_LENS, View, private_workload, random_case, two_stream_case
 from oracle import attention as OA
 from oracle import eviction as OE
 from oracle import kv4
@@ -34,7 +34,7 @@ def _reference(w, four, layer=0):
     return lse, OE.attention_weights(view.paths(), view.node_kv, view.q(), lse, w.num_kv_heads)
 
 
-def _check_weights(pa, weights, ref, layer=0, factor=1.0, before=0.0):
+def _check_weights(pa, weights, ref, layer=0, factor=1.0, before=0.0, untouched=None):
     w = pa.w
     mine = torch.zeros(weights.shape[2], dtype=torch.bool)
     for v, want in ref.items():
@@ -43,7 +43,7 @@ def _check_weights(pa, weights, ref, layer=0, factor=1.0, before=0.0):
         got = weights[layer, :, slot:slot + n].double().cpu().numpy()
         assert np.all(np.abs(got - (before + factor * want)) <= RTOL * (before + factor * want) + 1e-30), v
     rest = weights[layer][:, ~mine]
-    assert bool((rest == before).all()), "a slot of no token on a path was written"
+    assert bool((rest == (before if untouched is None else untouched)).all()), "a slot of no token on a path was written"
 
 
 @pytest.mark.parametrize("hq,hkv,d", [(4, 4, 64), (2, 1, 64), (16, 2, 64), (3, 3, 128), (4, 2, 128), (32, 8, 128), (8, 1, 128)])
@@ -133,6 +133,57 @@ def test_weights_refusals():
         pa.attention_weights(0, q.float(), lse, weights)
     assert B.gf_node_kv_release(pa.g, int(w.used_nodes()[0]), pa.stream) == B.GF_OK
     assert call() == B.GF_ERR_NOT_BUILT                       # tables are stale
+    pa.close()
+
+
+@pytest.mark.parametrize("four", [[], list(range(25)), [0, 2, 4]])
+def test_weights_on_two_streams_captured_on_another_stream_and_deferred(four):
+    """A batch whose two kernels run beside each other: against fp64, and the same bits from a call on another stream, from
+    replayed graphs and from deferred tables; the slots of tokens that no path has stay as they were."""
+    w = two_stream_case()
+    pa = _handle(w, four, extra_tiles=2)
+    q = pa.make_q(0, "host")
+    lse, ref = _reference(w, four)
+    lse = torch.from_numpy(lse.astype(np.float32)).cuda()
+    weights = pa.new_weights()
+    weights.fill_(-5.0)
+    pa.attention_weights(0, q, lse, weights, accumulate=False)
+    _check_weights(pa, weights, ref, untouched=-5.0)
+    other = torch.full_like(weights, -5.0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        pa.attention_weights(0, q, lse, other, accumulate=False)
+    side.synchronize()
+    assert torch.equal(other, weights)
+    twice = weights.clone()
+    pa.attention_weights(0, q, lse, twice, accumulate=True)
+    graph = torch.cuda.CUDAGraph()
+    sums = weights.clone()
+    with torch.cuda.graph(graph):
+        pa.attention_weights(0, q, lse, sums, accumulate=True)
+    for _ in range(2):
+        sums.copy_(weights)
+        graph.replay()
+        assert torch.equal(sums, twice)
+    pa.build(deferred=True)
+    other.fill_(-5.0)
+    pa.attention_weights(0, q, lse, other, accumulate=False)
+    assert torch.equal(other, weights)
+    assert pa.status() == 0
+    pa.close()
+
+
+def test_weights_of_an_invalid_deferred_batch_change_nothing():
+    from paper_2605_22566_b200 import binding as B
+    w = private_workload([100, 64], [[0], [1]], 4, 2, 64)
+    pa = _handle(w, [0])
+    pa.path_node = torch.tensor([0, 7], dtype=torch.int32, device="cuda")
+    pa.build(deferred=True)
+    weights = torch.full_like(pa.new_weights(), 3.0)
+    pa.attention_weights(0, pa.make_q(0, "host"), torch.zeros(2, 4, device="cuda"), weights)
+    assert pa.status() == B.GF_ERR_INVALID_PATH
+    assert bool((weights == 3.0).all())
     pa.close()
 
 
@@ -234,6 +285,36 @@ def test_evict_twice_into_the_same_node_and_one_source_into_two():
     for layer in range(2):
         for h in range(2):
             assert kept[layer, h].tolist() == OE.kept(again[layer, h].cpu().numpy(), 70, 0, 0)
+    pa.close()
+
+
+@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("keep", [100, 700])
+def test_evict_captured_and_on_another_stream(four, keep):
+    """Into a node that exists: a replayed graph chooses by the weights of the moment, as the plain call does."""
+    w = private_workload([900, keep], [[0], [1]], 2, 2, 128)
+    pa = _handle_unbuilt(w, [0, 1] if four else [])
+    pa.write_nodes("host", only=[0])
+    weights = pa.new_weights()
+    (first,) = pa.evict([(1, 0, keep, 2, 5)], weights)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        (kept,) = pa.evict([(1, 0, keep, 2, 5)], weights)
+    side = torch.cuda.Stream()
+    for seed in (1, 2):
+        pa.node_weights(weights, 0).copy_(torch.rand(1, 2, 900, generator=torch.Generator().manual_seed(seed)))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = kept.clone(), pa.node_weights(weights, 1).clone(), *pa.load_node(1, 0)
+        for h in range(2):
+            assert got[0][0, h].tolist() == OE.kept(pa.node_weights(weights, 0)[0, h].cpu().numpy(), keep, 2, 5)
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            (again,) = pa.evict([(1, 0, keep, 2, 5)], weights)
+            new = again, pa.node_weights(weights, 1), *pa.load_node(1, 0)
+        side.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, new))
+    assert pa.status() == 0
     pa.close()
 
 

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from helpers import assert_close
-from kv4_cases import ODD_LENS, View, private_workload, random_case
+from kv4_cases import ODD_LENS, View, private_workload, random_case, two_stream_case
 from oracle import attention as OA
 from oracle import kv4
 from oracle.residual import bf16_to_f64, f64_to_bf16_rne
@@ -344,6 +344,43 @@ def test_mixed_with_residual_nodes_layers_streams_static_and_capture():
             fourth.zero_()
             graph.replay()
             assert torch.equal(fourth, out)
+    assert pa.status() == 0
+    pa.close()
+
+
+@pytest.mark.parametrize("four", ["all", "some"])
+def test_decode_on_two_streams_captured_on_another_stream_and_twice(four):
+    """A batch whose kernels run beside each other: the plain call against fp64, then the same bits from a call on another
+    stream, from two captured graphs replayed in turn, and from deferred tables (one stream)."""
+    w = two_stream_case(layers=2)
+    nodes = list(range(25)) if four == "all" else [0] + list(range(1, 25, 2))
+    pa = _handle(w, nodes)
+    pa.write_nodes("host")
+    pa.build()
+    q = [pa.make_q(layer, "host") for layer in (0, 1)]
+    out = [pa.decode(layer, q[layer]) for layer in (0, 1)]
+    view = View(w, nodes)
+    ref, _ = OA.decode(view.paths(), view.node_kv, view.q(), 8)
+    assert_close(out[0].double().cpu().numpy(), ref, "out")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = pa.decode(0, q[0], out=torch.zeros_like(out[0]))
+    side.synchronize()
+    assert torch.equal(other, out[0])
+    graphs, outs = [], [torch.zeros_like(out[0]) for _ in (0, 1)]
+    for layer in (0, 1):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            pa.decode(layer, q[layer], out=outs[layer])
+    for _ in range(3):
+        for layer in (0, 1):
+            outs[layer].zero_()
+            graphs[layer].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(outs[layer], out[layer]) for layer in (0, 1))
+    pa.build(deferred=True)
+    assert torch.equal(pa.decode(0, q[0]), out[0])
     assert pa.status() == 0
     pa.close()
 
