@@ -179,10 +179,11 @@ gf_status_t gf_node_extent(const gf_wgraph_t* g, int32_t node, int32_t* n_tokens
  * form a group with two bf16 numbers, lo (its least entry) and s (hi / 16 - lo / 16 in fp32, rounded to bf16); an
  * entry x has the code floor((x - lo) / s) within 0..15 (0 where s is 0) and stands for
  * lo + s (code + 1/2), the middle of its cell, or lo where s is 0.  4.5 bits per entry; a normal group is
- * off by about 0.09 of its standard deviation (root mean square).  Inputs are finite.
+ * off by about 0.09 of its standard deviation (root mean square).  Inputs are finite, and below 2^100 in
+ * magnitude where attention is to read them.
  * Such states live in a pool of their own, and paths name them like any other: one batch may mix both
  * kinds, shared as usual.  gf_path_attention_decode (and _static) computes with the values that the codes
- * stand for, without rounding them to bf16 first.  Extend mode takes no path through such a node
+ * stand for, without rounding them to bf16 first (K of widely shared chunks to fp16).  Extend mode takes no path through such a node
  * (GF_ERR_INVALID_PATH: read it back and write it to a bf16 node for that), and it cannot be the base of a
  * residual or of a reconstruction (GF_ERR_INVALID_ARG). */
 

@@ -3,7 +3,7 @@
 // A unit is a chunk of a 4-bit segment and up to 128 stacked query rows (request x GQA head) of the requests that
 // share it.  The codes are expanded once per unit instead of once per 16 rows (decode4.cu), into shared memory, and
 // S = Q K^T and O += P C run as tcgen05 MMAs with accumulators in tensor memory:
-//   K as the values that the codes stand for, in fp16 times a power of two per 16 tokens, so that a score takes one
+//   K as the values that the codes stand for, in fp16 times a power of two per token, so that a score takes one
 //   multiplication; V as codes, fp16 subnormals c 2^-24 and 16 c 2^-24 (exact), one accumulator per group of 64
 //   entries, because values of different tokens may lie any power of two apart and none may be lost:
 //   O_rG = sum over tokens of  (p_rt s_tG) c_tG  +  sum of  p_rt (lo_tG + s_tG / 2)
@@ -34,7 +34,7 @@ constexpr int kThreads = 384;
 // Registers per thread after the roles' split, of the 80 that two CTAs of 384 threads leave; the shares of the three
 // groups of four warps add up to what the CTA was launched with.
 constexpr int kLaunchRegs = 80, kSoftmaxRegs = 136, kExpandRegs = 56, kControlRegs = 48;
-static_assert(kSoftmaxRegs + kExpandRegs + kControlRegs == 3 * kLaunchRegs, "setmaxnreg draws on the launch's registers");
+static_assert(kSoftmaxRegs + kExpandRegs + kControlRegs == 3 * kLaunchRegs, "setmaxnreg draws on the launch's registers");  // (see the launch)
 constexpr int kRows = 128;
 constexpr int kUnits = 4, kStages = 3;
 constexpr int kSub = 32;  // tokens per step of the softmax: half a tile
@@ -63,8 +63,8 @@ struct __align__(16) Unit {
   int32_t grp_begin, part_base, kvh, tok_count, ntile, pad0, pad1;
 };
 
-// s and z = lo + s / 2 of a tile's V, [group][token], and the powers of two that K's blocks of 16 tokens were divided by.
-struct Scales { float s[2][kTile], z[2][kTile], k[kTile / 16]; };
+// s and z = lo + s / 2 of a tile's V, [group][token], and what undoes the powers of two that K's tokens were multiplied by.
+struct Scales { float s[2][kTile], z[2][kTile], k[kTile]; };
 
 template <int D>
 struct Smem {
@@ -183,14 +183,14 @@ __device__ __forceinline__ void load_queries(Smem<D>& sm, const Params& p, const
   }
 }
 
-// Block b (16 tokens) of a tile's K: the values that the codes stand for, times a power of two that brings the block's
-// largest to 2^14..2^15, rounded to fp16 (2^-11 of a value; a score is wrong by 2^-11 of the sum of its terms at most,
-// where bf16 keys would be by 2^-8).  1024 + c and 1024 + 16 c are fp16 patterns with the code in their low bits.
+// Block b (16 tokens) of a tile's K: the values that the codes stand for, times a power of two that brings the token's
+// largest to 2^14..2^15, rounded to fp16 (2^-11 of a value, or 2^-39 of the token's largest; a score is wrong by 2^-11 of
+// the sum of its terms' sizes at most, where bf16 keys would be by 2^-8).  1024 + c and 1024 + 16 c are fp16 patterns with the code in their low bits.
 template <int D>
 __device__ __forceinline__ void expand_k(Smem<D>& sm, Scales& to, const char* part, int b, int lane) {
   constexpr int NG = D / kGroup4;
   const int l4 = lane & 3, l8 = lane >> 2;
-  // the block's numbers, a token per lane (twice)
+  // a token's numbers per lane (twice)
   uint32_t sl[NG], sz[NG];
   float big = 0.f;
 #pragma unroll
@@ -199,13 +199,13 @@ __device__ __forceinline__ void expand_k(Smem<D>& sm, Scales& to, const char* pa
     const float s = kv4_s(sl[g]), lo = kv4_lo(sl[g]);
     big = fmax3(big, fabsf(lo), fabsf(fmaf(16.f, s, lo)));
   }
-  const float mul = pow2_to(__uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(big))), 14);
+  const float mul = pow2_to(big, 14);
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
     const float s = kv4_s(sl[g]);
     sz[g] = pack_f16(s * mul, fmaf(0.5f, s, kv4_lo(sl[g])) * mul);
   }
-  if (lane == 0) to.k[b] = pow2_inverse(mul);
+  if (lane < 16) to.k[b * 16 + lane] = pow2_inverse(mul);
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
     const uint4 c = reinterpret_cast<const uint4*>(part)[(b * NG + g) * 32 + lane];
@@ -372,7 +372,7 @@ __device__ __forceinline__ void softmax(Smem<D>& sm, const Params& p, int warp, 
     const float scale = sm.row_scale[row];
     __syncwarp();
     if (lane == 0) mbar_arrive(&sm.q_empty);
-    float top = -INFINITY;    // the reference's score
+    float top = -INFINITY;    // the reference's score, in log2 units
     float f[2] = {1.f, 1.f};  // as in decode4.cu
     uint64_t l2 = 0, oz[2] = {0, 0};
     for (int left = u.tok_count, i = 0; left > 0; left -= kSub, ++i, ++step) {
@@ -388,18 +388,18 @@ __device__ __forceinline__ void softmax(Smem<D>& sm, const Params& p, int warp, 
       float big_s[2];
 #pragma unroll
       for (int g = 0; g < NG; ++g) big_s[g] = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(vs.s[g][at + lane])));
-      // scores of token pairs, in log2 units
+      // scores of token pairs, in units of 1 / scale
       uint64_t x[kSub / 2];
       {
         uint32_t a[kSub];
         tmem_ld32(cols, a);
         tmem_wait_ld();
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const float f = vs.k[at / 16 + b] * scale;
-          const uint64_t f2 = f2_pack(f, f);
+        for (int k = 0; k < kSub / 4; ++k) {
+          const float4 f = *reinterpret_cast<const float4*>(&vs.k[at + 4 * k]);
 #pragma unroll
-          for (int k = 8 * b; k < 8 * b + 8; ++k) x[k] = f2_mul(f2_pack(__uint_as_float(a[2 * k]), __uint_as_float(a[2 * k + 1])), f2);
+          for (int h = 0; h < 2; ++h)
+            x[2 * k + h] = f2_mul(f2_pack(__uint_as_float(a[4 * k + 2 * h]), __uint_as_float(a[4 * k + 2 * h + 1])), half(f, h));
         }
       }
       if (left < kSub) {
@@ -419,7 +419,7 @@ __device__ __forceinline__ void softmax(Smem<D>& sm, const Params& p, int warp, 
         f2_unpack(x[k + 1], lo, hi);
         m1 = fmax3(m1, lo, hi);
       }
-      m = fmaxf(m, m1);
+      m = fmaxf(m, m1) * scale;
       bool move = m > top + 8.f;
 #pragma unroll
       for (int g = 0; g < NG; ++g) move |= big_s[g] * f[g] > 128.f;
@@ -435,8 +435,8 @@ __device__ __forceinline__ void softmax(Smem<D>& sm, const Params& p, int warp, 
         for (int k = 0; k < kSub / 2; ++k) {
           float lo, hi;
           f2_unpack(x[k], lo, hi);
-          lo = fast_exp2(lo - top);
-          hi = fast_exp2(hi - top);
+          lo = fast_exp2(fmaf(lo, scale, -top));
+          hi = fast_exp2(fmaf(hi, scale, -top));
 #pragma unroll
           for (int g = 0; g < NG; ++g) {
             const float2 s2 = *reinterpret_cast<const float2*>(&vs.s[g][at + 2 * k]);
@@ -462,7 +462,7 @@ __device__ __forceinline__ void softmax(Smem<D>& sm, const Params& p, int warp, 
         }
       }
       // p, l, the second term of O, and p s f over the scores
-      const uint64_t ref2 = f2_pack(-top, -top), f0 = f2_pack(f[0], f[0]), f1 = f2_pack(f[1], f[1]);
+      const uint64_t scale2 = f2_pack(scale, scale), ref2 = f2_pack(-top, -top), f0 = f2_pack(f[0], f[0]), f1 = f2_pack(f[1], f[1]);
 #pragma unroll
       for (int c0 = 0; c0 < kSub; c0 += 16) {
         uint32_t pk[2][8];
@@ -475,7 +475,7 @@ __device__ __forceinline__ void softmax(Smem<D>& sm, const Params& p, int warp, 
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             float lo, hi;
-            f2_unpack(f2_add(x[(c0 + 4 * k + 2 * h) >> 1], ref2), lo, hi);
+            f2_unpack(f2_fma(x[(c0 + 4 * k + 2 * h) >> 1], scale2, ref2), lo, hi);
             const uint64_t pr = f2_pack(fast_exp2(lo), fast_exp2(hi));
             l2 = f2_add(l2, pr);
             oz[0] = f2_fma(pr, half(z0, h), oz[0]);
@@ -612,6 +612,13 @@ int launch_decode4_wide(const PoolGeom& pool, const AttnShape& sh, const TablesD
   const long long work = units < 0 ? (1ll << 40) : (long long)units * sh.num_kv_heads, most = 2ll * t.num_sms;
   const dim3 grid((unsigned)(work < most ? work : most));
   auto go = [&](auto kernel, size_t smem, bool (&optin)[kMaxDevices]) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return false;
+    if (dev >= kMaxDevices || !optin[dev]) {
+      // (a build that gives the kernel fewer registers would leave the split below waiting for them)
+      cudaFuncAttributes attr;
+      if (cudaFuncGetAttributes(&attr, kernel) != cudaSuccess || attr.numRegs != kLaunchRegs) return false;
+    }
     if (!ensure_dynamic_smem(kernel, smem, optin)) return false;
     if (chained) launch_chained(kernel, grid, dim3(kThreads), smem, st, p);
     else kernel<<<grid, dim3(kThreads), smem, st>>>(p);  // behind an event of another stream

@@ -76,7 +76,6 @@ class PathAttention:
             nbytes = max(kv4_tiles, 1) * B.gf_kv4_bytes_per_tile(w.head_dim) * w.num_kv_heads * self.layers
             self.pool4 = self.guarded(nbytes, "4-bit kv pool", align=1024)
             B.check(B.gf_kv4_pool_attach(self.g, self.pool4.data_ptr(), nbytes), "gf_kv4_pool_attach")
-        self.weight_slots = B.gf_weight_slots(self.g)
         self.path_ptr = torch.from_numpy(w.path_ptr.astype(np.int32)).to(self.dev)
         self.path_node = torch.from_numpy(w.path_node.astype(np.int32)).to(self.dev)
         self.tables = None
@@ -272,7 +271,7 @@ class PathAttention:
     # ---- eviction by accumulated attention weight --------------------------------------------
     def new_weights(self) -> torch.Tensor:
         """Zeroed weights for every token slot of both pools: fp32 [layers, Hkv, slots]."""
-        shape = (self.layers, self.w.num_kv_heads, self.weight_slots)
+        shape = (self.layers, self.w.num_kv_heads, B.gf_weight_slots(self.g))
         buf = self.guarded(4 * shape[0] * shape[1] * shape[2], "attention weights").view(torch.float32).view(shape)
         return buf.zero_()
 
@@ -289,7 +288,7 @@ class PathAttention:
         return weights.narrow(2, slot, n)
 
     def _check_weights(self, weights: torch.Tensor) -> None:
-        shape = (self.layers, self.w.num_kv_heads, self.weight_slots)
+        shape = (self.layers, self.w.num_kv_heads, B.gf_weight_slots(self.g))
         if weights.dtype != torch.float32 or weights.device != self.pool.device or not weights.is_contiguous() or \
                 weights.shape != shape:
             raise ValueError(f"weights: a contiguous fp32 tensor {list(shape)} on {self.pool.device}")

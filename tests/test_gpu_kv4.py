@@ -295,6 +295,28 @@ def test_decode_scales_far_apart(requests, hkv, copies):
     pa.close()
 
 
+@pytest.mark.parametrize("requests,hkv,copies", [(1, 1, 1), (24, 1, 1), (24, 8, 40)])
+def test_decode_an_outlying_key_that_carries_nothing(requests, hkv, copies):
+    """One token's key is 2^30 times the others' and points away from every query: its weight is 0, and the tokens beside it
+    in its block and its tile keep theirs."""
+    d, n, gqa = 128, 150, 8
+    rng = np.random.default_rng(17)
+    k, v, q = rng.standard_normal((n, 1, d)), rng.standard_normal((n, 1, d)) / 4, np.abs(rng.standard_normal((requests, gqa, d)))
+    k[[7, 100]] = -(2.0 ** 30) * (1 + np.abs(k[[7, 100]]))
+    k, v, q = (_bf16(np.repeat(x, hkv, 1)) for x in (k, v, q))
+    path = list(range(copies))
+    pa = _handle(private_workload([n] * copies, [path] * requests, gqa * hkv, hkv, d), path)
+    for node in path:
+        pa.write_node(node, 0, _tensor(k), _tensor(v))
+    pa.build()
+    out = pa.decode(0, _tensor(q)).double().cpu().numpy()
+    kv = kv4.values(k), kv4.values(v)
+    ref, _ = OA.decode([path] * requests, lambda _: kv, q, hkv)
+    assert pa.status() == 0
+    assert_close(out, ref, "out")
+    pa.close()
+
+
 def test_constant_values_and_equal_keys():
     """Equal keys give the mean of V; constant V comes back exactly (its groups are held exactly)."""
     d, n = 64, 77
