@@ -2,8 +2,8 @@
 // codes stand for (k_kv4_read).  Format and layout: kv4_device.cuh.
 //
 // Both are streams: 2 bytes of bf16 per entry on one side, 0.5625 on the other, nothing reused.  32 768 tokens of 8 heads
-// of 128, 172 MB either way: read in 28.6 us (6.0 TB/s, bound by HBM), written in 48 us (3.6 TB/s, bound by the
-// instructions of the exact quotients, 16 per entry; 113 us with divisions).  A short node costs its launch.  A warp works on one block of 16 tokens of one KV
+// of 128, 172 MB either way: read in 28.6 us (6.0 TB/s, bound by HBM), written in 46 us (3.7 TB/s, bound by the
+// instructions of the exact quotients, some 14 per entry; 113 us with divisions).  A short node costs its launch.  A warp works on one block of 16 tokens of one KV
 // head and one group of 64 entries, K or V: 2 KB of bf16, 512 bytes of codes.  The layout gives every lane
 // 16-byte runs on both sides, so nothing goes through shared memory; a token's least and largest entry are
 // found with shuffles among the lanes that hold it.
@@ -26,9 +26,12 @@ __device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b) {
   return r;
 }
 
-// The lesser and the greater number of a pair.
-__device__ __forceinline__ float low_of(uint32_t p) { return fminf(__uint_as_float(p << 16), __uint_as_float(p & 0xffff0000u)); }
-__device__ __forceinline__ float high_of(uint32_t p) { return fmaxf(__uint_as_float(p << 16), __uint_as_float(p & 0xffff0000u)); }
+// The least entry and, negated, the greatest of two pairs that hold the least and the greatest of a run: one pair of
+// bf16, so that one minimum (and one shuffle) serves both from here on.
+__device__ __forceinline__ uint32_t ends_of(uint32_t lo2, uint32_t hi2) {
+  hi2 ^= 0x80008000u;
+  return min_pair(__byte_perm(lo2, hi2, 0x5410), __byte_perm(lo2, hi2, 0x7632));
+}
 
 // A group's numbers as the coding of its entries takes them.  Everything is scaled by 1/16, which is exact and keeps
 // hi - lo from overflowing.
@@ -36,15 +39,21 @@ struct GroupCoder {
   uint32_t word;   // (s, lo) as stored
   float lo16, cell;  // -lo / 16, s / 16
   float inv;       // a little more than 16 / s; 0 where s is 0
-  __device__ __forceinline__ GroupCoder(float lo, float hi) {
+  __device__ __forceinline__ explicit GroupCoder(uint32_t ends) {  // see ends_of
+    const float lo = __uint_as_float(ends << 16), hi = -__uint_as_float(ends & 0xffff0000u);
     const __nv_bfloat16 s = __float2bfloat16_rn(__fsub_rn(hi * 0.0625f, lo * 0.0625f));
     word = (uint32_t)__bfloat16_as_ushort(s) | (__float_as_uint(lo) & 0xffff0000u);
     lo16 = lo * -0.0625f;
     cell = __bfloat162float(s) * 0.0625f;
-    inv = cell > 0.f ? __fmul_ru(__frcp_ru(cell), 1.0000003f) : 0.f;
+    if (cell >= 0x1p-100f) {
+      asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(cell));  // within 2^-23, the factor is 1 + 2^-21
+      inv = __fmul_ru(inv, 1.0000005f);
+    } else {
+      inv = cell > 0.f ? __fmul_ru(__frcp_ru(cell), 1.0000005f) : 0.f;
+    }
   }
   // The codes of N bf16 pairs, floor((x - lo) / s) within 0..15, one in each half of out[i].  The quotient from the
-  // reciprocal is never below the true one and less than 2^-20 of it above, so its whole part is the code or,
+  // reciprocal is never below the true one and less than 2^-19 of it above, so its whole part is the code or,
   // where a whole number lies between the two, one more: then the remainder (exact: an FMA on a small
   // whole number and two short numbers) is negative.  That is rare, and put right behind a vote.
   template <int N>
@@ -129,12 +138,10 @@ __global__ void __launch_bounds__(kThreads) k_kv4_write(char* __restrict__ layer
         uint32_t lo2 = x[0], hi2 = x[0];
 #pragma unroll
         for (int i = 1; i < 8; ++i) { lo2 = min_pair(lo2, x[i]); hi2 = max_pair(hi2, x[i]); }
+        uint32_t ends = ends_of(lo2, hi2);
 #pragma unroll
-        for (int d = 1; d < 4; d <<= 1) {
-          lo2 = min_pair(lo2, __shfl_xor_sync(0xffffffffu, lo2, d));
-          hi2 = max_pair(hi2, __shfl_xor_sync(0xffffffffu, hi2, d));
-        }
-        const GroupCoder coder(low_of(lo2), high_of(hi2));
+        for (int d = 1; d < 4; d <<= 1) ends = min_pair(ends, __shfl_xor_sync(0xffffffffu, ends, d));
+        const GroupCoder coder(ends);
         uint32_t c[8];
         coder.codes(x, c);
 #pragma unroll
@@ -157,12 +164,10 @@ __global__ void __launch_bounds__(kThreads) k_kv4_write(char* __restrict__ layer
         uint32_t lo2 = x[0], hi2 = x[0];
 #pragma unroll
         for (int i = 1; i < 4; ++i) { lo2 = min_pair(lo2, x[i]); hi2 = max_pair(hi2, x[i]); }
+        uint32_t ends = ends_of(lo2, hi2);
 #pragma unroll
-        for (int d = 4; d < 32; d <<= 1) {
-          lo2 = min_pair(lo2, __shfl_xor_sync(0xffffffffu, lo2, d));
-          hi2 = max_pair(hi2, __shfl_xor_sync(0xffffffffu, hi2, d));
-        }
-        const GroupCoder coder(low_of(lo2), high_of(hi2));
+        for (int d = 4; d < 32; d <<= 1) ends = min_pair(ends, __shfl_xor_sync(0xffffffffu, ends, d));
+        const GroupCoder coder(ends);
         uint32_t c[4];
         coder.codes(x, c);
 #pragma unroll

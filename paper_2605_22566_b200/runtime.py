@@ -181,10 +181,11 @@ class PathAttention:
         return both.unbind(0)
 
     def _check_kv(self, k: torch.Tensor, v: torch.Tensor) -> None:
-        for name, t in (("k", k), ("v", v)):
-            if t.dtype != torch.bfloat16 or t.device != self.pool.device or not t.is_contiguous() or t.dim() != 3 or \
-                    t.shape[1:] != (self.w.num_kv_heads, self.w.head_dim) or t.shape[0] != k.shape[0]:
-                raise ValueError(f"{name}: a contiguous bf16 tensor [tokens, {self.w.num_kv_heads}, {self.w.head_dim}] on {self.pool.device}")
+        row = (self.w.num_kv_heads, self.w.head_dim)
+        if k.dtype is v.dtype is torch.bfloat16 and k.shape == v.shape and k.dim() == 3 and k.shape[1:] == row and k.is_contiguous() and \
+                v.is_contiguous() and k.get_device() == v.get_device() == self.pool.get_device():
+            return
+        raise ValueError(f"k, v: two contiguous bf16 tensors [tokens, {row[0]}, {row[1]}] on {self.pool.device}")
 
     def new_nodes(self):
         """The last node of every path: in an extend batch, the request's new segment."""
