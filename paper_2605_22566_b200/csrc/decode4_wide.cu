@@ -3,9 +3,10 @@
 // A unit is a chunk of a 4-bit segment and up to 128 stacked query rows (request x GQA head) of the requests that
 // share it.  The codes are expanded once per unit instead of once per 16 rows (decode4.cu), into shared memory, and
 // S = Q K^T and O += P C run as tcgen05 MMAs with accumulators in tensor memory:
-//   K as the values that the codes stand for, in fp16 times a power of two per token, so that a score takes one
-//   multiplication; V as codes, fp16 subnormals c 2^-24 and 16 c 2^-24 (exact), one accumulator per group of 64
-//   entries, because values of different tokens may lie any power of two apart and none may be lost:
+//   S_rt = sum over groups G of  q_rG . (s_tG (c_tG - 8))  +  (sum of q_rG) (lo_tG + 8.5 s_tG)
+// K's scales are part of the operand, exact in fp16 (the second term takes a few entries more, see sums_offset), so that a
+// score costs its thread one multiplication.  V's operand are the codes, fp16 subnormals c 2^-24 and 16 c 2^-24 (exact), with
+// one accumulator per group of 64 entries, because values of different tokens may lie any power of two apart:
 //   O_rG = sum over tokens of  (p_rt s_tG) c_tG  +  sum of  p_rt (lo_tG + s_tG / 2)
 // A thread owns a query row: it takes the 32 scores of a step from tensor memory, exponentiates, applies the
 // tokens' scales (tables in shared memory, read as broadcasts), keeps l and the second term of O in fp32, and puts
@@ -21,8 +22,8 @@
 //
 // 1024 requests, 608 units of mostly 128 rows, 8776 tiles of 64 tokens: 119 us (the 16-row kernel takes 170 for the
 // same).  Bound by the latency of one softmax warp per scheduler and CTA, two CTAs being what tensor memory holds, and by
-// shared memory: the scales' broadcasts cost 512 of a step's 1800 cycles, the MMAs' operands 400.  Measured before:
-// K as codes with its scales applied to the scores, twice the broadcasts, 139 us; steps of a whole tile with one S, 155:
+// shared memory: the scales' broadcasts cost 600 of a step's 1800 cycles, the MMAs' operands 400.  Measured before:
+// K as codes with its scales applied to the scores, many more broadcasts, 139 us; steps of a whole tile with one S, 155:
 // an MMA or a commit costs its issuing thread 60 cycles, and there they stood between two softmaxes.
 #include "kv4_device.cuh"
 #include "tc_device.cuh"
@@ -33,7 +34,7 @@ namespace {
 constexpr int kThreads = 384;
 // Registers per thread after the roles' split, of the 80 that two CTAs of 384 threads leave; the shares of the three
 // groups of four warps add up to what the CTA was launched with.
-constexpr int kLaunchRegs = 80, kSoftmaxRegs = 136, kExpandRegs = 56, kControlRegs = 48;
+constexpr int kLaunchRegs = 80, kSoftmaxRegs = 120, kExpandRegs = 72, kControlRegs = 48;
 static_assert(kSoftmaxRegs + kExpandRegs + kControlRegs == 3 * kLaunchRegs, "setmaxnreg draws on the launch's registers");  // (see the launch)
 constexpr int kRows = 128;
 constexpr int kUnits = 4, kStages = 3;
@@ -72,6 +73,8 @@ struct Smem {
   unsigned char q[CB][kRows * 128];       // fp16, 128-byte-swizzled rows of 64 entries
   unsigned char k[CB][kTile * 128];       // codes of a tile, K-major
   unsigned char v[CB][kTile * 128];       // and MN-major: both are rows of a token's 64 entries
+  unsigned char q_sum[kRows * 32];        // 16 more entries of K's and Q's rows, for the term without codes (see sums_offset)
+  unsigned char k_mid[kTile * 32];
   unsigned char stage[kStages][kv4_tile_bytes(D)];
   Scales scales[kStages];                 // of tile n at n % kStages
   float row_scale[kRows];                 // softmax scale over the row's power of two
@@ -87,6 +90,19 @@ constexpr int kUnitReaders = 4 + 4 + 1;
 __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t phase, const Params& p) { return mbar_wait(bar, phase & 1, p.status); }
 // A pair of barriers that steps use in turn.
 __device__ __forceinline__ bool wait_step(uint64_t (&bar)[2], int step, const Params& p) { return wait(&bar[step & 1], (uint32_t)step >> 1, p); }
+// The term without codes, (sum of q_rG) (lo_tG + 8.5 s_tG), as more entries of the same product: two fp16 numbers hold 22
+// bits of either factor, so a group takes four entries, (qh, qh, ql, ql) times (zh, zl, zh, zl).  Rows of 16 entries
+// without a swizzle: eight rows of 16 bytes, twice, per 256 bytes; entries 8..15 stay zero.
+__device__ __forceinline__ uint32_t sums_offset(uint32_t row, uint32_t group) { return (row >> 3) * 256 + (row & 7) * 16 + group * 8; }
+__device__ __forceinline__ uint64_t sums_desc(uint32_t saddr) {  // lbo: 128 bytes to the next 8 entries, sbo: 256 to the next 8 rows
+  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(128 >> 4) << 16) | ((uint64_t)(256 >> 4) << 32) | ((uint64_t)1 << 46);
+}
+// x as the sum of two fp16 numbers.
+__device__ __forceinline__ void split_f16(float x, __half& hi, __half& lo) {
+  hi = __float2half_rn(x);
+  lo = __float2half_rn(x - __half2float(hi));
+}
+__device__ __forceinline__ uint32_t pair_of(__half a, __half b) { return (uint32_t)__half_as_ushort(a) | (uint32_t)__half_as_ushort(b) << 16; }
 // Instruction descriptor: D fp32, A and B fp16.
 __host__ __device__ constexpr uint32_t idesc_f16(int M, int N, bool b_mn_major) {
   return (1u << 4) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
@@ -175,55 +191,71 @@ __device__ __forceinline__ void load_queries(Smem<D>& sm, const Params& p, const
       for (int d = 1; d < kLanes; d <<= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, d));
       const float mul = pow2_to(big, 14);
       uint32_t h[4];
+      float sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) h[i] = pack_f16(__uint_as_float(w[i] << 16) * mul, __uint_as_float(w[i] & 0xffff0000u) * mul);
+      for (int i = 0; i < 4; ++i) {
+        h[i] = pack_f16(__uint_as_float(w[i] << 16) * mul, __uint_as_float(w[i] & 0xffff0000u) * mul);
+        const float2 r = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+        sum += r.x + r.y;
+      }
+#pragma unroll
+      for (int d = 1; d < 8; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+      if (chunk % 8 == 0) {
+        __half hi, lo;
+        split_f16(sum * 0x1p-6f, hi, lo);  // up to 2^15; the other factor has the 2^6
+        *reinterpret_cast<uint2*>(sm.q_sum + sums_offset(row, chunk / 8)) = make_uint2(pair_of(hi, hi), pair_of(lo, lo));
+      }
       *reinterpret_cast<uint4*>(sm.q[chunk / 8] + swz128(row, chunk % 8)) = make_uint4(h[0], h[1], h[2], h[3]);
       if (chunk == 0) sm.row_scale[row] = p.scale_log2 * pow2_inverse(mul);
     }
   }
 }
 
-// Block b (16 tokens) of a tile's K: the values that the codes stand for, times a power of two that brings the token's
-// largest to 2^14..2^15, rounded to fp16 (2^-11 of a value, or 2^-39 of the token's largest; a score is wrong by 2^-11 of
-// the sum of its terms' sizes at most, where bf16 keys would be by 2^-8).  1024 + c and 1024 + 16 c are fp16 patterns with the code in their low bits.
+// Block b (16 tokens) of a tile's K: s (c - 8), which eleven bits hold (eight of s, three of c - 8), times a power of two
+// that brings the token's largest value to 2^8..2^9; and lo + 8.5 s beside it.  1024 + c and 1024 + 16 c are fp16 patterns with
+// the code in their low bits.
 template <int D>
 __device__ __forceinline__ void expand_k(Smem<D>& sm, Scales& to, const char* part, int b, int lane) {
   constexpr int NG = D / kGroup4;
-  const int l4 = lane & 3, l8 = lane >> 2;
+  const int l4 = lane & 3, l8 = lane >> 2, own = b * 16 + (lane & 15);
   // a token's numbers per lane (twice)
-  uint32_t sl[NG], sz[NG];
-  float big = 0.f;
+  float s[NG], lo[NG], big = 0.f;
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
-    sl[g] = reinterpret_cast<const uint32_t*>(part + kv4_code_bytes(D))[(b * 16 + (lane & 15)) * NG + g];
-    const float s = kv4_s(sl[g]), lo = kv4_lo(sl[g]);
-    big = fmax3(big, fabsf(lo), fabsf(fmaf(16.f, s, lo)));
+    const uint32_t sl = reinterpret_cast<const uint32_t*>(part + kv4_code_bytes(D))[own * NG + g];
+    s[g] = kv4_s(sl);
+    lo[g] = kv4_lo(sl);
+    big = fmax3(big, fabsf(lo[g]), fabsf(fmaf(16.f, s[g], lo[g])));
   }
-  const float mul = pow2_to(big, 14);
+  const float mul = pow2_to(big, 8);
+  uint32_t step[NG];
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
-    const float s = kv4_s(sl[g]);
-    sz[g] = pack_f16(s * mul, fmaf(0.5f, s, kv4_lo(sl[g])) * mul);
+    step[g] = pack_f16(s[g] * mul, s[g] * mul);
+    if (lane < 16) {
+      __half hi, rest;
+      split_f16(fmaf(8.5f, s[g], lo[g]) * (mul * 64.f), hi, rest);
+      const uint32_t z = pair_of(hi, rest);
+      *reinterpret_cast<uint2*>(sm.k_mid + sums_offset(own, g)) = make_uint2(z, z);
+    }
   }
-  if (lane < 16) to.k[b * 16 + lane] = pow2_inverse(mul);
+  if (lane < 16) to.k[own] = pow2_inverse(mul);
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
     const uint4 c = reinterpret_cast<const uint4*>(part)[(b * NG + g) * 32 + lane];
     const uint32_t w[4] = {c.x, c.y, c.z, c.w};
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const uint32_t mask = h ? 0x00f000f0u : 0x000f000fu, row = b * 16 + l8 + 8 * h, token = __shfl_sync(0xffffffffu, sz[g], l8 + 8 * h);
-      const uint32_t s2 = __byte_perm(token, 0u, 0x1010u), z2 = __byte_perm(token, 0u, 0x3232u);
-      __half2 step = *reinterpret_cast<const __half2*>(&s2);
-      if (h) step = __hmul2(step, __float2half2_rn(0.0625f));
-      const __half2 least = *reinterpret_cast<const __half2*>(&z2), bias = __float2half2_rn(-1024.f);
+      const uint32_t mask = h ? 0x00f000f0u : 0x000f000fu, row = b * 16 + l8 + 8 * h, token = __shfl_sync(0xffffffffu, step[g], l8 + 8 * h);
+      const __half2 by = *reinterpret_cast<const __half2*>(&token);
       uint32_t x[8];
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const uint32_t code = ((e ? w[kk] >> 8 : w[kk]) & mask) | 0x64006400u;
-          const __half2 v = __hfma2(__hadd2(*reinterpret_cast<const __half2*>(&code), bias), step, least);
+          const __half2 c2 = *reinterpret_cast<const __half2*>(&code);
+          const __half2 v = __hmul2(h ? __hfma2(c2, __float2half2_rn(0.0625f), __float2half2_rn(-72.f)) : __hadd2(c2, __float2half2_rn(-1032.f)), by);
           x[2 * kk + e] = *reinterpret_cast<const uint32_t*>(&v);
         }
       *reinterpret_cast<uint4*>(sm.k[g] + swz128(row, l4)) = make_uint4(x[0], x[1], x[2], x[3]);
@@ -312,6 +344,7 @@ __device__ __forceinline__ void issue_scores(Smem<D>& sm, uint32_t tmem, uint32_
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) umma_ss(tmem + 32 * buf, qd + 2 * ks, kd + 2 * ks, idesc, g + ks > 0 ? 1u : 0u);  // 16 entries each
   }
+  umma_ss(tmem + 32 * buf, sums_desc(smem_u32(sm.q_sum)), sums_desc(smem_u32(sm.k_mid) + sub * (kSub * 32)), idesc, 1u);
   tc_commit(&sm.s_full[buf]);
 }
 template <int D>
@@ -553,6 +586,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_decode4_wide(const Params p) {
   chain_enter();
   const int num_units = tables_usable(*p.hdr, p.slot_cap) ? p.hdr->kv4_wide * p.num_kv_heads : 0;
   if (num_units > 0) {  // uniform over the launch
+    for (int i = threadIdx.x; i < (int)sizeof(sm.q_sum) / 16; i += kThreads) reinterpret_cast<uint4*>(sm.q_sum)[i] = make_uint4(0u, 0u, 0u, 0u);
+    for (int i = threadIdx.x; i < (int)sizeof(sm.k_mid) / 16; i += kThreads) reinterpret_cast<uint4*>(sm.k_mid)[i] = make_uint4(0u, 0u, 0u, 0u);
+    fence_proxy_async_smem();
     if (warp == 9) tmem_alloc(&sm.tmem_base, 256);
     tc_fence_before_sync();
     __syncthreads();

@@ -261,6 +261,18 @@ def test_decode_many_widely_shared_chunks(hq, hkv, d, requests, chunk, four):
     _decode(w, range(5) if four == "all" else [0, 3, 4], policy=(chunk, 8, 16, 1), deferred=four == "some")
 
 
+@pytest.mark.parametrize("hq,hkv,d,requests,chunk", [(32, 8, 128, 32, 192), (8, 8, 64, 200, 64), (32, 8, 128, 3, 256)])
+def test_decode_lse_is_exact_to_fp32(hq, hkv, d, requests, chunk):
+    """Scores are sums of exact products in fp32.  A score is off by at most (D + 8) 2^-24 of the sum of its products' sizes,
+    and by 2^-21 of (sum of q) (lo + 8.5 s), which two fp16 numbers each stand for: with q and k of unit spread 136 * 2^-24 *
+    82 * 0.088 + 2^-21 * 4 * 20 * 0.088 = 6e-5, here with a factor of two for larger rows; lse is off by no more."""
+    w = random_case(hq, hkv, d, requests, lens=[40 * chunk - 31, 40, 65, 3 * chunk - 1, 1], shared=0)
+    _, lse = _decode(w, range(5), policy=(chunk, 8, 16, 1))
+    view = View(w, range(5))
+    _, ref = OA.decode(view.paths(), view.node_kv, view.q(), hkv)
+    assert np.abs(lse - ref).max() <= 1.2e-4
+
+
 @pytest.mark.parametrize("requests,hkv,copies", [(1, 1, 1), (2, 1, 1), (24, 1, 1), (24, 8, 40)])
 def test_decode_scales_far_apart(requests, hkv, copies):
     """Every query row has one token with nearly all of its weight, and values and groups lie up to 2^180 apart: the output
