@@ -183,7 +183,7 @@ gf_status_t gf_node_extent(const gf_wgraph_t* g, int32_t node, int32_t* n_tokens
  * magnitude where attention is to read them.
  * Such states live in a pool of their own, and paths name them like any other: one batch may mix both
  * kinds, shared as usual.  gf_path_attention_decode (and _static) computes with the values that the codes
- * stand for, without rounding them to bf16 first (K of widely shared chunks to fp16).  Extend mode takes no path through such a node
+ * stand for, without rounding them to bf16 first.  Extend mode takes no path through such a node
  * (GF_ERR_INVALID_PATH: read it back and write it to a bf16 node for that), and it cannot be the base of a
  * residual or of a reconstruction (GF_ERR_INVALID_ARG). */
 

@@ -20,11 +20,12 @@
 //   warp 9     one thread issues the MMAs  (warps 10 and 11 only complete the group whose registers are handed over)
 // Every wait is bounded; a warp whose wait gave up leaves its role, and so do the others.
 //
-// 1024 requests, 608 units of mostly 128 rows, 8776 tiles of 64 tokens: 119 us (the 16-row kernel takes 170 for the
+// 1024 requests, 608 units of mostly 128 rows, 8776 tiles of 64 tokens: 132 us (the 16-row kernel takes 170 for the
 // same).  Bound by the latency of one softmax warp per scheduler and CTA, two CTAs being what tensor memory holds, and by
-// shared memory: the scales' broadcasts cost 600 of a step's 1800 cycles, the MMAs' operands 400.  Measured before:
-// K as codes with its scales applied to the scores, many more broadcasts, 139 us; steps of a whole tile with one S, 155:
-// an MMA or a commit costs its issuing thread 60 cycles, and there they stood between two softmaxes.
+// shared memory: the scales' broadcasts, four wavefronts for 16 bytes, cost 600 of a step's 2000 cycles, the MMAs'
+// operands 400.  Measured before: K as codes, its scales applied to the scores, 139 us; K as values rounded to fp16, 119,
+// but lse in fp32 lost bits to it; steps of a whole tile with one S, 155: an MMA or a commit costs its issuing thread
+// 60 cycles, and there they stood between two softmaxes.
 #include "kv4_device.cuh"
 #include "tc_device.cuh"
 

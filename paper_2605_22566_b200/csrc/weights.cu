@@ -400,7 +400,7 @@ struct Smem {
   uint64_t k_full[kKStages], k_empty[kKStages];
   uint64_t q_full[kSlots], q_empty[kSlots];
   uint64_t s_full[kBufs], s_empty[kBufs];
-  uint64_t handed_full, handed_empty;
+  uint64_t handed_full, handed_empty, mmas_done;
 };
 constexpr int kUnitReaders = 8 + kSlots + 4 + 1;  // warps that read a unit's slot
 
@@ -494,7 +494,8 @@ __device__ __forceinline__ void expand_keys(unsigned char* stage, float4* scales
 template <int D>
 __device__ __forceinline__ void load_keys(Smem& sm, const Params& p, int w, int lane) {
   constexpr int CB = D / 64;
-  for_units(sm, p, lane, [&](int n, const Unit& u) {
+  int issued = 0;  // units whose copies have been asked for
+  const bool done = for_units(sm, p, lane, [&](int n, const Unit& u) {
     const int st = n % kKStages;
     if (n >= kKStages && !wait(&sm.k_empty[st], n / kKStages - 1, p)) return false;
     if (u.four) {
@@ -514,9 +515,12 @@ __device__ __forceinline__ void load_keys(Smem& sm, const Params& p, int w, int 
         mbar_arrive(&sm.k_full[st]);
       }
     }
+    issued = n + 1;
     if (lane == 0) mbar_arrive(&sm.scales_full[n % kUnits]);
     return true;
   });
+  if (!done && w == 0 && lane == 0)  // (after a wait that gave up)
+    for (int n = max(0, issued - kKStages); n < issued; ++n) mbar_drain(&sm.k_full[n % kKStages], (n / kKStages) & 1, p.status);
 }
 
 // ---- warps 8-13: query rows --------------------------------------------------------------------------------
@@ -622,6 +626,10 @@ __device__ __forceinline__ void issue_mmas(Smem& sm, const Params& p, int lane) 
     }
     return true;
   });
+  if (lane == 0) {  // (every MMA is waited for already, unless a wait gave up)
+    tc_commit(&sm.mmas_done);
+    mbar_drain(&sm.mmas_done, 0, p.status);
+  }
 }
 
 // ---- warps 0-7: exponentials and sums --------------------------------------------------------------------------
@@ -753,6 +761,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_weights_wide(const Params p) {
     for (int i = 0; i < kBufs; ++i) { mbar_init(&sm.s_full[i], 1); mbar_init(&sm.s_empty[i], 4); }
     mbar_init(&sm.handed_full, 4);
     mbar_init(&sm.handed_empty, 4);
+    mbar_init(&sm.mmas_done, 1);
     mbar_fence_init();
   }
   chain_enter();

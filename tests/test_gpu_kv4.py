@@ -329,6 +329,42 @@ def test_decode_an_outlying_key_that_carries_nothing(requests, hkv, copies):
     pa.close()
 
 
+def test_a_node_behind_four_gigabytes_of_the_pool():
+    """Every kernel that addresses the 4-bit pool, at byte offsets that 32 bits do not hold: write, read, decode, weights and
+    eviction of a short node behind one of 60 million tokens."""
+    n, far = 200, 60_000_000
+    w = private_workload([far, n, 90], [[1], [1]], 2, 1, 64)
+    pa = _handle(w, [0, 1, 2], extra_kv4_tiles=far // 64 + 4)   # (only nodes on paths are counted)
+    zeros = torch.zeros(far, 1, 64, dtype=torch.bfloat16, device="cuda")
+    pa.write_node(0, 0, zeros, zeros)
+    del zeros
+    k, v = (W.bf16_bits_to_f64(x) for x in w.node_kv_bits(0, 1))
+    pa.write_node(1, 0, _tensor(k), _tensor(v))
+    from paper_2605_22566_b200 import binding as B
+    assert (pa.node_slot(1) - B.gf_pool_info(pa.g).capacity_tiles * 64) // 64 * 4608 > 2 ** 32
+    kv = kv4.values(k), kv4.values(v)
+    for got, want in zip(pa.load_node(1, 0), kv):
+        assert np.array_equal(_bits(got), f64_to_bf16_rne(want))
+    pa.build()
+    q, lse = pa.make_q(0, "host"), torch.empty(2, 2, device="cuda")
+    out = pa.decode(0, q, lse=lse)
+    qd = W.bf16_bits_to_f64(w.q_bits(0))
+    ref, ref_lse = OA.decode([[1], [1]], lambda _: kv, qd, 1)
+    assert_close(out.double().cpu().numpy(), ref, "out")
+    weights = pa.new_weights()
+    pa.attention_weights(0, q, lse, weights)
+    got = pa.node_weights(weights, 1)[0, 0].double().cpu().numpy()
+    want = np.exp(np.einsum("rhd,td->rht", qd, kv[0][:, 0]) / 8 - ref_lse[..., None]).sum((0, 1))
+    assert np.all(np.abs(got - want) <= 2e-3 * want)          # lse of decode is itself within that
+    assert float(weights.sum()) == pytest.approx(4, rel=1e-3)
+    (kept,) = pa.evict([(2, 1, 90, 4, 4)], weights)
+    idx = kept[0, 0].cpu().numpy()
+    for got, all_of in zip(pa.load_node(2, 0), pa.load_node(1, 0)):
+        assert torch.equal(got, all_of[idx])
+    assert pa.status() == 0
+    pa.close()
+
+
 def test_constant_values_and_equal_keys():
     """Equal keys give the mean of V; constant V comes back exactly (its groups are held exactly)."""
     d, n = 64, 77
