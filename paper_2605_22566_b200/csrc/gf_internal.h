@@ -38,8 +38,8 @@ struct __align__(32) Item {
 };
 
 // Longest chunk of a segment held in 4 bits, in multiples of the policy's chunk_tokens: its kernel gives a chunk's
-// 16 query rows to one warp, which has to come to an end.  256 requests: 163 us with 2, 172 with 4, 182 with 8 (fewer
-// partials against later ends); 1024 requests: 504, 475 and 465.
+// 16 query rows to one warp, which has to come to an end.  256 requests: 145 us with 2, 139 with 4, 137 with 8;
+// 1024 requests: 482, 461 and 460 (more partials against later ends; one kernel after the other, 163, 172 and 182).
 constexpr int kKv4ChunkMult = 4;
 // A chunk of such a segment goes 128 stacked query rows at a time to the tcgen05 kernel; where fewer rows than this
 // are left, to the kernels that take 16 (1024 requests: 464 us with 64, 467 with 128, 495 with 32).

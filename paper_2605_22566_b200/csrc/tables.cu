@@ -291,8 +291,8 @@ __global__ void k_scan_nodes_segments(GraphDev g, TablesDev t, gf_policy_t pol) 
     if (wide_units < t.wide_min_units) t.hdr->num_wide = 0;
     t.hdr->kv4_wide_first = t.hdr->num_wide > 0 ? wide_units : 0;
     // The tcgen05 kernel's units take two per multiprocessor as long as one: with fewer than that many, the rows are
-    // spread wider over the kernels that take 16 (256 requests over 128 units: 202 us against 190; 1024
-    // requests over 608: 500 against 532).
+    // spread wider over the kernels that take 16 (256 requests over 128 units: 165 us against 139; 1024
+    // requests over 608: 500 against 532, all kernels one after the other).
     int units = 0;
     for (int c = 0; c < kKv4Classes; ++c) units += kv4_split[2][c];
     const bool use = units >= 2 * t.wide_min_units;
