@@ -15,9 +15,10 @@
 // Up to kNarrowRows (k_weights_narrow): a stream of K, 64 tokens of it at a time copied into a warp's own piece of
 // shared memory; the warp walks the rows eight at a time: S^T = K Q^T (mma.sync), exp2, sums per token in
 // registers, and at the end a shuffle over the four lanes that share a token.  Nothing is shared between warps.
-// 256 requests, 256 nodes, a third in bf16: 73 us (K alone at the copy rate: 45), bound by the round trips of a unit (K, then
-// queries, sums before) that twelve warps per SM, as many as K finds room for, do not hide.  Walking K once for 16
-// rows spilled and took 120 us; queries through 4-byte loads in K's natural order 80.
+// 256 requests over 256 nodes in bf16: 416 MB of K in 73 us (5.7 TB/s), bound by HBM; with fewer keys per unit (4 bits: 168
+// MB, half of the tiles so, 47 us) by the round trips of a unit (K, then queries, sums before), which twelve warps per
+// SM, as many as K finds room for, do not hide.  Walking K once for 16 rows spilled and took 120 us instead of 94 in
+// all; queries through 4-byte loads in K's natural order 102.
 //
 // More (k_weights_wide): tcgen05 MMAs with the tokens as rows make the reduction run along the columns of tensor
 // memory: a thread owns a token, reads its scores 16 at a time and adds up 2^(scale s - lse), without a shuffle.
