@@ -49,6 +49,22 @@ def test_stored_values_bit_for_bit(hkv, d):
     pa.close()
 
 
+def test_stored_values_next_to_a_border_of_two_cells():
+    """Entries within an fp32 step of a whole number of cells above lo: x - lo rounded to fp32 decides."""
+    x = np.zeros((4, 1, 64))
+    x[:, 0, 0], x[:, 0, 1] = -4.0, 4.0                     # s = 1/2: cells begin at every half
+    tiny = 2.0 ** np.arange(-30, -8)
+    x[0, 0, 2:24], x[1, 0, 2:24], x[2, 0, 2:24], x[3, 0, 2:24] = tiny, -tiny, 1 - tiny, -2.5 - tiny
+    x = _bf16(x)
+    w = private_workload([4], [[0]], 1, 1, 64)
+    pa = _handle(w, [0])
+    t = _tensor(x)
+    pa.write_node(0, 0, t, t)
+    for got in pa.load_node(0, 0):
+        assert np.array_equal(_bits(got), f64_to_bf16_rne(kv4.values(x)))
+    pa.close()
+
+
 @pytest.mark.parametrize("scale", [1e-35, 1.0, 2e36])
 def test_stored_values_of_unusual_groups(scale):
     """Constant groups, one outlier, a spread far below the values, tiny and huge entries.  A value is computed in fp32 and
