@@ -34,23 +34,22 @@ __device__ __forceinline__ uint32_t ends_of(uint32_t lo2, uint32_t hi2) {
 }
 
 // A group's numbers as the coding of its entries takes them.  Everything is scaled by 1/16, which is exact and keeps
-// hi - lo from overflowing.
+// hi - lo from overflowing; a group whose s is below 2^-96 by 2^60 instead, exact too (its entries are below 2^-80: they
+// differ by at least a bf16 step), so that s, which goes down to 2^-133, has a reciprocal in fp32.
 struct GroupCoder {
   uint32_t word;   // (s, lo) as stored
-  float lo16, cell;  // -lo / 16, s / 16
-  float inv;       // a little more than 16 / s; 0 where s is 0
+  float unit;      // 1/16 or 2^60
+  float low, cell; // -lo unit, s unit
+  float inv;       // a little more than 1 / cell; 0 where s is 0
   __device__ __forceinline__ explicit GroupCoder(uint32_t ends) {  // see ends_of
     const float lo = __uint_as_float(ends << 16), hi = -__uint_as_float(ends & 0xffff0000u);
     const __nv_bfloat16 s = __float2bfloat16_rn(__fsub_rn(hi * 0.0625f, lo * 0.0625f));
     word = (uint32_t)__bfloat16_as_ushort(s) | (__float_as_uint(lo) & 0xffff0000u);
-    lo16 = lo * -0.0625f;
-    cell = __bfloat162float(s) * 0.0625f;
-    if (cell >= 0x1p-100f) {
-      asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(cell));  // within 2^-23, the factor is 1 + 2^-21
-      inv = __fmul_ru(inv, 1.0000005f);
-    } else {
-      inv = cell > 0.f ? __fmul_ru(__frcp_ru(cell), 1.0000005f) : 0.f;
-    }
+    unit = __bfloat162float(s) > 0.f && __bfloat162float(s) < 0x1p-96f ? 0x1p60f : 0.0625f;
+    low = lo * -unit;
+    cell = __bfloat162float(s) * unit;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(cell));  // within 2^-23, the factor is 1 + 2^-21
+    inv = cell > 0.f ? __fmul_ru(inv, 1.0000005f) : 0.f;
   }
   // The codes of N bf16 pairs, floor((x - lo) / s) within 0..15, one in each half of out[i].  The quotient from the
   // reciprocal is never below the true one and less than 2^-19 of it above, so its whole part is the code or,
@@ -58,13 +57,13 @@ struct GroupCoder {
   // whole number and two short numbers) is negative.  That is rare, and put right behind a vote.
   template <int N>
   __device__ __forceinline__ void codes(const uint32_t (&pair)[N], uint32_t (&out)[N]) const {
-    const uint64_t magic = f2_pack(8388608.f, 8388608.f), minus = f2_pack(-8388608.f, -8388608.f), sixteenth = f2_pack(0.0625f, 0.0625f);
-    const uint64_t l2 = f2_pack(lo16, lo16), i2 = f2_pack(inv, inv), c2 = f2_pack(-cell, -cell);
+    const uint64_t magic = f2_pack(8388608.f, 8388608.f), minus = f2_pack(-8388608.f, -8388608.f), unit2 = f2_pack(unit, unit);
+    const uint64_t l2 = f2_pack(low, low), i2 = f2_pack(inv, inv), c2 = f2_pack(-cell, -cell);
     uint32_t sign = 0u;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const uint64_t x = f2_pack(__uint_as_float(pair[i] << 16), __uint_as_float(pair[i] & 0xffff0000u));
-      const uint64_t r = f2_fma(x, sixteenth, l2);
+      const uint64_t r = f2_fma(x, unit2, l2);
       uint64_t t, u;
       asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(t) : "l"(r), "l"(i2));
       asm("add.rm.f32x2 %0, %1, %2;" : "=l"(u) : "l"(t), "l"(magic));  // 2^23 + the whole part: it stands in the low bits
@@ -78,7 +77,7 @@ struct GroupCoder {
     if (__any_sync(0xffffffffu, (sign >> 31) != 0u)) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const float r0 = fmaf(__uint_as_float(pair[i] << 16), 0.0625f, lo16), r1 = fmaf(__uint_as_float(pair[i] & 0xffff0000u), 0.0625f, lo16);
+        const float r0 = fmaf(__uint_as_float(pair[i] << 16), unit, low), r1 = fmaf(__uint_as_float(pair[i] & 0xffff0000u), unit, low);
         if (fmaf(-(float)(out[i] & 0xffffu), cell, r0) < 0.f) out[i] -= 1u;
         if (fmaf(-(float)(out[i] >> 16), cell, r1) < 0.f) out[i] -= 0x10000u;
       }

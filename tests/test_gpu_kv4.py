@@ -104,6 +104,37 @@ def test_largest_finite_range_does_not_overflow():
     pa.close()
 
 
+def test_stored_values_of_the_smallest_groups():
+    """Groups whose entries differ by 2^-118 down to the subnormals' step 2^-133: s has no reciprocal in fp32 from 2^-124 on,
+    and is a subnormal itself, or 0, further down.  Differences of such entries are exact in fp32, and so is every value."""
+    rng = np.random.default_rng(19)
+    steps = np.concatenate([np.arange(17), rng.integers(-16, 17, 47)])          # whole numbers of up to 16: exact in bf16
+    x = np.stack([np.stack([rng.permutation(steps), 128 + rng.permutation(np.arange(64) % 17)]) * 2.0 ** -e for e in range(118, 134)])
+    x[12:, 1] = np.abs(x[12:, 0])                                                # (the others there would not be small any more)
+    x[15, 1] = rng.integers(0, 6, 64) * 2.0 ** -133                              # s is 0, the entries are not equal
+    x = _bf16(x.reshape(-1, 1, 64))
+    n = len(x)
+    pa = _handle(private_workload([n], [[0]], 1, 1, 64), [0])
+    t = _tensor(x)
+    pa.write_node(0, 0, t, t)
+    _, s, _ = kv4.encode(x)
+    assert s.max() < 2.0 ** -115 and (s == 0).any() and ((s > 0) & (s < 2.0 ** -126)).any()
+    want = _bf16(kv4.values(x))
+    for got in pa.load_node(0, 0):
+        assert np.array_equal(bf16_to_f64(_bits(got)), want)
+    pa.close()
+
+
+@pytest.mark.parametrize("value", [1e30, -3.0, 2.0 ** -130])
+def test_constant_groups_of_any_size_are_exact(value):
+    x = _bf16(np.full((20, 2, 64), value))
+    pa = _handle(private_workload([20], [[0]], 2, 2, 64), [0])
+    t = _tensor(x)
+    pa.write_node(0, 0, t, t)
+    assert all(torch.equal(got, t) for got in pa.load_node(0, 0))
+    pa.close()
+
+
 def test_extents_release_rewrite_and_refusals():
     from paper_2605_22566_b200 import binding as B
     w = private_workload([100, 64, 30, 0, 100, 10], [[0], [1], [2]], 2, 2, 64)
