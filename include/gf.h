@@ -176,8 +176,8 @@ gf_status_t gf_node_extent(const gf_wgraph_t* g, int32_t node, int32_t* n_tokens
 
 /* ---- states held in 4 bits ------------------------------------------------------------------------
  * A node's state may be held in 4 bits instead of bf16: 64 neighbouring entries of one token and KV head
- * form a group with two bf16 numbers, lo (its least entry) and s (hi / 16 - lo / 16 in fp32, rounded to bf16); an
- * entry x has the code floor((x - lo) / s), x / 16 - lo / 16 in fp32 too, within 0..15 (0 where s is 0) and
+ * form a group with two bf16 numbers, lo (its least entry) and s (the bf16 number nearest to (hi - lo) / 16); an
+ * entry x has the code floor((x - lo) / s) of the exact quotient, within 0..15 (0 where s is 0), and
  * stands for lo + s (code + 1/2), the middle of its cell, or lo where s is 0.  4.5 bits per entry; a normal group is
  * off by about 0.09 of its standard deviation (root mean square).  Inputs are finite, and below 2^100 in
  * magnitude where attention is to read them.

@@ -4,8 +4,8 @@ TEST INFRASTRUCTURE ONLY (see the package docstring).
 
 64 neighbouring entries of one token and KV head form a group.  lo is its least entry, s the bf16 number
 nearest to (hi - lo) / 16 (ties to even), an entry's code floor((x - lo) / s) held within 0..15 (0 where s
-is 0), and what it stands for lo + s (code + 1/2) (lo where s is 0).  The differences, hi / 16 - lo / 16 and
-x / 16 - lo / 16, are rounded to fp32: an entry closer than that to the border of two cells may take either.
+is 0), and what it stands for lo + s (code + 1/2) (lo where s is 0).  The quotient is the exact one: what fp64 rounds
+off a difference or a quotient next to a border of two cells is put right.
 """
 from __future__ import annotations
 
@@ -27,10 +27,15 @@ def encode(x):
     """x fp64 [..., D] (bf16 numbers): (codes int [..., D], s [..., D / 64], lo [..., D / 64])."""
     g = x.reshape(x.shape[:-1] + (x.shape[-1] // GROUP, GROUP))
     lo, hi = g.min(-1), g.max(-1)
-    f32 = lambda y: y.astype(np.float32).astype(np.float64)
-    s = round_to_bf16(f32(hi / 16 - lo / 16))
+    s = round_to_bf16((hi - lo) / 16)
+    lo1, s1 = lo[..., None], s[..., None]
+    d = g - lo1
+    b = g - d
+    lost = (g - (d + b)) + (b - lo1)               # g - lo = d + lost
     with np.errstate(divide="ignore", invalid="ignore"):
-        c = np.floor(f32(g / 16 - lo[..., None] / 16) / (s[..., None] / 16))
+        c = np.clip(np.floor(d / s1), 0, 16)
+        rest = d - c * s1                          # exact: c s is a few whole steps of s
+        c = c - ((rest < 0) | ((rest == 0) & (lost < 0)))
     c = np.where(s[..., None] > 0, np.clip(c, 0, 15), 0).astype(np.int64)
     return c.reshape(x.shape), s, lo
 

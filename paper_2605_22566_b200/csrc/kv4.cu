@@ -33,6 +33,12 @@ __device__ __forceinline__ uint32_t ends_of(uint32_t lo2, uint32_t hi2) {
   return min_pair(__byte_perm(lo2, hi2, 0x5410), __byte_perm(lo2, hi2, 0x7632));
 }
 
+__device__ __forceinline__ uint64_t f2_fma_rz(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rz.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
 // A group's numbers as the coding of its entries takes them.  Everything is scaled by 1/16, which is exact and keeps
 // hi - lo from overflowing; a group whose s is below 2^-96 by 2^60 instead, exact too (its entries are below 2^-80: they
 // differ by at least a bf16 step), so that s, which goes down to 2^-133, has a reciprocal in fp32.
@@ -51,7 +57,11 @@ struct GroupCoder {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(cell));  // within 2^-23, the factor is 1 + 2^-21
     inv = cell > 0.f ? __fmul_ru(inv, 1.0000005f) : 0.f;
   }
-  // The codes of N bf16 pairs, floor((x - lo) / s) within 0..15, one in each half of out[i].  The quotient from the
+  // The codes of N bf16 pairs, floor((x - lo) / s) within 0..15, one in each half of out[i].  x - lo is rounded towards
+  // zero: fp32 holds every whole number of cells, so the rounded difference lies in the cell of the true one (rounded
+  // to nearest, one within 2^-24 below a border came to lie on it).  (s is the one of the true hi - lo too: where that
+  // difference is not exact in fp32, the smaller of the two numbers is below 2^-16 of the larger, which is then
+  // the bf16 number nearest to it either way.)  The quotient from the
   // reciprocal is never below the true one and less than 2^-19 of it above, so its whole part is the code or,
   // where a whole number lies between the two, one more: then the remainder (exact: an FMA on a small
   // whole number and two short numbers) is negative.  That is rare, and put right behind a vote.
@@ -63,7 +73,7 @@ struct GroupCoder {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const uint64_t x = f2_pack(__uint_as_float(pair[i] << 16), __uint_as_float(pair[i] & 0xffff0000u));
-      const uint64_t r = f2_fma(x, unit2, l2);
+      const uint64_t r = f2_fma_rz(x, unit2, l2);
       uint64_t t, u;
       asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(t) : "l"(r), "l"(i2));
       asm("add.rm.f32x2 %0, %1, %2;" : "=l"(u) : "l"(t), "l"(magic));  // 2^23 + the whole part: it stands in the low bits
@@ -77,7 +87,7 @@ struct GroupCoder {
     if (__any_sync(0xffffffffu, (sign >> 31) != 0u)) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const float r0 = fmaf(__uint_as_float(pair[i] << 16), unit, low), r1 = fmaf(__uint_as_float(pair[i] & 0xffff0000u), unit, low);
+        const float r0 = __fmaf_rz(__uint_as_float(pair[i] << 16), unit, low), r1 = __fmaf_rz(__uint_as_float(pair[i] & 0xffff0000u), unit, low);
         if (fmaf(-(float)(out[i] & 0xffffu), cell, r0) < 0.f) out[i] -= 1u;
         if (fmaf(-(float)(out[i] >> 16), cell, r1) < 0.f) out[i] -= 0x10000u;
       }

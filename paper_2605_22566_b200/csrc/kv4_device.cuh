@@ -2,7 +2,7 @@
 //
 // Format.  64 neighbouring entries of one (token, KV head) form a group with two bf16 numbers: lo, the
 // group's least value, and s, the bf16 nearest to (hi - lo) / 16.  An entry x has the code
-// c = floor((x - lo) / s) held within 0..15 (0 where s is 0; x - lo in fp32) and stands for lo + s (c + 1/2), the middle of
+// c = floor((x - lo) / s) held within 0..15 (0 where s is 0) and stands for lo + s (c + 1/2), the middle of
 // its cell (lo itself where s is 0); 4.5 bits per entry.  A group's numbers belong to one token, so that a
 // score is a sum of exact products: q . k = sum over groups of s (q . (c - 8)) + (lo + 8.5 s) (sum of q),
 // with c - 8 exact in bf16.

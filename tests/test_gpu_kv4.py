@@ -65,6 +65,26 @@ def test_stored_values_next_to_a_border_of_two_cells():
     pa.close()
 
 
+@pytest.mark.parametrize("exponent", [0, -100, 90])
+def test_stored_values_next_to_a_border_are_those_of_the_exact_quotient(exponent):
+    """Entries closer to a border of two cells than fp32 can tell beside lo: those below it lie in the lower cell."""
+    tiny = 2.0 ** -np.arange(10.0, 31)
+    x = np.zeros((4, 1, 64))
+    x[:, 0, 0], x[:, 0, 1] = -4.0, 4.0                     # s = 1/2
+    x[0, 0, 2:23], x[1, 0, 2:23] = tiny, -tiny
+    x[2, 0, 0], x[2, 0, 2] = -2.0 ** -30, 0.25             # s = 1/4; lo just below 0, then just above
+    x[3, 0, 0], x[3, 0, 2], x[3, 0, 3:] = 2.0 ** -30, 0.25, 2.0 ** -30
+    x *= 2.0 ** exponent
+    pa = _handle(private_workload([4], [[0]], 1, 1, 64), [0])
+    t = _tensor(_bf16(x))
+    pa.write_node(0, 0, t, t)
+    want = np.concatenate([np.full(21, 0.25), np.full(21, -0.25), [1.5 * 0.25, 0.5 * 0.25]]) * 2.0 ** exponent
+    for got in pa.load_node(0, 0):
+        got = bf16_to_f64(_bits(got))[:, 0]
+        assert np.array_equal(np.concatenate([got[0, 2:23], got[1, 2:23], [got[2, 2], got[3, 2]]]), want)
+    pa.close()
+
+
 @pytest.mark.parametrize("scale", [1e-35, 1.0, 2e36])
 def test_stored_values_of_unusual_groups(scale):
     """Constant groups, one outlier, a spread far below the values, tiny and huge entries.  A value is computed in fp32 and

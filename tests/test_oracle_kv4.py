@@ -51,3 +51,20 @@ def test_codes_against_rational_arithmetic_and_the_error_bound(scale):
             assert c[i, j] == want
             # half a cell, and where s was rounded down (by up to 2^-8 of itself) 16 such shortfalls at the top end
             assert abs(v[i, j] - x[i, j]) <= s[i, j // 64] * (0.5 + 16 * 2.0 ** -8)
+
+
+def test_codes_next_to_a_border_are_those_of_the_exact_quotient():
+    """Entries as little as 2^-130 from a whole number of cells above lo, which neither fp32 nor fp64 tells from the border."""
+    tiny = 2.0 ** -np.arange(10.0, 131, 4)
+    x = np.zeros((4, 64))
+    x[:, 0], x[:, 1] = -4.0, 4.0
+    x[0, 2:33], x[1, 2:33] = tiny, -tiny
+    x[2, 0], x[2, 1], x[2, 2:33] = -2.0 ** -60, 4.0, 0.25 + 0 * tiny          # lo is what is tiny
+    x[3, 0], x[3, 1], x[3, 2:33] = 2.0 ** -60, 4.0, 0.25 + 0 * tiny
+    c, s, lo = kv4.encode(x)
+    for i in range(4):
+        for j in range(64):
+            f = (Fraction(x[i, j]) - Fraction(lo[i, 0])) / Fraction(s[i, 0])
+            assert c[i, j] == min(15, f.numerator // f.denominator), (i, j)
+    assert c[0, 2:33].tolist() == [8] * 31 and c[1, 2:33].tolist() == [7] * 31
+    assert c[2, 2] == 1 and c[3, 2] == 1          # (0, which the rest of the group is, is the least entry of the last)
