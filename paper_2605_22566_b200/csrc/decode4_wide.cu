@@ -5,7 +5,8 @@
 // S = Q K^T and O += P C run as tcgen05 MMAs with accumulators in tensor memory:
 //   S_rt = sum over groups G of  q_rG . (s_tG (c_tG - 8))  +  (sum of q_rG) (lo_tG + 8.5 s_tG)
 // K's scales are part of the operand, exact in fp16 (the second term takes a few entries more, see sums_offset), so that a
-// score costs its thread one multiplication.  V's operand are the codes, fp16 subnormals c 2^-24 and 16 c 2^-24 (exact), with
+// score costs its thread one multiplication.  That needs a token's groups to be of about one size (see kNearGroups);
+// a tile with a token whose groups are not gets one S per group and two multiplications.  V's operand are the codes, fp16 subnormals c 2^-24 and 16 c 2^-24 (exact), with
 // one accumulator per group of 64 entries, because values of different tokens may lie any power of two apart:
 //   O_rG = sum over tokens of  (p_rt s_tG) c_tG  +  sum of  p_rt (lo_tG + s_tG / 2)
 // A thread owns a query row: it takes the 32 scores of a step from tensor memory, exponentiates, applies the
@@ -65,8 +66,13 @@ struct __align__(16) Unit {
   int32_t grp_begin, part_base, kvh, tok_count, ntile, pad0, pad1;
 };
 
-// s and z = lo + s / 2 of a tile's V, [group][token], and what undoes the powers of two that K's tokens were multiplied by.
-struct Scales { float s[2][kTile], z[2][kTile], k[kTile]; };
+// s and z = lo + s / 2 of a tile's V, [group][token]; what undoes the powers of two that K's tokens were multiplied by, per
+// group; and by block of 16 tokens whether the two groups have powers of their own.
+struct Scales { float s[2][kTile], z[2][kTile], k[2][kTile]; int32_t apart[4]; };
+// A token's groups share a power of two where their largest entries lie within 2^8 of each other: s, whose eight bits
+// begin at 2^-12 of its group's largest entry or above (entries are bf16), then stands at 2^-12 or above in the smaller
+// group, and s (c - 8) and lo + 8.5 s keep their bits in fp16.
+constexpr int kNearGroups = 8;
 
 template <int D>
 struct Smem {
@@ -75,7 +81,7 @@ struct Smem {
   unsigned char k[CB][kTile * 128];       // codes of a tile, K-major
   unsigned char v[CB][kTile * 128];       // and MN-major: both are rows of a token's 64 entries
   unsigned char q_sum[kRows * 32];        // 16 more entries of K's and Q's rows, for the term without codes (see sums_offset)
-  unsigned char k_mid[kTile * 32];
+  unsigned char k_mid[CB][kTile * 32];    // of the first S, and of the second one where the groups have one each
   unsigned char stage[kStages][kv4_tile_bytes(D)];
   Scales scales[kStages];                 // of tile n at n % kStages
   float row_scale[kRows];                 // softmax scale over the row's power of two
@@ -86,6 +92,7 @@ struct Smem {
   uint64_t s_full[2], p_full[2], o_full[2];  // by step parity
   uint64_t q_full, q_empty, k_full, v_full, o_empty, mmas_done;
 };
+static_assert(2 * (sizeof(Smem<128>) + 1024) <= 228 * 1024, "two CTAs share an SM's shared memory, of which each takes 1 KB more");
 constexpr int kUnitReaders = 4 + 4 + 1;
 
 __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t phase, const Params& p) { return mbar_wait(bar, phase & 1, p.status); }
@@ -213,34 +220,43 @@ __device__ __forceinline__ void load_queries(Smem<D>& sm, const Params& p, const
 }
 
 // Block b (16 tokens) of a tile's K: s (c - 8), which eleven bits hold (eight of s, three of c - 8), times a power of two
-// that brings the token's largest value to 2^8..2^9; and lo + 8.5 s beside it.  1024 + c and 1024 + 16 c are fp16 patterns with
+// that brings the token's largest value (or each group's, see kNearGroups) to 2^8..2^9; and lo + 8.5 s beside it.  1024 + c and 1024 + 16 c are fp16 patterns with
 // the code in their low bits.
 template <int D>
 __device__ __forceinline__ void expand_k(Smem<D>& sm, Scales& to, const char* part, int b, int lane) {
   constexpr int NG = D / kGroup4;
   const int l4 = lane & 3, l8 = lane >> 2, own = b * 16 + (lane & 15);
   // a token's numbers per lane (twice)
-  float s[NG], lo[NG], big = 0.f;
+  float s[NG], lo[NG], big[NG];
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
     const uint32_t sl = reinterpret_cast<const uint32_t*>(part + kv4_code_bytes(D))[own * NG + g];
     s[g] = kv4_s(sl);
     lo[g] = kv4_lo(sl);
-    big = fmax3(big, fabsf(lo[g]), fabsf(fmaf(16.f, s[g], lo[g])));
+    big[g] = fmaxf(fabsf(lo[g]), fabsf(fmaf(16.f, s[g], lo[g])));
   }
-  const float mul = pow2_to(big, 8);
+  bool apart = false;
+  if (NG == 2) {
+    const float least = fminf(big[0], big[NG - 1]), most = fmaxf(big[0], big[NG - 1]);
+    apart = __any_sync(0xffffffffu, least > 0.f && (__float_as_uint(most) >> 23) - (__float_as_uint(least) >> 23) > kNearGroups);
+    if (!apart) big[0] = big[NG - 1] = most;
+    if (lane == 0) to.apart[b] = apart;
+  }
   uint32_t step[NG];
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
+    const float mul = pow2_to(big[g], 8);
     step[g] = pack_f16(s[g] * mul, s[g] * mul);
     if (lane < 16) {
       __half hi, rest;
       split_f16(fmaf(8.5f, s[g], lo[g]) * (mul * 64.f), hi, rest);
       const uint32_t z = pair_of(hi, rest);
-      *reinterpret_cast<uint2*>(sm.k_mid + sums_offset(own, g)) = make_uint2(z, z);
+      const bool second = g == 1 && apart;
+      *reinterpret_cast<uint2*>(sm.k_mid[0] + sums_offset(own, g)) = second ? make_uint2(0u, 0u) : make_uint2(z, z);
+      if (g == 1) *reinterpret_cast<uint2*>(sm.k_mid[NG - 1] + sums_offset(own, g)) = second ? make_uint2(z, z) : make_uint2(0u, 0u);
+      to.k[g][own] = pow2_inverse(mul);
     }
   }
-  if (lane < 16) to.k[own] = pow2_inverse(mul);
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
     const uint4 c = reinterpret_cast<const uint4*>(part)[(b * NG + g) * 32 + lane];
@@ -333,19 +349,28 @@ __device__ __forceinline__ void expand(Smem<D>& sm, const Params& p, int w, int 
 }
 
 // ---- warp 9: MMAs ----------------------------------------------------------------------------------------
-// Tensor memory: S of step i at columns 32 (i % 2), P of group g over 16 g of them; O of group g at 128 + 64 g.  The scores of a step are formed while the softmax works on the step before.  (MMAs run in the order
-// of their issue: P of step i has been read when S of step i + 2 is written.  Each commit takes the issuing
-// thread as long as an MMA, 60 cycles, so there are two per step and every role takes them for what it waits for.)
+// Tensor memory: S of step i at columns 32 (i % 2), the second group's at 64 + 32 (i % 2) where it has one of its own, P of
+// group g over 16 g of the first; O of group g at 128 + 64 g.  The scores of a step are formed while the softmax works on
+// the step before.  (MMAs run in the order of their issue: P of step i has been read when S of step i + 2 is written.
+// Each commit takes the issuing thread as long as an MMA, 60 cycles, so there are two per step and every role takes them
+// for what it waits for.)
 template <int D>
-__device__ __forceinline__ void issue_scores(Smem<D>& sm, uint32_t tmem, uint32_t buf, uint32_t sub) {
+__device__ __forceinline__ bool any_apart(const Scales& s) {
+  const int4 x = *reinterpret_cast<const int4*>(s.apart);
+  return D == 128 && (x.x | x.y | x.z | x.w) != 0;
+}
+template <int D>
+__device__ __forceinline__ void issue_scores(Smem<D>& sm, uint32_t tmem, uint32_t buf, uint32_t sub, bool apart) {
   constexpr uint32_t idesc = idesc_f16(kRows, kSub, false);
 #pragma unroll
   for (int g = 0; g < D / kGroup4; ++g) {
     const uint64_t qd = tc_smem_desc(smem_u32(sm.q[g]), 0, 1024), kd = tc_smem_desc(smem_u32(sm.k[g]), 0, 1024) + sub * (kSub * 128 >> 4);
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) umma_ss(tmem + 32 * buf, qd + 2 * ks, kd + 2 * ks, idesc, g + ks > 0 ? 1u : 0u);  // 16 entries each
+    for (int ks = 0; ks < 4; ++ks)  // 16 entries each
+      umma_ss(tmem + 32 * buf + (apart ? 64 * g : 0), qd + 2 * ks, kd + 2 * ks, idesc, (apart ? 0 : g) + ks > 0 ? 1u : 0u);
   }
-  umma_ss(tmem + 32 * buf, sums_desc(smem_u32(sm.q_sum)), sums_desc(smem_u32(sm.k_mid) + sub * (kSub * 32)), idesc, 1u);
+  umma_ss(tmem + 32 * buf, sums_desc(smem_u32(sm.q_sum)), sums_desc(smem_u32(sm.k_mid[0]) + sub * (kSub * 32)), idesc, 1u);
+  if (apart) umma_ss(tmem + 64 + 32 * buf, sums_desc(smem_u32(sm.q_sum)), sums_desc(smem_u32(sm.k_mid[D / kGroup4 - 1]) + sub * (kSub * 32)), idesc, 1u);
   tc_commit(&sm.s_full[buf]);
 }
 template <int D>
@@ -356,14 +381,16 @@ __device__ __forceinline__ void issue_mmas(Smem<D>& sm, const Params& p, int lan
   for_units(sm, p, lane, [&](int n, const Unit& u) {
     const int steps = __shfl_sync(0xffffffffu, (u.tok_count + kSub - 1) / kSub, 0);
     if (!wait(&sm.q_full, n, p)) return false;
+    bool apart = false;  // of the tile whose scores are formed
     for (int i = -1; i < steps; ++i) {
       const uint32_t next = step + i + 1;
       if (i + 1 < steps) {  // the next step's scores
-        if ((i + 1) % 2 == 0 && !wait(&sm.k_full, tile + (i + 1) / 2, p)) return false;
-        tc_fence_after_sync();
-        if (lane == 0) {
-          issue_scores<D>(sm, tmem, next & 1, (i + 1) & 1);
+        if ((i + 1) % 2 == 0) {
+          if (!wait(&sm.k_full, tile + (i + 1) / 2, p)) return false;
+          apart = any_apart<D>(sm.scales[(tile + (i + 1) / 2) % kStages]);
         }
+        tc_fence_after_sync();
+        if (lane == 0) issue_scores<D>(sm, tmem, next & 1, (i + 1) & 1, apart);
         __syncwarp();
       }
       if (i < 0) continue;
@@ -430,10 +457,27 @@ __device__ __forceinline__ void softmax(Smem<D>& sm, const Params& p, int warp, 
         tmem_wait_ld();
 #pragma unroll
         for (int k = 0; k < kSub / 4; ++k) {
-          const float4 f = *reinterpret_cast<const float4*>(&vs.k[at + 4 * k]);
+          const float4 f = quad(vs.k, 0, k);
 #pragma unroll
           for (int h = 0; h < 2; ++h)
             x[2 * k + h] = f2_mul(f2_pack(__uint_as_float(a[4 * k + 2 * h]), __uint_as_float(a[4 * k + 2 * h + 1])), half(f, h));
+        }
+      }
+      if (any_apart<D>(vs)) {  // the second group's
+#pragma unroll
+        for (int c0 = 0; c0 < kSub; c0 += 16) {
+          uint32_t a[16];
+          tmem_ld16(cols + 64 + c0, a);
+          tmem_wait_ld();
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float4 f = quad(vs.k, 1, c0 / 4 + k);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              uint64_t& to = x[c0 / 2 + 2 * k + h];
+              to = f2_fma(f2_pack(__uint_as_float(a[4 * k + 2 * h]), __uint_as_float(a[4 * k + 2 * h + 1])), half(f, h), to);
+            }
+          }
         }
       }
       if (left < kSub) {

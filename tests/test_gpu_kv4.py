@@ -396,6 +396,33 @@ def test_decode_an_outlying_key_that_carries_nothing(requests, hkv, copies):
     pa.close()
 
 
+@pytest.mark.parametrize("requests,hkv,copies", [(1, 1, 1), (24, 1, 1), (24, 8, 40)])
+@pytest.mark.parametrize("gap,large", [(7, 0), (9, 1), (20, 1), (30, 0), (60, 1)])
+def test_decode_a_token_whose_groups_lie_far_apart(requests, hkv, copies, gap, large):
+    """Keys whose one group of 64 entries is 2^gap times the other, in which the queries are 0, in some blocks of 16 tokens and in
+    whole tiles: the scores are those of the other group, to the bound of test_decode_lse_is_exact_to_fp32."""
+    d, n, gqa = 128, 200, 8
+    rng = np.random.default_rng(23)
+    k, v, q = rng.standard_normal((n, 1, 2, 64)), rng.standard_normal((n, 1, d)) / 4, rng.standard_normal((requests, gqa, 2, 64))
+    far = np.r_[69, 100:103, 128:200]
+    k[far, :, large] *= 2.0 ** gap
+    q[:, :, large] = 0.0
+    k, v, q = (_bf16(np.repeat(x, hkv, 1)) for x in (k.reshape(n, 1, d), v, q.reshape(requests, gqa, d)))
+    path = list(range(copies))
+    pa = _handle(private_workload([n] * copies, [path] * requests, gqa * hkv, hkv, d), path)
+    for node in path:
+        pa.write_node(node, 0, _tensor(k), _tensor(v))
+    pa.build()
+    lse = torch.empty(requests, gqa * hkv, device="cuda")
+    out = pa.decode(0, _tensor(q), lse=lse).double().cpu().numpy()
+    kv = kv4.values(k), kv4.values(v)
+    ref, ref_lse = OA.decode([path] * requests, lambda _: kv, q, hkv)
+    assert pa.status() == 0
+    assert np.abs(lse.double().cpu().numpy() - ref_lse).max() <= 1.2e-4
+    assert_close(out, ref, "out")
+    pa.close()
+
+
 def test_a_node_behind_four_gigabytes_of_the_pool():
     """Every kernel that addresses the 4-bit pool, at byte offsets that 32 bits do not hold: write, read, decode, weights and
     eviction of a short node behind one of 60 million tokens."""
