@@ -109,6 +109,8 @@ struct gf_wgraph {
   // Host objects, created on first use; no device memory is allocated for them by this library.
   cudaStream_t side_stream = nullptr;
   cudaEvent_t ev_fork = nullptr, ev_join = nullptr;
+  cudaStream_t joined_stream = nullptr;  // the stream whose last operation of this handle is a join with the side stream
+  bool ends_in_join = false;
   int32_t wide_min_group = 64;  // decode: segments shared this widely go to the tensor-memory kernel
   // optional per-kernel timing
   bool profiling = false;
@@ -747,6 +749,13 @@ static gf_status_t read_back_tables(gf_tables* T) {
   return GF_OK;
 }
 
+// Whether the next kernel on `st` may be chained to the one before it (see launch_chained); the caller then says that it
+// has launched it.
+static bool may_chain(const gf_wgraph* g, cudaStream_t st) { return !(g->ends_in_join && g->joined_stream == st); }
+static void kernel_launched(gf_wgraph* g, cudaStream_t st) {
+  if (g->joined_stream == st) g->ends_in_join = false;
+}
+
 gf_status_t gf_build_path_tables(gf_wgraph_t* g, int32_t num_requests, int32_t num_path_nodes,
                                  const int32_t* path_ptr_dev, const int32_t* path_node_dev,
                                  int32_t mode, const gf_policy_t* policy, gf_tables_t** out,
@@ -839,8 +848,9 @@ gf_status_t gf_build_path_tables(gf_wgraph_t* g, int32_t num_requests, int32_t n
   T.info.num_requests = R;
   T.info.mode = mode;
 
-  int n = timed(g, kSpanTables, st, [&] { return launch_tables_phase_a(g->gd, t, path_ptr_dev, path_node_dev, pol, st); });
+  int n = timed(g, kSpanTables, st, [&] { return launch_tables_phase_a(g->gd, t, path_ptr_dev, path_node_dev, pol, may_chain(g, st), st); });
   if (n < 0) return GF_ERR_CUDA;
+  kernel_launched(g, st);
   g->launches += n;
   *out = &T;
   if (deferred) {
@@ -987,6 +997,8 @@ static int launch_decode_kernels(gf_wgraph* g, const gf_tables* t, const TablesD
   };
   const bool wide = !only4 && td.wide_min_group > 0 && t->num_wide != 0;
   const int split = wide ? (t->pending ? g->split_hint : t->split_sms) : 0;
+  bool chain = may_chain(g, st);  // of the next kernel on `st`
+  kernel_launched(g, st);         // (there is one: the build of a batch without items is itself behind any join)
   // Where two of them have work for every multiprocessor, one starts on what the other leaves free at its end.
   auto large = [&](int units) { return (int64_t)units * g->desc.num_kv_heads >= g->num_sms; };
   const int at_once = !any4 || t->pending ? 0 : large(num_items - t->kv4_items) + large(t->kv4_wide) + large(t->kv4_rows16) + large(t->kv4_rows8);
@@ -1002,11 +1014,14 @@ static int launch_decode_kernels(gf_wgraph* g, const gf_tables* t, const TablesD
     };
     // the warp kernel first: its CTAs are placed before the other kernel's, and those on the multiprocessors
     // it yields leave at once, so the tensor-memory kernel's first CTAs land there instead of ahead of it
-    if (!only4) count(launch_decode(g->pool, g->shape, td, num_items, layer, q, g->status_dev, split, residuals, st));
+    if (!only4) {
+      count(launch_decode(g->pool, g->shape, td, num_items, layer, q, g->status_dev, split, residuals, chain, st));
+      chain = true;
+    }
     if (split > 0) on_side += count(launch_decode_wide(g->pool, g->shape, td, num_items, layer, q, g->status_dev, 0, split, false, side));
     else if (wide) count(launch_decode_wide(g->pool, g->shape, td, num_items, layer, q, g->status_dev, 0, 0, true, st));
     on_side += count(wide4(on_side > 0, side));
-    count(rows16(true));
+    count(rows16(chain));
     count(rows8(on_side > 0, side));
     // (joined whatever happened, so that nothing of this call is left behind on the side stream)
     ok = cudaEventRecord(g->ev_join, side) == cudaSuccess && cudaStreamWaitEvent(st, g->ev_join, 0) == cudaSuccess && ok;
@@ -1015,13 +1030,16 @@ static int launch_decode_kernels(gf_wgraph* g, const gf_tables* t, const TablesD
   }
   int n = 0;
   if (!only4) {
-    const int b = launch_decode(g->pool, g->shape, td, num_items, layer, q, g->status_dev, 0, residuals, st);
+    const int b = launch_decode(g->pool, g->shape, td, num_items, layer, q, g->status_dev, 0, residuals, chain, st);
     if (b < 0) return -1;
     const int a = wide ? launch_decode_wide(g->pool, g->shape, td, num_items, layer, q, g->status_dev, 0, 0, true, st) : 0;
     if (a < 0) return -1;
     n = a + b;
+    chain = true;
   }
-  const int c = wide4(true, st), d = rows16(true), e = rows8(true, st);
+  const int c = wide4(chain, st);
+  const int d = rows16(chain || c > 0);
+  const int e = rows8(chain || c > 0 || d > 0, st);
   return c < 0 || d < 0 || e < 0 ? -1 : n + c + d + e;
 }
 
@@ -1164,8 +1182,13 @@ gf_status_t gf_path_attention_weights(gf_wgraph_t* g, const gf_tables_t* t, int3
     if (cudaEventRecord(g->ev_fork, st) != cudaSuccess || cudaStreamWaitEvent(side, g->ev_fork, 0) != cudaSuccess) return GF_ERR_CUDA;
   }
   const int n = launch_weights(g->pool, g->pool4, g->shape, t->dev, layer, q_dev, lse_dev, accumulate,
-                               weights_dev + (int64_t)layer * g->desc.num_kv_heads * slots, slots, most_rows, g->status_dev, st, side);
-  if (side && (cudaEventRecord(g->ev_join, side) != cudaSuccess || cudaStreamWaitEvent(st, g->ev_join, 0) != cudaSuccess)) return GF_ERR_CUDA;
+                               weights_dev + (int64_t)layer * g->desc.num_kv_heads * slots, slots, most_rows, g->status_dev, may_chain(g, st), st, side);
+  kernel_launched(g, st);
+  if (side) {
+    if (cudaEventRecord(g->ev_join, side) != cudaSuccess || cudaStreamWaitEvent(st, g->ev_join, 0) != cudaSuccess) return GF_ERR_CUDA;
+    g->joined_stream = st;
+    g->ends_in_join = true;
+  }
   if (n < 0) return GF_ERR_CUDA;
   g->launches += n;
   return GF_OK;

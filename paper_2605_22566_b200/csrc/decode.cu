@@ -585,7 +585,7 @@ int decode_grid_limit() {
 
 int launch_decode(const PoolGeom& pool, const AttnShape& sh, const TablesDev& t, int num_items,
                   int layer, const void* q, int32_t* status, int yield_sms, const ResidualEntry* residuals,
-                  cudaStream_t st) {
+                  bool chained, cudaStream_t st) {
   if (num_items == 0) return 0;  // num_items < 0: not known on the host, the kernel reads it
   DecodeParams p;
   p.pool_layer = pool.base + (uint64_t)layer * pool.layer_stride;
@@ -615,7 +615,8 @@ int launch_decode(const PoolGeom& pool, const AttnShape& sh, const TablesDev& t,
   p.yield_sms = ((int)grid.x == limit && yield_sms > 0 && 2 * yield_sms < limit) ? yield_sms : 0;
   auto go = [&](auto kernel, size_t smem, bool (&optin)[kMaxDevices]) {
     if (!ensure_dynamic_smem(kernel, smem, optin)) return false;
-    launch_chained(kernel, grid, dim3(kDecodeThreads), smem, st, p);
+    if (chained) launch_chained(kernel, grid, dim3(kDecodeThreads), smem, st, p);
+    else kernel<<<grid, dim3(kDecodeThreads), smem, st>>>(p);
     return true;
   };
   static bool optin[4][kMaxDevices] = {};
@@ -638,7 +639,7 @@ int launch_merge(const AttnShape& sh, const TablesDev& t, void* out, float* lse,
     if (chained)
       launch_chained(kernel, dim3(blocks), dim3(256), 0, st, t.part_o, t.part_ml, t.mrg_ptr, t.mrg_slot, t.num_requests,
                      sh.num_q_heads, (__nv_bfloat16*)out, lse, t.hdr, t.slot_cap, t.status);
-    else  // behind a join with another stream: must not be scheduled before that join is through
+    else
       kernel<<<dim3(blocks), dim3(256), 0, st>>>(t.part_o, t.part_ml, t.mrg_ptr, t.mrg_slot, t.num_requests, sh.num_q_heads,
                                                  (__nv_bfloat16*)out, lse, t.hdr, t.slot_cap, t.status);
   };

@@ -232,7 +232,8 @@ __device__ __forceinline__ bool bounds_report(bool ok, int32_t* status, int site
 // serialization, a kernel may be scheduled while its predecessor is still running; it first lets its
 // own successor be scheduled, then waits until the predecessor has completed and its writes are
 // visible, before it touches global memory.  What is saved is the launch and drain gap at every
-// boundary of the chain (a decode step on config 1 is nine short kernels).
+// boundary of the chain (a decode step on config 1 is nine short kernels).  The predecessor has to be a kernel of the
+// same stream: behind a join with another stream the next kernel is launched plainly, so that it waits for both.
 #ifdef __CUDACC__
 __device__ __forceinline__ void chain_enter() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -289,7 +290,7 @@ int launch_transition_counts(const GraphDev& g, int num_edges, int num_requests,
 int launch_select_transitions(const int32_t* counts, int num_edges, int min_count, uint8_t* keep,
                               unsigned long long* totals, cudaStream_t st);
 int launch_tables_phase_a(const GraphDev& g, const TablesDev& t, const int32_t* path_ptr,
-                          const int32_t* path_node, gf_policy_t pol, cudaStream_t st);
+                          const int32_t* path_node, gf_policy_t pol, bool chained, cudaStream_t st);
 // num_items < 0: not known on the host (deferred build); the kernels read the counts on the device.
 int launch_tables_phase_b(const TablesDev& t, const int32_t* path_ptr, const int32_t* path_node, gf_policy_t pol,
                           int num_items, cudaStream_t st);
@@ -298,14 +299,14 @@ int launch_tables_phase_b(const TablesDev& t, const int32_t* path_ptr, const int
 // residuals: the residual table rows of `layer` ([row] of ResidualEntry), or null when no node has one.
 int launch_decode(const PoolGeom& pool, const AttnShape& sh, const TablesDev& t, int num_items,
                   int layer, const void* q, int32_t* status, int yield_sms, const ResidualEntry* residuals,
-                  cudaStream_t st);
+                  bool chained, cudaStream_t st);
 int launch_set_residual(ResidualEntry* slot, const ResidualEntry& value, int32_t* node_res, int node, int row,
                         cudaStream_t st);
 // split: eight warps per (request, head) instead of one.
 int launch_merge(const AttnShape& sh, const TablesDev& t, void* out, float* lse, bool chained, bool split, cudaStream_t st);
 // Two launches: the kernel and, behind it, its exact variant, which leaves at once unless the first
 // met scores beyond what its lagging softmax reference may keep.  num_ctas / exact_ctas <= 0: one per
-// multiprocessor.  chained: launched with programmatic stream serialization (only when its
+// multiprocessor.  chained (here and below): launched with programmatic stream serialization (only when its
 // predecessor in `st` is the kernel it depends on).
 int launch_decode_wide(const PoolGeom& pool, const AttnShape& sh, const TablesDev& t, int num_items, int layer,
                        const void* q, int32_t* status, int num_ctas, int exact_ctas, bool chained, cudaStream_t st);
@@ -326,7 +327,8 @@ int launch_decode4(const PoolGeom& pool, const AttnShape& sh, const TablesDev& t
 // most_rows: query rows of the segment that has most, < 0: not known on the host.  side: a stream behind `st` that the
 // second of the two kernels may use, or null.
 int launch_weights(const PoolGeom& pool16, const PoolGeom& pool4, const AttnShape& sh, const TablesDev& t, int layer, const void* q,
-                   const float* lse, int accumulate, float* weights, int64_t slots, int most_rows, int32_t* status, cudaStream_t st, cudaStream_t side);
+                   const float* lse, int accumulate, float* weights, int64_t slots, int most_rows, int32_t* status, bool chained,
+                   cudaStream_t st, cudaStream_t side);
 int launch_evict(const PoolGeom& pool16, const PoolGeom& pool4, const EvictBatch& batch, int num_layers, int num_kv_heads,
                  int head_dim, float* weights, int64_t slots, int32_t* kept, const GraphDev& g, cudaStream_t st);
 int launch_wait_probe(int32_t* status, long long limit, int32_t* returned, cudaStream_t st);

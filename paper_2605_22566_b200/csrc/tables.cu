@@ -608,10 +608,11 @@ int launch_set_residual(ResidualEntry* slot, const ResidualEntry& value, int32_t
 }
 
 int launch_tables_phase_a(const GraphDev& g, const TablesDev& t, const int32_t* path_ptr,
-                          const int32_t* path_node, gf_policy_t pol, cudaStream_t st) {
+                          const int32_t* path_node, gf_policy_t pol, bool chained, cudaStream_t st) {
   const int R = t.num_requests;
   const int span = (g.num_nodes + 1 > t.seg_cap) ? g.num_nodes + 1 : t.seg_cap;
-  launch_chained(k_init, dim3(blocks_for(span, 256)), dim3(256), 0, st, t, g.num_nodes + 1);
+  if (chained) launch_chained(k_init, dim3(blocks_for(span, 256)), dim3(256), 0, st, t, g.num_nodes + 1);
+  else k_init<<<blocks_for(span, 256), 256, 0, st>>>(t, g.num_nodes + 1);
   launch_chained(k_validate, dim3(blocks_for(R * 32, 128)), dim3(128), 0, st, g, t, path_ptr, path_node);
   launch_chained(k_scan_nodes_segments, dim3(1), dim3(kScanThreads), 0, st, g, t, pol);
   launch_chained(k_fill_groups, dim3(blocks_for(R * 32, 128)), dim3(128), 0, st, t, path_ptr, path_node);

@@ -786,7 +786,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_weights_wide(const Params p) {
 }  // namespace
 
 int launch_weights(const PoolGeom& pool16, const PoolGeom& pool4, const AttnShape& sh, const TablesDev& t, int layer, const void* q,
-                   const float* lse, int accumulate, float* weights, int64_t slots, int most_rows, int32_t* status, cudaStream_t st, cudaStream_t side) {
+                   const float* lse, int accumulate, float* weights, int64_t slots, int most_rows, int32_t* status, bool chained,
+                   cudaStream_t st, cudaStream_t side) {
   const bool any_wide = most_rows < 0 || most_rows > kNarrowRows;
   Params p;
   p.layer16 = pool16.base + (uint64_t)layer * pool16.layer_stride;
@@ -819,10 +820,12 @@ int launch_weights(const PoolGeom& pool16, const PoolGeom& pool4, const AttnShap
   p.status = status;
   auto go = [&](auto wide, auto narrow, size_t narrow_smem, bool (&optin)[2][kMaxDevices]) {
     if (!ensure_dynamic_smem(wide, sizeof(Smem), optin[0]) || !ensure_dynamic_smem(narrow, narrow_smem, optin[1])) return false;
-    if (any_wide) launch_chained(wide, dim3((unsigned)t.num_sms), dim3(kThreads), sizeof(Smem), st, p);
+    if (any_wide && chained) launch_chained(wide, dim3((unsigned)t.num_sms), dim3(kThreads), sizeof(Smem), st, p);
+    else if (any_wide) wide<<<t.num_sms, kThreads, sizeof(Smem), st>>>(p);
     const dim3 grid((unsigned)(3 * t.num_sms));
     if (side) narrow<<<grid, kNarrowThreads, narrow_smem, side>>>(p);
-    else launch_chained(narrow, grid, dim3(kNarrowThreads), narrow_smem, st, p);
+    else if (any_wide || chained) launch_chained(narrow, grid, dim3(kNarrowThreads), narrow_smem, st, p);
+    else narrow<<<grid, kNarrowThreads, narrow_smem, st>>>(p);
     return true;
   };
   static bool optin[2][2][kMaxDevices] = {};

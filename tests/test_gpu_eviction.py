@@ -174,6 +174,48 @@ def test_weights_on_two_streams_captured_on_another_stream_and_deferred(four):
     pa.close()
 
 
+@pytest.mark.parametrize("captured", [False, True])
+def test_calls_at_once_behind_weights_on_two_streams(captured):
+    """Weights that run on two streams, and behind them, without a wait, a decode into the very lse that they read and a build of
+    the tables: nothing of what follows overtakes the second stream."""
+    w = two_stream_case()
+    pa = _handle(w, [0, 2, 4])
+    q = pa.make_q(0, "host")
+    other = torch.flip(q, [0]).contiguous()
+    lse, out = torch.empty(40, 32, device="cuda"), torch.empty_like(q)
+    wants = []
+    for x in (q, other):                                      # one after the other
+        pa.decode(0, x, out=out, lse=lse)
+        torch.cuda.synchronize()
+        weights = pa.new_weights()
+        pa.attention_weights(0, x, lse, weights, accumulate=False)
+        torch.cuda.synchronize()
+        wants.append((lse.clone(), out.clone(), weights))
+    got = [torch.zeros_like(wants[0][2]) for _ in wants]
+
+    def run():
+        for x, y in zip((q, other), got):
+            pa.decode(0, x, out=out, lse=lse)
+            pa.attention_weights(0, x, lse, y, accumulate=False)
+        pa.decode(0, q, out=out, lse=lse)
+    if captured:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            run()
+    for _ in range(50):
+        for y in got:
+            y.zero_()
+        if captured:
+            graph.replay()
+        else:
+            run()
+            pa.build()
+        assert torch.equal(lse, wants[0][0]) and torch.equal(out, wants[0][1])
+        assert all(torch.equal(y, want[2]) for y, want in zip(got, wants))
+    assert pa.status() == 0
+    pa.close()
+
+
 def test_weights_of_an_invalid_deferred_batch_change_nothing():
     from paper_2605_22566_b200 import binding as B
     w = private_workload([100, 64], [[0], [1]], 4, 2, 64)
