@@ -38,6 +38,9 @@ constexpr int kThreads = 384;
 // groups of four warps add up to what the CTA was launched with.
 constexpr int kLaunchRegs = 80, kSoftmaxRegs = 120, kExpandRegs = 72, kControlRegs = 48;
 static_assert(kSoftmaxRegs + kExpandRegs + kControlRegs == 3 * kLaunchRegs, "setmaxnreg draws on the launch's registers");  // (see the launch)
+// What a warp gets of a kernel that needs `regs` per thread: registers are handed out by eights.
+constexpr int allocated_regs(int regs) { return (regs + 7) / 8 * 8; }
+static_assert(allocated_regs(72) == 72 && allocated_regs(73) == 80 && allocated_regs(80) == 80, "");
 constexpr int kRows = 128;
 constexpr int kUnits = 4, kStages = 3;
 constexpr int kSub = 32;  // tokens per step of the softmax: half a tile
@@ -696,9 +699,9 @@ int launch_decode4_wide(const PoolGeom& pool, const AttnShape& sh, const TablesD
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return false;
     if (dev >= kMaxDevices || !optin[dev]) {
-      // (a build that gives the kernel fewer registers would leave the split below waiting for them)
+      // (a build that gives the kernel fewer registers would leave the roles waiting for their shares)
       cudaFuncAttributes attr;
-      if (cudaFuncGetAttributes(&attr, kernel) != cudaSuccess || attr.numRegs != kLaunchRegs) return false;
+      if (cudaFuncGetAttributes(&attr, kernel) != cudaSuccess || allocated_regs(attr.numRegs) != kLaunchRegs) return false;
     }
     if (!ensure_dynamic_smem(kernel, smem, optin)) return false;
     if (chained) launch_chained(kernel, grid, dim3(kThreads), smem, st, p);
