@@ -209,14 +209,17 @@ gf_status_t gf_node_kv4_write(gf_wgraph_t* g, int32_t node, int32_t layer, const
  * Every token of a pool has a slot: its offset in the bf16 pool, or the bf16 pool's capacity in tokens
  * plus its offset in the 4-bit pool; a node's tokens have consecutive slots from the offset that
  * gf_node_extent reports.  gf_weight_slots: how many there are, 64 * (tiles of both pools); it grows
- * with gf_kv4_pool_attach.  The weights are the caller's array, fp32 [num_layers, num_kv_heads, slots]. */
+ * with gf_kv4_pool_attach.  The weights are the caller's array, fp32 [num_layers, num_kv_heads, slots], which no
+ * write or release of a node touches: a node that takes the slots of a released one finds that one's sums there.  Before
+ * a node's first accumulated step the caller sets its slots to zero (num_layers * num_kv_heads rows of n_tokens
+ * floats, `slots` apart); gf_node_kv_evict fills those of its destinations itself. */
 int64_t gf_weight_slots(const gf_wgraph_t* g);
 
 /* What share of the attention of one decode step every resident token received, one layer:
  *   weight[kvh][slot of t] = sum over the requests whose path holds t's node and the query heads h of KV
  *                            head kvh of exp(scale * q_rh . k_t - lse_rh)
  * q_dev and lse_dev are those of the step's gf_path_attention_decode with the same tables.  accumulate 1
- * adds the sum to what weights_dev holds, 0 replaces it (a node's first step); slots of tokens that are
+ * adds the sum to what weights_dev holds, 0 replaces it, either for every node of the batch; slots of tokens that are
  * on no path of the batch are left as they are, and so are those of nodes kept as base + residual, which
  * have no tiles of their own.  Sums run in a fixed order: equal inputs give equal bits.  weights_dev is the
  * whole array, 4-byte aligned; only `layer`'s part is touched.  Asynchronous. */

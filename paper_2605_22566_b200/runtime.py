@@ -288,6 +288,12 @@ class PathAttention:
         B.check(st, "gf_node_extent")
         return weights.narrow(2, slot, n)
 
+    def clear_node_weights(self, weights: torch.Tensor, node: int) -> None:
+        """Zeroes one node's weights.  A node that takes the token slots of a released one finds that one's sums there:
+        call this before the first step that accumulates into it.  (The destinations of `evict` are filled by it.)"""
+        self._check_weights(weights)
+        self.node_weights(weights, node).zero_()
+
     def _check_weights(self, weights: torch.Tensor) -> None:
         shape = (self.layers, self.w.num_kv_heads, B.gf_weight_slots(self.g))
         if weights.dtype != torch.float32 or weights.device != self.pool.device or not weights.is_contiguous() or \
@@ -297,7 +303,8 @@ class PathAttention:
     def attention_weights(self, layer: int, q: torch.Tensor, lse: torch.Tensor, weights: torch.Tensor,
                           accumulate: bool = True) -> torch.Tensor:
         """gf_path_attention_weights: adds to `weights` (or sets) what every token of the batch's paths received in
-        the decode step of q and lse."""
+        the decode step of q and lse.  With nodes that have weights already beside new ones in a batch: accumulate, the
+        new ones cleared before (clear_node_weights)."""
         self._check_weights(weights)
         rows = (self.w.num_requests, self.w.num_q_heads)
         if q.dtype != torch.bfloat16 or not q.is_contiguous() or tuple(q.shape) != rows + (self.w.head_dim,) or q.device != self.pool.device:

@@ -216,6 +216,38 @@ def test_calls_at_once_behind_weights_on_two_streams(captured):
     pa.close()
 
 
+@pytest.mark.parametrize("four", [False, True])
+def test_a_new_node_on_the_slots_of_a_released_one_beside_an_old_node(four):
+    """One batch with a node that has weights already and one that takes a released node's slots: cleared, the new one's are
+    its own step's, and the old one's go on."""
+    from paper_2605_22566_b200 import binding as B
+    w = private_workload([100, 200, 130], [[0, 1], [0, 1], [0, 2]], 4, 2, 64)
+    pa = _handle_unbuilt(w, range(3) if four else [])
+    pa.write_nodes("host", only=[0, 1])
+    pa.build()                                                 # (node 2 does not exist yet: an empty segment)
+    q, lse, weights = pa.make_q(0, "host"), torch.empty(3, 4, device="cuda"), pa.new_weights()
+    pa.decode(0, q, lse=lse)
+    pa.attention_weights(0, q, lse, weights)
+    slot, old = pa.node_slot(1), pa.node_weights(weights, 0).clone()
+    assert float(pa.node_weights(weights, 1).sum()) > 1
+    assert B.gf_node_kv_release(pa.g, 1, pa.stream) == B.GF_OK
+    pa.write_nodes("host", only=[2])
+    assert pa.node_slot(2) == slot and float(pa.node_weights(weights, 2).sum()) > 1      # the released node's sums
+    pa.clear_node_weights(weights, 2)
+    assert float(pa.node_weights(weights, 2).abs().sum()) == 0 and torch.equal(pa.node_weights(weights, 0), old)
+    pa.build()
+    pa.decode(0, q, lse=lse)
+    alone = torch.zeros_like(weights)
+    pa.attention_weights(0, q, lse, alone, accumulate=False)
+    pa.attention_weights(0, q, lse, weights, accumulate=True)
+    assert torch.equal(pa.node_weights(weights, 2), pa.node_weights(alone, 2))
+    assert torch.equal(pa.node_weights(weights, 0), old + pa.node_weights(alone, 0))
+    with pytest.raises(ValueError):
+        pa.clear_node_weights(weights[:, :, :-1], 2)
+    assert pa.status() == 0
+    pa.close()
+
+
 def test_weights_of_an_invalid_deferred_batch_change_nothing():
     from paper_2605_22566_b200 import binding as B
     w = private_workload([100, 64], [[0], [1]], 4, 2, 64)
