@@ -985,7 +985,8 @@ static int launch_decode_kernels(gf_wgraph* g, const gf_tables* t, const TablesD
   const ResidualEntry* residuals =
       g->res_rows_in_use > 0 ? g->res_table_dev + (size_t)layer * g->desc.max_residual_nodes : nullptr;
   // Segments held in 4 bits: up to three kernels of their own.  All kernels of a layer work on disjoint items.
-  const bool any4 = g->kv4_nodes > 0, only4 = !t->pending && t->kv4_items > 0 && t->kv4_items == num_items;
+  // (Deferred tables may be built again by the replay of a graph, over nodes that are held in 4 bits only by then.)
+  const bool any4 = t->pending ? g->pool4.base != nullptr : g->kv4_nodes > 0, only4 = !t->pending && t->kv4_items > 0 && t->kv4_items == num_items;
   auto rows16 = [&](bool chained) {
     return launch_decode4(g->pool4, g->shape, td, 16, any4 ? t->kv4_rows16 : 0, layer, q, g->status_dev, chained, st);
   };

@@ -549,6 +549,33 @@ def test_decode_on_two_streams_captured_on_another_stream_and_twice(four):
     pa.close()
 
 
+@pytest.mark.parametrize("requests", [2, 70])
+def test_a_captured_step_of_deferred_tables_takes_a_node_written_in_4_bits_later(requests):
+    """A graph of a deferred build and its decode, captured while no node is held in 4 bits and replayed when one on its paths is."""
+    w = private_workload([200, 130, 64], [[0, 1, 2]] * requests, 4, 2, 64)
+    pa = _handle(w, [1])
+    pa.write_nodes("host", only=[0, 2])
+    pa.build()
+    q = pa.make_q(0, "host")
+    out = torch.zeros_like(q)
+    pa.decode(0, q, out=out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        pa.build(deferred=True)
+        pa.decode(0, q, out=out)
+    view = View(w, [1])
+    for nodes in ([0, 2], [0, 1, 2]):
+        if 1 in nodes:
+            pa.write_nodes("host", only=[1])
+        out.zero_()
+        graph.replay()
+        ref, _ = OA.decode([nodes] * requests, view.node_kv, view.q(), 2)
+        assert_close(out.double().cpu().numpy(), ref, str(nodes))
+    assert pa.status() == 0
+    pa.close()
+
+
 def test_extend_refuses_paths_through_4_bit_nodes():
     from paper_2605_22566_b200 import binding as B
     w = private_workload([70, 64, 10], [[0, 2], [1, 2]], 4, 2, 64)
