@@ -362,6 +362,70 @@ def test_evict_twice_into_the_same_node_and_one_source_into_two():
     pa.close()
 
 
+def _tail_of_4_bit_part(part, d, values, first):
+    """The codes and (s, lo) words of a 4-bit tile's K (values False) or V part that belong to tokens from `first` on (the layout
+    of kv4_device.cuh)."""
+    groups = d // 64
+    words = part[:32 * d].view(np.uint32).reshape(4, groups, 32, 4)          # [block of 16, group, lane, word]
+    b, lane, nibble = np.arange(4)[:, None, None], np.arange(32)[:, None], np.arange(8)
+    half, j, l4, l8 = nibble // 4, nibble % 4, lane % 4, lane // 4
+    token = 16 * b + (2 * l4 + half + 8 * (j // 2) if values else l8 + 8 * (j % 2) + 0 * half)
+    codes = words[..., None] >> (16 * half + 4 * j).astype(np.uint32) & 15   # [block, group, lane, word, nibble]
+    at = np.broadcast_to(token[:, None, :, None, :], codes.shape) >= first
+    return np.concatenate([codes[at], part[32 * d:].view(np.uint32).reshape(64, groups)[first:].ravel()])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("n,m", [(1, 1), (70, 7), (150, 33), (300, 177), (500, 64)])
+def test_rows_behind_the_last_token_are_zeros(d, four, n, m):
+    """Pools full of NaN patterns: the last tile of a written node (n tokens) and of an evicted one (m of them; in one launch and in
+    two) holds zeros behind the last token, in every layer and head; attention multiplies them by 0."""
+    hkv, layers = 3, 2
+    w = private_workload([n, m], [[0], [1]], hkv, hkv, d, layers=layers)
+    pa = _handle_unbuilt(w, [0, 1] if four else [])
+    pool = pa.pool4 if four else pa.pool
+    pool.fill_(0xFF)
+    pa.write_nodes("host", only=[0])
+    weights = pa.new_weights()
+    pa.node_weights(weights, 0).copy_(torch.rand(layers, hkv, n, generator=torch.Generator().manual_seed(n)))
+    pa.evict([(1, 0, m, 0, 0)], weights)
+    from paper_2605_22566_b200 import binding as B
+    info, size = (B.gf_kv4_pool_info(pa.g), B.gf_kv4_bytes_per_tile(d)) if four else (B.gf_pool_info(pa.g), B.gf_pool_bytes_per_tile(d))
+    tiles = pool.cpu().numpy()[:layers * hkv * info.capacity_tiles * size].reshape(layers * hkv, info.capacity_tiles, size)
+    before = 0 if not four else B.gf_pool_info(pa.g).capacity_tiles
+    for node, count in ((0, n), (1, m)):
+        last, rows = pa.node_slot(node) // 64 - before + (count - 1) // 64, (count - 1) % 64 + 1
+        for tile in tiles[:, last]:
+            if four:
+                parts = [_tail_of_4_bit_part(part, d, i == 1, rows) for i, part in enumerate(tile.reshape(2, size // 2))]
+                assert sum(map(len, parts)) == 2 * (64 - rows) * (d + d // 64) and not np.concatenate(parts).any()
+            else:
+                assert not tile.reshape(2 * d // 64, 64, 128)[:, rows:].any()
+    assert pa.status() == 0
+    pa.close()
+
+
+@pytest.mark.parametrize("four", [False, True])
+def test_evict_one_source_into_two_nodes(four):
+    w = private_workload([200, 70, 129], [[0], [1], [2]], 2, 2, 64)
+    pa = _handle_unbuilt(w, range(3) if four else [])
+    pa.write_nodes("host", only=[0])
+    weights = pa.new_weights()
+    pa.node_weights(weights, 0).copy_(torch.rand(1, 2, 200, generator=torch.Generator().manual_seed(3)))
+    given = pa.node_weights(weights, 0)[0].cpu().numpy()
+    kept = pa.evict([(1, 0, 70, 3, 0), (2, 0, 129, 0, 8)], weights)
+    for node, m, first, last in ((1, 70, 3, 0), (2, 129, 0, 8)):
+        for h in range(2):
+            want = OE.kept(given[h], m, first, last)
+            assert kept[node - 1][0, h].tolist() == want
+            assert np.array_equal(pa.node_weights(weights, node)[0, h].cpu().numpy(), given[h][want])
+            for src, dst in zip(pa.load_node(0, 0), pa.load_node(node, 0)):
+                assert torch.equal(src[want, h], dst[:, h])
+    assert pa.status() == 0
+    pa.close()
+
+
 @pytest.mark.parametrize("four", [False, True])
 @pytest.mark.parametrize("keep", [100, 700])
 def test_evict_captured_and_on_another_stream(four, keep):
