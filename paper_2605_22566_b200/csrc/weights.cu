@@ -170,37 +170,31 @@ struct QueryRows {
 template <bool k4>
 __device__ __forceinline__ int token_of_row(int r) { return k4 ? r : (r >> 1) + 4 * (r & 1); }
 
-// The scores of 16 tokens (block b of the unit's K in shared memory) and 8 NT rows, in units of 1 / scale.
-template <int D, bool k4, int NT>
-__device__ __forceinline__ void block_scores(float (&s)[NT][4], const unsigned char* k, int b, const QueryRows<D> (&q)[NT],
-                                             const float (&qsum)[NT][D / kGroup4][2], int lane) {
+// The scores of 16 tokens (block b of the unit's K in shared memory) and eight rows, in units of 1 / scale.
+template <int D, bool k4>
+__device__ __forceinline__ void block_scores(float (&s)[4], const unsigned char* k, int b, const QueryRows<D>& q,
+                                             const float (&qsum)[D / kGroup4][2], int lane) {
   constexpr int NG = D / kGroup4;
   const int l4 = lane & 3, l8 = lane >> 2;
-#pragma unroll
-  for (int j = 0; j < NT; ++j) s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
+  s[0] = s[1] = s[2] = s[3] = 0.f;
   if (k4) {
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
       const uint4 c = reinterpret_cast<const uint4*>(k)[(b * NG + g) * 32 + lane];
       const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-      float acc[NT][4];
-#pragma unroll
-      for (int j = 0; j < NT; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
+      float acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) {
         uint32_t a[4];
         kv4_expand(a, w[kk]);
-#pragma unroll
-        for (int j = 0; j < NT; ++j) mma_bf16(acc[j], a, q[j].f[g * 4 + kk][0], q[j].f[g * 4 + kk][1]);
+        mma_bf16(acc, a, q.f[g * 4 + kk][0], q.f[g * 4 + kk][1]);
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const uint32_t sl = reinterpret_cast<const uint32_t*>(k + kv4_code_bytes(D))[(b * 16 + l8 + 8 * h) * NG + g];
         const float sc = kv4_s(sl), z = fmaf(8.5f, sc, kv4_lo(sl));
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-          for (int c2 = 0; c2 < 2; ++c2) s[j][2 * h + c2] = fmaf(acc[j][2 * h + c2], sc, fmaf(qsum[j][g][c2], z, s[j][2 * h + c2]));
+        for (int c2 = 0; c2 < 2; ++c2) s[2 * h + c2] = fmaf(acc[2 * h + c2], sc, fmaf(qsum[g][c2], z, s[2 * h + c2]));
       }
     }
   } else {
@@ -211,59 +205,47 @@ __device__ __forceinline__ void block_scores(float (&s)[NT][4], const unsigned c
       const unsigned char* at = k + (chunk >> 3) * (kTile * 128u);
       const uint4 lo = *reinterpret_cast<const uint4*>(at + swz128(row, chunk & 7u)), hi = *reinterpret_cast<const uint4*>(at + swz128(row + 8, chunk & 7u));
       const uint32_t a0[4] = {lo.x, hi.x, lo.y, hi.y}, a1[4] = {lo.z, hi.z, lo.w, hi.w};
-#pragma unroll
-      for (int j = 0; j < NT; ++j) mma_bf16(s[j], a0, q[j].f[2 * x][0], q[j].f[2 * x][1]);
-#pragma unroll
-      for (int j = 0; j < NT; ++j) mma_bf16(s[j], a1, q[j].f[2 * x + 1][0], q[j].f[2 * x + 1][1]);
+      mma_bf16(s, a0, q.f[2 * x][0], q.f[2 * x][1]);
+      mma_bf16(s, a1, q.f[2 * x + 1][0], q.f[2 * x + 1][1]);
     }
   }
 }
 
 // Adds the unit's rows to sum[b][h] (MMA rows l8 and l8 + 8 of block b, this lane's columns).  id and off: request and
-// -lse in log2 units of rows lane and lane + 32 (-inf: no such row).  Sixteen rows share a walk over K (a walk's
-// reads of shared memory, 16 KB, are what it costs); the first are asked for before K has come, the next before
-// these are worked on.
+// -lse in log2 units of rows lane and lane + 32 (-inf: no such row).  Eight rows share a walk over K; the first are asked
+// for before K has come, the next before these are worked on.
 template <int D, bool k4, typename Arrived>
 __device__ __forceinline__ bool walk_rows(const Params& p, const unsigned char* k, const int (&id)[2], const float (&off)[2], int rows, int kvh,
                                           int lane, float (&sum)[4][2], Arrived&& arrived) {
   constexpr int NG = D / kGroup4;
   const int l4 = lane & 3, l8 = lane >> 2;
-  constexpr int NT = 1;
-  auto load = [&](QueryRows<D> (&q)[NT], int row0) {
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      const int row = row0 + 8 * j + l8;
-      const int req = __shfl_sync(0xffffffffu, row0 < 32 ? id[0] : id[1], row & 31);
-      q[j].load(p.q + ((size_t)req * p.num_q_heads + kvh * p.gqa + (row & (p.gqa - 1))) * D, row < rows, l4);
-    }
+  auto load = [&](QueryRows<D>& q, int row0) {
+    const int row = row0 + l8;
+    const int req = __shfl_sync(0xffffffffu, row0 < 32 ? id[0] : id[1], row & 31);
+    q.load(p.q + ((size_t)req * p.num_q_heads + kvh * p.gqa + (row & (p.gqa - 1))) * D, row < rows, l4);
   };
-  QueryRows<D> q[NT];
+  QueryRows<D> q;
   auto walk = [&](int row0) {
-    float o[NT][2], qsum[NT][NG][2];
+    float o[2], qsum[NG][2];
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
+    for (int c = 0; c < 2; ++c) o[c] = __shfl_sync(0xffffffffu, row0 < 32 ? off[0] : off[1], (row0 + l4 * 2 + c) & 31);
+    if (k4) {
 #pragma unroll
-      for (int c = 0; c < 2; ++c) o[j][c] = __shfl_sync(0xffffffffu, row0 < 32 ? off[0] : off[1], (row0 + 8 * j + l4 * 2 + c) & 31);
-      if (k4) {
+      for (int x = 0; x < NG; ++x) {
+        const uint32_t ones[4] = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+        float acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int x = 0; x < NG; ++x) {
-          const uint32_t ones[4] = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
-          float acc[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int kk = 0; kk < 4; ++kk) mma_bf16(acc, ones, q[j].f[x * 4 + kk][0], q[j].f[x * 4 + kk][1]);
-          qsum[j][x][0] = acc[0];
-          qsum[j][x][1] = acc[1];
-        }
+        for (int kk = 0; kk < 4; ++kk) mma_bf16(acc, ones, q.f[x * 4 + kk][0], q.f[x * 4 + kk][1]);
+        qsum[x][0] = acc[0];
+        qsum[x][1] = acc[1];
       }
     }
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
-      float s[NT][4];
-      block_scores<D, k4, NT>(s, k, b, q, qsum, lane);
+      float s[4];
+      block_scores<D, k4>(s, k, b, q, qsum, lane);
 #pragma unroll
-      for (int j = 0; j < NT; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum[b][e >> 1] += fast_exp2(fmaf(s[j][e], p.scale_log2, o[j][e & 1]));
+      for (int e = 0; e < 4; ++e) sum[b][e >> 1] += fast_exp2(fmaf(s[e], p.scale_log2, o[e & 1]));
     }
   };
   load(q, 0);
@@ -271,13 +253,12 @@ __device__ __forceinline__ bool walk_rows(const Params& p, const unsigned char* 
 #pragma unroll 1
   for (int row0 = 0;;) {
     const int left = rows - row0;
-    QueryRows<D> next[NT];
-    if (left > 8 * NT) load(next, row0 + 8 * NT);
+    QueryRows<D> next;
+    if (left > 8) load(next, row0 + 8);
     walk(row0);
-    if (left <= 8 * NT) return true;
-#pragma unroll
-    for (int j = 0; j < NT; ++j) q[j] = next[j];
-    row0 += 8 * NT;
+    if (left <= 8) return true;
+    q = next;
+    row0 += 8;
   }
 }
 
@@ -716,15 +697,12 @@ __device__ __forceinline__ void sum_weights(Smem& sm, const Params& p, int warp,
         mbar_arrive(&sm.q_empty[slot]);
       }
     }
-    const int first = item;
     item = end;
     float lo, hi;
     f2_unpack(f2_add(f2_add(part[0], part[1]), f2_add(part[2], part[3])), lo, hi);
     float sum = lo + hi;
-    // one item: its group writes; more: group 1 hands its sums to group 0
-    if (u.items == 1) {
-      if ((first & 1) != group) return true;
-    } else if (group == 1) {
+    static_assert(kNarrowRows >= kItemRows, "a unit has two items or more, some of either group");
+    if (group == 1) {  // hands its sums to group 0
       if (handed > 0 && !wait(&sm.handed_empty, handed - 1, p)) return false;
       sm.handed[token] = sum;
       __syncwarp();
