@@ -25,6 +25,8 @@
  *     gf_path_attention_decode and gf_path_attention_extend only enqueue work.  gf_build_path_tables enqueues its kernels and then
  *     waits on the stream once, to read back four table sizes and the
  *     validation result.
+ *   - A call that enqueues work makes the device that the pool lies on current meanwhile and puts the caller's
+ *     back; `stream` belongs to that device.
  *   - Argument errors are detected on the host before anything is launched.
  *   - One handle is used from one host thread at a time.
  *   - bf16 everywhere for K, V, Q and the output (a node's state may be held in 4 bits instead, see
@@ -406,8 +408,8 @@ gf_status_t gf_path_attention_decode(gf_wgraph_t* g, const gf_tables_t* t, int32
  *     (gf_workspace_bytes, partials included): gf_build_path_tables lays out the same tables either
  *     way, this entry point only does not use the partials' part of it.
  *   - Calls no cudaMalloc / cudaFree or other allocating routine.  The first call on each device
- *     looks up the array's device address (cudaGetSymbolAddress, with the caller's current device,
- *     which must be the one that owns the pool); make that first call outside any stream capture.
+ *     looks up the array's device address (cudaGetSymbolAddress); make that first call outside any
+ *     stream capture.
  *   - The array is shared by every handle and every call on that GPU and keeps the previous call's
  *     contents.  Nothing in it has to start at zero: each launch overwrites every partial it later
  *     reads.  Two calls whose kernels overlap on the GPU (different streams, no ordering) race on

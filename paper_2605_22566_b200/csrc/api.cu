@@ -94,7 +94,7 @@ struct gf_wgraph {
   TilePool tiles4;
   std::vector<uint8_t> node_kv4;  // 1: the node's extent lies in the 4-bit pool
   int32_t kv4_nodes = 0;          // how many such nodes exist
-  int device = 0;                 // the device the handle was created on
+  int device = 0;                 // the device that the pool lies on
   char* ws = nullptr;
   size_t ws_bytes = 0;
   size_t ws_graph_end = 0;  // tables are carved after this offset
@@ -406,11 +406,11 @@ gf_status_t gf_wgraph_create(const gf_wgraph_desc_t* d, gf_wgraph_t** out) {
   g->node_kv4.assign(d->num_nodes, 0);
   for (int r = d->max_residual_nodes - 1; r >= 0; --r) g->free_res_rows.push_back(r);
   {
-    int dev = 0, sms = 0;
-    if (cudaGetDevice(&dev) == cudaSuccess) g->device = dev;
-    if (cudaGetDevice(&dev) == cudaSuccess &&
-        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && sms > 0)
-      g->num_sms = sms;
+    int sms = 0;
+    cudaPointerAttributes pool{};
+    g->device = cudaPointerGetAttributes(&pool, d->kv_pool_dev) == cudaSuccess ? pool.device : -1;
+    if (g->device < 0 || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, g->device) != cudaSuccess || sms <= 0) { delete g; return GF_ERR_CUDA; }
+    g->num_sms = sms;
   }
   g->tables.owner = g;
   *out = g;
@@ -460,6 +460,8 @@ gf_status_t gf_node_kv_write(gf_wgraph_t* g, int32_t node, int32_t layer, const 
   if (n_tokens > 0 && (!k_dev || !v_dev || ((uintptr_t)k_dev & 15) || ((uintptr_t)v_dev & 15)))
     return GF_ERR_INVALID_ARG;
   cudaStream_t st = (cudaStream_t)stream;
+  DeviceGuard dev(g->device);
+  if (!dev.ok) return GF_ERR_CUDA;
   bool fresh = false;
   const gf_status_t rs = reserve_extent(g, node, n_tokens, &fresh);
   if (rs != GF_OK) return rs;
@@ -479,6 +481,8 @@ gf_status_t gf_node_kv_write(gf_wgraph_t* g, int32_t node, int32_t layer, const 
 
 gf_status_t gf_node_kv_reserve(gf_wgraph_t* g, int32_t node, int32_t n_tokens, void* stream) {
   if (!g || node < 0 || node >= g->desc.num_nodes || n_tokens < 0) return GF_ERR_INVALID_ARG;
+  DeviceGuard dev(g->device);
+  if (!dev.ok) return GF_ERR_CUDA;
   bool fresh = false;
   const gf_status_t rs = reserve_extent(g, node, n_tokens, &fresh);
   if (rs != GF_OK) return rs;
@@ -494,6 +498,8 @@ gf_status_t gf_node_kv_release(gf_wgraph_t* g, int32_t node, void* stream) {
   if (!g || node < 0 || node >= g->desc.num_nodes) return GF_ERR_INVALID_ARG;
   if (g->node_len[node] < 0) return GF_ERR_NOT_WRITTEN;
   if (g->variants_of[node] > 0) return GF_ERR_INVALID_ARG;  // states kept as this node's tiles + residual still exist
+  DeviceGuard dev(g->device);
+  if (!dev.ok) return GF_ERR_CUDA;
   cudaStream_t st = (cudaStream_t)stream;
   if (g->node_base[node] >= 0) {
     // a state kept as base + residual owns no tiles: only its row of the residual table comes back
@@ -545,9 +551,9 @@ gf_status_t gf_node_kv_read(gf_wgraph_t* g, int32_t node, int32_t layer, void* k
   const int n_tokens = g->node_len[node];
   if (n_tokens > 0 && (!k_out_dev || !v_out_dev || ((uintptr_t)k_out_dev & 15) || ((uintptr_t)v_out_dev & 15)))
     return GF_ERR_INVALID_ARG;
+  DeviceGuard dev(g->device);
+  if (!dev.ok) return GF_ERR_CUDA;
   if (g->node_kv4[node]) {
-    DeviceGuard dev(g->device);
-    if (!dev.ok) return GF_ERR_CUDA;
     const int m = launch_kv4_read(g->pool4, layer, g->desc.num_kv_heads, g->desc.head_dim, tile_in_pool(g, node), k_out_dev,
                                   v_out_dev, n_tokens, g->num_sms, (cudaStream_t)stream);
     if (m < 0) return GF_ERR_CUDA;
@@ -578,6 +584,8 @@ gf_status_t gf_node_kv_reconstruct(gf_wgraph_t* g, int32_t node, int32_t layer, 
   const int n_tokens = g->node_len[base_node];
   if (((int64_t)n_tokens + kTile) * g->desc.num_kv_heads > 0x7fffffff) return GF_ERR_INVALID_ARG;  // rows are indexed with int32
   cudaStream_t st = (cudaStream_t)stream;
+  DeviceGuard dev(g->device);
+  if (!dev.ok) return GF_ERR_CUDA;
   bool fresh = false;
   const gf_status_t rs = reserve_extent(g, node, n_tokens, &fresh);
   if (rs != GF_OK) return rs;
@@ -604,6 +612,8 @@ gf_status_t gf_node_kv_attach_residual(gf_wgraph_t* g, int32_t node, int32_t lay
   if (g->node_kv4[base_node]) return GF_ERR_INVALID_ARG;        // and hold them in bf16
   const int n_tokens = g->node_len[base_node];
   if ((int64_t)n_tokens * g->desc.num_kv_heads > 0x7fffffff) return GF_ERR_INVALID_ARG;  // rows are indexed with int32
+  DeviceGuard dev(g->device);
+  if (!dev.ok) return GF_ERR_CUDA;
   cudaStream_t st = (cudaStream_t)stream;
   if (g->node_len[node] < 0) {
     if (g->free_res_rows.empty()) return GF_ERR_CAPACITY;
@@ -653,6 +663,8 @@ gf_status_t gf_residual_encode(gf_wgraph_t* g, int32_t base_node, int32_t layer,
   if (g->node_kv4[base_node]) return GF_ERR_INVALID_ARG;  // the base must be held in bf16
   const int n_tokens = g->node_len[base_node];
   if ((int64_t)n_tokens * g->desc.num_kv_heads > 0x7fffffff) return GF_ERR_INVALID_ARG;  // rows are indexed with int32
+  DeviceGuard dev(g->device);
+  if (!dev.ok) return GF_ERR_CUDA;
   int n = launch_residual_encode(g->pool, layer, g->desc.num_kv_heads, g->desc.head_dim,
                                  g->node_off[base_node] / kTile, k_full_dev, v_full_dev, n_tokens, threshold,
                                  k_out, v_out, g->status_dev, (cudaStream_t)stream);
@@ -667,6 +679,8 @@ gf_status_t gf_transition_counts(gf_wgraph_t* g, int32_t num_requests, int32_t n
   if (!g || num_requests < 0 || num_path_nodes < 0 || !misses_dev || (g->desc.num_edges > 0 && !counts_dev) ||
       (num_requests > 0 && (!path_ptr_dev || !path_node_dev)) || ((uintptr_t)misses_dev & 7))
     return GF_ERR_INVALID_ARG;
+  DeviceGuard dev(g->device);
+  if (!dev.ok) return GF_ERR_CUDA;
   int n = launch_transition_counts(g->gd, g->desc.num_edges, num_requests, num_path_nodes, path_ptr_dev,
                                    path_node_dev, counts_dev, (unsigned long long*)misses_dev, (cudaStream_t)stream);
   if (n < 0) return GF_ERR_CUDA;
@@ -678,6 +692,8 @@ gf_status_t gf_select_transitions(gf_wgraph_t* g, const int32_t* counts_dev, int
                                   uint8_t* keep_dev, uint64_t* totals_dev, void* stream) {
   if (!g || !totals_dev || ((uintptr_t)totals_dev & 7) || (g->desc.num_edges > 0 && (!counts_dev || !keep_dev)))
     return GF_ERR_INVALID_ARG;
+  DeviceGuard dev(g->device);
+  if (!dev.ok) return GF_ERR_CUDA;
   int n = launch_select_transitions(counts_dev, g->desc.num_edges, min_count, keep_dev,
                                     (unsigned long long*)totals_dev, (cudaStream_t)stream);
   if (n < 0) return GF_ERR_CUDA;
@@ -775,6 +791,8 @@ gf_status_t gf_build_path_tables(gf_wgraph_t* g, int32_t num_requests, int32_t n
   if (!policy_ok(pol, gqa)) return GF_ERR_INVALID_ARG;
   cudaStream_t st = (cudaStream_t)stream;
 
+  DeviceGuard dev(g->device);
+  if (!dev.ok) return GF_ERR_CUDA;
   gf_tables& T = g->tables;
   T.built = false;
   T.bad_req = -1;
@@ -1057,6 +1075,8 @@ gf_status_t gf_path_attention_decode(gf_wgraph_t* g, const gf_tables_t* t, int32
                                      const void* q_dev, void* out_dev, float* lse_dev, void* stream) {
   gf_status_t s = check_attention_args(g, t, layer, q_dev, out_dev, GF_MODE_DECODE);
   if (s != GF_OK) return s;
+  DeviceGuard dev(g->device);
+  if (!dev.ok) return GF_ERR_CUDA;
   cudaStream_t st = (cudaStream_t)stream;
   bool joined = false;
   int n = timed(g, kSpanDecode, st, [&] { return launch_decode_kernels(g, t, t->dev, layer, q_dev, st, &joined); });
@@ -1072,6 +1092,8 @@ gf_status_t gf_path_attention_extend(gf_wgraph_t* g, const gf_tables_t* t, int32
                                      const void* q_dev, void* out_dev, float* lse_dev, void* stream) {
   gf_status_t s = check_attention_args(g, t, layer, q_dev, out_dev, GF_MODE_EXTEND);
   if (s != GF_OK) return s;
+  DeviceGuard dev(g->device);
+  if (!dev.ok) return GF_ERR_CUDA;
   cudaStream_t st = (cudaStream_t)stream;
   int n = timed(g, kSpanExtend, st, [&] {
     return launch_extend_tc(g->pool, g->shape, t->dev, layer, t->max_q_rows, t->info.num_q_rows, q_dev, nullptr, nullptr, out_dev, lse_dev,
@@ -1088,6 +1110,8 @@ gf_status_t gf_path_attention_extend_append(gf_wgraph_t* g, const gf_tables_t* t
   gf_status_t s = check_attention_args(g, t, layer, q_dev, out_dev, GF_MODE_EXTEND);
   if (s != GF_OK) return s;
   if (!k_new_dev || !v_new_dev || ((uintptr_t)k_new_dev & 15) || ((uintptr_t)v_new_dev & 15)) return GF_ERR_INVALID_ARG;
+  DeviceGuard dev(g->device);
+  if (!dev.ok) return GF_ERR_CUDA;
   cudaStream_t st = (cudaStream_t)stream;
   int n = timed(g, kSpanExtend, st, [&] {
     return launch_extend_tc(g->pool, g->shape, t->dev, layer, t->max_q_rows, t->info.num_q_rows, q_dev, k_new_dev, v_new_dev, out_dev,
@@ -1298,6 +1322,8 @@ gf_status_t gf_edge_scores(gf_wgraph_t* g, const gf_scorer_t* m, const float* x_
   for (int cand = num_tasks; cand >= 1; cand = cand > 1 ? (cand + 1) / 2 : 0)
     if ((uint64_t)edge_scores_scratch_floats(n, *m, num_tasks, cand) * 4 <= scratch_bytes) { per_pass = cand; break; }
   if (per_pass == 0) return GF_ERR_CAPACITY;
+  DeviceGuard dev(g->device);
+  if (!dev.ok) return GF_ERR_CUDA;
   const int k = launch_edge_scores(g->score_graph, *m, x_op_dev, num_tasks, x_task_dev, scores_dev, (float*)scratch_dev,
                                    per_pass, (cudaStream_t)stream);
   if (k < 0) return GF_ERR_CUDA;
@@ -1401,6 +1427,8 @@ extern "C" gf_status_t gf_path_attention_decode_static(gf_wgraph_t* g, const gf_
   gf_status_t s = check_attention_args(g, t, layer, q_dev, out_dev, GF_MODE_DECODE);
   if (s != GF_OK) return s;
   if (t->pending && (s = finalize_tables(t)) != GF_OK) return s;
+  DeviceGuard dev(g->device);
+  if (!dev.ok) return GF_ERR_CUDA;
   const size_t ml_bytes = align_up((size_t)t->info.num_slots * g->shape.num_q_heads * 2 * 4, 256);
   const size_t o_bytes = (size_t)t->info.num_slots * g->shape.num_q_heads * g->shape.head_dim * 4;
   if (ml_bytes + o_bytes > kStaticScratchBytes) return GF_ERR_CAPACITY;
