@@ -70,6 +70,21 @@ def test_weights_every_head_layout_and_odd_lengths(hq, hkv, d, four):
     pa.close()
 
 
+@pytest.mark.parametrize("requests", [5, 40])
+@pytest.mark.parametrize("four", [[], [0, 2]])
+def test_weights_of_a_later_layer_leave_the_others(requests, four):
+    w = random_case(8, 2, 128, requests, lens=[300, 40, 129, 64], shared=0, layers=3)
+    pa = _handle(w, four)
+    weights = pa.new_weights()
+    weights.fill_(0.5)
+    for layer in (2, 1):
+        lse, ref = _reference(w, four, layer)
+        pa.attention_weights(layer, pa.make_q(layer, "host"), torch.from_numpy(lse.astype(np.float32)).cuda(), weights, accumulate=False)
+        _check_weights(pa, weights, ref, layer, untouched=0.5)
+    assert bool((weights[0] == 0.5).all())
+    pa.close()
+
+
 @pytest.mark.parametrize("requests", [1, 2, 40, 150])
 @pytest.mark.parametrize("four", [[], [0, 2]])
 def test_weights_of_widely_shared_nodes(requests, four):

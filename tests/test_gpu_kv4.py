@@ -423,6 +423,33 @@ def test_decode_a_token_whose_groups_lie_far_apart(requests, hkv, copies, gap, l
     pa.close()
 
 
+@pytest.mark.parametrize("requests,hkv,copies", [(1, 1, 1), (24, 1, 1), (24, 8, 40)])
+@pytest.mark.parametrize("gap", [-16, -6, 6, 16])
+def test_decode_queries_whose_groups_lie_apart_as_the_keys_do_the_other_way(requests, hkv, copies, gap):
+    """Both groups of 64 entries add scores of one size.  A query's entries are held to 2^-39 of its row's largest and a group's sum
+    of them to 2^-33: times keys 2^16 as large that is below 2^-16 of a score's terms, within the bound of
+    test_decode_lse_is_exact_to_fp32."""
+    d, n, gqa = 128, 150, 8
+    rng = np.random.default_rng(29)
+    k, v, q = rng.standard_normal((n, 1, 2, 64)), rng.standard_normal((n, 1, d)) / 4, rng.standard_normal((requests, gqa, 2, 64))
+    k[:, :, 1] *= 2.0 ** gap
+    q[:, :, 1] *= 2.0 ** -gap
+    k, v, q = (_bf16(np.repeat(x, hkv, 1)) for x in (k.reshape(n, 1, d), v, q.reshape(requests, gqa, d)))
+    path = list(range(copies))
+    pa = _handle(private_workload([n] * copies, [path] * requests, gqa * hkv, hkv, d), path)
+    for node in path:
+        pa.write_node(node, 0, _tensor(k), _tensor(v))
+    pa.build()
+    lse = torch.empty(requests, gqa * hkv, device="cuda")
+    out = pa.decode(0, _tensor(q), lse=lse).double().cpu().numpy()
+    kv = kv4.values(k), kv4.values(v)
+    ref, ref_lse = OA.decode([path] * requests, lambda _: kv, q, hkv)
+    assert pa.status() == 0
+    assert np.abs(lse.double().cpu().numpy() - ref_lse).max() <= 1.2e-4
+    assert_close(out, ref, "out")
+    pa.close()
+
+
 def test_a_node_behind_four_gigabytes_of_the_pool():
     """Every kernel that addresses the 4-bit pool, at byte offsets that 32 bits do not hold: write, read, decode, weights and
     eviction of a short node behind one of 60 million tokens."""
