@@ -185,7 +185,10 @@ gf_status_t gf_node_extent(const gf_wgraph_t* g, int32_t node, int32_t* n_tokens
  * magnitude where attention is to read them.
  * Such states live in a pool of their own, and paths name them like any other: one batch may mix both
  * kinds, shared as usual.  gf_path_attention_decode (and _static) computes with the values that the codes
- * stand for, without rounding them to bf16 first.  Extend mode takes no path through such a node
+ * stand for, without rounding them to bf16 first; an entry of a query is held to 2^-39 of its row's largest
+ * (with all its bits where it is within 2^31 of it), and a group's sum of them to 2^-33.  With such nodes the partials of
+ * a batch whose tables are deferred may be added in another order than with read-back ones, and the results
+ * differ in their last bits.  Extend mode takes no path through such a node
  * (GF_ERR_INVALID_PATH: read it back and write it to a bf16 node for that), and it cannot be the base of a
  * residual or of a reconstruction (GF_ERR_INVALID_ARG). */
 
@@ -387,7 +390,10 @@ gf_status_t gf_tables_export(const gf_tables_t* t, gf_tables_host_t* out_host); 
  * (segment chunk, group tile) item streams its K/V tiles once for the requests that share them
  * and writes per-request partial (o, m, l); a log-sum-exp merge then forms out.
  * q_dev/out_dev: [num_requests, num_q_heads, head_dim] bf16; lse_dev: optional fp32
- * [num_requests, num_q_heads] natural-log sum of exp of the scaled scores.  Asynchronous. */
+ * [num_requests, num_q_heads] natural-log sum of exp of the scaled scores.  Asynchronous.
+ * The partials and unit counters are the workspace's: two decode or extend calls of one handle whose kernels
+ * overlap on the GPU (two streams, two graphs replayed beside each other) race on them; order them.
+ * gf_path_attention_weights and the calls on single nodes use no workspace of their own. */
 gf_status_t gf_path_attention_decode(gf_wgraph_t* g, const gf_tables_t* t, int32_t layer,
                                      const void* q_dev, void* out_dev, float* lse_dev,
                                      void* stream);

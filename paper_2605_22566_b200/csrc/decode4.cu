@@ -12,17 +12,23 @@
 // a power of two per row (all eight bits of every entry down to 2^-31 of the row's largest), p s is fp16 times
 // one power of two per row and group, chosen with the softmax's reference; scores, sums, O and the terms without
 // codes are fp32.
+// What that rounding of p s costs: the codes that it multiplies are 0..15, not centred, which makes it count 2.2 times
+// as much as with c - 8 (over 2000 tokens of normal values 4.8e-4 of the output instead of 2.2e-4; p in bf16, as the
+// kernel for bf16 states has it, 1.5e-3; the output's own rounding to bf16 1.6e-3).  Centred operands would take 128 more
+// instructions per tile.
 //
 // Every warp is on its own: it takes units (an item's 16 query rows, or what is left of them) from a counter,
 // longest segments first, streams their tiles through a ring of its own in shared memory (bulk copies,
 // completion counted in bytes on mbarriers; the layout of kv4_device.cuh makes every operand load a
 // conflict-free 16 bytes per lane) and writes the partial.  The next unit is claimed while the current one
 // streams, a step of the claim (counter, list, item) per tile, so that none of its round trips is waited for.
-// 256 requests over 256 nodes, all in 4 bits: 98 us for the groups of 9..16 rows and 55 for the others, 27 of them beside
-// the first (one kernel that takes 16 rows for all: 154 us in all against 162 one after the other and 137
-// beside each other; one request over 57 000 tokens: 41 against 36; 1024 requests: 499 against 464).  A warp issues
-// an instruction every 4.5 to 6.5 cycles, a third of them waiting for results of fixed latency: registers, that is warps,
-// are what is short.  Unpacking takes 320 of the 1100 (8 rows) or 1300 (16) instructions of a tile.
+// 256 requests over 256 nodes, all in 4 bits, 133 us with the merge: 101 us for the groups of 9..16 rows, the others
+// (47 alone) mostly beside them on a second stream.
+// One kernel that takes 16 rows for all was slower: 154 us for that call then against 137, 41 against 36 for one request
+// over 57 000 tokens, 499 against 464 for 1024 requests.
+// The schedulers issue in 43 to 46 % of their cycles, with 8 and 11 warps per SM and a third of a warp's time in waits
+// for results of fixed latency: registers, that is warps, are what is short.  Unpacking takes 320 of the 1100 (8 rows)
+// or 1300 (16) instructions of a tile.
 // Units of up to 8 rows use one column block of the MMA and run twelve warps to an SM, the others eight: what 168 and
 // 255 registers per thread allow.  Chunks shared by 64 rows and more go to decode4_wide.cu where those fill the GPU.
 #include <stddef.h>
@@ -230,8 +236,8 @@ struct Warp4 {
   // when a score outgrew it by more than 2^8.  The second product's p s are fp16 times a power of two f per row and
   // group, chosen whenever the reference moves so that the row's largest p s so far stands at 2^2 or above (a move may
   // count what came before it half as large as it is); an s with which p s could pass fp16's range, or the first
-  // one that is not 0, makes it move too.  Rounding costs a token 2^-11 of its part at most, or 2^-27 of the row's
-  // largest p s.
+  // one that is not 0, makes it move too.  Rounding changes a token's p s by 2^-11 of it at most, or by 2^-27 of the
+  // row's largest p s, and what it adds to O by as much of p s c.
   __device__ __forceinline__ void accumulate(const uint64_t (&x)[4][NT][2], const char* part, int lane) {
     bool move = false;
 #pragma unroll

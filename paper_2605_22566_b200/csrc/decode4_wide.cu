@@ -6,8 +6,9 @@
 //   S_rt = sum over groups G of  q_rG . (s_tG (c_tG - 8))  +  (sum of q_rG) (lo_tG + 8.5 s_tG)
 // K's scales are part of the operand, exact in fp16 (the second term takes a few entries more, see sums_offset), so that a
 // score costs its thread one multiplication.  That needs a token's groups to be of about one size (see kNearGroups);
-// a tile with a token whose groups are not gets one S per group and two multiplications.  V's operand are the codes, fp16 subnormals c 2^-24 and 16 c 2^-24 (exact), with
-// one accumulator per group of 64 entries, because values of different tokens may lie any power of two apart:
+// a tile with a token whose groups are not gets one S per group and two multiplications.  V's operand are the codes, fp16
+// subnormals c 2^-24 and 16 c 2^-24 (exact), with one accumulator per group of 64 entries, because values of different
+// tokens may lie any power of two apart:
 //   O_rG = sum over tokens of  (p_rt s_tG) c_tG  +  sum of  p_rt (lo_tG + s_tG / 2)
 // A thread owns a query row: it takes the 32 scores of a step from tensor memory, exponentiates, applies the
 // tokens' scales (tables in shared memory, read as broadcasts), keeps l and the second term of O in fp32, and puts
@@ -21,12 +22,13 @@
 //   warp 9     one thread issues the MMAs  (warps 10 and 11 only complete the group whose registers are handed over)
 // Every wait is bounded; a warp whose wait gave up leaves its role, and so do the others.
 //
-// 1024 requests, 608 units of mostly 128 rows, 8776 tiles of 64 tokens: 132 us (the 16-row kernel takes 170 for the
-// same).  Bound by the latency of one softmax warp per scheduler and CTA, two CTAs being what tensor memory holds, and by
-// shared memory: the scales' broadcasts, four wavefronts for 16 bytes, cost 600 of a step's 2000 cycles, the MMAs'
-// operands 400.  Measured before: K as codes, its scales applied to the scores, 139 us; K as values rounded to fp16, 119,
-// but lse in fp32 lost bits to it; steps of a whole tile with one S, 155: an MMA or a commit costs its issuing thread
-// 60 cycles, and there they stood between two softmaxes.
+// 1024 requests, 608 units of mostly 128 rows, 8776 tiles of 64 tokens: 137 us (the 16-row kernel takes 170 for the
+// same), 4 of them since every tile is asked whether its groups lie apart.  The tensor pipe is busy 16 % of the time, the
+// schedulers issue in 44 % of their cycles.  Bound by the latency of one softmax warp per scheduler and CTA, two CTAs
+// being what tensor memory holds, and by shared memory: the scales' broadcasts, four wavefronts for 16 bytes, cost 600 of
+// a step's 2000 cycles, the MMAs' operands 400.  Measured on the way: K as codes, its scales applied to the scores, 7 us
+// more; K as values rounded to fp16, 13 less, but lse in fp32 lost bits to it; steps of a whole tile with one S, 23 more:
+// an MMA or a commit costs its issuing thread 60 cycles, and there they stood between two softmaxes.
 #include "kv4_device.cuh"
 #include "tc_device.cuh"
 
@@ -102,7 +104,9 @@ __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t phase, const Params
 // A pair of barriers that steps use in turn.
 __device__ __forceinline__ bool wait_step(uint64_t (&bar)[2], int step, const Params& p) { return wait(&bar[step & 1], (uint32_t)step >> 1, p); }
 // The term without codes, (sum of q_rG) (lo_tG + 8.5 s_tG), as more entries of the same product: two fp16 numbers hold 22
-// bits of either factor, so a group takes four entries, (qh, qh, ql, ql) times (zh, zl, zh, zl).  Rows of 16 entries
+// bits of either factor (the sum to 2^-33 of its row's largest entry, where that is coarser), which is a 2^-21 of the
+// term, of the size of the fp32 sum's own roundings; a group takes four entries, (qh, qh, ql, ql) times (zh, zl, zh, zl).
+// Rows of 16 entries
 // without a swizzle: eight rows of 16 bytes, twice, per 256 bytes; entries 8..15 stay zero.
 __device__ __forceinline__ uint32_t sums_offset(uint32_t row, uint32_t group) { return (row >> 3) * 256 + (row & 7) * 16 + group * 8; }
 __device__ __forceinline__ uint64_t sums_desc(uint32_t saddr) {  // lbo: 128 bytes to the next 8 entries, sbo: 256 to the next 8 rows
@@ -223,8 +227,8 @@ __device__ __forceinline__ void load_queries(Smem<D>& sm, const Params& p, const
 }
 
 // Block b (16 tokens) of a tile's K: s (c - 8), which eleven bits hold (eight of s, three of c - 8), times a power of two
-// that brings the token's largest value (or each group's, see kNearGroups) to 2^8..2^9; and lo + 8.5 s beside it.  1024 + c and 1024 + 16 c are fp16 patterns with
-// the code in their low bits.
+// that brings the token's largest value (or each group's, see kNearGroups) to 2^8..2^9; and lo + 8.5 s beside it.  1024 + c
+// and 1024 + 16 c are fp16 patterns with the code in their low bits.
 template <int D>
 __device__ __forceinline__ void expand_k(Smem<D>& sm, Scales& to, const char* part, int b, int lane) {
   constexpr int NG = D / kGroup4;

@@ -6,16 +6,17 @@
 //   k_select  one CTA per (entry, layer, head).  32-bit keys have the weights' order; the key of rank m is found from
 //             its top bits down, then one ordered pass writes the kept indices and carries the weights to the
 //             destination's slots.  The choice is a function of the weights alone: integer counts, and ranks from
-//             scans.  Up to kHeldTokens tokens the keys stay in registers and two bits cost a count over
-//             them (the search ends when nothing is left to decide); longer nodes are read five times, from L2, by
-//             a radix select of eight bits a pass.
+//             scans.  Up to kHeldTokens tokens, what a CTA's registers hold, the keys stay there and two bits cost a
+//             count over them (the search ends when nothing is left to decide); longer nodes are read five times,
+//             from L2, by a radix select of eight bits a pass, still by one CTA.
 //   k_gather  copies the kept rows, in the 4-bit layout by moving the codes of whole tokens (the values are
 //             not touched).  Rows of the last tile past the end become zeros, as every writer of the pools
 //             leaves them.
 //
 // Four nodes of 6000 to 8192 tokens, two layers of 8 heads of 128, half kept: chosen in 17 us (64 CTAs, bound by their
-// chain of sixteen counts; a radix select with counts in shared memory 30), copied in 32 us (146 MB, 4.6 TB/s).  300
-// tokens: 7 us in one launch.
+// chain of sixteen counts; a radix select with counts in shared memory 30), copied in 31 us (146 MB, 4.7 TB/s).  300
+// tokens: 7.5 us in one launch.  One node, half kept, chosen in 15 us with 8192 tokens, 34 with one more, 119 with 32 768 and
+// 600 with 131 072 (copied in 13, 13, 44 and 85): there a pass is 16 or 8 CTAs' walk over the weights.
 //
 // The destination is another node, so nothing is read after it was overwritten and both kernels spread over
 // everything at once.
@@ -27,8 +28,8 @@ namespace {
 constexpr int kSelectThreads = 512;
 constexpr int kHeldKeys = 16, kHeldTokens = kHeldKeys * kSelectThreads;  // keys a thread keeps
 // Up to so many kept tokens per entry, one round of two tiles, the CTA that chose the rows copies them too, which saves
-// a launch (120 of 300 tokens: 96 us instead of 107 for a call and what a program does around it; 255 of them: 93
-// instead of 90).
+// a launch (120 of 300 tokens: 12.3 us instead of 13.3, 128 in 4 bits 14.3 instead of 17.4).  More rounds would leave the
+// copy to a CTA per layer and head where a launch spreads it (255 of 300 tokens: 14.3 instead of 15.3 still).
 constexpr int kOneLaunch = 2 * kTile;
 constexpr int kGatherThreads = 256;  // 64 rows, 32 at a time, of eight 16-byte pieces
 

@@ -38,11 +38,13 @@ struct __align__(32) Item {
 };
 
 // Longest chunk of a segment held in 4 bits, in multiples of the policy's chunk_tokens: its kernel gives a chunk's
-// 16 query rows to one warp, which has to come to an end.  256 requests: 145 us with 2, 139 with 4, 137 with 8;
-// 1024 requests: 482, 461 and 460 (more partials against later ends; one kernel after the other, 163, 172 and 182).
+// 16 query rows to one warp, which has to come to an end.  256 requests: 140 us with 2, 133 with 4, 131 with 8;
+// 1024 requests: 488, 466 and 466; one request over 57 000 tokens 35 with any (more partials against later ends).  4 and 8
+// are the same within 2 %; of the two, 4 bounds a warp's longest unit at 1024 tokens.
 constexpr int kKv4ChunkMult = 4;
 // A chunk of such a segment goes 128 stacked query rows at a time to the tcgen05 kernel; where fewer rows than this
-// are left, to the kernels that take 16 (1024 requests: 464 us with 64, 467 with 128, 495 with 32).
+// are left, to the kernels that take 16 (1024 requests: 489 us with 32, 466 with 64, 462 with 128, which would leave
+// segments shared by 64 to 127 rows out altogether).
 constexpr int kKv4WideUnit = 128, kKv4WideRows = 64;
 // Length class of a chunk: the kernels take the longest first, so that no long one is begun when the others end.
 constexpr int kKv4Classes = 8;

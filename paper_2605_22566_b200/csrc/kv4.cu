@@ -2,8 +2,11 @@
 // codes stand for (k_kv4_read).  Format and layout: kv4_device.cuh.
 //
 // Both are streams: 2 bytes of bf16 per entry on one side, 0.5625 on the other, nothing reused.  32 768 tokens of 8 heads
-// of 128, 172 MB either way: read in 28.6 us (6.0 TB/s, bound by HBM), written in 46 us (3.7 TB/s, bound by the
-// instructions of the exact quotients, some 14 per entry; 113 us with divisions).  A short node costs its launch.  A warp works on one block of 16 tokens of one KV
+// of 128, 172 MB either way: read in 29 us (5.9 TB/s, bound by HBM), written in 48 us (3.6 TB/s; 113 us with divisions).
+// The write issues 31.8 M warp instructions, 15 per entry, which fill 66 % of its issue slots; in the rest its
+// 29 warps per SM (64 registers) wait for the rows of their next block, which are asked for when the one before is
+// coded.  A short node costs its launch.
+// A warp works on one block of 16 tokens of one KV
 // head and one group of 64 entries, K or V: 2 KB of bf16, 512 bytes of codes.  The layout gives every lane
 // 16-byte runs on both sides, so nothing goes through shared memory; a token's least and largest entry are
 // found with shuffles among the lanes that hold it.
