@@ -393,7 +393,7 @@ gf_status_t gf_tables_export(const gf_tables_t* t, gf_tables_host_t* out_host); 
  * [num_requests, num_q_heads] natural-log sum of exp of the scaled scores.  Asynchronous.
  * The partials and unit counters are the workspace's: two decode or extend calls of one handle whose kernels
  * overlap on the GPU (two streams, two graphs replayed beside each other) race on them; order them.
- * gf_path_attention_weights and the calls on single nodes use no workspace of their own. */
+ * gf_path_attention_weights reads the tables and uses neither partials nor counters. */
 gf_status_t gf_path_attention_decode(gf_wgraph_t* g, const gf_tables_t* t, int32_t layer,
                                      const void* q_dev, void* out_dev, float* lse_dev,
                                      void* stream);
