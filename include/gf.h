@@ -21,6 +21,8 @@
  *   - `stream` is a cudaStream_t passed as void* (NULL = default stream).
  *     gf_node_kv_write, gf_node_kv_read, gf_node_kv_reconstruct,
  *     gf_node_kv4_write, gf_path_attention_weights, gf_node_kv_evict,
+ *     gf_node_kv_open, gf_node_kv_close, gf_append_slots, gf_node_kv_append,
+ *     gf_adapter_project, gf_token_logprobs,
  *     gf_residual_encode, gf_transition_counts, gf_select_transitions,
  *     gf_path_attention_decode and gf_path_attention_extend only enqueue work.  gf_build_path_tables enqueues its kernels and then
  *     waits on the stream once, to read back four table sizes and the
@@ -175,6 +177,43 @@ gf_status_t gf_node_kv_release(gf_wgraph_t* g, int32_t node, void* stream);
 /* Length and pool offset (both in tokens; the offset is what seg_off reports) of a node's extent.
  * Either pointer may be NULL.  GF_ERR_NOT_WRITTEN for a node without an extent. */
 gf_status_t gf_node_extent(const gf_wgraph_t* g, int32_t node, int32_t* n_tokens_host, int32_t* token_offset_host);
+
+/* ---- nodes that grow ----------------------------------------------------------------------------------
+ * A request's own suffix gets longer with every token it generates.  An open node has room for a stated number
+ * of tokens and a length that lives on the device, where gf_append_slots moves it on and gf_build_path_tables
+ * reads it: a decode step is gf_append_slots, gf_build_path_tables (deferred), and per layer gf_node_kv_append and
+ * gf_path_attention_decode, with nothing waited for.  Paths name an open node like any other, extend takes it at its
+ * present length, and gf_node_kv_read and gf_node_extent take it at its room (rows that it does not hold yet read
+ * as zeros).  What needs a length on the host refuses it with GF_ERR_INVALID_ARG until gf_node_kv_close: the
+ * writes, gf_node_kv_reserve, residuals and reconstruction over it, eviction. */
+
+/* Opens an unwritten node (GF_ERR_INVALID_ARG for any other) with room for that many tokens, in bf16, holding none.
+ * Takes the tiles (first fit) and clears them in every layer.  GF_ERR_CAPACITY when no run of free tiles is long
+ * enough.  gf_node_kv_release gives the tiles back. */
+gf_status_t gf_node_kv_open(gf_wgraph_t* g, int32_t node, int32_t room, void* stream);
+
+/* Ends its growth: the node has n_tokens from here on, like a written one, and tiles beyond them are free again.
+ * n_tokens is what it holds; less drops the last tokens; more leaves zeros in the rows that it does not hold, and
+ * gf_last_status reports GF_ERR_INVALID_ARG. */
+gf_status_t gf_node_kv_close(gf_wgraph_t* g, int32_t node, int32_t n_tokens, void* stream);
+
+/* Where a batch's new tokens go.  Request r gets count_dev[r] tokens in the open node node_dev[r], behind the
+ * held_dev[r] that it holds (held_dev NULL: behind all that it holds; fewer than it holds takes the others back, as
+ * after drafted tokens that were not accepted: their rows are cleared in every layer).  New rows are request-major:
+ * slots_dev[i], [num_new], is the pool's token slot of row i, -1 for rows behind the last request's.  len_dev [num_requests],
+ * or NULL: the nodes' new lengths.  A request whose node is not open, whose held or count is negative, that
+ * holds more than its node, or whose rows pass num_new is left out: its slots and length are -1, its node is as it was,
+ * and gf_last_status reports GF_ERR_INVALID_ARG; GF_ERR_CAPACITY where the node has no room.  Two requests must not name the
+ * same node.  Built tables become stale; tables of a captured graph are built anew behind the call by its replay. */
+gf_status_t gf_append_slots(gf_wgraph_t* g, int32_t num_requests, const int32_t* node_dev, const int32_t* held_dev,
+                            const int32_t* count_dev, int32_t num_new, int32_t* slots_dev, int32_t* len_dev, void* stream);
+
+/* One layer's K and V rows of the new tokens to their slots.  k_dev, v_dev: bf16 rows of [num_kv_heads, head_dim], the rows
+ * k_stride and v_stride entries apart (multiples of 8, so that keys and values can be parts of a wider projection's
+ * rows), 16-byte aligned.  Rows with slot -1 are skipped; a slot beyond the bf16 pool is skipped and reported as
+ * GF_ERR_INVALID_ARG by gf_last_status. */
+gf_status_t gf_node_kv_append(gf_wgraph_t* g, int32_t layer, int32_t num_new, const int32_t* slots_dev, const void* k_dev, int64_t k_stride,
+                              const void* v_dev, int64_t v_stride, void* stream);
 
 /* ---- states held in 4 bits ------------------------------------------------------------------------
  * A node's state may be held in 4 bits instead of bf16: 64 neighbouring entries of one token and KV head
@@ -483,6 +522,54 @@ uint64_t gf_edge_scores_scratch_bytes(const gf_wgraph_t* g, const gf_scorer_t* m
 gf_status_t gf_edge_scores(gf_wgraph_t* g, const gf_scorer_t* model, const float* x_op_dev, int32_t num_tasks,
                            const float* x_task_dev, float* scores_dev, void* scratch_dev, uint64_t scratch_bytes,
                            void* stream);
+
+/* ---- what stands before and behind a step's attention ---------------------------------------------------
+ * A projection that all requests share, with a low-rank adapter of each request's own (the queries, keys and values of
+ * agents that run under adapters of their own, the output behind the attention, the logits at the end):
+ *   y[t] = W x[t] + scale[a] B[a] (A[a] x[t]),   a = adapter[t]; -1: no adapter.
+ * bf16 row-major, caller-owned, 16-byte aligned; A [num_adapters, rank, in_dim], B [num_adapters, out_dim, rank], contiguous;
+ * scale NULL: 1.  in_dim and w_stride (entries between rows of W) are multiples of 8; rank a multiple of 8, at most 64
+ * (adapters of a smaller rank are filled up with zeros); num_adapters 0: none. */
+typedef struct {
+  int32_t in_dim, out_dim;
+  const void* w_dev; /* [out_dim, in_dim] */
+  int64_t w_stride;
+  int32_t num_adapters, rank;
+  const void* a_dev;
+  const void* b_dev;
+  const float* scale_dev; /* fp32 [num_adapters] */
+} gf_projection_t;
+
+/* Scratch of a call with adapters: fp32, 16-byte aligned; two calls that may overlap on the GPU each need their own. */
+uint64_t gf_adapter_project_scratch_bytes(const gf_projection_t* p, int32_t rows);
+
+/* x_dev: bf16 [rows, in_dim], rows x_stride entries apart (a multiple of 8), 16-byte aligned.  adapter_dev: int32 [rows], or NULL for
+ * none at all; any value outside [-1, num_adapters) counts as -1 and gf_last_status reports GF_ERR_INVALID_ARG.  y_dev: bf16 or
+ * (y_fp32 1) fp32 [rows, out_dim], rows y_stride entries apart, not overlapping the inputs.  Sums are fp32 and rounded once; the
+ * order of additions is fixed for a given number of rows.  GF_ERR_CAPACITY when the scratch is too small.  Asynchronous. */
+gf_status_t gf_adapter_project(gf_wgraph_t* g, const gf_projection_t* p, int32_t rows, const void* x_dev, int64_t x_stride,
+                               const int32_t* adapter_dev, void* y_dev, int64_t y_stride, int32_t y_fp32, void* scratch_dev,
+                               uint64_t scratch_bytes, void* stream);
+
+/* What a step's logits say of its tokens, per row, natural logarithms, fp32; any pointer may be NULL:
+ *   lse = log sum exp x;  logprob = x[token] - lse;  entropy = sum p (lse - x), p = exp(x - lse), all from differences with the
+ *   largest logit, so that they hold their digits where the logits are large;
+ *   top_ids, top_logprobs [rows, top]: the tokens with the largest logits in descending order, ties to the lowest id. */
+#define GF_MAX_TOP 32
+typedef struct {
+  float* logprob_dev; /* [rows] */
+  float* entropy_dev; /* [rows] */
+  float* lse_dev;     /* [rows] */
+  int32_t* top_ids_dev;
+  float* top_logprobs_dev;
+} gf_logprobs_t;
+
+/* logits_dev: bf16 or (fp32 1) fp32 [rows, vocab], rows `stride` entries apart, any alignment.  tokens_dev: int32 [rows], -1: no token
+ * (logprob 0); any other value outside [0, vocab) gives NaN.  top: 0 .. GF_MAX_TOP, at most vocab.  A logit of minus
+ * infinity has no probability; a row of nothing else has lse and every log probability at minus infinity, entropy 0.  A
+ * row with a NaN or plus infinity gives NaN for all but the ids (a NaN ranks below everything).  Asynchronous. */
+gf_status_t gf_token_logprobs(gf_wgraph_t* g, int32_t rows, int32_t vocab, const void* logits_dev, int64_t stride, int32_t fp32,
+                              const int32_t* tokens_dev, int32_t top, const gf_logprobs_t* out, void* stream);
 
 /* Synchronises `stream` and returns what the kernels reported since the last call, then clears it:
  * GF_ERR_TIMEOUT if a bounded wait inside a kernel gave up (results of that launch are undefined;

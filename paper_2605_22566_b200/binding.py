@@ -24,6 +24,7 @@ GF_MODE_DECODE, GF_MODE_EXTEND = 0, 1
 GF_MODE_DEFERRED = 0x100
 GF_TILE_TOKENS = 64
 GF_STATIC_SCRATCH_BYTES = 32 << 20
+GF_MAX_TOP = 32
 
 EXPORTS = [
     "gf_status_string", "gf_pool_bytes_per_tile", "gf_workspace_bytes", "gf_wgraph_create",
@@ -35,6 +36,8 @@ EXPORTS = [
     "gf_node_kv_attach_residual", "gf_edge_scores", "gf_edge_scores_scratch_bytes",
     "gf_kv4_bytes_per_tile", "gf_kv4_pool_attach", "gf_kv4_pool_info", "gf_node_kv4_write", "gf_weight_slots",
     "gf_path_attention_weights", "gf_node_kv_evict",
+    "gf_node_kv_open", "gf_node_kv_close", "gf_append_slots", "gf_node_kv_append",
+    "gf_adapter_project", "gf_adapter_project_scratch_bytes", "gf_token_logprobs",
 ]
 
 
@@ -61,6 +64,16 @@ class Residual(C.Structure):
 class ResidualBuf(C.Structure):
     _fields_ = [("bitmap_dev", C.c_void_p), ("values_dev", C.c_void_p), ("row_ptr_dev", C.c_void_p),
                 ("capacity", C.c_int64), ("nnz_dev", C.c_void_p)]
+
+
+class ProjectionDesc(C.Structure):
+    _fields_ = [("in_dim", C.c_int32), ("out_dim", C.c_int32), ("w_dev", C.c_void_p), ("w_stride", C.c_int64),
+                ("num_adapters", C.c_int32), ("rank", C.c_int32), ("a_dev", C.c_void_p), ("b_dev", C.c_void_p), ("scale_dev", C.c_void_p)]
+
+
+class Logprobs(C.Structure):
+    _fields_ = [("logprob_dev", C.c_void_p), ("entropy_dev", C.c_void_p), ("lse_dev", C.c_void_p), ("top_ids_dev", C.c_void_p),
+                ("top_logprobs_dev", C.c_void_p)]
 
 
 class Policy(C.Structure):
@@ -171,6 +184,15 @@ def lib():
         L.gf_path_attention_weights.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32,
                                                 C.c_void_p, C.c_void_p]
         L.gf_node_kv_evict.argtypes = [C.c_void_p, C.POINTER(Evict), C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]
+        L.gf_node_kv_open.argtypes = L.gf_node_kv_close.argtypes = L.gf_node_kv_reserve.argtypes
+        L.gf_append_slots.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]
+        L.gf_node_kv_append.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]
+        L.gf_adapter_project_scratch_bytes.restype = C.c_uint64
+        L.gf_adapter_project_scratch_bytes.argtypes = [C.POINTER(ProjectionDesc), C.c_int32]
+        L.gf_adapter_project.argtypes = [C.c_void_p, C.POINTER(ProjectionDesc), C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64,
+                                         C.c_int32, C.c_void_p, C.c_uint64, C.c_void_p]
+        L.gf_token_logprobs.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_int32,
+                                        C.POINTER(Logprobs), C.c_void_p]
         L.gf_debug_bounds_enabled.restype = C.c_int32
         L.gf_debug_bounds_site.restype = C.c_int32
         L.gf_debug_bounds_site.argtypes = [C.c_void_p]
@@ -387,6 +409,36 @@ def gf_node_kv_evict(g, entries, weights_ptr, kept_ptr, stream=0) -> int:
     """entries: (node, src_node, keep, keep_first, keep_last) tuples."""
     arr = (Evict * max(len(entries), 1))(*[Evict(*e) for e in entries])
     return lib().gf_node_kv_evict(g, arr, len(entries), weights_ptr, kept_ptr, stream)
+
+
+def gf_node_kv_open(g, node, room, stream=0) -> int:
+    return lib().gf_node_kv_open(g, node, room, stream)
+
+
+def gf_node_kv_close(g, node, n_tokens, stream=0) -> int:
+    return lib().gf_node_kv_close(g, node, n_tokens, stream)
+
+
+def gf_append_slots(g, num_requests, node_ptr, held_ptr, count_ptr, num_new, slots_ptr, len_ptr=None, stream=0) -> int:
+    return lib().gf_append_slots(g, num_requests, node_ptr, held_ptr, count_ptr, num_new, slots_ptr, len_ptr, stream)
+
+
+def gf_node_kv_append(g, layer, num_new, slots_ptr, k_ptr, k_stride, v_ptr, v_stride, stream=0) -> int:
+    return lib().gf_node_kv_append(g, layer, num_new, slots_ptr, k_ptr, k_stride, v_ptr, v_stride, stream)
+
+
+def gf_adapter_project_scratch_bytes(projection: ProjectionDesc, rows) -> int:
+    return int(lib().gf_adapter_project_scratch_bytes(C.byref(projection), rows))
+
+
+def gf_adapter_project(g, projection: ProjectionDesc, rows, x_ptr, x_stride, adapter_ptr, y_ptr, y_stride, y_fp32, scratch_ptr=None,
+                       scratch_bytes=0, stream=0) -> int:
+    return lib().gf_adapter_project(g, C.byref(projection), rows, x_ptr, x_stride, adapter_ptr, y_ptr, y_stride, y_fp32, scratch_ptr,
+                                    scratch_bytes, stream)
+
+
+def gf_token_logprobs(g, rows, vocab, logits_ptr, stride, fp32, tokens_ptr, top, out: Logprobs, stream=0) -> int:
+    return lib().gf_token_logprobs(g, rows, vocab, logits_ptr, stride, fp32, tokens_ptr, top, C.byref(out), stream)
 
 
 def gf_edge_scores_scratch_bytes(g, scorer: Scorer, num_tasks: int, tasks_per_pass: int) -> int:

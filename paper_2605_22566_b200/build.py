@@ -20,7 +20,7 @@ GEN_PATH = os.path.join(HERE, "libgfgen.so")
 ARCH = ["-gencode", "arch=compute_100a,code=sm_100a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
 PATH_SOURCES = ["api.cu", "tables.cu", "kvpool.cu", "decode.cu", "extend_tc.cu", "pruning.cu", "residual_encode.cu", "debug.cu", "scoring.cu",
-                "kv4.cu", "decode4.cu", "decode4_wide.cu", "weights.cu", "evict.cu"]
+                "kv4.cu", "decode4.cu", "decode4_wide.cu", "weights.cu", "evict.cu", "append.cu", "project.cu", "logprobs.cu"]
 
 
 def _nvcc() -> str:

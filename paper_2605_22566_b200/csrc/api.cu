@@ -80,6 +80,7 @@ struct gf_wgraph {
   int32_t* status_dev = nullptr;
   std::vector<int32_t> node_len;  // -1 = never written
   std::vector<int32_t> node_off;
+  std::vector<uint8_t> node_open;   // 1: the node grows; node_len is the room of its extent, the device has its length
   // nodes whose state is kept as a base node's tiles plus a sparse residual (no extent of their own)
   std::vector<int32_t> node_base;   // base node, -1: an ordinary node
   std::vector<int32_t> node_res;    // row of the residual table, -1: none
@@ -142,6 +143,7 @@ size_t graph_region_bytes(int num_nodes, int num_shared, int num_edges, int resi
   size_t b = 0;
   b = align_up(b + (size_t)(num_shared + 1) * 4, 16);
   b = align_up(b + (size_t)(num_edges > 0 ? num_edges : 1) * 4, 16);
+  b = align_up(b + (size_t)num_nodes * 4, 16);
   b = align_up(b + (size_t)num_nodes * 4, 16);
   b = align_up(b + (size_t)num_nodes * 4, 16);
   b = align_up(b + (size_t)num_nodes * 4, 16);
@@ -350,6 +352,7 @@ gf_status_t gf_wgraph_create(const gf_wgraph_desc_t* d, gf_wgraph_t** out) {
   int32_t* adj_dst_dev = c.take<int32_t>(E > 0 ? E : 1);
   g->gd.node_len = c.take<int32_t>(d->num_nodes);
   g->gd.node_off = c.take<int32_t>(d->num_nodes);
+  g->gd.node_room = c.take<int32_t>(d->num_nodes);
   g->gd.node_res = c.take<int32_t>(d->num_nodes);
   g->res_table_dev = c.take<ResidualEntry>((size_t)d->max_residual_nodes * d->num_layers);
   // the task-conditioned graph of the scoring model (Sec. 4.1): operation edges in both directions,
@@ -395,11 +398,13 @@ gf_status_t gf_wgraph_create(const gf_wgraph_desc_t* d, gf_wgraph_t** out) {
   g->score_graph = ScoreGraphDev{sym_ptr_dev, sym_idx_dev, inv_sqrt_dev, e_src_dev, adj_dst_dev, NS, E};
   ok = ok && cudaMemset(g->gd.node_len, 0xFF, (size_t)d->num_nodes * 4) == cudaSuccess;
   ok = ok && cudaMemset(g->gd.node_off, 0xFF, (size_t)d->num_nodes * 4) == cudaSuccess;
+  ok = ok && cudaMemset(g->gd.node_room, 0xFF, (size_t)d->num_nodes * 4) == cudaSuccess;
   ok = ok && cudaMemset(g->gd.node_res, 0xFF, (size_t)d->num_nodes * 4) == cudaSuccess;
   ok = ok && cudaMemset(g->status_dev, 0, kStatusWords * 4) == cudaSuccess;
   if (!ok) { delete g; return GF_ERR_CUDA; }
   g->node_len.assign(d->num_nodes, -1);
   g->node_off.assign(d->num_nodes, -1);
+  g->node_open.assign(d->num_nodes, 0);
   g->node_base.assign(d->num_nodes, -1);
   g->node_res.assign(d->num_nodes, -1);
   g->variants_of.assign(d->num_nodes, 0);
@@ -442,6 +447,7 @@ static gf_status_t reserve_extent(gf_wgraph* g, int32_t node, int32_t n_tokens, 
   *fresh = false;
   if (g->node_base[node] >= 0) return GF_ERR_INVALID_ARG;  // kept as base + residual: it has no extent to write
   if (g->node_kv4[node]) return GF_ERR_INVALID_ARG;         // held in 4 bits
+  if (g->node_open[node]) return GF_ERR_INVALID_ARG;        // its rows come by gf_node_kv_append
   if (g->node_len[node] >= 0) return g->node_len[node] == n_tokens ? GF_OK : GF_ERR_INVALID_ARG;
   uint32_t first = 0;
   if (!g->tiles.take((uint32_t)((n_tokens + kTile - 1) / kTile), &first)) return GF_ERR_CAPACITY;
@@ -520,6 +526,7 @@ gf_status_t gf_node_kv_release(gf_wgraph_t* g, int32_t node, void* stream) {
   }
   g->node_len[node] = -1;
   g->node_off[node] = -1;
+  g->node_open[node] = 0;
   g->generation++;  // built tables may name the node: stale
   const int n = launch_graph_set_node(g->gd, node, -1, -1, st);
   if (n < 0) return GF_ERR_CUDA;
@@ -567,6 +574,73 @@ gf_status_t gf_node_kv_read(gf_wgraph_t* g, int32_t node, int32_t layer, void* k
   return GF_OK;
 }
 
+gf_status_t gf_node_kv_open(gf_wgraph_t* g, int32_t node, int32_t room, void* stream) {
+  if (!g || node < 0 || node >= g->desc.num_nodes || room < 0 || g->node_len[node] >= 0) return GF_ERR_INVALID_ARG;
+  DeviceGuard dev(g->device);
+  if (!dev.ok) return GF_ERR_CUDA;
+  cudaStream_t st = (cudaStream_t)stream;
+  uint32_t first = 0;
+  const uint32_t tiles = (uint32_t)(((int64_t)room + kTile - 1) / kTile);
+  if (!g->tiles.take(tiles, &first)) return GF_ERR_CAPACITY;
+  g->node_len[node] = room;
+  g->node_off[node] = (int32_t)(first * kTile);
+  g->node_open[node] = 1;
+  g->generation++;
+  const int n = launch_clear_extent(g->pool, g->desc.num_layers, g->desc.num_kv_heads, (int)first, (int)tiles, st);
+  const int m = launch_graph_set_node(g->gd, node, 0, g->node_off[node], st, room);
+  if (n < 0 || m < 0) return GF_ERR_CUDA;
+  g->launches += n + m;
+  return GF_OK;
+}
+
+gf_status_t gf_node_kv_close(gf_wgraph_t* g, int32_t node, int32_t n_tokens, void* stream) {
+  if (!g || node < 0 || node >= g->desc.num_nodes || !g->node_open[node] || n_tokens < 0 || n_tokens > g->node_len[node])
+    return GF_ERR_INVALID_ARG;
+  DeviceGuard dev(g->device);
+  if (!dev.ok) return GF_ERR_CUDA;
+  const int n = launch_close_node(g->gd, g->pool, g->desc.num_layers, g->desc.num_kv_heads, g->desc.head_dim, node, n_tokens,
+                                  g->status_dev, (cudaStream_t)stream);
+  if (n < 0) return GF_ERR_CUDA;
+  g->launches += n;
+  const int32_t had = (int32_t)(((int64_t)g->node_len[node] + kTile - 1) / kTile), need = (int32_t)(((int64_t)n_tokens + kTile - 1) / kTile);
+  g->tiles.give((uint32_t)(g->node_off[node] / kTile + need), (uint32_t)(had - need));
+  g->node_len[node] = n_tokens;
+  g->node_open[node] = 0;
+  g->generation++;
+  return GF_OK;
+}
+
+gf_status_t gf_append_slots(gf_wgraph_t* g, int32_t num_requests, const int32_t* node_dev, const int32_t* held_dev,
+                            const int32_t* count_dev, int32_t num_new, int32_t* slots_dev, int32_t* len_dev, void* stream) {
+  if (!g || num_requests < 0 || num_new < 0 || (num_requests > 0 && (!node_dev || !count_dev)) || (num_new > 0 && !slots_dev) ||
+      (((uintptr_t)node_dev | (uintptr_t)held_dev | (uintptr_t)count_dev | (uintptr_t)slots_dev | (uintptr_t)len_dev) & 3))
+    return GF_ERR_INVALID_ARG;
+  if (num_requests == 0 && num_new == 0) return GF_OK;
+  DeviceGuard dev(g->device);
+  if (!dev.ok) return GF_ERR_CUDA;
+  g->generation++;  // lengths change: built tables are stale
+  const int n = launch_append_slots(g->gd, g->pool, g->desc.num_layers, g->desc.num_kv_heads, g->desc.head_dim, num_requests, node_dev, held_dev,
+                                    count_dev, num_new, slots_dev, len_dev, g->status_dev, (cudaStream_t)stream);
+  if (n < 0) return GF_ERR_CUDA;
+  g->launches += n;
+  return GF_OK;
+}
+
+gf_status_t gf_node_kv_append(gf_wgraph_t* g, int32_t layer, int32_t num_new, const int32_t* slots_dev, const void* k_dev, int64_t k_stride,
+                              const void* v_dev, int64_t v_stride, void* stream) {
+  if (!g || layer < 0 || layer >= g->desc.num_layers || num_new < 0 || k_stride < 0 || v_stride < 0 || ((k_stride | v_stride) & 7))
+    return GF_ERR_INVALID_ARG;
+  if (num_new == 0) return GF_OK;
+  if (!slots_dev || !k_dev || !v_dev || ((uintptr_t)slots_dev & 3) || (((uintptr_t)k_dev | (uintptr_t)v_dev) & 15)) return GF_ERR_INVALID_ARG;
+  DeviceGuard dev(g->device);
+  if (!dev.ok) return GF_ERR_CUDA;
+  const int n = launch_kv_append(g->pool, layer, g->desc.num_kv_heads, g->desc.head_dim, num_new, slots_dev, k_dev, k_stride, v_dev, v_stride,
+                                 g->num_sms, g->status_dev, (cudaStream_t)stream);
+  if (n < 0) return GF_ERR_CUDA;
+  g->launches += n;
+  return GF_OK;
+}
+
 static bool residual_ok(const gf_residual_t* r) {
   if (!r) return true;
   if (r->nnz < 0 || r->nnz > 0x7fffffff || !r->bitmap_dev || !r->row_ptr_dev || (r->nnz > 0 && !r->values_dev)) return false;
@@ -580,7 +654,7 @@ gf_status_t gf_node_kv_reconstruct(gf_wgraph_t* g, int32_t node, int32_t layer, 
       node == base_node || layer < 0 || layer >= g->desc.num_layers || !residual_ok(k_res) || !residual_ok(v_res))
     return GF_ERR_INVALID_ARG;
   if (g->node_len[base_node] < 0) return GF_ERR_NOT_WRITTEN;
-  if (g->node_kv4[base_node]) return GF_ERR_INVALID_ARG;  // the base must be held in bf16
+  if (g->node_kv4[base_node] || g->node_open[base_node]) return GF_ERR_INVALID_ARG;  // the base must be held in bf16 and have its length
   const int n_tokens = g->node_len[base_node];
   if (((int64_t)n_tokens + kTile) * g->desc.num_kv_heads > 0x7fffffff) return GF_ERR_INVALID_ARG;  // rows are indexed with int32
   cudaStream_t st = (cudaStream_t)stream;
@@ -609,7 +683,7 @@ gf_status_t gf_node_kv_attach_residual(gf_wgraph_t* g, int32_t node, int32_t lay
     return GF_ERR_INVALID_ARG;
   if (g->node_len[base_node] < 0) return GF_ERR_NOT_WRITTEN;
   if (g->node_base[base_node] >= 0) return GF_ERR_INVALID_ARG;  // the base must own its tiles
-  if (g->node_kv4[base_node]) return GF_ERR_INVALID_ARG;        // and hold them in bf16
+  if (g->node_kv4[base_node] || g->node_open[base_node]) return GF_ERR_INVALID_ARG;  // hold them in bf16 and have its length
   const int n_tokens = g->node_len[base_node];
   if ((int64_t)n_tokens * g->desc.num_kv_heads > 0x7fffffff) return GF_ERR_INVALID_ARG;  // rows are indexed with int32
   DeviceGuard dev(g->device);
@@ -660,7 +734,7 @@ gf_status_t gf_residual_encode(gf_wgraph_t* g, int32_t base_node, int32_t layer,
       !(threshold >= 0.f) || !residual_buf_ok(k_out, k_full_dev) || !residual_buf_ok(v_out, v_full_dev))
     return GF_ERR_INVALID_ARG;
   if (g->node_len[base_node] < 0) return GF_ERR_NOT_WRITTEN;
-  if (g->node_kv4[base_node]) return GF_ERR_INVALID_ARG;  // the base must be held in bf16
+  if (g->node_kv4[base_node] || g->node_open[base_node]) return GF_ERR_INVALID_ARG;  // the base must be held in bf16 and have its length
   const int n_tokens = g->node_len[base_node];
   if ((int64_t)n_tokens * g->desc.num_kv_heads > 0x7fffffff) return GF_ERR_INVALID_ARG;  // rows are indexed with int32
   DeviceGuard dev(g->device);
@@ -1238,6 +1312,7 @@ gf_status_t gf_node_kv_evict(gf_wgraph_t* g, const gf_evict_t* list, int32_t cou
       return GF_ERR_INVALID_ARG;
     if (g->node_len[e.src_node] < 0) return GF_ERR_NOT_WRITTEN;
     if (g->node_base[e.src_node] >= 0 || g->node_base[e.node] >= 0) return GF_ERR_INVALID_ARG;  // no tiles of their own
+    if (g->node_open[e.src_node] || g->node_open[e.node]) return GF_ERR_INVALID_ARG;            // no length yet
     const int32_t m = std::min(e.keep, g->node_len[e.src_node]);
     if (g->node_len[e.node] >= 0 && (g->node_len[e.node] != m || g->node_kv4[e.node] != g->node_kv4[e.src_node])) return GF_ERR_INVALID_ARG;
     dst.push_back(e.node);
@@ -1328,6 +1403,62 @@ gf_status_t gf_edge_scores(gf_wgraph_t* g, const gf_scorer_t* m, const float* x_
                                    per_pass, (cudaStream_t)stream);
   if (k < 0) return GF_ERR_CUDA;
   g->launches += k;
+  return GF_OK;
+}
+
+static bool projection_ok(const gf_projection_t* p) {
+  if (!p || p->in_dim < 8 || (p->in_dim & 7) || p->out_dim < 1 || !p->w_dev || ((uintptr_t)p->w_dev & 15) || p->w_stride < p->in_dim ||
+      (p->w_stride & 7) || p->w_stride > (1ll << 38) || p->num_adapters < 0)
+    return false;
+  if (p->num_adapters == 0) return true;
+  return p->rank >= 8 && p->rank <= 64 && (p->rank & 7) == 0 && p->a_dev && p->b_dev && !(((uintptr_t)p->a_dev | (uintptr_t)p->b_dev) & 15) &&
+         !((uintptr_t)p->scale_dev & 3);
+}
+
+uint64_t gf_adapter_project_scratch_bytes(const gf_projection_t* p, int32_t rows) {
+  if (!projection_ok(p) || rows < 1 || p->num_adapters == 0) return 0;
+  return (uint64_t)project_parts(p->in_dim) * (uint64_t)rows * (uint64_t)p->rank * 4;
+}
+
+gf_status_t gf_adapter_project(gf_wgraph_t* g, const gf_projection_t* p, int32_t rows, const void* x_dev, int64_t x_stride,
+                               const int32_t* adapter_dev, void* y_dev, int64_t y_stride, int32_t y_fp32, void* scratch_dev,
+                               uint64_t scratch_bytes, void* stream) {
+  if (!g || !projection_ok(p) || rows < 0 || y_fp32 < 0 || y_fp32 > 1 || x_stride < p->in_dim || (x_stride & 7) || x_stride > (1ll << 38) ||
+      y_stride < p->out_dim)
+    return GF_ERR_INVALID_ARG;
+  if (rows == 0) return GF_OK;
+  if (!x_dev || !y_dev || ((uintptr_t)x_dev & 15) || ((uintptr_t)y_dev & (y_fp32 ? 3 : 1)) || ((uintptr_t)adapter_dev & 3)) return GF_ERR_INVALID_ARG;
+  // (rows of W and of x are TMA coordinates, tiles of both a grid)
+  if ((int64_t)((p->out_dim + 127) / 128) * ((rows + 255) / 256) > (1ll << 27)) return GF_ERR_INVALID_ARG;
+  if (adapter_dev && p->num_adapters > 0) {
+    if (!scratch_dev || ((uintptr_t)scratch_dev & 15)) return GF_ERR_INVALID_ARG;
+    if (scratch_bytes < gf_adapter_project_scratch_bytes(p, rows)) return GF_ERR_CAPACITY;
+  }
+  DeviceGuard dev(g->device);
+  if (!dev.ok) return GF_ERR_CUDA;
+  const int n = launch_project(*p, rows, x_dev, x_stride, adapter_dev, y_dev, y_stride, y_fp32, (float*)scratch_dev, g->num_sms, g->status_dev,
+                               (cudaStream_t)stream);
+  if (n < 0) return GF_ERR_CUDA;
+  g->launches += n;
+  return GF_OK;
+}
+
+gf_status_t gf_token_logprobs(gf_wgraph_t* g, int32_t rows, int32_t vocab, const void* logits_dev, int64_t stride, int32_t fp32,
+                              const int32_t* tokens_dev, int32_t top, const gf_logprobs_t* out, void* stream) {
+  if (!g || rows < 0 || rows > (1 << 27) || vocab < 1 || stride < vocab || fp32 < 0 || fp32 > 1 || top < 0 || top > GF_MAX_TOP || top > vocab || !out)
+    return GF_ERR_INVALID_ARG;
+  if (rows == 0) return GF_OK;
+  if (!logits_dev || ((uintptr_t)logits_dev & (fp32 ? 3 : 1)) || (out->logprob_dev && !tokens_dev) ||
+      (((uintptr_t)tokens_dev | (uintptr_t)out->logprob_dev | (uintptr_t)out->entropy_dev | (uintptr_t)out->lse_dev |
+        (uintptr_t)out->top_ids_dev | (uintptr_t)out->top_logprobs_dev) & 3))
+    return GF_ERR_INVALID_ARG;
+  DeviceGuard dev(g->device);
+  if (!dev.ok) return GF_ERR_CUDA;
+  const int n = launch_token_logprobs(logits_dev, fp32, stride, rows, vocab, tokens_dev, out->top_ids_dev || out->top_logprobs_dev ? top : 0,
+                                      out->logprob_dev, out->entropy_dev, out->lse_dev, out->top_ids_dev, out->top_logprobs_dev, g->num_sms,
+                                      (cudaStream_t)stream);
+  if (n < 0) return GF_ERR_CUDA;
+  g->launches += n;
   return GF_OK;
 }
 

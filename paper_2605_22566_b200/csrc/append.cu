@@ -1,0 +1,180 @@
+// Nodes that grow: the token slots of a batch's new tokens from the requests' lengths, and the new K/V rows put into
+// the pool.
+//
+// Request r has held_r tokens in its node and gets count_r more; its rows in the batch start at the sum of the counts
+// before it, and row i of them goes to the slot off(node_r) + held_r + i.  All of it stays on the device: the node's new
+// length is written where the table builder reads it.  Every row of an open node at or beyond its length is zero in
+// every layer (gf_node_kv_open clears the extent, a call that takes tokens back clears theirs), so that the tails of
+// its tiles contribute exact zeros to P*V as everywhere in the pool.
+#include "gf_device.cuh"
+#include "gf_internal.h"
+
+namespace gf {
+namespace {
+
+constexpr int kSlotThreads = 256, kSlotRequests = 32;  // requests per CTA
+
+__device__ __forceinline__ char* chunk_at(const PoolGeom& pool, int layer, int head, int slot, int chunk, int value) {
+  const uint32_t row = (uint32_t)slot & (kTile - 1);
+  return pool.base + (uint64_t)layer * pool.layer_stride + (uint64_t)head * pool.head_stride +
+         (uint64_t)(slot / kTile) * pool.tile_bytes + (value ? pool.tile_bytes >> 1 : 0u) +
+         (uint32_t)(chunk >> 3) * (kTile * 128u) + swz128(row, (uint32_t)chunk & 7u);
+}
+
+// Zeros in the rows [from, to) of the pool, every layer and head, by all threads of the CTA.
+__device__ void clear_rows(const PoolGeom& pool, int layers, int heads, int chunks, int from, int to) {
+  const long long total = (long long)(to - from) * layers * heads * 2 * chunks;
+  for (long long i = threadIdx.x; i < total; i += blockDim.x) {
+    const int c = (int)(i % chunks);
+    long long j = i / chunks;
+    const int value = (int)(j & 1);
+    j >>= 1;
+    const int slot = from + (int)(j % (to - from));
+    j /= to - from;
+    *reinterpret_cast<uint4*>(chunk_at(pool, (int)(j / heads), (int)(j % heads), slot, c, value)) = make_uint4(0u, 0u, 0u, 0u);
+  }
+}
+
+// A CTA has 32 requests: it adds up the counts of those before them (each CTA by itself: 4 bytes a request from L2, against a
+// launch or a chain of CTAs), one warp checks its requests and sets their lengths, and all warps write the slots.
+// Latency-bound: a chain of four dependent loads.
+__global__ void __launch_bounds__(kSlotThreads) k_append_slots(GraphDev g, PoolGeom pool, int layers, int heads, int chunks, int num_requests,
+                                                               const int32_t* __restrict__ node, const int32_t* __restrict__ held,
+                                                               const int32_t* __restrict__ count, int num_new, int32_t* __restrict__ slots,
+                                                               int32_t* __restrict__ lens, int32_t* status) {
+  __shared__ long long warp_sums[kSlotThreads / 32];
+  __shared__ int s_begin[kSlotRequests + 1], s_slot[kSlotRequests], s_from[kSlotRequests], s_to[kSlotRequests];
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  const int r0 = blockIdx.x * kSlotRequests;
+  long long before = 0;
+  for (int r = tid; r < r0; r += kSlotThreads) before += max(count[r], 0);
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) before += __shfl_xor_sync(0xffffffffu, before, d);
+  if (lane == 0) warp_sums[wid] = before;
+  __syncthreads();
+  if (wid == 0) {
+    long long begin = 0;
+#pragma unroll
+    for (int w = 0; w < kSlotThreads / 32; ++w) begin += warp_sums[w];
+    const int r = r0 + lane;
+    const bool mine = r < num_requests;
+    const int c = mine ? count[r] : 0, v = mine ? node[r] : -1;
+    const bool known = v >= 0 && v < g.num_nodes;
+    const int room = known ? g.node_room[v] : -1, now = known ? g.node_len[v] : 0;
+    const int h = !mine ? 0 : held != nullptr ? held[r] : now;
+    long long end = max(c, 0);
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, end, d);
+      if (lane >= d) end += y;
+    }
+    end += begin;
+    const long long first = end - max(c, 0);
+    int why = GF_OK;
+    if (mine) {
+      if (room < 0 || c < 0 || h < 0 || h > now || end > num_new) why = GF_ERR_INVALID_ARG;
+      else if ((long long)h + c > room) why = GF_ERR_CAPACITY;
+      if (why != GF_OK) atomicCAS(status + kStatusReport, 0, why);
+    }
+    const bool ok = mine && why == GF_OK;
+    if (ok) g.node_len[v] = h + c;
+    if (mine && lens != nullptr) lens[r] = ok ? h + c : -1;
+    const int off = ok ? g.node_off[v] : 0;
+    s_slot[lane] = ok ? off + h : -1;
+    s_from[lane] = off + h + c;
+    s_to[lane] = ok && now > h + c ? off + now : 0;  // tokens taken back
+    s_begin[lane] = (int)min(first, (long long)num_new);
+    if (lane == 31) s_begin[32] = (int)min(end, (long long)num_new);
+  }
+  __syncthreads();
+  for (int i = wid; i < kSlotRequests; i += kSlotThreads / 32) {
+    const int a = s_begin[i], b = s_begin[i + 1], s = s_slot[i];
+    for (int t = a + lane; t < b; t += 32) slots[t] = s < 0 ? -1 : s + (t - a);
+  }
+  if (r0 + kSlotRequests >= num_requests)  // rows behind the last request's
+    for (int t = s_begin[kSlotRequests] + tid; t < num_new; t += kSlotThreads) slots[t] = -1;
+  for (int i = 0; i < kSlotRequests; ++i)
+    if (s_to[i] > s_from[i]) clear_rows(pool, layers, heads, chunks, s_from[i], s_to[i]);
+}
+
+// One layer's new rows from the caller's layout to their slots: 16 bytes of K and of V per step of a thread, a few tokens per
+// CTA.  Bound: HBM, 4 bytes there and back per entry pair.
+__global__ void __launch_bounds__(256) k_kv_append(PoolGeom pool, int layer, int heads, int chunk_bits, int num_new, int per_cta,
+                                                   const int32_t* __restrict__ slots, const char* __restrict__ k, int64_t k_stride,
+                                                   const char* __restrict__ v, int64_t v_stride, int32_t* status) {
+  const int t0 = blockIdx.x * per_cta, per_token = heads << chunk_bits;
+  const int n = min(per_cta, num_new - t0) * per_token;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < n; i += 256) {
+    const int t = i / per_token, at = i - t * per_token;
+    const int slot = slots[t0 + t];
+    const uint4 kv = *reinterpret_cast<const uint4*>(k + (int64_t)(t0 + t) * k_stride + at * 16);
+    const uint4 vv = *reinterpret_cast<const uint4*>(v + (int64_t)(t0 + t) * v_stride + at * 16);
+    if (slot < 0) continue;
+    if ((uint32_t)(slot / kTile) >= pool.cap_tiles) {
+      atomicCAS(status + kStatusReport, 0, (int)GF_ERR_INVALID_ARG);
+      continue;
+    }
+    const int head = at >> chunk_bits, c = at & ((1 << chunk_bits) - 1);
+    *reinterpret_cast<uint4*>(chunk_at(pool, layer, head, slot, c, 0)) = kv;
+    *reinterpret_cast<uint4*>(chunk_at(pool, layer, head, slot, c, 1)) = vv;
+  }
+}
+
+// Zeros in a whole extent, every layer and head.
+__global__ void __launch_bounds__(256) k_clear_extent(PoolGeom pool, int rows, int tile0, int tiles) {
+  const uint64_t n = (uint64_t)tiles * (pool.tile_bytes / 16);
+  for (int j = blockIdx.y; j < rows; j += gridDim.y) {
+    uint4* p = reinterpret_cast<uint4*>(pool.base + (uint64_t)j * pool.head_stride + (uint64_t)tile0 * pool.tile_bytes);
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (uint64_t)gridDim.x * 256) p[i] = make_uint4(0u, 0u, 0u, 0u);
+  }
+}
+
+// The end of a node's growth: its length, and zeros in what is left of its last tile.
+__global__ void __launch_bounds__(256) k_close_node(GraphDev g, PoolGeom pool, int layers, int heads, int chunks, int node, int n_tokens,
+                                                    int32_t* status) {
+  const int off = g.node_off[node], now = g.node_len[node];
+  if (threadIdx.x == 0 && now < n_tokens) atomicCAS(status + kStatusReport, 0, (int)GF_ERR_INVALID_ARG);
+  const int end = min(now, (n_tokens + kTile - 1) / kTile * kTile);
+  if (end > n_tokens) clear_rows(pool, layers, heads, chunks, off + n_tokens, off + end);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    g.node_len[node] = n_tokens;
+    g.node_room[node] = -1;
+  }
+}
+
+}  // namespace
+
+int launch_append_slots(const GraphDev& g, const PoolGeom& pool, int layers, int heads, int head_dim, int num_requests, const int32_t* node,
+                        const int32_t* held, const int32_t* count, int num_new, int32_t* slots, int32_t* lens, int32_t* status, cudaStream_t st) {
+  const int ctas = num_requests > 0 ? (num_requests + kSlotRequests - 1) / kSlotRequests : 1;  // (no request: the rows' -1 are left)
+  k_append_slots<<<ctas, kSlotThreads, 0, st>>>(
+      g, pool, layers, heads, head_dim / 8, num_requests, node, held, count, num_new, slots, lens, status);
+  return cudaGetLastError() == cudaSuccess ? 1 : -1;
+}
+
+int launch_kv_append(const PoolGeom& pool, int layer, int heads, int head_dim, int num_new, const int32_t* slots, const void* k,
+                     int64_t k_stride, const void* v, int64_t v_stride, int num_sms, int32_t* status, cudaStream_t st) {
+  // tokens per CTA: one while that leaves multiprocessors without work, up to eight
+  int per_cta = num_new / (num_sms * 8);
+  per_cta = per_cta < 1 ? 1 : per_cta > 8 ? 8 : per_cta;
+  k_kv_append<<<(num_new + per_cta - 1) / per_cta, 256, 0, st>>>(pool, layer, heads, head_dim == 128 ? 4 : 3, num_new, per_cta, slots,
+                                                                (const char*)k, k_stride * 2, (const char*)v, v_stride * 2, status);
+  return cudaGetLastError() == cudaSuccess ? 1 : -1;
+}
+
+int launch_clear_extent(const PoolGeom& pool, int layers, int heads, int tile0, int tiles, cudaStream_t st) {
+  if (tiles <= 0) return 0;
+  const long long rows = (long long)layers * heads, blocks = (long long)tiles * (pool.tile_bytes / 16) / 1024;
+  k_clear_extent<<<dim3((unsigned)(blocks < 64 ? blocks : 64), (unsigned)(rows < 65535 ? rows : 65535)), 256, 0, st>>>(pool, (int)rows, tile0, tiles);
+  return cudaGetLastError() == cudaSuccess ? 1 : -1;
+}
+
+int launch_close_node(const GraphDev& g, const PoolGeom& pool, int layers, int heads, int head_dim, int node, int n_tokens, int32_t* status,
+                      cudaStream_t st) {
+  k_close_node<<<1, 256, 0, st>>>(g, pool, layers, heads, head_dim / 8, node, n_tokens, status);
+  return cudaGetLastError() == cudaSuccess ? 1 : -1;
+}
+
+}  // namespace gf

@@ -98,6 +98,7 @@ struct GraphDev {
   const int32_t* adj_dst;  // [num_edges] ascending within a row
   int32_t* node_len;       // [num_nodes] tokens; -1 = never written
   int32_t* node_off;       // [num_nodes] pool token offset (tile aligned)
+  int32_t* node_room;      // [num_nodes] tokens that an open node's extent has room for; -1: a node of fixed length, or none
   int32_t* node_res;       // [num_nodes] row of the residual table of a node whose state is base + residual; -1: none
   int32_t num_nodes, num_shared_nodes;
 };
@@ -272,7 +273,15 @@ inline bool ensure_dynamic_smem(K kernel, size_t bytes, bool (&done)[kMaxDevices
 }
 
 // ---- launchers (each returns the number of kernels it enqueued, or -1 on a launch error) ----
-int launch_graph_set_node(const GraphDev& g, int node, int len, int off, cudaStream_t st);
+int launch_graph_set_node(const GraphDev& g, int node, int len, int off, cudaStream_t st, int room = -1);
+// Growing nodes (see gf_append_slots).  Strides in entries.
+int launch_append_slots(const GraphDev& g, const PoolGeom& pool, int layers, int heads, int head_dim, int num_requests, const int32_t* node,
+                        const int32_t* held, const int32_t* count, int num_new, int32_t* slots, int32_t* lens, int32_t* status, cudaStream_t st);
+int launch_kv_append(const PoolGeom& pool, int layer, int heads, int head_dim, int num_new, const int32_t* slots, const void* k,
+                     int64_t k_stride, const void* v, int64_t v_stride, int num_sms, int32_t* status, cudaStream_t st);
+int launch_clear_extent(const PoolGeom& pool, int layers, int heads, int tile0, int tiles, cudaStream_t st);
+int launch_close_node(const GraphDev& g, const PoolGeom& pool, int layers, int heads, int head_dim, int node, int n_tokens, int32_t* status,
+                      cudaStream_t st);
 // set != nullptr: the kernel also records the node's length and pool offset on the device (first write).
 int launch_kv_write(const PoolGeom& pool, int layer, int num_kv_heads, int head_dim, int tile0,
                     const void* k, const void* v, int n_tokens, const GraphDev* set, int node, int32_t* status,
@@ -333,6 +342,12 @@ int launch_weights(const PoolGeom& pool16, const PoolGeom& pool4, const AttnShap
                    cudaStream_t st, cudaStream_t side);
 int launch_evict(const PoolGeom& pool16, const PoolGeom& pool4, const EvictBatch& batch, int num_layers, int num_kv_heads,
                  int head_dim, float* weights, int64_t slots, int32_t* kept, const GraphDev& g, cudaStream_t st);
+// parts that the adapters' inner results come in: rows * rank floats of scratch each.
+int project_parts(int in_dim);
+int launch_project(const gf_projection_t& p, int rows, const void* x, int64_t x_stride, const int32_t* adapter, void* y, int64_t y_stride, int y_fp32,
+                   float* scratch, int num_sms, int32_t* status, cudaStream_t st);
+int launch_token_logprobs(const void* logits, int fp32, int64_t stride, int rows, int vocab, const int32_t* tokens, int top, float* logprob,
+                          float* entropy, float* lse, int32_t* top_ids, float* top_logprobs, int num_sms, cudaStream_t st);
 int launch_wait_probe(int32_t* status, long long limit, int32_t* returned, cudaStream_t st);
 // k_new / v_new non-null: the new segments' K/V (caller layout, request-major rows) are written to their
 // pool extents by the same launch (extend with append).

@@ -582,9 +582,10 @@ __global__ void k_emit(TablesDev t, gf_policy_t pol, int item_blocks, const int3
   }
 }
 
-__global__ void k_set_node(GraphDev g, int node, int len, int off) {
+__global__ void k_set_node(GraphDev g, int node, int len, int off, int room) {
   g.node_len[node] = len;
   g.node_off[node] = off;
+  g.node_room[node] = room;
 }
 
 __global__ void k_set_residual(ResidualEntry* slot, ResidualEntry value, int32_t* node_res, int node, int row) {
@@ -596,8 +597,8 @@ inline int blocks_for(int n, int threads) { return n <= 0 ? 1 : (n + threads - 1
 
 }  // namespace
 
-int launch_graph_set_node(const GraphDev& g, int node, int len, int off, cudaStream_t st) {
-  k_set_node<<<1, 1, 0, st>>>(g, node, len, off);
+int launch_graph_set_node(const GraphDev& g, int node, int len, int off, cudaStream_t st, int room) {
+  k_set_node<<<1, 1, 0, st>>>(g, node, len, off, room);
   return cudaGetLastError() == cudaSuccess ? 1 : -1;
 }
 

@@ -4,7 +4,7 @@ table arithmetic lives here; PyTorch only supplies memory and streams."""
 from __future__ import annotations
 
 import weakref
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import numpy as np
 import torch
@@ -30,6 +30,44 @@ def _bits_to_tensor(bits: np.ndarray, device) -> torch.Tensor:
 
 def tensor_to_f64(t: torch.Tensor) -> np.ndarray:
     return t.detach().to(torch.float64).cpu().numpy()
+
+
+class Projection:
+    """A shared weight [out, in] with the low-rank adapters that rows may name: a [adapters, rank, in], b [adapters, out, rank],
+    scale fp32 [adapters] (None: 1).  bf16, on one device; kept alive here.  The weight's rows may lie apart, the adapters are contiguous."""
+
+    def __init__(self, weight: torch.Tensor, a: Optional[torch.Tensor] = None, b: Optional[torch.Tensor] = None,
+                 scale: Optional[torch.Tensor] = None):
+        if weight.dtype != torch.bfloat16 or weight.dim() != 2 or weight.stride(1) != 1 or not weight.is_cuda:
+            raise ValueError("weight: a bf16 tensor [out, in] on a CUDA device, entries of a row next to each other")
+        out_dim, in_dim = weight.shape
+        adapters = rank = 0
+        if a is not None or b is not None:
+            if a is None or b is None or a.dim() != 3 or b.dim() != 3 or a.dtype != torch.bfloat16 or b.dtype != torch.bfloat16 or \
+                    a.shape[2] != in_dim or tuple(b.shape) != (a.shape[0], out_dim, a.shape[1]) or not a.is_contiguous() or \
+                    not b.is_contiguous() or a.device != weight.device or b.device != weight.device:
+                raise ValueError(f"a, b: contiguous bf16 tensors [adapters, rank, {in_dim}] and [adapters, {out_dim}, rank] on {weight.device}")
+            adapters, rank = a.shape[:2]
+        if scale is not None and (a is None or scale.dtype != torch.float32 or tuple(scale.shape) != (adapters,) or not scale.is_contiguous() or
+                                  scale.device != weight.device):
+            raise ValueError(f"scale: a contiguous fp32 tensor [{adapters}] on {weight.device}")
+        self.weight, self.a, self.b, self.scale = weight, a, b, scale
+        # (a weight of one row may have any stride)
+        stride = weight.stride(0) if out_dim > 1 else -(-in_dim // 8) * 8
+        self.desc = B.ProjectionDesc(in_dim, out_dim, weight.data_ptr(), stride, adapters, rank, _ptr(a), _ptr(b), _ptr(scale))
+
+
+class TokenLogprobs(NamedTuple):
+    """Per row: the given token's log probability, the entropy, the log-sum-exp, and the most likely tokens with theirs."""
+    logprob: Optional[torch.Tensor]
+    entropy: torch.Tensor
+    lse: torch.Tensor
+    top_ids: torch.Tensor
+    top_logprobs: torch.Tensor
+
+
+def _ptr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
 
 
 class PathAttention:
@@ -268,6 +306,99 @@ class PathAttention:
                                                   None if lse is None else lse.data_ptr(), self.stream),
                 "gf_path_attention_extend_append")
         return out
+
+    # ---- nodes that grow ---------------------------------------------------------------------
+    def open_node(self, node: int, room: int) -> None:
+        """gf_node_kv_open: an unwritten node gets room for that many tokens and holds none."""
+        B.check(B.gf_node_kv_open(self.g, node, room, self.stream), "gf_node_kv_open")
+
+    def close_node(self, node: int, tokens: int) -> None:
+        """gf_node_kv_close: the node has this many tokens from here on."""
+        B.check(B.gf_node_kv_close(self.g, node, tokens, self.stream), "gf_node_kv_close")
+
+    def _check_ints(self, name: str, t: torch.Tensor, n: Optional[int] = None) -> None:
+        if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.get_device() != self.pool.get_device() or (n is not None and t.shape[0] != n):
+            raise ValueError(f"{name}: a contiguous int32 tensor [{'requests' if n is None else n}] on {self.pool.device}")
+
+    def append_slots(self, nodes: torch.Tensor, counts: torch.Tensor, num_new: int, held: Optional[torch.Tensor] = None):
+        """gf_append_slots: request r gets counts[r] tokens in the open node nodes[r], behind the held[r] that stay (None: behind all
+        that it holds).  Token slots of the num_new rows and the nodes' new lengths, int32.  Build the tables anew after it."""
+        self._check_ints("nodes", nodes)
+        n = nodes.shape[0]
+        self._check_ints("counts", counts, n)
+        if held is not None:
+            self._check_ints("held", held, n)
+        if num_new < 0:
+            raise ValueError("num_new: at least 0")
+        both = self.path_ptr.new_empty((num_new + n,))
+        slots, lens = both[:num_new], both[num_new:]
+        B.check(B.gf_append_slots(self.g, n, nodes.data_ptr(), _ptr(held), counts.data_ptr(), num_new, slots.data_ptr(), lens.data_ptr(),
+                                  self.stream), "gf_append_slots")
+        return slots, lens
+
+    def append(self, layer: int, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor) -> None:
+        """gf_node_kv_append of bf16 rows [new, Hkv, D], which may be parts of wider rows (heads next to each other)."""
+        self._check_ints("slots", slots)
+        row = (slots.shape[0], self.w.num_kv_heads, self.w.head_dim)
+        for t in (k, v):
+            if t.dtype != torch.bfloat16 or tuple(t.shape) != row or t.get_device() != self.pool.get_device() or t.stride(2) != 1 or \
+                    (row[1] > 1 and t.stride(1) != row[2]):
+                raise ValueError(f"k, v: bf16 tensors {list(row)} on {self.pool.device}, the entries of a token next to each other")
+        B.check(B.gf_node_kv_append(self.g, layer, row[0], slots.data_ptr(), k.data_ptr(), k.stride(0) if row[0] > 1 else 0, v.data_ptr(),
+                                    v.stride(0) if row[0] > 1 else 0, self.stream), "gf_node_kv_append")
+
+    # ---- before and behind the attention -------------------------------------------------------
+    def project(self, projection: Projection, x: torch.Tensor, adapters: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+        """gf_adapter_project: x [rows, in] times the shared weight, each row with the adapter that adapters[row] names (-1, or
+        adapters None: none).  [rows, out] in bf16 or fp32, into `out` where given."""
+        d = projection.desc
+        rows = x.shape[0]
+        if x.dtype != torch.bfloat16 or x.dim() != 2 or x.shape[1] != d.in_dim or x.stride(1) != 1 or x.get_device() != self.pool.get_device() or \
+                projection.weight.get_device() != self.pool.get_device():
+            raise ValueError(f"x: a bf16 tensor [rows, {d.in_dim}] on {self.pool.device} like the projection, entries of a row next to each other")
+        if adapters is not None:
+            self._check_ints("adapters", adapters, rows)
+            if d.num_adapters == 0:
+                raise ValueError("adapters: the projection has none")
+        if out is None:
+            if dtype not in (torch.bfloat16, torch.float32):
+                raise ValueError("dtype: bf16 or fp32")
+            out = x.new_empty((rows, d.out_dim), dtype=dtype)
+        elif out.dtype not in (torch.bfloat16, torch.float32) or tuple(out.shape) != (rows, d.out_dim) or out.stride(1) != 1 or \
+                out.get_device() != x.get_device():
+            raise ValueError(f"out: a bf16 or fp32 tensor [{rows}, {d.out_dim}] on {self.pool.device}, entries of a row next to each other")
+        if rows == 0:
+            return out
+        scratch, nbytes = None, 0
+        if adapters is not None:
+            nbytes = B.gf_adapter_project_scratch_bytes(d, rows)
+            scratch = x.new_empty((nbytes,), dtype=torch.uint8)
+        B.check(B.gf_adapter_project(self.g, d, rows, x.data_ptr(), x.stride(0) if rows > 1 else d.in_dim, _ptr(adapters), out.data_ptr(),
+                                     out.stride(0) if rows > 1 else d.out_dim, out.dtype == torch.float32, _ptr(scratch), nbytes, self.stream),
+                "gf_adapter_project")
+        return out
+
+    def token_logprobs(self, logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, top: int = 0) -> TokenLogprobs:
+        """gf_token_logprobs of bf16 or fp32 logits [rows, vocab]: log probabilities of the given tokens (-1: none), entropy,
+        log-sum-exp, and the `top` most likely tokens with their log probabilities."""
+        if logits.dtype not in (torch.bfloat16, torch.float32) or logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1) or \
+                logits.get_device() != self.pool.get_device():
+            raise ValueError(f"logits: a bf16 or fp32 tensor [rows, vocab] on {self.pool.device}, entries of a row next to each other")
+        rows, vocab = logits.shape
+        if tokens is not None:
+            self._check_ints("tokens", tokens, rows)
+        if not 0 <= top <= min(B.GF_MAX_TOP, vocab):
+            raise ValueError(f"top: 0 to {min(B.GF_MAX_TOP, vocab)}")
+        stats = logits.new_empty((3 + top, rows), dtype=torch.float32)
+        logprob, entropy, lse = stats[:3].unbind(0)
+        top_logprobs = stats[3:].view(rows, top)
+        top_ids = self.path_ptr.new_empty((rows, top))
+        out = B.Logprobs(None if tokens is None else logprob.data_ptr(), entropy.data_ptr(), lse.data_ptr(), top_ids.data_ptr() if top else None,
+                         top_logprobs.data_ptr() if top else None)
+        B.check(B.gf_token_logprobs(self.g, rows, vocab, logits.data_ptr(), logits.stride(0) if rows > 1 else vocab,
+                                    logits.dtype == torch.float32, _ptr(tokens), top, out, self.stream), "gf_token_logprobs")
+        return TokenLogprobs(None if tokens is None else logprob, entropy, lse, top_ids, top_logprobs)
 
     # ---- eviction by accumulated attention weight --------------------------------------------
     def new_weights(self) -> torch.Tensor:
