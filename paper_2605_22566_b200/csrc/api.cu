@@ -1456,7 +1456,7 @@ gf_status_t gf_token_logprobs(gf_wgraph_t* g, int32_t rows, int32_t vocab, const
   if (!dev.ok) return GF_ERR_CUDA;
   const int n = launch_token_logprobs(logits_dev, fp32, stride, rows, vocab, tokens_dev, out->top_ids_dev || out->top_logprobs_dev ? top : 0,
                                       out->logprob_dev, out->entropy_dev, out->lse_dev, out->top_ids_dev, out->top_logprobs_dev, g->num_sms,
-                                      (cudaStream_t)stream);
+                                      g->status_dev, (cudaStream_t)stream);
   if (n < 0) return GF_ERR_CUDA;
   g->launches += n;
   return GF_OK;

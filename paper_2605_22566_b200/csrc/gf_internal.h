@@ -347,7 +347,7 @@ int project_parts(int in_dim);
 int launch_project(const gf_projection_t& p, int rows, const void* x, int64_t x_stride, const int32_t* adapter, void* y, int64_t y_stride, int y_fp32,
                    float* scratch, int num_sms, int32_t* status, cudaStream_t st);
 int launch_token_logprobs(const void* logits, int fp32, int64_t stride, int rows, int vocab, const int32_t* tokens, int top, float* logprob,
-                          float* entropy, float* lse, int32_t* top_ids, float* top_logprobs, int num_sms, cudaStream_t st);
+                          float* entropy, float* lse, int32_t* top_ids, float* top_logprobs, int num_sms, int32_t* status, cudaStream_t st);
 int launch_wait_probe(int32_t* status, long long limit, int32_t* returned, cudaStream_t st);
 // k_new / v_new non-null: the new segments' K/V (caller layout, request-major rows) are written to their
 // pool extents by the same launch (extend with append).

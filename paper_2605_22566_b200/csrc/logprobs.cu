@@ -3,26 +3,39 @@
 // With m the largest logit seen so far, a thread keeps l = sum 2^d and s = sum d 2^d of d = (x - m) log2 e over its part of the
 // row (both relative to m, and moved when m does); then lse = m + ln l and the entropy, sum p (lse - x), is
 // ln 2 (log2 l - s / l): no second pass, and no difference of large numbers where one token has nearly everything.
+// d is x log2 e - c in one fused step, two entries at a time; c, m log2 e rounded, is what all of a row's d are relative to, so
+// its rounding cancels.  Where that would overflow (a largest logit beyond 1e38) d is (x - m) log2 e.  Masked entries' d, minus
+// infinity, is held to -1000, so that its product with p = 0 is a number.
 //
-// The k most likely: every logit gets a 64-bit key, its value's order above the complement of its index, so that keys differ and
-// equal values rank by the lower index.  A threshold that at least k keys of the CTA's part reach is known after each thread's first
-// vector; from then on a vector's maximum is compared with it, and only what reaches it goes to a list in shared memory, which is
-// cut to its k largest (each counts the keys above it) when it has grown, which raises the threshold.  On 128 000 normal
-// values some 100 to 200 get there.
+// The k most likely: where n warps of a CTA each have m lanes whose largest logit so far reaches t, n m logits do, so with n m > k
+// nothing below t can be among them.  The warps tell each other these levels (m lanes') through shared memory, with no barrier (a
+// level that is read late is lower, which is right too), and a logit above the n-th largest of them goes to a list; the largest of a
+// lane's round is compared, so that this costs little where nothing happens.  On 128 000 normal values some 20 to 200 get there.
+// At the end the list has every logit above the last t.  If those are k, its k largest are the answer (each counts those above it); if
+// not, the others are the first ones equal to t, and are looked for from the row's start.  More than the list holds (a row
+// that rises from end to end): a second pass in steps that it cannot overrun, cut to k in between.
+//
+// A warp brings its own pieces of the row to shared memory, two rounds of 2 KB ahead of the one it works on, and waits for no other
+// (two rounds of loads into registers leave room for half the warps, and one ahead left HBM idle in between).
 //
 // A row is one CTA's, or that of a cluster, whose first CTA joins the parts through shared memory.
-#include "gf_device.cuh"
+#include <algorithm>
+
+#include "tc_device.cuh"
 #include "gf_internal.h"
 
 namespace gf {
 namespace {
 
-constexpr int kMinThreads = 128, kMaxThreads = 512, kMaxTop = 32, kMaxCluster = 8;
-constexpr int kList = 2048;      // candidates that the list has room for
-constexpr int kCutAt = 256;      // it is cut when it holds more than this
-constexpr int kAhead = 4;        // vectors that a thread asks for at a time
+constexpr int kMinThreads = 128, kMaxThreads = 256, kMaxTop = 32, kMaxCluster = 8;
+constexpr int kList = 1024;      // candidates that the list has room for
+constexpr int kAhead = 8;        // vectors that a lane takes at a time
+constexpr int kStages = 2;       // such rounds that a warp has on the way
+constexpr int kRound = 32 * kAhead;
+constexpr int kMargin = 4;       // so many more than k reach a level, so that logits equal to it seldom have to be looked for
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kNegInf = -__builtin_huge_valf();
+constexpr float kNegInf = -__builtin_huge_valf(), kNan = __builtin_nanf("");
+constexpr uint32_t kLowest = 0x007fffffu;  // order of minus infinity
 
 typedef unsigned long long Key;  // 0: none
 
@@ -32,6 +45,10 @@ struct Shared {
   Key list[kList];
   Key best[kMaxTop];             // the k largest, descending, after a cut
   Key bound[kMaxThreads / 32];
+  uint32_t level[kMaxThreads / 32];  // order of the logit that enough lanes of the warp reach
+  uint32_t common;                   // the highest of what the warps have made of all levels
+  int before[kMaxThreads / 32 + 1];
+  uint64_t full[kMaxThreads / 32][kStages];
   Stats stats[kMaxThreads / 32];
   Stats part;                    // the CTA's
   Key join[kMaxCluster * kMaxTop];
@@ -45,15 +62,21 @@ __device__ __forceinline__ uint32_t order_of(float x) {
   return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float value_of(uint32_t order) {
-  if (order == 0u) return __int_as_float(0x7fffffff);
+  if (order == 0u) return kNan;
   return __uint_as_float((order & 0x80000000u) ? order & 0x7fffffffu : ~order);
 }
 __device__ __forceinline__ Key key_of(float x, int64_t index) { return (Key)order_of(x) << 32 | (uint32_t)~(uint32_t)index; }
 
+constexpr float kFar = 1e38f, kLag = 4.f;
+
+// (x - m) log2 e, relative to the same c wherever |m| is not far.
+__device__ __forceinline__ float diff(float x, float m) { return fabsf(m) < kFar ? fmaf(x, kLog2e, -(m * kLog2e)) : (x - m) * kLog2e; }
+
 __device__ __forceinline__ void stats_move(Stats& a, float m) {  // to the reference m >= a.m
   if (a.m != kNegInf) {
-    const float d = fmaxf((a.m - m) * kLog2e, -1000.f), f = fast_exp2(d);
-    a.s = f * (a.s + a.l * d);
+    const float d = fabsf(a.m) < kFar && fabsf(m) < kFar ? a.m * kLog2e - m * kLog2e : (a.m - m) * kLog2e;
+    const float e = fmaxf(d, -1000.f), f = fast_exp2(e);
+    a.s = f * (a.s + a.l * e);
     a.l *= f;
   }
   a.m = m;
@@ -66,11 +89,21 @@ __device__ __forceinline__ Stats stats_join(Stats a, Stats b) {
   a.s += b.s;
   return a;
 }
-// One more logit, at most a.m.  (A difference below -1000 has no probability left; the product with it has to stay a number.)
+// The larger one, NaN if either is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+// One more logit, at most a.m; any value.
 __device__ __forceinline__ void stats_add(Stats& a, float x) {
-  const float d = fmaxf((x - a.m) * kLog2e, -1000.f), p = fast_exp2(d);
-  a.l += x == x ? p : x;
-  a.s = fmaf(p, d, a.s);
+  if (a.m == kNegInf) {
+    if (x != x) a.l = x;
+    return;
+  }
+  const float d = diff(x, a.m), p = fast_exp2(d);
+  a.l += p;
+  a.s = fmaf(p, fmaxf(d, -1000.f), a.s);
 }
 
 template <typename T> struct Vec;
@@ -78,6 +111,20 @@ template <> struct Vec<float> {
   static constexpr int n = 4;
   static __device__ __forceinline__ void get(uint4 v, float (&x)[4]) {
     x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
+  }
+  static constexpr uint32_t kNothing = 0xff800000u;  // minus infinity in every entry
+  static __device__ __forceinline__ void word(uint32_t w, float (&x)[1]) { x[0] = __uint_as_float(w); }
+  // the largest of a round; NaN only where there is nothing else
+  static __device__ __forceinline__ float largest(const uint4 (&v)[kAhead]) {
+    float x[4];
+    get(v[0], x);
+    float top = fmax3(fmaxf(x[0], x[1]), x[2], x[3]);
+#pragma unroll
+    for (int u = 1; u < kAhead; ++u) {
+      get(v[u], x);
+      top = fmax3(fmax3(top, x[0], x[1]), x[2], x[3]);
+    }
+    return top;
   }
   static __device__ __forceinline__ float one(const float* p) { return *p; }
 };
@@ -91,8 +138,92 @@ template <> struct Vec<__nv_bfloat16> {
       x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
     }
   }
+  static __device__ __forceinline__ void word(uint32_t w, float (&x)[2]) {
+    x[0] = __uint_as_float(w << 16);
+    x[1] = __uint_as_float(w & 0xffff0000u);
+  }
+  static __device__ __forceinline__ __nv_bfloat162 pair(uint32_t w) { return *reinterpret_cast<__nv_bfloat162*>(&w); }
+  static constexpr uint32_t kNothing = 0xff80ff80u;
+  static __device__ __forceinline__ float largest(const uint4 (&v)[kAhead]) {
+    __nv_bfloat162 t = pair(v[0].x);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (u > 0) t = __hmax2(t, pair(v[u].x));
+      t = __hmax2(t, pair(v[u].y));
+      t = __hmax2(t, pair(v[u].z));
+      t = __hmax2(t, pair(v[u].w));
+    }
+    return fmaxf(__low2float(t), __high2float(t));
+  }
   static __device__ __forceinline__ float one(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 };
+
+// The k largest of the list's first n keys to its front, in descending order.  All threads; n is theirs alike.
+__device__ void rank(Shared& sm, int n, int k) {
+  for (int i = threadIdx.x; i < n; i += blockDim.x) {
+    const Key x = sm.list[i];
+    int above = 0;
+    for (int j = 0; j < n; ++j) above += sm.list[j] > x;
+    if (above < k) sm.best[above] = x;
+  }
+  __syncthreads();
+  const int m = min(n, k);
+  for (int i = threadIdx.x; i < m; i += blockDim.x) sm.list[i] = sm.best[i];
+  if (threadIdx.x == 0) sm.count = m;
+  __syncthreads();
+}
+
+// Keeps of the list the keys whose value's order is above `order`, then ranks them.
+__device__ void cut_above(Shared& sm, int k, uint32_t order) {
+  constexpr int kOwn = kList / kMinThreads;
+  const int n = sm.count;
+  if (threadIdx.x == 0) sm.kept = 0;
+  Key own[kOwn];
+#pragma unroll
+  for (int j = 0; j < kOwn; ++j) {
+    const int i = threadIdx.x + j * blockDim.x;
+    own[j] = i < n ? sm.list[i] : 0;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < kOwn; ++j)
+    if ((uint32_t)(own[j] >> 32) > order) sm.list[atomicAdd(&sm.kept, 1)] = own[j];
+  __syncthreads();
+  rank(sm, sm.kept, k);
+}
+
+// Publishes the largest order that `enough` lanes of the warp reach with their largest logit so far (it never falls).
+__device__ __forceinline__ void publish(Shared& sm, float seen, int enough) {
+  const int lane = threadIdx.x & 31;
+  const uint32_t b = __float_as_uint(seen);  // (a number, so the plain form of order_of)
+  uint32_t mine = b ^ ((uint32_t)((int)b >> 31) | 0x80000000u);
+  for (int j = 1; j < enough; ++j) {
+    const uint32_t holders = __ballot_sync(0xffffffffu, mine == __reduce_max_sync(0xffffffffu, mine));
+    if (lane == __ffs(holders) - 1) mine = 0;
+  }
+  const uint32_t level = __reduce_max_sync(0xffffffffu, mine);
+  if (lane == 0 && level > kLowest) *(volatile uint32_t*)&sm.level[threadIdx.x >> 5] = level;
+}
+// The `nth` largest of all warps' levels, as a value: nth * enough lanes reach it.
+__device__ __forceinline__ float common_level(Shared& sm, int nth, int warps) {
+  const int lane = threadIdx.x & 31;
+  uint32_t mine = lane < warps ? *(volatile uint32_t*)&sm.level[lane] : 0u, level;
+  if (2 * nth <= warps) {
+    for (int j = 1; j < nth; ++j) {
+      const uint32_t holders = __ballot_sync(0xffffffffu, mine == __reduce_max_sync(0xffffffffu, mine));
+      if (lane == __ffs(holders) - 1) mine = 0u;
+    }
+    level = __reduce_max_sync(0xffffffffu, mine);
+  } else {
+    if (lane >= warps) mine = 0xffffffffu;
+    for (int j = nth; j < warps; ++j) {
+      const uint32_t holders = __ballot_sync(0xffffffffu, mine == __reduce_min_sync(0xffffffffu, mine));
+      if (lane == __ffs(holders) - 1) mine = 0xffffffffu;
+    }
+    level = __reduce_min_sync(0xffffffffu, mine);
+  }
+  return value_of(level);
+}
 
 // Cuts the list to its k largest keys, in descending order, and raises the threshold to the k-th.  All threads.
 __device__ void cut(Shared& sm, int k, Key& least) {
@@ -137,17 +268,8 @@ __device__ void cut(Shared& sm, int k, Key& least) {
     __syncthreads();
     n = sm.kept;
   }
-  for (int i = tid; i < n; i += blockDim.x) {
-    const Key x = sm.list[i];
-    int above = 0;
-    for (int j = 0; j < n; ++j) above += sm.list[j] > x;
-    if (above < k) sm.best[above] = x;
-  }
-  __syncthreads();
-  const int m = min(n, k);
-  for (int i = tid; i < m; i += blockDim.x) sm.list[i] = sm.best[i];
-  if (tid == 0) sm.count = m;
-  if (m == k) least = sm.best[k - 1];
+  rank(sm, n, k);
+  if (n >= k) least = sm.best[k - 1];
   __syncthreads();
 }
 
@@ -175,227 +297,389 @@ __device__ __forceinline__ float peer_float(const float* p, uint32_t rank) {
   return x;
 }
 
+// The k largest of a CTA's part from what was listed, to best; how many there are.  All threads.
+template <typename T, typename P>
+__device__ int finish(Shared& sm, int k, float least, const P& p, int loose, int my_loose, int vocab, int warps) {
+  constexpr int kN = Vec<T>::n;
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, threads = blockDim.x;
+  const int n = sm.count;
+  if (n <= threads) {
+    const Key mine = tid < n ? sm.list[tid] : 0;
+    if (__syncthreads_count((uint32_t)(mine >> 32) > order_of(least)) >= k) {
+      int above = 0;
+      if (mine != 0) {
+#pragma unroll 4
+        for (int j = 0; j < n; ++j) above += sm.list[j] > mine;
+        if (above < k) sm.best[above] = mine;
+      }
+      __syncthreads();
+      return k;
+    }
+  }
+  const T* x = p.x;
+  const int head = p.head, tail = p.tail, v0 = p.v0, v1 = p.v1;
+  if (n > kList) {
+    Key bound = 0;
+    cut(sm, k, bound);
+    // (what the first pass listed is met again: from an empty list, against a key that k of them reach)
+    if (tid == 0) sm.count = 0;
+    __syncthreads();
+    auto again = [&](bool mine, float v, int64_t index) {
+      if (sm.count > kList - threads) cut(sm, k, bound);
+      __syncthreads();
+      const Key key = mine ? key_of(v, index) : 0;
+      if (mine && key >= bound) {
+        const int at = atomicAdd(&sm.count, 1);
+        sm.list[at] = key;
+      }
+      __syncthreads();
+    };
+    again(tid < loose, tid < loose ? Vec<T>::one(x + my_loose) : 0.f, my_loose);
+#pragma unroll 1
+    for (int base = v0; base < v1; base += threads)
+#pragma unroll 1
+      for (int i = 0; i < kN; ++i) {
+        const int64_t at = head + (int64_t)(base + tid) * kN + i;
+        again(base + tid < v1, base + tid < v1 ? Vec<T>::one(x + at) : 0.f, at);
+      }
+    cut(sm, k, bound);
+    return sm.count;
+  }
+  cut_above(sm, k, order_of(least));
+  // the others: the first ones equal to `least`, and behind them, where nothing is left but NaN, the first of those
+  for (int nan = 0; nan < 2 && sm.count < k; ++nan) {
+    auto same = [&](float v) { return nan ? v != v : v == least; };
+    // in the order of the row: the entries before the vectors, theirs, those behind
+    auto take = [&](uint32_t found, int64_t first) {  // `found`: which of the thread's entries, from index `first` on
+      const int here = __popc(found);
+      int upto = here;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += y;
+      }
+      const int have = sm.count;
+      if (lane == 31) sm.before[wid] = upto;
+      __syncthreads();
+      int at = have + upto - here, all = have;
+      for (int w = 0; w < warps; ++w) {
+        if (w < wid) at += sm.before[w];
+        all += sm.before[w];
+      }
+      for (; found && at < k; found &= found - 1, ++at) sm.list[at] = key_of(nan ? kNan : least, first + (__ffs(found) - 1));
+      __syncthreads();
+      if (tid == 0) sm.count = min(all, k);
+      __syncthreads();
+    };
+    if (loose) take(tid < head && same(Vec<T>::one(x + tid)) ? 1u : 0u, tid);
+    for (int base = v0; base < v1 && sm.count < k; base += threads) {
+      uint32_t found = 0;
+      if (base + tid < v1) {
+        float e[kN];
+        Vec<T>::get(__ldg(p.xv + base + tid), e);
+#pragma unroll
+        for (int i = 0; i < kN; ++i) found |= (same(e[i]) ? 1u : 0u) << i;
+      }
+      take(found, head + (int64_t)(base + tid) * kN);
+    }
+    if (loose && sm.count < k) take(tid < vocab - tail && same(Vec<T>::one(x + tail + tid)) ? 1u : 0u, tail + tid);
+  }
+  const int have = sm.count;
+  for (int i = tid; i < have; i += threads) sm.best[i] = sm.list[i];
+  __syncthreads();
+  return have;
+}
+
+// Where the part of a row that a CTA has lies: 16-byte vectors from the row's first aligned entry on, v0 .. v1 of them the CTA's, a
+// warp's first round from `first` on, `len` long, the next `stride` further.  The entries before and behind the vectors go one by one.
 template <typename T>
-__global__ void __launch_bounds__(kMaxThreads) k_token_logprobs(const T* __restrict__ logits, int64_t stride, int vocab, int parts,
+struct Place {
+  const T* x;
+  const uint4* xv;
+  int head, tail, v0, v1, first, len, stride;
+  __device__ __forceinline__ Place(const T* row, int vocab, int part, int parts, int warp, int warps) : x(row) {
+    head = min(vocab, (int)((16 - ((uintptr_t)x & 15)) & 15) / (int)sizeof(T));
+    const int vecs = (vocab - head) / Vec<T>::n;
+    tail = head + vecs * Vec<T>::n;
+    const int each = (vecs + parts - 1) / parts;
+    v0 = min(vecs, part * each);
+    v1 = min(vecs, v0 + each);
+    len = v1 - v0 >= kRound * warps ? kRound : (v1 - v0 + warps - 1) / warps;  // (short parts: every warp has some)
+    first = v0 + warp * len;
+    stride = warps * len;
+    xv = reinterpret_cast<const uint4*>(x + head);
+  }
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kMaxThreads, 3) k_token_logprobs(const T* __restrict__ logits, int64_t row_stride, int rows, int vocab, int parts,
                                                                 const int32_t* __restrict__ tokens, int k, float* __restrict__ logprob,
                                                                 float* __restrict__ entropy, float* __restrict__ lse_out,
-                                                                int32_t* __restrict__ top_ids, float* __restrict__ top_logprobs) {
-  constexpr int kN = Vec<T>::n;
+                                                                int32_t* __restrict__ top_ids, float* __restrict__ top_logprobs, int32_t* status) {
+  constexpr int kN = Vec<T>::n, kPer = kN / 4;  // entries of a vector, of a word
+  static_assert(kAhead * 4 == 32, "a lane's round is 32 words");
   __shared__ Shared sm;
+  extern __shared__ __align__(128) uint4 ring[];  // [warps][kStages][kRound]
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, threads = blockDim.x, warps = threads >> 5;
-  const int64_t row = blockIdx.x / parts;
   const int part = parts > 1 ? (int)cluster_rank() : 0;
-  const T* __restrict__ x = logits + row * stride;
-  // 16-byte vectors from the row's first aligned entry on; the entries before and behind them go one by one
-  const int head = min(vocab, (int)((16 - ((uintptr_t)x & 15)) & 15) / (int)sizeof(T));
-  const int vecs = (vocab - head) / kN, tail = head + vecs * kN;
-  const int v0 = (int)((int64_t)vecs * part / parts), v1 = (int)((int64_t)vecs * (part + 1) / parts);
-  const uint4* __restrict__ xv = reinterpret_cast<const uint4*>(x + head);
-  if (tid == 0) sm.count = 0;
-  __syncthreads();
-
-  Stats st{kNegInf, 0.f, 0.f};
-  Key least = 0;  // a key of the CTA's part that k of its keys reach, or 0
-  float least_value = kNegInf;
-  auto push = [&](Key key) {
-    const int at = atomicAdd(&sm.count, 1);
-    if (at < kList) sm.list[at] = key;
-  };
-  auto consider = [&](float v, int64_t index) {
-    const Key key = key_of(v, index);
-    if (key >= least) push(key);
-  };
-  auto add_stats = [&](const float (&e)[kN]) {
-    float top = e[0];
-#pragma unroll
-    for (int i = 1; i < kN; ++i) top = fmaxf(top, e[i]);
-    if (top > st.m) stats_move(st, top);
-    if (st.m != kNegInf) {
-#pragma unroll
-      for (int i = 0; i < kN; ++i) stats_add(st, e[i]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < kN; ++i)
-        if (e[i] != e[i]) st.l = e[i];
-    }
-    return top;
-  };
-
-  if (k > 0 && v1 - v0 >= threads) {
-    // the first threshold, from the largest of every thread's first vector
-    float e[kN];
-    Vec<T>::get(xv[v0 + tid], e);
-    Key mine = 0;
-#pragma unroll
-    for (int i = 0; i < kN; ++i) mine = max(mine, key_of(e[i], head + (int64_t)(v0 + tid) * kN + i));
-    const int each = (k + warps - 1) / warps;
-    Key level = 0;
-    for (int j = 0; j < each; ++j) {
-      Key top = mine;
-#pragma unroll
-      for (int d = 16; d > 0; d >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
-      if (mine == top) mine = 0;
-      level = top;
-    }
-    if (lane == 0) sm.bound[wid] = level;
-    __syncthreads();
-    least = sm.bound[0];
-    for (int w = 1; w < warps; ++w) least = min(least, sm.bound[w]);
-    least_value = (uint32_t)(least >> 32) ? value_of((uint32_t)(least >> 32)) : kNegInf;
-  }
-
-  // the entries that no vector holds
-  if (part == 0 && tid < head + (vocab - tail)) {
-    const int i = tid < head ? tid : tail + (tid - head);
-    const float v = Vec<T>::one(x + i);
-    if (v > st.m) stats_move(st, v);
-    if (st.m != kNegInf) stats_add(st, v);
-    else if (v != v) st.l = v;
-    if (k > 0) consider(v, i);
-  }
-  for (int base = v0; base < v1; base += kAhead * threads) {
-    if (k > 0) {
-      __syncthreads();
-      const int before = sm.count;
-      if (before > kCutAt) {
-        cut(sm, k, least);
-        least_value = (uint32_t)(least >> 32) ? value_of((uint32_t)(least >> 32)) : kNegInf;
+  const int64_t first_row = blockIdx.x / parts, row_step = gridDim.x / parts;
+  // (three quarters of the warps: the least of all levels lies lower than that which all but two reach with more lanes)
+  const int want = k + kMargin, most_warps = warps - warps / 4, enough = (want + most_warps - 1) / most_warps, nth = (want + enough - 1) / enough;
+  // Lane 0 brings the warp's rounds, those of the next row behind those of this one, so that HBM is not left idle by a row's end.
+  uint4* my_ring = ring + wid * kStages * kRound;
+  int64_t bring_row = first_row;
+  const uint4* bring_from = nullptr;  // the next round of bring_row, null: its first
+  int bring_left = 0;                 // vectors from there to the end of the CTA's part
+  int bring_len = 0, bring_stride = 0;
+  uint32_t brought = 0, taken = 0;
+  auto bring = [&] {
+    for (; bring_row < rows; bring_row += row_step, bring_from = nullptr) {
+      if (bring_from == nullptr) {
+        const Place<T> p(logits + bring_row * row_stride, vocab, part, parts, wid, warps);
+        bring_from = p.xv + p.first;
+        bring_left = p.v1 - p.first;
+        bring_len = p.len;
+        bring_stride = p.stride;
+      }
+      if (bring_left > 0) {
+        const uint32_t bytes = (uint32_t)min(bring_len, bring_left) * 16u;
+        uint64_t* full = &sm.full[wid][brought % kStages];
+        mbar_arrive_expect_tx(full, bytes);
+        bulk_g2s(my_ring + (brought % kStages) * kRound, bring_from, bytes, full);
+        ++brought;
+        bring_from += bring_stride;
+        bring_left -= bring_stride;
+        return;
       }
     }
-    uint4 raw[kAhead];
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const int v = base + u * threads + tid;
-      raw[u] = v < v1 ? __ldg(xv + v) : make_uint4(0u, 0u, 0u, 0u);
+  };
+  if (lane == 0) {
+    for (int i = 0; i < kStages; ++i) mbar_init(&sm.full[wid][i], 1);
+    mbar_fence_init();
+    for (int i = 0; i < kStages; ++i) bring();
+  }
+  __syncwarp();
+
+  bool ok = true;
+  for (int64_t row = first_row; row < rows; row += row_step) {
+    const Place<T> p(logits + row * row_stride, vocab, part, parts, wid, warps);
+    const T* __restrict__ x = p.x;
+    const int head = p.head, tail = p.tail, v0 = p.v0, v1 = p.v1;
+    Stats st{kNegInf, 0.f, 0.f};
+    float least = kNegInf;  // more than k logits of the CTA's part reach it, or minus infinity
+    auto push = [&](float v, int64_t index) {
+      const int at = atomicAdd(&sm.count, 1);
+      if (at < kList) sm.list[at] = key_of(v, index);
+    };
+    if (lane == 0) sm.level[wid] = kLowest;
+    if (tid == 0) {
+      sm.count = 0;
+      sm.common = kLowest;
     }
-    const int start = k > 0 ? *(volatile int*)&sm.count : 0;
-    if (k > 0) __syncthreads();
+    // asked for here, used at the row's end
+    int token = -1;
+    float given = 0.f;
+    if (tid == 0 && part == 0 && tokens != nullptr) {
+      token = tokens[row];
+      if (token >= 0 && token < vocab) given = Vec<T>::one(x + token);
+    }
+    const int loose = part == 0 ? head + (vocab - tail) : 0;  // the entries that no vector holds: the first CTA's
+    const int my_loose = tid < head ? tid : tail + (tid - head);
+    float loose_value = kNegInf;
+    if (tid < loose) {
+      loose_value = Vec<T>::one(x + my_loose);
+      if (loose_value > st.m) st.m = loose_value;
+      stats_add(st, loose_value);
+    }
+    uint64_t l2 = 0ull, s2 = 0ull;  // l and s of the vectors, two halves
+    auto fold = [&] {
+      float lo, hi;
+      f2_unpack(l2, lo, hi);
+      st.l += lo + hi;
+      f2_unpack(s2, lo, hi);
+      st.s += lo + hi;
+      l2 = s2 = 0ull;
+    };
+    float seen = st.m;  // the thread's largest logit; st.m, what its sums are relative to, follows when it is left far behind
+    int round = 0;
+    for (int base = v0; base < v1; base += p.stride, ++round) {
+      const int begin = base + (p.first - v0), end = min(v1, begin + p.len);
+      const uint4* piece = my_ring + (taken % kStages) * kRound;
+      if (begin < v1) {
+        ok = ok && mbar_wait(&sm.full[wid][taken % kStages], (taken / kStages) & 1u, status);
+        ++taken;
+      }
+      __syncwarp();
+      uint4 raw[kAhead];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const int v = base + u * threads + tid;
-      if (v < v1) {
-        float e[kN];
-        Vec<T>::get(raw[u], e);
-        const float top = add_stats(e);
-        if (k > 0 && !(top < least_value)) {
+      for (int u = 0; u < kAhead; ++u) raw[u] = piece[u * 32 + lane];
+      if (begin + kRound > end) {
 #pragma unroll
-          for (int i = 0; i < kN; ++i) consider(e[i], head + (int64_t)v * kN + i);
+        for (int u = 0; u < kAhead; ++u)
+          if (begin + u * 32 + lane >= end) raw[u] = make_uint4(Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing);
+      }
+      const float most = Vec<T>::largest(raw);
+      seen = fmaxf(seen, most);
+      if (seen > st.m + kLag || st.m == kNegInf) {  // (a lag of 4 leaves a sum's terms below 2^6 and costs 2^-24 of it in the entropy)
+        fold();
+        if (seen > st.m) stats_move(st, seen);
+      }
+      if (k > 0) {
+        if (round == 0 || round == 2 || (round & 7) == 5) {  // (a level rises less and less)
+          publish(sm, seen, enough);
+          if (round == 0) __syncthreads();  // (nothing is listed before all warps have one)
+          const float level = common_level(sm, nth, warps);
+          if (lane == 0) atomicMax(&sm.common, order_of(level));
+          least = level;
+        } else {
+          least = value_of(*(volatile uint32_t*)&sm.common);
         }
+        if (round == 0 && loose_value > least) push(loose_value, my_loose);
       }
-    }
-    if (k > 0) {
-      __syncthreads();
-      if (sm.count > kList) {
-        // more reached the threshold than the list holds: once more from where this round began, one entry of each thread at a time
-        __syncthreads();
-        if (tid == 0) sm.count = start;
-        __syncthreads();
-#pragma unroll 1
+      if (__all_sync(0xffffffffu, fabsf(st.m) < kFar || st.m == kNegInf)) {
+        const float c = st.m == kNegInf ? 0.f : -(st.m * kLog2e);  // (no logit with a probability yet: any reference will do)
+        const uint64_t cc = f2_pack(c, c), ee = f2_pack(kLog2e, kLog2e);
+#pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-          const int v = base + u * threads + tid;
+          float e[kN];
+          Vec<T>::get(raw[u], e);
+#pragma unroll
+          for (int i = 0; i < kN; i += 2) {
+            float d0, d1;
+            f2_unpack(f2_fma(f2_pack(e[i], e[i + 1]), ee, cc), d0, d1);
+            d0 = max_nan(d0, -1000.f);
+            d1 = max_nan(d1, -1000.f);
+            const uint64_t p2 = f2_pack(fast_exp2(d0), fast_exp2(d1));
+            l2 = f2_add(l2, p2);
+            s2 = f2_fma(p2, f2_pack(d0, d1), s2);
+          }
+        }
+      } else {
 #pragma unroll 1
-          for (int i = 0; i < kN; ++i) {
-            if (sm.count > kList - threads) {
-              cut(sm, k, least);
-              least_value = (uint32_t)(least >> 32) ? value_of((uint32_t)(least >> 32)) : kNegInf;
-            }
-            __syncthreads();
-            if (v < v1) consider(Vec<T>::one(x + head + (int64_t)v * kN + i), head + (int64_t)v * kN + i);
-            __syncthreads();
+        for (int v = lane; v < end - begin; v += 32)
+#pragma unroll 1
+          for (int i = 0; i < kN; ++i) stats_add(st, Vec<T>::one(reinterpret_cast<const T*>(piece + v) + i));
+      }
+      if (k > 0) {
+        // a lane that has a logit above the least: the warp looks at its entries, 32 words of them
+        for (uint32_t who = __ballot_sync(0xffffffffu, most > least); who; who &= who - 1) {
+          const int at = (lane >> 2) * 32 + __ffs(who) - 1;
+          float e[kPer];
+          Vec<T>::word(reinterpret_cast<const uint32_t*>(piece + at)[lane & 3], e);
+          if (begin + at < end) {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+              if (e[i] > least) push(e[i], head + (int64_t)(begin + at) * kN + (lane & 3) * kPer + i);
           }
         }
       }
+      __syncwarp();
+      if (lane == 0 && ok && begin < v1) bring();
     }
-  }
-
-  // the CTA's part
+    fold();
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) {
-    Stats o;
-    o.m = __shfl_xor_sync(0xffffffffu, st.m, d);
-    o.l = __shfl_xor_sync(0xffffffffu, st.l, d);
-    o.s = __shfl_xor_sync(0xffffffffu, st.s, d);
-    st = stats_join(st, o);
-  }
-  if (lane == 0) sm.stats[wid] = st;
-  __syncthreads();
-  if (k > 0) cut(sm, k, least);
-  if (tid == 0) {
-    st = sm.stats[0];
-    for (int w = 1; w < warps; ++w) st = stats_join(st, sm.stats[w]);
-    sm.part = st;
-  }
-  __syncthreads();
-  if (parts > 1) {
-    if (k > 0)
-      for (int i = sm.count + tid; i < kMaxTop; i += threads) sm.best[i] = 0;
+    for (int d = 16; d > 0; d >>= 1) {
+      Stats o;
+      o.m = __shfl_xor_sync(0xffffffffu, st.m, d);
+      o.l = __shfl_xor_sync(0xffffffffu, st.l, d);
+      o.s = __shfl_xor_sync(0xffffffffu, st.s, d);
+      st = stats_join(st, o);
+    }
+    if (lane == 0) sm.stats[wid] = st;
     __syncthreads();
-    cluster_sync();
-    if (part == 0) {
-      if (tid < 32) {
-        Stats a{kNegInf, 0.f, 0.f};
-        for (int p = 0; p < parts; ++p) {
-          Stats b;
-          b.m = peer_float(&sm.part.m, p); b.l = peer_float(&sm.part.l, p); b.s = peer_float(&sm.part.s, p);
-          a = stats_join(a, b);
-        }
-        st = a;
-      }
-      if (k > 0) {
-        for (int i = tid; i < parts * k; i += threads) sm.join[i] = peer_key(&sm.best[i % k], i / k);
+    int have = 0;  // the largest of the CTA's part: best[0 .. have)
+    if (k > 0) {
+      if (v0 >= v1) {  // a row that is no longer than its loose entries
+        if (tid < loose && loose_value > kNegInf) push(loose_value, my_loose);
         __syncthreads();
-        for (int i = tid; i < parts * k; i += threads) {
-          const Key key = sm.join[i];
+      }
+      least = value_of(sm.common);
+      have = finish<T>(sm, k, least, p, loose, my_loose, vocab, warps);
+    }
+
+    if (wid == 0) {
+      st = lane < warps ? sm.stats[lane] : Stats{kNegInf, 0.f, 0.f};
+#pragma unroll
+      for (int d = kMaxThreads / 64; d > 0; d >>= 1) {
+        Stats o;
+        o.m = __shfl_xor_sync(0xffffffffu, st.m, d);
+        o.l = __shfl_xor_sync(0xffffffffu, st.l, d);
+        o.s = __shfl_xor_sync(0xffffffffu, st.s, d);
+        st = stats_join(st, o);
+      }
+      st.m = __shfl_sync(0xffffffffu, st.m, 0);
+      st.l = __shfl_sync(0xffffffffu, st.l, 0);
+      st.s = __shfl_sync(0xffffffffu, st.s, 0);
+    }
+    if (parts > 1) {
+      if (tid == 0) sm.part = st;
+      for (int i = have + tid; i < k; i += threads) sm.best[i] = 0;
+      __syncthreads();
+      cluster_sync();
+      if (part == 0) {
+        if (wid == 0) {
+          st = Stats{kNegInf, 0.f, 0.f};
+          for (int i = 0; i < parts; ++i) {
+            Stats o;
+            o.m = peer_float(&sm.part.m, i); o.l = peer_float(&sm.part.l, i); o.s = peer_float(&sm.part.s, i);
+            st = stats_join(st, o);
+          }
+        }
+        if (k > 0) {
+          Key mine = 0;
+          if (tid < parts * k) sm.join[tid] = mine = peer_key(&sm.best[tid % k], tid / k);
+          __syncthreads();
           int above = 0;
-          for (int j = 0; j < parts * k; ++j) above += sm.join[j] > key;
-          if (key != 0 && above < k) sm.list[above] = key;
+          if (mine != 0)
+            for (int j = 0; j < parts * k; ++j) above += sm.join[j] > mine;
+          __syncthreads();
+          if (mine != 0 && above < k) sm.list[above] = mine;  // (not to best, which the others may still read)
         }
       }
+      __syncthreads();
+      cluster_sync();  // nobody leaves while its shared memory is read
     }
-    __syncthreads();
-    cluster_sync();  // nobody leaves while its shared memory is read
-    if (part != 0) return;
-  } else if (tid < 32) {
-    st = sm.part;
-  }
-  if (tid >= 32) return;
-  // l is NaN where a logit is; nothing but minus infinity leaves l = 0
-  if (st.m == -kNegInf) st.l = __int_as_float(0x7fffffff);
-  // (log probabilities relative to m: lse itself may be too large to hold ln l)
-  const float log_sum = logf(st.l), lse = st.l == 0.f ? kNegInf : st.m + log_sum;
-  auto of = [&](float v) { return lse == kNegInf ? lse : v - st.m - log_sum; };
-  if (lane == 0) {
-    const int token = tokens != nullptr ? tokens[row] : -1;
-    if (logprob != nullptr) {
-      float lp = 0.f;
-      if (token != -1) {
-        if (token < 0 || token >= vocab) lp = __int_as_float(0x7fffffff);
-        else lp = of(Vec<T>::one(x + token));
+    if (wid == 0 && part == 0) {
+      // l is NaN where a logit is; nothing but minus infinity leaves l = 0
+      if (st.m == -kNegInf) st.l = kNan;
+      // (log probabilities relative to m: lse itself may be too large to hold ln l)
+      const float log_sum = logf(st.l), lse = st.l == 0.f ? kNegInf : st.m + log_sum;
+      auto of = [&](float v) { return lse == kNegInf ? lse : (fabsf(v) < kFar ? diff(v, st.m) * kLn2 : v - st.m) - log_sum; };
+      if (lane == 0) {
+        if (logprob != nullptr) logprob[row] = token == -1 ? 0.f : token < 0 || token >= vocab ? kNan : of(given);
+        if (entropy != nullptr) entropy[row] = st.l == 0.f ? 0.f : log_sum - kLn2 * (st.s / st.l);
+        if (lse_out != nullptr) lse_out[row] = lse;
       }
-      logprob[row] = lp;
+      if (lane < k) {
+        const Key key = (parts > 1 ? sm.list : sm.best)[lane];
+        if (top_ids != nullptr) top_ids[row * k + lane] = (int32_t)~(uint32_t)key;
+        if (top_logprobs != nullptr) top_logprobs[row * k + lane] = of(value_of((uint32_t)(key >> 32)));
+      }
     }
-    if (entropy != nullptr) entropy[row] = st.l == 0.f ? 0.f : log_sum - kLn2 * (st.s / st.l);
-    if (lse_out != nullptr) lse_out[row] = lse;
+    if (__syncthreads_or(!ok)) break;
   }
-  for (int i = lane; i < k; i += 32) {
-    const Key key = sm.list[i];
-    if (top_ids != nullptr) top_ids[row * k + i] = (int32_t)~(uint32_t)key;
-    if (top_logprobs != nullptr) top_logprobs[row * k + i] = of(value_of((uint32_t)(key >> 32)));
-  }
+  if (lane == 0)  // where it gave up, its copies on the way land before the memory is another's
+    for (uint32_t i = taken < brought ? taken : brought; i < brought; ++i) mbar_drain(&sm.full[wid][i % kStages], (i / kStages) & 1u, status);
 }
 
 }  // namespace
 
 int launch_token_logprobs(const void* logits, int fp32, int64_t stride, int rows, int vocab, const int32_t* tokens, int top, float* logprob,
-                          float* entropy, float* lse, int32_t* top_ids, float* top_logprobs, int num_sms, cudaStream_t st) {
+                          float* entropy, float* lse, int32_t* top_ids, float* top_logprobs, int num_sms, int32_t* status, cudaStream_t st) {
   // CTAs per row: until two per multiprocessor have work, a part not below 4096 entries
   int parts = 1;
   while (parts < kMaxCluster && (int64_t)rows * parts * 2 <= 2 * num_sms && vocab / (parts * 2) >= 4096) parts *= 2;
   const int per_vec = fp32 ? 4 : 8, vecs = vocab / parts / per_vec;
-  const int threads = vecs >= 1024 ? 512 : vecs >= 256 ? 256 : 128;
+  const int threads = vecs < 256 ? kMinThreads : kMaxThreads;
+  const size_t smem = (size_t)(threads / 32) * kStages * kRound * 16;
+  static bool done[2][kMaxDevices];
+  if (!(fp32 ? ensure_dynamic_smem(k_token_logprobs<float>, kMaxThreads / 32 * kStages * kRound * 16, done[0])
+             : ensure_dynamic_smem(k_token_logprobs<__nv_bfloat16>, kMaxThreads / 32 * kStages * kRound * 16, done[1])))
+    return -1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(rows * parts));
   cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -403,10 +687,10 @@ int launch_token_logprobs(const void* logits, int fp32, int64_t stride, int rows
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = parts > 1 ? 1 : 0;
-  const cudaError_t e = fp32 ? cudaLaunchKernelEx(&cfg, k_token_logprobs<float>, (const float*)logits, stride, vocab, parts, tokens, top, logprob,
-                                                  entropy, lse, top_ids, top_logprobs)
-                             : cudaLaunchKernelEx(&cfg, k_token_logprobs<__nv_bfloat16>, (const __nv_bfloat16*)logits, stride, vocab, parts, tokens,
-                                                  top, logprob, entropy, lse, top_ids, top_logprobs);
+  const cudaError_t e = fp32 ? cudaLaunchKernelEx(&cfg, k_token_logprobs<float>, (const float*)logits, stride, rows, vocab, parts, tokens, top, logprob,
+                                                  entropy, lse, top_ids, top_logprobs, status)
+                             : cudaLaunchKernelEx(&cfg, k_token_logprobs<__nv_bfloat16>, (const __nv_bfloat16*)logits, stride, rows, vocab, parts, tokens,
+                                                  top, logprob, entropy, lse, top_ids, top_logprobs, status);
   return e == cudaSuccess ? 1 : -1;
 }
 
