@@ -529,7 +529,8 @@ gf_status_t gf_edge_scores(gf_wgraph_t* g, const gf_scorer_t* model, const float
  *   y[t] = W x[t] + scale[a] B[a] (A[a] x[t]),   a = adapter[t]; -1: no adapter.
  * bf16 row-major, caller-owned, 16-byte aligned; A [num_adapters, rank, in_dim], B [num_adapters, out_dim, rank], contiguous;
  * scale NULL: 1.  in_dim and w_stride (entries between rows of W) are multiples of 8; rank a multiple of 8, at most 64
- * (adapters of a smaller rank are filled up with zeros); num_adapters 0: none. */
+ * (adapters of a smaller rank are filled up with zeros); num_adapters at most GF_MAX_ADAPTERS, 0: none. */
+#define GF_MAX_ADAPTERS 32768
 typedef struct {
   int32_t in_dim, out_dim;
   const void* w_dev; /* [out_dim, in_dim] */
@@ -540,7 +541,7 @@ typedef struct {
   const float* scale_dev; /* fp32 [num_adapters] */
 } gf_projection_t;
 
-/* Scratch of a call with adapters: fp32, 16-byte aligned; two calls that may overlap on the GPU each need their own. */
+/* Scratch of a call with adapters, 16-byte aligned: up to 512 bytes per rank, row and 256 adapters, for at most 16 384 rows at a time; two calls that may overlap on the GPU each need their own. */
 uint64_t gf_adapter_project_scratch_bytes(const gf_projection_t* p, int32_t rows);
 
 /* x_dev: bf16 [rows, in_dim], rows x_stride entries apart (a multiple of 8), 16-byte aligned.  adapter_dev: int32 [rows], or NULL for

@@ -1408,7 +1408,7 @@ gf_status_t gf_edge_scores(gf_wgraph_t* g, const gf_scorer_t* m, const float* x_
 
 static bool projection_ok(const gf_projection_t* p) {
   if (!p || p->in_dim < 8 || (p->in_dim & 7) || p->out_dim < 1 || !p->w_dev || ((uintptr_t)p->w_dev & 15) || p->w_stride < p->in_dim ||
-      (p->w_stride & 7) || p->w_stride > (1ll << 38) || p->num_adapters < 0)
+      (p->w_stride & 7) || p->w_stride > (1ll << 38) || p->num_adapters < 0 || p->num_adapters > GF_MAX_ADAPTERS)
     return false;
   if (p->num_adapters == 0) return true;
   return p->rank >= 8 && p->rank <= 64 && (p->rank & 7) == 0 && p->a_dev && p->b_dev && !(((uintptr_t)p->a_dev | (uintptr_t)p->b_dev) & 15) &&
@@ -1417,7 +1417,7 @@ static bool projection_ok(const gf_projection_t* p) {
 
 uint64_t gf_adapter_project_scratch_bytes(const gf_projection_t* p, int32_t rows) {
   if (!projection_ok(p) || rows < 1 || p->num_adapters == 0) return 0;
-  return (uint64_t)project_parts(p->in_dim) * (uint64_t)rows * (uint64_t)p->rank * 4;
+  return (uint64_t)project_scratch_bytes(rows, p->rank, p->num_adapters);
 }
 
 gf_status_t gf_adapter_project(gf_wgraph_t* g, const gf_projection_t* p, int32_t rows, const void* x_dev, int64_t x_stride,
@@ -1436,7 +1436,7 @@ gf_status_t gf_adapter_project(gf_wgraph_t* g, const gf_projection_t* p, int32_t
   }
   DeviceGuard dev(g->device);
   if (!dev.ok) return GF_ERR_CUDA;
-  const int n = launch_project(*p, rows, x_dev, x_stride, adapter_dev, y_dev, y_stride, y_fp32, (float*)scratch_dev, g->num_sms, g->status_dev,
+  const int n = launch_project(*p, rows, x_dev, x_stride, adapter_dev, y_dev, y_stride, y_fp32, scratch_dev, g->num_sms, g->status_dev,
                                (cudaStream_t)stream);
   if (n < 0) return GF_ERR_CUDA;
   g->launches += n;

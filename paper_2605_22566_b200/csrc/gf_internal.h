@@ -342,10 +342,9 @@ int launch_weights(const PoolGeom& pool16, const PoolGeom& pool4, const AttnShap
                    cudaStream_t st, cudaStream_t side);
 int launch_evict(const PoolGeom& pool16, const PoolGeom& pool4, const EvictBatch& batch, int num_layers, int num_kv_heads,
                  int head_dim, float* weights, int64_t slots, int32_t* kept, const GraphDev& g, cudaStream_t st);
-// parts that the adapters' inner results come in: rows * rank floats of scratch each.
-int project_parts(int in_dim);
+size_t project_scratch_bytes(int rows, int rank, int num_adapters);  // with adapters
 int launch_project(const gf_projection_t& p, int rows, const void* x, int64_t x_stride, const int32_t* adapter, void* y, int64_t y_stride, int y_fp32,
-                   float* scratch, int num_sms, int32_t* status, cudaStream_t st);
+                   void* scratch, int num_sms, int32_t* status, cudaStream_t st);
 int launch_token_logprobs(const void* logits, int fp32, int64_t stride, int rows, int vocab, const int32_t* tokens, int top, float* logprob,
                           float* entropy, float* lse, int32_t* top_ids, float* top_logprobs, int num_sms, int32_t* status, cudaStream_t st);
 int launch_wait_probe(int32_t* status, long long limit, int32_t* returned, cudaStream_t st);
