@@ -9,8 +9,11 @@
 // The adapters are more entries of K.  For every adapter that rows of a tile of x name (a slot of the tile), h = scale_a A_a x is a
 // [rows, rank] operand with zeros in the other rows, and B_a, [features, rank], stands beside W: the sums go on over the tile's
 // slots, in the same pipeline, and nothing is left for the warps that take them out of tensor memory.  h is rounded to two bf16
-// numbers, its nearest and the nearest of what is left (2^-17 of it), and multiplied twice.  k_adapter_down writes these operands in the layout
-// of shared memory; only the copies behind a tile's last entry of W wait for it.
+// numbers, its nearest and the nearest of what is left (2^-17 of it), and multiplied twice.
+// A x goes the same way as W x: the rows of the A of 8, 4 or 2 slots (of rank 16, 32, 64) stand in W's place, for all rows of the tile, and
+// what comes out is kept where row and slot belong together and written as those operands, in the layout of shared memory.
+// Three launches: the slots, A x, W x; only the copies behind a tile's last entry of W wait for the second.  (Few rows: the first two are
+// one, k_adapter_rows.)
 // (The same sums on the CUDA cores, while the MMAs ran, took 568 us for 8192 rows with adapters of rank 16 and 1143 of rank 64,
 // where W x alone takes 295: their reads of B and h wait behind the copies' traffic.)
 #include <cuda.h>
@@ -31,6 +34,8 @@ constexpr int kGroup = 8;         // rows of x that are taken out of tensor memo
 struct Slots {
   int32_t* count;        // [row_tiles]
   int32_t* adapter;      // [row_tiles][most]
+  int32_t* of_row;       // [rows] a row's slot in its tile, -1: none
+  const float* scale;    // [num_adapters] or null
   char* h;               // [row_tiles][most][2][nt][padded rank], swizzled like a stage's operand
   int most;
   int rank, padded;      // padded: 16, 32 or 64
@@ -40,12 +45,13 @@ struct Slots {
 struct ProjectArgs {
   int rows, in_dim, out_dim, nt;        // nt: rows of x in a tile
   int feat_tiles, row_tiles, stages;
+  int pair;                             // stages that are given back together: 1 or 2
   int splits;                           // CTAs that share a tile
   uint32_t tmem_cols, acc_cols;         // allocated; from one accumulator to the next
   Slots slots;
   void* y;
   int64_t y_stride;
-  int y_fp32;
+  int y_fp32, y_vec;                    // y_vec: four neighbouring results can be stored at once
   int32_t* status;
 };
 
@@ -61,8 +67,6 @@ __device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
                : "r"(taddr)
                : "memory");
 }
-
-__device__ __forceinline__ uint64_t bf16x2_to_f2(uint32_t v) { return f2_pack(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)); }
 
 __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
   asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(smem_u32(dst)),
@@ -81,6 +85,25 @@ __device__ __forceinline__ uint32_t operand_at(int r, int c, int row_bytes) {
   return (uint32_t)(r * row_bytes + ((c ^ x) << 4));
 }
 
+__device__ __forceinline__ uint64_t bf16x2_to_f2(uint32_t v) { return f2_pack(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)); }
+
+// Four MMAs along a stage's 64 entries of K, 32 bytes apart in both operands.  (In one block: the issuing thread is alone on its
+// scheduler, and with few rows of x its instructions between the MMAs are what takes the time.)
+__device__ __forceinline__ void umma_ss4(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, t;\n\t.reg .b64 a, b;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\tsetp.eq.b32 t, 0, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t"
+      "add.s64 a, %1, 2;\n\tadd.s64 b, %2, 2;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n\t"
+      "add.s64 a, %1, 4;\n\tadd.s64 b, %2, 4;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n\t"
+      "add.s64 a, %1, 6;\n\tadd.s64 b, %2, 6;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n\t}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
 __device__ __forceinline__ void store_y(const ProjectArgs& a, int row, int feat, float v) {
   if (feat < a.out_dim && row >= 0 && row < a.rows) {
     const int64_t at = (int64_t)row * a.y_stride + feat;
@@ -89,15 +112,74 @@ __device__ __forceinline__ void store_y(const ProjectArgs& a, int row, int feat,
   }
 }
 
+// (a warp's lanes together; every warp of every CTA of the cluster takes part in each barrier)
 __device__ __forceinline__ void cluster_sync_all() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// What a launch is: W x alone, W x with the adapters behind it, or A x for the adapters.
+enum { kPlain = 0, kWith = 1, kDown = 2 };
+
+// Four results of a row at features f .. f + 3.
+__device__ __forceinline__ void store_y4(const ProjectArgs& a, int row, int f, float4 v) {
+  const int64_t at = (int64_t)row * a.y_stride + f;
+  if (a.y_vec && f + 3 < a.out_dim) {
+    if (a.y_fp32) *reinterpret_cast<float4*>(static_cast<float*>(a.y) + at) = v;
+    else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.y) + at) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+  } else {
+    store_y(a, row, f, v.x);
+    store_y(a, row, f + 1, v.y);
+    store_y(a, row, f + 2, v.z);
+    store_y(a, row, f + 3, v.w);
+  }
+}
+// Where the results of row `m` of a tile of A's go: into a slot's operands, scaled.
+struct HPlace {
+  char* at;      // the slot's first operand; null: no slot, or beyond the rank's padding
+  int slot, r;   // the slot, the rank
+  float scale;   // 0 beyond the rank
+  __device__ HPlace() : at(nullptr), slot(-1), r(0), scale(0.f) {}
+  __device__ HPlace(const Slots& sl, int row_tile, int first_slot, int slots, int m) {
+    const int j = m / sl.padded;
+    r = m - j * sl.padded;
+    slot = first_slot + j;
+    at = slot < slots ? sl.h + ((int64_t)row_tile * sl.most + slot) * 2 * sl.block : nullptr;
+    scale = 0.f;
+    if (at != nullptr && r < sl.rank) scale = sl.scale != nullptr ? __ldg(sl.scale + __ldcg(sl.adapter + (int64_t)row_tile * sl.most + slot)) : 1.f;
+  }
+};
+__device__ __forceinline__ void split_h(float v, __nv_bfloat16& first, __nv_bfloat16& left) {
+  first = __float2bfloat16_rn(v);
+  left = __float2bfloat16_rn(fabsf(v) <= 3.3895e38f ? v - __bfloat162float(first) : 0.f);  // (nothing is left of an infinity, or a NaN)
+}
+// One result, or four of neighbouring ranks, of a row; zeros where the row is another slot's.
+__device__ __forceinline__ void store_h(const Slots& sl, const HPlace& p, int row_in_tile, int row_slot, float v) {
+  if (p.at == nullptr) return;
+  __nv_bfloat16 first, left;
+  split_h(row_slot == p.slot && p.r < sl.rank ? v * p.scale : 0.f, first, left);
+  char* at = p.at + operand_at(row_in_tile, p.r >> 3, sl.padded * 2) + (p.r & 7) * 2;
+  *reinterpret_cast<__nv_bfloat16*>(at) = first;
+  *reinterpret_cast<__nv_bfloat16*>(at + sl.block) = left;
+}
+__device__ __forceinline__ void store_h4(const Slots& sl, const HPlace& p, int row_in_tile, int row_slot, float4 v) {
+  if (p.at == nullptr) return;
+  const bool mine = row_slot == p.slot && p.r < sl.rank;  // (ranks are multiples of 8)
+  __align__(8) __nv_bfloat16 first[4], left[4];
+  split_h(mine ? v.x * p.scale : 0.f, first[0], left[0]);
+  split_h(mine ? v.y * p.scale : 0.f, first[1], left[1]);
+  split_h(mine ? v.z * p.scale : 0.f, first[2], left[2]);
+  split_h(mine ? v.w * p.scale : 0.f, first[3], left[3]);
+  char* at = p.at + operand_at(row_in_tile, p.r >> 3, sl.padded * 2) + (p.r & 7) * 2;
+  *reinterpret_cast<uint2*>(at) = *reinterpret_cast<uint2*>(first);
+  *reinterpret_cast<uint2*>(at + sl.block) = *reinterpret_cast<uint2*>(left);
 }
 
 // Shared memory: the ring of stages (kFeat rows of W, then nt rows of x, 128 bytes each, 128-byte swizzle; a stage of the
 // adapters holds one slot of rank 32, two of rank 16, or the first or second half of one of rank 64), which a cluster uses
 // again for its parts of the sums; behind it the barriers.
-template <bool kAdapters>
-__global__ void __launch_bounds__(kThreads, 1) k_project(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map,
+// Warp 0 issues the copies, warp 1 the MMAs, warps 4 to 7 take the sums out; the parts of a cluster are joined by all.
+template <int kMode>
+__global__ void __launch_bounds__(kThreads, 2) k_project(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map,
                                                          const __grid_constant__ CUtensorMap b_map, const __grid_constant__ ProjectArgs a) {
   extern __shared__ __align__(1024) char smem_raw[];
   char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -117,11 +199,35 @@ __global__ void __launch_bounds__(kThreads, 1) k_project(const __grid_constant__
   const Slots& sl = a.slots;
   const int h_row = sl.padded * 2;                       // bytes of a row of h, and of B's
   const uint32_t b_bytes = kFeat * (uint32_t)h_row;
-  // the CTA's slots of a tile of x
-  auto my_slots = [&](int row_tile, int& s0, int& s1) {
-    const int n = *(volatile int32_t*)(sl.count + row_tile);
-    s0 = n * part / a.splits;
-    s1 = n * (part + 1) / a.splits;
+  const int per_tile = kMode == kDown ? kFeat / sl.padded : 1;  // slots whose A a tile takes
+  auto slots_of = [&](int row_tile) { return *(volatile int32_t*)(sl.count + row_tile); };
+  // The tiles of a CTA or cluster: features f of W (or slots, from f * per_tile on) and rows r of x.  Those of A x are only as many as there
+  // are slots, so a tile of x is left when they end.
+  struct Tile { int index, f, r, slots; };
+  const int f_step = max(1, groups / a.row_tiles);
+  auto more = [&](const Tile& t) { return kMode == kDown ? t.r < a.row_tiles : t.index < tiles; };
+  auto settle = [&](Tile& t) {
+    if (kMode == kDown) {
+      while (t.r < a.row_tiles && t.f * per_tile >= t.slots) {
+        t.r += groups;
+        t.f = 0;
+        t.slots = t.r < a.row_tiles ? slots_of(t.r) : 0;
+      }
+    } else {
+      t.r = t.index / a.feat_tiles;
+      t.f = t.index - t.r * a.feat_tiles;
+    }
+  };
+  auto start = [&] {
+    Tile t{group, group / a.row_tiles, group % a.row_tiles, 0};
+    if (kMode == kDown) t.slots = slots_of(t.r);
+    settle(t);
+    return t;
+  };
+  auto advance = [&](Tile& t) {
+    t.index += groups;
+    t.f += f_step;
+    settle(t);
   };
   if (tid == 0) {
     for (int i = 0; i < a.stages; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, 1); }
@@ -134,193 +240,282 @@ __global__ void __launch_bounds__(kThreads, 1) k_project(const __grid_constant__
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = *tmem_slot;
+  if (kMode == kDown) {
+    // (the slots are there when all CTAs of the kernel before have ended; those of the next may start when all of these have begun)
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+  }
 
-  if (wid == 0) {
-    if (lane == 0) {
-      int s = 0;
-      int64_t issued = 0;
-      uint32_t phase = 0;
-      bool ok = true, waited = false;
-      auto next = [&] { if (++s == a.stages) { s = 0; phase ^= 1u; } ++issued; };
-      for (int tile = group; tile < tiles && ok; tile += groups) {
-        const int f0 = (tile % a.feat_tiles) * kFeat, row_tile = tile / a.feat_tiles, t0 = row_tile * a.nt;
-        int s0 = 0, s1 = 0;
-        if (kAdapters && waited) my_slots(row_tile, s0, s1);  // (asked for here, used behind the loop)
-        for (int k = step0; k < step1; ++k) {
-          if (!(ok = mbar_wait(empty + s, phase ^ 1u, a.status))) break;
-          mbar_arrive_expect_tx(full + s, stage_bytes);
-          tma_load_2d(smem + s * stage_bytes, &w_map, k * kStep, f0, full + s);
-          tma_load_2d(smem + s * stage_bytes + w_bytes, &x_map, k * kStep, t0, full + s);
-          next();
-        }
-        if (kAdapters && ok) {
-          if (!waited) {
-            asm volatile("griddepcontrol.wait;" ::: "memory");  // the slots are the kernel's before this one
-            waited = true;
-            my_slots(row_tile, s0, s1);
-          }
+  int s = 0;           // the role's stage and its phase
+  uint32_t phase = 0;
+  uint32_t used = 0, phases = 0;  // stages that copies have been issued for, and the last phase of each
+  int done = 0;                   // tiles
+  bool ok = true, waited = kMode != kWith;
+  // A CTA by itself goes through its tiles in one round, so that the roles run ahead of each other; a cluster takes a round per tile.
+  Tile now = start();
+  while (more(now)) {
+    if (wid == 0) {
+      if (lane == 0) {
+        auto free = [&] { return s % a.pair != 0 || mbar_wait(empty + s / a.pair, phase ^ 1u, a.status); };
+        auto next = [&] {
+          used |= 1u << s;
+          phases = (phases & ~(1u << s)) | phase << s;
+          if (++s == a.stages) { s = 0; phase ^= 1u; }
+        };
+        for (Tile t = now; more(t) && ok; advance(t)) {
+          const int f = t.f, f0 = f * kFeat, row_tile = t.r, t0 = row_tile * a.nt;
           const int32_t* which = sl.adapter + (int64_t)row_tile * sl.most;
-          int ahead[2] = {s0 < s1 ? __ldcg(which + s0) : 0, s0 + 1 < s1 ? __ldcg(which + s0 + 1) : 0};  // of the next two slots
-          const char* h = sl.h + (int64_t)row_tile * sl.most * 2 * sl.block;
-          for (int i = s0; i < s1 && ok; ++i) {
+          int s0 = 0, s1 = 0, ids[8];
+          if (kMode == kWith && waited) s1 = slots_of(row_tile);  // (asked for here, used behind the loop)
+          if (kMode == kDown) {
+            s1 = min(per_tile, t.slots - f * per_tile);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) ids[j] = j < s1 ? __ldcg(which + f * per_tile + j) : 0;
+          }
+          for (int k = step0; k < step1; ++k) {
+            if (!(ok = free())) break;
             char* at = smem + s * stage_bytes;
-            const int id = ahead[0], id2 = ahead[1];
-            const int taken = h_row == 32 ? 2 : 1;
-            ahead[0] = taken == 2 ? (i + 2 < s1 ? __ldcg(which + i + 2) : 0) : id2;
-            ahead[1] = i + taken + 1 < s1 ? __ldcg(which + i + taken + 1) : 0;
-            if (!(ok = mbar_wait(empty + s, phase ^ 1u, a.status))) break;
-            if (h_row == 128) {
-              for (int half = 0; half < 2 && ok; ++half) {
-                at = smem + s * stage_bytes;
-                if (half && !(ok = mbar_wait(empty + s, phase ^ 1u, a.status))) break;
-                mbar_arrive_expect_tx(full + s, b_bytes + sl.block);
-                tma_load_3d(at, &b_map, 0, f0, id, full + s);
-                bulk_g2s(at + w_bytes, h + (int64_t)(2 * i + half) * sl.block, sl.block, full + s);
-                next();
-              }
-            } else if (h_row == 64) {
-              mbar_arrive_expect_tx(full + s, b_bytes + 2 * sl.block);
-              tma_load_3d(at, &b_map, 0, f0, id, full + s);
-              bulk_g2s(at + w_bytes, h + (int64_t)(2 * i) * sl.block, 2 * sl.block, full + s);
-              next();
+            if (kMode == kDown) {
+              mbar_arrive_expect_tx(full + s, s1 * sl.rank * 128u + x_bytes);
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                if (j < s1) tma_load_2d(at + j * sl.padded * 128, &w_map, k * kStep, ids[j] * sl.rank, full + s);
             } else {
-              const int both = i + 1 < s1 ? 2 : 1;
-              mbar_arrive_expect_tx(full + s, both * (b_bytes + 2 * sl.block));
-              tma_load_3d(at, &b_map, 0, f0, id, full + s);
-              if (both == 2) tma_load_3d(at + b_bytes, &b_map, 0, f0, id2, full + s);
-              bulk_g2s(at + w_bytes, h + (int64_t)(2 * i) * sl.block, both * 2 * sl.block, full + s);
-              i += both - 1;
-              next();
+              mbar_arrive_expect_tx(full + s, stage_bytes);
+              tma_load_2d(at, &w_map, k * kStep, f0, full + s);
             }
-          }
-        }
-      }
-      // nothing of its own is on the way when it leaves, also where it gave up
-      for (int64_t i = issued > a.stages ? issued - a.stages : 0; i < issued; ++i)
-        mbar_drain(full + i % a.stages, (uint32_t)(i / a.stages) & 1u, a.status);
-    }
-  } else if (wid == 1) {
-    if (lane == 0) {
-      const uint32_t idesc = tc_idesc_bf16(kFeat, a.nt, false);
-      int s = 0, n = 0;
-      uint32_t phase = 0;
-      bool ok = true, waited = false;
-      auto next = [&] {
-        tc_commit(empty + s);
-        if (++s == a.stages) { s = 0; phase ^= 1u; }
-      };
-      for (int tile = group; tile < tiles && ok; tile += groups, ++n) {
-        const int buf = n & 1;
-        int s0 = 0, s1 = 0;
-        if (kAdapters && waited) my_slots(tile / a.feat_tiles, s0, s1);
-        if (!(ok = mbar_wait(acc_empty + buf, ((n >> 1) & 1) ^ 1, a.status))) break;
-        tc_fence_after_sync();
-        const uint32_t d = tmem + buf * a.acc_cols;
-        for (int k = step0; k < step1; ++k) {
-          if (!(ok = mbar_wait(full + s, phase, a.status))) break;
-          tc_fence_after_sync();
-          const uint64_t wd = tc_smem_desc(smem_u32(smem + s * stage_bytes), 0, 1024);
-          const uint64_t xd = tc_smem_desc(smem_u32(smem + s * stage_bytes + w_bytes), 0, 1024);
-#pragma unroll
-          for (int i = 0; i < kStep / 16; ++i) umma_ss(d, wd + 2 * i, xd + 2 * i, idesc, k > step0 || i > 0);
-          next();
-        }
-        if (kAdapters && ok) {
-          if (!waited) {
-            asm volatile("griddepcontrol.wait;" ::: "memory");
-            waited = true;
-            my_slots(tile / a.feat_tiles, s0, s1);
-          }
-          // stages: two a slot of rank 64, one of rank 32, one for two of rank 16
-          const int stages = h_row == 128 ? 2 * (s1 - s0) : h_row == 64 ? s1 - s0 : (s1 - s0 + 1) / 2;
-          for (int i = 0; i < stages; ++i) {
-            if (!(ok = mbar_wait(full + s, phase, a.status))) break;
-            tc_fence_after_sync();
-            const uint32_t at = smem_u32(smem + s * stage_bytes), ht = at + w_bytes;
-            if (h_row == 128) {
-              const uint64_t bd = operand_desc(at, 128), hd = operand_desc(ht, 128);
-#pragma unroll
-              for (int j = 0; j < 4; ++j) umma_ss(d, bd + 2 * j, hd + 2 * j, idesc, 1);
-            } else if (h_row == 64) {
-              const uint64_t bd = operand_desc(at, 64);
-#pragma unroll
-              for (int j = 0; j < 4; ++j) umma_ss(d, bd + 2 * (j & 1), operand_desc(ht + (j >> 1) * sl.block, 64) + 2 * (j & 1), idesc, 1);
-            } else {
-              const int both = s0 + 2 * i + 1 < s1 ? 4 : 2;
-              for (int j = 0; j < both; ++j) umma_ss(d, operand_desc(at + (j >> 1) * b_bytes, 32), operand_desc(ht + j * sl.block, 32), idesc, 1);
-            }
+            tma_load_2d(at + w_bytes, &x_map, k * kStep, t0, full + s);
             next();
           }
+          if (kMode == kWith && ok) {
+            if (!waited) {
+              asm volatile("griddepcontrol.wait;" ::: "memory");  // the slots' operands are the kernel's before this one
+              waited = true;
+              s1 = slots_of(row_tile);
+            }
+            s0 = s1 * part / a.splits;
+            s1 = s1 * (part + 1) / a.splits;
+            int ahead[2] = {s0 < s1 ? __ldcg(which + s0) : 0, s0 + 1 < s1 ? __ldcg(which + s0 + 1) : 0};  // of the next two slots
+            const char* h = sl.h + (int64_t)row_tile * sl.most * 2 * sl.block;
+            for (int i = s0; i < s1 && ok; ++i) {
+              const int id = ahead[0], id2 = ahead[1];
+              const int taken = h_row == 32 ? 2 : 1;
+              ahead[0] = taken == 2 ? (i + 2 < s1 ? __ldcg(which + i + 2) : 0) : id2;
+              ahead[1] = i + taken + 1 < s1 ? __ldcg(which + i + taken + 1) : 0;
+              if (!(ok = free())) break;
+              char* at = smem + s * stage_bytes;
+              if (h_row == 128) {
+                for (int half = 0; half < 2 && ok; ++half) {
+                  at = smem + s * stage_bytes;
+                  if (half && !(ok = free())) break;
+                  mbar_arrive_expect_tx(full + s, b_bytes + sl.block);
+                  tma_load_3d(at, &b_map, 0, f0, id, full + s);
+                  bulk_g2s(at + w_bytes, h + (int64_t)(2 * i + half) * sl.block, sl.block, full + s);
+                  next();
+                }
+              } else if (h_row == 64) {
+                mbar_arrive_expect_tx(full + s, b_bytes + 2 * sl.block);
+                tma_load_3d(at, &b_map, 0, f0, id, full + s);
+                bulk_g2s(at + w_bytes, h + (int64_t)(2 * i) * sl.block, 2 * sl.block, full + s);
+                next();
+              } else {
+                const int both = i + 1 < s1 ? 2 : 1;
+                mbar_arrive_expect_tx(full + s, both * (b_bytes + 2 * sl.block));
+                tma_load_3d(at, &b_map, 0, f0, id, full + s);
+                if (both == 2) tma_load_3d(at + b_bytes, &b_map, 0, f0, id2, full + s);
+                bulk_g2s(at + w_bytes, h + (int64_t)(2 * i) * sl.block, both * 2 * sl.block, full + s);
+                i += both - 1;
+                next();
+              }
+            }
+          }
+          if (ok && s % a.pair != 0) {  // the next tile's begin with a pair: the other one of this passes empty
+            mbar_arrive(full + s);
+            next();
+          }
+          if (a.splits > 1) break;
         }
-        tc_commit(acc_full + buf);
+        // nothing of its own is on the way when it leaves, also where it gave up
+        for (int i = 0; i < a.stages; ++i)
+          if (used >> i & 1u) mbar_drain(full + i, phases >> i & 1u, a.status);
       }
-      if (!ok) {  // (otherwise the tiles' own waits have seen the last of them)
-        tc_commit(drained);
-        mbar_drain(drained, 0, a.status);
+    } else if (wid == 1) {
+      if (lane == 0) {
+        const uint32_t idesc = tc_idesc_bf16(kFeat, a.nt, false);
+        const uint64_t first_desc = tc_smem_desc(smem_u32(smem), 0, 1024);  // (its address is the low field, which the ring does not overrun)
+        bool ready = false;  // the stage has been seen to be full
+        auto filled = [&] { return ready || mbar_wait(full + s, phase, a.status); };
+        auto peek = [&] {    // (before a stage's MMAs, so that the answer is there behind them)
+          const bool wraps = s + 1 == a.stages;
+          ready = mbar_try_wait(full + (wraps ? 0 : s + 1), wraps ? phase ^ 1u : phase);
+        };
+        auto next = [&] {
+          if ((s + 1) % a.pair == 0) tc_commit(empty + s / a.pair);
+          if (++s == a.stages) { s = 0; phase ^= 1u; }
+        };
+        for (Tile t = now; more(t) && ok; advance(t)) {
+          const int buf = done & 1, row_tile = t.r;
+          int s0 = 0, s1 = 0;
+          if (kMode == kWith && waited) s1 = slots_of(row_tile);
+          if (!(ok = mbar_wait(acc_empty + buf, ((done >> 1) & 1) ^ 1, a.status))) break;
+          tc_fence_after_sync();
+          const uint32_t d = tmem + buf * a.acc_cols;
+          for (int k = step0; k < step1; ++k) {
+            if (!(ok = filled())) break;
+            tc_fence_after_sync();
+            const uint64_t wd = first_desc + (uint64_t)((uint32_t)s * stage_bytes >> 4);
+            peek();
+            umma_ss4(d, wd, wd + (w_bytes >> 4), idesc, k > step0);
+            next();
+          }
+          if (kMode == kWith && ok) {
+            if (!waited) {
+              asm volatile("griddepcontrol.wait;" ::: "memory");
+              waited = true;
+              s1 = slots_of(row_tile);
+            }
+            s0 = s1 * part / a.splits;
+            s1 = s1 * (part + 1) / a.splits;
+            // stages: two a slot of rank 64, one of rank 32, one for two of rank 16
+            const int stages = h_row == 128 ? 2 * (s1 - s0) : h_row == 64 ? s1 - s0 : (s1 - s0 + 1) / 2;
+            for (int i = 0; i < stages; ++i) {
+              if (!(ok = filled())) break;
+              tc_fence_after_sync();
+              const uint32_t at = smem_u32(smem + s * stage_bytes), ht = at + w_bytes;
+              peek();
+              if (h_row == 128) {
+                umma_ss4(d, operand_desc(at, 128), operand_desc(ht, 128), idesc, 1);
+              } else if (h_row == 64) {
+                const uint64_t bd = operand_desc(at, 64);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) umma_ss(d, bd + 2 * (j & 1), operand_desc(ht + (j >> 1) * sl.block, 64) + 2 * (j & 1), idesc, 1);
+              } else {
+                const int both = s0 + 2 * i + 1 < s1 ? 4 : 2;
+                for (int j = 0; j < both; ++j) umma_ss(d, operand_desc(at + (j >> 1) * b_bytes, 32), operand_desc(ht + j * sl.block, 32), idesc, 1);
+              }
+              next();
+            }
+          }
+          if (s % a.pair != 0) {
+            tc_commit(empty + s / a.pair);
+            if (++s == a.stages) { s = 0; phase ^= 1u; }
+            ready = false;
+          }
+          tc_commit(acc_full + buf);
+          ++done;
+          if (a.splits > 1) break;
+        }
+        if (!ok) {  // (otherwise the tiles' own waits have seen the last of them)
+          tc_commit(drained);
+          mbar_drain(drained, 0, a.status);
+        }
+      }
+    } else if (wid >= 4) {
+      const int w = wid - 4;
+      const uint32_t lanes = tmem + ((uint32_t)(w * 32) << 16);
+      if (kMode == kWith && !waited) {
+        asm volatile("griddepcontrol.wait;" ::: "memory");  // (what is written here may be read by kernels before)
+        waited = true;
+      }
+      for (Tile t = now; more(t); advance(t)) {
+        const int f = t.f, m = w * 32 + lane, row_tile = t.r, t0 = row_tile * a.nt, buf = done & 1;
+        if (!(ok = __all_sync(0xffffffffu, ok && mbar_wait(acc_full + buf, (done >> 1) & 1, a.status)))) break;
+        tc_fence_after_sync();
+        if (a.splits > 1) break;  // taken out below, by the whole cluster
+        ++done;
+        auto take = [&](auto&& store) {
+          for (int g = 0; g < a.nt && t0 + g < a.rows; g += kGroup) {
+            uint32_t r[kGroup];
+            tmem_ld8(lanes + buf * a.acc_cols + g, r);
+            tmem_wait_ld();
+#pragma unroll
+            for (int j = 0; j < kGroup; ++j) store(g + j, __uint_as_float(r[j]));
+          }
+        };
+        if (kMode == kDown) {
+          const HPlace place(sl, row_tile, f * per_tile, t.slots, m);
+          take([&](int r, float v) { if (t0 + r < a.rows) store_h(sl, place, r, __ldcg(sl.of_row + t0 + r), v); });
+        } else {
+          take([&](int r, float v) { store_y(a, t0 + r, f * kFeat + m, v); });
+        }
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(acc_empty + buf);
       }
     }
-  } else if (wid >= 4) {
-    const int w = wid - 4;
-    const uint32_t lanes = tmem + ((uint32_t)(w * 32) << 16);
-    if (kAdapters) asm volatile("griddepcontrol.wait;" ::: "memory");  // (what is written here may be read by kernels before)
-    int n = 0;
-    for (int tile = group; tile < tiles; tile += groups, ++n) {
-      const int feat = (tile % a.feat_tiles) * kFeat + w * 32 + lane, t0 = (tile / a.feat_tiles) * a.nt, buf = n & 1;
-      if (!mbar_wait(acc_full + buf, (n >> 1) & 1, a.status)) break;
-      tc_fence_after_sync();
-      if (a.splits > 1) break;  // joined below
-      for (int g = 0; g < a.nt && t0 + g < a.rows; g += kGroup) {
-        uint32_t r[kGroup];
-        tmem_ld8(lanes + buf * a.acc_cols + g, r);
-        tmem_wait_ld();
+    __syncwarp();
+    if (a.splits == 1) break;
+    {
+      // The parts go to shared memory (the ring's: the tile's last MMA is done), [row of x][feature], and row r is joined by CTA r mod
+      // splits, a warp a row, 16 reads on the way.  (Parts written to the CTA that joins them took 30 us where this takes 20, with 256 rows.)
+      const int f = now.f, row_tile = now.r, t0 = row_tile * a.nt, n = min(a.nt, a.rows - t0);
+      const HPlace place = kMode == kDown ? HPlace(sl, row_tile, f * per_tile, now.slots, lane * 4) : HPlace();
+      float* parts = reinterpret_cast<float*>(smem);
+      if (wid >= 4) {
+        const int m = (wid - 4) * 32 + lane, buf = done & 1;
+        const uint32_t from = tmem + ((uint32_t)((wid - 4) * 32) << 16) + buf * a.acc_cols;
+        for (int g = 0; g < a.nt; g += 16) {
+          uint32_t r[2][kGroup];
+          tmem_ld8(from + g, r[0]);
+          tmem_ld8(from + g + kGroup, r[1]);
+          tmem_wait_ld();
 #pragma unroll
-        for (int j = 0; j < kGroup; ++j) store_y(a, t0 + g + j, feat, __uint_as_float(r[j]));
+          for (int j = 0; j < 16; ++j) parts[(g + j) * kFeat + m] = __uint_as_float(r[j >> 3][j & 7]);
+        }
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(acc_empty + buf);
+        ++done;
       }
-      tc_fence_before_sync();
       __syncwarp();
-      if (lane == 0) mbar_arrive(acc_empty + buf);
-    }
-  }
-  __syncwarp();
-  if (a.splits > 1) {
-    __syncthreads();
-    // One tile a cluster: the parts go to shared memory (the ring's: its last MMA is done), [row of x][feature], and each CTA adds
-    // those of its share of the rows.
-    const int f0 = (group % a.feat_tiles) * kFeat, t0 = (group / a.feat_tiles) * a.nt;
-    float* parts = reinterpret_cast<float*>(smem);
-    const int w = wid - 4;
-    if (wid >= 4) {
-      for (int g = 0; g < a.nt; g += kGroup) {
-        uint32_t r[kGroup];
-        tmem_ld8(tmem + ((uint32_t)(w * 32) << 16) + g, r);
-        tmem_wait_ld();
+      cluster_sync_all();
+      constexpr int kRows = 4, kParts = 4;  // of a warp on the way
+      const int apart = a.splits * (kThreads / 32);
+      for (int r0 = part + a.splits * wid; r0 < n; r0 += apart * kRows) {
+        float4 sum[kRows];
+        int row_slot[kRows];
 #pragma unroll
-        for (int j = 0; j < kGroup; ++j) parts[(g + j) * kFeat + w * 32 + lane] = __uint_as_float(r[j]);
-      }
-    }
-    __syncthreads();
-    cluster_sync_all();
-    if (wid >= 4) {
-      for (int g = part * kGroup; g < a.nt && t0 + g < a.rows; g += a.splits * kGroup) {
-        float sum[kGroup];
+        for (int i = 0; i < kRows; ++i) {
+          sum[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+          row_slot[i] = kMode == kDown ? __ldcg(sl.of_row + t0 + min(r0 + i * apart, n - 1)) : 0;
+        }
+        for (int p0 = 0; p0 < a.splits; p0 += kParts) {
+          float4 x[kParts][kRows];
 #pragma unroll
-        for (int j = 0; j < kGroup; ++j) sum[j] = 0.f;
-        for (int p = 0; p < a.splits; ++p) {
-          uint32_t from;
-          asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(from) : "r"(smem_u32(parts + g * kFeat + w * 32 + lane)), "r"(p));
+          for (int p = 0; p < kParts; ++p) {
+            if (p0 + p < a.splits) {
+              uint32_t from;
+              asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(from) : "r"(smem_u32(parts + lane * 4)), "r"(p0 + p));
 #pragma unroll
-          for (int j = 0; j < kGroup; ++j) {
-            float x;
-            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(from + j * kFeat * 4) : "memory");
-            sum[j] += x;
+              for (int i = 0; i < kRows; ++i)
+                asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];"
+                             : "=f"(x[p][i].x), "=f"(x[p][i].y), "=f"(x[p][i].z), "=f"(x[p][i].w)
+                             : "r"(from + min(r0 + i * apart, n - 1) * kFeat * 4)
+                             : "memory");
+            }
+          }
+#pragma unroll
+          for (int p = 0; p < kParts; ++p)
+            if (p0 + p < a.splits) {
+#pragma unroll
+              for (int i = 0; i < kRows; ++i) { sum[i].x += x[p][i].x; sum[i].y += x[p][i].y; sum[i].z += x[p][i].z; sum[i].w += x[p][i].w; }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+          const int r = r0 + i * apart;
+          if (r < n) {
+            if (kMode == kDown) store_h4(sl, place, r, row_slot[i], sum[i]);
+            else store_y4(a, t0 + r, f * kFeat + lane * 4, sum[i]);
           }
         }
-#pragma unroll
-        for (int j = 0; j < kGroup; ++j) store_y(a, t0 + g + j, f0 + w * 32 + lane, sum[j]);
       }
+      __syncwarp();
+      cluster_sync_all();  // nobody leaves, or takes new stages to where its part was, while that is read
+      fence_proxy_async_smem();  // (before the next round's copies to the ring)
+      if (__syncthreads_or(!ok)) break;
+      advance(now);
     }
-    __syncthreads();
-    cluster_sync_all();  // nobody leaves while its part is read
   }
   tc_fence_before_sync();
   __syncthreads();
@@ -328,240 +523,141 @@ __global__ void __launch_bounds__(kThreads, 1) k_project(const __grid_constant__
   if (wid == 1) tmem_dealloc(tmem, a.tmem_cols);
 }
 
-// ---- h -------------------------------------------------------------------------------------------------
-// Both kernels below find a tile's slots by themselves: the adapters that its rows name, ascending, as bits in shared memory (one
-// bit an adapter), so that an adapter's slot is the number of bits below its own.
-constexpr int kMaxAdapters = GF_MAX_ADAPTERS;
-
-struct TileSlots {
-  uint32_t bits[kMaxAdapters / 32];
+// The slots of a tile of x: the adapters that its rows name, ascending; one bit an adapter in shared memory, so that an adapter's slot is
+// the number of bits below its own.
+constexpr int kMaxWords = GF_MAX_ADAPTERS / 32;
+struct SlotBits {
+  uint32_t bits[kMaxWords];
+  int before[kMaxWords];  // bits in the words before
+  int count;
+  __device__ int slot(int id) const { return id < 0 ? -1 : before[id >> 5] + __popc(bits[id >> 5] & ((1u << (id & 31)) - 1u)); }
 };
-
-__device__ __forceinline__ int adapter_of(const int32_t* __restrict__ adapter, int row, int num_adapters, bool report, int32_t* status) {
+// An adapter's number, -1 where it is none.
+__device__ __forceinline__ int adapter_of(const int32_t* __restrict__ adapter, int row, int num_adapters, int32_t* status) {
   const int id = adapter[row];
   if (id >= 0 && id < num_adapters) return id;
-  if (id != -1 && report) atomicCAS(status + kStatusReport, 0, (int)GF_ERR_INVALID_ARG);
+  if (id != -1) atomicCAS(status + kStatusReport, 0, (int)GF_ERR_INVALID_ARG);
   return -1;
 }
-// All threads of a CTA: the bits of rows t0 .. t0 + n.
-__device__ void tile_slots(TileSlots& ts, const int32_t* __restrict__ adapter, int t0, int n, int num_adapters, int32_t* status) {
-  for (int i = threadIdx.x; i < (num_adapters + 31) / 32; i += blockDim.x) ts.bits[i] = 0u;
+// All threads of a CTA, at least n of them; returns the adapter of row t0 + (thread).
+__device__ int find_slots(SlotBits& sb, const int32_t* __restrict__ adapter, int t0, int n, int num_adapters, int32_t* status) {
+  const int tid = threadIdx.x, lane = tid & 31, words = (num_adapters + 31) / 32;
+  const int id = tid < n ? adapter_of(adapter, t0 + tid, num_adapters, status) : -1;
+  for (int i = tid; i < words; i += blockDim.x) sb.bits[i] = 0u;
   __syncthreads();
-  for (int i = threadIdx.x; i < n; i += blockDim.x) {
-    const int id = adapter_of(adapter, t0 + i, num_adapters, true, status);
-    if (id >= 0) atomicOr(&ts.bits[id >> 5], 1u << (id & 31));
-  }
+  if (id >= 0) atomicOr(&sb.bits[id >> 5], 1u << (id & 31));
   __syncthreads();
-}
-// All lanes of a warp: how many slots come before the adapter `id` (num_adapters: how many there are).
-__device__ __forceinline__ int slot_of(const TileSlots& ts, int id) {
-  int n = 0;
-  for (int i = threadIdx.x & 31; i <= id >> 5; i += 32) n += __popc(i < id >> 5 ? ts.bits[i] : id & 31 ? ts.bits[i] & ((1u << (id & 31)) - 1u) : 0u);
-  return __reduce_add_sync(0xffffffffu, n);
-}
-// All threads of a CTA write the list of a tile's slots.
-__device__ void write_slots(const TileSlots& ts, const Slots& sl, int row_tile, int num_adapters, int count) {
-  if (threadIdx.x == 0) sl.count[row_tile] = count;
-  const int lane = threadIdx.x & 31, words = (num_adapters + 31) / 32;
-  for (int i = threadIdx.x >> 5; i < words; i += blockDim.x >> 5) {
-    const int first = slot_of(ts, i * 32);
-    const uint32_t w = ts.bits[i];
-    if (w >> lane & 1u) sl.adapter[(int64_t)row_tile * sl.most + first + __popc(w & ((1u << lane) - 1u))] = i * 32 + lane;
-  }
-}
-// One 16-byte piece (8 ranks, from h in shared memory) of a row's operand, of the first or second number.
-__device__ __forceinline__ uint4 h_piece(const float* __restrict__ h, int half) {
-  uint32_t w[4];
+  if (tid < 32) {
+    int sum = 0;
+    for (int i0 = 0; i0 < words; i0 += 32) {
+      const int here = i0 + lane < words ? __popc(sb.bits[i0 + lane]) : 0;
+      int upto = here;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float v[2];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      v[j] = h[2 * i + j];
-      const float first = __bfloat162float(__float2bfloat16_rn(v[j]));
-      if (half) v[j] = fabsf(first) <= 3.3895e38f ? v[j] - first : 0.f;  // (nothing is left of an infinity, or a NaN)
+      for (int d = 1; d < 32; d <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += y;
+      }
+      if (i0 + lane < words) sb.before[i0 + lane] = sum + upto - here;
+      sum += __shfl_sync(0xffffffffu, upto, 31);
     }
-    w[i] = pack_bf16(v[0], v[1]);
+    if (lane == 0) sb.count = sum;
   }
-  return make_uint4(w[0], w[1], w[2], w[3]);
+  __syncthreads();
+  return id;
 }
-// A row's part of its tile's operands: h in its adapter's slot (-1: none), zeros in the others.  By `threads` threads, this the `who`-th.
-__device__ void write_row(const Slots& sl, int row_tile, int row_in_tile, int count, int slot, const float* h, int who, int threads) {
-  const int pieces = sl.padded >> 3, per_slot = 2 * pieces;
-  char* base = sl.h + (int64_t)row_tile * sl.most * 2 * sl.block;
-  for (int i = who; i < count * per_slot; i += threads) {
-    const int s = i / per_slot, half = (i - s * per_slot) / pieces, c = i % pieces;
-    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-    if (s == slot && c * 8 < sl.rank) v = h_piece(h + c * 8, half);
-    *reinterpret_cast<uint4*>(base + (int64_t)(2 * s + half) * sl.block + operand_at(row_in_tile, c, sl.padded * 2)) = v;
-  }
+// The same threads write the tile's list.  (Rows of one adapter write the same.)
+__device__ __forceinline__ void write_slots(const SlotBits& sb, const Slots& sl, int tile, int id) {
+  if (threadIdx.x == 0) sl.count[tile] = sb.count;
+  if (id >= 0) sl.adapter[(int64_t)tile * sl.most + sb.slot(id)] = id;
 }
 
-// A CTA per row: the warps share K, each lane 8 entries of x against 16 rows of A at a time, all asked for at once; the lanes' sums
-// are joined by halving the values that a lane holds.  fp32 throughout.  Bound: latency (a load of the row's adapter, one of A, and the
-// join), and for hundreds of rows L2, which reads A once per row.
-constexpr int kRowThreads = 512, kRowWarps = kRowThreads / 32;
-__global__ void __launch_bounds__(kRowThreads) k_adapter_down_rows(const __nv_bfloat16* __restrict__ x, int64_t x_stride, int rows, int in_dim, int nt,
-                                                                   const int32_t* __restrict__ adapter, int num_adapters, Slots sl,
-                                                                   const __nv_bfloat16* __restrict__ a, const float* __restrict__ scale, int32_t* status) {
+__global__ void __launch_bounds__(256) k_adapter_slots(const int32_t* __restrict__ adapter, int rows, int nt, int num_adapters, Slots sl, int32_t* status) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  __shared__ TileSlots ts;
-  __shared__ float sums[kRowWarps][64], h[64];
-  const int t = blockIdx.x, tile = t / nt, t0 = tile * nt, tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, rank = sl.rank;
-  const int which = adapter_of(adapter, t, num_adapters, false, status);
-  tile_slots(ts, adapter, t0, min(nt, rows - t0), num_adapters, status);
-  const int count = slot_of(ts, num_adapters), slot = which < 0 ? -1 : slot_of(ts, which);
-  if (t == t0) write_slots(ts, sl, tile, num_adapters, count);
+  __shared__ SlotBits sb;
+  const int t0 = blockIdx.x * nt, n = min(nt, rows - t0);
+  const int id = find_slots(sb, adapter, t0, n, num_adapters, status);
+  write_slots(sb, sl, blockIdx.x, id);
+  if (threadIdx.x < n) sl.of_row[t0 + threadIdx.x] = sb.slot(id);
+}
+
+// A x for few rows, where the tiles' kernel would be all latency (slots 3 us, A x 15 to 20; this 7).  A CTA per row and 16 ranks: the warps
+// share K, each lane 8 entries of x against 16 rows of A, all asked for at once; the lanes' sums are joined by halving the values that a
+// lane holds.  fp32 throughout.  Bound: latency (the rows' adapters, A, the join), and for hundreds of rows L2, which reads A once per row.
+constexpr int kRowThreads = 512, kRowWarps = kRowThreads / 32, kRowRanks = 16;
+__global__ void __launch_bounds__(kRowThreads, 2) k_adapter_rows(const __nv_bfloat16* __restrict__ x, int64_t x_stride, int rows, int in_dim, int nt,
+                                                                 const int32_t* __restrict__ adapter, int num_adapters, Slots sl,
+                                                                 const __nv_bfloat16* __restrict__ a, int32_t* status) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  __shared__ SlotBits sb;
+  __shared__ float sums[kRowWarps][kRowRanks], h[kRowRanks];
+  const int t = blockIdx.x, tile = t / nt, t0 = tile * nt, tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, r0 = blockIdx.y * kRowRanks;
+  const int which = adapter_of(adapter, t, num_adapters, status), ranks = min(kRowRanks, sl.rank - r0);
   if (which >= 0) {
     const __nv_bfloat16* xr = x + (int64_t)t * x_stride;
-    const __nv_bfloat16* ar = a + (int64_t)which * rank * in_dim;
-    for (int r0 = 0; r0 < rank; r0 += 16) {
-      uint64_t acc[16];
+    const __nv_bfloat16* ar = a + ((int64_t)which * sl.rank + r0) * in_dim;
+    float v[kRowRanks];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[r] = 0ull;
-      for (int k = (wid * 32 + lane) * 8; k < in_dim; k += kRowThreads * 8) {
-        const uint4 xv = *reinterpret_cast<const uint4*>(xr + k);
-        uint4 av[16];
+    for (int half = 0; half < 2; ++half) {  // (8 ranks at a time: registers)
+      uint64_t acc[8];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) av[r] = r0 + r < rank ? __ldg(reinterpret_cast<const uint4*>(ar + (int64_t)(r0 + r) * in_dim + k)) : make_uint4(0u, 0u, 0u, 0u);
-        const uint64_t x0 = bf16x2_to_f2(xv.x), x1 = bf16x2_to_f2(xv.y), x2 = bf16x2_to_f2(xv.z), x3 = bf16x2_to_f2(xv.w);
+      for (int r = 0; r < 8; ++r) acc[r] = 0ull;
+      if (half * 8 < ranks)  // (ranks are multiples of 8)
+        for (int k = tid * 8; k < in_dim; k += kRowThreads * 8) {
+          const uint4 xv = *reinterpret_cast<const uint4*>(xr + k);
+          uint4 av[8];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          acc[r] = f2_fma(bf16x2_to_f2(av[r].x), x0, acc[r]);
-          acc[r] = f2_fma(bf16x2_to_f2(av[r].y), x1, acc[r]);
-          acc[r] = f2_fma(bf16x2_to_f2(av[r].z), x2, acc[r]);
-          acc[r] = f2_fma(bf16x2_to_f2(av[r].w), x3, acc[r]);
+          for (int r = 0; r < 8; ++r) av[r] = __ldg(reinterpret_cast<const uint4*>(ar + (int64_t)(half * 8 + r) * in_dim + k));
+          const uint64_t x0 = bf16x2_to_f2(xv.x), x1 = bf16x2_to_f2(xv.y), x2 = bf16x2_to_f2(xv.z), x3 = bf16x2_to_f2(xv.w);
+#pragma unroll
+          for (int r = 0; r < 8; ++r) {
+            acc[r] = f2_fma(bf16x2_to_f2(av[r].x), x0, acc[r]);
+            acc[r] = f2_fma(bf16x2_to_f2(av[r].y), x1, acc[r]);
+            acc[r] = f2_fma(bf16x2_to_f2(av[r].z), x2, acc[r]);
+            acc[r] = f2_fma(bf16x2_to_f2(av[r].w), x3, acc[r]);
+          }
         }
-      }
-      float v[16];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
+      for (int r = 0; r < 8; ++r) {
         float lo, hi;
         f2_unpack(acc[r], lo, hi);
-        v[r] = lo + hi;
+        v[half * 8 + r] = lo + hi;
       }
-      // sixteen sums over 32 lanes: each exchange halves the values held, the last adds the two that are left
-#pragma unroll
-      for (int half = 8; half > 0; half >>= 1) {
-        const bool upper = (lane & half) != 0;
-#pragma unroll
-        for (int i = 0; i < half; ++i) {
-          const float keep = upper ? v[i + half] : v[i], give = upper ? v[i] : v[i + half];
-          v[i] = keep + __shfl_xor_sync(0xffffffffu, give, half);
-        }
-      }
-      v[0] += __shfl_xor_sync(0xffffffffu, v[0], 16);
-      if (lane < 16 && r0 + lane < rank) sums[wid][r0 + lane] = v[0];
     }
+    // sixteen sums over 32 lanes: each exchange halves the values held, the last adds the two that are left
+#pragma unroll
+    for (int half = 8; half > 0; half >>= 1) {
+      const bool upper = (lane & half) != 0;
+#pragma unroll
+      for (int i = 0; i < half; ++i) {
+        const float keep = upper ? v[i + half] : v[i], give = upper ? v[i] : v[i + half];
+        v[i] = keep + __shfl_xor_sync(0xffffffffu, give, half);
+      }
+    }
+    v[0] += __shfl_xor_sync(0xffffffffu, v[0], 16);
+    if (lane < kRowRanks) sums[wid][lane] = v[0];
   }
-  __syncthreads();
-  if (which >= 0 && tid < rank) {
+  const int id = find_slots(sb, adapter, t0, min(nt, rows - t0), num_adapters, status);
+  if (t == t0 && r0 == 0) write_slots(sb, sl, tile, id);
+  if (which >= 0 && tid < kRowRanks) {
     float sum = 0.f;
 #pragma unroll
     for (int w = 0; w < kRowWarps; ++w) sum += sums[w][tid];
-    h[tid] = sum * (scale != nullptr ? scale[which] : 1.f);
+    h[tid] = tid < ranks ? sum * (sl.scale != nullptr ? __ldg(sl.scale + which) : 1.f) : 0.f;
   }
   __syncthreads();
-  write_row(sl, tile, t - t0, count, slot, h, tid, kRowThreads);
-}
-
-// Many rows.  A CTA has 32 rows that are next to each other in the order of their adapters within a tile (each CTA ranks its tile's
-// rows by itself), so most have one adapter, or a few; for each of them the warps share K, 32 entries at a time, and multiply
-// the CTA's rows by A (mma.sync, rows x rank, both operands straight from L2 in 16-byte pieces: K's order within a step does
-// not matter as long as both have the same), and those of the adapter's rows are kept.  The warps' sums are added in a fixed
-// order.  Bound: L2, which reads A once per 32 rows of one adapter.
-constexpr int kDownThreads = 256, kDownWarps = kDownThreads / 32, kDownRows = 32;
-template <int RT>  // 8-row pieces of A at most
-__global__ void __launch_bounds__(kDownThreads) k_adapter_down(const __nv_bfloat16* __restrict__ x, int64_t x_stride, int rows, int in_dim, int nt,
-                                                               const int32_t* __restrict__ adapter, int num_adapters, Slots sl,
-                                                               const __nv_bfloat16* __restrict__ a, const float* __restrict__ scale, int32_t* status) {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  constexpr int MT = kDownRows / 16;
-  extern __shared__ float sums[];  // [kDownWarps][kDownRows][rank]
-  __shared__ TileSlots ts;
-  __shared__ int s_id[256], s_row[256], s_sorted[256];
-  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, rank = sl.rank;
-  const int chunks = (nt + kDownRows - 1) / kDownRows, tile = blockIdx.x / chunks, chunk = blockIdx.x - tile * chunks;
-  const int t0 = tile * nt, n = min(nt, rows - t0), p0 = chunk * kDownRows;
-  if (p0 >= n) return;
-  const int id = tid < n ? adapter_of(adapter, t0 + tid, num_adapters, false, status) : 0x7fffffff;
-  s_id[tid] = id;
-  tile_slots(ts, adapter, t0, n, num_adapters, status);
-  const int count = slot_of(ts, num_adapters);
-  if (chunk == 0) write_slots(ts, sl, tile, num_adapters, count);
-  if (tid < n) {
-    int before = 0;
-    for (int j = 0; j < n; ++j) before += s_id[j] < id || (s_id[j] == id && j < tid);
-    s_row[before] = tid;
-    s_sorted[before] = id;
-  }
-  __syncthreads();
-  const int end = min(p0 + kDownRows, n), g = lane >> 2, q = lane & 3, pieces = rank >> 3;
-  const __nv_bfloat16* xr[2 * MT];
+  // the row's pieces (8 ranks) of these 16 ranks, or of their padding, in all slots
+  const int pieces = min(2, (sl.padded - r0) >> 3), slot = sb.slot(which);
+  char* base = sl.h + (int64_t)tile * sl.most * 2 * sl.block;
+  for (int i = tid; i < sb.count * 2 * pieces; i += kRowThreads) {
+    const int c = i % pieces, half = i / pieces & 1, at = i / (2 * pieces);
+    __align__(16) __nv_bfloat16 p[8];
 #pragma unroll
-  for (int i = 0; i < 2 * MT; ++i) xr[i] = x + (int64_t)(t0 + s_row[min(p0 + i * 8 + g, end - 1)]) * x_stride + q * 8;
-  for (int j0 = p0; j0 < end;) {
-    const int which = s_sorted[j0];
-    int j1 = j0 + 1;
-    while (j1 < end && s_sorted[j1] == which) ++j1;
-    if (which >= 0) {
-      float acc[MT][RT][4];
-#pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc[m][r][i] = 0.f;
-      const __nv_bfloat16* ar = a + ((int64_t)which * rank + g) * in_dim + q * 8;
-#pragma unroll 2
-      for (int k = wid * 32; k < in_dim; k += kDownWarps * 32) {
-        const bool in = k + q * 8 < in_dim;
-        uint4 xv[2 * MT], av[RT];
-#pragma unroll
-        for (int i = 0; i < 2 * MT; ++i) xv[i] = in ? *reinterpret_cast<const uint4*>(xr[i] + k) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-          av[r] = in && r < pieces ? __ldg(reinterpret_cast<const uint4*>(ar + (int64_t)r * 8 * in_dim + k)) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-          const uint32_t lo[4] = {xv[2 * m].x, xv[2 * m + 1].x, xv[2 * m].y, xv[2 * m + 1].y};
-          const uint32_t hi[4] = {xv[2 * m].z, xv[2 * m + 1].z, xv[2 * m].w, xv[2 * m + 1].w};
-#pragma unroll
-          for (int r = 0; r < RT; ++r)
-            if (r < pieces) {
-              mma_bf16(acc[m][r], lo, av[r].x, av[r].y);
-              mma_bf16(acc[m][r], hi, av[r].z, av[r].w);
-            }
-        }
-      }
-#pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const int i = m * 16 + half * 8 + g;
-          if (p0 + i >= j0 && p0 + i < j1) {
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-              if (r < pieces)
-                *reinterpret_cast<float2*>(sums + ((size_t)wid * kDownRows + i) * rank + r * 8 + q * 2) = make_float2(acc[m][r][2 * half], acc[m][r][2 * half + 1]);
-          }
-        }
+    for (int j = 0; j < 8; ++j) {
+      __nv_bfloat16 first, left;
+      split_h(at == slot ? h[c * 8 + j] : 0.f, first, left);
+      p[j] = half ? left : first;
     }
-    j0 = j1;
-  }
-  __syncthreads();
-  for (int i = tid; i < (end - p0) * rank; i += kDownThreads) {
-    const int which = s_sorted[p0 + i / rank];
-    if (which < 0) continue;
-    float sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < kDownWarps; ++w) sum += sums[(size_t)w * kDownRows * rank + i];
-    sums[i] = sum * (scale != nullptr ? scale[which] : 1.f);  // (the first warp's place, read by this thread alone)
-  }
-  __syncthreads();
-  for (int j = p0 + wid; j < end; j += kDownWarps) {
-    const int which = s_sorted[j], slot = which < 0 ? -1 : slot_of(ts, which);
-    write_row(sl, tile, s_row[j], count, slot, sums + (j - p0) * rank, lane, 32);
+    *reinterpret_cast<uint4*>(base + (int64_t)(2 * at + half) * sl.block + operand_at(t - t0, (r0 >> 3) + c, sl.padded * 2)) = *reinterpret_cast<uint4*>(p);
   }
 }
 
@@ -593,14 +689,85 @@ bool make_map(CUtensorMap* map, const void* base, int64_t matrices, int64_t rows
                 swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool kAdapters>
-int launch_main(const CUtensorMap& w_map, const CUtensorMap& x_map, const CUtensorMap& b_map, const ProjectArgs& a, int ctas, size_t smem, cudaStream_t st) {
+constexpr int kHalfKb = 110;  // of shared memory, of which two CTAs share a multiprocessor
+// Never launched: the occupancy calculation takes a kernel with tensor memory for one that has a multiprocessor to itself, though two of
+// k_project's CTAs run side by side where they have room (4096 -> 6144 in 192 CTAs: 11 us, and 19 when registers allowed but one).
+__global__ void __launch_bounds__(kThreads, 2) k_room() {}
+// How many clusters of `size` CTAs the device has room for at once, with all of a multiprocessor's shared memory each or half of it.
+// (Asked once: a GPC whose multiprocessors are no multiple of the size has some left over.)
+int clusters_at_once(int size, bool half, int num_sms) {
+  static int known[kMaxDevices][2][9];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return 0;
+  int& n = known[dev][half][size];
+  if (n == 0) {
+    static bool done[kMaxDevices];
+    if (!ensure_dynamic_smem(k_room, 227 * 1024, done)) return 0;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(size * num_sms));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = (half ? kHalfKb : 227) * 1024;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)size;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int got = 0;
+    if (cudaOccupancyMaxActiveClusters(&got, k_room, &cfg) != cudaSuccess) {
+      cudaGetLastError();
+      got = 0;
+    }
+    n = got > 0 ? got : -1;
+  }
+  return n;
+}
+
+// How a launch shares out its tiles: CTAs and what they have.  Few tiles are shared by clusters of up to 8 CTAs, whose time is the stages
+// of the multiprocessor that has most: the size with the fewest is taken, the smallest of those (a join costs 1 to 3 us), if all clusters
+// find room at once.  Where four stages fit into half a multiprocessor's shared memory, two CTAs may share it.  (4096 -> 6144 for 64
+// rows: 26 us with clusters of 1, 16.6 of 2, 15.7 of 4, which leave some multiprocessors with two CTAs.)
+struct Shape {
+  int ctas;
+  size_t smem;
+};
+Shape shape_of(ProjectArgs& a, int64_t tiles, int num_sms) {
+  const int steps = (a.in_dim + kStep - 1) / kStep;
+  const uint32_t stage_bytes = kFeat * 128u + a.nt * 128u, extra = 1024 + 512;
+  const int per_sm = 4 * stage_bytes + extra <= kHalfKb * 1024 ? 2 : 1;
+  a.splits = 1;
+  int64_t best = (tiles + num_sms - 1) / num_sms * steps;
+  for (int n = 2; n <= 8 && tiles * n <= (int64_t)per_sm * num_sms && steps >= 4 * n; ++n) {
+    const int64_t most = (tiles * n + num_sms - 1) / num_sms * ((steps + n - 1) / n);
+    if (most < best - best / 16 && tiles <= clusters_at_once(n, per_sm == 2, num_sms)) {
+      best = most;
+      a.splits = n;
+    }
+  }
+  const bool shared = per_sm == 2 && (a.splits > 1 || (tiles > num_sms && tiles <= 2 * num_sms));
+  const uint32_t room = (shared ? kHalfKb : 227) * 1024 - extra;
+  a.stages = (int)std::min<uint32_t>(12, room / stage_bytes);
+  // (with six and more, two at a time: a commit costs the issuing thread 100 cycles, a stage's MMAs 300, whatever the rows)
+  a.pair = a.stages >= 6 ? 2 : 1;
+  a.stages -= a.stages % a.pair;
+  const int64_t groups = a.splits > 1 || shared ? tiles : std::min<int64_t>(tiles, num_sms);
+  return Shape{(int)(groups * a.splits), extra + std::max<uint32_t>(stage_bytes * a.stages, a.splits > 1 ? (uint32_t)a.nt * kFeat * 4u : 0u)};
+}
+
+template <int kMode>
+int launch_main(const CUtensorMap& w_map, const CUtensorMap& x_map, const CUtensorMap& b_map, ProjectArgs a, const Shape& shape, cudaStream_t st) {
   static bool done[kMaxDevices];
-  if (!ensure_dynamic_smem(k_project<kAdapters>, 227 * 1024, done)) return -1;
+  if (!ensure_dynamic_smem(k_project<kMode>, 227 * 1024, done)) return -1;
+  // one accumulator where a CTA, or each round of a cluster, has one tile
+  const bool single = (int64_t)a.feat_tiles * a.row_tiles <= shape.ctas / a.splits;
+  uint32_t cols = 32;
+  while (cols < (uint32_t)a.nt) cols *= 2;
+  a.acc_cols = single ? 0 : cols;
+  a.tmem_cols = single ? cols : 2 * cols;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)ctas);
+  cfg.gridDim = dim3((unsigned)shape.ctas);
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
+  cfg.dynamicSmemBytes = shape.smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   int n = 0;
@@ -610,23 +777,14 @@ int launch_main(const CUtensorMap& w_map, const CUtensorMap& x_map, const CUtens
     attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
     ++n;
   }
-  if (kAdapters) {  // behind the kernel for h, whose results only a tile's last stages need
+  if (kMode != kPlain) {  // behind the kernel for the slots, or that for h, whose results only a tile's last stages need
     attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[n].val.programmaticStreamSerializationAllowed = 1;
     ++n;
   }
   cfg.attrs = attr;
   cfg.numAttrs = n;
-  return cudaLaunchKernelEx(&cfg, k_project<kAdapters>, w_map, x_map, b_map, a) == cudaSuccess ? 1 : -1;
-}
-
-template <int RT>
-bool launch_down(const gf_projection_t& p, const ProjectArgs& a, const void* x, int64_t x_stride, const int32_t* adapter, cudaStream_t st) {
-  static bool done[kMaxDevices];
-  if (!ensure_dynamic_smem(k_adapter_down<RT>, kDownWarps * kDownRows * RT * 8 * 4, done)) return false;
-  k_adapter_down<RT><<<(unsigned)(a.row_tiles * ((a.nt + kDownRows - 1) / kDownRows)), kDownThreads, (size_t)kDownWarps * kDownRows * p.rank * 4, st>>>(
-      (const __nv_bfloat16*)x, x_stride, a.rows, p.in_dim, a.nt, adapter, p.num_adapters, a.slots, (const __nv_bfloat16*)p.a_dev, p.scale_dev, a.status);
-  return cudaGetLastError() == cudaSuccess;
+  return cudaLaunchKernelEx(&cfg, k_project<kMode>, w_map, x_map, b_map, a) == cudaSuccess ? 1 : -1;
 }
 
 // Rows of x that one pass takes: more go in several, one behind the other, so that the scratch stays bounded.
@@ -639,9 +797,9 @@ size_t align_to(size_t n, size_t a) { return (n + a - 1) / a * a; }
 size_t place_slots(Slots* sl, char* scratch, int rows, int rank, int num_adapters) {
   const int nt = tile_rows(rows), tiles = (rows + nt - 1) / nt, most = std::min(nt, num_adapters);
   const int padded = rank <= 16 ? 16 : rank <= 32 ? 32 : 64;
-  const size_t count = 0, ids = align_to((size_t)tiles * 4, 128), h = ids + align_to((size_t)tiles * most * 4, 128);
+  const size_t ids = align_to((size_t)tiles * 4, 128), of_row = ids + align_to((size_t)tiles * most * 4, 128), h = of_row + align_to((size_t)rows * 4, 128);
   const size_t block = (size_t)nt * padded * 2;
-  if (sl) *sl = Slots{(int32_t*)(scratch + count), (int32_t*)(scratch + ids), scratch + h, most, rank, padded, (uint32_t)block};
+  if (sl) *sl = Slots{(int32_t*)scratch, (int32_t*)(scratch + ids), (int32_t*)(scratch + of_row), nullptr, scratch + h, most, rank, padded, (uint32_t)block};
   return h + (size_t)tiles * most * 2 * block;
 }
 
@@ -663,44 +821,39 @@ static int launch_pass(const gf_projection_t& p, int rows, const void* x, int64_
   a.y_stride = y_stride;
   a.y_fp32 = y_fp32;
   a.status = status;
-  if (with) place_slots(&a.slots, (char*)scratch, rows, p.rank, p.num_adapters);
-  const int64_t tiles = (int64_t)a.feat_tiles * a.row_tiles;
-  const int steps = (p.in_dim + kStep - 1) / kStep;
-  // Few tiles: clusters of 2, 4 or 8 share them (others do not fill the GPCs), two CTAs to a multiprocessor where the stages are
-  // small enough for four of them in half its shared memory.
-  const uint32_t stage_bytes = kFeat * 128u + a.nt * 128u, extra = 1024 + 512;
-  const int per_sm = 4 * stage_bytes + extra <= 113 * 1024 ? 2 : 1;
-  a.splits = 1;
-  auto fit = [&](int splits) { return (int64_t)per_sm * num_sms * (splits <= 2 ? 8 : splits == 4 ? 7 : 6) / 8; };  // (a GPC's rest takes no cluster)
-  while (a.splits < 8 && tiles * a.splits * 2 <= fit(a.splits * 2) && steps / (a.splits * 2) >= 4) a.splits *= 2;
-  const bool shared = tiles * a.splits > num_sms && tiles * a.splits <= (int64_t)per_sm * num_sms;
-  const uint32_t room = (shared ? 113 : 227) * 1024 - extra;
-  a.stages = (int)std::min<uint32_t>(12, room / stage_bytes);
-  const size_t smem = extra + std::max<uint32_t>(stage_bytes * a.stages, a.splits > 1 ? (uint32_t)a.nt * kFeat * 4u : 0u);
-  const int64_t groups = a.splits > 1 || shared ? tiles : std::min<int64_t>(tiles, num_sms);
-  const bool single = tiles <= groups;
-  uint32_t cols = 32;
-  while (cols < (uint32_t)a.nt) cols *= 2;
-  a.acc_cols = single ? 0 : cols;
-  a.tmem_cols = single ? cols : 2 * cols;
+  a.y_vec = (y_stride & 3) == 0 && ((uintptr_t)y & (y_fp32 ? 15 : 7)) == 0;
   CUtensorMap w_map, x_map, b_map = {};
-  if (!make_map(&w_map, p.w_dev, 0, p.out_dim, p.in_dim, p.w_stride, kStep, kFeat) || !make_map(&x_map, x, 0, rows, p.in_dim, x_stride, kStep, a.nt) ||
-      (with && !make_map(&b_map, p.b_dev, p.num_adapters, p.out_dim, p.rank, p.rank, a.slots.padded, kFeat)))
-    return -1;
-  int launched = 0;
-  if (with) {
-    if (rows <= 4 * num_sms) {
-      k_adapter_down_rows<<<(unsigned)rows, kRowThreads, 0, st>>>((const __nv_bfloat16*)x, x_stride, rows, p.in_dim, a.nt, adapter, p.num_adapters, a.slots,
-                                                                  (const __nv_bfloat16*)p.a_dev, p.scale_dev, status);
-      if (cudaGetLastError() != cudaSuccess) return -1;
-    } else if (!(p.rank <= 16 ? launch_down<2>(p, a, x, x_stride, adapter, st) : launch_down<8>(p, a, x, x_stride, adapter, st))) {
-      return -1;
-    }
-    ++launched;
+  if (!make_map(&w_map, p.w_dev, 0, p.out_dim, p.in_dim, p.w_stride, kStep, kFeat) || !make_map(&x_map, x, 0, rows, p.in_dim, x_stride, kStep, a.nt)) return -1;
+  if (!with) {
+    const Shape shape = shape_of(a, (int64_t)a.feat_tiles * a.row_tiles, num_sms);
+    return launch_main<kPlain>(w_map, x_map, b_map, a, shape, st);
   }
-  const int ctas = (int)(groups * a.splits);
-  const int n = with ? launch_main<true>(w_map, x_map, b_map, a, ctas, smem, st) : launch_main<false>(w_map, x_map, b_map, a, ctas, smem, st);
-  return n < 0 ? -1 : launched + n;
+  place_slots(&a.slots, (char*)scratch, rows, p.rank, p.num_adapters);
+  a.slots.scale = p.scale_dev;
+  if (!make_map(&b_map, p.b_dev, p.num_adapters, p.out_dim, p.rank, p.rank, a.slots.padded, kFeat)) return -1;
+  const Shape main_shape = shape_of(a, (int64_t)a.feat_tiles * a.row_tiles, num_sms);
+  const int chunks = (a.slots.padded + kRowRanks - 1) / kRowRanks;
+  if ((int64_t)rows * chunks <= 8 * num_sms) {
+    k_adapter_rows<<<dim3((unsigned)rows, (unsigned)chunks), kRowThreads, 0, st>>>((const __nv_bfloat16*)x, x_stride, rows, p.in_dim, a.nt, adapter,
+                                                                                    p.num_adapters, a.slots, (const __nv_bfloat16*)p.a_dev, status);
+    if (cudaGetLastError() != cudaSuccess) return -1;
+    return launch_main<kWith>(w_map, x_map, b_map, a, main_shape, st) < 0 ? -1 : 2;
+  }
+  k_adapter_slots<<<(unsigned)a.row_tiles, 256, 0, st>>>(adapter, rows, a.nt, p.num_adapters, a.slots, status);
+  if (cudaGetLastError() != cudaSuccess) return -1;
+  // A x: as many tiles as there can be slots; those of none are passed over.  Shared out as if every tile of x had one.
+  ProjectArgs d = a;
+  CUtensorMap a_map;
+  if (!make_map(&a_map, p.a_dev, 0, (int64_t)p.num_adapters * p.rank, p.in_dim, p.in_dim, kStep, p.rank)) return -1;
+  const int per_tile = kFeat / a.slots.padded;
+  d.feat_tiles = (a.slots.most + per_tile - 1) / per_tile;
+  Shape shape = shape_of(d, (int64_t)a.row_tiles, num_sms);
+  const int most_groups = std::max(1, num_sms * 3 / 4 / d.splits);
+  int64_t down_groups = shape.ctas / d.splits;  // at most one per tile of x; more where multiprocessors are left
+  if (down_groups == a.row_tiles) down_groups *= std::max<int64_t>(1, std::min<int64_t>(d.feat_tiles, most_groups / down_groups));
+  shape.ctas = (int)down_groups * d.splits;
+  if (launch_main<kDown>(a_map, x_map, b_map, d, shape, st) < 0) return -1;
+  return launch_main<kWith>(w_map, x_map, b_map, a, main_shape, st) < 0 ? -1 : 3;
 }
 
 int launch_project(const gf_projection_t& p, int rows, const void* x, int64_t x_stride, const int32_t* adapter, void* y, int64_t y_stride, int y_fp32,
