@@ -52,9 +52,19 @@ class Projection:
                                   scale.device != weight.device):
             raise ValueError(f"scale: a contiguous fp32 tensor [{adapters}] on {weight.device}")
         self.weight, self.a, self.b, self.scale = weight, a, b, scale
+        self.in_dim, self.out_dim, self.adapters, self.index = in_dim, out_dim, adapters, weight.get_device()
+        self._scratch = {}
         # (a weight of one row may have any stride)
         stride = weight.stride(0) if out_dim > 1 else -(-in_dim // 8) * 8
         self.desc = B.ProjectionDesc(in_dim, out_dim, weight.data_ptr(), stride, adapters, rank, _ptr(a), _ptr(b), _ptr(scale))
+
+
+    def scratch_bytes(self, rows: int) -> int:
+        """gf_adapter_project_scratch_bytes."""
+        n = self._scratch.get(rows)
+        if n is None:
+            n = self._scratch[rows] = B.gf_adapter_project_scratch_bytes(self.desc, rows)
+        return n
 
 
 class TokenLogprobs(NamedTuple):
@@ -68,6 +78,14 @@ class TokenLogprobs(NamedTuple):
 
 def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
+
+
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
+
+
+def _ints(t: torch.Tensor, n: int, index: int) -> bool:
+    """A contiguous int32 tensor [n] on the CUDA device `index`."""
+    return t.dtype is torch.int32 and t.dim() == 1 and t.numel() == n and t.is_contiguous() and t.get_device() == index
 
 
 class PathAttention:
@@ -116,6 +134,7 @@ class PathAttention:
             B.check(B.gf_kv4_pool_attach(self.g, self.pool4.data_ptr(), nbytes), "gf_kv4_pool_attach")
         self.path_ptr = torch.from_numpy(w.path_ptr.astype(np.int32)).to(self.dev)
         self.path_node = torch.from_numpy(w.path_node.astype(np.int32)).to(self.dev)
+        self._lib, self._index = B.lib(), self.pool.get_device()
         self.tables = None
         self._qtab = None
         _live.add(self)
@@ -316,88 +335,100 @@ class PathAttention:
         """gf_node_kv_close: the node has this many tokens from here on."""
         B.check(B.gf_node_kv_close(self.g, node, tokens, self.stream), "gf_node_kv_close")
 
-    def _check_ints(self, name: str, t: torch.Tensor, n: Optional[int] = None) -> None:
-        if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.get_device() != self.pool.get_device() or (n is not None and t.shape[0] != n):
-            raise ValueError(f"{name}: a contiguous int32 tensor [{'requests' if n is None else n}] on {self.pool.device}")
+    def _refuse_ints(self, **tensors) -> None:
+        """(The checks of the calls below stand in one expression each: a decode step makes many of them, at 0.1 us a question.)"""
+        n = {name: want for name, (_, want) in tensors.items()}
+        raise ValueError(", ".join(f"{name}: a contiguous int32 tensor [{want}]" for name, want in n.items()) + f" on {self.pool.device}")
 
     def append_slots(self, nodes: torch.Tensor, counts: torch.Tensor, num_new: int, held: Optional[torch.Tensor] = None):
         """gf_append_slots: request r gets counts[r] tokens in the open node nodes[r], behind the held[r] that stay (None: behind all
         that it holds).  Token slots of the num_new rows and the nodes' new lengths, int32.  Build the tables anew after it."""
-        self._check_ints("nodes", nodes)
-        n = nodes.shape[0]
-        self._check_ints("counts", counts, n)
-        if held is not None:
-            self._check_ints("held", held, n)
+        n, ix = nodes.numel(), self._index
+        if not (_ints(nodes, n, ix) and _ints(counts, n, ix) and (held is None or _ints(held, n, ix))):
+            self._refuse_ints(nodes=(nodes, "requests"), counts=(counts, "requests"), held=(held, "requests"))
         if num_new < 0:
             raise ValueError("num_new: at least 0")
-        both = self.path_ptr.new_empty((num_new + n,))
-        slots, lens = both[:num_new], both[num_new:]
-        B.check(B.gf_append_slots(self.g, n, nodes.data_ptr(), _ptr(held), counts.data_ptr(), num_new, slots.data_ptr(), lens.data_ptr(),
-                                  self.stream), "gf_append_slots")
-        return slots, lens
+        both = nodes.new_empty((num_new + n,))
+        at = both.data_ptr()
+        st = self._lib.gf_append_slots(self.g, n, nodes.data_ptr(), None if held is None else held.data_ptr(), counts.data_ptr(), num_new, at,
+                                       at + 4 * num_new, _raw_stream(ix))
+        if st:
+            B.check(st, "gf_append_slots")
+        return both.split_with_sizes((num_new, n))
 
     def append(self, layer: int, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor) -> None:
         """gf_node_kv_append of bf16 rows [new, Hkv, D], which may be parts of wider rows (heads next to each other)."""
-        self._check_ints("slots", slots)
-        row = (slots.shape[0], self.w.num_kv_heads, self.w.head_dim)
-        for t in (k, v):
-            if t.dtype != torch.bfloat16 or tuple(t.shape) != row or t.get_device() != self.pool.get_device() or t.stride(2) != 1 or \
-                    (row[1] > 1 and t.stride(1) != row[2]):
-                raise ValueError(f"k, v: bf16 tensors {list(row)} on {self.pool.device}, the entries of a token next to each other")
-        B.check(B.gf_node_kv_append(self.g, layer, row[0], slots.data_ptr(), k.data_ptr(), k.stride(0) if row[0] > 1 else 0, v.data_ptr(),
-                                    v.stride(0) if row[0] > 1 else 0, self.stream), "gf_node_kv_append")
+        n, ix, hkv, d = slots.numel(), self._index, self.w.num_kv_heads, self.w.head_dim
+        ks, vs = k.stride(), v.stride()
+        if not (_ints(slots, n, ix) and k.dtype is v.dtype is torch.bfloat16 and k.shape == v.shape == (n, hkv, d) and
+                k.get_device() == v.get_device() == ix and ks[2] == vs[2] == 1 and (hkv == 1 or ks[1] == vs[1] == d)):
+            raise ValueError(f"slots: a contiguous int32 tensor [new]; k, v: bf16 tensors [new, {hkv}, {d}], the entries of a token next to each "
+                             f"other; on {self.pool.device}")
+        many = n > 1  # (one row may have any stride)
+        st = self._lib.gf_node_kv_append(self.g, layer, n, slots.data_ptr(), k.data_ptr(), ks[0] if many else 0, v.data_ptr(), vs[0] if many else 0,
+                                         _raw_stream(ix))
+        if st:
+            B.check(st, "gf_node_kv_append")
 
     # ---- before and behind the attention -------------------------------------------------------
     def project(self, projection: Projection, x: torch.Tensor, adapters: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                 dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
         """gf_adapter_project: x [rows, in] times the shared weight, each row with the adapter that adapters[row] names (-1, or
         adapters None: none).  [rows, out] in bf16 or fp32, into `out` where given."""
-        d = projection.desc
+        p, ix = projection, self._index
+        xs = x.stride()
+        if not (x.dtype is torch.bfloat16 and len(xs) == 2 and x.shape[1] == p.in_dim and xs[1] == 1 and x.get_device() == p.index == ix):
+            raise ValueError(f"x: a bf16 tensor [rows, {p.in_dim}] on {self.pool.device} like the projection, entries of a row next to each other")
         rows = x.shape[0]
-        if x.dtype != torch.bfloat16 or x.dim() != 2 or x.shape[1] != d.in_dim or x.stride(1) != 1 or x.get_device() != self.pool.get_device() or \
-                projection.weight.get_device() != self.pool.get_device():
-            raise ValueError(f"x: a bf16 tensor [rows, {d.in_dim}] on {self.pool.device} like the projection, entries of a row next to each other")
-        if adapters is not None:
-            self._check_ints("adapters", adapters, rows)
-            if d.num_adapters == 0:
+        if adapters is not None and not (p.adapters and _ints(adapters, rows, ix)):
+            if not p.adapters:
                 raise ValueError("adapters: the projection has none")
+            self._refuse_ints(adapters=(adapters, rows))
         if out is None:
             if dtype not in (torch.bfloat16, torch.float32):
                 raise ValueError("dtype: bf16 or fp32")
-            out = x.new_empty((rows, d.out_dim), dtype=dtype)
-        elif out.dtype not in (torch.bfloat16, torch.float32) or tuple(out.shape) != (rows, d.out_dim) or out.stride(1) != 1 or \
-                out.get_device() != x.get_device():
-            raise ValueError(f"out: a bf16 or fp32 tensor [{rows}, {d.out_dim}] on {self.pool.device}, entries of a row next to each other")
+            out = x.new_empty((rows, p.out_dim), dtype=dtype)
+            ys = p.out_dim
+        else:
+            dtype = out.dtype
+            if dtype not in (torch.bfloat16, torch.float32) or out.shape != (rows, p.out_dim) or out.stride(1) != 1 or out.get_device() != ix:
+                raise ValueError(f"out: a bf16 or fp32 tensor [{rows}, {p.out_dim}] on {self.pool.device}, entries of a row next to each other")
+            ys = out.stride(0) if rows > 1 else p.out_dim
         if rows == 0:
             return out
         scratch, nbytes = None, 0
         if adapters is not None:
-            nbytes = B.gf_adapter_project_scratch_bytes(d, rows)
+            nbytes = p.scratch_bytes(rows)
             scratch = x.new_empty((nbytes,), dtype=torch.uint8)
-        B.check(B.gf_adapter_project(self.g, d, rows, x.data_ptr(), x.stride(0) if rows > 1 else d.in_dim, _ptr(adapters), out.data_ptr(),
-                                     out.stride(0) if rows > 1 else d.out_dim, out.dtype == torch.float32, _ptr(scratch), nbytes, self.stream),
-                "gf_adapter_project")
+        st = self._lib.gf_adapter_project(self.g, p.desc, rows, x.data_ptr(), xs[0] if rows > 1 else p.in_dim,
+                                          None if adapters is None else adapters.data_ptr(), out.data_ptr(), ys, dtype is torch.float32,
+                                          None if scratch is None else scratch.data_ptr(), nbytes, _raw_stream(ix))
+        if st:
+            B.check(st, "gf_adapter_project")
         return out
 
     def token_logprobs(self, logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, top: int = 0) -> TokenLogprobs:
         """gf_token_logprobs of bf16 or fp32 logits [rows, vocab]: log probabilities of the given tokens (-1: none), entropy,
         log-sum-exp, and the `top` most likely tokens with their log probabilities."""
-        if logits.dtype not in (torch.bfloat16, torch.float32) or logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1) or \
-                logits.get_device() != self.pool.get_device():
+        ix, strides = self._index, logits.stride()
+        fp32 = logits.dtype is torch.float32
+        if not ((fp32 or logits.dtype is torch.bfloat16) and len(strides) == 2 and (strides[1] == 1 or logits.shape[1] == 1) and logits.get_device() == ix):
             raise ValueError(f"logits: a bf16 or fp32 tensor [rows, vocab] on {self.pool.device}, entries of a row next to each other")
         rows, vocab = logits.shape
-        if tokens is not None:
-            self._check_ints("tokens", tokens, rows)
+        if tokens is not None and not _ints(tokens, rows, ix):
+            self._refuse_ints(tokens=(tokens, rows))
         if not 0 <= top <= min(B.GF_MAX_TOP, vocab):
             raise ValueError(f"top: 0 to {min(B.GF_MAX_TOP, vocab)}")
-        stats = logits.new_empty((3 + top, rows), dtype=torch.float32)
-        logprob, entropy, lse = stats[:3].unbind(0)
-        top_logprobs = stats[3:].view(rows, top)
-        top_ids = self.path_ptr.new_empty((rows, top))
-        out = B.Logprobs(None if tokens is None else logprob.data_ptr(), entropy.data_ptr(), lse.data_ptr(), top_ids.data_ptr() if top else None,
+        stats = logits.new_empty((3, rows), dtype=torch.float32)
+        at = stats.data_ptr()
+        top_ids, top_logprobs = logits.new_empty((rows, top), dtype=torch.int32), logits.new_empty((rows, top), dtype=torch.float32)
+        out = B.Logprobs(None if tokens is None else at, at + 4 * rows, at + 8 * rows, top_ids.data_ptr() if top else None,
                          top_logprobs.data_ptr() if top else None)
-        B.check(B.gf_token_logprobs(self.g, rows, vocab, logits.data_ptr(), logits.stride(0) if rows > 1 else vocab,
-                                    logits.dtype == torch.float32, _ptr(tokens), top, out, self.stream), "gf_token_logprobs")
+        st = self._lib.gf_token_logprobs(self.g, rows, vocab, logits.data_ptr(), strides[0] if rows > 1 else vocab, fp32,
+                                         None if tokens is None else tokens.data_ptr(), top, out, _raw_stream(ix))
+        if st:
+            B.check(st, "gf_token_logprobs")
+        logprob, entropy, lse = stats.unbind(0)
         return TokenLogprobs(None if tokens is None else logprob, entropy, lse, top_ids, top_logprobs)
 
     # ---- eviction by accumulated attention weight --------------------------------------------
