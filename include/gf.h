@@ -541,7 +541,7 @@ typedef struct {
   const float* scale_dev; /* fp32 [num_adapters] */
 } gf_projection_t;
 
-/* Scratch of a call with adapters, 16-byte aligned: up to 512 bytes per rank, row and 256 adapters, for at most 16 384 rows at a time; two calls that may overlap on the GPU each need their own. */
+/* Scratch of a call with adapters, 16-byte aligned: up to 6 bytes per rank (16, 32 or 64), row and adapter (256 at most), for at most 16 384 rows at a time; two calls that may overlap on the GPU each need their own. */
 uint64_t gf_adapter_project_scratch_bytes(const gf_projection_t* p, int32_t rows);
 
 /* x_dev: bf16 [rows, in_dim], rows x_stride entries apart (a multiple of 8), 16-byte aligned.  adapter_dev: int32 [rows], or NULL for

@@ -8,12 +8,16 @@
 //
 // The adapters are more entries of K.  For every adapter that rows of a tile of x name (a slot of the tile), h = scale_a A_a x is a
 // [rows, rank] operand with zeros in the other rows, and B_a, [features, rank], stands beside W: the sums go on over the tile's
-// slots, in the same pipeline, and nothing is left for the warps that take them out of tensor memory.  h is rounded to two bf16
-// numbers, its nearest and the nearest of what is left (2^-17 of it), and multiplied twice.
+// slots, in the same pipeline, and nothing is left for the warps that take them out of tensor memory.  h is held in two bf16
+// numbers, its nearest and the nearest of what is left (off by 2^-17 of it), and multiplied twice; for results in fp32 in three (2^-25).
 // A x goes the same way as W x: the rows of the A of 8, 4 or 2 slots (of rank 16, 32, 64) stand in W's place, for all rows of the tile, and
 // what comes out is kept where row and slot belong together and written as those operands, in the layout of shared memory.
 // Three launches: the slots, A x, W x; only the copies behind a tile's last entry of W wait for the second.  (Few rows: the first two are
 // one, k_adapter_rows.)
+//
+// Results in fp32: tensor memory's sums are cut off, not rounded, where an MMA adds to them, 1.8e-8 of the sum each time (measured: 4.4e-6 after
+// 256), so every 8 stages they are taken out and added, rounded, to sums that stand beside them; 5e-7 is left.  (Those sums in registers spilled.)
+//
 // (The same sums on the CUDA cores, while the MMAs ran, took 568 us for 8192 rows with adapters of rank 16 and 1143 of rank 64,
 // where W x alone takes 295: their reads of B and h wait behind the copies' traffic.)
 #include <cuda.h>
@@ -28,6 +32,8 @@ namespace {
 constexpr int kFeat = 128;        // output features of a tile
 constexpr int kStep = 64;         // entries of K in a stage
 constexpr int kThreads = 256;
+constexpr int kWideThreads = 384; // with eight warps that take the sums out
+constexpr int kChunk = 8;         // fp32 results: stages after which the sums are taken out
 constexpr int kGroup = 8;         // rows of x that are taken out of tensor memory together
 
 // The slots of the tiles of x, in the caller's scratch.
@@ -36,8 +42,9 @@ struct Slots {
   int32_t* adapter;      // [row_tiles][most]
   int32_t* of_row;       // [rows] a row's slot in its tile, -1: none
   const float* scale;    // [num_adapters] or null
-  char* h;               // [row_tiles][most][2][nt][padded rank], swizzled like a stage's operand
+  char* h;               // [row_tiles][most][numbers][nt][padded rank], swizzled like a stage's operand
   int most;
+  int numbers;           // that h is held in: 2 or 3
   int rank, padded;      // padded: 16, 32 or 64
   uint32_t block;        // bytes of one [nt][padded]
 };
@@ -48,6 +55,8 @@ struct ProjectArgs {
   int pair;                             // stages that are given back together: 1 or 2
   int splits;                           // CTAs that share a tile
   uint32_t tmem_cols, acc_cols;         // allocated; from one accumulator to the next
+  int accs;                             // accumulators: 1 or 2
+  uint32_t sum_cols;                    // fp32: where the sums stand
   Slots slots;
   void* y;
   int64_t y_stride;
@@ -143,44 +152,48 @@ struct HPlace {
     const int j = m / sl.padded;
     r = m - j * sl.padded;
     slot = first_slot + j;
-    at = slot < slots ? sl.h + ((int64_t)row_tile * sl.most + slot) * 2 * sl.block : nullptr;
+    at = slot < slots ? sl.h + ((int64_t)row_tile * sl.most + slot) * sl.numbers * sl.block : nullptr;
     scale = 0.f;
     if (at != nullptr && r < sl.rank) scale = sl.scale != nullptr ? __ldg(sl.scale + __ldcg(sl.adapter + (int64_t)row_tile * sl.most + slot)) : 1.f;
   }
 };
-__device__ __forceinline__ void split_h(float v, __nv_bfloat16& first, __nv_bfloat16& left) {
-  first = __float2bfloat16_rn(v);
-  left = __float2bfloat16_rn(fabsf(v) <= 3.3895e38f ? v - __bfloat162float(first) : 0.f);  // (nothing is left of an infinity, or a NaN)
+// v's next number: the nearest bf16 to it; v becomes what is left.  (Nothing is left of an infinity, or a NaN.)
+__device__ __forceinline__ __nv_bfloat16 take_number(float& v) {
+  const __nv_bfloat16 n = __float2bfloat16_rn(v);
+  v = fabsf(v) <= 3.3895e38f ? v - __bfloat162float(n) : 0.f;
+  return n;
 }
 // One result, or four of neighbouring ranks, of a row; zeros where the row is another slot's.
 __device__ __forceinline__ void store_h(const Slots& sl, const HPlace& p, int row_in_tile, int row_slot, float v) {
   if (p.at == nullptr) return;
-  __nv_bfloat16 first, left;
-  split_h(row_slot == p.slot && p.r < sl.rank ? v * p.scale : 0.f, first, left);
+  v = row_slot == p.slot && p.r < sl.rank ? v * p.scale : 0.f;
   char* at = p.at + operand_at(row_in_tile, p.r >> 3, sl.padded * 2) + (p.r & 7) * 2;
-  *reinterpret_cast<__nv_bfloat16*>(at) = first;
-  *reinterpret_cast<__nv_bfloat16*>(at + sl.block) = left;
+  for (int i = 0; i < sl.numbers; ++i) *reinterpret_cast<__nv_bfloat16*>(at + i * sl.block) = take_number(v);
 }
 __device__ __forceinline__ void store_h4(const Slots& sl, const HPlace& p, int row_in_tile, int row_slot, float4 v) {
   if (p.at == nullptr) return;
   const bool mine = row_slot == p.slot && p.r < sl.rank;  // (ranks are multiples of 8)
-  __align__(8) __nv_bfloat16 first[4], left[4];
-  split_h(mine ? v.x * p.scale : 0.f, first[0], left[0]);
-  split_h(mine ? v.y * p.scale : 0.f, first[1], left[1]);
-  split_h(mine ? v.z * p.scale : 0.f, first[2], left[2]);
-  split_h(mine ? v.w * p.scale : 0.f, first[3], left[3]);
+  v.x = mine ? v.x * p.scale : 0.f;
+  v.y = mine ? v.y * p.scale : 0.f;
+  v.z = mine ? v.z * p.scale : 0.f;
+  v.w = mine ? v.w * p.scale : 0.f;
   char* at = p.at + operand_at(row_in_tile, p.r >> 3, sl.padded * 2) + (p.r & 7) * 2;
-  *reinterpret_cast<uint2*>(at) = *reinterpret_cast<uint2*>(first);
-  *reinterpret_cast<uint2*>(at + sl.block) = *reinterpret_cast<uint2*>(left);
+  for (int i = 0; i < sl.numbers; ++i) {
+    __align__(8) __nv_bfloat16 n[4] = {take_number(v.x), take_number(v.y), take_number(v.z), take_number(v.w)};
+    *reinterpret_cast<uint2*>(at + i * sl.block) = *reinterpret_cast<uint2*>(n);
+  }
 }
 
 // Shared memory: the ring of stages (kFeat rows of W, then nt rows of x, 128 bytes each, 128-byte swizzle; a stage of the
-// adapters holds one slot of rank 32, two of rank 16, or the first or second half of one of rank 64), which a cluster uses
-// again for its parts of the sums; behind it the barriers.
+// adapters holds a slot's B and as many of its h's numbers as are 128 bytes a row, or two slots of rank 16 with both their numbers),
+// which a cluster uses again for its parts of the sums; behind it the barriers.
 // Warp 0 issues the copies, warp 1 the MMAs, warps 4 to 7 take the sums out; the parts of a cluster are joined by all.
-template <int kMode>
-__global__ void __launch_bounds__(kThreads, 2) k_project(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map,
+// kExact: results in fp32, whose sums are taken out by so many warps: 4, or 8 for the tiles of 256 rows, for which tensor memory holds no second
+// accumulator to go on in meanwhile.  0: results in bf16.
+template <int kMode, int kExact>
+__global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact == 8 ? 1 : 2) k_project(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map,
                                                          const __grid_constant__ CUtensorMap b_map, const __grid_constant__ ProjectArgs a) {
+  constexpr int kWarps = (kExact == 8 ? kWideThreads : kThreads) / 32, kTakers = kWarps - 4;
   extern __shared__ __align__(1024) char smem_raw[];
   char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   const uint32_t w_bytes = kFeat * 128u, x_bytes = (uint32_t)a.nt * 128u, stage_bytes = w_bytes + x_bytes;
@@ -231,7 +244,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_project(const __grid_constant__
   };
   if (tid == 0) {
     for (int i = 0; i < a.stages; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(acc_full + i, 1); mbar_init(acc_empty + i, 4); }
+    for (int i = 0; i < 2; ++i) { mbar_init(acc_full + i, 1); mbar_init(acc_empty + i, kTakers); }
     mbar_init(drained, 1);
     mbar_fence_init();
   }
@@ -246,11 +259,23 @@ __global__ void __launch_bounds__(kThreads, 2) k_project(const __grid_constant__
     asm volatile("griddepcontrol.wait;" ::: "memory");
   }
 
+  // the stages of n slots
+  constexpr int kNumbers = kExact ? 3 : 2;
+  const bool two_slots = kNumbers == 2 && h_row == 32;
+  const int per_stage = h_row == 128 ? 1 : h_row == 64 ? 2 : 4;  // numbers
+  const int a_slot = h_row == 128 ? kNumbers : h_row == 64 ? (kNumbers + 1) / 2 : 1;
+  auto slot_stages = [&](int n) { return two_slots ? (n + 1) / 2 : n * a_slot; };
+
   int s = 0;           // the role's stage and its phase
   uint32_t phase = 0;
   uint32_t used = 0, phases = 0;  // stages that copies have been issued for, and the last phase of each
-  int done = 0;                   // tiles
+  int done = 0;                   // accumulators: tiles, or their chunks
+  auto acc_at = [&] { return a.accs == 2 ? done & 1 : 0; };
+  auto acc_phase = [&] { return (uint32_t)(a.accs == 2 ? done >> 1 : done) & 1u; };
   bool ok = true, waited = kMode != kWith;
+  // a warp that takes sums out: row m of the tile of W, columns col0 .. col0 + cols (rows of x)
+  const int m = (wid & 3) * 32 + lane, cols = kTakers == 8 ? a.nt / 2 : a.nt, col0 = kTakers == 8 && wid >= 8 ? cols : 0;
+  const uint32_t lanes = tmem + ((uint32_t)((wid & 3) * 32) << 16);
   // A CTA by itself goes through its tiles in one round, so that the roles run ahead of each other; a cluster takes a round per tile.
   Tile now = start();
   while (more(now)) {
@@ -296,36 +321,32 @@ __global__ void __launch_bounds__(kThreads, 2) k_project(const __grid_constant__
             s0 = s1 * part / a.splits;
             s1 = s1 * (part + 1) / a.splits;
             int ahead[2] = {s0 < s1 ? __ldcg(which + s0) : 0, s0 + 1 < s1 ? __ldcg(which + s0 + 1) : 0};  // of the next two slots
-            const char* h = sl.h + (int64_t)row_tile * sl.most * 2 * sl.block;
-            for (int i = s0; i < s1 && ok; ++i) {
-              const int id = ahead[0], id2 = ahead[1];
-              const int taken = h_row == 32 ? 2 : 1;
-              ahead[0] = taken == 2 ? (i + 2 < s1 ? __ldcg(which + i + 2) : 0) : id2;
-              ahead[1] = i + taken + 1 < s1 ? __ldcg(which + i + taken + 1) : 0;
-              if (!(ok = free())) break;
-              char* at = smem + s * stage_bytes;
-              if (h_row == 128) {
-                for (int half = 0; half < 2 && ok; ++half) {
-                  at = smem + s * stage_bytes;
-                  if (half && !(ok = free())) break;
-                  mbar_arrive_expect_tx(full + s, b_bytes + sl.block);
-                  tma_load_3d(at, &b_map, 0, f0, id, full + s);
-                  bulk_g2s(at + w_bytes, h + (int64_t)(2 * i + half) * sl.block, sl.block, full + s);
-                  next();
-                }
-              } else if (h_row == 64) {
-                mbar_arrive_expect_tx(full + s, b_bytes + 2 * sl.block);
+            const uint64_t slot_bytes = (uint64_t)kNumbers * sl.block;
+            const char* h = sl.h + ((int64_t)row_tile * sl.most + s0) * slot_bytes;
+            for (int i = s0; i < s1 && ok; h += slot_bytes) {
+              const int id = ahead[0], id2 = ahead[1], taken = two_slots && i + 1 < s1 ? 2 : 1;
+              i += taken;
+              ahead[0] = taken == 2 ? (i < s1 ? __ldcg(which + i) : 0) : id2;
+              ahead[1] = i + 1 < s1 ? __ldcg(which + i + 1) : 0;
+              if (two_slots) {
+                if (!(ok = free())) break;
+                char* at = smem + s * stage_bytes;
+                mbar_arrive_expect_tx(full + s, taken * (b_bytes + 2 * sl.block));
                 tma_load_3d(at, &b_map, 0, f0, id, full + s);
-                bulk_g2s(at + w_bytes, h + (int64_t)(2 * i) * sl.block, 2 * sl.block, full + s);
+                if (taken == 2) tma_load_3d(at + b_bytes, &b_map, 0, f0, id2, full + s);
+                bulk_g2s(at + w_bytes, h, taken * 2 * sl.block, full + s);
+                h += (taken - 1) * slot_bytes;
                 next();
               } else {
-                const int both = i + 1 < s1 ? 2 : 1;
-                mbar_arrive_expect_tx(full + s, both * (b_bytes + 2 * sl.block));
-                tma_load_3d(at, &b_map, 0, f0, id, full + s);
-                if (both == 2) tma_load_3d(at + b_bytes, &b_map, 0, f0, id2, full + s);
-                bulk_g2s(at + w_bytes, h + (int64_t)(2 * i) * sl.block, both * 2 * sl.block, full + s);
-                i += both - 1;
-                next();
+                for (int j = 0; j < kNumbers; j += per_stage) {
+                  if (!(ok = free())) break;
+                  char* at = smem + s * stage_bytes;
+                  const uint32_t bytes = min(per_stage, kNumbers - j) * sl.block;
+                  mbar_arrive_expect_tx(full + s, b_bytes + bytes);
+                  tma_load_3d(at, &b_map, 0, f0, id, full + s);
+                  bulk_g2s(at + w_bytes, h + j * (int64_t)sl.block, bytes, full + s);
+                  next();
+                }
               }
             }
           }
@@ -354,18 +375,34 @@ __global__ void __launch_bounds__(kThreads, 2) k_project(const __grid_constant__
           if (++s == a.stages) { s = 0; phase ^= 1u; }
         };
         for (Tile t = now; more(t) && ok; advance(t)) {
-          const int buf = done & 1, row_tile = t.r;
+          const int row_tile = t.r;
           int s0 = 0, s1 = 0;
           if (kMode == kWith && waited) s1 = slots_of(row_tile);
-          if (!(ok = mbar_wait(acc_empty + buf, ((done >> 1) & 1) ^ 1, a.status))) break;
-          tc_fence_after_sync();
-          const uint32_t d = tmem + buf * a.acc_cols;
+          uint32_t d = 0;
+          int in_acc = 0;  // stages in the accumulator
+          auto open = [&] {
+            in_acc = 0;
+            d = tmem + acc_at() * a.acc_cols;
+            const bool got = mbar_wait(acc_empty + acc_at(), acc_phase() ^ 1u, a.status);
+            tc_fence_after_sync();
+            return got;
+          };
+          auto chunk = [&] {  // the next stage's accumulator
+            if (kExact && in_acc == kChunk) {
+              tc_commit(acc_full + acc_at());
+              ++done;
+              if (!open()) return false;
+            }
+            ++in_acc;
+            return true;
+          };
+          if (!(ok = open())) break;
           for (int k = step0; k < step1; ++k) {
-            if (!(ok = filled())) break;
+            if (!(ok = filled() && chunk())) break;
             tc_fence_after_sync();
             const uint64_t wd = first_desc + (uint64_t)((uint32_t)s * stage_bytes >> 4);
             peek();
-            umma_ss4(d, wd, wd + (w_bytes >> 4), idesc, k > step0);
+            umma_ss4(d, wd, wd + (w_bytes >> 4), idesc, in_acc > 1);
             next();
           }
           if (kMode == kWith && ok) {
@@ -376,22 +413,37 @@ __global__ void __launch_bounds__(kThreads, 2) k_project(const __grid_constant__
             }
             s0 = s1 * part / a.splits;
             s1 = s1 * (part + 1) / a.splits;
-            // stages: two a slot of rank 64, one of rank 32, one for two of rank 16
-            const int stages = h_row == 128 ? 2 * (s1 - s0) : h_row == 64 ? s1 - s0 : (s1 - s0 + 1) / 2;
+            const int stages = slot_stages(s1 - s0);
             for (int i = 0; i < stages; ++i) {
-              if (!(ok = filled())) break;
+              if (!(ok = filled() && chunk())) break;
               tc_fence_after_sync();
               const uint32_t at = smem_u32(smem + s * stage_bytes), ht = at + w_bytes;
               peek();
+              // the numbers of h in this stage, each with its slot's B
+              const uint32_t on = in_acc > 1;
               if (h_row == 128) {
-                umma_ss4(d, operand_desc(at, 128), operand_desc(ht, 128), idesc, 1);
+                umma_ss4(d, operand_desc(at, 128), operand_desc(ht, 128), idesc, on);
               } else if (h_row == 64) {
-                const uint64_t bd = operand_desc(at, 64);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) umma_ss(d, bd + 2 * (j & 1), operand_desc(ht + (j >> 1) * sl.block, 64) + 2 * (j & 1), idesc, 1);
+                const uint64_t bd = operand_desc(at, 64), hd = operand_desc(ht, 64), hd2 = operand_desc(ht + sl.block, 64);
+                umma_ss(d, bd, hd, idesc, on);
+                umma_ss(d, bd + 2, hd + 2, idesc, 1);
+                if (kNumbers == 2 || (i & 1) == 0) {
+                  umma_ss(d, bd, hd2, idesc, 1);
+                  umma_ss(d, bd + 2, hd2 + 2, idesc, 1);
+                }
+              } else if (kNumbers == 2) {
+                const uint64_t bd = operand_desc(at, 32), bd2 = operand_desc(at + b_bytes, 32), hd = operand_desc(ht, 32);
+                const uint64_t next_h = sl.block >> 4;
+                umma_ss(d, bd, hd, idesc, on);
+                umma_ss(d, bd, hd + next_h, idesc, 1);
+                if (s0 + 2 * i + 1 < s1) {
+                  umma_ss(d, bd2, hd + 2 * next_h, idesc, 1);
+                  umma_ss(d, bd2, hd + 3 * next_h, idesc, 1);
+                }
               } else {
-                const int both = s0 + 2 * i + 1 < s1 ? 4 : 2;
-                for (int j = 0; j < both; ++j) umma_ss(d, operand_desc(at + (j >> 1) * b_bytes, 32), operand_desc(ht + j * sl.block, 32), idesc, 1);
+                const uint64_t bd = operand_desc(at, 32), hd = operand_desc(ht, 32);
+#pragma unroll
+                for (int j = 0; j < kNumbers; ++j) umma_ss(d, bd, hd + j * (sl.block >> 4), idesc, on || j > 0);
               }
               next();
             }
@@ -401,7 +453,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_project(const __grid_constant__
             if (++s == a.stages) { s = 0; phase ^= 1u; }
             ready = false;
           }
-          tc_commit(acc_full + buf);
+          tc_commit(acc_full + acc_at());
           ++done;
           if (a.splits > 1) break;
         }
@@ -411,26 +463,61 @@ __global__ void __launch_bounds__(kThreads, 2) k_project(const __grid_constant__
         }
       }
     } else if (wid >= 4) {
-      const int w = wid - 4;
-      const uint32_t lanes = tmem + ((uint32_t)(w * 32) << 16);
       if (kMode == kWith && !waited) {
         asm volatile("griddepcontrol.wait;" ::: "memory");  // (what is written here may be read by kernels before)
         waited = true;
       }
       for (Tile t = now; more(t); advance(t)) {
-        const int f = t.f, m = w * 32 + lane, row_tile = t.r, t0 = row_tile * a.nt, buf = done & 1;
-        if (!(ok = __all_sync(0xffffffffu, ok && mbar_wait(acc_full + buf, (done >> 1) & 1, a.status)))) break;
-        tc_fence_after_sync();
-        if (a.splits > 1) break;  // taken out below, by the whole cluster
-        ++done;
+        const int f = t.f, row_tile = t.r, t0 = row_tile * a.nt;
+        auto wait_sums = [&] {
+          ok = __all_sync(0xffffffffu, ok && mbar_wait(acc_full + acc_at(), acc_phase(), a.status));
+          tc_fence_after_sync();
+          return ok;
+        };
+        auto sums_taken = [&] {
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(acc_empty + acc_at());
+          ++done;
+        };
+        uint32_t from = lanes + acc_at() * a.acc_cols + col0;
+        if (kExact) {
+          int stages = step1 - step0;
+          if (kMode == kWith) {
+            const int n = slots_of(row_tile);
+            stages += slot_stages(n * (part + 1) / a.splits - n * part / a.splits);
+          }
+          const uint32_t sums = lanes + a.sum_cols + col0;
+          for (int c = 0; c < stages && wait_sums(); c += kChunk) {
+            from = lanes + acc_at() * a.acc_cols + col0;
+            for (int g = 0; g < cols; g += kGroup) {
+              uint32_t r[kGroup], q[kGroup];
+              tmem_ld8(from + g, r);
+              if (c > 0) tmem_ld8(sums + g, q);
+              tmem_wait_ld();
+              if (c > 0) {
+#pragma unroll
+                for (int j = 0; j < kGroup; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) + __uint_as_float(q[j]));
+              }
+              tmem_st8(sums + g, r);
+            }
+            tmem_wait_st();
+            sums_taken();
+          }
+          from = sums;
+        } else {
+          wait_sums();
+        }
+        if (!ok || a.splits > 1) break;  // (joined below, by the whole cluster)
         auto take = [&](auto&& store) {
-          for (int g = 0; g < a.nt && t0 + g < a.rows; g += kGroup) {
+          for (int g = 0; g < cols && t0 + col0 + g < a.rows; g += kGroup) {
             uint32_t r[kGroup];
-            tmem_ld8(lanes + buf * a.acc_cols + g, r);
+            tmem_ld8(from + g, r);
             tmem_wait_ld();
 #pragma unroll
-            for (int j = 0; j < kGroup; ++j) store(g + j, __uint_as_float(r[j]));
+            for (int j = 0; j < kGroup; ++j) store(col0 + g + j, __uint_as_float(r[j]));
           }
+          if (!kExact) sums_taken();
         };
         if (kMode == kDown) {
           const HPlace place(sl, row_tile, f * per_tile, t.slots, m);
@@ -438,9 +525,6 @@ __global__ void __launch_bounds__(kThreads, 2) k_project(const __grid_constant__
         } else {
           take([&](int r, float v) { store_y(a, t0 + r, f * kFeat + m, v); });
         }
-        tc_fence_before_sync();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(acc_empty + buf);
       }
     }
     __syncwarp();
@@ -452,25 +536,25 @@ __global__ void __launch_bounds__(kThreads, 2) k_project(const __grid_constant__
       const HPlace place = kMode == kDown ? HPlace(sl, row_tile, f * per_tile, now.slots, lane * 4) : HPlace();
       float* parts = reinterpret_cast<float*>(smem);
       if (wid >= 4) {
-        const int m = (wid - 4) * 32 + lane, buf = done & 1;
-        const uint32_t from = tmem + ((uint32_t)((wid - 4) * 32) << 16) + buf * a.acc_cols;
-        for (int g = 0; g < a.nt; g += 16) {
-          uint32_t r[2][kGroup];
-          tmem_ld8(from + g, r[0]);
-          tmem_ld8(from + g + kGroup, r[1]);
+        const uint32_t from = lanes + (kExact ? a.sum_cols : acc_at() * a.acc_cols) + col0;
+        for (int g = 0; g < cols; g += kGroup) {
+          uint32_t r[kGroup];
+          tmem_ld8(from + g, r);
           tmem_wait_ld();
 #pragma unroll
-          for (int j = 0; j < 16; ++j) parts[(g + j) * kFeat + m] = __uint_as_float(r[j >> 3][j & 7]);
+          for (int j = 0; j < kGroup; ++j) parts[(col0 + g + j) * kFeat + m] = __uint_as_float(r[j]);
         }
-        tc_fence_before_sync();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(acc_empty + buf);
-        ++done;
+        if (!kExact) {
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(acc_empty + acc_at());
+          ++done;
+        }
       }
       __syncwarp();
       cluster_sync_all();
       constexpr int kRows = 4, kParts = 4;  // of a warp on the way
-      const int apart = a.splits * (kThreads / 32);
+      const int apart = a.splits * kWarps;
       for (int r0 = part + a.splits * wid; r0 < n; r0 += apart * kRows) {
         float4 sum[kRows];
         int row_slot[kRows];
@@ -647,17 +731,18 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_adapter_rows(const __nv_bflo
   __syncthreads();
   // the row's pieces (8 ranks) of these 16 ranks, or of their padding, in all slots
   const int pieces = min(2, (sl.padded - r0) >> 3), slot = sb.slot(which);
-  char* base = sl.h + (int64_t)tile * sl.most * 2 * sl.block;
-  for (int i = tid; i < sb.count * 2 * pieces; i += kRowThreads) {
-    const int c = i % pieces, half = i / pieces & 1, at = i / (2 * pieces);
-    __align__(16) __nv_bfloat16 p[8];
+  char* base = sl.h + (int64_t)tile * sl.most * sl.numbers * sl.block;
+  for (int i = tid; i < sb.count * pieces; i += kRowThreads) {
+    const int c = i % pieces, at = i / pieces;
+    float v[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      __nv_bfloat16 first, left;
-      split_h(at == slot ? h[c * 8 + j] : 0.f, first, left);
-      p[j] = half ? left : first;
+    for (int j = 0; j < 8; ++j) v[j] = at == slot ? h[c * 8 + j] : 0.f;
+    for (int n = 0; n < sl.numbers; ++n) {
+      __align__(16) __nv_bfloat16 p[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) p[j] = take_number(v[j]);
+      *reinterpret_cast<uint4*>(base + (int64_t)(sl.numbers * at + n) * sl.block + operand_at(t - t0, (r0 >> 3) + c, sl.padded * 2)) = *reinterpret_cast<uint4*>(p);
     }
-    *reinterpret_cast<uint4*>(base + (int64_t)(2 * at + half) * sl.block + operand_at(t - t0, (r0 >> 3) + c, sl.padded * 2)) = *reinterpret_cast<uint4*>(p);
   }
 }
 
@@ -734,7 +819,8 @@ struct Shape {
 Shape shape_of(ProjectArgs& a, int64_t tiles, int num_sms) {
   const int steps = (a.in_dim + kStep - 1) / kStep;
   const uint32_t stage_bytes = kFeat * 128u + a.nt * 128u, extra = 1024 + 512;
-  const int per_sm = 4 * stage_bytes + extra <= kHalfKb * 1024 ? 2 : 1;
+  // (and only where tensor memory has room for two: CTAs of clusters that wait for each other must never wait for that)
+  const int per_sm = 4 * stage_bytes + extra <= kHalfKb * 1024 && a.nt <= (a.y_fp32 ? 64 : 128) ? 2 : 1;
   a.splits = 1;
   int64_t best = (tiles + num_sms - 1) / num_sms * steps;
   for (int n = 2; n <= 8 && tiles * n <= (int64_t)per_sm * num_sms && steps >= 4 * n; ++n) {
@@ -744,29 +830,32 @@ Shape shape_of(ProjectArgs& a, int64_t tiles, int num_sms) {
       a.splits = n;
     }
   }
-  const bool shared = per_sm == 2 && (a.splits > 1 || (tiles > num_sms && tiles <= 2 * num_sms));
+  const bool shared = per_sm == 2 && (a.splits > 1 || tiles > num_sms);
   const uint32_t room = (shared ? kHalfKb : 227) * 1024 - extra;
   a.stages = (int)std::min<uint32_t>(12, room / stage_bytes);
   // (with six and more, two at a time: a commit costs the issuing thread 100 cycles, a stage's MMAs 300, whatever the rows)
   a.pair = a.stages >= 6 ? 2 : 1;
   a.stages -= a.stages % a.pair;
-  const int64_t groups = a.splits > 1 || shared ? tiles : std::min<int64_t>(tiles, num_sms);
+  const int64_t groups = a.splits > 1 ? tiles : std::min<int64_t>(tiles, shared ? 2 * num_sms : num_sms);
   return Shape{(int)(groups * a.splits), extra + std::max<uint32_t>(stage_bytes * a.stages, a.splits > 1 ? (uint32_t)a.nt * kFeat * 4u : 0u)};
 }
 
-template <int kMode>
-int launch_main(const CUtensorMap& w_map, const CUtensorMap& x_map, const CUtensorMap& b_map, ProjectArgs a, const Shape& shape, cudaStream_t st) {
+template <int kMode, int kExact>
+int launch_kind(const CUtensorMap& w_map, const CUtensorMap& x_map, const CUtensorMap& b_map, ProjectArgs a, const Shape& shape, cudaStream_t st) {
   static bool done[kMaxDevices];
-  if (!ensure_dynamic_smem(k_project<kMode>, 227 * 1024, done)) return -1;
-  // one accumulator where a CTA, or each round of a cluster, has one tile
-  const bool single = (int64_t)a.feat_tiles * a.row_tiles <= shape.ctas / a.splits;
+  if (!ensure_dynamic_smem(k_project<kMode, kExact>, 227 * 1024, done)) return -1;
+  // accumulators: one where a CTA has one tile of one chunk, or tensor memory holds no more beside the sums; the sums behind them
+  const bool single = !kExact && (int64_t)a.feat_tiles * a.row_tiles <= shape.ctas / a.splits;
   uint32_t cols = 32;
   while (cols < (uint32_t)a.nt) cols *= 2;
-  a.acc_cols = single ? 0 : cols;
-  a.tmem_cols = single ? cols : 2 * cols;
+  a.accs = single || kExact == 8 ? 1 : 2;
+  a.acc_cols = cols;
+  a.sum_cols = a.accs * cols;
+  a.tmem_cols = a.accs * cols + (kExact ? cols : 0);
+  while (a.tmem_cols & (a.tmem_cols - 1)) a.tmem_cols += a.tmem_cols & -a.tmem_cols;  // (a power of two)
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)shape.ctas);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(kExact == 8 ? kWideThreads : kThreads);
   cfg.dynamicSmemBytes = shape.smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
@@ -784,7 +873,12 @@ int launch_main(const CUtensorMap& w_map, const CUtensorMap& x_map, const CUtens
   }
   cfg.attrs = attr;
   cfg.numAttrs = n;
-  return cudaLaunchKernelEx(&cfg, k_project<kMode>, w_map, x_map, b_map, a) == cudaSuccess ? 1 : -1;
+  return cudaLaunchKernelEx(&cfg, k_project<kMode, kExact>, w_map, x_map, b_map, a) == cudaSuccess ? 1 : -1;
+}
+template <int kMode>
+int launch_main(const CUtensorMap& w_map, const CUtensorMap& x_map, const CUtensorMap& b_map, const ProjectArgs& a, const Shape& shape, cudaStream_t st) {
+  if (!a.y_fp32) return launch_kind<kMode, 0>(w_map, x_map, b_map, a, shape, st);
+  return a.nt <= 128 ? launch_kind<kMode, 4>(w_map, x_map, b_map, a, shape, st) : launch_kind<kMode, 8>(w_map, x_map, b_map, a, shape, st);
 }
 
 // Rows of x that one pass takes: more go in several, one behind the other, so that the scratch stays bounded.
@@ -794,18 +888,18 @@ int tile_rows(int rows) { return rows >= 256 ? 256 : (rows + 15) / 16 * 16; }
 size_t align_to(size_t n, size_t a) { return (n + a - 1) / a * a; }
 
 // Where the slots of a pass stand in the scratch; its size.
-size_t place_slots(Slots* sl, char* scratch, int rows, int rank, int num_adapters) {
+size_t place_slots(Slots* sl, char* scratch, int rows, int rank, int num_adapters, int numbers) {
   const int nt = tile_rows(rows), tiles = (rows + nt - 1) / nt, most = std::min(nt, num_adapters);
   const int padded = rank <= 16 ? 16 : rank <= 32 ? 32 : 64;
   const size_t ids = align_to((size_t)tiles * 4, 128), of_row = ids + align_to((size_t)tiles * most * 4, 128), h = of_row + align_to((size_t)rows * 4, 128);
   const size_t block = (size_t)nt * padded * 2;
-  if (sl) *sl = Slots{(int32_t*)scratch, (int32_t*)(scratch + ids), (int32_t*)(scratch + of_row), nullptr, scratch + h, most, rank, padded, (uint32_t)block};
-  return h + (size_t)tiles * most * 2 * block;
+  if (sl) *sl = Slots{(int32_t*)scratch, (int32_t*)(scratch + ids), (int32_t*)(scratch + of_row), nullptr, scratch + h, most, numbers, rank, padded, (uint32_t)block};
+  return h + (size_t)tiles * most * numbers * block;
 }
 
 }  // namespace
 
-size_t project_scratch_bytes(int rows, int rank, int num_adapters) { return place_slots(nullptr, nullptr, std::min(rows, kPassRows), rank, num_adapters); }
+size_t project_scratch_bytes(int rows, int rank, int num_adapters) { return place_slots(nullptr, nullptr, std::min(rows, kPassRows), rank, num_adapters, 3); }
 
 static int launch_pass(const gf_projection_t& p, int rows, const void* x, int64_t x_stride, const int32_t* adapter, void* y, int64_t y_stride, int y_fp32,
                        void* scratch, int num_sms, int32_t* status, cudaStream_t st) {
@@ -828,7 +922,7 @@ static int launch_pass(const gf_projection_t& p, int rows, const void* x, int64_
     const Shape shape = shape_of(a, (int64_t)a.feat_tiles * a.row_tiles, num_sms);
     return launch_main<kPlain>(w_map, x_map, b_map, a, shape, st);
   }
-  place_slots(&a.slots, (char*)scratch, rows, p.rank, p.num_adapters);
+  place_slots(&a.slots, (char*)scratch, rows, p.rank, p.num_adapters, y_fp32 ? 3 : 2);
   a.slots.scale = p.scale_dev;
   if (!make_map(&b_map, p.b_dev, p.num_adapters, p.out_dim, p.rank, p.rank, a.slots.padded, kFeat)) return -1;
   const Shape main_shape = shape_of(a, (int64_t)a.feat_tiles * a.row_tiles, num_sms);
