@@ -3,7 +3,7 @@
 //
 // W x: tcgen05 MMAs with the output features as the MMA's rows (128 of W at a time, K-major) and up to 256 rows of x as its
 // columns, so that one row and thousands go the same way; both operands come by TMA in stages of 64 entries of K, the sums stay in
-// tensor memory in fp32.  Few rows leave few tiles: then a cluster of CTAs shares a tile, each with a part of K, and
+// tensor memory in fp32.  256 rows and more: two CTAs share a tile of 256 features (cta_group::2).  Few rows leave few tiles: then a cluster of CTAs shares a tile, each with a part of K, and
 // joins its parts through shared memory in a fixed order.
 //
 // The adapters are more entries of K.  For every adapter that rows of a tile of x name (a slot of the tile), h = scale_a A_a x is a
@@ -11,7 +11,7 @@
 // slots, in the same pipeline, and nothing is left for the warps that take them out of tensor memory.  h is held in two bf16
 // numbers, its nearest and the nearest of what is left (off by 2^-17 of it), and multiplied twice; for results in fp32 in three (2^-25).
 // A x goes the same way as W x: the rows of the A of 8, 4 or 2 slots (of rank 16, 32, 64) stand in W's place, for all rows of the tile, and
-// what comes out is kept where row and slot belong together and written as those operands, in the layout of shared memory.
+// what comes out is kept where row and slot belong together and written as those operands.
 // Three launches: the slots, A x, W x; only the copies behind a tile's last entry of W wait for the second.  (Few rows: the first two are
 // one, k_adapter_rows.)
 //
@@ -19,7 +19,7 @@
 // 256), so every 8 stages they are taken out and added, rounded, to sums that stand beside them; 5e-7 is left.  (Those sums in registers spilled.)
 //
 // (The same sums on the CUDA cores, while the MMAs ran, took 568 us for 8192 rows with adapters of rank 16 and 1143 of rank 64,
-// where W x alone takes 295: their reads of B and h wait behind the copies' traffic.)
+// where W x alone took 295: their reads of B and h wait behind the copies' traffic.)
 #include <cuda.h>
 
 #include <algorithm>
@@ -34,6 +34,8 @@ constexpr int kStep = 64;         // entries of K in a stage
 constexpr int kThreads = 256;
 constexpr int kWideThreads = 384; // with eight warps that take the sums out
 constexpr int kChunk = 8;         // fp32 results: stages after which the sums are taken out
+constexpr int kPanel = 8;         // tiles of x that the tiles of W go over together, so that those at work at once read few rows of either:
+                                  // 8192 rows of 4096 -> 28672 take 1530 us with 1, 1230 with 8
 constexpr int kGroup = 8;         // rows of x that are taken out of tensor memory together
 
 // The slots of the tiles of x, in the caller's scratch.
@@ -42,7 +44,7 @@ struct Slots {
   int32_t* adapter;      // [row_tiles][most]
   int32_t* of_row;       // [rows] a row's slot in its tile, -1: none
   const float* scale;    // [num_adapters] or null
-  char* h;               // [row_tiles][most][numbers][nt][padded rank], swizzled like a stage's operand
+  char* h;               // [row_tiles][most][numbers][nt][padded rank], read by TMA like the others
   int most;
   int numbers;           // that h is held in: 2 or 3
   int rank, padded;      // padded: 16, 32 or 64
@@ -52,7 +54,8 @@ struct Slots {
 struct ProjectArgs {
   int rows, in_dim, out_dim, nt;        // nt: rows of x in a tile
   int feat_tiles, row_tiles, stages;
-  int pair;                             // stages that are given back together: 1 or 2
+  int pair;                             // stages that share their barriers: 1 or 2
+  int two;                              // two CTAs a tile
   int splits;                           // CTAs that share a tile
   uint32_t tmem_cols, acc_cols;         // allocated; from one accumulator to the next
   int accs;                             // accumulators: 1 or 2
@@ -64,10 +67,68 @@ struct ProjectArgs {
   int32_t* status;
 };
 
-__device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, int x, int y, uint64_t* bar) {
-  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(smem_u32(dst)),
-               "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar))
-               : "memory");
+// kTwo: the CTA is one of two that work on one tile with MMAs of both (cta_group::2), the even one, which issues them, the leader.  Each brings
+// its own half of either operand; all of a stage's bytes count on the leader's barrier, whose address in the cluster `bar` is.
+template <bool kTwo>
+__device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  if constexpr (kTwo)
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(smem_u32(dst)),
+                 "l"(map), "r"(x), "r"(y), "r"(bar)
+                 : "memory");
+  else
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(smem_u32(dst)),
+                 "l"(map), "r"(x), "r"(y), "r"(bar)
+                 : "memory");
+}
+template <bool kTwo>
+__device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  if constexpr (kTwo)
+    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(smem_u32(dst)),
+                 "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+                 : "memory");
+  else
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(smem_u32(dst)),
+                 "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+                 : "memory");
+}
+// The address in the cluster of CTA `rank`'s copy of what is at p here.
+__device__ __forceinline__ uint32_t at_rank(const void* p, int rank) {
+  uint32_t a;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
+  return a;
+}
+// An arrival at another CTA's barrier; what this thread has done is seen there (kRelease), or it has done nothing that is to be.  (A thread with
+// copies on the way waits for long in a release: 1500 cycles a stage.)
+template <bool kRelease>
+__device__ __forceinline__ void arrive_at(uint32_t bar) {
+  if constexpr (kRelease) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+  else asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+template <bool kTwo>
+__device__ __forceinline__ void tmem_take(uint32_t* dst_smem, uint32_t ncols) {
+  if constexpr (kTwo) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(dst_smem)), "r"(ncols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  } else {
+    tmem_alloc(dst_smem, ncols);
+  }
+}
+template <bool kTwo>
+__device__ __forceinline__ void tmem_give(uint32_t taddr, uint32_t ncols) {
+  if constexpr (kTwo) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
+  else tmem_dealloc(taddr, ncols);
+}
+// The barrier gets one arrival when all MMAs issued so far have ended; or that of both CTAs (mask: theirs in the cluster) does.
+template <bool kTwo>
+__device__ __forceinline__ void commit(uint64_t* bar) {
+  if constexpr (kTwo) asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+  else tc_commit(bar);
+}
+template <bool kTwo>
+__device__ __forceinline__ void commit_both(uint64_t* bar, uint16_t mask) {
+  if constexpr (kTwo)
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)), "h"(mask) : "memory");
+  else tc_commit(bar);
 }
 
 __device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
@@ -77,40 +138,38 @@ __device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
                : "memory");
 }
 
-__device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
-  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(smem_u32(dst)),
-               "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
-               : "memory");
-}
-
 // Shared-memory matrix descriptor of a K-major operand whose rows are `row_bytes` (32, 64 or 128) long and swizzled over that many.
 __device__ __forceinline__ uint64_t operand_desc(uint32_t saddr, int row_bytes) {
   const uint64_t kind = row_bytes == 128 ? 2 : row_bytes == 64 ? 4 : 6;
   return (tc_smem_desc(saddr, 0, 8 * row_bytes) & ~((uint64_t)7 << 61)) | kind << 61;
 }
-// Where the 16-byte piece c of row r of such an operand is.
-__device__ __forceinline__ uint32_t operand_at(int r, int c, int row_bytes) {
-  const int x = row_bytes == 128 ? r & 7 : row_bytes == 64 ? (r >> 1) & 3 : (r >> 2) & 1;
-  return (uint32_t)(r * row_bytes + ((c ^ x) << 4));
-}
-
 __device__ __forceinline__ uint64_t bf16x2_to_f2(uint32_t v) { return f2_pack(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)); }
 
 // Four MMAs along a stage's 64 entries of K, 32 bytes apart in both operands.  (In one block: the issuing thread is alone on its
 // scheduler, and with few rows of x its instructions between the MMAs are what takes the time.)
-__device__ __forceinline__ void umma_ss4(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p, t;\n\t.reg .b64 a, b;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\tsetp.eq.b32 t, 0, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t"
-      "add.s64 a, %1, 2;\n\tadd.s64 b, %2, 2;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n\t"
-      "add.s64 a, %1, 4;\n\tadd.s64 b, %2, 4;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n\t"
-      "add.s64 a, %1, 6;\n\tadd.s64 b, %2, 6;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n\t}" ::"r"(d_tmem),
-      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
-      : "memory");
+#define GF_MMA4(GROUP)                                                           \
+  "{\n\t.reg .pred p, t;\n\t.reg .b64 a, b;\n\t"                                \
+  "setp.ne.b32 p, %4, 0;\n\tsetp.eq.b32 t, 0, 0;\n\t"                           \
+  "tcgen05.mma.cta_group::" GROUP ".kind::f16 [%0], %1, %2, %3, p;\n\t"         \
+  "add.s64 a, %1, 2;\n\tadd.s64 b, %2, 2;\n\t"                                  \
+  "tcgen05.mma.cta_group::" GROUP ".kind::f16 [%0], a, b, %3, t;\n\t"           \
+  "add.s64 a, %1, 4;\n\tadd.s64 b, %2, 4;\n\t"                                  \
+  "tcgen05.mma.cta_group::" GROUP ".kind::f16 [%0], a, b, %3, t;\n\t"           \
+  "add.s64 a, %1, 6;\n\tadd.s64 b, %2, 6;\n\t"                                  \
+  "tcgen05.mma.cta_group::" GROUP ".kind::f16 [%0], a, b, %3, t;\n\t}"
+template <bool kTwo>
+__device__ __forceinline__ void mma4(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  if constexpr (kTwo) asm volatile(GF_MMA4("2")::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+  else asm volatile(GF_MMA4("1")::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+#undef GF_MMA4
+template <bool kTwo>
+__device__ __forceinline__ void mma1(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  if constexpr (kTwo)
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem), "l"(a_desc),
+                 "l"(b_desc), "r"(idesc), "r"(accumulate)
+                 : "memory");
+  else umma_ss(d_tmem, a_desc, b_desc, idesc, accumulate);
 }
 
 __device__ __forceinline__ void store_y(const ProjectArgs& a, int row, int feat, float v) {
@@ -167,7 +226,7 @@ __device__ __forceinline__ __nv_bfloat16 take_number(float& v) {
 __device__ __forceinline__ void store_h(const Slots& sl, const HPlace& p, int row_in_tile, int row_slot, float v) {
   if (p.at == nullptr) return;
   v = row_slot == p.slot && p.r < sl.rank ? v * p.scale : 0.f;
-  char* at = p.at + operand_at(row_in_tile, p.r >> 3, sl.padded * 2) + (p.r & 7) * 2;
+  char* at = p.at + (row_in_tile * sl.padded + p.r) * 2;
   for (int i = 0; i < sl.numbers; ++i) *reinterpret_cast<__nv_bfloat16*>(at + i * sl.block) = take_number(v);
 }
 __device__ __forceinline__ void store_h4(const Slots& sl, const HPlace& p, int row_in_tile, int row_slot, float4 v) {
@@ -177,7 +236,7 @@ __device__ __forceinline__ void store_h4(const Slots& sl, const HPlace& p, int r
   v.y = mine ? v.y * p.scale : 0.f;
   v.z = mine ? v.z * p.scale : 0.f;
   v.w = mine ? v.w * p.scale : 0.f;
-  char* at = p.at + operand_at(row_in_tile, p.r >> 3, sl.padded * 2) + (p.r & 7) * 2;
+  char* at = p.at + (row_in_tile * sl.padded + p.r) * 2;
   for (int i = 0; i < sl.numbers; ++i) {
     __align__(8) __nv_bfloat16 n[4] = {take_number(v.x), take_number(v.y), take_number(v.z), take_number(v.w)};
     *reinterpret_cast<uint2*>(at + i * sl.block) = *reinterpret_cast<uint2*>(n);
@@ -190,13 +249,17 @@ __device__ __forceinline__ void store_h4(const Slots& sl, const HPlace& p, int r
 // Warp 0 issues the copies, warp 1 the MMAs, warps 4 to 7 take the sums out; the parts of a cluster are joined by all.
 // kExact: results in fp32, whose sums are taken out by so many warps: 4, or 8 for the tiles of 256 rows, for which tensor memory holds no second
 // accumulator to go on in meanwhile.  0: results in bf16.
-template <int kMode, int kExact>
-__global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact == 8 ? 1 : 2) k_project(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map,
-                                                         const __grid_constant__ CUtensorMap b_map, const __grid_constant__ ProjectArgs a) {
-  constexpr int kWarps = (kExact == 8 ? kWideThreads : kThreads) / 32, kTakers = kWarps - 4;
+// kTwo: two CTAs, neighbours in a cluster, share a tile of 256 features and 256 rows of x.  Each has 128 of the features, so its own accumulator, but
+// brings only 128 of the rows: what the MMAs read of a stage comes from both, 32 KB a CTA and stage in place of 48, so that there are six stages on
+// the way in place of four.  8192 rows of 4096 -> 6144: 277 us, one CTA a tile 319; of 4096 -> 28672: 1192 (1614 TFLOP/s) and 1432.
+template <int kMode, int kExact, bool kTwo>
+__global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact == 8 ? 1 : 2) k_project(
+    const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap b_map,
+    const __grid_constant__ CUtensorMap h_map, const __grid_constant__ ProjectArgs a) {
+  constexpr int kWarps = (kExact == 8 ? kWideThreads : kThreads) / 32, kTakers = kWarps - 4, kCtas = kTwo ? 2 : 1, kTileFeat = kFeat * kCtas;
   extern __shared__ __align__(1024) char smem_raw[];
   char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  const uint32_t w_bytes = kFeat * 128u, x_bytes = (uint32_t)a.nt * 128u, stage_bytes = w_bytes + x_bytes;
+  const uint32_t w_bytes = kFeat * 128u, x_bytes = (uint32_t)a.nt / kCtas * 128u, stage_bytes = w_bytes + x_bytes;
   const uint32_t ring = max(stage_bytes * a.stages, a.splits > 1 ? (uint32_t)a.nt * kFeat * 4u : 0u);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + ring);
   uint64_t* empty = full + a.stages;
@@ -205,13 +268,16 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
   uint64_t* drained = acc_empty + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drained + 1);
   const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31;
-  const int group = blockIdx.x / a.splits, groups = gridDim.x / a.splits, part = blockIdx.x - group * a.splits;
+  const int size = a.splits * kCtas;  // of a cluster
+  const int group = blockIdx.x / size, groups = gridDim.x / size, rank = blockIdx.x - group * size, part = rank / kCtas, half = rank - part * kCtas;
+  const bool leader = half == 0;
+  const uint16_t both = (uint16_t)(3u << (part * kCtas));
   const int tiles = a.feat_tiles * a.row_tiles;
   const int steps_all = (a.in_dim + kStep - 1) / kStep;
   const int step0 = (int)((int64_t)steps_all * part / a.splits), step1 = (int)((int64_t)steps_all * (part + 1) / a.splits);
   const Slots& sl = a.slots;
   const int h_row = sl.padded * 2;                       // bytes of a row of h, and of B's
-  const uint32_t b_bytes = kFeat * (uint32_t)h_row;
+  const uint32_t b_bytes = kFeat * (uint32_t)h_row, h_bytes = sl.block / kCtas;  // of a slot's B, of a number of its h
   const int per_tile = kMode == kDown ? kFeat / sl.padded : 1;  // slots whose A a tile takes
   auto slots_of = [&](int row_tile) { return *(volatile int32_t*)(sl.count + row_tile); };
   // The tiles of a CTA or cluster: features f of W (or slots, from f * per_tile on) and rows r of x.  Those of A x are only as many as there
@@ -227,8 +293,9 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
         t.slots = t.r < a.row_tiles ? slots_of(t.r) : 0;
       }
     } else {
-      t.r = t.index / a.feat_tiles;
-      t.f = t.index - t.r * a.feat_tiles;
+      const int panel = t.index / (a.feat_tiles * kPanel), i = t.index - panel * a.feat_tiles * kPanel, n = min(kPanel, a.row_tiles - panel * kPanel);
+      t.f = i / n;
+      t.r = panel * kPanel + i - t.f * n;
     }
   };
   auto start = [&] {
@@ -243,14 +310,15 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
     settle(t);
   };
   if (tid == 0) {
-    for (int i = 0; i < a.stages; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(acc_full + i, 1); mbar_init(acc_empty + i, kTakers); }
+    for (int i = 0; i < a.stages; ++i) { mbar_init(full + i, a.pair); mbar_init(empty + i, 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(acc_full + i, 1); mbar_init(acc_empty + i, kTakers * kCtas); }
     mbar_init(drained, 1);
     mbar_fence_init();
   }
-  if (wid == 1) tmem_alloc(tmem_slot, a.tmem_cols);
+  if (wid == 1) tmem_take<kTwo>(tmem_slot, a.tmem_cols);
   tc_fence_before_sync();
   __syncthreads();
+  if (kTwo) cluster_sync_all();  // (the other one's barriers are there)
   tc_fence_after_sync();
   const uint32_t tmem = *tmem_slot;
   if (kMode == kDown) {
@@ -266,12 +334,17 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
   const int a_slot = h_row == 128 ? kNumbers : h_row == 64 ? (kNumbers + 1) / 2 : 1;
   auto slot_stages = [&](int n) { return two_slots ? (n + 1) / 2 : n * a_slot; };
 
+  const int odd = a.pair - 1;  // (a stage's barriers are those at s >> odd)
   int s = 0;           // the role's stage and its phase
   uint32_t phase = 0;
   uint32_t used = 0, phases = 0;  // stages that copies have been issued for, and the last phase of each
   int done = 0;                   // accumulators: tiles, or their chunks
   auto acc_at = [&] { return a.accs == 2 ? done & 1 : 0; };
   auto acc_phase = [&] { return (uint32_t)(a.accs == 2 ? done >> 1 : done) & 1u; };
+  auto give_acc = [&] {  // to the thread that issues the MMAs
+    if (kTwo) arrive_at<true>(at_rank(acc_empty + acc_at(), part * kCtas));
+    else mbar_arrive(acc_empty + acc_at());
+  };
   bool ok = true, waited = kMode != kWith;
   // a warp that takes sums out: row m of the tile of W, columns col0 .. col0 + cols (rows of x)
   const int m = (wid & 3) * 32 + lane, cols = kTakers == 8 ? a.nt / 2 : a.nt, col0 = kTakers == 8 && wid >= 8 ? cols : 0;
@@ -281,14 +354,22 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
   while (more(now)) {
     if (wid == 0) {
       if (lane == 0) {
-        auto free = [&] { return s % a.pair != 0 || mbar_wait(empty + s / a.pair, phase ^ 1u, a.status); };
+        // (the leader passes on to the other CTA what it has waited for)
+        auto free = [&] {
+          if ((s & odd) != 0) return true;
+          if (!mbar_wait(empty + (s >> odd), phase ^ 1u, a.status)) return false;
+          if (kTwo && leader && (used >> s & 1u)) arrive_at<false>(at_rank(empty + (s >> odd), part * kCtas + 1));
+          return true;
+        };
         auto next = [&] {
           used |= 1u << s;
           phases = (phases & ~(1u << s)) | phase << s;
           if (++s == a.stages) { s = 0; phase ^= 1u; }
         };
+        auto full_at = [&] { return kTwo ? at_rank(full + (s >> odd), part * kCtas) : smem_u32(full + (s >> odd)); };
+        auto expect = [&](uint32_t bytes) { if (leader) mbar_arrive_expect_tx(full + (s >> odd), bytes * kCtas); };
         for (Tile t = now; more(t) && ok; advance(t)) {
-          const int f = t.f, f0 = f * kFeat, row_tile = t.r, t0 = row_tile * a.nt;
+          const int f = t.f, f0 = f * kTileFeat + half * kFeat, row_tile = t.r, t0 = row_tile * a.nt, mine0 = t0 + half * (a.nt / kCtas);
           const int32_t* which = sl.adapter + (int64_t)row_tile * sl.most;
           int s0 = 0, s1 = 0, ids[8];
           if (kMode == kWith && waited) s1 = slots_of(row_tile);  // (asked for here, used behind the loop)
@@ -300,16 +381,17 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
           for (int k = step0; k < step1; ++k) {
             if (!(ok = free())) break;
             char* at = smem + s * stage_bytes;
+            const uint32_t bar = full_at();
             if (kMode == kDown) {
-              mbar_arrive_expect_tx(full + s, s1 * sl.rank * 128u + x_bytes);
+              expect(s1 * sl.rank * 128u + x_bytes);
 #pragma unroll
               for (int j = 0; j < 8; ++j)
-                if (j < s1) tma_load_2d(at + j * sl.padded * 128, &w_map, k * kStep, ids[j] * sl.rank, full + s);
+                if (j < s1) tma_load_2d<kTwo>(at + j * sl.padded * 128, &w_map, k * kStep, ids[j] * sl.rank, bar);
             } else {
-              mbar_arrive_expect_tx(full + s, stage_bytes);
-              tma_load_2d(at, &w_map, k * kStep, f0, full + s);
+              expect(stage_bytes);
+              tma_load_2d<kTwo>(at, &w_map, k * kStep, f0, bar);
             }
-            tma_load_2d(at + w_bytes, &x_map, k * kStep, t0, full + s);
+            tma_load_2d<kTwo>(at + w_bytes, &x_map, k * kStep, mine0, bar);
             next();
           }
           if (kMode == kWith && ok) {
@@ -321,57 +403,54 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
             s0 = s1 * part / a.splits;
             s1 = s1 * (part + 1) / a.splits;
             int ahead[2] = {s0 < s1 ? __ldcg(which + s0) : 0, s0 + 1 < s1 ? __ldcg(which + s0 + 1) : 0};  // of the next two slots
-            const uint64_t slot_bytes = (uint64_t)kNumbers * sl.block;
-            const char* h = sl.h + ((int64_t)row_tile * sl.most + s0) * slot_bytes;
-            for (int i = s0; i < s1 && ok; h += slot_bytes) {
+            int y = (row_tile * sl.most + s0) * kNumbers * a.nt + half * (a.nt / kCtas);  // of the next number of h
+            for (int i = s0; i < s1 && ok;) {
               const int id = ahead[0], id2 = ahead[1], taken = two_slots && i + 1 < s1 ? 2 : 1;
               i += taken;
               ahead[0] = taken == 2 ? (i < s1 ? __ldcg(which + i) : 0) : id2;
               ahead[1] = i + 1 < s1 ? __ldcg(which + i + 1) : 0;
-              if (two_slots) {
+              for (int j = 0; j < taken * kNumbers;) {
                 if (!(ok = free())) break;
                 char* at = smem + s * stage_bytes;
-                mbar_arrive_expect_tx(full + s, taken * (b_bytes + 2 * sl.block));
-                tma_load_3d(at, &b_map, 0, f0, id, full + s);
-                if (taken == 2) tma_load_3d(at + b_bytes, &b_map, 0, f0, id2, full + s);
-                bulk_g2s(at + w_bytes, h, taken * 2 * sl.block, full + s);
-                h += (taken - 1) * slot_bytes;
+                const uint32_t bar = full_at();
+                const int n = two_slots ? taken * kNumbers : min(per_stage, kNumbers - j);
+                expect(taken * b_bytes + n * h_bytes);
+                tma_load_3d<kTwo>(at, &b_map, 0, f0, id, bar);
+                if (taken == 2) tma_load_3d<kTwo>(at + b_bytes, &b_map, 0, f0, id2, bar);
+                for (int q = 0; q < n; ++q, y += a.nt) tma_load_2d<kTwo>(at + w_bytes + q * h_bytes, &h_map, 0, y, bar);
+                j += n;
                 next();
-              } else {
-                for (int j = 0; j < kNumbers; j += per_stage) {
-                  if (!(ok = free())) break;
-                  char* at = smem + s * stage_bytes;
-                  const uint32_t bytes = min(per_stage, kNumbers - j) * sl.block;
-                  mbar_arrive_expect_tx(full + s, b_bytes + bytes);
-                  tma_load_3d(at, &b_map, 0, f0, id, full + s);
-                  bulk_g2s(at + w_bytes, h + j * (int64_t)sl.block, bytes, full + s);
-                  next();
-                }
               }
             }
           }
-          if (ok && s % a.pair != 0) {  // the next tile's begin with a pair: the other one of this passes empty
-            mbar_arrive(full + s);
+          if (ok && (s & odd) != 0) {  // the next tile's begin with a pair: the other one of this passes empty
+            if (leader) mbar_arrive(full + (s >> odd));
             next();
           }
           if (a.splits > 1) break;
         }
         // nothing of its own is on the way when it leaves, also where it gave up
-        for (int i = 0; i < a.stages; ++i)
-          if (used >> i & 1u) mbar_drain(full + i, phases >> i & 1u, a.status);
+        for (int i = 0; i < a.stages && leader; i += a.pair)
+          if (used >> i & 1u) mbar_drain(full + (i >> odd), phases >> i & 1u, a.status);
       }
     } else if (wid == 1) {
-      if (lane == 0) {
-        const uint32_t idesc = tc_idesc_bf16(kFeat, a.nt, false);
+      if (lane == 0 && leader) {
+        const uint32_t idesc = tc_idesc_bf16(kTileFeat, a.nt, false);
         const uint64_t first_desc = tc_smem_desc(smem_u32(smem), 0, 1024);  // (its address is the low field, which the ring does not overrun)
-        bool ready = false;  // the stage has been seen to be full
-        auto filled = [&] { return ready || mbar_wait(full + s, phase, a.status); };
+        bool ready = false;  // the next pair has been seen to be full
+        auto filled = [&] {
+          if ((s & odd) != 0) return true;
+          const bool there = ready || mbar_wait(full + (s >> odd), phase, a.status);
+          tc_fence_after_sync();
+          return there;
+        };
         auto peek = [&] {    // (before a stage's MMAs, so that the answer is there behind them)
+          if ((s & odd) != odd) return;
           const bool wraps = s + 1 == a.stages;
-          ready = mbar_try_wait(full + (wraps ? 0 : s + 1), wraps ? phase ^ 1u : phase);
+          ready = mbar_try_wait(full + (wraps ? 0 : (s + 1) >> odd), wraps ? phase ^ 1u : phase);
         };
         auto next = [&] {
-          if ((s + 1) % a.pair == 0) tc_commit(empty + s / a.pair);
+          if ((s & odd) == odd) commit<kTwo>(empty + (s >> odd));
           if (++s == a.stages) { s = 0; phase ^= 1u; }
         };
         for (Tile t = now; more(t) && ok; advance(t)) {
@@ -389,7 +468,7 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
           };
           auto chunk = [&] {  // the next stage's accumulator
             if (kExact && in_acc == kChunk) {
-              tc_commit(acc_full + acc_at());
+              commit_both<kTwo>(acc_full + acc_at(), both);
               ++done;
               if (!open()) return false;
             }
@@ -397,12 +476,27 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
             return true;
           };
           if (!(ok = open())) break;
-          for (int k = step0; k < step1; ++k) {
+          int k = step0;
+          if (a.pair == 2) {  // in few instructions
+            const uint32_t stage_desc = stage_bytes >> 4, x_desc = w_bytes >> 4;
+            for (; k + 2 <= step1; k += 2) {
+              if (!(ok = filled() && chunk())) break;
+              ++in_acc;
+              const uint64_t wd = first_desc + (uint32_t)s * stage_desc;
+              mma4<kTwo>(d, wd, wd + x_desc, idesc, in_acc > 2);
+              const bool wraps = s + 2 == a.stages;
+              ready = mbar_try_wait(full + (wraps ? 0 : (s >> 1) + 1), wraps ? phase ^ 1u : phase);
+              mma4<kTwo>(d, wd + stage_desc, wd + (stage_desc + x_desc), idesc, 1);
+              commit<kTwo>(empty + (s >> 1));
+              s = wraps ? 0 : s + 2;
+              phase ^= wraps;
+            }
+          }
+          for (; k < step1 && ok; ++k) {
             if (!(ok = filled() && chunk())) break;
-            tc_fence_after_sync();
             const uint64_t wd = first_desc + (uint64_t)((uint32_t)s * stage_bytes >> 4);
             peek();
-            umma_ss4(d, wd, wd + (w_bytes >> 4), idesc, in_acc > 1);
+            mma4<kTwo>(d, wd, wd + (w_bytes >> 4), idesc, in_acc > 1);
             next();
           }
           if (kMode == kWith && ok) {
@@ -416,49 +510,48 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
             const int stages = slot_stages(s1 - s0);
             for (int i = 0; i < stages; ++i) {
               if (!(ok = filled() && chunk())) break;
-              tc_fence_after_sync();
               const uint32_t at = smem_u32(smem + s * stage_bytes), ht = at + w_bytes;
               peek();
               // the numbers of h in this stage, each with its slot's B
               const uint32_t on = in_acc > 1;
               if (h_row == 128) {
-                umma_ss4(d, operand_desc(at, 128), operand_desc(ht, 128), idesc, on);
+                mma4<kTwo>(d, operand_desc(at, 128), operand_desc(ht, 128), idesc, on);
               } else if (h_row == 64) {
-                const uint64_t bd = operand_desc(at, 64), hd = operand_desc(ht, 64), hd2 = operand_desc(ht + sl.block, 64);
-                umma_ss(d, bd, hd, idesc, on);
-                umma_ss(d, bd + 2, hd + 2, idesc, 1);
+                const uint64_t bd = operand_desc(at, 64), hd = operand_desc(ht, 64), hd2 = operand_desc(ht + h_bytes, 64);
+                mma1<kTwo>(d, bd, hd, idesc, on);
+                mma1<kTwo>(d, bd + 2, hd + 2, idesc, 1);
                 if (kNumbers == 2 || (i & 1) == 0) {
-                  umma_ss(d, bd, hd2, idesc, 1);
-                  umma_ss(d, bd + 2, hd2 + 2, idesc, 1);
+                  mma1<kTwo>(d, bd, hd2, idesc, 1);
+                  mma1<kTwo>(d, bd + 2, hd2 + 2, idesc, 1);
                 }
               } else if (kNumbers == 2) {
                 const uint64_t bd = operand_desc(at, 32), bd2 = operand_desc(at + b_bytes, 32), hd = operand_desc(ht, 32);
-                const uint64_t next_h = sl.block >> 4;
-                umma_ss(d, bd, hd, idesc, on);
-                umma_ss(d, bd, hd + next_h, idesc, 1);
+                const uint64_t next_h = h_bytes >> 4;
+                mma1<kTwo>(d, bd, hd, idesc, on);
+                mma1<kTwo>(d, bd, hd + next_h, idesc, 1);
                 if (s0 + 2 * i + 1 < s1) {
-                  umma_ss(d, bd2, hd + 2 * next_h, idesc, 1);
-                  umma_ss(d, bd2, hd + 3 * next_h, idesc, 1);
+                  mma1<kTwo>(d, bd2, hd + 2 * next_h, idesc, 1);
+                  mma1<kTwo>(d, bd2, hd + 3 * next_h, idesc, 1);
                 }
               } else {
                 const uint64_t bd = operand_desc(at, 32), hd = operand_desc(ht, 32);
 #pragma unroll
-                for (int j = 0; j < kNumbers; ++j) umma_ss(d, bd, hd + j * (sl.block >> 4), idesc, on || j > 0);
+                for (int j = 0; j < kNumbers; ++j) mma1<kTwo>(d, bd, hd + j * (h_bytes >> 4), idesc, on || j > 0);
               }
               next();
             }
           }
-          if (s % a.pair != 0) {
-            tc_commit(empty + s / a.pair);
+          if ((s & odd) != 0) {
+            commit<kTwo>(empty + (s >> odd));
             if (++s == a.stages) { s = 0; phase ^= 1u; }
             ready = false;
           }
-          tc_commit(acc_full + acc_at());
+          commit_both<kTwo>(acc_full + acc_at(), both);
           ++done;
           if (a.splits > 1) break;
         }
         if (!ok) {  // (otherwise the tiles' own waits have seen the last of them)
-          tc_commit(drained);
+          commit<kTwo>(drained);
           mbar_drain(drained, 0, a.status);
         }
       }
@@ -477,7 +570,7 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
         auto sums_taken = [&] {
           tc_fence_before_sync();
           __syncwarp();
-          if (lane == 0) mbar_arrive(acc_empty + acc_at());
+          if (lane == 0) give_acc();
           ++done;
         };
         uint32_t from = lanes + acc_at() * a.acc_cols + col0;
@@ -523,7 +616,7 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
           const HPlace place(sl, row_tile, f * per_tile, t.slots, m);
           take([&](int r, float v) { if (t0 + r < a.rows) store_h(sl, place, r, __ldcg(sl.of_row + t0 + r), v); });
         } else {
-          take([&](int r, float v) { store_y(a, t0 + r, f * kFeat + m, v); });
+          take([&](int r, float v) { store_y(a, t0 + r, f * kTileFeat + half * kFeat + m, v); });
         }
       }
     }
@@ -547,7 +640,7 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
         if (!kExact) {
           tc_fence_before_sync();
           __syncwarp();
-          if (lane == 0) mbar_arrive(acc_empty + acc_at());
+          if (lane == 0) give_acc();
           ++done;
         }
       }
@@ -568,8 +661,7 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
 #pragma unroll
           for (int p = 0; p < kParts; ++p) {
             if (p0 + p < a.splits) {
-              uint32_t from;
-              asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(from) : "r"(smem_u32(parts + lane * 4)), "r"(p0 + p));
+              const uint32_t from = at_rank(parts + lane * 4, (p0 + p) * kCtas + half);
 #pragma unroll
               for (int i = 0; i < kRows; ++i)
                 asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];"
@@ -590,7 +682,7 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
           const int r = r0 + i * apart;
           if (r < n) {
             if (kMode == kDown) store_h4(sl, place, r, row_slot[i], sum[i]);
-            else store_y4(a, t0 + r, f * kFeat + lane * 4, sum[i]);
+            else store_y4(a, t0 + r, f * kTileFeat + half * kFeat + lane * 4, sum[i]);
           }
         }
       }
@@ -603,8 +695,9 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
   }
   tc_fence_before_sync();
   __syncthreads();
+  if (kTwo) cluster_sync_all();  // (neither leaves while the other's MMAs or arrivals may still come)
   tc_fence_after_sync();
-  if (wid == 1) tmem_dealloc(tmem, a.tmem_cols);
+  if (wid == 1) tmem_give<kTwo>(tmem, a.tmem_cols);
 }
 
 // The slots of a tile of x: the adapters that its rows name, ascending; one bit an adapter in shared memory, so that an adapter's slot is
@@ -741,7 +834,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_adapter_rows(const __nv_bflo
       __align__(16) __nv_bfloat16 p[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) p[j] = take_number(v[j]);
-      *reinterpret_cast<uint4*>(base + (int64_t)(sl.numbers * at + n) * sl.block + operand_at(t - t0, (r0 >> 3) + c, sl.padded * 2)) = *reinterpret_cast<uint4*>(p);
+      *reinterpret_cast<uint4*>(base + (int64_t)(sl.numbers * at + n) * sl.block + ((t - t0) * sl.padded + r0 + c * 8) * 2) = *reinterpret_cast<uint4*>(p);
     }
   }
 }
@@ -817,15 +910,16 @@ struct Shape {
   size_t smem;
 };
 Shape shape_of(ProjectArgs& a, int64_t tiles, int num_sms) {
-  const int steps = (a.in_dim + kStep - 1) / kStep;
-  const uint32_t stage_bytes = kFeat * 128u + a.nt * 128u, extra = 1024 + 512;
+  const int steps = (a.in_dim + kStep - 1) / kStep, ctas = a.two ? 2 : 1;
+  const uint32_t stage_bytes = kFeat * 128u + a.nt / ctas * 128u, extra = 1024 + 512;
   // (and only where tensor memory has room for two: CTAs of clusters that wait for each other must never wait for that)
   const int per_sm = 4 * stage_bytes + extra <= kHalfKb * 1024 && a.nt <= (a.y_fp32 ? 64 : 128) ? 2 : 1;
+  const int room_for = num_sms / ctas;  // tiles at once
   a.splits = 1;
-  int64_t best = (tiles + num_sms - 1) / num_sms * steps;
-  for (int n = 2; n <= 8 && tiles * n <= (int64_t)per_sm * num_sms && steps >= 4 * n; ++n) {
-    const int64_t most = (tiles * n + num_sms - 1) / num_sms * ((steps + n - 1) / n);
-    if (most < best - best / 16 && tiles <= clusters_at_once(n, per_sm == 2, num_sms)) {
+  int64_t best = (tiles + room_for - 1) / room_for * steps;
+  for (int n = 2; n * ctas <= 8 && tiles * n <= (int64_t)per_sm * room_for && steps >= 4 * n; ++n) {
+    const int64_t most = (tiles * n + room_for - 1) / room_for * ((steps + n - 1) / n);
+    if (most < best - best / 16 && tiles <= clusters_at_once(n * ctas, per_sm == 2, num_sms)) {
       best = most;
       a.splits = n;
     }
@@ -833,19 +927,22 @@ Shape shape_of(ProjectArgs& a, int64_t tiles, int num_sms) {
   const bool shared = per_sm == 2 && (a.splits > 1 || tiles > num_sms);
   const uint32_t room = (shared ? kHalfKb : 227) * 1024 - extra;
   a.stages = (int)std::min<uint32_t>(12, room / stage_bytes);
-  // (with six and more, two at a time: a commit costs the issuing thread 100 cycles, a stage's MMAs 300, whatever the rows)
+  // With six and more, two share their barriers: the issuing thread is what bounds the kernel, and a commit costs it 100 cycles and a wait 65 where a
+  // stage's MMAs cost 280.  (8192 rows: 332 us with a wait for each, 280 with a wait for two; 1 row 14.4 and 11.5.  Four stages in pairs leave too
+  // few on the way: 707 us became 868 for 14336 -> 4096 where a CTA works by itself.)
   a.pair = a.stages >= 6 ? 2 : 1;
   a.stages -= a.stages % a.pair;
-  const int64_t groups = a.splits > 1 ? tiles : std::min<int64_t>(tiles, shared ? 2 * num_sms : num_sms);
-  return Shape{(int)(groups * a.splits), extra + std::max<uint32_t>(stage_bytes * a.stages, a.splits > 1 ? (uint32_t)a.nt * kFeat * 4u : 0u)};
+  const int64_t groups = a.splits > 1 ? tiles : std::min<int64_t>(tiles, shared ? 2 * room_for : room_for);
+  return Shape{(int)(groups * a.splits * ctas), extra + std::max<uint32_t>(stage_bytes * a.stages, a.splits > 1 ? (uint32_t)a.nt * kFeat * 4u : 0u)};
 }
 
-template <int kMode, int kExact>
-int launch_kind(const CUtensorMap& w_map, const CUtensorMap& x_map, const CUtensorMap& b_map, ProjectArgs a, const Shape& shape, cudaStream_t st) {
+struct Maps { CUtensorMap w, x, b, h; };
+template <int kMode, int kExact, bool kTwo>
+int launch_kind(const Maps& maps, ProjectArgs a, const Shape& shape, cudaStream_t st) {
   static bool done[kMaxDevices];
-  if (!ensure_dynamic_smem(k_project<kMode, kExact>, 227 * 1024, done)) return -1;
+  if (!ensure_dynamic_smem(k_project<kMode, kExact, kTwo>, 227 * 1024, done)) return -1;
   // accumulators: one where a CTA has one tile of one chunk, or tensor memory holds no more beside the sums; the sums behind them
-  const bool single = !kExact && (int64_t)a.feat_tiles * a.row_tiles <= shape.ctas / a.splits;
+  const bool single = !kExact && (int64_t)a.feat_tiles * a.row_tiles <= shape.ctas / (a.splits * (kTwo ? 2 : 1));
   uint32_t cols = 32;
   while (cols < (uint32_t)a.nt) cols *= 2;
   a.accs = single || kExact == 8 ? 1 : 2;
@@ -860,9 +957,9 @@ int launch_kind(const CUtensorMap& w_map, const CUtensorMap& x_map, const CUtens
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   int n = 0;
-  if (a.splits > 1) {
+  if (kTwo || a.splits > 1) {
     attr[n].id = cudaLaunchAttributeClusterDimension;
-    attr[n].val.clusterDim.x = (unsigned)a.splits;
+    attr[n].val.clusterDim.x = (unsigned)(a.splits * (kTwo ? 2 : 1));
     attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
     ++n;
   }
@@ -873,12 +970,14 @@ int launch_kind(const CUtensorMap& w_map, const CUtensorMap& x_map, const CUtens
   }
   cfg.attrs = attr;
   cfg.numAttrs = n;
-  return cudaLaunchKernelEx(&cfg, k_project<kMode, kExact>, w_map, x_map, b_map, a) == cudaSuccess ? 1 : -1;
+  return cudaLaunchKernelEx(&cfg, k_project<kMode, kExact, kTwo>, maps.w, maps.x, maps.b, maps.h, a) == cudaSuccess ? 1 : -1;
 }
 template <int kMode>
-int launch_main(const CUtensorMap& w_map, const CUtensorMap& x_map, const CUtensorMap& b_map, const ProjectArgs& a, const Shape& shape, cudaStream_t st) {
-  if (!a.y_fp32) return launch_kind<kMode, 0>(w_map, x_map, b_map, a, shape, st);
-  return a.nt <= 128 ? launch_kind<kMode, 4>(w_map, x_map, b_map, a, shape, st) : launch_kind<kMode, 8>(w_map, x_map, b_map, a, shape, st);
+int launch_main(const Maps& maps, const ProjectArgs& a, const Shape& shape, cudaStream_t st) {
+  if constexpr (kMode != kDown)
+    if (a.two) return a.y_fp32 ? launch_kind<kMode, 8, true>(maps, a, shape, st) : launch_kind<kMode, 0, true>(maps, a, shape, st);
+  if (!a.y_fp32) return launch_kind<kMode, 0, false>(maps, a, shape, st);
+  return a.nt <= 128 ? launch_kind<kMode, 4, false>(maps, a, shape, st) : launch_kind<kMode, 8, false>(maps, a, shape, st);
 }
 
 // Rows of x that one pass takes: more go in several, one behind the other, so that the scratch stays bounded.
@@ -909,45 +1008,50 @@ static int launch_pass(const gf_projection_t& p, int rows, const void* x, int64_
   a.in_dim = p.in_dim;
   a.out_dim = p.out_dim;
   a.nt = tile_rows(rows);
-  a.feat_tiles = (p.out_dim + kFeat - 1) / kFeat;
+  a.two = a.nt == 256 && p.out_dim > kFeat;
+  const int tile_feat = kFeat * (a.two ? 2 : 1);
+  a.feat_tiles = (p.out_dim + tile_feat - 1) / tile_feat;
   a.row_tiles = (rows + a.nt - 1) / a.nt;
   a.y = y;
   a.y_stride = y_stride;
   a.y_fp32 = y_fp32;
   a.status = status;
   a.y_vec = (y_stride & 3) == 0 && ((uintptr_t)y & (y_fp32 ? 15 : 7)) == 0;
-  CUtensorMap w_map, x_map, b_map = {};
-  if (!make_map(&w_map, p.w_dev, 0, p.out_dim, p.in_dim, p.w_stride, kStep, kFeat) || !make_map(&x_map, x, 0, rows, p.in_dim, x_stride, kStep, a.nt)) return -1;
-  if (!with) {
-    const Shape shape = shape_of(a, (int64_t)a.feat_tiles * a.row_tiles, num_sms);
-    return launch_main<kPlain>(w_map, x_map, b_map, a, shape, st);
-  }
+  Maps maps = {};
+  const int x_box = a.nt / (a.two ? 2 : 1);
+  if (!make_map(&maps.w, p.w_dev, 0, p.out_dim, p.in_dim, p.w_stride, kStep, kFeat) || !make_map(&maps.x, x, 0, rows, p.in_dim, x_stride, kStep, x_box)) return -1;
+  const Shape main_shape = shape_of(a, (int64_t)a.feat_tiles * a.row_tiles, num_sms);
+  if (!with) return launch_main<kPlain>(maps, a, main_shape, st);
   place_slots(&a.slots, (char*)scratch, rows, p.rank, p.num_adapters, y_fp32 ? 3 : 2);
   a.slots.scale = p.scale_dev;
-  if (!make_map(&b_map, p.b_dev, p.num_adapters, p.out_dim, p.rank, p.rank, a.slots.padded, kFeat)) return -1;
-  const Shape main_shape = shape_of(a, (int64_t)a.feat_tiles * a.row_tiles, num_sms);
+  if (!make_map(&maps.b, p.b_dev, p.num_adapters, p.out_dim, p.rank, p.rank, a.slots.padded, kFeat) ||
+      !make_map(&maps.h, a.slots.h, 0, (int64_t)a.row_tiles * a.slots.most * a.slots.numbers * a.nt, a.slots.padded, a.slots.padded, a.slots.padded, x_box))
+    return -1;
   const int chunks = (a.slots.padded + kRowRanks - 1) / kRowRanks;
   if ((int64_t)rows * chunks <= 8 * num_sms) {
     k_adapter_rows<<<dim3((unsigned)rows, (unsigned)chunks), kRowThreads, 0, st>>>((const __nv_bfloat16*)x, x_stride, rows, p.in_dim, a.nt, adapter,
                                                                                     p.num_adapters, a.slots, (const __nv_bfloat16*)p.a_dev, status);
     if (cudaGetLastError() != cudaSuccess) return -1;
-    return launch_main<kWith>(w_map, x_map, b_map, a, main_shape, st) < 0 ? -1 : 2;
+    return launch_main<kWith>(maps, a, main_shape, st) < 0 ? -1 : 2;
   }
   k_adapter_slots<<<(unsigned)a.row_tiles, 256, 0, st>>>(adapter, rows, a.nt, p.num_adapters, a.slots, status);
   if (cudaGetLastError() != cudaSuccess) return -1;
   // A x: as many tiles as there can be slots; those of none are passed over.  Shared out as if every tile of x had one.
   ProjectArgs d = a;
-  CUtensorMap a_map;
-  if (!make_map(&a_map, p.a_dev, 0, (int64_t)p.num_adapters * p.rank, p.in_dim, p.in_dim, kStep, p.rank)) return -1;
+  Maps down = maps;
+  if (!make_map(&down.w, p.a_dev, 0, (int64_t)p.num_adapters * p.rank, p.in_dim, p.in_dim, kStep, p.rank) ||
+      (a.two && !make_map(&down.x, x, 0, rows, p.in_dim, x_stride, kStep, a.nt)))
+    return -1;
   const int per_tile = kFeat / a.slots.padded;
+  d.two = 0;
   d.feat_tiles = (a.slots.most + per_tile - 1) / per_tile;
   Shape shape = shape_of(d, (int64_t)a.row_tiles, num_sms);
   const int most_groups = std::max(1, num_sms * 3 / 4 / d.splits);
   int64_t down_groups = shape.ctas / d.splits;  // at most one per tile of x; more where multiprocessors are left
   if (down_groups == a.row_tiles) down_groups *= std::max<int64_t>(1, std::min<int64_t>(d.feat_tiles, most_groups / down_groups));
   shape.ctas = (int)down_groups * d.splits;
-  if (launch_main<kDown>(a_map, x_map, b_map, d, shape, st) < 0) return -1;
-  return launch_main<kWith>(w_map, x_map, b_map, a, main_shape, st) < 0 ? -1 : 3;
+  if (launch_main<kDown>(down, d, shape, st) < 0) return -1;
+  return launch_main<kWith>(maps, a, main_shape, st) < 0 ? -1 : 3;
 }
 
 int launch_project(const gf_projection_t& p, int rows, const void* x, int64_t x_stride, const int32_t* adapter, void* y, int64_t y_stride, int y_fp32,
