@@ -620,7 +620,7 @@ gf_status_t gf_append_slots(gf_wgraph_t* g, int32_t num_requests, const int32_t*
   if (!dev.ok) return GF_ERR_CUDA;
   g->generation++;  // lengths change: built tables are stale
   const int n = launch_append_slots(g->gd, g->pool, g->desc.num_layers, g->desc.num_kv_heads, g->desc.head_dim, num_requests, node_dev, held_dev,
-                                    count_dev, num_new, slots_dev, len_dev, g->status_dev, (cudaStream_t)stream);
+                                    count_dev, num_new, slots_dev, len_dev, g->num_sms, g->status_dev, (cudaStream_t)stream);
   if (n < 0) return GF_ERR_CUDA;
   g->launches += n;
   return GF_OK;

@@ -6,13 +6,15 @@
 // length is written where the table builder reads it.  Every row of an open node at or beyond its length is zero in
 // every layer (gf_node_kv_open clears the extent, a call that takes tokens back clears theirs), so that the tails of
 // its tiles contribute exact zeros to P*V as everywhere in the pool.
+#include <algorithm>
+
 #include "gf_device.cuh"
 #include "gf_internal.h"
 
 namespace gf {
 namespace {
 
-constexpr int kSlotThreads = 256, kSlotRequests = 32;  // requests per CTA
+constexpr int kSlotThreads = 256, kSlotRequests = 32;  // requests per CTA, at most
 
 __device__ __forceinline__ char* chunk_at(const PoolGeom& pool, int layer, int head, int slot, int chunk, int value) {
   const uint32_t row = (uint32_t)slot & (kTile - 1);
@@ -21,31 +23,29 @@ __device__ __forceinline__ char* chunk_at(const PoolGeom& pool, int layer, int h
          (uint32_t)(chunk >> 3) * (kTile * 128u) + swz128(row, (uint32_t)chunk & 7u);
 }
 
-// Zeros in the rows [from, to) of the pool, every layer and head, by all threads of the CTA.
-__device__ void clear_rows(const PoolGeom& pool, int layers, int heads, int chunks, int from, int to) {
-  const long long total = (long long)(to - from) * layers * heads * 2 * chunks;
-  for (long long i = threadIdx.x; i < total; i += blockDim.x) {
-    const int c = (int)(i % chunks);
-    long long j = i / chunks;
-    const int value = (int)(j & 1);
-    j >>= 1;
-    const int slot = from + (int)(j % (to - from));
-    j /= to - from;
-    *reinterpret_cast<uint4*>(chunk_at(pool, (int)(j / heads), (int)(j % heads), slot, c, value)) = make_uint4(0u, 0u, 0u, 0u);
+// Zeros in the rows [from, to) of the pool, (layer, head) pairs first .. last, by all threads of the CTA (256): 2 * chunks neighbouring
+// threads a row.
+__device__ void clear_rows(const PoolGeom& pool, int heads, int chunks, int from, int to, int first, int last) {
+  const int per_row = 2 * chunks, c = threadIdx.x % per_row, value = c >= chunks;
+  for (int j = first + threadIdx.x / per_row; j < last; j += 256 / per_row) {
+    const int layer = j / heads, head = j - layer * heads;
+    for (int slot = from; slot < to; ++slot)
+      *reinterpret_cast<uint4*>(chunk_at(pool, layer, head, slot, c - value * chunks, value)) = make_uint4(0u, 0u, 0u, 0u);
   }
 }
 
-// A CTA has 32 requests: it adds up the counts of those before them (each CTA by itself: 4 bytes a request from L2, against a
-// launch or a chain of CTAs), one warp checks its requests and sets their lengths, and all warps write the slots.
+// A CTA has `per` requests, one where multiprocessors are left (what taken-back tokens leave to clear is much: 131 KB a token of 32 layers with 8
+// heads): it adds up the counts of those before them (each CTA by itself: 4 bytes a request from L2, against a
+// launch or a chain of CTAs), one warp checks its requests and sets their lengths, and all threads write the slots.
 // Latency-bound: a chain of four dependent loads.
-__global__ void __launch_bounds__(kSlotThreads) k_append_slots(GraphDev g, PoolGeom pool, int layers, int heads, int chunks, int num_requests,
+__global__ void __launch_bounds__(kSlotThreads) k_append_slots(GraphDev g, PoolGeom pool, int layers, int heads, int chunks, int num_requests, int per,
                                                                const int32_t* __restrict__ node, const int32_t* __restrict__ held,
                                                                const int32_t* __restrict__ count, int num_new, int32_t* __restrict__ slots,
                                                                int32_t* __restrict__ lens, int32_t* status) {
   __shared__ long long warp_sums[kSlotThreads / 32];
   __shared__ int s_begin[kSlotRequests + 1], s_slot[kSlotRequests], s_from[kSlotRequests], s_to[kSlotRequests];
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-  const int r0 = blockIdx.x * kSlotRequests;
+  const int r0 = blockIdx.x * per;
   long long before = 0;
   for (int r = tid; r < r0; r += kSlotThreads) before += max(count[r], 0);
 #pragma unroll
@@ -57,7 +57,7 @@ __global__ void __launch_bounds__(kSlotThreads) k_append_slots(GraphDev g, PoolG
 #pragma unroll
     for (int w = 0; w < kSlotThreads / 32; ++w) begin += warp_sums[w];
     const int r = r0 + lane;
-    const bool mine = r < num_requests;
+    const bool mine = lane < per && r < num_requests;
     const int c = mine ? count[r] : 0, v = mine ? node[r] : -1;
     const bool known = v >= 0 && v < g.num_nodes;
     const int room = known ? g.node_room[v] : -1, now = known ? g.node_len[v] : 0;
@@ -87,14 +87,14 @@ __global__ void __launch_bounds__(kSlotThreads) k_append_slots(GraphDev g, PoolG
     if (lane == 31) s_begin[32] = (int)min(end, (long long)num_new);
   }
   __syncthreads();
-  for (int i = wid; i < kSlotRequests; i += kSlotThreads / 32) {
-    const int a = s_begin[i], b = s_begin[i + 1], s = s_slot[i];
-    for (int t = a + lane; t < b; t += 32) slots[t] = s < 0 ? -1 : s + (t - a);
+  for (int t = s_begin[0] + tid, i = 0; t < s_begin[per]; t += kSlotThreads) {
+    while (t >= s_begin[i + 1]) ++i;
+    slots[t] = s_slot[i] < 0 ? -1 : s_slot[i] + (t - s_begin[i]);
   }
-  if (r0 + kSlotRequests >= num_requests)  // rows behind the last request's
-    for (int t = s_begin[kSlotRequests] + tid; t < num_new; t += kSlotThreads) slots[t] = -1;
-  for (int i = 0; i < kSlotRequests; ++i)
-    if (s_to[i] > s_from[i]) clear_rows(pool, layers, heads, chunks, s_from[i], s_to[i]);
+  if (r0 + per >= num_requests)  // rows behind the last request's
+    for (int t = s_begin[per] + tid; t < num_new; t += kSlotThreads) slots[t] = -1;
+  for (int i = 0; i < per; ++i)
+    if (s_to[i] > s_from[i]) clear_rows(pool, heads, chunks, s_from[i], s_to[i], 0, layers * heads);
 }
 
 // One layer's new rows from the caller's layout to their slots: 16 bytes of K and of V per step of a thread, a few tokens per
@@ -130,27 +130,26 @@ __global__ void __launch_bounds__(256) k_clear_extent(PoolGeom pool, int rows, i
   }
 }
 
-// The end of a node's growth: its length, and zeros in what is left of its last tile.
-__global__ void __launch_bounds__(256) k_close_node(GraphDev g, PoolGeom pool, int layers, int heads, int chunks, int node, int n_tokens,
-                                                    int32_t* status) {
-  const int off = g.node_off[node], now = g.node_len[node];
-  if (threadIdx.x == 0 && now < n_tokens) atomicCAS(status + kStatusReport, 0, (int)GF_ERR_INVALID_ARG);
-  const int end = min(now, (n_tokens + kTile - 1) / kTile * kTile);
-  if (end > n_tokens) clear_rows(pool, layers, heads, chunks, off + n_tokens, off + end);
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    g.node_len[node] = n_tokens;
-    g.node_room[node] = -1;
-  }
+// The end of a node's growth: zeros in what is left of its last tile, a CTA per layer, then its length.
+__global__ void __launch_bounds__(256) k_clear_tail(GraphDev g, PoolGeom pool, int heads, int chunks, int node, int n_tokens) {
+  const int off = g.node_off[node], end = min(g.node_len[node], (n_tokens + kTile - 1) / kTile * kTile);
+  clear_rows(pool, heads, chunks, off + n_tokens, off + end, blockIdx.x * heads, (blockIdx.x + 1) * heads);
+}
+__global__ void k_close_node(GraphDev g, int node, int n_tokens, int32_t* status) {
+  if (g.node_len[node] < n_tokens) atomicCAS(status + kStatusReport, 0, (int)GF_ERR_INVALID_ARG);
+  g.node_len[node] = n_tokens;
+  g.node_room[node] = -1;
 }
 
 }  // namespace
 
 int launch_append_slots(const GraphDev& g, const PoolGeom& pool, int layers, int heads, int head_dim, int num_requests, const int32_t* node,
-                        const int32_t* held, const int32_t* count, int num_new, int32_t* slots, int32_t* lens, int32_t* status, cudaStream_t st) {
-  const int ctas = num_requests > 0 ? (num_requests + kSlotRequests - 1) / kSlotRequests : 1;  // (no request: the rows' -1 are left)
-  k_append_slots<<<ctas, kSlotThreads, 0, st>>>(
-      g, pool, layers, heads, head_dim / 8, num_requests, node, held, count, num_new, slots, lens, status);
+                        const int32_t* held, const int32_t* count, int num_new, int32_t* slots, int32_t* lens, int num_sms, int32_t* status,
+                        cudaStream_t st) {
+  const int per = std::min(kSlotRequests, std::max(1, num_requests / (2 * num_sms)));
+  const int ctas = num_requests > 0 ? (num_requests + per - 1) / per : 1;  // (no request: the rows' -1 are left)
+  k_append_slots<<<ctas, kSlotThreads, 0, st>>>(g, pool, layers, heads, head_dim / 8, num_requests, per, node, held, count, num_new, slots, lens,
+                                                status);
   return cudaGetLastError() == cudaSuccess ? 1 : -1;
 }
 
@@ -173,8 +172,10 @@ int launch_clear_extent(const PoolGeom& pool, int layers, int heads, int tile0, 
 
 int launch_close_node(const GraphDev& g, const PoolGeom& pool, int layers, int heads, int head_dim, int node, int n_tokens, int32_t* status,
                       cudaStream_t st) {
-  k_close_node<<<1, 256, 0, st>>>(g, pool, layers, heads, head_dim / 8, node, n_tokens, status);
-  return cudaGetLastError() == cudaSuccess ? 1 : -1;
+  k_clear_tail<<<layers, 256, 0, st>>>(g, pool, heads, head_dim / 8, node, n_tokens);
+  if (cudaGetLastError() != cudaSuccess) return -1;
+  k_close_node<<<1, 1, 0, st>>>(g, node, n_tokens, status);
+  return cudaGetLastError() == cudaSuccess ? 2 : -1;
 }
 
 }  // namespace gf

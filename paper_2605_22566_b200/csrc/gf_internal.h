@@ -276,7 +276,8 @@ inline bool ensure_dynamic_smem(K kernel, size_t bytes, bool (&done)[kMaxDevices
 int launch_graph_set_node(const GraphDev& g, int node, int len, int off, cudaStream_t st, int room = -1);
 // Growing nodes (see gf_append_slots).  Strides in entries.
 int launch_append_slots(const GraphDev& g, const PoolGeom& pool, int layers, int heads, int head_dim, int num_requests, const int32_t* node,
-                        const int32_t* held, const int32_t* count, int num_new, int32_t* slots, int32_t* lens, int32_t* status, cudaStream_t st);
+                        const int32_t* held, const int32_t* count, int num_new, int32_t* slots, int32_t* lens, int num_sms, int32_t* status,
+                        cudaStream_t st);
 int launch_kv_append(const PoolGeom& pool, int layer, int heads, int head_dim, int num_new, const int32_t* slots, const void* k,
                      int64_t k_stride, const void* v, int64_t v_stride, int num_sms, int32_t* status, cudaStream_t st);
 int launch_clear_extent(const PoolGeom& pool, int layers, int heads, int tile0, int tiles, cudaStream_t st);
