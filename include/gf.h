@@ -529,7 +529,8 @@ gf_status_t gf_edge_scores(gf_wgraph_t* g, const gf_scorer_t* model, const float
  *   y[t] = W x[t] + scale[a] B[a] (A[a] x[t]),   a = adapter[t]; -1: no adapter.
  * bf16 row-major, caller-owned, 16-byte aligned; A [num_adapters, rank, in_dim], B [num_adapters, out_dim, rank], contiguous;
  * scale NULL: 1.  in_dim and w_stride (entries between rows of W) are multiples of 8; rank a multiple of 8, at most 64
- * (adapters of a smaller rank are filled up with zeros); num_adapters at most GF_MAX_ADAPTERS, 0: none. */
+ * (adapters of a smaller rank are filled up with zeros); num_adapters at most GF_MAX_ADAPTERS, 0: none.  B's entries are finite: rows of
+ * other adapters meet them times zero.  What A, x, or a scale hold of infinities and NaN stays in the rows that it belongs to. */
 #define GF_MAX_ADAPTERS 32768
 typedef struct {
   int32_t in_dim, out_dim;
@@ -541,7 +542,8 @@ typedef struct {
   const float* scale_dev; /* fp32 [num_adapters] */
 } gf_projection_t;
 
-/* Scratch of a call with adapters, 16-byte aligned: up to 6 bytes per rank (16, 32 or 64), row and adapter (256 at most), for at most 16 384 rows at a time; two calls that may overlap on the GPU each need their own. */
+/* Scratch of a call with adapters, 16-byte aligned: up to 6 bytes per rank (16, 32 or 64), row and adapter (256 at most), for at most 16 384
+ * rows at a time; two calls that may overlap on the GPU each need their own. */
 uint64_t gf_adapter_project_scratch_bytes(const gf_projection_t* p, int32_t rows);
 
 /* x_dev: bf16 [rows, in_dim], rows x_stride entries apart (a multiple of 8), 16-byte aligned.  adapter_dev: int32 [rows], or NULL for

@@ -25,6 +25,7 @@ GF_MODE_DEFERRED = 0x100
 GF_TILE_TOKENS = 64
 GF_STATIC_SCRATCH_BYTES = 32 << 20
 GF_MAX_TOP = 32
+GF_MAX_ADAPTERS = 32768
 
 EXPORTS = [
     "gf_status_string", "gf_pool_bytes_per_tile", "gf_workspace_bytes", "gf_wgraph_create",

@@ -34,7 +34,8 @@ def tensor_to_f64(t: torch.Tensor) -> np.ndarray:
 
 class Projection:
     """A shared weight [out, in] with the low-rank adapters that rows may name: a [adapters, rank, in], b [adapters, out, rank],
-    scale fp32 [adapters] (None: 1).  bf16, on one device; kept alive here.  The weight's rows may lie apart, the adapters are contiguous."""
+    scale fp32 [adapters] (None: 1).  bf16, on one device; kept alive here.  The weight's rows may lie apart, the adapters are contiguous.  b holds finite entries only, which is
+    looked at here (once: whoever writes to it later keeps them so)."""
 
     def __init__(self, weight: torch.Tensor, a: Optional[torch.Tensor] = None, b: Optional[torch.Tensor] = None,
                  scale: Optional[torch.Tensor] = None):
@@ -48,6 +49,8 @@ class Projection:
                     not b.is_contiguous() or a.device != weight.device or b.device != weight.device:
                 raise ValueError(f"a, b: contiguous bf16 tensors [adapters, rank, {in_dim}] and [adapters, {out_dim}, rank] on {weight.device}")
             adapters, rank = a.shape[:2]
+            if not bool(torch.isfinite(b).all()):
+                raise ValueError("b: finite entries (rows of other adapters meet them times zero)")
         if scale is not None and (a is None or scale.dtype != torch.float32 or tuple(scale.shape) != (adapters,) or not scale.is_contiguous() or
                                   scale.device != weight.device):
             raise ValueError(f"scale: a contiguous fp32 tensor [{adapters}] on {weight.device}")
@@ -57,7 +60,6 @@ class Projection:
         # (a weight of one row may have any stride)
         stride = weight.stride(0) if out_dim > 1 else -(-in_dim // 8) * 8
         self.desc = B.ProjectionDesc(in_dim, out_dim, weight.data_ptr(), stride, adapters, rank, _ptr(a), _ptr(b), _ptr(scale))
-
 
     def scratch_bytes(self, rows: int) -> int:
         """gf_adapter_project_scratch_bytes."""

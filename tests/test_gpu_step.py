@@ -104,6 +104,34 @@ def test_slots_of_many_requests_with_refused_ones_among_them():
     pa.close()
 
 
+@pytest.mark.parametrize("n", [297, 600, 20000])
+def test_slots_of_batches_of_any_size(n):
+    """More requests than multiprocessors, in blocks of one, of two and of 32; some take tokens back, whose rows are zeros in every layer."""
+    rng = np.random.default_rng(n)
+    few = 600
+    pa = _pa([70] * few, 2, 2, 64, 3)
+    model = OS.OpenNodes()
+    for v in range(few):
+        pa.open_node(v, 70)
+        model.open(v, 70, pa.node_slot(v))
+    pa.pool.fill_(0xFF)
+    nodes = rng.permutation(few).tolist()[:n] + [-1] * (n - few)       # (the others are refused)
+    counts = rng.integers(0, 66, n).tolist()
+    for held in (None, [int(rng.integers(0, c + 1)) for c in counts]):
+        new = counts if held is None else rng.integers(0, 5, n).tolist()
+        before = [len(model.rows[v]) for v in range(few)]
+        slots, lens = pa.append_slots(_ints(*nodes), _ints(*new), sum(new), None if held is None else _ints(*held))
+        want, want_lens = model.append(nodes, held, new, sum(new))
+        assert slots.tolist() == want and lens.tolist() == want_lens
+    pa.status()
+    for v in rng.permutation(few)[:40].tolist():
+        for layer in range(3):
+            k, val = pa.load_node(v, layer)
+            gone = slice(len(model.rows[v]), max(before[v], len(model.rows[v])))
+            assert not k[gone].any() and not val[gone].any()
+    pa.close()
+
+
 def test_close_reopen_release_and_refusals():
     from paper_2605_22566_b200 import binding as B
     pa = _pa([300, 64, 64, 10], 2, 2, 64, 2, extra_tiles=4, max_residual_nodes=1)
@@ -255,6 +283,65 @@ def test_projection_sizes(rows, k, n, adapters, rank, dtype):
     pa.close()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,k,n,adapters,rank", [
+    # a pair's tiles: 128, 129, 256 and 257 features, the last with two of three halves empty; K in a few and in many parts; odd numbers of stages
+    (256, 192, 128, 0, 0), (256, 192, 129, 2, 16), (511, 64, 256, 3, 64), (512, 4096, 257, 0, 0), (256, 2624, 300, 3, 24), (300, 8192, 513, 5, 40),
+    (2304, 72, 600, 2, 8), (2305, 128, 520, 0, 0),
+    # every row its own adapter, odd numbers of slots; the ways to A x on either side of their border
+    (256, 64, 300, 1000, 64), (97, 136, 200, 97, 32), (101, 64, 140, 400, 24), (592, 64, 140, 3, 32), (593, 64, 140, 3, 32), (1184, 40, 70, 9, 16), (1185, 40, 70, 9, 16),
+    # all the adapters that there may be; rows in more than one pass, the last of one row and of many
+    (40, 16, 24, 32768, 8), (16385, 24, 40, 3, 8), (16384 + 300, 16, 33, 40, 16), (2 * 16384 + 5, 8, 16, 2, 8)])
+def test_projection_at_the_borders_of_its_launches(rows, k, n, adapters, rank, dtype):
+    from paper_2605_22566_b200.runtime import Projection
+    rng = np.random.default_rng(rows * 3 + k + n)
+    pa = _pa()
+    x, w = _bf16(rng, rows, k).cuda(), (_bf16(rng, n, k) * k ** -0.5).cuda()
+    a = b = scale = which = None
+    if adapters:
+        a, b = (_bf16(rng, adapters, rank, k) * k ** -0.5).cuda(), _bf16(rng, adapters, n, rank).cuda()
+        scale = torch.from_numpy(rng.uniform(-1, 1, adapters)).float().cuda()
+        which = _ints(*rng.integers(-1, adapters, rows).tolist())
+        which[-1] = adapters - 1
+    p = Projection(w, a, b, scale)
+    got = pa.project(p, x, which, dtype=dtype)
+    _check_projection(got, x, w, a, b, scale, which)
+    assert torch.equal(got, pa.project(p, x, which, dtype=dtype)) and pa.status() == 0
+    pa.close()
+
+
+def test_projections_of_two_handles_and_threads_at_once():
+    """Two threads, each with a stream of its own, with one projection; one, two and three launches a call."""
+    import threading
+    from paper_2605_22566_b200.runtime import Projection
+    rng = np.random.default_rng(9)
+    pas = [_pa(), _pa()]
+    p = Projection((_bf16(rng, 900, 256) * 0.06).cuda(), (_bf16(rng, 6, 16, 256) * 0.06).cuda(), _bf16(rng, 6, 900, 16).cuda())
+    xs = [_bf16(rng, rows, 256).cuda() for rows in (3, 300, 1500)]
+    ids = [_ints(*rng.integers(-1, 6, len(x)).tolist()) for x in xs]
+    want = [pas[0].project(p, x, i) for x, i in zip(xs, ids)]
+    for y, x, i in zip(want, xs, ids):
+        _check_projection(y, x, p.weight, p.a, p.b, None, i)
+    torch.cuda.synchronize()
+    bad = []
+
+    def work(pa):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(20):
+                got = [pa.project(p, x, i) for x, i in zip(xs, ids)]
+            torch.cuda.current_stream().synchronize()
+        bad.extend(n for n, (y, z) in enumerate(zip(got, want)) if not torch.equal(y, z))
+    threads = [threading.Thread(target=work, args=(pa,)) for pa in pas]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad
+    for pa in pas:
+        assert pa.status() == 0
+        pa.close()
+
+
 def test_projection_strides_bad_adapters_and_what_lies_beside():
     from paper_2605_22566_b200 import binding as B
     from paper_2605_22566_b200.runtime import Projection
@@ -377,6 +464,12 @@ def test_projection_refusals():
         Projection(w, a)
     with pytest.raises(ValueError):
         Projection(w, a, b[:, :31].contiguous())
+    b[1, 3, 2] = float("inf")                                       # (it would reach rows of the other adapters)
+    with pytest.raises(ValueError, match="finite"):
+        Projection(w, a, b)
+    desc = B.ProjectionDesc(*[B.GF_MAX_ADAPTERS + 1 if n == "num_adapters" else getattr(p.desc, n) for n, _ in p.desc._fields_])
+    assert B.gf_adapter_project_scratch_bytes(desc, 4) == 0
+    assert B.gf_adapter_project(pa.g, desc, 4, *[good[n] for n in ("x", "xs", "which", "y", "ys", "fp32", "scratch", "nbytes")], pa.stream) == B.GF_ERR_INVALID_ARG
     assert pa.status() == 0
     pa.close()
 
@@ -427,6 +520,19 @@ def test_logprobs_sizes_and_strides(rows, v, top, stride, dtype):
     if top:
         none = pa.token_logprobs(x, None, 0)
         assert none.logprob is None and torch.equal(none.lse, got.lse) and torch.equal(none.entropy, got.entropy)
+    assert pa.status() == 0
+    pa.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,v,top", [(1, 1000003, 32), (149, 12000, 5), (148, 12001, 5), (2100, 257, 1), (37, 30011, 2)])
+def test_logprobs_of_long_and_of_many_rows(rows, v, top, dtype):
+    """Rows in one part and in several, with values on a coarse grid, so that many are equal."""
+    rng = np.random.default_rng(rows + v)
+    pa = _pa()
+    x = torch.from_numpy(np.round(rng.standard_normal((rows, v)) * 8) / 4).to(dtype).cuda()
+    tokens = _ints(*rng.integers(-1, v, rows).tolist())
+    _check_logprobs(pa.token_logprobs(x, tokens, top), x, tokens, top)
     assert pa.status() == 0
     pa.close()
 
