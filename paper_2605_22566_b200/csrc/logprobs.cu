@@ -412,7 +412,7 @@ struct Place {
 };
 
 template <typename T>
-__global__ void __launch_bounds__(kMaxThreads, 3) k_token_logprobs(const T* __restrict__ logits, int64_t row_stride, int rows, int vocab, int parts,
+__global__ void __launch_bounds__(kMaxThreads, 3) k_token_logprobs(const T* __restrict__ logits, int64_t row_stride, int vocab, int parts,
                                                                 const int32_t* __restrict__ tokens, int k, float* __restrict__ logprob,
                                                                 float* __restrict__ entropy, float* __restrict__ lse_out,
                                                                 int32_t* __restrict__ top_ids, float* __restrict__ top_logprobs, int32_t* status) {
@@ -422,36 +422,24 @@ __global__ void __launch_bounds__(kMaxThreads, 3) k_token_logprobs(const T* __re
   extern __shared__ __align__(128) uint4 ring[];  // [warps][kStages][kRound]
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, threads = blockDim.x, warps = threads >> 5;
   const int part = parts > 1 ? (int)cluster_rank() : 0;
-  const int64_t first_row = blockIdx.x / parts, row_step = gridDim.x / parts;
+  const int64_t row = blockIdx.x / parts;
+  const Place<T> p(logits + row * row_stride, vocab, part, parts, wid, warps);
+  const T* __restrict__ x = p.x;
+  const int head = p.head, tail = p.tail, v0 = p.v0, v1 = p.v1;
   // (three quarters of the warps: the least of all levels lies lower than that which all but two reach with more lanes)
   const int want = k + kMargin, most_warps = warps - warps / 4, enough = (want + most_warps - 1) / most_warps, nth = (want + enough - 1) / enough;
-  // Lane 0 brings the warp's rounds, those of the next row behind those of this one, so that HBM is not left idle by a row's end.
+  // Lane 0 brings the warp's rounds.
   uint4* my_ring = ring + wid * kStages * kRound;
-  int64_t bring_row = first_row;
-  const uint4* bring_from = nullptr;  // the next round of bring_row, null: its first
-  int bring_left = 0;                 // vectors from there to the end of the CTA's part
-  int bring_len = 0, bring_stride = 0;
+  int bring_at = p.first;  // the next round's first vector
   uint32_t brought = 0, taken = 0;
   auto bring = [&] {
-    for (; bring_row < rows; bring_row += row_step, bring_from = nullptr) {
-      if (bring_from == nullptr) {
-        const Place<T> p(logits + bring_row * row_stride, vocab, part, parts, wid, warps);
-        bring_from = p.xv + p.first;
-        bring_left = p.v1 - p.first;
-        bring_len = p.len;
-        bring_stride = p.stride;
-      }
-      if (bring_left > 0) {
-        const uint32_t bytes = (uint32_t)min(bring_len, bring_left) * 16u;
-        uint64_t* full = &sm.full[wid][brought % kStages];
-        mbar_arrive_expect_tx(full, bytes);
-        bulk_g2s(my_ring + (brought % kStages) * kRound, bring_from, bytes, full);
-        ++brought;
-        bring_from += bring_stride;
-        bring_left -= bring_stride;
-        return;
-      }
-    }
+    if (bring_at >= v1) return;
+    const uint32_t bytes = (uint32_t)min(p.len, v1 - bring_at) * 16u;
+    uint64_t* full = &sm.full[wid][brought % kStages];
+    mbar_arrive_expect_tx(full, bytes);
+    bulk_g2s(my_ring + (brought % kStages) * kRound, p.xv + bring_at, bytes, full);
+    ++brought;
+    bring_at += p.stride;
   };
   if (lane == 0) {
     for (int i = 0; i < kStages; ++i) mbar_init(&sm.full[wid][i], 1);
@@ -461,202 +449,196 @@ __global__ void __launch_bounds__(kMaxThreads, 3) k_token_logprobs(const T* __re
   __syncwarp();
 
   bool ok = true;
-  for (int64_t row = first_row; row < rows; row += row_step) {
-    const Place<T> p(logits + row * row_stride, vocab, part, parts, wid, warps);
-    const T* __restrict__ x = p.x;
-    const int head = p.head, tail = p.tail, v0 = p.v0, v1 = p.v1;
-    Stats st{kNegInf, 0.f, 0.f};
-    float least = kNegInf;  // more than k logits of the CTA's part reach it, or minus infinity
-    auto push = [&](float v, int64_t index) {
-      const int at = atomicAdd(&sm.count, 1);
-      if (at < kList) sm.list[at] = key_of(v, index);
-    };
-    if (lane == 0) sm.level[wid] = kLowest;
-    if (tid == 0) {
-      sm.count = 0;
-      sm.common = kLowest;
+  Stats st{kNegInf, 0.f, 0.f};
+  float least = kNegInf;  // more than k logits of the CTA's part reach it, or minus infinity
+  auto push = [&](float v, int64_t index) {
+    const int at = atomicAdd(&sm.count, 1);
+    if (at < kList) sm.list[at] = key_of(v, index);
+  };
+  if (lane == 0) sm.level[wid] = kLowest;
+  if (tid == 0) {
+    sm.count = 0;
+    sm.common = kLowest;
+  }
+  // asked for here, used at the row's end
+  int token = -1;
+  float given = 0.f;
+  if (tid == 0 && part == 0 && tokens != nullptr) {
+    token = tokens[row];
+    if (token >= 0 && token < vocab) given = Vec<T>::one(x + token);
+  }
+  const int loose = part == 0 ? head + (vocab - tail) : 0;  // the entries that no vector holds: the first CTA's
+  const int my_loose = tid < head ? tid : tail + (tid - head);
+  float loose_value = kNegInf;
+  if (tid < loose) {
+    loose_value = Vec<T>::one(x + my_loose);
+    if (loose_value > st.m) st.m = loose_value;
+    stats_add(st, loose_value);
+  }
+  uint64_t l2 = 0ull, s2 = 0ull;  // l and s of the vectors, two halves
+  auto fold = [&] {
+    float lo, hi;
+    f2_unpack(l2, lo, hi);
+    st.l += lo + hi;
+    f2_unpack(s2, lo, hi);
+    st.s += lo + hi;
+    l2 = s2 = 0ull;
+  };
+  float seen = st.m;  // the thread's largest logit; st.m, what its sums are relative to, follows when it is left far behind
+  int round = 0;
+  for (int base = v0; base < v1; base += p.stride, ++round) {
+    const int begin = base + (p.first - v0), end = min(v1, begin + p.len);
+    const uint4* piece = my_ring + (taken % kStages) * kRound;
+    if (begin < v1) {
+      ok = ok && mbar_wait(&sm.full[wid][taken % kStages], (taken / kStages) & 1u, status);
+      ++taken;
     }
-    // asked for here, used at the row's end
-    int token = -1;
-    float given = 0.f;
-    if (tid == 0 && part == 0 && tokens != nullptr) {
-      token = tokens[row];
-      if (token >= 0 && token < vocab) given = Vec<T>::one(x + token);
+    __syncwarp();
+    uint4 raw[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) raw[u] = piece[u * 32 + lane];
+    if (begin + kRound > end) {
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (begin + u * 32 + lane >= end) raw[u] = make_uint4(Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing);
     }
-    const int loose = part == 0 ? head + (vocab - tail) : 0;  // the entries that no vector holds: the first CTA's
-    const int my_loose = tid < head ? tid : tail + (tid - head);
-    float loose_value = kNegInf;
-    if (tid < loose) {
-      loose_value = Vec<T>::one(x + my_loose);
-      if (loose_value > st.m) st.m = loose_value;
-      stats_add(st, loose_value);
+    const float most = Vec<T>::largest(raw);
+    seen = fmaxf(seen, most);
+    if (seen > st.m + kLag || st.m == kNegInf) {  // (a lag of 4 leaves a sum's terms below 2^6 and costs 2^-24 of it in the entropy)
+      fold();
+      if (seen > st.m) stats_move(st, seen);
     }
-    uint64_t l2 = 0ull, s2 = 0ull;  // l and s of the vectors, two halves
-    auto fold = [&] {
-      float lo, hi;
-      f2_unpack(l2, lo, hi);
-      st.l += lo + hi;
-      f2_unpack(s2, lo, hi);
-      st.s += lo + hi;
-      l2 = s2 = 0ull;
-    };
-    float seen = st.m;  // the thread's largest logit; st.m, what its sums are relative to, follows when it is left far behind
-    int round = 0;
-    for (int base = v0; base < v1; base += p.stride, ++round) {
-      const int begin = base + (p.first - v0), end = min(v1, begin + p.len);
-      const uint4* piece = my_ring + (taken % kStages) * kRound;
-      if (begin < v1) {
-        ok = ok && mbar_wait(&sm.full[wid][taken % kStages], (taken / kStages) & 1u, status);
-        ++taken;
-      }
-      __syncwarp();
-      uint4 raw[kAhead];
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) raw[u] = piece[u * 32 + lane];
-      if (begin + kRound > end) {
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-          if (begin + u * 32 + lane >= end) raw[u] = make_uint4(Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing, Vec<T>::kNothing);
-      }
-      const float most = Vec<T>::largest(raw);
-      seen = fmaxf(seen, most);
-      if (seen > st.m + kLag || st.m == kNegInf) {  // (a lag of 4 leaves a sum's terms below 2^6 and costs 2^-24 of it in the entropy)
-        fold();
-        if (seen > st.m) stats_move(st, seen);
-      }
-      if (k > 0) {
-        if (round == 0 || round == 2 || (round & 7) == 5) {  // (a level rises less and less)
-          publish(sm, seen, enough);
-          if (round == 0) __syncthreads();  // (nothing is listed before all warps have one)
-          const float level = common_level(sm, nth, warps);
-          if (lane == 0) atomicMax(&sm.common, order_of(level));
-          least = level;
-        } else {
-          least = value_of(*(volatile uint32_t*)&sm.common);
-        }
-        if (round == 0 && loose_value > least) push(loose_value, my_loose);
-      }
-      if (__all_sync(0xffffffffu, fabsf(st.m) < kFar || st.m == kNegInf)) {
-        const float c = st.m == kNegInf ? 0.f : -(st.m * kLog2e);  // (no logit with a probability yet: any reference will do)
-        const uint64_t cc = f2_pack(c, c), ee = f2_pack(kLog2e, kLog2e);
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-          float e[kN];
-          Vec<T>::get(raw[u], e);
-#pragma unroll
-          for (int i = 0; i < kN; i += 2) {
-            float d0, d1;
-            f2_unpack(f2_fma(f2_pack(e[i], e[i + 1]), ee, cc), d0, d1);
-            d0 = max_nan(d0, -1000.f);
-            d1 = max_nan(d1, -1000.f);
-            const uint64_t p2 = f2_pack(fast_exp2(d0), fast_exp2(d1));
-            l2 = f2_add(l2, p2);
-            s2 = f2_fma(p2, f2_pack(d0, d1), s2);
-          }
-        }
+    if (k > 0) {
+      if (round == 0 || round == 2 || (round & 7) == 5) {  // (a level rises less and less)
+        publish(sm, seen, enough);
+        if (round == 0) __syncthreads();  // (nothing is listed before all warps have one)
+        const float level = common_level(sm, nth, warps);
+        if (lane == 0) atomicMax(&sm.common, order_of(level));
+        least = level;
       } else {
-#pragma unroll 1
-        for (int v = lane; v < end - begin; v += 32)
-#pragma unroll 1
-          for (int i = 0; i < kN; ++i) stats_add(st, Vec<T>::one(reinterpret_cast<const T*>(piece + v) + i));
+        least = value_of(*(volatile uint32_t*)&sm.common);
       }
-      if (k > 0) {
-        // a lane that has a logit above the least: the warp looks at its entries, 32 words of them
-        for (uint32_t who = __ballot_sync(0xffffffffu, most > least); who; who &= who - 1) {
-          const int at = (lane >> 2) * 32 + __ffs(who) - 1;
-          float e[kPer];
-          Vec<T>::word(reinterpret_cast<const uint32_t*>(piece + at)[lane & 3], e);
-          if (begin + at < end) {
+      if (round == 0 && loose_value > least) push(loose_value, my_loose);
+    }
+    if (__all_sync(0xffffffffu, fabsf(st.m) < kFar || st.m == kNegInf)) {
+      const float c = st.m == kNegInf ? 0.f : -(st.m * kLog2e);  // (no logit with a probability yet: any reference will do)
+      const uint64_t cc = f2_pack(c, c), ee = f2_pack(kLog2e, kLog2e);
 #pragma unroll
-            for (int i = 0; i < kPer; ++i)
-              if (e[i] > least) push(e[i], head + (int64_t)(begin + at) * kN + (lane & 3) * kPer + i);
-          }
+      for (int u = 0; u < kAhead; ++u) {
+        float e[kN];
+        Vec<T>::get(raw[u], e);
+#pragma unroll
+        for (int i = 0; i < kN; i += 2) {
+          float d0, d1;
+          f2_unpack(f2_fma(f2_pack(e[i], e[i + 1]), ee, cc), d0, d1);
+          d0 = max_nan(d0, -1000.f);
+          d1 = max_nan(d1, -1000.f);
+          const uint64_t p2 = f2_pack(fast_exp2(d0), fast_exp2(d1));
+          l2 = f2_add(l2, p2);
+          s2 = f2_fma(p2, f2_pack(d0, d1), s2);
         }
       }
-      __syncwarp();
-      if (lane == 0 && ok && begin < v1) bring();
+    } else {
+#pragma unroll 1
+      for (int v = lane; v < end - begin; v += 32)
+#pragma unroll 1
+        for (int i = 0; i < kN; ++i) stats_add(st, Vec<T>::one(reinterpret_cast<const T*>(piece + v) + i));
     }
-    fold();
+    if (k > 0) {
+      // a lane that has a logit above the least: the warp looks at its entries, 32 words of them
+      for (uint32_t who = __ballot_sync(0xffffffffu, most > least); who; who &= who - 1) {
+        const int at = (lane >> 2) * 32 + __ffs(who) - 1;
+        float e[kPer];
+        Vec<T>::word(reinterpret_cast<const uint32_t*>(piece + at)[lane & 3], e);
+        if (begin + at < end) {
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) {
+          for (int i = 0; i < kPer; ++i)
+            if (e[i] > least) push(e[i], head + (int64_t)(begin + at) * kN + (lane & 3) * kPer + i);
+        }
+      }
+    }
+    __syncwarp();
+    if (lane == 0 && ok && begin < v1) bring();
+  }
+  fold();
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) {
+    Stats o;
+    o.m = __shfl_xor_sync(0xffffffffu, st.m, d);
+    o.l = __shfl_xor_sync(0xffffffffu, st.l, d);
+    o.s = __shfl_xor_sync(0xffffffffu, st.s, d);
+    st = stats_join(st, o);
+  }
+  if (lane == 0) sm.stats[wid] = st;
+  __syncthreads();
+  int have = 0;  // the largest of the CTA's part: best[0 .. have)
+  if (k > 0) {
+    if (v0 >= v1) {  // a row that is no longer than its loose entries
+      if (tid < loose && loose_value > kNegInf) push(loose_value, my_loose);
+      __syncthreads();
+    }
+    least = value_of(sm.common);
+    have = finish<T>(sm, k, least, p, loose, my_loose, vocab, warps);
+  }
+
+  if (wid == 0) {
+    st = lane < warps ? sm.stats[lane] : Stats{kNegInf, 0.f, 0.f};
+#pragma unroll
+    for (int d = kMaxThreads / 64; d > 0; d >>= 1) {
       Stats o;
       o.m = __shfl_xor_sync(0xffffffffu, st.m, d);
       o.l = __shfl_xor_sync(0xffffffffu, st.l, d);
       o.s = __shfl_xor_sync(0xffffffffu, st.s, d);
       st = stats_join(st, o);
     }
-    if (lane == 0) sm.stats[wid] = st;
+    st.m = __shfl_sync(0xffffffffu, st.m, 0);
+    st.l = __shfl_sync(0xffffffffu, st.l, 0);
+    st.s = __shfl_sync(0xffffffffu, st.s, 0);
+  }
+  if (parts > 1) {
+    if (tid == 0) sm.part = st;
+    for (int i = have + tid; i < k; i += threads) sm.best[i] = 0;
     __syncthreads();
-    int have = 0;  // the largest of the CTA's part: best[0 .. have)
-    if (k > 0) {
-      if (v0 >= v1) {  // a row that is no longer than its loose entries
-        if (tid < loose && loose_value > kNegInf) push(loose_value, my_loose);
+    cluster_sync();
+    if (part == 0) {
+      if (wid == 0) {
+        st = Stats{kNegInf, 0.f, 0.f};
+        for (int i = 0; i < parts; ++i) {
+          Stats o;
+          o.m = peer_float(&sm.part.m, i); o.l = peer_float(&sm.part.l, i); o.s = peer_float(&sm.part.s, i);
+          st = stats_join(st, o);
+        }
+      }
+      if (k > 0) {
+        Key mine = 0;
+        if (tid < parts * k) sm.join[tid] = mine = peer_key(&sm.best[tid % k], tid / k);
         __syncthreads();
-      }
-      least = value_of(sm.common);
-      have = finish<T>(sm, k, least, p, loose, my_loose, vocab, warps);
-    }
-
-    if (wid == 0) {
-      st = lane < warps ? sm.stats[lane] : Stats{kNegInf, 0.f, 0.f};
-#pragma unroll
-      for (int d = kMaxThreads / 64; d > 0; d >>= 1) {
-        Stats o;
-        o.m = __shfl_xor_sync(0xffffffffu, st.m, d);
-        o.l = __shfl_xor_sync(0xffffffffu, st.l, d);
-        o.s = __shfl_xor_sync(0xffffffffu, st.s, d);
-        st = stats_join(st, o);
-      }
-      st.m = __shfl_sync(0xffffffffu, st.m, 0);
-      st.l = __shfl_sync(0xffffffffu, st.l, 0);
-      st.s = __shfl_sync(0xffffffffu, st.s, 0);
-    }
-    if (parts > 1) {
-      if (tid == 0) sm.part = st;
-      for (int i = have + tid; i < k; i += threads) sm.best[i] = 0;
-      __syncthreads();
-      cluster_sync();
-      if (part == 0) {
-        if (wid == 0) {
-          st = Stats{kNegInf, 0.f, 0.f};
-          for (int i = 0; i < parts; ++i) {
-            Stats o;
-            o.m = peer_float(&sm.part.m, i); o.l = peer_float(&sm.part.l, i); o.s = peer_float(&sm.part.s, i);
-            st = stats_join(st, o);
-          }
-        }
-        if (k > 0) {
-          Key mine = 0;
-          if (tid < parts * k) sm.join[tid] = mine = peer_key(&sm.best[tid % k], tid / k);
-          __syncthreads();
-          int above = 0;
-          if (mine != 0)
-            for (int j = 0; j < parts * k; ++j) above += sm.join[j] > mine;
-          __syncthreads();
-          if (mine != 0 && above < k) sm.list[above] = mine;  // (not to best, which the others may still read)
-        }
-      }
-      __syncthreads();
-      cluster_sync();  // nobody leaves while its shared memory is read
-    }
-    if (wid == 0 && part == 0) {
-      // l is NaN where a logit is; nothing but minus infinity leaves l = 0
-      if (st.m == -kNegInf) st.l = kNan;
-      // (log probabilities relative to m: lse itself may be too large to hold ln l)
-      const float log_sum = logf(st.l), lse = st.l == 0.f ? kNegInf : st.m + log_sum;
-      auto of = [&](float v) { return lse == kNegInf ? lse : (fabsf(v) < kFar ? diff(v, st.m) * kLn2 : v - st.m) - log_sum; };
-      if (lane == 0) {
-        if (logprob != nullptr) logprob[row] = token == -1 ? 0.f : token < 0 || token >= vocab ? kNan : of(given);
-        if (entropy != nullptr) entropy[row] = st.l == 0.f ? 0.f : log_sum - kLn2 * (st.s / st.l);
-        if (lse_out != nullptr) lse_out[row] = lse;
-      }
-      if (lane < k) {
-        const Key key = (parts > 1 ? sm.list : sm.best)[lane];
-        if (top_ids != nullptr) top_ids[row * k + lane] = (int32_t)~(uint32_t)key;
-        if (top_logprobs != nullptr) top_logprobs[row * k + lane] = of(value_of((uint32_t)(key >> 32)));
+        int above = 0;
+        if (mine != 0)
+          for (int j = 0; j < parts * k; ++j) above += sm.join[j] > mine;
+        __syncthreads();
+        if (mine != 0 && above < k) sm.list[above] = mine;  // (not to best, which the others may still read)
       }
     }
-    if (__syncthreads_or(!ok)) break;
+    __syncthreads();
+    cluster_sync();  // nobody leaves while its shared memory is read
+  }
+  if (wid == 0 && part == 0) {
+    // l is NaN where a logit is; nothing but minus infinity leaves l = 0
+    if (st.m == -kNegInf) st.l = kNan;
+    // (log probabilities relative to m: lse itself may be too large to hold ln l)
+    const float log_sum = logf(st.l), lse = st.l == 0.f ? kNegInf : st.m + log_sum;
+    auto of = [&](float v) { return lse == kNegInf ? lse : (fabsf(v) < kFar ? diff(v, st.m) * kLn2 : v - st.m) - log_sum; };
+    if (lane == 0) {
+      if (logprob != nullptr) logprob[row] = token == -1 ? 0.f : token < 0 || token >= vocab ? kNan : of(given);
+      if (entropy != nullptr) entropy[row] = st.l == 0.f ? 0.f : log_sum - kLn2 * (st.s / st.l);
+      if (lse_out != nullptr) lse_out[row] = lse;
+    }
+    if (lane < k) {
+      const Key key = (parts > 1 ? sm.list : sm.best)[lane];
+      if (top_ids != nullptr) top_ids[row * k + lane] = (int32_t)~(uint32_t)key;
+      if (top_logprobs != nullptr) top_logprobs[row * k + lane] = of(value_of((uint32_t)(key >> 32)));
+    }
   }
   if (lane == 0)  // where it gave up, its copies on the way land before the memory is another's
     for (uint32_t i = taken < brought ? taken : brought; i < brought; ++i) mbar_drain(&sm.full[wid][i % kStages], (i / kStages) & 1u, status);
@@ -687,9 +669,9 @@ int launch_token_logprobs(const void* logits, int fp32, int64_t stride, int rows
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = parts > 1 ? 1 : 0;
-  const cudaError_t e = fp32 ? cudaLaunchKernelEx(&cfg, k_token_logprobs<float>, (const float*)logits, stride, rows, vocab, parts, tokens, top, logprob,
+  const cudaError_t e = fp32 ? cudaLaunchKernelEx(&cfg, k_token_logprobs<float>, (const float*)logits, stride, vocab, parts, tokens, top, logprob,
                                                   entropy, lse, top_ids, top_logprobs, status)
-                             : cudaLaunchKernelEx(&cfg, k_token_logprobs<__nv_bfloat16>, (const __nv_bfloat16*)logits, stride, rows, vocab, parts, tokens,
+                             : cudaLaunchKernelEx(&cfg, k_token_logprobs<__nv_bfloat16>, (const __nv_bfloat16*)logits, stride, vocab, parts, tokens,
                                                   top, logprob, entropy, lse, top_ids, top_logprobs, status);
   return e == cudaSuccess ? 1 : -1;
 }
