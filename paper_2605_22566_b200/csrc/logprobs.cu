@@ -4,8 +4,8 @@
 // row (both relative to m, and moved when m does); then lse = m + ln l and the entropy, sum p (lse - x), is
 // ln 2 (log2 l - s / l): no second pass, and no difference of large numbers where one token has nearly everything.
 // d is x log2 e - c in one fused step, two entries at a time; c, m log2 e rounded, is what all of a row's d are relative to, so
-// its rounding cancels.  Where that would overflow (a largest logit beyond 1e38) d is (x - m) log2 e.  Masked entries' d, minus
-// infinity, is held to -1000, so that its product with p = 0 is a number.
+// its rounding cancels.  Where that rounding is no small number (a largest logit beyond 1e6) d is (x - m) log2 e.
+// Masked entries are held to -1.2e38, so that d and its product with p = 0 are numbers.
 //
 // The k most likely: where n warps of a CTA each have m lanes whose largest logit so far reaches t, n m logits do, so with n m > k
 // nothing below t can be among them.  The warps tell each other these levels (m lanes') through shared memory, with no barrier (a
@@ -67,26 +67,34 @@ __device__ __forceinline__ float value_of(uint32_t order) {
 }
 __device__ __forceinline__ Key key_of(float x, int64_t index) { return (Key)order_of(x) << 32 | (uint32_t)~(uint32_t)index; }
 
-constexpr float kFar = 1e38f, kLag = 4.f;
+constexpr float kFar = 1e6f, kLag = 4.f;
 
 // (x - m) log2 e, relative to the same c wherever |m| is not far.
 __device__ __forceinline__ float diff(float x, float m) { return fabsf(m) < kFar ? fmaf(x, kLog2e, -(m * kLog2e)) : (x - m) * kLog2e; }
 
 __device__ __forceinline__ void stats_move(Stats& a, float m) {  // to the reference m >= a.m
   if (a.m != kNegInf) {
-    const float d = fabsf(a.m) < kFar && fabsf(m) < kFar ? a.m * kLog2e - m * kLog2e : (a.m - m) * kLog2e;
+    // (what a reference stands for is its c where it is not far, itself times log2 e where it is)
+    const bool near_a = fabsf(a.m) < kFar, near_m = fabsf(m) < kFar;
+    const float ca = __fmul_rn(a.m, kLog2e), cm = __fmul_rn(m, kLog2e);
+    const float d = near_a ? (near_m ? ca - cm : fmaf(-m, kLog2e, ca)) : near_m ? fmaf(a.m, kLog2e, -cm) : (a.m - m) * kLog2e;
     const float e = fmaxf(d, -1000.f), f = fast_exp2(e);
     a.s = f * (a.s + a.l * e);
     a.l *= f;
   }
   a.m = m;
 }
-__device__ __forceinline__ Stats stats_join(Stats a, Stats b) {
-  const float m = fmaxf(a.m, b.m);
+// The sum over a warp's lanes, in all of them: to the largest reference first.
+__device__ __forceinline__ Stats stats_sum(Stats a) {
+  float m = a.m;
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
   if (a.m < m) stats_move(a, m);
-  if (b.m < m) stats_move(b, m);
-  a.l += b.l;
-  a.s += b.s;
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) {
+    a.l += __shfl_xor_sync(0xffffffffu, a.l, d);
+    a.s += __shfl_xor_sync(0xffffffffu, a.s, d);
+  }
   return a;
 }
 // The larger one, NaN if either is.
@@ -127,6 +135,10 @@ template <> struct Vec<float> {
     return top;
   }
   static __device__ __forceinline__ float one(const float* p) { return *p; }
+  static __device__ __forceinline__ uint32_t held(uint32_t w) {
+    return __float_as_uint(max_nan(__uint_as_float(w), -1.2e38f));
+  }
+  static __device__ __forceinline__ uint4 held(uint4 v) { return make_uint4(held(v.x), held(v.y), held(v.z), held(v.w)); }
 };
 template <> struct Vec<__nv_bfloat16> {
   static constexpr int n = 8;
@@ -156,6 +168,12 @@ template <> struct Vec<__nv_bfloat16> {
     return fmaxf(__low2float(t), __high2float(t));
   }
   static __device__ __forceinline__ float one(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+  static __device__ __forceinline__ uint32_t held(uint32_t w) {
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0xfeb4feb4u));  // -1.2e38
+    return r;
+  }
+  static __device__ __forceinline__ uint4 held(uint4 v) { return make_uint4(held(v.x), held(v.y), held(v.z), held(v.w)); }
 };
 
 // The k largest of the list's first n keys to its front, in descending order.  All threads; n is theirs alike.
@@ -520,9 +538,38 @@ __global__ void __launch_bounds__(kMaxThreads, 3) k_token_logprobs(const T* __re
       }
       if (round == 0 && loose_value > least) push(loose_value, my_loose);
     }
-    if (__all_sync(0xffffffffu, fabsf(st.m) < kFar || st.m == kNegInf)) {
+    bool near = __all_sync(0xffffffffu, fabsf(st.m) < kFar || st.m == kNegInf);
+    if (!near) {  // (lanes that have seen nothing but a mask's low values: the largest of the warp will do for them)
+      float m = seen;
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+      near = fabsf(m) < kFar;
+      if (near && st.m < m) {
+        fold();
+        stats_move(st, m);
+      }
+    }
+    if (near) {
       const float c = st.m == kNegInf ? 0.f : -(st.m * kLog2e);  // (no logit with a probability yet: any reference will do)
       const uint64_t cc = f2_pack(c, c), ee = f2_pack(kLog2e, kLog2e);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        float e[kN];
+        Vec<T>::get(Vec<T>::held(raw[u]), e);
+#pragma unroll
+        for (int i = 0; i < kN; i += 2) {
+          const uint64_t d2 = f2_fma(f2_pack(e[i], e[i + 1]), ee, cc);
+          float d0, d1;
+          f2_unpack(d2, d0, d1);
+          const uint64_t p2 = f2_pack(fast_exp2(d0), fast_exp2(d1));
+          l2 = f2_add(l2, p2);
+          s2 = f2_fma(p2, d2, s2);
+        }
+      }
+    } else {
+      const bool far = fabsf(st.m) >= kFar && st.m != kNegInf;
+      const float m = far ? -st.m : 0.f, c = far || st.m == kNegInf ? 0.f : -(st.m * kLog2e);
+      const uint64_t mm = f2_pack(m, m), cc = f2_pack(c, c), ee = f2_pack(kLog2e, kLog2e);
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
         float e[kN];
@@ -530,7 +577,7 @@ __global__ void __launch_bounds__(kMaxThreads, 3) k_token_logprobs(const T* __re
 #pragma unroll
         for (int i = 0; i < kN; i += 2) {
           float d0, d1;
-          f2_unpack(f2_fma(f2_pack(e[i], e[i + 1]), ee, cc), d0, d1);
+          f2_unpack(f2_fma(f2_add(f2_pack(e[i], e[i + 1]), mm), ee, cc), d0, d1);
           d0 = max_nan(d0, -1000.f);
           d1 = max_nan(d1, -1000.f);
           const uint64_t p2 = f2_pack(fast_exp2(d0), fast_exp2(d1));
@@ -538,11 +585,6 @@ __global__ void __launch_bounds__(kMaxThreads, 3) k_token_logprobs(const T* __re
           s2 = f2_fma(p2, f2_pack(d0, d1), s2);
         }
       }
-    } else {
-#pragma unroll 1
-      for (int v = lane; v < end - begin; v += 32)
-#pragma unroll 1
-        for (int i = 0; i < kN; ++i) stats_add(st, Vec<T>::one(reinterpret_cast<const T*>(piece + v) + i));
     }
     if (k > 0) {
       // a lane that has a logit above the least: the warp looks at its entries, 32 words of them
@@ -561,14 +603,7 @@ __global__ void __launch_bounds__(kMaxThreads, 3) k_token_logprobs(const T* __re
     if (lane == 0 && ok && begin < v1) bring();
   }
   fold();
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) {
-    Stats o;
-    o.m = __shfl_xor_sync(0xffffffffu, st.m, d);
-    o.l = __shfl_xor_sync(0xffffffffu, st.l, d);
-    o.s = __shfl_xor_sync(0xffffffffu, st.s, d);
-    st = stats_join(st, o);
-  }
+  st = stats_sum(st);
   if (lane == 0) sm.stats[wid] = st;
   __syncthreads();
   int have = 0;  // the largest of the CTA's part: best[0 .. have)
@@ -582,18 +617,7 @@ __global__ void __launch_bounds__(kMaxThreads, 3) k_token_logprobs(const T* __re
   }
 
   if (wid == 0) {
-    st = lane < warps ? sm.stats[lane] : Stats{kNegInf, 0.f, 0.f};
-#pragma unroll
-    for (int d = kMaxThreads / 64; d > 0; d >>= 1) {
-      Stats o;
-      o.m = __shfl_xor_sync(0xffffffffu, st.m, d);
-      o.l = __shfl_xor_sync(0xffffffffu, st.l, d);
-      o.s = __shfl_xor_sync(0xffffffffu, st.s, d);
-      st = stats_join(st, o);
-    }
-    st.m = __shfl_sync(0xffffffffu, st.m, 0);
-    st.l = __shfl_sync(0xffffffffu, st.l, 0);
-    st.s = __shfl_sync(0xffffffffu, st.s, 0);
+    st = stats_sum(lane < warps ? sm.stats[lane] : Stats{kNegInf, 0.f, 0.f});
   }
   if (parts > 1) {
     if (tid == 0) sm.part = st;
@@ -603,11 +627,12 @@ __global__ void __launch_bounds__(kMaxThreads, 3) k_token_logprobs(const T* __re
     if (part == 0) {
       if (wid == 0) {
         st = Stats{kNegInf, 0.f, 0.f};
-        for (int i = 0; i < parts; ++i) {
-          Stats o;
-          o.m = peer_float(&sm.part.m, i); o.l = peer_float(&sm.part.l, i); o.s = peer_float(&sm.part.s, i);
-          st = stats_join(st, o);
+        if (lane < parts) {
+          st.m = peer_float(&sm.part.m, lane);
+          st.l = peer_float(&sm.part.l, lane);
+          st.s = peer_float(&sm.part.s, lane);
         }
+        st = stats_sum(st);
       }
       if (k > 0) {
         Key mine = 0;

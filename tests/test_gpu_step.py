@@ -496,6 +496,8 @@ def _check_logprobs(got, x, tokens, top):
         spread = float((p * (np.minimum(d, 1e3) + 1) ** 2).sum()) + 4
 
         def near(a, b, t):
+            if math.isfinite(b) and abs(b) >= 2.0 ** 128 - 2.0 ** 103:     # (half a step beyond fp32's largest: rounded, it is an infinity)
+                b = math.copysign(math.inf, b)
             return (math.isnan(a) and math.isnan(b)) or a == b or abs(a - b) <= t
         assert near(float(got.lse[r]), lse, tol), (r, float(got.lse[r]), lse, tol)
         if tokens is not None:
@@ -575,6 +577,45 @@ def test_logprobs_values_where_they_can_go_wrong(v, dtype):
     got = pa.token_logprobs(x, tokens, top)
     _check_logprobs(got, x, tokens, top)
     assert all(torch.equal(a.nan_to_num(7.0), b.nan_to_num(7.0)) for a, b in zip(got, pa.token_logprobs(x, tokens, top)))
+    pa.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("v", [9, 300, 20003])
+def test_logprobs_where_differences_pass_the_range_of_fp32(v, dtype):
+    """Largest logits on either side of 1e38, the others at the ends of the range, with masked ones among them."""
+    rng = np.random.default_rng(v)
+    pa = _pa()
+    ends = np.array([-3.38e38, -1.3e38, -1.21e38, -1.19e38, -1e38, -math.inf])
+    tops = [-1.01e38, -9.9e37, -9e37, 0.0, 9e37, 9.9e37, 1.01e38, 3.38e38]
+    x = rng.choice(ends, (len(tops), v))
+    for r, top in enumerate(tops):
+        x[r] = np.minimum(x[r], top)
+        x[r, rng.integers(0, v, 3)] = top
+    x = torch.from_numpy(x).to(dtype).cuda()
+    tokens = _ints(*rng.integers(0, v, len(tops)).tolist())
+    _check_logprobs(pa.token_logprobs(x, tokens, 7), x, tokens, 7)
+    assert pa.status() == 0
+    pa.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("v", [61, 2500, 40009])
+def test_logprobs_of_large_logits_and_finite_masks(v, dtype):
+    """Logits far from zero and close to each other, on either side of where differences are formed in another way; rows of which a finite mask
+    leaves a few entries, one, or none."""
+    rng = np.random.default_rng(v)
+    pa = _pa()
+    rows = [base + rng.standard_normal(v) * 3 for base in (-3e6, -1e6, -1e3, 4e3, 9.99995e5, 1e6, 1.00001e6, 5e7, 2e12)]
+    for mask in (-1e4, -65504.0, -1e9, -1e30, float(torch.finfo(dtype).min)):
+        for left in (v // 20, 3, 1, 0):
+            row = np.full(v, mask)
+            row[rng.permutation(v)[:left]] = rng.standard_normal(left) * 3
+            rows.append(row)
+    x = torch.from_numpy(np.stack(rows)).to(dtype).cuda()
+    tokens = _ints(*x.argmax(1).tolist())
+    _check_logprobs(pa.token_logprobs(x, tokens, 5), x, tokens, 5)
+    assert pa.status() == 0
     pa.close()
 
 
