@@ -180,6 +180,23 @@ __device__ __forceinline__ void store_y(const ProjectArgs& a, int row, int feat,
   }
 }
 
+// A feature's results for kGroup rows from `row` on.
+__device__ __forceinline__ void store_rows(const ProjectArgs& a, int row, int feat, const uint32_t (&r)[kGroup]) {
+  const int64_t at = (int64_t)row * a.y_stride + feat;
+  const int n = min(kGroup, a.rows - row);
+  if (a.y_fp32) {
+    float* y = static_cast<float*>(a.y) + at;
+#pragma unroll
+    for (int j = 0; j < kGroup; ++j, y += a.y_stride)
+      if (j < n) *y = __uint_as_float(r[j]);
+  } else {
+    __nv_bfloat16* y = static_cast<__nv_bfloat16*>(a.y) + at;
+#pragma unroll
+    for (int j = 0; j < kGroup; ++j, y += a.y_stride)
+      if (j < n) *y = __float2bfloat16_rn(__uint_as_float(r[j]));
+  }
+}
+
 // (a warp's lanes together; every warp of every CTA of the cluster takes part in each barrier)
 __device__ __forceinline__ void cluster_sync_all() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -222,12 +239,19 @@ __device__ __forceinline__ __nv_bfloat16 take_number(float& v) {
   v = fabsf(v) <= 3.3895e38f ? v - __bfloat162float(n) : 0.f;
   return n;
 }
-// One result, or four of neighbouring ranks, of a row; zeros where the row is another slot's.
-__device__ __forceinline__ void store_h(const Slots& sl, const HPlace& p, int row_in_tile, int row_slot, float v) {
-  if (p.at == nullptr) return;
-  v = row_slot == p.slot && p.r < sl.rank ? v * p.scale : 0.f;
+// A rank's results for kGroup neighbouring rows (there is room for a whole tile of them), or those of four neighbouring ranks for one
+// row; zeros where the row is another slot's.
+__device__ __forceinline__ void store_h(const Slots& sl, const HPlace& p, int row_in_tile, float (&v)[kGroup]) {
   char* at = p.at + (row_in_tile * sl.padded + p.r) * 2;
-  for (int i = 0; i < sl.numbers; ++i) *reinterpret_cast<__nv_bfloat16*>(at + i * sl.block) = take_number(v);
+  const int step = sl.padded * 2;
+  const bool mine = p.r < sl.rank;
+  __nv_bfloat16 n[kGroup];
+  for (int i = 0; i < sl.numbers; ++i) {
+#pragma unroll
+    for (int j = 0; j < kGroup; ++j) n[j] = mine ? take_number(v[j]) : __float2bfloat16_rn(0.f);
+#pragma unroll
+    for (int j = 0; j < kGroup; ++j) *reinterpret_cast<__nv_bfloat16*>(at + i * sl.block + j * step) = n[j];
+  }
 }
 __device__ __forceinline__ void store_h4(const Slots& sl, const HPlace& p, int row_in_tile, int row_slot, float4 v) {
   if (p.at == nullptr) return;
@@ -602,21 +626,36 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
           wait_sums();
         }
         if (!ok || a.splits > 1) break;  // (joined below, by the whole cluster)
-        auto take = [&](auto&& store) {
-          for (int g = 0; g < cols && t0 + col0 + g < a.rows; g += kGroup) {
+        auto take = [&](auto&& store) {  // a group of rows at a time, from row g on
+          for (int g = col0; g < col0 + cols && t0 + g < a.rows; g += kGroup) {
             uint32_t r[kGroup];
-            tmem_ld8(from + g, r);
+            tmem_ld8(from + (g - col0), r);
             tmem_wait_ld();
-#pragma unroll
-            for (int j = 0; j < kGroup; ++j) store(col0 + g + j, __uint_as_float(r[j]));
+            store(g, r);
           }
           if (!kExact) sums_taken();
         };
         if (kMode == kDown) {
+          // (a row's slot is asked for by a lane, 32 rows at a time and as many ahead: a load among every row's stores took 300 ns a row)
           const HPlace place(sl, row_tile, f * per_tile, t.slots, m);
-          take([&](int r, float v) { if (t0 + r < a.rows) store_h(sl, place, r, __ldcg(sl.of_row + t0 + r), v); });
+          auto slot_at = [&](int r) { return t0 + r + lane < a.rows ? __ldcg(sl.of_row + t0 + r + lane) : -1; };
+          int next = slot_at(col0), here = 0;
+          take([&](int g, const uint32_t (&r)[kGroup]) {
+            const int i = (g - col0) & 31;
+            if (i == 0) {
+              here = next;
+              next = slot_at(g + 32);
+            }
+            float v[kGroup];
+#pragma unroll
+            for (int j = 0; j < kGroup; ++j) v[j] = __shfl_sync(0xffffffffu, here, i + j) == place.slot ? __uint_as_float(r[j]) * place.scale : 0.f;
+            if (place.at != nullptr) store_h(sl, place, g, v);
+          });
         } else {
-          take([&](int r, float v) { store_y(a, t0 + r, f * kTileFeat + half * kFeat + m, v); });
+          const int feat = f * kTileFeat + half * kFeat + m;
+          take([&](int g, const uint32_t (&r)[kGroup]) {
+            if (feat < a.out_dim) store_rows(a, t0 + g, feat, r);
+          });
         }
       }
     }
