@@ -239,21 +239,8 @@ __device__ __forceinline__ __nv_bfloat16 take_number(float& v) {
   v = fabsf(v) <= 3.3895e38f ? v - __bfloat162float(n) : 0.f;
   return n;
 }
-// A rank's results for kGroup neighbouring rows (there is room for a whole tile of them), or those of four neighbouring ranks for one
-// row; zeros where the row is another slot's.
-__device__ __forceinline__ void store_h(const Slots& sl, const HPlace& p, int row_in_tile, float (&v)[kGroup]) {
-  char* at = p.at + (row_in_tile * sl.padded + p.r) * 2;
-  const int step = sl.padded * 2;
-  const bool mine = p.r < sl.rank;
-  __nv_bfloat16 n[kGroup];
-  for (int i = 0; i < sl.numbers; ++i) {
-#pragma unroll
-    for (int j = 0; j < kGroup; ++j) n[j] = mine ? take_number(v[j]) : __float2bfloat16_rn(0.f);
-#pragma unroll
-    for (int j = 0; j < kGroup; ++j) *reinterpret_cast<__nv_bfloat16*>(at + i * sl.block + j * step) = n[j];
-  }
-}
-__device__ __forceinline__ void store_h4(const Slots& sl, const HPlace& p, int row_in_tile, int row_slot, float4 v) {
+// Four results of neighbouring ranks of a row; zeros where the row is another slot's.
+__device__ __forceinline__ void store_h(const Slots& sl, const HPlace& p, int row_in_tile, int row_slot, float4 v) {
   if (p.at == nullptr) return;
   const bool mine = row_slot == p.slot && p.r < sl.rank;  // (ranks are multiples of 8)
   v.x = mine ? v.x * p.scale : 0.f;
@@ -284,13 +271,15 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
   extern __shared__ __align__(1024) char smem_raw[];
   char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   const uint32_t w_bytes = kFeat * 128u, x_bytes = (uint32_t)a.nt / kCtas * 128u, stage_bytes = w_bytes + x_bytes;
-  const uint32_t ring = max(stage_bytes * a.stages, a.splits > 1 ? (uint32_t)a.nt * kFeat * 4u : 0u);
+  const bool rounds = kMode == kDown || a.splits > 1;  // the results leave through shared memory, a tile at a time
+  const uint32_t ring = max(stage_bytes * a.stages, rounds ? (uint32_t)a.nt * kFeat * 4u : 0u);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + ring);
   uint64_t* empty = full + a.stages;
   uint64_t* acc_full = empty + a.stages;
   uint64_t* acc_empty = acc_full + 2;
   uint64_t* drained = acc_empty + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drained + 1);
+  uint32_t* gave_up = tmem_slot + 1;  // the CTA has; what a cluster does next goes by those of all its CTAs, so that none leaves alone
   const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31;
   const int size = a.splits * kCtas;  // of a cluster
   const int group = blockIdx.x / size, groups = gridDim.x / size, rank = blockIdx.x - group * size, part = rank / kCtas, half = rank - part * kCtas;
@@ -298,7 +287,7 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
   const uint16_t both = (uint16_t)(3u << (part * kCtas));
   const int tiles = a.feat_tiles * a.row_tiles;
   const int steps_all = (a.in_dim + kStep - 1) / kStep;
-  const int step0 = (int)((int64_t)steps_all * part / a.splits), step1 = (int)((int64_t)steps_all * (part + 1) / a.splits);
+  int step0 = (int)((int64_t)steps_all * part / a.splits), step1 = (int)((int64_t)steps_all * (part + 1) / a.splits);
   const Slots& sl = a.slots;
   const int h_row = sl.padded * 2;                       // bytes of a row of h, and of B's
   const uint32_t b_bytes = kFeat * (uint32_t)h_row, h_bytes = sl.block / kCtas;  // of a slot's B, of a number of its h
@@ -337,6 +326,7 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
     for (int i = 0; i < a.stages; ++i) { mbar_init(full + i, a.pair); mbar_init(empty + i, 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(acc_full + i, 1); mbar_init(acc_empty + i, kTakers * kCtas); }
     mbar_init(drained, 1);
+    *gave_up = 0;
     mbar_fence_init();
   }
   if (wid == 1) tmem_take<kTwo>(tmem_slot, a.tmem_cols);
@@ -373,10 +363,22 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
   // a warp that takes sums out: row m of the tile of W, columns col0 .. col0 + cols (rows of x)
   const int m = (wid & 3) * 32 + lane, cols = kTakers == 8 ? a.nt / 2 : a.nt, col0 = kTakers == 8 && wid >= 8 ? cols : 0;
   const uint32_t lanes = tmem + ((uint32_t)((wid & 3) * 32) << 16);
-  // A CTA by itself goes through its tiles in one round, so that the roles run ahead of each other; a cluster takes a round per tile.
+  // W x of a CTA by itself goes through its tiles in one round, so that the roles run ahead of each other.  A cluster takes a round per tile, and
+  // so does A x, whose results are short pieces for places far apart (stored as they come from tensor memory: 31 us for 256 rows).
   Tile now = start();
   while (more(now)) {
-    if (wid == 0) {
+    // A x: where there are more than half as many tiles left in a tile of x as the cluster has CTAs, they take one each, with all of K.
+    bool whole = false, idle = false;
+    if (kMode == kDown) {
+      const int left = ((now.slots + per_tile - 1) / per_tile - now.f + f_step - 1) / f_step;
+      whole = 2 * left > a.splits;
+      idle = whole && part >= left;
+      step0 = whole ? 0 : steps_all * part / a.splits;
+      step1 = whole ? steps_all : steps_all * (part + 1) / a.splits;
+      if (whole) now.f += part * f_step;
+    }
+    if (idle) {
+    } else if (wid == 0) {
       if (lane == 0) {
         // (the leader passes on to the other CTA what it has waited for)
         auto free = [&] {
@@ -451,7 +453,7 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
             if (leader) mbar_arrive(full + (s >> odd));
             next();
           }
-          if (a.splits > 1) break;
+          if (rounds) break;
         }
         // nothing of its own is on the way when it leaves, also where it gave up
         for (int i = 0; i < a.stages && leader; i += a.pair)
@@ -572,7 +574,7 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
           }
           commit_both<kTwo>(acc_full + acc_at(), both);
           ++done;
-          if (a.splits > 1) break;
+          if (rounds) break;
         }
         if (!ok) {  // (otherwise the tiles' own waits have seen the last of them)
           commit<kTwo>(drained);
@@ -625,49 +627,27 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
         } else {
           wait_sums();
         }
-        if (!ok || a.splits > 1) break;  // (joined below, by the whole cluster)
-        auto take = [&](auto&& store) {  // a group of rows at a time, from row g on
-          for (int g = col0; g < col0 + cols && t0 + g < a.rows; g += kGroup) {
-            uint32_t r[kGroup];
-            tmem_ld8(from + (g - col0), r);
-            tmem_wait_ld();
-            store(g, r);
-          }
-          if (!kExact) sums_taken();
-        };
-        if (kMode == kDown) {
-          // (a row's slot is asked for by a lane, 32 rows at a time and as many ahead: a load among every row's stores took 300 ns a row)
-          const HPlace place(sl, row_tile, f * per_tile, t.slots, m);
-          auto slot_at = [&](int r) { return t0 + r + lane < a.rows ? __ldcg(sl.of_row + t0 + r + lane) : -1; };
-          int next = slot_at(col0), here = 0;
-          take([&](int g, const uint32_t (&r)[kGroup]) {
-            const int i = (g - col0) & 31;
-            if (i == 0) {
-              here = next;
-              next = slot_at(g + 32);
-            }
-            float v[kGroup];
-#pragma unroll
-            for (int j = 0; j < kGroup; ++j) v[j] = __shfl_sync(0xffffffffu, here, i + j) == place.slot ? __uint_as_float(r[j]) * place.scale : 0.f;
-            if (place.at != nullptr) store_h(sl, place, g, v);
-          });
-        } else {
-          const int feat = f * kTileFeat + half * kFeat + m;
-          take([&](int g, const uint32_t (&r)[kGroup]) {
-            if (feat < a.out_dim) store_rows(a, t0 + g, feat, r);
-          });
+        if (!ok || rounds) break;  // (joined below, by the whole cluster)
+        const int feat = f * kTileFeat + half * kFeat + m;
+        for (int g = col0; g < col0 + cols && t0 + g < a.rows; g += kGroup) {
+          uint32_t r[kGroup];
+          tmem_ld8(from + (g - col0), r);
+          tmem_wait_ld();
+          if (feat < a.out_dim) store_rows(a, t0 + g, feat, r);
         }
+        if (!kExact) sums_taken();
       }
     }
     __syncwarp();
-    if (a.splits == 1) break;
+    if (!rounds) break;
     {
       // The parts go to shared memory (the ring's: the tile's last MMA is done), [row of x][feature], and row r is joined by CTA r mod
-      // splits, a warp a row, 16 reads on the way.  (Parts written to the CTA that joins them took 30 us where this takes 20, with 256 rows.)
-      const int f = now.f, row_tile = now.r, t0 = row_tile * a.nt, n = min(a.nt, a.rows - t0);
+      // splits (its own, where it has all of K), a warp a row, 16 reads on the way.  (Parts written to the CTA that joins them took 30 us where this takes 20, with 256 rows.)
+      const int f = now.f, row_tile = now.r, t0 = row_tile * a.nt, n = idle ? 0 : min(a.nt, a.rows - t0);
+      const int first = whole ? part : 0, joined = whole ? 1 : a.splits, mine = whole ? 0 : part;  // the parts of its rows, and which are its
       const HPlace place = kMode == kDown ? HPlace(sl, row_tile, f * per_tile, now.slots, lane * 4) : HPlace();
       float* parts = reinterpret_cast<float*>(smem);
-      if (wid >= 4) {
+      if (wid >= 4 && !idle) {
         const uint32_t from = lanes + (kExact ? a.sum_cols : acc_at() * a.acc_cols) + col0;
         for (int g = 0; g < cols; g += kGroup) {
           uint32_t r[kGroup];
@@ -683,11 +663,14 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
           ++done;
         }
       }
+      if (!ok) *gave_up = 1;
       __syncwarp();
       cluster_sync_all();
-      constexpr int kRows = 4, kParts = 4;  // of a warp on the way
-      const int apart = a.splits * kWarps;
-      for (int r0 = part + a.splits * wid; r0 < n; r0 += apart * kRows) {
+      uint32_t stop = 0;
+      if (tid < size) asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(stop) : "r"(at_rank(gave_up, tid)) : "memory");
+      constexpr int kRows = kMode == kDown ? 2 : 4, kParts = 4;  // of a warp on the way
+      const int apart = joined * kWarps;
+      for (int r0 = mine + joined * wid; r0 < n; r0 += apart * kRows) {
         float4 sum[kRows];
         int row_slot[kRows];
 #pragma unroll
@@ -695,12 +678,12 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
           sum[i] = make_float4(0.f, 0.f, 0.f, 0.f);
           row_slot[i] = kMode == kDown ? __ldcg(sl.of_row + t0 + min(r0 + i * apart, n - 1)) : 0;
         }
-        for (int p0 = 0; p0 < a.splits; p0 += kParts) {
+        for (int p0 = 0; p0 < joined; p0 += kParts) {
           float4 x[kParts][kRows];
 #pragma unroll
           for (int p = 0; p < kParts; ++p) {
-            if (p0 + p < a.splits) {
-              const uint32_t from = at_rank(parts + lane * 4, (p0 + p) * kCtas + half);
+            if (p0 + p < joined) {
+              const uint32_t from = at_rank(parts + lane * 4, (first + p0 + p) * kCtas + half);
 #pragma unroll
               for (int i = 0; i < kRows; ++i)
                 asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];"
@@ -711,7 +694,7 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
           }
 #pragma unroll
           for (int p = 0; p < kParts; ++p)
-            if (p0 + p < a.splits) {
+            if (p0 + p < joined) {
 #pragma unroll
               for (int i = 0; i < kRows; ++i) { sum[i].x += x[p][i].x; sum[i].y += x[p][i].y; sum[i].z += x[p][i].z; sum[i].w += x[p][i].w; }
             }
@@ -720,7 +703,7 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
         for (int i = 0; i < kRows; ++i) {
           const int r = r0 + i * apart;
           if (r < n) {
-            if (kMode == kDown) store_h4(sl, place, r, row_slot[i], sum[i]);
+            if (kMode == kDown) store_h(sl, place, r, row_slot[i], sum[i]);
             else store_y4(a, t0 + r, f * kTileFeat + half * kFeat + lane * 4, sum[i]);
           }
         }
@@ -728,7 +711,8 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
       __syncwarp();
       cluster_sync_all();  // nobody leaves, or takes new stages to where its part was, while that is read
       fence_proxy_async_smem();  // (before the next round's copies to the ring)
-      if (__syncthreads_or(!ok)) break;
+      if (__syncthreads_or((int)stop)) break;
+      if (whole) now.f += (a.splits - 1 - part) * f_step;
       advance(now);
     }
   }
@@ -948,7 +932,7 @@ struct Shape {
   int ctas;
   size_t smem;
 };
-Shape shape_of(ProjectArgs& a, int64_t tiles, int num_sms) {
+Shape shape_of(ProjectArgs& a, int64_t tiles, bool rounds, int num_sms) {
   const int steps = (a.in_dim + kStep - 1) / kStep, ctas = a.two ? 2 : 1;
   const uint32_t stage_bytes = kFeat * 128u + a.nt / ctas * 128u, extra = 1024 + 512;
   // (and only where tensor memory has room for two: CTAs of clusters that wait for each other must never wait for that)
@@ -972,7 +956,7 @@ Shape shape_of(ProjectArgs& a, int64_t tiles, int num_sms) {
   a.pair = a.stages >= 6 ? 2 : 1;
   a.stages -= a.stages % a.pair;
   const int64_t groups = a.splits > 1 ? tiles : std::min<int64_t>(tiles, shared ? 2 * room_for : room_for);
-  return Shape{(int)(groups * a.splits * ctas), extra + std::max<uint32_t>(stage_bytes * a.stages, a.splits > 1 ? (uint32_t)a.nt * kFeat * 4u : 0u)};
+  return Shape{(int)(groups * a.splits * ctas), extra + std::max<uint32_t>(stage_bytes * a.stages, a.splits > 1 || rounds ? (uint32_t)a.nt * kFeat * 4u : 0u)};
 }
 
 struct Maps { CUtensorMap w, x, b, h; };
@@ -1059,7 +1043,7 @@ static int launch_pass(const gf_projection_t& p, int rows, const void* x, int64_
   Maps maps = {};
   const int x_box = a.nt / (a.two ? 2 : 1);
   if (!make_map(&maps.w, p.w_dev, 0, p.out_dim, p.in_dim, p.w_stride, kStep, kFeat) || !make_map(&maps.x, x, 0, rows, p.in_dim, x_stride, kStep, x_box)) return -1;
-  const Shape main_shape = shape_of(a, (int64_t)a.feat_tiles * a.row_tiles, num_sms);
+  const Shape main_shape = shape_of(a, (int64_t)a.feat_tiles * a.row_tiles, false, num_sms);
   if (!with) return launch_main<kPlain>(maps, a, main_shape, st);
   place_slots(&a.slots, (char*)scratch, rows, p.rank, p.num_adapters, y_fp32 ? 3 : 2);
   a.slots.scale = p.scale_dev;
@@ -1084,7 +1068,7 @@ static int launch_pass(const gf_projection_t& p, int rows, const void* x, int64_
   const int per_tile = kFeat / a.slots.padded;
   d.two = 0;
   d.feat_tiles = (a.slots.most + per_tile - 1) / per_tile;
-  Shape shape = shape_of(d, (int64_t)a.row_tiles, num_sms);
+  Shape shape = shape_of(d, (int64_t)a.row_tiles, true, num_sms);
   const int most_groups = std::max(1, num_sms * 3 / 4 / d.splits);
   int64_t down_groups = shape.ctas / d.splits;  // at most one per tile of x; more where multiprocessors are left
   if (down_groups == a.row_tiles) down_groups *= std::max<int64_t>(1, std::min<int64_t>(d.feat_tiles, most_groups / down_groups));
