@@ -668,24 +668,24 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
       cluster_sync_all();
       uint32_t stop = 0;
       if (tid < size) asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(stop) : "r"(at_rank(gave_up, tid)) : "memory");
-      constexpr int kRows = kMode == kDown ? 2 : 4, kParts = 4;  // of a warp on the way
+      constexpr int kAtOnce = kMode == kDown ? 2 : 4, kParts = 4;  // rows and parts of a warp on the way
       const int apart = joined * kWarps;
-      for (int r0 = mine + joined * wid; r0 < n; r0 += apart * kRows) {
-        float4 sum[kRows];
-        int row_slot[kRows];
+      for (int r0 = mine + joined * wid; r0 < n; r0 += apart * kAtOnce) {
+        float4 sum[kAtOnce];
+        int row_slot[kAtOnce];
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
+        for (int i = 0; i < kAtOnce; ++i) {
           sum[i] = make_float4(0.f, 0.f, 0.f, 0.f);
           row_slot[i] = kMode == kDown ? __ldcg(sl.of_row + t0 + min(r0 + i * apart, n - 1)) : 0;
         }
         for (int p0 = 0; p0 < joined; p0 += kParts) {
-          float4 x[kParts][kRows];
+          float4 x[kParts][kAtOnce];
 #pragma unroll
           for (int p = 0; p < kParts; ++p) {
             if (p0 + p < joined) {
               const uint32_t from = at_rank(parts + lane * 4, (first + p0 + p) * kCtas + half);
 #pragma unroll
-              for (int i = 0; i < kRows; ++i)
+              for (int i = 0; i < kAtOnce; ++i)
                 asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];"
                              : "=f"(x[p][i].x), "=f"(x[p][i].y), "=f"(x[p][i].z), "=f"(x[p][i].w)
                              : "r"(from + min(r0 + i * apart, n - 1) * kFeat * 4)
@@ -696,11 +696,11 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
           for (int p = 0; p < kParts; ++p)
             if (p0 + p < joined) {
 #pragma unroll
-              for (int i = 0; i < kRows; ++i) { sum[i].x += x[p][i].x; sum[i].y += x[p][i].y; sum[i].z += x[p][i].z; sum[i].w += x[p][i].w; }
+              for (int i = 0; i < kAtOnce; ++i) { sum[i].x += x[p][i].x; sum[i].y += x[p][i].y; sum[i].z += x[p][i].z; sum[i].w += x[p][i].w; }
             }
         }
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
+        for (int i = 0; i < kAtOnce; ++i) {
           const int r = r0 + i * apart;
           if (r < n) {
             if (kMode == kDown) store_h(sl, place, r, row_slot[i], sum[i]);
@@ -1006,13 +1006,46 @@ int launch_main(const Maps& maps, const ProjectArgs& a, const Shape& shape, cuda
 // Rows of x that one pass takes: more go in several, one behind the other, so that the scratch stays bounded.
 constexpr int kPassRows = 16384;
 
-int tile_rows(int rows) { return rows >= 256 ? 256 : (rows + 15) / 16 * 16; }
+// Rows of x in a tile.
+constexpr int kRows = 256, kFewerRows = 128;
+int padded_rank(int rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : 64; }
+void set_tiles(ProjectArgs& a, int nt) {
+  a.nt = nt;
+  a.two = nt == 256 && a.out_dim > kFeat;
+  const int tile_feat = kFeat * (a.two ? 2 : 1);
+  a.feat_tiles = (a.out_dim + tile_feat - 1) / tile_feat;
+  a.row_tiles = (a.rows + nt - 1) / nt;
+}
+// 256 where there are as many, unless 128 give the multiprocessors a shorter way: a stage of 256 columns takes two of them 0.39 us (fp32: 0.54), one of
+// 128 takes one 0.28 (0.31).  (4096 -> 6144: 300 rows 22.8 us with 128 and 27.7 with 256, 512 rows 39.2 and 28.2; 4096 -> 1328: 300 rows 12.1 and
+// 16.3, 1294 rows 22.5 and 27.0, 2048 rows 38.5 and 29.6; in fp32 4096 -> 6144 for 1024 rows 65.8 and 73.2, 2048 rows 122.9 and 108.3.)
+// Turns of A x beyond the first count too, 5 us (3.5) each beside their stages, as if every row named another adapter (7954 rows of 136 under 61
+// adapters of rank 64: 219 us with 256, 304 with 128).
+void choose_tiles(ProjectArgs& a, int num_adapters, int rank, int num_sms) {
+  if (a.rows < kRows) return set_tiles(a, (a.rows + 15) / 16 * 16);
+  const int steps = (a.in_dim + kStep - 1) / kStep;
+  int64_t cost[2];
+  for (int i = 0; i < 2; ++i) {
+    ProjectArgs b = a;
+    set_tiles(b, i ? kFewerRows : kRows);
+    const int64_t tiles = (int64_t)b.feat_tiles * b.row_tiles, at_once = num_sms / (b.two ? 2 : 1);
+    shape_of(b, tiles, false, num_sms);
+    const int64_t turns = b.splits > 1 ? 1 : (tiles + at_once - 1) / at_once;
+    const int64_t stage = i ? (a.y_fp32 ? 31 : 28) : (a.y_fp32 ? 54 : 39);
+    cost[i] = turns * ((steps + b.splits - 1) / b.splits) * stage;
+    if (num_adapters > 0) {
+      const int per_tile = kFeat / padded_rank(rank), most = (std::min(b.nt, num_adapters) + per_tile - 1) / per_tile;
+      cost[i] += ((int64_t)b.row_tiles * most - 1) / num_sms * (steps * stage + (i ? 350 : 500));
+    }
+  }
+  set_tiles(a, cost[1] < cost[0] ? kFewerRows : kRows);
+}
 size_t align_to(size_t n, size_t a) { return (n + a - 1) / a * a; }
 
-// Where the slots of a pass stand in the scratch; its size.
-size_t place_slots(Slots* sl, char* scratch, int rows, int rank, int num_adapters, int numbers) {
-  const int nt = tile_rows(rows), tiles = (rows + nt - 1) / nt, most = std::min(nt, num_adapters);
-  const int padded = rank <= 16 ? 16 : rank <= 32 ? 32 : 64;
+// Where the slots of a pass stand in the scratch, with tiles of nt rows; its size.
+size_t place_slots(Slots* sl, char* scratch, int rows, int nt, int rank, int num_adapters, int numbers) {
+  const int tiles = (rows + nt - 1) / nt, most = std::min(nt, num_adapters);
+  const int padded = padded_rank(rank);
   const size_t ids = align_to((size_t)tiles * 4, 128), of_row = ids + align_to((size_t)tiles * most * 4, 128), h = of_row + align_to((size_t)rows * 4, 128);
   const size_t block = (size_t)nt * padded * 2;
   if (sl) *sl = Slots{(int32_t*)scratch, (int32_t*)(scratch + ids), (int32_t*)(scratch + of_row), nullptr, scratch + h, most, numbers, rank, padded, (uint32_t)block};
@@ -1021,7 +1054,12 @@ size_t place_slots(Slots* sl, char* scratch, int rows, int rank, int num_adapter
 
 }  // namespace
 
-size_t project_scratch_bytes(int rows, int rank, int num_adapters) { return place_slots(nullptr, nullptr, std::min(rows, kPassRows), rank, num_adapters, 3); }
+// (a last pass of fewer rows needs no more than a whole one)
+size_t project_scratch_bytes(int rows, int rank, int num_adapters) {
+  rows = std::min(rows, kPassRows);
+  if (rows < kRows) return place_slots(nullptr, nullptr, rows, (rows + 15) / 16 * 16, rank, num_adapters, 3);
+  return std::max(place_slots(nullptr, nullptr, rows, kRows, rank, num_adapters, 3), place_slots(nullptr, nullptr, rows, kFewerRows, rank, num_adapters, 3));
+}
 
 static int launch_pass(const gf_projection_t& p, int rows, const void* x, int64_t x_stride, const int32_t* adapter, void* y, int64_t y_stride, int y_fp32,
                        void* scratch, int num_sms, int32_t* status, cudaStream_t st) {
@@ -1030,22 +1068,18 @@ static int launch_pass(const gf_projection_t& p, int rows, const void* x, int64_
   a.rows = rows;
   a.in_dim = p.in_dim;
   a.out_dim = p.out_dim;
-  a.nt = tile_rows(rows);
-  a.two = a.nt == 256 && p.out_dim > kFeat;
-  const int tile_feat = kFeat * (a.two ? 2 : 1);
-  a.feat_tiles = (p.out_dim + tile_feat - 1) / tile_feat;
-  a.row_tiles = (rows + a.nt - 1) / a.nt;
   a.y = y;
   a.y_stride = y_stride;
   a.y_fp32 = y_fp32;
   a.status = status;
+  choose_tiles(a, with ? p.num_adapters : 0, p.rank, num_sms);
   a.y_vec = (y_stride & 3) == 0 && ((uintptr_t)y & (y_fp32 ? 15 : 7)) == 0;
   Maps maps = {};
   const int x_box = a.nt / (a.two ? 2 : 1);
   if (!make_map(&maps.w, p.w_dev, 0, p.out_dim, p.in_dim, p.w_stride, kStep, kFeat) || !make_map(&maps.x, x, 0, rows, p.in_dim, x_stride, kStep, x_box)) return -1;
   const Shape main_shape = shape_of(a, (int64_t)a.feat_tiles * a.row_tiles, false, num_sms);
   if (!with) return launch_main<kPlain>(maps, a, main_shape, st);
-  place_slots(&a.slots, (char*)scratch, rows, p.rank, p.num_adapters, y_fp32 ? 3 : 2);
+  place_slots(&a.slots, (char*)scratch, rows, a.nt, p.rank, p.num_adapters, y_fp32 ? 3 : 2);
   a.slots.scale = p.scale_dev;
   if (!make_map(&maps.b, p.b_dev, p.num_adapters, p.out_dim, p.rank, p.rank, a.slots.padded, kFeat) ||
       !make_map(&maps.h, a.slots.h, 0, (int64_t)a.row_tiles * a.slots.most * a.slots.numbers * a.nt, a.slots.padded, a.slots.padded, a.slots.padded, x_box))

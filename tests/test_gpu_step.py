@@ -290,6 +290,8 @@ def test_projection_sizes(rows, k, n, adapters, rank, dtype):
     (2304, 72, 600, 2, 8), (2305, 128, 520, 0, 0),
     # every row its own adapter, odd numbers of slots; the ways to A x on either side of their border
     (256, 64, 300, 1000, 64), (97, 136, 200, 97, 32), (101, 64, 140, 400, 24), (592, 64, 140, 3, 32), (593, 64, 140, 3, 32), (1184, 40, 70, 9, 16), (1185, 40, 70, 9, 16),
+    # tiles of 128 rows; more tiles of adapters for a tile of x than a cluster has blocks, a few more than half, and fewer
+    (300, 1024, 700, 9, 24), (1294, 1400, 700, 46, 8), (1100, 1224, 40, 58, 8), (600, 2048, 300, 30, 64), (300, 4096, 140, 7, 32), (4500, 328, 60, 40, 64),
     # all the adapters that there may be; rows in more than one pass, the last of one row and of many
     (40, 16, 24, 32768, 8), (16385, 24, 40, 3, 8), (16384 + 300, 16, 33, 40, 16), (2 * 16384 + 5, 8, 16, 2, 8)])
 def test_projection_at_the_borders_of_its_launches(rows, k, n, adapters, rank, dtype):
