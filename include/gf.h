@@ -549,7 +549,7 @@ uint64_t gf_adapter_project_scratch_bytes(const gf_projection_t* p, int32_t rows
 /* x_dev: bf16 [rows, in_dim], rows x_stride entries apart (a multiple of 8), 16-byte aligned.  adapter_dev: int32 [rows], or NULL for
  * none at all; any value outside [-1, num_adapters) counts as -1 and gf_last_status reports GF_ERR_INVALID_ARG.  y_dev: bf16 or
  * (y_fp32 1) fp32 [rows, out_dim], rows y_stride entries apart, not overlapping the inputs.  Sums are fp32 and rounded once; the
- * order of additions is fixed for a given number of rows.  GF_ERR_CAPACITY when the scratch is too small.  Asynchronous. */
+ * order of additions is fixed for given sizes and adapters.  GF_ERR_CAPACITY when the scratch is too small.  Asynchronous. */
 gf_status_t gf_adapter_project(gf_wgraph_t* g, const gf_projection_t* p, int32_t rows, const void* x_dev, int64_t x_stride,
                                const int32_t* adapter_dev, void* y_dev, int64_t y_stride, int32_t y_fp32, void* scratch_dev,
                                uint64_t scratch_bytes, void* stream);

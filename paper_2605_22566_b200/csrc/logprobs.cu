@@ -19,6 +19,9 @@
 // (two rounds of loads into registers leave room for half the warps, and one ahead left HBM idle in between).
 //
 // A row is one CTA's, or that of a cluster, whose first CTA joins the parts through shared memory.
+//
+// Measured: 2048 rows of 128 000 bf16 logits 100.5 us, 5.2 TB/s, 64 % of the issue slots (5 instructions an entry, exponentials at half the
+// special-function unit's rate) and HBM at 80 % of a copy's; 256 rows 21 us, two rows on most multiprocessors and 44 % of the slots; one row 8.0 us, latency.
 #include <algorithm>
 
 #include "tc_device.cuh"
