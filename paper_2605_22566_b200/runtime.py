@@ -350,13 +350,12 @@ class PathAttention:
             self._refuse_ints(nodes=(nodes, "requests"), counts=(counts, "requests"), held=(held, "requests"))
         if num_new < 0:
             raise ValueError("num_new: at least 0")
-        both = nodes.new_empty((num_new + n,))
-        at = both.data_ptr()
-        st = self._lib.gf_append_slots(self.g, n, nodes.data_ptr(), None if held is None else held.data_ptr(), counts.data_ptr(), num_new, at,
-                                       at + 4 * num_new, _raw_stream(ix))
+        slots, lens = nodes.new_empty(num_new), torch.empty_like(nodes)
+        st = self._lib.gf_append_slots(self.g, n, nodes.data_ptr(), None if held is None else held.data_ptr(), counts.data_ptr(), num_new,
+                                       slots.data_ptr(), lens.data_ptr(), _raw_stream(ix))
         if st:
             B.check(st, "gf_append_slots")
-        return both.split_with_sizes((num_new, n))
+        return slots, lens
 
     def append(self, layer: int, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor) -> None:
         """gf_node_kv_append of bf16 rows [new, Hkv, D], which may be parts of wider rows (heads next to each other)."""
@@ -389,7 +388,7 @@ class PathAttention:
         if out is None:
             if dtype not in (torch.bfloat16, torch.float32):
                 raise ValueError("dtype: bf16 or fp32")
-            out = x.new_empty((rows, p.out_dim), dtype=dtype)
+            out = x.new_empty(rows, p.out_dim) if dtype is torch.bfloat16 else x.new_empty(rows, p.out_dim, dtype=dtype)
             ys = p.out_dim
         else:
             dtype = out.dtype
@@ -401,7 +400,7 @@ class PathAttention:
         scratch, nbytes = None, 0
         if adapters is not None:
             nbytes = p.scratch_bytes(rows)
-            scratch = x.new_empty((nbytes,), dtype=torch.uint8)
+            scratch = adapters.new_empty(nbytes + 3 >> 2)
         st = self._lib.gf_adapter_project(self.g, p.desc, rows, x.data_ptr(), xs[0] if rows > 1 else p.in_dim,
                                           None if adapters is None else adapters.data_ptr(), out.data_ptr(), ys, dtype is torch.float32,
                                           None if scratch is None else scratch.data_ptr(), nbytes, _raw_stream(ix))
@@ -421,9 +420,9 @@ class PathAttention:
             self._refuse_ints(tokens=(tokens, rows))
         if not 0 <= top <= min(B.GF_MAX_TOP, vocab):
             raise ValueError(f"top: 0 to {min(B.GF_MAX_TOP, vocab)}")
-        stats = logits.new_empty((3, rows), dtype=torch.float32)
+        stats = logits.new_empty(3, rows, dtype=torch.float32)
         at = stats.data_ptr()
-        top_ids, top_logprobs = logits.new_empty((rows, top), dtype=torch.int32), logits.new_empty((rows, top), dtype=torch.float32)
+        top_ids, top_logprobs = logits.new_empty(rows, top, dtype=torch.int32), stats.new_empty(rows, top)
         out = B.Logprobs(None if tokens is None else at, at + 4 * rows, at + 8 * rows, top_ids.data_ptr() if top else None,
                          top_logprobs.data_ptr() if top else None)
         st = self._lib.gf_token_logprobs(self.g, rows, vocab, logits.data_ptr(), strides[0] if rows > 1 else vocab, fp32,
