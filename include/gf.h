@@ -203,8 +203,8 @@ gf_status_t gf_node_kv_close(gf_wgraph_t* g, int32_t node, int32_t n_tokens, voi
  * slots_dev[i], [num_new], is the pool's token slot of row i, -1 for rows behind the last request's.  len_dev [num_requests],
  * or NULL: the nodes' new lengths.  A request whose node is not open, whose held or count is negative, that
  * holds more than its node, or whose rows pass num_new is left out: its slots and length are -1, its node is as it was,
- * and gf_last_status reports GF_ERR_INVALID_ARG; GF_ERR_CAPACITY where the node has no room.  Two requests must not name the
- * same node.  Built tables become stale; tables of a captured graph are built anew behind the call by its replay. */
+ * and gf_last_status reports GF_ERR_INVALID_ARG; GF_ERR_CAPACITY where the node has no room.  Of requests that name the
+ * same node all but the first are left out like that.  Built tables become stale; tables of a captured graph are built anew behind the call by its replay. */
 gf_status_t gf_append_slots(gf_wgraph_t* g, int32_t num_requests, const int32_t* node_dev, const int32_t* held_dev,
                             const int32_t* count_dev, int32_t num_new, int32_t* slots_dev, int32_t* len_dev, void* stream);
 

@@ -21,12 +21,14 @@ class OpenNodes:
 
     def append(self, nodes, held, counts, num_new, rows=None):
         """held None: all.  (slots, lengths): -1 where a request is refused.  rows: what arrives, [num_new, ...]."""
-        slots, lens, at = [-1] * num_new, [], 0
+        slots, lens, at, seen = [-1] * num_new, [], 0, set()
         for r, (v, c) in enumerate(zip(nodes, counts)):
             h = len(self.rows[v]) if held is None and v in self.rows else (0 if held is None else held[r])
             begin = at
             at += max(c, 0)
-            if v not in self.rows or c < 0 or h < 0 or h > len(self.rows[v]) or at > num_new or h + c > self.room[v]:
+            again = v in seen  # (of requests that name the same node the first one counts)
+            seen.add(v)
+            if again or v not in self.rows or c < 0 or h < 0 or h > len(self.rows[v]) or at > num_new or h + c > self.room[v]:
                 lens.append(-1)
                 continue
             del self.rows[v][h:]

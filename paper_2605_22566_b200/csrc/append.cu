@@ -35,8 +35,8 @@ __device__ void clear_rows(const PoolGeom& pool, int heads, int chunks, int from
 }
 
 // A CTA has `per` requests, one where multiprocessors are left (what taken-back tokens leave to clear is much: 131 KB a token of 32 layers with 8
-// heads): it adds up the counts of those before them (each CTA by itself: 4 bytes a request from L2, against a
-// launch or a chain of CTAs), one warp checks its requests and sets their lengths, and all threads write the slots.
+// heads): it adds up the counts of those before them and looks for its nodes among theirs (each CTA by itself: 8 bytes a request from L2, against
+// a launch or a chain of CTAs), one warp checks its requests and sets their lengths, and all threads write the slots.
 // Latency-bound: a chain of four dependent loads; with the rows' copy 3.9 us for one request, 4.6 for 256.  256 requests that take back 4 tokens of
 // 32 layers: 29 us (134 MB of zeros).
 __global__ void __launch_bounds__(kSlotThreads) k_append_slots(GraphDev g, PoolGeom pool, int layers, int heads, int chunks, int num_requests, int per,
@@ -46,12 +46,32 @@ __global__ void __launch_bounds__(kSlotThreads) k_append_slots(GraphDev g, PoolG
   __shared__ long long warp_sums[kSlotThreads / 32];
   __shared__ int s_begin[kSlotRequests + 1], s_slot[kSlotRequests], s_from[kSlotRequests], s_to[kSlotRequests];
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  __shared__ int s_node[kSlotRequests];
+  __shared__ uint32_t s_twice;  // bit i: a request before has request i's node
   const int r0 = blockIdx.x * per;
   long long before = 0;
-  for (int r = tid; r < r0; r += kSlotThreads) before += max(count[r], 0);
+  uint32_t twice = 0;
+  if (tid == 0) s_twice = 0;
+  if (per == 1) {
+    const int own = num_requests > 0 ? node[r0] : -1;
+    for (int r = tid; r < r0; r += kSlotThreads) {
+      before += max(count[r], 0);
+      twice |= node[r] == own;
+    }
+  } else {
+    if (tid < per) s_node[tid] = r0 + tid < num_requests ? node[r0 + tid] : -1;
+    __syncthreads();
+    for (int r = tid; r < r0; r += kSlotThreads) {
+      before += max(count[r], 0);
+      const int v = node[r];
+      for (int i = 0; i < per; ++i) twice |= (uint32_t)(v == s_node[i]) << i;
+    }
+  }
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) before += __shfl_xor_sync(0xffffffffu, before, d);
   if (lane == 0) warp_sums[wid] = before;
+  __syncthreads();
+  if (twice) atomicOr(&s_twice, twice);
   __syncthreads();
   if (wid == 0) {
     long long begin = 0;
@@ -72,8 +92,10 @@ __global__ void __launch_bounds__(kSlotThreads) k_append_slots(GraphDev g, PoolG
     end += begin;
     const long long first = end - max(c, 0);
     int why = GF_OK;
+    const uint32_t alike = __match_any_sync(0xffffffffu, v);  // (by all lanes, whatever is known of theirs)
+    const bool again = ((alike & ((1u << lane) - 1u)) | (s_twice >> lane & 1u)) != 0;
     if (mine) {
-      if (room < 0 || c < 0 || h < 0 || h > now || end > num_new) why = GF_ERR_INVALID_ARG;
+      if (again || room < 0 || c < 0 || h < 0 || h > now || end > num_new) why = GF_ERR_INVALID_ARG;
       else if ((long long)h + c > room) why = GF_ERR_CAPACITY;
       if (why != GF_OK) atomicCAS(status + kStatusReport, 0, why);
     }

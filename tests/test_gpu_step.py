@@ -132,6 +132,29 @@ def test_slots_of_batches_of_any_size(n):
     pa.close()
 
 
+@pytest.mark.parametrize("n", [2, 40, 700])
+def test_a_node_named_twice_in_a_batch(n):
+    """The first request counts, the others are refused; near to each other and far apart."""
+    from paper_2605_22566_b200 import binding as B
+    rng = np.random.default_rng(n)
+    pa = _pa([90] * n, 1, 1, 64)
+    model = OS.OpenNodes()
+    for v in range(n):
+        pa.open_node(v, 90)
+        model.open(v, 90, pa.node_slot(v))
+    for _ in range(3):
+        nodes = rng.permutation(n)
+        nodes[rng.integers(0, n, n // 3 + 1)] = nodes[rng.integers(0, n, n // 3 + 1)]
+        nodes[-1] = nodes[0]
+        counts = rng.integers(0, 9, n).tolist()
+        held = [int(rng.integers(0, len(model.rows[v]) + 1)) for v in nodes.tolist()]
+        slots, lens = pa.append_slots(_ints(*nodes.tolist()), _ints(*counts), sum(counts), _ints(*held))
+        want, want_lens = model.append(nodes.tolist(), held, counts, sum(counts))
+        assert slots.tolist() == want and lens.tolist() == want_lens and lens.tolist()[-1] == -1
+        assert pa.status() == B.GF_ERR_INVALID_ARG
+    pa.close()
+
+
 def test_close_reopen_release_and_refusals():
     from paper_2605_22566_b200 import binding as B
     pa = _pa([300, 64, 64, 10], 2, 2, 64, 2, extra_tiles=4, max_residual_nodes=1)
