@@ -489,9 +489,10 @@ def test_projection_refusals():
         Projection(w, a)
     with pytest.raises(ValueError):
         Projection(w, a, b[:, :31].contiguous())
-    b[1, 3, 2] = float("inf")                                       # (it would reach rows of the other adapters)
-    with pytest.raises(ValueError, match="finite"):
-        Projection(w, a, b)
+    for bad in (float("inf"), -float("inf"), float("nan")):
+        b[1, 3, 2] = bad                                            # (it would reach rows of the other adapters)
+        with pytest.raises(ValueError, match="finite"):
+            Projection(w, a, b)
     desc = B.ProjectionDesc(*[B.GF_MAX_ADAPTERS + 1 if n == "num_adapters" else getattr(p.desc, n) for n, _ in p.desc._fields_])
     assert B.gf_adapter_project_scratch_bytes(desc, 4) == 0
     assert B.gf_adapter_project(pa.g, desc, 4, *[good[n] for n in ("x", "xs", "which", "y", "ys", "fp32", "scratch", "nbytes")], pa.stream) == B.GF_ERR_INVALID_ARG
