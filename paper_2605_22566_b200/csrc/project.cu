@@ -20,7 +20,7 @@
 //
 // Measured, 4096 -> 6144 in bf16: one row 11.4 us, where W alone is 7.8 of HBM (launch, the first copies and the join of 6 parts are the rest); 256 rows 20.1,
 // with 64 adapters of rank 16 37 (their stages are half as many as W's, in 96 CTAs: clusters of 6 do not all find room); 8192 rows 275 us, 1500
-// TFLOP/s, tensor pipe 85 % busy.  64 rows of 4096 -> 128 000 in fp32: 180 to 195 us, 5.6 TB/s of W and results.
+// TFLOP/s, tensor pipe 85 % busy.  64 rows of 4096 -> 128 000 in fp32: 176 to 190 us, 5.7 to 6.2 TB/s of W and results.
 //
 // (The same sums on the CUDA cores, while the MMAs ran, took 568 us for 8192 rows with adapters of rank 16 and 1143 of rank 64,
 // where W x alone took 295: their reads of B and h wait behind the copies' traffic.)
