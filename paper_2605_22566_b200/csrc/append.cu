@@ -104,8 +104,10 @@ __global__ void __launch_bounds__(kSlotThreads) k_append_slots(GraphDev g, PoolG
     if (mine && lens != nullptr) lens[r] = ok ? h + c : -1;
     const int off = ok ? g.node_off[v] : 0;
     s_slot[lane] = ok ? off + h : -1;
-    s_from[lane] = off + h + c;
-    s_to[lane] = ok && now > h + c ? off + now : 0;  // tokens taken back
+    // tokens taken back; none of a request that is left out (whose held and count may be anything)
+    const bool back = ok && now > h + c;
+    s_from[lane] = back ? off + h + c : 0;
+    s_to[lane] = back ? off + now : 0;
     s_begin[lane] = (int)min(first, (long long)num_new);
     if (lane == 31) s_begin[32] = (int)min(end, (long long)num_new);
   }
