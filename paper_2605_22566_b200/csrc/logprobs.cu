@@ -26,6 +26,7 @@
 
 #include "tc_device.cuh"
 #include "gf_internal.h"
+#include "rounds.h"
 
 namespace gf {
 namespace {
@@ -452,14 +453,14 @@ __global__ void __launch_bounds__(kMaxThreads, 3) k_token_logprobs(const T* __re
   // Lane 0 brings the warp's rounds.
   uint4* my_ring = ring + wid * kStages * kRound;
   int bring_at = p.first;  // the next round's first vector
-  uint32_t brought = 0, taken = 0;
+  Rounds rounds;           // (a lane's own waits; lane 0 starts the copies)
   auto bring = [&] {
     if (bring_at >= v1) return;
     const uint32_t bytes = (uint32_t)min(p.len, v1 - bring_at) * 16u;
-    uint64_t* full = &sm.full[wid][brought % kStages];
+    uint64_t* full = &sm.full[wid][rounds.started % kStages];
     mbar_arrive_expect_tx(full, bytes);
-    bulk_g2s(my_ring + (brought % kStages) * kRound, p.xv + bring_at, bytes, full);
-    ++brought;
+    bulk_g2s(my_ring + (rounds.started % kStages) * kRound, p.xv + bring_at, bytes, full);
+    rounds.start();
     bring_at += p.stride;
   };
   if (lane == 0) {
@@ -469,7 +470,6 @@ __global__ void __launch_bounds__(kMaxThreads, 3) k_token_logprobs(const T* __re
   }
   __syncwarp();
 
-  bool ok = true;
   Stats st{kNegInf, 0.f, 0.f};
   float least = kNegInf;  // more than k logits of the CTA's part reach it, or minus infinity
   auto push = [&](float v, int64_t index) {
@@ -509,11 +509,8 @@ __global__ void __launch_bounds__(kMaxThreads, 3) k_token_logprobs(const T* __re
   int round = 0;
   for (int base = v0; base < v1; base += p.stride, ++round) {
     const int begin = base + (p.first - v0), end = min(v1, begin + p.len);
-    const uint4* piece = my_ring + (taken % kStages) * kRound;
-    if (begin < v1) {
-      ok = ok && mbar_wait(&sm.full[wid][taken % kStages], (taken / kStages) & 1u, status);
-      ++taken;
-    }
+    const uint4* piece = my_ring + (rounds.landed % kStages) * kRound;
+    if (begin < v1) rounds.waited(rounds.ok && mbar_wait(&sm.full[wid][rounds.landed % kStages], (rounds.landed / kStages) & 1u, status));
     __syncwarp();
     uint4 raw[kAhead];
 #pragma unroll
@@ -603,7 +600,7 @@ __global__ void __launch_bounds__(kMaxThreads, 3) k_token_logprobs(const T* __re
       }
     }
     __syncwarp();
-    if (lane == 0 && ok && begin < v1) bring();
+    if (lane == 0 && rounds.ok && begin < v1) bring();
   }
   fold();
   st = stats_sum(st);
@@ -669,7 +666,7 @@ __global__ void __launch_bounds__(kMaxThreads, 3) k_token_logprobs(const T* __re
     }
   }
   if (lane == 0)  // where it gave up, its copies on the way land before the memory is another's
-    for (uint32_t i = taken < brought ? taken : brought; i < brought; ++i) mbar_drain(&sm.full[wid][i % kStages], (i / kStages) & 1u, status);
+    for (uint32_t i = rounds.landed; i < rounds.started; ++i) mbar_drain(&sm.full[wid][i % kStages], (i / kStages) & 1u, status);
 }
 
 }  // namespace

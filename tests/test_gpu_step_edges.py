@@ -64,3 +64,31 @@ def test_refused_requests_leave_every_row_as_it_was(many):
     want[:, :, at // 64, :, 5:40] = 0
     assert torch.equal(view, want)
     pa.close()
+
+
+# ---- waits that ran out --------------------------------------------------------------------------------
+
+
+def test_calls_behind_a_wait_that_ran_out_end_and_the_next_ones_are_right():
+    """A wait that gave up makes the waits behind it give up too, copies and all: those calls end, the report says so once, and the next calls give
+    what they gave before."""
+    from paper_2605_22566_b200 import binding as B
+    from paper_2605_22566_b200.runtime import Projection
+    rng = np.random.default_rng(1)
+    pa = _pa()
+    logits = [torch.from_numpy(rng.standard_normal((rows, v)) * 3).to(kind).cuda() for rows, v, kind in ((1, 40000, torch.bfloat16), (400, 9000, torch.float32))]
+    p = Projection((_bf16(rng, 900, 512) * 0.05).cuda(), (_bf16(rng, 6, 16, 512) * 0.05).cuda(), _bf16(rng, 6, 900, 16).cuda())
+    xs = [_bf16(rng, rows, 512).cuda() for rows in (3, 300, 1500)]
+    ids = [_ints(*rng.integers(-1, 6, len(x)).tolist()) for x in xs]
+
+    def calls():
+        return [t for x in logits for t in pa.token_logprobs(x, None, 9)[1:]] + [pa.project(p, x, i, dtype=d) for x, i in zip(xs, ids) for d in (torch.bfloat16, torch.float32)]
+    want = calls()
+    assert pa.status() == 0
+    for _ in range(3):
+        st, gave_up = B.gf_debug_wait_probe(pa.g, 5000, pa.stream)
+        assert st == B.GF_OK and gave_up == 1
+        calls()
+        assert pa.status() == B.GF_ERR_TIMEOUT and pa.status() == 0
+        assert all(torch.equal(a, b) for a, b in zip(calls(), want)) and pa.status() == 0
+    pa.close()
