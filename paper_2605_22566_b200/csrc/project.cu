@@ -243,7 +243,8 @@ __device__ __forceinline__ __nv_bfloat16 take_number(float& v) {
   v = fabsf(v) <= 3.3895e38f ? v - __bfloat162float(n) : 0.f;
   return n;
 }
-// Four results of neighbouring ranks of a row; zeros where the row is another slot's.
+// Four results of neighbouring ranks of a row; zeros where the row is another slot's.  The numbers stand, and are added, from the least to the first:
+// an MMA cuts each of its products off at some 2^-24 of the sum that is there, and behind the first number's sum most of the third's would be gone.
 __device__ __forceinline__ void store_h(const Slots& sl, const HPlace& p, int row_in_tile, int row_slot, float4 v) {
   if (p.at == nullptr) return;
   const bool mine = row_slot == p.slot && p.r < sl.rank;  // (ranks are multiples of 8)
@@ -254,7 +255,7 @@ __device__ __forceinline__ void store_h(const Slots& sl, const HPlace& p, int ro
   char* at = p.at + (row_in_tile * sl.padded + p.r) * 2;
   for (int i = 0; i < sl.numbers; ++i) {
     __align__(8) __nv_bfloat16 n[4] = {take_number(v.x), take_number(v.y), take_number(v.z), take_number(v.w)};
-    *reinterpret_cast<uint2*>(at + i * sl.block) = *reinterpret_cast<uint2*>(n);
+    *reinterpret_cast<uint2*>(at + (sl.numbers - 1 - i) * sl.block) = *reinterpret_cast<uint2*>(n);
   }
 }
 
@@ -538,6 +539,7 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
             s0 = s1 * part / a.splits;
             s1 = s1 * (part + 1) / a.splits;
             const int stages = slot_stages(s1 - s0);
+            if (kExact && stages > 0 && in_acc > 0) in_acc = kChunk;  // (to an empty accumulator: h's last number would be lost beside W x)
             for (int i = 0; i < stages; ++i) {
               if (!(ok = filled() && chunk())) break;
               const uint32_t at = smem_u32(smem + s * stage_bytes), ht = at + w_bytes;
@@ -605,13 +607,13 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
         };
         uint32_t from = lanes + acc_at() * a.acc_cols + col0;
         if (kExact) {
-          int stages = step1 - step0;
+          int chunks = (step1 - step0 + kChunk - 1) / kChunk;
           if (kMode == kWith) {
             const int n = slots_of(row_tile);
-            stages += slot_stages(n * (part + 1) / a.splits - n * part / a.splits);
+            chunks += (slot_stages(n * (part + 1) / a.splits - n * part / a.splits) + kChunk - 1) / kChunk;
           }
           const uint32_t sums = lanes + a.sum_cols + col0;
-          for (int c = 0; c < stages && wait_sums(); c += kChunk) {
+          for (int c = 0; c < chunks && wait_sums(); ++c) {
             from = lanes + acc_at() * a.acc_cols + col0;
             for (int g = 0; g < cols; g += kGroup) {
               uint32_t r[kGroup], q[kGroup];
@@ -857,7 +859,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_adapter_rows(const __nv_bflo
     float v[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = at == slot ? h[c * 8 + j] : 0.f;
-    for (int n = 0; n < sl.numbers; ++n) {
+    for (int n = sl.numbers - 1; n >= 0; --n) {  // (the first number last, as in store_h)
       __align__(16) __nv_bfloat16 p[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) p[j] = take_number(v[j]);

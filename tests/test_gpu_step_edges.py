@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 import torch
 
+import step_digits as D
 from kv4_cases import private_workload
 from oracle import step as OS
 
@@ -91,4 +92,46 @@ def test_calls_behind_a_wait_that_ran_out_end_and_the_next_ones_are_right():
         calls()
         assert pa.status() == B.GF_ERR_TIMEOUT and pa.status() == 0
         assert all(torch.equal(a, b) for a, b in zip(calls(), want)) and pa.status() == 0
+    pa.close()
+
+
+# ---- digits of projections -----------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("rows,k,n", [
+    # K in parts and whole, tiles of one block of 16 to 128 rows and of two with 256; 128 features and fewer
+    (5, 16384, 129), (100, 16384, 700), (100, 8192, 20000), (255, 16384, 520), (256, 16384, 300), (2048, 8192, 2500), (300, 16384, 100), (700, 8200, 40)])
+def test_fp32_results_hold_their_digits_over_long_sums(rows, k, n):
+    """All products of one sign: additions that are cut off all take away, and what is not taken out in time shows in the norm."""
+    from paper_2605_22566_b200.runtime import Projection
+    pa = _pa()
+    x, w = (t.cuda() for t in D.same_sign(rows, k, n, k))
+    got = pa.project(Projection(w), x, dtype=torch.float32).double()
+    ref = x.double() @ w.double().T
+    off = float((got - ref).norm() / ref.norm())
+    assert off <= D.SAME_SIGN + 2.0 ** -24, off                         # (and the result's rounding)
+    assert pa.status() == 0
+    pa.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,n,rank", [(1, 200, 8), (3, 300, 16), (100, 300, 24), (100, 129, 64), (255, 260, 32), (300, 600, 16), (700, 130, 64), (2000, 100, 32), (2300, 700, 8)])
+def test_adapters_hold_their_digits(rows, n, rank, dtype):
+    """h next to the middle between what its bf16 numbers can hold: with nothing beside the adapter's part, and with a W x that takes all but its last bits away."""
+    from paper_2605_22566_b200.runtime import Projection
+    pa = _pa()
+    x, a, b = (t.cuda() for t in D.between_numbers(rows, n, 3, rank))
+    which = torch.arange(rows, dtype=torch.int32, device="cuda") % 4 - 1
+    for w, ids in ((torch.zeros(n, 16, dtype=torch.bfloat16, device="cuda"), which), (D.cancelling(x.cpu(), b[1].cpu()).cuda(), torch.ones_like(which))):
+        got = pa.project(Projection(w, a, b), x, ids, dtype=dtype).double()
+        shared = x.double() @ w.double().T
+        part = torch.zeros_like(shared)
+        for i in range(3):
+            mine = ids == i
+            part[mine] = (x[mine].double() @ a[i].double().T) @ b[i].double().T
+        ref = shared + part
+        # (W x is one addition of 16 entries and one to what is there; its own digits are those of the row's magnitudes)
+        bound = (D.THREE if dtype == torch.float32 else D.TWO) * part + 2 * 2.0 ** -23 * shared.abs() + torch.finfo(dtype).eps / 2 * ref.abs()
+        assert bool(((got - ref).abs() <= bound).all()), float(((got - ref).abs() / (bound + 1e-300)).max())
+    assert pa.status() == 0
     pa.close()
