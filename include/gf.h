@@ -529,8 +529,9 @@ gf_status_t gf_edge_scores(gf_wgraph_t* g, const gf_scorer_t* model, const float
  *   y[t] = W x[t] + scale[a] B[a] (A[a] x[t]),   a = adapter[t]; -1: no adapter.
  * bf16 row-major, caller-owned, 16-byte aligned; A [num_adapters, rank, in_dim], B [num_adapters, out_dim, rank], contiguous;
  * scale NULL: 1.  in_dim and w_stride (entries between rows of W) are multiples of 8; rank a multiple of 8, at most 64
- * (adapters of a smaller rank are filled up with zeros); num_adapters at most GF_MAX_ADAPTERS, 0: none.  B's entries are finite: rows of
- * other adapters meet them times zero.  What A, x, or a scale hold of infinities and NaN stays in the rows that it belongs to. */
+ * (adapters of a smaller rank are filled up with zeros); num_adapters at most GF_MAX_ADAPTERS, 0: none.  What W, A, B, x or a scale hold of
+ * infinities and NaN stays in the results whose formula has it.  (Entries of B that are no finite numbers cost the rows beside theirs time: every result that meets one is
+ * worked out by a thread by itself.) */
 #define GF_MAX_ADAPTERS 32768
 typedef struct {
   int32_t in_dim, out_dim;

@@ -69,6 +69,10 @@ struct ProjectArgs {
   int64_t y_stride;
   int y_fp32, y_vec;                    // y_vec: four neighbouring results can be stored at once
   int32_t* status;
+  // what a single result is worked out from (settle)
+  const __nv_bfloat16 *w, *x, *b;
+  int64_t w_stride, x_stride;
+  const int32_t* adapter;               // [rows] as given
 };
 
 // kTwo: the CTA is one of two that work on one tile with MMAs of both (cta_group::2), the even one, which issues them, the leader.  Each brings
@@ -201,6 +205,65 @@ __device__ __forceinline__ void store_rows(const ProjectArgs& a, int row, int fe
   }
 }
 
+__device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u; }
+// A result that came out of the MMAs as no finite number.  Every row of a tile meets the B of each of its slots, times zero where the slot is another's, and an infinity or
+// a NaN there makes a NaN of that.  So where the feature's row of a slot's B has one, the result is worked out anew from what belongs to it; else it is what
+// the formula gives.  (A thread by itself, some 30 us at K = 4096: adapters with such entries are slow, and no other's row pays but for looking.)
+__device__ float settle(const ProjectArgs& a, int row_tile, int row, int feat, float v) {
+  const Slots& sl = a.slots;
+  if (row >= a.rows || feat >= a.out_dim) return v;
+  const int32_t* which = sl.adapter + (int64_t)row_tile * sl.most;
+  const int n = __ldcg(sl.count + row_tile), mine = a.adapter[row], per_row = sl.rank / 8;
+  auto b_row = [&](int id) { return reinterpret_cast<const uint4*>(a.b + ((int64_t)id * a.out_dim + feat) * sl.rank); };
+  auto none = [](uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; };
+  int own = -1;  // the row's slot
+  bool spoiled = false;
+  for (int i = 0; i < n; ++i) {
+    const int id = __ldcg(which + i);
+    if (id == mine) own = i;
+    for (int c = 0; c < per_row; ++c) {
+      const uint4 w = __ldg(b_row(id) + c);
+      spoiled = spoiled || none(w.x) || none(w.y) || none(w.z) || none(w.w);
+    }
+  }
+  if (!spoiled) return v;
+  float lo = 0.f, hi = 0.f;
+  auto add = [&](uint32_t p, uint32_t q) {
+    lo = fmaf(__uint_as_float(p << 16), __uint_as_float(q << 16), lo);
+    hi = fmaf(__uint_as_float(p & 0xffff0000u), __uint_as_float(q & 0xffff0000u), hi);
+  };
+  const uint4 *wr = reinterpret_cast<const uint4*>(a.w + feat * a.w_stride), *xr = reinterpret_cast<const uint4*>(a.x + row * a.x_stride);
+  for (int k = 0; k < a.in_dim / 8; ++k) {
+    const uint4 p = __ldg(wr + k), q = __ldg(xr + k);
+    add(p.x, q.x);
+    add(p.y, q.y);
+    add(p.z, q.z);
+    add(p.w, q.w);
+  }
+  float sum = lo + hi;
+  if (own < 0) return sum;
+  const char* h = sl.h + ((int64_t)row_tile * sl.most + own) * sl.numbers * sl.block + (int64_t)(row - row_tile * a.nt) * sl.padded * 2;
+  for (int i = 0; i < sl.rank; ++i) {
+    float value = 0.f;
+    for (int j = 0; j < sl.numbers; ++j) value += __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(h + j * sl.block)[i]);
+    sum = fmaf(__bfloat162float(reinterpret_cast<const __nv_bfloat16*>(b_row(mine))[i]), value, sum);
+  }
+  return sum;
+}
+// Of a thread's stored results those that are no finite numbers are settled: bit i of `where` stands for the rows from row0 + i step on, `count` of them, each with `feats`
+// features from `feat` on.  (Behind the tile, where the thread has few registers to put aside.)
+__device__ __noinline__ void settle_stored(const ProjectArgs& a, int row_tile, uint32_t where, int row0, int step, int count, int feat, int feats) {
+  for (; where; where &= where - 1) {
+    const int first = row0 + (__ffs(where) - 1) * step;
+    for (int row = first; row < min(first + count, a.rows); ++row)
+      for (int f = feat; f < min(feat + feats, a.out_dim); ++f) {
+        const int64_t at = (int64_t)row * a.y_stride + f;
+        const float v = a.y_fp32 ? static_cast<float*>(a.y)[at] : __bfloat162float(static_cast<__nv_bfloat16*>(a.y)[at]);
+        if (!finite(v)) store_y(a, row, f, settle(a, row_tile, row, f, v));
+      }
+  }
+}
+
 // (a warp's lanes together; every warp of every CTA of the cluster takes part in each barrier)
 __device__ __forceinline__ void cluster_sync_all() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -285,6 +348,7 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
   uint64_t* drained = acc_empty + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drained + 1);
   uint32_t* gave_up = tmem_slot + 1;  // the CTA has; what a cluster does next goes by those of all its CTAs, so that none leaves alone
+  volatile uint32_t* odd_ones = gave_up + 1;  // a result of a round was no finite number (in shared memory: there is no register to spare)
   const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31;
   const int size = a.splits * kCtas;  // of a cluster
   const int group = blockIdx.x / size, groups = gridDim.x / size, rank = blockIdx.x - group * size, part = rank / kCtas, half = rank - part * kCtas;
@@ -332,6 +396,7 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
     for (int i = 0; i < 2; ++i) { mbar_init(acc_full + i, 1); mbar_init(acc_empty + i, kTakers * kCtas); }
     mbar_init(drained, 1);
     *gave_up = 0;
+    *odd_ones = 0;
     mbar_fence_init();
   }
   if (wid == 1) tmem_take<kTwo>(tmem_slot, a.tmem_cols);
@@ -635,13 +700,21 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
         }
         if (!ok || rounds) break;  // (joined below, by the whole cluster)
         const int feat = f * kTileFeat + half * kFeat + m;
+        uint32_t unsettled = 0;  // (32 groups of rows at most)
         for (int g = col0; g < col0 + cols && t0 + g < a.rows; g += kGroup) {
           uint32_t r[kGroup];
           tmem_ld8(from + (g - col0), r);
           tmem_wait_ld();
           if (feat < a.out_dim) store_rows(a, t0 + g, feat, r);
+          if (kMode == kWith) {
+            bool all = true;
+#pragma unroll
+            for (int j = 0; j < kGroup; ++j) all = all && finite(__uint_as_float(r[j]));
+            if (!all) unsettled |= 1u << (g - col0) / kGroup;
+          }
         }
         if (!kExact) sums_taken();
+        if (kMode == kWith && unsettled) settle_stored(a, row_tile, unsettled, t0 + col0, kGroup, kGroup, feat, 1);
       }
     }
     __syncwarp();
@@ -711,8 +784,13 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
           if (r < n) {
             if (kMode == kDown) store_h(sl, place, r, row_slot[i], sum[i]);
             else store_y4(a, t0 + r, f * kTileFeat + half * kFeat + lane * 4, sum[i]);
+            if (kMode == kWith && !(finite(sum[i].x) && finite(sum[i].y) && finite(sum[i].z) && finite(sum[i].w))) *odd_ones = 1;
           }
         }
+      }
+      if (kMode == kWith && *odd_ones) {  // (a warp has at most 16 of a tile's rows: W x of a round is in two parts at least)
+        const int from = mine + joined * wid;
+        settle_stored(a, row_tile, (1u << (n - from + apart - 1) / apart) - 1u, t0 + from, apart, 1, f * kTileFeat + half * kFeat + lane * 4, 4);
       }
       __syncwarp();
       cluster_sync_all();  // nobody leaves, or takes new stages to where its part was, while that is read
@@ -1081,6 +1159,12 @@ static int launch_pass(const gf_projection_t& p, int rows, const void* x, int64_
   a.y_stride = y_stride;
   a.y_fp32 = y_fp32;
   a.status = status;
+  a.w = (const __nv_bfloat16*)p.w_dev;
+  a.x = (const __nv_bfloat16*)x;
+  a.b = (const __nv_bfloat16*)p.b_dev;
+  a.w_stride = p.w_stride;
+  a.x_stride = x_stride;
+  a.adapter = adapter;
   choose_tiles(a, with ? p.num_adapters : 0, p.rank, num_sms);
   a.y_vec = (y_stride & 3) == 0 && ((uintptr_t)y & (y_fp32 ? 15 : 7)) == 0;
   Maps maps = {};

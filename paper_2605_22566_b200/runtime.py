@@ -34,8 +34,8 @@ def tensor_to_f64(t: torch.Tensor) -> np.ndarray:
 
 class Projection:
     """A shared weight [out, in] with the low-rank adapters that rows may name: a [adapters, rank, in], b [adapters, out, rank],
-    scale fp32 [adapters] (None: 1).  bf16, on one device; kept alive here.  The weight's rows may lie apart, the adapters are contiguous.  b holds finite entries only, which is
-    looked at here (once: whoever writes to it later keeps them so)."""
+    scale fp32 [adapters] (None: 1).  bf16, on one device; kept alive here.  The weight's rows may lie apart, the adapters are contiguous.  b with an infinity or a
+    NaN is refused: such an adapter gives no results of use and makes a call slow.  (Looked at here, once; written to it later they stay in its own rows.)"""
 
     def __init__(self, weight: torch.Tensor, a: Optional[torch.Tensor] = None, b: Optional[torch.Tensor] = None,
                  scale: Optional[torch.Tensor] = None):
@@ -50,7 +50,7 @@ class Projection:
                 raise ValueError(f"a, b: contiguous bf16 tensors [adapters, rank, {in_dim}] and [adapters, {out_dim}, rank] on {weight.device}")
             adapters, rank = a.shape[:2]
             if b.numel() and not bool(torch.isfinite(torch.stack(torch.aminmax(b))).all()):  # (a NaN comes through either)
-                raise ValueError("b: finite entries (rows of other adapters meet them times zero)")
+                raise ValueError("b: finite entries")
         if scale is not None and (a is None or scale.dtype != torch.float32 or tuple(scale.shape) != (adapters,) or not scale.is_contiguous() or
                                   scale.device != weight.device):
             raise ValueError(f"scale: a contiguous fp32 tensor [{adapters}] on {weight.device}")

@@ -135,3 +135,49 @@ def test_adapters_hold_their_digits(rows, n, rank, dtype):
         assert bool(((got - ref).abs() <= bound).all()), float(((got - ref).abs() / (bound + 1e-300)).max())
     assert pa.status() == 0
     pa.close()
+
+
+# ---- entries that are no numbers -------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,k,n,rank", [(5, 4096, 300, 8), (40, 264, 129, 16), (130, 1024, 700, 24), (100, 64, 20000, 16), (256, 2048, 600, 32), (300, 200, 100, 16), (700, 264, 520, 64),
+                                           (2100, 128, 2500, 8)])
+def test_an_adapter_that_is_no_number_spoils_its_own_rows_only(rows, k, n, rank, dtype):
+    """Infinities and NaN in one adapter's B, one entry and all of it: other adapters' rows and rows without one are what they are without it, to rounding, its own what the formula
+    gives.  (Written after the Projection was made, which refuses them.)"""
+    from paper_2605_22566_b200.runtime import Projection
+    rng = np.random.default_rng(rows + k)
+    pa = _pa()
+    x, w = _bf16(rng, rows, k).cuda(), (_bf16(rng, n, k) * k ** -0.5).cuda()
+    a, b = (_bf16(rng, 5, rank, k) * k ** -0.5).cuda(), _bf16(rng, 5, n, rank).cuda()
+    which = torch.from_numpy(rng.integers(-1, 5, rows)).to(torch.int32).cuda()
+    which[0], which[-1] = 2, 3
+    p = Projection(w, a, b)
+    clean = pa.project(p, x, which, dtype=dtype)
+    b[2, n // 2, rank - 1] = float("inf")
+    b[2, 0, 0] = float("-inf")
+    b[4, n - 1, 3] = float("nan")
+    b[3] = float("nan")                                                 # every row of a tile that has one of this
+    x[rows // 2, 1] = float("nan")
+    got = pa.project(p, x, which, dtype=dtype)
+    ok = (which != 3).cpu()
+    ok[rows // 2] = False
+    where = torch.arange(rows)
+    ref, size = OS.project(*(t.double().cpu().numpy() for t in (x, w, a, b)), None, which.tolist())
+    _, size = OS.project(*(t.double().cpu().nan_to_num(0.0, 0.0, 0.0).numpy() for t in (x, w, a, b)), None, which.tolist())
+    y = got.double().cpu().numpy()
+    bad = ~np.isfinite(ref)
+    assert np.array_equal(np.isnan(y), np.isnan(ref)) and np.array_equal(y[bad & ~np.isnan(ref)], ref[bad & ~np.isnan(ref)])
+    assert bad[~ok.numpy()].all() and bad[ok.numpy()].sum() == 2 * int((which[ok] == 2).sum()) + int((which[ok] == 4).sum())
+    # (sums of k + rank products in fp32, in another order: 2^-23 of the magnitudes for each at most, twice for the adapter's; then half a step of the type)
+    bound = 2 * (k + 80) * 2.0 ** -23 * size + np.abs(np.where(bad, 0.0, ref)) * torch.finfo(dtype).eps / 2
+    assert np.all(np.abs(np.where(bad, 0.0, y) - np.where(bad, 0.0, ref)) <= bound * 1.001 + 1e-37)
+    # tiles without such an adapter, and features without such an entry, have the same bits as before
+    spoiled = {int(t) // 256 for t in where[(which == 3).cpu()]} | {rows // 2 // 256}
+    same = [int(t) for t in where if int(t) // 256 not in spoiled and int(which[t]) not in (2, 4)]
+    assert torch.equal(got[same], clean[same])
+    none = pa.project(p, x, torch.full_like(which, -1), dtype=dtype)
+    assert torch.equal(none[:rows // 2], pa.project(p, x, None, dtype=dtype)[:rows // 2])
+    assert pa.status() == 0
+    pa.close()
