@@ -256,7 +256,9 @@ gf_status_t gf_node_kv4_write(gf_wgraph_t* g, int32_t node, int32_t layer, const
  * with gf_kv4_pool_attach.  The weights are the caller's array, fp32 [num_layers, num_kv_heads, slots], which no
  * write or release of a node touches: a node that takes the slots of a released one finds that one's sums there.  Before
  * a node's first accumulated step the caller sets its slots to zero (num_layers * num_kv_heads rows of n_tokens
- * floats, `slots` apart); gf_node_kv_evict fills those of its destinations itself. */
+ * floats, `slots` apart); gf_node_kv_evict fills those of its destinations itself.  An open node's tokens are such nodes by
+ * themselves: a slot that gf_append_slots gives to a new token may have been that of one taken back, whose sum is still there, so
+ * the slots that it names are set to zero before the first accumulated step behind it. */
 int64_t gf_weight_slots(const gf_wgraph_t* g);
 
 /* What share of the attention of one decode step every resident token received, one layer:

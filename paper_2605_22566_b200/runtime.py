@@ -457,6 +457,19 @@ class PathAttention:
         self._check_weights(weights)
         self.node_weights(weights, node).zero_()
 
+    def clear_slot_weights(self, weights: torch.Tensor, slots: torch.Tensor) -> None:
+        """Zeroes the weights of the token slots that `append_slots` gave to new tokens (-1: none), which tokens taken back may have had before: call
+        this before the first step that accumulates into them.  Nothing is waited for."""
+        self._check_weights(weights)
+        if not _ints(slots, slots.numel(), self._index):
+            self._refuse_ints(slots=(slots, "new"))
+        if slots.numel() == 0:
+            return
+        # (-1 stands for the largest slot named; where none is, all stand for slot 0, which keeps what it has)
+        last = slots.amax()
+        at = torch.where(slots >= 0, slots, last.clamp(min=0)).long()
+        weights.index_copy_(2, at, weights.index_select(2, at).masked_fill_(last >= 0, 0.0))
+
     def _check_weights(self, weights: torch.Tensor) -> None:
         shape = (self.layers, self.w.num_kv_heads, B.gf_weight_slots(self.g))
         if weights.dtype != torch.float32 or weights.device != self.pool.device or not weights.is_contiguous() or \

@@ -6,6 +6,8 @@ import torch
 
 import step_digits as D
 from kv4_cases import private_workload
+from oracle import attention as OA
+from oracle import eviction as OE
 from oracle import step as OS
 
 pytestmark = pytest.mark.gpu
@@ -180,4 +182,104 @@ def test_an_adapter_that_is_no_number_spoils_its_own_rows_only(rows, k, n, rank,
     none = pa.project(p, x, torch.full_like(which, -1), dtype=dtype)
     assert torch.equal(none[:rows // 2], pa.project(p, x, None, dtype=dtype)[:rows // 2])
     assert pa.status() == 0
+    pa.close()
+
+
+# ---- weights of tokens that took others' slots -------------------------------------------------------------
+
+
+@pytest.mark.parametrize("captured", [False, True])
+def test_weights_of_tokens_in_the_slots_of_tokens_taken_back(captured):
+    """Steps of decode over open nodes that take tokens back, as after drafts that were not accepted: what every token has received is its own, and an
+    eviction behind the last step goes by that."""
+    rng = np.random.default_rng(2)
+    hq, hkv, d, layers = 4, 2, 64, 2
+    paths = [[0, 1], [0, 2], [0, 3]]
+    pa = _pa([90, 150, 150, 150, 20], hq, hkv, d, layers, paths, extra_tiles=4)
+    kv, mine = {}, {}
+    for layer in range(layers):
+        k, v = _bf16(rng, 90, hkv, d), _bf16(rng, 90, hkv, d)
+        pa.write_node(0, layer, k.cuda(), v.cuda())
+        kv[layer, 0] = [k.double().numpy(), v.double().numpy()]
+        mine[layer, 0] = np.zeros((hkv, 90))
+        for n in (1, 2, 3):
+            kv[layer, n], mine[layer, n] = [np.zeros((0, hkv, d))] * 2, np.zeros((hkv, 0))
+    for n in (1, 2, 3):
+        pa.open_node(n, 150)
+    weights = pa.new_weights()
+    nodes = _ints(1, 2, 3)
+    new = 90
+    counts, held = torch.zeros(3, dtype=torch.int32, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    k, v = (torch.zeros(layers, new, hkv, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    q = torch.zeros(layers, 3, hq, d, dtype=torch.bfloat16, device="cuda")
+    lse = torch.zeros(layers, 3, hq, device="cuda")
+    out = torch.empty_like(q)
+
+    def step():
+        slots, _ = pa.append_slots(nodes, counts, new, held)
+        pa.clear_slot_weights(weights, slots)
+        pa.build(deferred=True)
+        for layer in range(layers):
+            pa.append(layer, slots, k[layer], v[layer])
+            pa.decode(layer, q[layer], out=out[layer], lse=lse[layer])
+            pa.attention_weights(layer, q[layer], lse[layer], weights)
+    graph = None
+    pa.build(deferred=True)
+    if captured:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step()
+        assert pa.status() == 0
+    for kept, more in (([0, 0, 0], [70, 1, 0]), ([70, 1, 0], [5, 2, 1]), ([71, 0, 1], [4, 1, 0]), ([60, 1, 1], [30, 0, 3]), ([90, 0, 2], [0, 0, 2])):
+        held.copy_(_ints(*kept))
+        counts.copy_(_ints(*more))
+        for t in (k, v, q):
+            t.copy_(_bf16(rng, *t.shape))
+        graph.replay() if captured else step()
+        torch.cuda.synchronize()
+        for layer in range(layers):
+            begin = 0
+            for i, n in enumerate((1, 2, 3)):
+                rows = [t[layer, begin:begin + more[i]].double().cpu().numpy() for t in (k, v)]
+                kv[layer, n] = [np.concatenate([old[:kept[i]], new_rows]) for old, new_rows in zip(kv[layer, n], rows)]
+                mine[layer, n] = np.concatenate([mine[layer, n][:, :kept[i]], np.zeros((hkv, more[i]))], axis=1)
+                begin += more[i]
+            queries = q[layer].double().cpu().numpy()
+            node_kv = lambda n: kv[layer, n]  # noqa: E731
+            _, ref_lse = OA.decode(paths, node_kv, queries, hkv)
+            for n, got in OE.attention_weights(paths, node_kv, queries, ref_lse, hkv).items():
+                mine[layer, n] = mine[layer, n] + got
+                held_now = weights[layer, :, pa.node_slot(n):pa.node_slot(n) + got.shape[1]].double().cpu().numpy()
+                assert np.all(np.abs(held_now - mine[layer, n]) <= 2e-4 * mine[layer, n] + 1e-30), (layer, n)
+        at = [a + b for a, b in zip(kept, more)]
+    assert pa.status() == 0
+    pa.close_node(1, at[0])
+    before = weights.clone()
+    kept_ids, = pa.evict([(4, 1, 20, 1, 1)], weights)
+    for layer in range(layers):
+        for h in range(hkv):
+            slot = pa.node_slot(1)
+            assert kept_ids[layer, h].tolist() == OE.kept(before[layer, h, slot:slot + at[0]].cpu().tolist(), 20, 1, 1)
+    assert pa.status() == 0
+    del graph
+    pa.close()
+
+
+def test_weights_are_cleared_where_new_tokens_are():
+    pa = _pa([100, 64], 2, 2, 64, 2)
+    weights = pa.new_weights()
+    for slots, cleared in (([3, 70, 4, 3], {3, 4, 70}), ([-1, 5, -1], {5}), ([-1, -1], set()), ([0, -1], {0}), ([], set())):
+        weights.fill_(1.5)
+        pa.clear_slot_weights(weights, _ints(*slots))
+        want = torch.full_like(weights, 1.5)
+        want[:, :, sorted(cleared)] = 0
+        assert torch.equal(weights, want), slots
+    weights.fill_(float("nan"))
+    pa.clear_slot_weights(weights, _ints(7, -1))
+    assert bool((weights[:, :, 7] == 0).all()) and bool(weights[:, :, 0].isnan().all())
+    for bad in (torch.tensor([1]), _ints(1).long(), _ints(1, 2)[::2].expand(2)):
+        with pytest.raises(ValueError):
+            pa.clear_slot_weights(weights, bad)
+    with pytest.raises(ValueError):
+        pa.clear_slot_weights(weights[:1], _ints(1))
     pa.close()
