@@ -533,7 +533,7 @@ gf_status_t gf_edge_scores(gf_wgraph_t* g, const gf_scorer_t* model, const float
  * scale NULL: 1.  in_dim and w_stride (entries between rows of W) are multiples of 8; rank a multiple of 8, at most 64
  * (adapters of a smaller rank are filled up with zeros); num_adapters at most GF_MAX_ADAPTERS, 0: none.  What W, A, B, x or a scale hold of
  * infinities and NaN stays in the results whose formula has it.  (Entries of B that are no finite numbers cost the rows beside theirs time: every result that meets one is
- * worked out by a thread by itself.) */
+ * worked out apart from the others.) */
 #define GF_MAX_ADAPTERS 32768
 typedef struct {
   int32_t in_dim, out_dim;

@@ -69,7 +69,7 @@ struct ProjectArgs {
   int64_t y_stride;
   int y_fp32, y_vec;                    // y_vec: four neighbouring results can be stored at once
   int32_t* status;
-  // what a single result is worked out from (settle)
+  // what a single result is worked out from (rework)
   const __nv_bfloat16 *w, *x, *b;
   int64_t w_stride, x_stride;
   const int32_t* adapter;               // [rows] as given
@@ -206,61 +206,84 @@ __device__ __forceinline__ void store_rows(const ProjectArgs& a, int row, int fe
 }
 
 __device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u; }
-// A result that came out of the MMAs as no finite number.  Every row of a tile meets the B of each of its slots, times zero where the slot is another's, and an infinity or
-// a NaN there makes a NaN of that.  So where the feature's row of a slot's B has one, the result is worked out anew from what belongs to it; else it is what
-// the formula gives.  (A thread by itself, some 30 us at K = 4096: adapters with such entries are slow, and no other's row pays but for looking.)
-__device__ float settle(const ProjectArgs& a, int row_tile, int row, int feat, float v) {
-  const Slots& sl = a.slots;
-  if (row >= a.rows || feat >= a.out_dim) return v;
-  const int32_t* which = sl.adapter + (int64_t)row_tile * sl.most;
-  const int n = __ldcg(sl.count + row_tile), mine = a.adapter[row], per_row = sl.rank / 8;
-  auto b_row = [&](int id) { return reinterpret_cast<const uint4*>(a.b + ((int64_t)id * a.out_dim + feat) * sl.rank); };
+// Whether a feature's row of a slot's B, of all slots of a tile of x, has an entry that is no finite number.
+__device__ __forceinline__ bool spoiled(const ProjectArgs& a, int row_tile, int feat) {
+  const int32_t* which = a.slots.adapter + (int64_t)row_tile * a.slots.most;
+  const int n = __ldcg(a.slots.count + row_tile), pieces = a.slots.rank / 8;
   auto none = [](uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; };
-  int own = -1;  // the row's slot
-  bool spoiled = false;
-  for (int i = 0; i < n; ++i) {
-    const int id = __ldcg(which + i);
-    if (id == mine) own = i;
-    for (int c = 0; c < per_row; ++c) {
-      const uint4 w = __ldg(b_row(id) + c);
-      spoiled = spoiled || none(w.x) || none(w.y) || none(w.z) || none(w.w);
+  bool found = false;
+  for (int i0 = 0; i0 < n; i0 += 8) {
+    const uint4* row[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) row[i] = reinterpret_cast<const uint4*>(a.b + ((int64_t)__ldcg(which + min(i0 + i, n - 1)) * a.out_dim + feat) * a.slots.rank);
+    for (int c = 0; c < pieces; ++c) {
+      uint4 w[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = __ldg(row[i] + c);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) found = found || none(w[i].x) || none(w[i].y) || none(w[i].z) || none(w[i].w);
     }
   }
-  if (!spoiled) return v;
-  float lo = 0.f, hi = 0.f;
-  auto add = [&](uint32_t p, uint32_t q) {
-    lo = fmaf(__uint_as_float(p << 16), __uint_as_float(q << 16), lo);
-    hi = fmaf(__uint_as_float(p & 0xffff0000u), __uint_as_float(q & 0xffff0000u), hi);
-  };
-  const uint4 *wr = reinterpret_cast<const uint4*>(a.w + feat * a.w_stride), *xr = reinterpret_cast<const uint4*>(a.x + row * a.x_stride);
-  for (int k = 0; k < a.in_dim / 8; ++k) {
-    const uint4 p = __ldg(wr + k), q = __ldg(xr + k);
-    add(p.x, q.x);
-    add(p.y, q.y);
-    add(p.z, q.z);
-    add(p.w, q.w);
-  }
-  float sum = lo + hi;
-  if (own < 0) return sum;
-  const char* h = sl.h + ((int64_t)row_tile * sl.most + own) * sl.numbers * sl.block + (int64_t)(row - row_tile * a.nt) * sl.padded * 2;
-  for (int i = 0; i < sl.rank; ++i) {
-    float value = 0.f;
-    for (int j = 0; j < sl.numbers; ++j) value += __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(h + j * sl.block)[i]);
-    sum = fmaf(__bfloat162float(reinterpret_cast<const __nv_bfloat16*>(b_row(mine))[i]), value, sum);
-  }
-  return sum;
+  return found;
 }
-// Of a thread's stored results those that are no finite numbers are settled: bit i of `where` stands for the rows from row0 + i step on, `count` of them, each with `feats`
-// features from `feat` on.  (Behind the tile, where the thread has few registers to put aside.)
-__device__ __noinline__ void settle_stored(const ProjectArgs& a, int row_tile, uint32_t where, int row0, int step, int count, int feat, int feats) {
-  for (; where; where &= where - 1) {
-    const int first = row0 + (__ffs(where) - 1) * step;
-    for (int row = first; row < min(first + count, a.rows); ++row)
-      for (int f = feat; f < min(feat + feats, a.out_dim); ++f) {
-        const int64_t at = (int64_t)row * a.y_stride + f;
-        const float v = a.y_fp32 ? static_cast<float*>(a.y)[at] : __bfloat162float(static_cast<__nv_bfloat16*>(a.y)[at]);
-        if (!finite(v)) store_y(a, row, f, settle(a, row_tile, row, f, v));
+// Results that came out of the MMAs as no finite numbers, by the warp that stored them.  Every row of a tile meets the B
+// of each of its slots, times zero where the slot is another's, and an infinity or a NaN there makes a NaN of that: where the feature has one, such results are
+// worked out anew, each from what belongs to it; the others are what the formula gives.  Bit i of `where` stands for the kGroup rows from row0 + i kGroup step on (of
+// those below `end`), with `feats` features from the lane's `feat` on.  The lanes share K: 8 results in some 20 us at K = 4096
+// (1024 rows of 4096 -> 6144 under 12 adapters of rank 64: 0.8 ms in place of 0.1 for one such entry, 43 ms where an adapter has nothing else).
+__device__ __noinline__ void rework(const ProjectArgs& a, int row_tile, uint32_t where, int row0, int step, int end, int feat, int feats) {
+  const Slots& sl = a.slots;
+  const int lane = threadIdx.x & 31, n = __ldcg(sl.count + row_tile);
+  const int32_t* which = sl.adapter + (int64_t)row_tile * sl.most;
+  __syncwarp();  // (the lanes read what others have stored)
+  for (int f = feat; f < feat + feats; ++f) {
+    for (uint32_t lanes = __ballot_sync(0xffffffffu, f < a.out_dim && spoiled(a, row_tile, f)); lanes; lanes &= lanes - 1) {
+      const int of = __ffs(lanes) - 1, col = __shfl_sync(0xffffffffu, f, of);
+      const uint4* wr = reinterpret_cast<const uint4*>(a.w + col * a.w_stride);
+      for (uint32_t groups = where; groups; groups &= groups - 1) {
+        const int first = row0 + (__ffs(groups) - 1) * kGroup * step, mine = first + (lane & (kGroup - 1)) * step;
+        bool wrong = lane < kGroup && mine < end;
+        if (wrong) {
+          const int64_t at = (int64_t)mine * a.y_stride + col;
+          wrong = !finite(a.y_fp32 ? static_cast<float*>(a.y)[at] : __bfloat162float(static_cast<__nv_bfloat16*>(a.y)[at]));
+        }
+        const uint32_t todo = __ballot_sync(0xffffffffu, wrong);
+        if (todo == 0) continue;
+        float sum[kGroup] = {};
+        for (int k = lane; k < a.in_dim / 8; k += 32) {
+          const uint4 p = __ldg(wr + k);
+          const uint64_t p0 = bf16x2_to_f2(p.x), p1 = bf16x2_to_f2(p.y), p2 = bf16x2_to_f2(p.z), p3 = bf16x2_to_f2(p.w);
+#pragma unroll
+          for (int j = 0; j < kGroup; ++j) {
+            const uint4 q = __ldg(reinterpret_cast<const uint4*>(a.x + min(first + j * step, end - 1) * a.x_stride) + k);
+            float lo, hi;
+            f2_unpack(f2_fma(p0, bf16x2_to_f2(q.x), f2_fma(p1, bf16x2_to_f2(q.y), f2_fma(p2, bf16x2_to_f2(q.z), f2_fma(p3, bf16x2_to_f2(q.w), 0ull)))), lo, hi);
+            sum[j] += lo + hi;
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j) {
+          const int row = min(first + j * step, end - 1), id = a.adapter[row];
+          int own = -1;  // the row's slot
+          for (int i0 = 0; i0 < n && own < 0; i0 += 32) {
+            const uint32_t here = __ballot_sync(0xffffffffu, i0 + lane < n && __ldcg(which + min(i0 + lane, n - 1)) == id);
+            if (here) own = i0 + __ffs(here) - 1;
+          }
+          if (own >= 0) {
+            const __nv_bfloat16* b = a.b + ((int64_t)id * a.out_dim + col) * sl.rank;
+            const char* h = sl.h + ((int64_t)row_tile * sl.most + own) * sl.numbers * sl.block + (int64_t)(row - row_tile * a.nt) * sl.padded * 2;
+            for (int i = lane; i < sl.rank; i += 32) {
+              float value = 0.f;
+              for (int c = 0; c < sl.numbers; ++c) value += __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(h + c * sl.block)[i]);
+              sum[j] = fmaf(__bfloat162float(b[i]), value, sum[j]);
+            }
+          }
+#pragma unroll
+          for (int d = 16; d > 0; d >>= 1) sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], d);
+          if (lane == j && (todo >> j & 1u)) store_y(a, mine, col, sum[j]);
+        }
       }
+    }
   }
 }
 
@@ -348,7 +371,7 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
   uint64_t* drained = acc_empty + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drained + 1);
   uint32_t* gave_up = tmem_slot + 1;  // the CTA has; what a cluster does next goes by those of all its CTAs, so that none leaves alone
-  volatile uint32_t* odd_ones = gave_up + 1;  // a result of a round was no finite number (in shared memory: there is no register to spare)
+  volatile uint32_t* odd_ones = gave_up + 1;  // a result was no finite number (in shared memory: there is no register to spare)
   const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31;
   const int size = a.splits * kCtas;  // of a cluster
   const int group = blockIdx.x / size, groups = gridDim.x / size, rank = blockIdx.x - group * size, part = rank / kCtas, half = rank - part * kCtas;
@@ -700,7 +723,6 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
         }
         if (!ok || rounds) break;  // (joined below, by the whole cluster)
         const int feat = f * kTileFeat + half * kFeat + m;
-        uint32_t unsettled = 0;  // (32 groups of rows at most)
         for (int g = col0; g < col0 + cols && t0 + g < a.rows; g += kGroup) {
           uint32_t r[kGroup];
           tmem_ld8(from + (g - col0), r);
@@ -710,11 +732,10 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
             bool all = true;
 #pragma unroll
             for (int j = 0; j < kGroup; ++j) all = all && finite(__uint_as_float(r[j]));
-            if (!all) unsettled |= 1u << (g - col0) / kGroup;
+            if (!all) *odd_ones = 1;
           }
         }
         if (!kExact) sums_taken();
-        if (kMode == kWith && unsettled) settle_stored(a, row_tile, unsettled, t0 + col0, kGroup, kGroup, feat, 1);
       }
     }
     __syncwarp();
@@ -788,16 +809,24 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
           }
         }
       }
-      if (kMode == kWith && *odd_ones) {  // (a warp has at most 16 of a tile's rows: W x of a round is in two parts at least)
-        const int from = mine + joined * wid;
-        settle_stored(a, row_tile, (1u << (n - from + apart - 1) / apart) - 1u, t0 + from, apart, 1, f * kTileFeat + half * kFeat + lane * 4, 4);
-      }
       __syncwarp();
       cluster_sync_all();  // nobody leaves, or takes new stages to where its part was, while that is read
       fence_proxy_async_smem();  // (before the next round's copies to the ring)
       if (__syncthreads_or((int)stop)) break;
       if (whole) now.f += (a.splits - 1 - part) * f_step;
       advance(now);
+    }
+  }
+  if (kMode == kWith) {
+    __syncwarp();
+    if (__any_sync(0xffffffffu, *odd_ones != 0)) {
+      // (behind everything: a call in the loops above would cost them registers.  A round has one tile, and a warp of it two groups of rows at most: splits are two at least.)
+      const int step = rounds ? a.splits * kWarps : 1;
+      for (Tile t = start(); more(t); advance(t)) {
+        const int t0 = t.r * a.nt, end = min(t0 + a.nt, a.rows), from = t0 + (rounds ? part + a.splits * wid : col0);
+        const int groups = rounds ? 2 : cols / kGroup, feat = t.f * kTileFeat + half * kFeat + (rounds ? lane * 4 : m);
+        if (rounds || wid >= 4) rework(a, t.r, (uint32_t)((1ull << groups) - 1ull), from, step, end, feat, rounds ? 4 : 1);
+      }
     }
   }
   tc_fence_before_sync();
