@@ -852,6 +852,11 @@ __device__ __forceinline__ int adapter_of(const int32_t* __restrict__ adapter, i
   if (id != -1) atomicCAS(status + kStatusReport, 0, (int)GF_ERR_INVALID_ARG);
   return -1;
 }
+// A projection without adapters has none to name: only the report of ids that do.
+__global__ void __launch_bounds__(256) k_adapter_none(const int32_t* __restrict__ adapter, int rows, int32_t* status) {
+  const int64_t row = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (row < rows) adapter_of(adapter, (int)row, 0, status);
+}
 // All threads of a CTA, at least n of them; returns the adapter of row t0 + (thread).
 __device__ int find_slots(SlotBits& sb, const int32_t* __restrict__ adapter, int t0, int n, int num_adapters, int32_t* status) {
   const int tid = threadIdx.x, lane = tid & 31, words = (num_adapters + 31) / 32;
@@ -1236,6 +1241,12 @@ static int launch_pass(const gf_projection_t& p, int rows, const void* x, int64_
 int launch_project(const gf_projection_t& p, int rows, const void* x, int64_t x_stride, const int32_t* adapter, void* y, int64_t y_stride, int y_fp32,
                    void* scratch, int num_sms, int32_t* status, cudaStream_t st) {
   int launched = 0;
+  if (adapter != nullptr && p.num_adapters == 0) {
+    k_adapter_none<<<(unsigned)(((int64_t)rows + 255) / 256), 256, 0, st>>>(adapter, rows, status);
+    if (cudaGetLastError() != cudaSuccess) return -1;
+    ++launched;
+    adapter = nullptr;
+  }
   const int pass = adapter != nullptr && p.num_adapters > 0 ? kPassRows : 1 << 22;
   for (int64_t t = 0; t < rows; t += pass) {
     const int n = launch_pass(p, (int)std::min<int64_t>(pass, rows - t), (const char*)x + t * x_stride * 2, x_stride, adapter ? adapter + t : nullptr,

@@ -283,3 +283,23 @@ def test_weights_are_cleared_where_new_tokens_are():
     with pytest.raises(ValueError):
         pa.clear_slot_weights(weights[:1], _ints(1))
     pa.close()
+
+
+# ---- ids, and nodes that grow under an extend ----------------------------------------------------------------
+
+
+@pytest.mark.parametrize("rows", [1, 300, 700])
+def test_ids_of_a_projection_without_adapters_count_as_none_and_are_reported(rows):
+    from paper_2605_22566_b200 import binding as B
+    from paper_2605_22566_b200.runtime import Projection
+    rng = np.random.default_rng(rows)
+    pa = _pa()
+    x, p = _bf16(rng, rows, 64).cuda(), Projection(_bf16(rng, 40, 64).cuda())
+    want = pa.project(p, x, dtype=torch.float32)
+    for last in (-1, 0, 5, -2, 2 ** 31 - 1):
+        ids = torch.full((rows,), -1, dtype=torch.int32, device="cuda")
+        ids[-1] = last
+        y = torch.full_like(want, 7.0)
+        assert B.gf_adapter_project(pa.g, p.desc, rows, x.data_ptr(), 64, ids.data_ptr(), y.data_ptr(), 40, 1, None, 0, pa.stream) == B.GF_OK
+        assert torch.equal(y, want) and pa.status() == (B.GF_OK if last == -1 else B.GF_ERR_INVALID_ARG) and pa.status() == 0
+    pa.close()
