@@ -82,7 +82,12 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
-_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
+def _current_stream(index: int) -> int:
+    return torch.cuda.current_stream(index).cuda_stream
+
+
+# (building a torch.cuda.Stream object costs as much as a kernel launch)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _current_stream)
 
 
 def _ints(t: torch.Tensor, n: int, index: int) -> bool:
@@ -178,8 +183,7 @@ class PathAttention:
 
     @property
     def stream(self) -> int:
-        # (the raw handle: building a torch.cuda.Stream object costs as much as a kernel launch)
-        return torch._C._cuda_getCurrentRawStream(self.pool.device.index)
+        return _raw_stream(self.pool.device.index)
 
     # ---- inputs -------------------------------------------------------------------------
     def _fill(self, key: int, count: int, out: torch.Tensor, start: int = 0):
