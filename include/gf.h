@@ -183,9 +183,9 @@ gf_status_t gf_node_extent(const gf_wgraph_t* g, int32_t node, int32_t* n_tokens
  * of tokens and a length that lives on the device, where gf_append_slots moves it on and gf_build_path_tables
  * reads it: a decode step is gf_append_slots, gf_build_path_tables (deferred), and per layer gf_node_kv_append and
  * gf_path_attention_decode, with nothing waited for.  Paths name an open node like any other, extend takes it at its
- * present length, and gf_node_kv_read and gf_node_extent take it at its room (rows that it does not hold yet read
- * as zeros).  What needs a length on the host refuses it with GF_ERR_INVALID_ARG until gf_node_kv_close: the
- * writes, gf_node_kv_reserve, residuals and reconstruction over it, eviction. */
+ * present length (and extend with append writes it at that: a prompt's rows, which gf_append_slots has made room for), and gf_node_kv_read and gf_node_extent take it at its room (rows that it does not hold yet read
+ * as zeros).  What needs a length on the host refuses it with GF_ERR_INVALID_ARG until gf_node_kv_close:
+ * gf_node_kv_write, gf_node_kv4_write, gf_node_kv_reserve, residuals and reconstruction over it, eviction. */
 
 /* Opens an unwritten node (GF_ERR_INVALID_ARG for any other) with room for that many tokens, in bf16, holding none.
  * Takes the tiles (first fit) and clears them in every layer.  GF_ERR_CAPACITY when no run of free tiles is long
@@ -484,8 +484,8 @@ gf_status_t gf_path_attention_extend(gf_wgraph_t* g, const gf_tables_t* t, int32
  * gf_path_attention_extend, except that the new segments' K/V do not have to be in the pool: they
  * arrive as k_new_dev / v_new_dev, [num_q_rows, num_kv_heads, head_dim] bf16 in the row order of
  * q_dev (request r's new tokens are rows q_ptr[r]..q_ptr[r+1]), and the same launch writes layer
- * `layer` of every request's new node (the last node of its path, reserved with gf_node_kv_reserve or
- * written before) while the queries attend over the prefix; the new segment is streamed once its
+ * `layer` of every request's new node (the last node of its path, reserved with gf_node_kv_reserve,
+ * written before, or open) while the queries attend over the prefix; the new segment is streamed once its
  * tiles are in the pool.  Afterwards the nodes hold those K/V like after gf_node_kv_write.  Two
  * requests must not name the same new node.  Inputs are read in stream order, never modified. */
 gf_status_t gf_path_attention_extend_append(gf_wgraph_t* g, const gf_tables_t* t, int32_t layer,

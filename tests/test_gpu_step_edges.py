@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import step_digits as D
+from helpers import assert_close
 from kv4_cases import private_workload
 from oracle import attention as OA
 from oracle import eviction as OE
@@ -302,4 +303,49 @@ def test_ids_of_a_projection_without_adapters_count_as_none_and_are_reported(row
         y = torch.full_like(want, 7.0)
         assert B.gf_adapter_project(pa.g, p.desc, rows, x.data_ptr(), 64, ids.data_ptr(), y.data_ptr(), 40, 1, None, 0, pa.stream) == B.GF_OK
         assert torch.equal(y, want) and pa.status() == (B.GF_OK if last == -1 else B.GF_ERR_INVALID_ARG) and pa.status() == 0
+    pa.close()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_extend_with_append_over_open_nodes(d):
+    """Prompts that come into open nodes by the attention launch, at the length that the nodes have by then; zeros behind them, and growth goes on."""
+    from paper_2605_22566_b200 import binding as B
+    rng = np.random.default_rng(d)
+    hq, hkv, layers = 4, 2, 2
+    paths = [[0, 1], [0, 2], [3]]
+    pa = _pa([70, 200, 130, 300], hq, hkv, d, layers, paths)
+    pa.pool.fill_(0xFF)
+    kv = {}
+    for layer in range(layers):
+        k, v = _bf16(rng, 70, hkv, d), _bf16(rng, 70, hkv, d)
+        pa.write_node(0, layer, k.cuda(), v.cuda())
+        kv[layer, 0] = (k.double().numpy(), v.double().numpy())
+    for n, room in ((1, 200), (2, 130), (3, 300)):
+        pa.open_node(n, room)
+    lens = [65, 1, 129]
+    pa.append_slots(_ints(1, 2, 3), _ints(*lens), sum(lens))
+    pa.build(mode=B.GF_MODE_EXTEND)
+    begin = np.concatenate([[0], np.cumsum(lens)])
+    for layer in range(layers):
+        q, k, v = _bf16(rng, sum(lens), hq, d), _bf16(rng, sum(lens), hkv, d), _bf16(rng, sum(lens), hkv, d)
+        out = pa.extend_append(layer, q.cuda(), k.cuda(), v.cuda())
+        for i, n in enumerate((1, 2, 3)):
+            kv[layer, n] = tuple(t[begin[i]:begin[i + 1]].double().numpy() for t in (k, v))
+        ref, _ = OA.extend(paths, lambda n: kv[layer, n], q.double().numpy(), hkv)
+        assert_close(out.double().cpu().numpy(), ref, f"layer {layer}")
+        assert torch.equal(pa.extend(layer, q.cuda()), out)               # (as over written nodes)
+    slots, now = pa.append_slots(_ints(2, 1, 3), _ints(3, 0, 1), 4)
+    assert now.tolist() == [4, 65, 130]
+    k, v = _bf16(rng, 4, hkv, d), _bf16(rng, 4, hkv, d)
+    for layer in range(layers):
+        pa.append(layer, slots, k.cuda(), v.cuda())
+        for n, rows in ((2, slice(0, 3)), (3, slice(3, 4))):
+            kv[layer, n] = tuple(np.concatenate([a, b[rows].double().numpy()]) for a, b in zip(kv[layer, n], (k, v)))
+        for n in (1, 2, 3):
+            for got, want in zip(pa.load_node(n, layer), kv[layer, n]):
+                got = got.double().cpu().numpy()
+                assert np.array_equal(got[:len(want)], want) and not got[len(want):].any()
+    one = torch.zeros(64, hkv, d, dtype=torch.bfloat16, device="cuda")
+    assert B.gf_node_kv4_write(pa.g, 1, 0, one.data_ptr(), one.data_ptr(), 64, pa.stream) == B.GF_ERR_INVALID_ARG
+    assert pa.status() == 0
     pa.close()
