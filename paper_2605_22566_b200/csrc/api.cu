@@ -586,7 +586,7 @@ gf_status_t gf_node_kv_open(gf_wgraph_t* g, int32_t node, int32_t room, void* st
   g->node_off[node] = (int32_t)(first * kTile);
   g->node_open[node] = 1;
   g->generation++;
-  const int n = launch_clear_extent(g->pool, g->desc.num_layers, g->desc.num_kv_heads, (int)first, (int)tiles, st);
+  const int n = launch_clear_extent(g->pool, g->desc.num_layers, g->desc.num_kv_heads, (int)first, (int)tiles, g->status_dev, st);
   const int m = launch_graph_set_node(g->gd, node, 0, g->node_off[node], st, room);
   if (n < 0 || m < 0) return GF_ERR_CUDA;
   g->launches += n + m;

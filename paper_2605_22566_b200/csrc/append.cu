@@ -25,7 +25,8 @@ __device__ __forceinline__ char* chunk_at(const PoolGeom& pool, int layer, int h
 
 // Zeros in the rows [from, to) of the pool, (layer, head) pairs first .. last, by all threads of the CTA (256): 2 * chunks neighbouring
 // threads a row.
-__device__ void clear_rows(const PoolGeom& pool, int heads, int chunks, int from, int to, int first, int last) {
+__device__ void clear_rows(const PoolGeom& pool, int heads, int chunks, int from, int to, int first, int last, int32_t* status) {
+  if (!GF_CHECK(from >= 0 && (from >= to || (uint32_t)((to - 1) / kTile) < pool.cap_tiles), status, 501)) return;
   const int per_row = 2 * chunks, c = threadIdx.x % per_row, value = c >= chunks;
   for (int j = first + threadIdx.x / per_row; j < last; j += 256 / per_row) {
     const int layer = j / heads, head = j - layer * heads;
@@ -99,7 +100,7 @@ __global__ void __launch_bounds__(kSlotThreads) k_append_slots(GraphDev g, PoolG
       else if ((long long)h + c > room) why = GF_ERR_CAPACITY;
       if (why != GF_OK) atomicCAS(status + kStatusReport, 0, why);
     }
-    const bool ok = mine && why == GF_OK;
+    const bool ok = mine && why == GF_OK && GF_CHECK(g.node_off[v] >= 0 && (int64_t)g.node_off[v] + room <= (int64_t)pool.cap_tiles * kTile, status, 502);
     if (ok) g.node_len[v] = h + c;
     if (mine && lens != nullptr) lens[r] = ok ? h + c : -1;
     const int off = ok ? g.node_off[v] : 0;
@@ -114,12 +115,13 @@ __global__ void __launch_bounds__(kSlotThreads) k_append_slots(GraphDev g, PoolG
   __syncthreads();
   for (int t = s_begin[0] + tid, i = 0; t < s_begin[per]; t += kSlotThreads) {
     while (t >= s_begin[i + 1]) ++i;
+    if (!GF_CHECK(t >= 0 && t < num_new && i < per, status, 503)) break;
     slots[t] = s_slot[i] < 0 ? -1 : s_slot[i] + (t - s_begin[i]);
   }
   if (r0 + per >= num_requests)  // rows behind the last request's
     for (int t = s_begin[per] + tid; t < num_new; t += kSlotThreads) slots[t] = -1;
   for (int i = 0; i < per; ++i)
-    if (s_to[i] > s_from[i]) clear_rows(pool, heads, chunks, s_from[i], s_to[i], 0, layers * heads);
+    if (s_to[i] > s_from[i]) clear_rows(pool, heads, chunks, s_from[i], s_to[i], 0, layers * heads, status);
 }
 
 // One layer's new rows from the caller's layout to their slots: 16 bytes of K and of V per step of a thread, a few tokens per
@@ -147,7 +149,8 @@ __global__ void __launch_bounds__(256) k_kv_append(PoolGeom pool, int layer, int
 }
 
 // Zeros in a whole extent, every layer and head.
-__global__ void __launch_bounds__(256) k_clear_extent(PoolGeom pool, int rows, int tile0, int tiles) {
+__global__ void __launch_bounds__(256) k_clear_extent(PoolGeom pool, int rows, int tile0, int tiles, int32_t* status) {
+  if (!GF_CHECK(tile0 >= 0 && (uint32_t)(tile0 + tiles) <= pool.cap_tiles, status, 504)) return;
   const uint64_t n = (uint64_t)tiles * (pool.tile_bytes / 16);
   for (int j = blockIdx.y; j < rows; j += gridDim.y) {
     uint4* p = reinterpret_cast<uint4*>(pool.base + (uint64_t)j * pool.head_stride + (uint64_t)tile0 * pool.tile_bytes);
@@ -156,9 +159,9 @@ __global__ void __launch_bounds__(256) k_clear_extent(PoolGeom pool, int rows, i
 }
 
 // The end of a node's growth: zeros in what is left of its last tile, a CTA per layer, then its length.
-__global__ void __launch_bounds__(256) k_clear_tail(GraphDev g, PoolGeom pool, int heads, int chunks, int node, int n_tokens) {
+__global__ void __launch_bounds__(256) k_clear_tail(GraphDev g, PoolGeom pool, int heads, int chunks, int node, int n_tokens, int32_t* status) {
   const int off = g.node_off[node], end = min(g.node_len[node], (n_tokens + kTile - 1) / kTile * kTile);
-  clear_rows(pool, heads, chunks, off + n_tokens, off + end, blockIdx.x * heads, (blockIdx.x + 1) * heads);
+  clear_rows(pool, heads, chunks, off + n_tokens, off + end, blockIdx.x * heads, (blockIdx.x + 1) * heads, status);
 }
 __global__ void k_close_node(GraphDev g, int node, int n_tokens, int32_t* status) {
   if (g.node_len[node] < n_tokens) atomicCAS(status + kStatusReport, 0, (int)GF_ERR_INVALID_ARG);
@@ -188,16 +191,16 @@ int launch_kv_append(const PoolGeom& pool, int layer, int heads, int head_dim, i
   return cudaGetLastError() == cudaSuccess ? 1 : -1;
 }
 
-int launch_clear_extent(const PoolGeom& pool, int layers, int heads, int tile0, int tiles, cudaStream_t st) {
+int launch_clear_extent(const PoolGeom& pool, int layers, int heads, int tile0, int tiles, int32_t* status, cudaStream_t st) {
   if (tiles <= 0) return 0;
   const long long rows = (long long)layers * heads, blocks = (long long)tiles * (pool.tile_bytes / 16) / 1024;
-  k_clear_extent<<<dim3((unsigned)(blocks < 64 ? blocks : 64), (unsigned)(rows < 65535 ? rows : 65535)), 256, 0, st>>>(pool, (int)rows, tile0, tiles);
+  k_clear_extent<<<dim3((unsigned)(blocks < 64 ? blocks : 64), (unsigned)(rows < 65535 ? rows : 65535)), 256, 0, st>>>(pool, (int)rows, tile0, tiles, status);
   return cudaGetLastError() == cudaSuccess ? 1 : -1;
 }
 
 int launch_close_node(const GraphDev& g, const PoolGeom& pool, int layers, int heads, int head_dim, int node, int n_tokens, int32_t* status,
                       cudaStream_t st) {
-  k_clear_tail<<<layers, 256, 0, st>>>(g, pool, heads, head_dim / 8, node, n_tokens);
+  k_clear_tail<<<layers, 256, 0, st>>>(g, pool, heads, head_dim / 8, node, n_tokens, status);
   if (cudaGetLastError() != cudaSuccess) return -1;
   k_close_node<<<1, 1, 0, st>>>(g, node, n_tokens, status);
   return cudaGetLastError() == cudaSuccess ? 2 : -1;

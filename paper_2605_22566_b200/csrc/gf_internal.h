@@ -280,7 +280,7 @@ int launch_append_slots(const GraphDev& g, const PoolGeom& pool, int layers, int
                         cudaStream_t st);
 int launch_kv_append(const PoolGeom& pool, int layer, int heads, int head_dim, int num_new, const int32_t* slots, const void* k,
                      int64_t k_stride, const void* v, int64_t v_stride, int num_sms, int32_t* status, cudaStream_t st);
-int launch_clear_extent(const PoolGeom& pool, int layers, int heads, int tile0, int tiles, cudaStream_t st);
+int launch_clear_extent(const PoolGeom& pool, int layers, int heads, int tile0, int tiles, int32_t* status, cudaStream_t st);
 int launch_close_node(const GraphDev& g, const PoolGeom& pool, int layers, int heads, int head_dim, int node, int n_tokens, int32_t* status,
                       cudaStream_t st);
 // set != nullptr: the kernel also records the node's length and pool offset on the device (first write).

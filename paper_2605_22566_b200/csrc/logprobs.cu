@@ -181,7 +181,8 @@ template <> struct Vec<__nv_bfloat16> {
 };
 
 // The k largest of the list's first n keys to its front, in descending order.  All threads; n is theirs alike.
-__device__ void rank(Shared& sm, int n, int k) {
+__device__ void rank(Shared& sm, int n, int k, int32_t* status) {
+  if (!GF_CHECK(n >= 0 && n <= kList && k <= kMaxTop, status, 702)) n = 0;
   for (int i = threadIdx.x; i < n; i += blockDim.x) {
     const Key x = sm.list[i];
     int above = 0;
@@ -196,7 +197,7 @@ __device__ void rank(Shared& sm, int n, int k) {
 }
 
 // Keeps of the list the keys whose value's order is above `order`, then ranks them.
-__device__ void cut_above(Shared& sm, int k, uint32_t order) {
+__device__ void cut_above(Shared& sm, int k, uint32_t order, int32_t* status) {
   constexpr int kOwn = kList / kMinThreads;
   const int n = sm.count;
   if (threadIdx.x == 0) sm.kept = 0;
@@ -209,9 +210,12 @@ __device__ void cut_above(Shared& sm, int k, uint32_t order) {
   __syncthreads();
 #pragma unroll
   for (int j = 0; j < kOwn; ++j)
-    if ((uint32_t)(own[j] >> 32) > order) sm.list[atomicAdd(&sm.kept, 1)] = own[j];
+    if ((uint32_t)(own[j] >> 32) > order) {
+      const int at = atomicAdd(&sm.kept, 1);
+      if (GF_CHECK(at < kList, status, 703)) sm.list[at] = own[j];
+    }
   __syncthreads();
-  rank(sm, sm.kept, k);
+  rank(sm, sm.kept, k, status);
 }
 
 // Publishes the largest order that `enough` lanes of the warp reach with their largest logit so far (it never falls).
@@ -248,7 +252,7 @@ __device__ __forceinline__ float common_level(Shared& sm, int nth, int warps) {
 }
 
 // Cuts the list to its k largest keys, in descending order, and raises the threshold to the k-th.  All threads.
-__device__ void cut(Shared& sm, int k, Key& least) {
+__device__ void cut(Shared& sm, int k, Key& least, int32_t* status) {
   const int tid = threadIdx.x, lane = tid & 31, warps = blockDim.x >> 5;
   int n = min(sm.count, kList);
   __syncthreads();
@@ -285,12 +289,12 @@ __device__ void cut(Shared& sm, int k, Key& least) {
       int at = atomicAdd(&sm.kept, have);
 #pragma unroll
       for (int j = 0; j < kOwn; ++j)
-        if (own[j] >= bound && own[j] != 0) sm.list[at++] = own[j];
+        if (own[j] >= bound && own[j] != 0 && GF_CHECK(at < kList, status, 704)) sm.list[at++] = own[j];
     }
     __syncthreads();
     n = sm.kept;
   }
-  rank(sm, n, k);
+  rank(sm, n, k, status);
   if (n >= k) least = sm.best[k - 1];
   __syncthreads();
 }
@@ -321,7 +325,7 @@ __device__ __forceinline__ float peer_float(const float* p, uint32_t rank) {
 
 // The k largest of a CTA's part from what was listed, to best; how many there are.  All threads.
 template <typename T, typename P>
-__device__ int finish(Shared& sm, int k, float least, const P& p, int loose, int my_loose, int vocab, int warps) {
+__device__ int finish(Shared& sm, int k, float least, const P& p, int loose, int my_loose, int vocab, int warps, int32_t* status) {
   constexpr int kN = Vec<T>::n;
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, threads = blockDim.x;
   const int n = sm.count;
@@ -342,17 +346,17 @@ __device__ int finish(Shared& sm, int k, float least, const P& p, int loose, int
   const int head = p.head, tail = p.tail, v0 = p.v0, v1 = p.v1;
   if (n > kList) {
     Key bound = 0;
-    cut(sm, k, bound);
+    cut(sm, k, bound, status);
     // (what the first pass listed is met again: from an empty list, against a key that k of them reach)
     if (tid == 0) sm.count = 0;
     __syncthreads();
     auto again = [&](bool mine, float v, int64_t index) {
-      if (sm.count > kList - threads) cut(sm, k, bound);
+      if (sm.count > kList - threads) cut(sm, k, bound, status);
       __syncthreads();
       const Key key = mine ? key_of(v, index) : 0;
       if (mine && key >= bound) {
         const int at = atomicAdd(&sm.count, 1);
-        sm.list[at] = key;
+        if (GF_CHECK(at < kList && index >= 0 && index < vocab, status, 705)) sm.list[at] = key;
       }
       __syncthreads();
     };
@@ -364,10 +368,10 @@ __device__ int finish(Shared& sm, int k, float least, const P& p, int loose, int
         const int64_t at = head + (int64_t)(base + tid) * kN + i;
         again(base + tid < v1, base + tid < v1 ? Vec<T>::one(x + at) : 0.f, at);
       }
-    cut(sm, k, bound);
+    cut(sm, k, bound, status);
     return sm.count;
   }
-  cut_above(sm, k, order_of(least));
+  cut_above(sm, k, order_of(least), status);
   // the others: the first ones equal to `least`, and behind them, where nothing is left but NaN, the first of those
   for (int nan = 0; nan < 2 && sm.count < k; ++nan) {
     auto same = [&](float v) { return nan ? v != v : v == least; };
@@ -457,6 +461,7 @@ __global__ void __launch_bounds__(kMaxThreads, 3) k_token_logprobs(const T* __re
   auto bring = [&] {
     if (bring_at >= v1) return;
     const uint32_t bytes = (uint32_t)min(p.len, v1 - bring_at) * 16u;
+    if (!GF_CHECK(bring_at >= 0 && bytes <= kRound * 16u && head + (int64_t)bring_at * kN + bytes / sizeof(T) <= vocab, status, 701)) return;
     uint64_t* full = &sm.full[wid][rounds.started % kStages];
     mbar_arrive_expect_tx(full, bytes);
     bulk_g2s(my_ring + (rounds.started % kStages) * kRound, p.xv + bring_at, bytes, full);
@@ -613,7 +618,7 @@ __global__ void __launch_bounds__(kMaxThreads, 3) k_token_logprobs(const T* __re
       __syncthreads();
     }
     least = value_of(sm.common);
-    have = finish<T>(sm, k, least, p, loose, my_loose, vocab, warps);
+    have = finish<T>(sm, k, least, p, loose, my_loose, vocab, warps, status);
   }
 
   if (wid == 0) {
@@ -661,7 +666,7 @@ __global__ void __launch_bounds__(kMaxThreads, 3) k_token_logprobs(const T* __re
     }
     if (lane < k) {
       const Key key = (parts > 1 ? sm.list : sm.best)[lane];
-      if (top_ids != nullptr) top_ids[row * k + lane] = (int32_t)~(uint32_t)key;
+      if (top_ids != nullptr && GF_CHECK((int32_t)~(uint32_t)key >= 0 && (int32_t)~(uint32_t)key < vocab, status, 706)) top_ids[row * k + lane] = (int32_t)~(uint32_t)key;
       if (top_logprobs != nullptr) top_logprobs[row * k + lane] = of(value_of((uint32_t)(key >> 32)));
     }
   }

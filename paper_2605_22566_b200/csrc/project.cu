@@ -73,6 +73,7 @@ struct ProjectArgs {
   const __nv_bfloat16 *w, *x, *b;
   int64_t w_stride, x_stride;
   const int32_t* adapter;               // [rows] as given
+  int num_adapters;
 };
 
 // kTwo: the CTA is one of two that work on one tile with MMAs of both (cta_group::2), the even one, which issues them, the leader.  Each brings
@@ -384,7 +385,11 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
   const int h_row = sl.padded * 2;                       // bytes of a row of h, and of B's
   const uint32_t b_bytes = kFeat * (uint32_t)h_row, h_bytes = sl.block / kCtas;  // of a slot's B, of a number of its h
   const int per_tile = kMode == kDown ? kFeat / sl.padded : 1;  // slots whose A a tile takes
-  auto slots_of = [&](int row_tile) { return *(volatile int32_t*)(sl.count + row_tile); };
+  auto slots_of = [&](int row_tile) {
+    const int n = *(volatile int32_t*)(sl.count + row_tile);
+    return GF_CHECK(n >= 0 && n <= sl.most && row_tile < a.row_tiles, a.status, 601) ? n : 0;
+  };
+  auto adapter_at = [&](const int32_t* which, int i) { return GF_CLAMP(__ldcg(which + i), a.num_adapters, a.status, 602); };  // of a tile's slot i
   // The tiles of a CTA or cluster: features f of W (or slots, from f * per_tile on) and rows r of x.  Those of A x are only as many as there
   // are slots, so a tile of x is left when they end.
   struct Tile { int index, f, r, slots; };
@@ -495,7 +500,7 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
           if (kMode == kDown) {
             s1 = min(per_tile, t.slots - f * per_tile);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) ids[j] = j < s1 ? __ldcg(which + f * per_tile + j) : 0;
+            for (int j = 0; j < 8; ++j) ids[j] = j < s1 ? adapter_at(which, f * per_tile + j) : 0;
           }
           for (int k = step0; k < step1; ++k) {
             if (!(ok = free())) break;
@@ -521,13 +526,13 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
             }
             s0 = s1 * part / a.splits;
             s1 = s1 * (part + 1) / a.splits;
-            int ahead[2] = {s0 < s1 ? __ldcg(which + s0) : 0, s0 + 1 < s1 ? __ldcg(which + s0 + 1) : 0};  // of the next two slots
+            int ahead[2] = {s0 < s1 ? adapter_at(which, s0) : 0, s0 + 1 < s1 ? adapter_at(which, s0 + 1) : 0};  // of the next two slots
             int y = (row_tile * sl.most + s0) * kNumbers * a.nt + half * (a.nt / kCtas);  // of the next number of h
             for (int i = s0; i < s1 && ok;) {
               const int id = ahead[0], id2 = ahead[1], taken = two_slots && i + 1 < s1 ? 2 : 1;
               i += taken;
-              ahead[0] = taken == 2 ? (i < s1 ? __ldcg(which + i) : 0) : id2;
-              ahead[1] = i + 1 < s1 ? __ldcg(which + i + 1) : 0;
+              ahead[0] = taken == 2 ? (i < s1 ? adapter_at(which, i) : 0) : id2;
+              ahead[1] = i + 1 < s1 ? adapter_at(which, i + 1) : 0;
               for (int j = 0; j < taken * kNumbers;) {
                 if (!(ok = free())) break;
                 char* at = smem + s * stage_bytes;
@@ -803,7 +808,9 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
         for (int i = 0; i < kAtOnce; ++i) {
           const int r = r0 + i * apart;
           if (r < n) {
-            if (kMode == kDown) store_h(sl, place, r, row_slot[i], sum[i]);
+            if (kMode == kDown) {
+              if (GF_CHECK((place.at == nullptr || place.slot < sl.most) && row_slot[i] < sl.most && r < a.nt, a.status, 603)) store_h(sl, place, r, row_slot[i], sum[i]);
+            }
             else store_y4(a, t0 + r, f * kTileFeat + half * kFeat + lane * 4, sum[i]);
             if (kMode == kWith && !(finite(sum[i].x) && finite(sum[i].y) && finite(sum[i].z) && finite(sum[i].w))) *odd_ones = 1;
           }
@@ -884,7 +891,8 @@ __device__ int find_slots(SlotBits& sb, const int32_t* __restrict__ adapter, int
   return id;
 }
 // The same threads write the tile's list.  (Rows of one adapter write the same.)
-__device__ __forceinline__ void write_slots(const SlotBits& sb, const Slots& sl, int tile, int id) {
+__device__ __forceinline__ void write_slots(const SlotBits& sb, const Slots& sl, int tile, int id, int32_t* status) {
+  if (!GF_CHECK(sb.count <= sl.most && sb.slot(id) < sb.count, status, 604)) return;
   if (threadIdx.x == 0) sl.count[tile] = sb.count;
   if (id >= 0) sl.adapter[(int64_t)tile * sl.most + sb.slot(id)] = id;
 }
@@ -894,7 +902,7 @@ __global__ void __launch_bounds__(256) k_adapter_slots(const int32_t* __restrict
   __shared__ SlotBits sb;
   const int t0 = blockIdx.x * nt, n = min(nt, rows - t0);
   const int id = find_slots(sb, adapter, t0, n, num_adapters, status);
-  write_slots(sb, sl, blockIdx.x, id);
+  write_slots(sb, sl, blockIdx.x, id, status);
   if (threadIdx.x < n) sl.of_row[t0 + threadIdx.x] = sb.slot(id);
 }
 
@@ -955,7 +963,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_adapter_rows(const __nv_bflo
     if (lane < kRowRanks) sums[wid][lane] = v[0];
   }
   const int id = find_slots(sb, adapter, t0, min(nt, rows - t0), num_adapters, status);
-  if (t == t0 && r0 == 0) write_slots(sb, sl, tile, id);
+  if (t == t0 && r0 == 0) write_slots(sb, sl, tile, id, status);
   if (which >= 0 && tid < kRowRanks) {
     float sum = 0.f;
 #pragma unroll
@@ -968,6 +976,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) k_adapter_rows(const __nv_bflo
   char* base = sl.h + (int64_t)tile * sl.most * sl.numbers * sl.block;
   for (int i = tid; i < sb.count * pieces; i += kRowThreads) {
     const int c = i % pieces, at = i / pieces;
+    if (!GF_CHECK(at < sl.most && t - t0 < nt && r0 + (c + 1) * 8 <= sl.padded, status, 605)) break;
     float v[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = at == slot ? h[c * 8 + j] : 0.f;
@@ -1199,6 +1208,7 @@ static int launch_pass(const gf_projection_t& p, int rows, const void* x, int64_
   a.w_stride = p.w_stride;
   a.x_stride = x_stride;
   a.adapter = adapter;
+  a.num_adapters = p.num_adapters;
   choose_tiles(a, with ? p.num_adapters : 0, p.rank, num_sms);
   a.y_vec = (y_stride & 3) == 0 && ((uintptr_t)y & (y_fp32 ? 15 : 7)) == 0;
   Maps maps = {};

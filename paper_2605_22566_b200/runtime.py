@@ -3,6 +3,7 @@ uploads a workload's wGraph, node KV and paths, and forwards to the library.  No
 table arithmetic lives here; PyTorch only supplies memory and streams."""
 from __future__ import annotations
 
+import os
 import weakref
 from typing import NamedTuple, Optional
 
@@ -154,6 +155,14 @@ class PathAttention:
         raw[lo + nbytes:lo + nbytes + GUARD_BYTES].fill_(GUARD_VALUE)
         self._guards.append((name, raw, lo, nbytes))
         return raw[lo:lo + nbytes]
+
+    # True: the results and scratch of append_slots, project and token_logprobs are guarded too, and kept until the handle is closed (for tests: GF_GUARD_OUTPUTS=1, or set
+    # on a handle)
+    guard_outputs = os.environ.get("GF_GUARD_OUTPUTS") == "1"
+
+    def _guarded_new(self, shape: tuple, dtype: torch.dtype, name: str) -> torch.Tensor:
+        n = int(np.prod(shape, dtype=np.int64))
+        return self.guarded(n * torch.empty((), dtype=dtype).element_size(), name).view(dtype).view(shape)
 
     def guarded_like(self, t: torch.Tensor, name: str) -> torch.Tensor:
         return self.guarded(t.numel() * t.element_size(), name).view(t.dtype).view(t.shape)
@@ -355,6 +364,8 @@ class PathAttention:
         if num_new < 0:
             raise ValueError("num_new: at least 0")
         slots, lens = nodes.new_empty(num_new), torch.empty_like(nodes)
+        if self.guard_outputs:
+            slots, lens = self._guarded_new((num_new,), torch.int32, "slots"), self._guarded_new((n,), torch.int32, "lengths")
         st = self._lib.gf_append_slots(self.g, n, nodes.data_ptr(), None if held is None else held.data_ptr(), counts.data_ptr(), num_new,
                                        slots.data_ptr(), lens.data_ptr(), _raw_stream(ix))
         if st:
@@ -393,6 +404,8 @@ class PathAttention:
             if dtype not in (torch.bfloat16, torch.float32):
                 raise ValueError("dtype: bf16 or fp32")
             out = x.new_empty(rows, p.out_dim) if dtype is torch.bfloat16 else x.new_empty(rows, p.out_dim, dtype=dtype)
+            if self.guard_outputs:
+                out = self._guarded_new((rows, p.out_dim), dtype, "projection")
             ys = p.out_dim
         else:
             dtype = out.dtype
@@ -404,7 +417,7 @@ class PathAttention:
         scratch, nbytes = None, 0
         if adapters is not None:
             nbytes = p.scratch_bytes(rows)
-            scratch = adapters.new_empty(nbytes + 3 >> 2)
+            scratch = self.guarded(nbytes, "projection scratch") if self.guard_outputs else adapters.new_empty(nbytes + 3 >> 2)
         st = self._lib.gf_adapter_project(self.g, p.desc, rows, x.data_ptr(), xs[0] if rows > 1 else p.in_dim,
                                           None if adapters is None else adapters.data_ptr(), out.data_ptr(), ys, dtype is torch.float32,
                                           None if scratch is None else scratch.data_ptr(), nbytes, _raw_stream(ix))
@@ -425,8 +438,11 @@ class PathAttention:
         if not 0 <= top <= min(B.GF_MAX_TOP, vocab):
             raise ValueError(f"top: 0 to {min(B.GF_MAX_TOP, vocab)}")
         stats = logits.new_empty(3, rows, dtype=torch.float32)
-        at = stats.data_ptr()
         top_ids, top_logprobs = logits.new_empty(rows, top, dtype=torch.int32), stats.new_empty(rows, top)
+        if self.guard_outputs:
+            stats = self._guarded_new((3, rows), torch.float32, "token statistics")
+            top_ids, top_logprobs = self._guarded_new((rows, top), torch.int32, "top ids"), self._guarded_new((rows, top), torch.float32, "top log probabilities")
+        at = stats.data_ptr()
         out = B.Logprobs(None if tokens is None else at, at + 4 * rows, at + 8 * rows, top_ids.data_ptr() if top else None,
                          top_logprobs.data_ptr() if top else None)
         st = self._lib.gf_token_logprobs(self.g, rows, vocab, logits.data_ptr(), strides[0] if rows > 1 else vocab, fp32,

@@ -349,3 +349,35 @@ def test_extend_with_append_over_open_nodes(d):
     assert B.gf_node_kv4_write(pa.g, 1, 0, one.data_ptr(), one.data_ptr(), 64, pa.stream) == B.GF_ERR_INVALID_ARG
     assert pa.status() == 0
     pa.close()
+
+
+# ---- what lies beside results ----------------------------------------------------------------------------
+
+
+def test_nothing_is_written_beside_results_and_scratch():
+    """Results and scratch between bands of a pattern, of odd sizes; each band is looked at behind the calls."""
+    from paper_2605_22566_b200.runtime import Projection
+    rng = np.random.default_rng(3)
+    pa = _pa([300] * 40, 2, 2, 64, 2)
+    pa.guard_outputs = True
+    for v in range(40):
+        pa.open_node(v, 300)
+    for n, more in ((1, 1), (7, 30), (40, 299)):
+        slots, _ = pa.append_slots(_ints(*range(n)), torch.full((n,), more, dtype=torch.int32, device="cuda"), n * more + 3, torch.zeros(n, dtype=torch.int32, device="cuda"))
+        rows = _bf16(rng, n * more + 3, 2, 64).cuda()
+        pa.append(1, slots, rows, rows)
+    for rows, k, n, adapters, rank in ((1, 64, 129, 3, 8), (77, 200, 999, 5, 24), (255, 128, 131, 70, 64), (300, 264, 100, 40, 16), (513, 72, 4099, 9, 32), (2100, 64, 257, 300, 8)):
+        p = Projection((_bf16(rng, n, k) * 0.1).cuda(), (_bf16(rng, adapters, rank, k) * 0.1).cuda(), _bf16(rng, adapters, n, rank).cuda())
+        ids = torch.from_numpy(rng.integers(-1, adapters, rows)).to(torch.int32).cuda()
+        x = _bf16(rng, rows, k).cuda()
+        for dtype in (torch.bfloat16, torch.float32):
+            pa.project(p, x, ids, dtype=dtype)
+            pa.project(p, x, None, dtype=dtype)
+    for rows, v, top in ((1, 1, 1), (3, 70001, 32), (149, 999, 7), (2100, 130, 5)):
+        for dtype in (torch.bfloat16, torch.float32):
+            x = torch.from_numpy(rng.standard_normal((rows, v))).to(dtype).cuda()
+            pa.token_logprobs(x, torch.zeros(rows, dtype=torch.int32, device="cuda"), top)
+    assert len(pa._guards) > 60
+    assert pa.status() == 0
+    pa.verify_guards()
+    pa.close()
