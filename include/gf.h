@@ -204,7 +204,7 @@ gf_status_t gf_node_kv_close(gf_wgraph_t* g, int32_t node, int32_t n_tokens, voi
  * or NULL: the nodes' new lengths.  A request whose node is not open, whose held or count is negative, that
  * holds more than its node, or whose rows pass num_new is left out: its slots and length are -1, its node is as it was,
  * and gf_last_status reports GF_ERR_INVALID_ARG; GF_ERR_CAPACITY where the node has no room.  Of requests that name the
- * same node all but the first are left out like that.  Built tables become stale; tables of a captured graph are built anew behind the call by its replay. */
+ * same node all but the first are left out like that.  Requests and new rows: at most 2^30 each.  Built tables become stale; tables of a captured graph are built anew behind the call by its replay. */
 gf_status_t gf_append_slots(gf_wgraph_t* g, int32_t num_requests, const int32_t* node_dev, const int32_t* held_dev,
                             const int32_t* count_dev, int32_t num_new, int32_t* slots_dev, int32_t* len_dev, void* stream);
 
@@ -531,7 +531,8 @@ gf_status_t gf_edge_scores(gf_wgraph_t* g, const gf_scorer_t* model, const float
  *   y[t] = W x[t] + scale[a] B[a] (A[a] x[t]),   a = adapter[t]; -1: no adapter.
  * bf16 row-major, caller-owned, 16-byte aligned; A [num_adapters, rank, in_dim], B [num_adapters, out_dim, rank], contiguous;
  * scale NULL: 1.  in_dim and w_stride (entries between rows of W) are multiples of 8; rank a multiple of 8, at most 64
- * (adapters of a smaller rank are filled up with zeros); num_adapters at most GF_MAX_ADAPTERS, 0: none.  What W, A, B, x or a scale hold of
+ * (adapters of a smaller rank are filled up with zeros); num_adapters at most GF_MAX_ADAPTERS, 0: none.  in_dim is
+ * at most 2^30, out_dim and rows at most 2^31 - 512.  What W, A, B, x or a scale hold of
  * infinities and NaN stays in the results whose formula has it.  (Entries of B that are no finite numbers cost the rows beside theirs time: every result that meets one is
  * worked out apart from the others.) */
 #define GF_MAX_ADAPTERS 32768

@@ -574,6 +574,9 @@ gf_status_t gf_node_kv_read(gf_wgraph_t* g, int32_t node, int32_t layer, void* k
   return GF_OK;
 }
 
+// Sizes whose loops' counters would pass 2^31 are refused.
+static constexpr int32_t kMostRows = 0x7fffffff - 511, kMostNew = 1 << 30;
+
 gf_status_t gf_node_kv_open(gf_wgraph_t* g, int32_t node, int32_t room, void* stream) {
   if (!g || node < 0 || node >= g->desc.num_nodes || room < 0 || g->node_len[node] >= 0) return GF_ERR_INVALID_ARG;
   DeviceGuard dev(g->device);
@@ -612,7 +615,7 @@ gf_status_t gf_node_kv_close(gf_wgraph_t* g, int32_t node, int32_t n_tokens, voi
 
 gf_status_t gf_append_slots(gf_wgraph_t* g, int32_t num_requests, const int32_t* node_dev, const int32_t* held_dev,
                             const int32_t* count_dev, int32_t num_new, int32_t* slots_dev, int32_t* len_dev, void* stream) {
-  if (!g || num_requests < 0 || num_new < 0 || (num_requests > 0 && (!node_dev || !count_dev)) || (num_new > 0 && !slots_dev) ||
+  if (!g || num_requests < 0 || num_requests > kMostNew || num_new < 0 || num_new > kMostNew || (num_requests > 0 && (!node_dev || !count_dev)) || (num_new > 0 && !slots_dev) ||
       (((uintptr_t)node_dev | (uintptr_t)held_dev | (uintptr_t)count_dev | (uintptr_t)slots_dev | (uintptr_t)len_dev) & 3))
     return GF_ERR_INVALID_ARG;
   if (num_requests == 0 && num_new == 0) return GF_OK;
@@ -628,7 +631,7 @@ gf_status_t gf_append_slots(gf_wgraph_t* g, int32_t num_requests, const int32_t*
 
 gf_status_t gf_node_kv_append(gf_wgraph_t* g, int32_t layer, int32_t num_new, const int32_t* slots_dev, const void* k_dev, int64_t k_stride,
                               const void* v_dev, int64_t v_stride, void* stream) {
-  if (!g || layer < 0 || layer >= g->desc.num_layers || num_new < 0 || k_stride < 0 || v_stride < 0 || ((k_stride | v_stride) & 7))
+  if (!g || layer < 0 || layer >= g->desc.num_layers || num_new < 0 || num_new > kMostNew || k_stride < 0 || v_stride < 0 || ((k_stride | v_stride) & 7))
     return GF_ERR_INVALID_ARG;
   if (num_new == 0) return GF_OK;
   if (!slots_dev || !k_dev || !v_dev || ((uintptr_t)slots_dev & 3) || (((uintptr_t)k_dev | (uintptr_t)v_dev) & 15)) return GF_ERR_INVALID_ARG;
@@ -1407,7 +1410,7 @@ gf_status_t gf_edge_scores(gf_wgraph_t* g, const gf_scorer_t* m, const float* x_
 }
 
 static bool projection_ok(const gf_projection_t* p) {
-  if (!p || p->in_dim < 8 || (p->in_dim & 7) || p->out_dim < 1 || !p->w_dev || ((uintptr_t)p->w_dev & 15) || p->w_stride < p->in_dim ||
+  if (!p || p->in_dim < 8 || (p->in_dim & 7) || p->in_dim > kMostNew || p->out_dim < 1 || p->out_dim > kMostRows || !p->w_dev || ((uintptr_t)p->w_dev & 15) || p->w_stride < p->in_dim ||
       (p->w_stride & 7) || p->w_stride > (1ll << 38) || p->num_adapters < 0 || p->num_adapters > GF_MAX_ADAPTERS)
     return false;
   if (p->num_adapters == 0) return true;
@@ -1416,14 +1419,14 @@ static bool projection_ok(const gf_projection_t* p) {
 }
 
 uint64_t gf_adapter_project_scratch_bytes(const gf_projection_t* p, int32_t rows) {
-  if (!projection_ok(p) || rows < 1 || p->num_adapters == 0) return 0;
+  if (!projection_ok(p) || rows < 1 || rows > kMostRows || p->num_adapters == 0) return 0;
   return (uint64_t)project_scratch_bytes(rows, p->rank, p->num_adapters);
 }
 
 gf_status_t gf_adapter_project(gf_wgraph_t* g, const gf_projection_t* p, int32_t rows, const void* x_dev, int64_t x_stride,
                                const int32_t* adapter_dev, void* y_dev, int64_t y_stride, int32_t y_fp32, void* scratch_dev,
                                uint64_t scratch_bytes, void* stream) {
-  if (!g || !projection_ok(p) || rows < 0 || y_fp32 < 0 || y_fp32 > 1 || x_stride < p->in_dim || (x_stride & 7) || x_stride > (1ll << 38) ||
+  if (!g || !projection_ok(p) || rows < 0 || rows > kMostRows || y_fp32 < 0 || y_fp32 > 1 || x_stride < p->in_dim || (x_stride & 7) || x_stride > (1ll << 38) ||
       y_stride < p->out_dim)
     return GF_ERR_INVALID_ARG;
   if (rows == 0) return GF_OK;

@@ -381,3 +381,18 @@ def test_nothing_is_written_beside_results_and_scratch():
     assert pa.status() == 0
     pa.verify_guards()
     pa.close()
+
+
+def test_sizes_next_to_the_end_of_int32_are_refused_before_a_launch():
+    from paper_2605_22566_b200 import binding as B
+    pa = _pa()
+    t = torch.zeros(1 << 12, device="cuda")
+    p, most = t.data_ptr(), 2 ** 31 - 1
+    for n in (2 ** 30 + 1, most):
+        assert B.gf_append_slots(pa.g, n, p, None, p, 1, p, None, pa.stream) == B.gf_append_slots(pa.g, 1, p, None, p, n, p, None, pa.stream) == B.GF_ERR_INVALID_ARG
+        assert B.gf_node_kv_append(pa.g, 0, n, p, p, 1024, p, 1024, pa.stream) == B.GF_ERR_INVALID_ARG
+    for rows, out_dim in ((most, 8), (most - 510, 8), (1, most), (1, most - 510)):
+        desc = B.ProjectionDesc(64, out_dim, p, 64, 0, 0, None, None, None)
+        assert B.gf_adapter_project(pa.g, desc, rows, p, 64, None, p, out_dim, 1, None, 0, pa.stream) == B.GF_ERR_INVALID_ARG
+    assert pa.status() == 0
+    pa.close()

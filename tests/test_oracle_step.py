@@ -57,3 +57,15 @@ def test_refusals_without_a_handle():
                 dict(a_dev=None), dict(b_dev=(1 << 20) + 2), dict(num_adapters=-1), dict(scale_dev=2)):
         q = B.ProjectionDesc(*[bad.get(n, getattr(p, n)) for n, _ in p._fields_])
         assert B.gf_adapter_project_scratch_bytes(q, 4) == 0, bad
+
+
+def test_sizes_next_to_the_end_of_int32_are_refused():
+    from paper_2605_22566_b200 import binding as B
+    p = B.ProjectionDesc(1032, 8, 1 << 20, 1032, 2, 24, 1 << 20, 1 << 20, None)
+    assert B.gf_adapter_project_scratch_bytes(p, 2 ** 31 - 512) > 0
+    assert B.gf_adapter_project_scratch_bytes(p, 2 ** 31 - 511) == B.gf_adapter_project_scratch_bytes(p, 2 ** 31 - 1) == 0
+    for out_dim, ok in ((2 ** 31 - 512, True), (2 ** 31 - 511, False), (2 ** 31 - 1, False)):
+        q = B.ProjectionDesc(*[out_dim if n == "out_dim" else getattr(p, n) for n, _ in p._fields_])
+        assert (B.gf_adapter_project_scratch_bytes(q, 4) > 0) == ok
+    q = B.ProjectionDesc(*[{"in_dim": 2 ** 30 + 8, "w_stride": 2 ** 30 + 8}.get(n, getattr(p, n)) for n, _ in p._fields_])
+    assert B.gf_adapter_project_scratch_bytes(q, 4) == 0
