@@ -204,7 +204,8 @@ gf_status_t gf_node_kv_close(gf_wgraph_t* g, int32_t node, int32_t n_tokens, voi
  * or NULL: the nodes' new lengths.  A request whose node is not open, whose held or count is negative, that
  * holds more than its node, or whose rows pass num_new is left out: its slots and length are -1, its node is as it was,
  * and gf_last_status reports GF_ERR_INVALID_ARG; GF_ERR_CAPACITY where the node has no room.  Of requests that name the
- * same node all but the first are left out like that.  Requests and new rows: at most 2^30 each.  Built tables become stale; tables of a captured graph are built anew behind the call by its replay. */
+ * same node all but the first are left out like that.  Requests and new rows: at most 2^30 each.  Built tables become stale; tables of a captured graph are built anew behind the call by its replay.  The host
+ * does not see a replay: tables that were built outside of the graph are built again by hand behind it. */
 gf_status_t gf_append_slots(gf_wgraph_t* g, int32_t num_requests, const int32_t* node_dev, const int32_t* held_dev,
                             const int32_t* count_dev, int32_t num_new, int32_t* slots_dev, int32_t* len_dev, void* stream);
 
@@ -546,14 +547,19 @@ typedef struct {
   const float* scale_dev; /* fp32 [num_adapters] */
 } gf_projection_t;
 
-/* Scratch of a call with adapters, 16-byte aligned: up to 6 bytes per rank (16, 32 or 64), row and adapter (256 at most), for at most 16 384
- * rows at a time; two calls that may overlap on the GPU each need their own. */
+/* Scratch of a call with adapters, for results of either type, 16-byte aligned: up to 6 bytes per rank (16, 32 or 64), row and adapter (256 at most), for at most 16 384
+ * rows at a time (8192 rows under 256 adapters of rank 64: 805 MB); two calls that may overlap on the GPU each need their own. */
 uint64_t gf_adapter_project_scratch_bytes(const gf_projection_t* p, int32_t rows);
 
 /* x_dev: bf16 [rows, in_dim], rows x_stride entries apart (a multiple of 8), 16-byte aligned.  adapter_dev: int32 [rows], or NULL for
  * none at all; any value outside [-1, num_adapters) counts as -1 and gf_last_status reports GF_ERR_INVALID_ARG.  y_dev: bf16 or
- * (y_fp32 1) fp32 [rows, out_dim], rows y_stride entries apart, not overlapping the inputs.  Sums are fp32 and rounded once; the
- * order of additions is fixed for given sizes and adapters.  GF_ERR_CAPACITY when the scratch is too small.  Asynchronous. */
+ * (y_fp32 1) fp32 [rows, out_dim], rows y_stride entries apart, not overlapping the inputs.  The
+ * order of additions is fixed for given sizes and adapters.  Digits: sums are fp32, but those of the tensor cores are cut off, not rounded, at each
+ * 16 entries of K.  For fp32 results they are taken out every 512 entries and added with rounding: 2 to 5e-7 of the result for any K (its 2-norm;
+ * products of either sign or of one).  For bf16 results they are taken out once, as in any product on tensor cores: 4e-6 at 4096 entries of either sign;
+ * where all products have one sign 1e-4 of the result at 4096 entries and 5e-4 at 32 768, beside 4e-3 that its rounding may take.  h = scale A x, between the two products
+ * of an adapter, is held in 24 bits for fp32 results, and for bf16 ones to 2^-17 of it, which passes the result's rounding only where W x takes all but 2^-9 of the
+ * adapter's part away.  GF_ERR_CAPACITY when the scratch is too small.  Asynchronous. */
 gf_status_t gf_adapter_project(gf_wgraph_t* g, const gf_projection_t* p, int32_t rows, const void* x_dev, int64_t x_stride,
                                const int32_t* adapter_dev, void* y_dev, int64_t y_stride, int32_t y_fp32, void* scratch_dev,
                                uint64_t scratch_bytes, void* stream);
@@ -574,7 +580,8 @@ typedef struct {
 /* logits_dev: bf16 or (fp32 1) fp32 [rows, vocab], rows `stride` entries apart, any alignment.  tokens_dev: int32 [rows], -1: no token
  * (logprob 0); any other value outside [0, vocab) gives NaN.  top: 0 .. GF_MAX_TOP, at most vocab.  A logit of minus
  * infinity has no probability; a row of nothing else has lse and every log probability at minus infinity, entropy 0.  A
- * row with a NaN or plus infinity gives NaN for all but the ids (a NaN ranks below everything).  Asynchronous. */
+ * row with a NaN or plus infinity gives NaN for all but the ids (a NaN ranks below everything).  Exponentials are the hardware's (ex2.approx, two units in the last
+ * place), sums and all else fp32.  Asynchronous. */
 gf_status_t gf_token_logprobs(gf_wgraph_t* g, int32_t rows, int32_t vocab, const void* logits_dev, int64_t stride, int32_t fp32,
                               const int32_t* tokens_dev, int32_t top, const gf_logprobs_t* out, void* stream);
 

@@ -37,9 +37,9 @@ __device__ void clear_rows(const PoolGeom& pool, int heads, int chunks, int from
 
 // A CTA has `per` requests, one where multiprocessors are left (what taken-back tokens leave to clear is much: 131 KB a token of 32 layers with 8
 // heads): it adds up the counts of those before them and looks for its nodes among theirs (each CTA by itself: 8 bytes a request from L2, against
-// a launch or a chain of CTAs), one warp checks its requests and sets their lengths, and all threads write the slots.
+// a launch or a chain of CTAs; so the work grows with the square of the requests: 4096 take 11.5 us, 16 384 64, 65 536 600), one warp checks its requests and sets their lengths, and all threads write the slots.
 // Latency-bound: a chain of four dependent loads; with the rows' copy 3.9 us for one request, 4.6 for 256.  256 requests that take back 4 tokens of
-// 32 layers: 29 us (134 MB of zeros).
+// 32 layers: 29 us (134 MB of zeros); one request's are one CTA's, 2.1 us a token: 1024 of 32 layers 2.1 ms.
 __global__ void __launch_bounds__(kSlotThreads) k_append_slots(GraphDev g, PoolGeom pool, int layers, int heads, int chunks, int num_requests, int per,
                                                                const int32_t* __restrict__ node, const int32_t* __restrict__ held,
                                                                const int32_t* __restrict__ count, int num_new, int32_t* __restrict__ slots,
@@ -125,7 +125,8 @@ __global__ void __launch_bounds__(kSlotThreads) k_append_slots(GraphDev g, PoolG
 }
 
 // One layer's new rows from the caller's layout to their slots: 16 bytes of K and of V per step of a thread, a few tokens per
-// CTA.  Bound: HBM; 15 800 tokens of 8 heads of 128 entries: 20 us, 6.4 TB/s there and back.
+// CTA.  15 800 tokens of 8 heads of 128 entries: 20 us, 130 MB asked for, there and back, at 6.4 TB/s; L2 takes in most of what is written (counters: 65 MB read and 16 of
+// 65 written by the kernel's end, DRAM at 49 %), so what bounds it is loads on the way, not HBM alone.
 __global__ void __launch_bounds__(256) k_kv_append(PoolGeom pool, int layer, int heads, int chunk_bits, int num_new, int per_cta,
                                                    const int32_t* __restrict__ slots, const char* __restrict__ k, int64_t k_stride,
                                                    const char* __restrict__ v, int64_t v_stride, int32_t* status) {
@@ -148,7 +149,7 @@ __global__ void __launch_bounds__(256) k_kv_append(PoolGeom pool, int layer, int
   }
 }
 
-// Zeros in a whole extent, every layer and head.
+// Zeros in a whole extent, every layer and head.  With the two words of the node: 1088 tokens of 32 layers of 8 heads of 128 27 us, 8256 156 us (1.08 GB at 6.9 TB/s).
 __global__ void __launch_bounds__(256) k_clear_extent(PoolGeom pool, int rows, int tile0, int tiles, int32_t* status) {
   if (!GF_CHECK(tile0 >= 0 && (uint32_t)(tile0 + tiles) <= pool.cap_tiles, status, 504)) return;
   const uint64_t n = (uint64_t)tiles * (pool.tile_bytes / 16);
@@ -158,7 +159,7 @@ __global__ void __launch_bounds__(256) k_clear_extent(PoolGeom pool, int rows, i
   }
 }
 
-// The end of a node's growth: zeros in what is left of its last tile, a CTA per layer, then its length.
+// The end of a node's growth: zeros in what is left of its last tile, a CTA per layer, then its length: 6 to 8 us, two launches.
 __global__ void __launch_bounds__(256) k_clear_tail(GraphDev g, PoolGeom pool, int heads, int chunks, int node, int n_tokens, int32_t* status) {
   const int off = g.node_off[node], end = min(g.node_len[node], (n_tokens + kTile - 1) / kTile * kTile);
   clear_rows(pool, heads, chunks, off + n_tokens, off + end, blockIdx.x * heads, (blockIdx.x + 1) * heads, status);

@@ -15,13 +15,13 @@
 // not, the others are the first ones equal to t, and are looked for from the row's start.  More than the list holds (a row
 // that rises from end to end): a second pass in steps that it cannot overrun, cut to k in between.
 //
-// A warp brings its own pieces of the row to shared memory, two rounds of 2 KB ahead of the one it works on, and waits for no other
-// (two rounds of loads into registers leave room for half the warps, and one ahead left HBM idle in between).
+// A warp brings its own pieces of the row to shared memory, in rounds of 4 KB, one on the way while it works on another, and waits for no other warp
+// (rounds of loads into registers leave room for half the warps).
 //
 // A row is one CTA's, or that of a cluster, whose first CTA joins the parts through shared memory.
 //
 // Measured: 2048 rows of 128 000 bf16 logits 100.5 us, 5.2 TB/s, 64 % of the issue slots (5 instructions an entry, exponentials at half the
-// special-function unit's rate) and HBM at 80 % of a copy's; 256 rows 21 us, two rows on most multiprocessors and 44 % of the slots; one row 8.0 us, latency.
+// special-function unit's rate; ex2.approx, two units in the last place) and HBM at 80 % of a copy's; 256 rows 21 us, two rows on most multiprocessors and 44 % of the slots; one row 8.0 us, latency.
 #include <algorithm>
 
 #include "tc_device.cuh"

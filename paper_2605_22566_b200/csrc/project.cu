@@ -9,14 +9,17 @@
 // The adapters are more entries of K.  For every adapter that rows of a tile of x name (a slot of the tile), h = scale_a A_a x is a
 // [rows, rank] operand with zeros in the other rows, and B_a, [features, rank], stands beside W: the sums go on over the tile's
 // slots, in the same pipeline, and nothing is left for the warps that take them out of tensor memory.  h is held in two bf16
-// numbers, its nearest and the nearest of what is left (off by 2^-17 of it), and multiplied twice; for results in fp32 in three (2^-25).
+// numbers, its nearest and the nearest of what is left (off by 2^-17 of it at most: less than a result's rounding unless W x nearly takes the adapter's part away), and
+// multiplied twice; for results in fp32 in three (2^-26), the least first and into an empty accumulator.
 // A x goes the same way as W x: the rows of the A of 8, 4 or 2 slots (of rank 16, 32, 64) stand in W's place, for all rows of the tile, and
 // what comes out is kept where row and slot belong together and written as those operands.
 // Three launches: the slots, A x, W x; only the copies behind a tile's last entry of W wait for the second.  (Few rows: the first two are
 // one, k_adapter_rows.)
 //
-// Results in fp32: tensor memory's sums are cut off, not rounded, where an MMA adds to them, 1.8e-8 of the sum each time (measured: 4.4e-6 after
-// 256), so every 8 stages they are taken out and added, rounded, to sums that stand beside them; 5e-7 is left.  (Those sums in registers spilled.)
+// Results in fp32: tensor memory's sums are cut off, not rounded, where an MMA adds to them, each of its products at some 2^-24 of the sum (measured, K = 4096: 4.4e-6 of the
+// result with products of either sign, 1e-4 with products of one; 32 768: 5e-4), so every 8 stages they are taken out and added, rounded, to sums that stand beside
+// them; 2.4e-7 (one sign) to 5e-7 is left at any K.  (Those sums in registers spilled.)  Results in bf16 take them out once: a take-out in between stops the MMAs
+// (8192 rows 380 us in place of 275), for digits that their rounding, 4e-3, takes away.
 //
 // Measured, 4096 -> 6144 in bf16: one row 11.4 us, where W alone is 7.8 of HBM (launch, the first copies and the join of 6 parts are the rest); 256 rows 20.1,
 // with 64 adapters of rank 16 37 (their stages are half as many as W's, in 96 CTAs: clusters of 6 do not all find room); 8192 rows 275 us, 1500

@@ -63,7 +63,7 @@ def cancelling(x, b):
 # Three bf16 numbers hold 24 bits: these h exactly.  What is left is the additions of the three products, 16 ranks at a time (64 ranks: 12 additions), and two more that join them
 # to the rest, each cut off by at most 2^-23.
 THREE = 14 * 2.0 ** -23
-# Two: half a step of the second, which is at most 2^-9 of the value, and 10 additions.
+# Two: half a step of the second, which is below 2^-9 of these values, and 10 additions.
 TWO = 2.0 ** -18 + 10 * 2.0 ** -23
 
 
