@@ -731,17 +731,21 @@ __global__ void __launch_bounds__(kExact == 8 ? kWideThreads : kThreads, kExact 
         }
         if (!ok || rounds) break;  // (joined below, by the whole cluster)
         const int feat = f * kTileFeat + half * kFeat + m;
+        uint64_t nothing = 0ull;  // results times zero, in two halves: NaN where one is no finite number
         for (int g = col0; g < col0 + cols && t0 + g < a.rows; g += kGroup) {
           uint32_t r[kGroup];
           tmem_ld8(from + (g - col0), r);
           tmem_wait_ld();
           if (feat < a.out_dim) store_rows(a, t0 + g, feat, r);
           if (kMode == kWith) {
-            bool all = true;
 #pragma unroll
-            for (int j = 0; j < kGroup; ++j) all = all && finite(__uint_as_float(r[j]));
-            if (!all) *odd_ones = 1;
+            for (int j = 0; j < kGroup; j += 2) nothing = f2_fma(f2_pack(__uint_as_float(r[j]), __uint_as_float(r[j + 1])), 0ull, nothing);
           }
+        }
+        if (kMode == kWith) {
+          float lo, hi;
+          f2_unpack(nothing, lo, hi);
+          if (!(lo + hi == 0.f)) *odd_ones = 1;
         }
         if (!kExact) sums_taken();
       }
