@@ -199,7 +199,8 @@ gf_status_t gf_node_kv_close(gf_wgraph_t* g, int32_t node, int32_t n_tokens, voi
 
 /* Where a batch's new tokens go.  Request r gets count_dev[r] tokens in the open node node_dev[r], behind the
  * held_dev[r] that it holds (held_dev NULL: behind all that it holds; fewer than it holds takes the others back, as
- * after drafted tokens that were not accepted: their rows are cleared in every layer).  New rows are request-major:
+ * after drafted tokens that were not accepted: their rows are cleared in every layer, but for those
+ * that the new tokens take, which hold the old ones until gf_node_kv_append writes them).  New rows are request-major:
  * slots_dev[i], [num_new], is the pool's token slot of row i, -1 for rows behind the last request's.  len_dev [num_requests],
  * or NULL: the nodes' new lengths.  A request whose node is not open, whose held or count is negative, that
  * holds more than its node, or whose rows pass num_new is left out: its slots and length are -1, its node is as it was,
